@@ -376,6 +376,140 @@ psa_status_t psa_attn_task(int32_t task, const void *q, const void *k, const voi
                            int32_t head_dim, float sm_scale, float *out, float *m_out, float *l_out, void *cuda_stream);
 
 /*
+ * Page tables and slot maps on the device, from request lengths.  psa_append_kv_alloc grows every sample by one token;
+ * these two serve any number of new tokens per sample -- a batch of samples that is admitted or resumed, several tokens
+ * at once, or one -- and say where each of them goes, so that the lengths never have to reach the host.
+ *
+ * psa_build_page_table lays out the lists of num_samples samples from scratch:
+ *   seq_lens      [B] int32 device: tokens of sample s that are to be stored (>= 0).
+ *   reserve_lens  [B] int32 device or NULL (= seq_lens): tokens its list must have room for, >= seq_lens[s].
+ *   page_indptr   [B+1] int32 device, out: running sums of ceil(reserve / 16).
+ *   page_indices  [num_entries] int32 device, out: the first ceil(seq / 16) entries of a list get pages, all others -1.
+ * psa_extend_page_table adds tokens to lists that exist (as for psa_append_kv_alloc: entries 0 .. ceil(held / 16) - 1 hold pages):
+ *   held_lens     [B] int32 device: tokens sample s holds;  new_lens [B] int32 device: tokens it gets (>= 0).
+ *   max_lens      [B] int32 device or NULL: a sample may not grow beyond this (the planned bounds, for instance).
+ *   page_indptr   [B+1] int32 device, in;  page_indices [num_entries] int32 device, in/out: entries ceil(held / 16) ..
+ *                 ceil((held + new) / 16) - 1 receive pages, the others stay as they are.
+ * Both:
+ *   free_pages, free_count  as for psa_append_kv_alloc; the new height goes to *free_count_out, which may be free_count.
+ *                 In sample order, list entry by list entry, pages are taken from the top of the stack.
+ *   token_indptr  [B+1] int32 device, out: running sums of the new tokens, the offsets of a packed batch [tokens, ...].
+ *   slot_map      [max_tokens] int64 device, out: slot (page * 16 + position in the page) of every packed token; -1 behind
+ *                 the last one, so that a batch padded to max_tokens can be stored whole.
+ *   lens_out      [B] int32 device or NULL, out: tokens sample s holds afterwards; may be seq_lens / held_lens / new_lens.
+ *   status        int32 device or NULL: receives PSA_ERR_BOUNDS (see psa_read_status); the first word of a plan's workspace is such
+ *                 a word, psa_check_status then reports it.
+ *   scratch       device, 8-byte aligned, psa_page_table_scratch_bytes(B) bytes, overwritten by every call (calls that share it
+ *                 must be ordered on one stream).
+ * A sample is refused -- no page, -1 for all its slots, its length unchanged (0 when built from scratch), its list untouched,
+ * status PSA_ERR_BOUNDS -- when a length is negative, exceeds reserve_lens / max_lens or its list, when a page that it should hold
+ * already is missing (a negative id), when its tokens or list entries do not fit max_tokens / num_entries (offsets are then cut
+ * there), or when the stack has too few pages left; in that last case no later sample that needs a page gets one either.
+ * At most 2^20 samples.  One launch for small batches, two otherwise; only enqueues work.
+ */
+size_t psa_page_table_scratch_bytes(int32_t num_samples);
+psa_status_t psa_build_page_table(const int32_t *seq_lens, const int32_t *reserve_lens, int32_t num_samples, const int32_t *free_pages,
+                                  const int32_t *free_count, int32_t *free_count_out, int32_t *page_indptr, int32_t *page_indices,
+                                  int64_t num_entries, int32_t *token_indptr, int64_t *slot_map, int64_t max_tokens,
+                                  int32_t *lens_out, int32_t *status, void *scratch, size_t scratch_bytes, void *cuda_stream);
+psa_status_t psa_extend_page_table(const int32_t *held_lens, const int32_t *new_lens, const int32_t *max_lens, int32_t num_samples,
+                                   const int32_t *free_pages, const int32_t *free_count, int32_t *free_count_out,
+                                   const int32_t *page_indptr, int32_t *page_indices, int64_t num_entries, int32_t *token_indptr,
+                                   int64_t *slot_map, int64_t max_tokens, int32_t *lens_out, int32_t *status, void *scratch,
+                                   size_t scratch_bytes, void *cuda_stream);
+
+/* Synchronise `cuda_stream`, return the status word at `status` (device) and clear it. */
+psa_status_t psa_read_status(int32_t *status, void *cuda_stream);
+
+/*
+ * A suffix cache held in 4 bits: 5 bits per element with its parameters, 3.2 times less memory and traffic than bf16.  Every group
+ * of 32 consecutive channels of a token's K (or V) row has a scale s and an offset b, both bf16:
+ *     b = min,   s = bf16((max - min) / 15),   code = rint((x - b) / s) in 0 .. 15 (0 when s = 0),   value = s * code + b
+ * (differences, quotients and rounding in IEEE fp32, ties to even).  A group whose range is not finite reads back as NaN.
+ * A CELL holds the 16 tokens of one page for one KV head, K and V, in psa_kv4_cell_bytes(D) = 20 * D bytes:
+ *     [0, 8 D)      K codes: the 16-byte chunk of (token t, group g) is chunk t * (D / 32) + (g ^ z), z = (t / 2) % 4 for D = 128,
+ *                   (t / 4) % 2 for D = 64; byte i of it holds channel 32 g + 2 i (low nibble) and 32 g + 2 i + 1 (high nibble)
+ *     [8 D, 16 D)   V codes, the same
+ *     [16 D, 20 D)  parameters.  D = 128: for K, then for V, 16 tokens x {s of groups 0-3, b of groups 0-3};
+ *                   D = 64: 16 tokens x {K: s0 s1 b0 b1, V: s0 s1 b0 b1}
+ * and the pool is an array of cells: (page, KV head) at page * pool_strides[0] + head * pool_strides[1] BYTES (multiples of 16).
+ *
+ * psa_store_kv4 quantises token t of new_k / new_v (bf16, element (t, head, d) at t*kv_strides[0] + head*kv_strides[1] + d) into
+ * slot_map[t] (page * 16 + position, as the page tables above give them); a negative slot is skipped, one beyond num_pool_pages is
+ * skipped and raises PSA_ERR_BOUNDS in *status (device, may be NULL).  The slots of one call must be distinct.
+ * psa_load_kv4 reads the tokens of slot_map back into bf16 rows (s * code + b in fp32, rounded once), for instance to make a
+ * finished sample part of a shared prefix; rows of skipped slots are left as they were.
+ * D in {64, 128}; K, V and the pool 16-byte aligned, kv_strides multiples of 8 elements.  Only enqueue one kernel.
+ */
+size_t psa_kv4_cell_bytes(int32_t head_dim);
+psa_status_t psa_store_kv4(const void *new_k, const void *new_v, const int64_t kv_strides[2], const int64_t *slot_map, int64_t num_tokens,
+                           int32_t num_kv_heads, int32_t head_dim, void *pool, const int64_t pool_strides[2], int64_t num_pool_pages,
+                           int32_t *status, void *cuda_stream);
+psa_status_t psa_load_kv4(const void *pool, const int64_t pool_strides[2], int64_t num_pool_pages, const int64_t *slot_map,
+                          int64_t num_tokens, int32_t num_kv_heads, int32_t head_dim, void *out_k, void *out_v,
+                          const int64_t kv_strides[2], int32_t *status, void *cuda_stream);
+/*
+ * psa_decode / psa_decode_suffix with the samples' own tokens in such a pool (the shared prefix stays bf16).  Any plan serves
+ * either cache; every other argument is that of psa_decode.  K and V enter the products as their exact codes; probabilities are
+ * rounded to bf16 as in psa_decode.
+ */
+psa_status_t psa_decode_kv4(const psa_plan_t *plan, const void *q, const void *prefix_k, const void *prefix_v,
+                            const int64_t prefix_strides[2], const void *kv4_pool, const int64_t pool_strides[2],
+                            const int32_t *page_indptr, const int32_t *page_indices, const int32_t *suffix_lens,
+                            void *out, float *lse, void *workspace, size_t workspace_bytes, void *cuda_stream);
+psa_status_t psa_decode_suffix_kv4(const psa_plan_t *plan, const void *q, const void *kv4_pool, const int64_t pool_strides[2],
+                                   const int32_t *page_indptr, const int32_t *page_indices, const int32_t *suffix_lens,
+                                   void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * Rules on logits before a token is drawn: what the samples of one prompt must not repeat, may prefer, and are allowed to say.  For
+ * logit x of token i in row r, c = how often i stands among the row's generated tokens:
+ *     x <- x > 0 ? x / repetition[r] : x * repetition[r]      if c > 0 or i is in the row's prompt set
+ *     x <- x - frequency[r] * c - presence[r] * [c > 0]
+ *     x <- x + (the row's biases for i, added in list order)
+ *     x <- -inf                                               if the row's mask has bit i clear
+ * in fp32, rounded once to the output type.  Every pointer is device memory and may be NULL, which leaves that rule out:
+ *   repetition, frequency, presence  [R] f32 (a repetition that is not > 0 counts as 1)
+ *   history        int32, row r at r*history_stride; the first history_lens[r] (0 .. history_capacity, clamped) entries are the
+ *                  row's generated tokens
+ *   prompt_bits    num_prompt_bitmaps bitmaps of prompt_row_words uint32 each, bit i % 32 of word i / 32 = token i; row r uses bitmap
+ *                  prompt_rows[r], or bitmap r when prompt_rows is NULL (a number outside 0 .. num_prompt_bitmaps-1: none).
+ *                  psa_mark_tokens makes them from token lists.
+ *   bias_indptr    [R+1] int32, bias_ids int32, bias_values f32 of num_biases entries: bias_indptr[r] .. bias_indptr[r+1]-1 (cut to
+ *                  0 .. num_biases) belong to row r
+ *   mask_bits      bitmaps like prompt_bits (set = allowed): num_mask_bitmaps of mask_row_words words; mask_rows as prompt_rows
+ * Token ids outside 0 .. vocab-1 are ignored.  A row whose mask allows nothing becomes -inf throughout.  Types, alignment and strides
+ * as for psa_sample_tokens, for input and output each; out may be logits (same type and stride).  NaN logits stay NaN unless
+ * masked.  Only enqueues one kernel.
+ */
+typedef struct {
+    const float *repetition, *frequency, *presence;
+    const int32_t *history, *history_lens;
+    int64_t history_stride;
+    int32_t history_capacity;
+    const uint32_t *prompt_bits;
+    int64_t prompt_row_words;
+    int32_t num_prompt_bitmaps;
+    const int32_t *prompt_rows;
+    const int32_t *bias_indptr, *bias_ids;
+    const float *bias_values;
+    int32_t num_biases;
+    const uint32_t *mask_bits;
+    int64_t mask_row_words;
+    int32_t num_mask_bitmaps;
+    const int32_t *mask_rows;
+} psa_logits_rules_t;
+psa_status_t psa_process_logits(const void *logits, int32_t logits_dtype, int64_t row_stride, int32_t num_rows, int32_t vocab,
+                                const psa_logits_rules_t *rules, void *out, int32_t out_dtype, int64_t out_row_stride, void *cuda_stream);
+/*
+ * Token sets as bitmaps: bit i of row m (bits + m*row_words, i as above) is set when token i is among ids[indptr[m] .. indptr[m+1])
+ * (int32 device, indptr [num_rows+1], cut to 0 .. num_ids), all others are cleared (the ceil(vocab / 32) words of a row are written whole).  Ids outside 0 .. vocab-1 are ignored.  For the
+ * prompt sets of psa_process_logits and for masks given as lists of allowed tokens.  Only enqueues one kernel.
+ */
+psa_status_t psa_mark_tokens(const int32_t *ids, int32_t num_ids, const int32_t *indptr, int32_t num_rows, int32_t vocab, uint32_t *bits,
+                             int64_t row_words, void *cuda_stream);
+
+/*
  * Self-test of the device-side error path (no counterpart in the paper).  Enqueues one tiny kernel whose only
  * wait is on a barrier that nothing completes; the wait gives up after `limit_ns` (<= 1 s), the kernel writes
  * PSA_ERR_TIMEOUT into the status word of `workspace` and exits normally.  psa_check_status then reports and

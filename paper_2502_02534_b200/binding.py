@@ -1,6 +1,7 @@
 from __future__ import annotations
 
 import ctypes
+import functools
 from ctypes import POINTER, c_char_p, c_float, c_int32, c_int64, c_size_t, c_void_p
 from dataclasses import dataclass
 from pathlib import Path
@@ -19,6 +20,8 @@ EXPORTED_SYMBOLS = [
     "psa_plan_bind_workspace", "psa_plan_prefix_items", "psa_plan_suffix_items",
     "psa_decode", "psa_decode_static", "psa_static_check_status", "psa_static_selftest_bounded_wait", "psa_decode_prefix", "psa_decode_suffix", "psa_decode_merge",
     "psa_decode_host_staging_bytes", "psa_decode_host", "psa_check_status", "psa_selftest_bounded_wait", "psa_append_kv", "psa_append_kv_alloc", "psa_validate_page_table", "psa_sample_scratch_bytes", "psa_sample_tokens", "psa_sample_tokens_at", "psa_attn_task",
+    "psa_page_table_scratch_bytes", "psa_build_page_table", "psa_extend_page_table", "psa_read_status", "psa_kv4_cell_bytes", "psa_store_kv4",
+    "psa_load_kv4", "psa_decode_kv4", "psa_decode_suffix_kv4", "psa_process_logits", "psa_mark_tokens",
     "psa_status_string", "psa_last_error_message", "psa_version",
 ]
 
@@ -39,6 +42,14 @@ class _Info(ctypes.Structure):
     _fields_ = [("num_sms", c_int32), ("num_samples", c_int32), ("num_prefix_items", c_int32),
                 ("num_suffix_items", c_int32), ("prefix_tile_keys", c_int32), ("prefix_tiles_per_item", c_int32),
                 ("suffix_chunk_tokens", c_int32), ("kernel_launches", c_int32), ("num_partial_rows", c_int64)]
+
+
+class _LogitsRules(ctypes.Structure):
+    _fields_ = [("repetition", c_void_p), ("frequency", c_void_p), ("presence", c_void_p), ("history", c_void_p),
+                ("history_lens", c_void_p), ("history_stride", c_int64), ("history_capacity", c_int32), ("prompt_bits", c_void_p),
+                ("prompt_row_words", c_int64), ("num_prompt_bitmaps", c_int32), ("prompt_rows", c_void_p), ("bias_indptr", c_void_p),
+                ("bias_ids", c_void_p), ("bias_values", c_void_p), ("num_biases", c_int32), ("mask_bits", c_void_p),
+                ("mask_row_words", c_int64), ("num_mask_bitmaps", c_int32), ("mask_rows", c_void_p)]
 
 
 @dataclass
@@ -122,6 +133,28 @@ def library():
         lib.psa_attn_task.argtypes = [c_int32, P, P, P, c_int32, c_int32, c_int32, c_float, P, P, P, P]
         lib.psa_selftest_bounded_wait.restype = c_int32
         lib.psa_selftest_bounded_wait.argtypes = [P, c_size_t, ctypes.c_uint64, P]
+        lib.psa_page_table_scratch_bytes.restype = c_size_t
+        lib.psa_page_table_scratch_bytes.argtypes = [c_int32]
+        lib.psa_build_page_table.restype = c_int32
+        lib.psa_build_page_table.argtypes = [P, P, c_int32, P, P, P, P, P, c_int64, P, P, c_int64, P, P, P, c_size_t, P]
+        lib.psa_extend_page_table.restype = c_int32
+        lib.psa_extend_page_table.argtypes = [P, P, P, c_int32, P, P, P, P, P, c_int64, P, P, c_int64, P, P, P, c_size_t, P]
+        lib.psa_read_status.restype = c_int32
+        lib.psa_read_status.argtypes = [P, P]
+        lib.psa_kv4_cell_bytes.restype = c_size_t
+        lib.psa_kv4_cell_bytes.argtypes = [c_int32]
+        lib.psa_store_kv4.restype = c_int32
+        lib.psa_store_kv4.argtypes = [P, P, POINTER(c_int64), P, c_int64, c_int32, c_int32, P, POINTER(c_int64), c_int64, P, P]
+        lib.psa_load_kv4.restype = c_int32
+        lib.psa_load_kv4.argtypes = [P, POINTER(c_int64), c_int64, P, c_int64, c_int32, c_int32, P, P, POINTER(c_int64), P, P]
+        lib.psa_decode_kv4.restype = c_int32
+        lib.psa_decode_kv4.argtypes = [P, P, P, P, POINTER(c_int64), P, POINTER(c_int64), P, P, P, P, P, P, c_size_t, P]
+        lib.psa_decode_suffix_kv4.restype = c_int32
+        lib.psa_decode_suffix_kv4.argtypes = [P, P, P, POINTER(c_int64), P, P, P, P, c_size_t, P]
+        lib.psa_process_logits.restype = c_int32
+        lib.psa_process_logits.argtypes = [P, c_int32, c_int64, c_int32, c_int32, POINTER(_LogitsRules), P, c_int32, c_int64, P]
+        lib.psa_mark_tokens.restype = c_int32
+        lib.psa_mark_tokens.argtypes = [P, c_int32, P, c_int32, c_int32, P, c_int64, P]
         lib.psa_status_string.restype = c_char_p
         lib.psa_status_string.argtypes = [c_int32]
         lib.psa_last_error_message.restype = c_char_p
@@ -411,3 +444,266 @@ def decode_host(plan: Plan, q, prefix_k, prefix_v, suffix_k_pool, suffix_v_pool,
 
 def host_staging_bytes(plan: Plan, n_prefix_tokens: int, n_pool_pages: int, n_page_indices: int) -> int:
     return int(library().psa_decode_host_staging_bytes(plan.handle, n_prefix_tokens, n_pool_pages, n_page_indices))
+
+
+# ---- page tables, the 4-bit cache and rules on logits.  These check the tensors they are given: type, layout, size, and that all of
+# ---- them live on the current CUDA device (ValueError otherwise); what the library itself refuses comes back as PsaError.
+
+def _flat(t, dtype, name, dev, size=None):
+    """Address of a contiguous tensor of at least `size` elements on device `dev` (None passes through)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
+    if not t.is_contiguous() or (size is not None and t.numel() < size):
+        raise ValueError(f"{name} must be contiguous" + (f" and hold at least {size} elements" if size is not None else ""))
+    if t.get_device() != dev:
+        raise ValueError(f"{name} must be on the current CUDA device")
+    return t.data_ptr()
+
+
+def _device_of(t, name):
+    """The device the call runs on: that of tensor `t`, which must be the current one."""
+    import torch
+    dev = t.get_device()
+    if dev < 0 or dev != torch.cuda.current_device():
+        raise ValueError(f"{name} must be on the current CUDA device")
+    return dev
+
+
+@functools.lru_cache(maxsize=256)
+def _strides2(a, b):
+    return (c_int64 * 2)(a, b)
+
+
+def _outer_strides(t, inner, name):
+    """Strides of dimensions 0 and 1 of a 3-d tensor whose last dimension is contiguous; a dimension of one element has none of its own."""
+    s0, s1, s2 = t.stride()
+    n0, n1, n2 = t.shape
+    if n2 != inner or (s2 != 1 and n2 > 1):
+        raise ValueError(f"{name} must be [.., .., {inner}] with a contiguous last dimension")
+    if n1 <= 1:
+        s1 = inner
+    if n0 <= 1:
+        s0 = max(1, n1) * max(s1, inner)
+    return _strides2(s0, s1)
+
+
+def page_table_scratch(num_samples):
+    """Scratch tensor for build_page_table / extend_page_table, to be kept by callers that must not allocate (uint8)."""
+    import torch
+    return torch.empty(int(library().psa_page_table_scratch_bytes(int(num_samples))), dtype=torch.uint8, device="cuda")
+
+
+def build_page_table(seq_lens, free_pages, free_count, page_indptr, page_indices, token_indptr, slot_map, *, reserve_lens=None,
+                     lens_out=None, free_count_out=None, status=None, scratch=None, stream=None):
+    """psa_build_page_table on torch CUDA tensors (int32; slot_map int64): page lists for samples of seq_lens tokens (room for
+    reserve_lens), pages from the stack free_pages[0 .. free_count), and the slot of every token.  Outputs: page_indptr [B+1],
+    page_indices (any capacity), token_indptr [B+1], slot_map (any capacity), lens_out [B], free_count_out (free_count in place
+    when None)."""
+    import torch
+    n, i32 = seq_lens.numel(), torch.int32
+    p_seq = _flat(seq_lens, i32, "seq_lens", seq_lens.get_device())
+    p_indptr, p_tokens = (_flat(t, i32, name, seq_lens.get_device(), n + 1) for t, name in ((page_indptr, "page_indptr"), (token_indptr, "token_indptr")))
+    dev = _device_of(seq_lens, "seq_lens")
+    if scratch is None:
+        scratch = page_table_scratch(n)
+    _check(library().psa_build_page_table(
+        p_seq, _flat(reserve_lens, i32, "reserve_lens", dev, n), n, _flat(free_pages, i32, "free_pages", dev),
+        _flat(free_count, i32, "free_count", dev, 1), _flat(free_count if free_count_out is None else free_count_out, i32, "free_count_out", dev, 1),
+        p_indptr, _flat(page_indices, i32, "page_indices", dev), page_indices.numel(), p_tokens,
+        _flat(slot_map, torch.int64, "slot_map", dev), slot_map.numel(), _flat(lens_out, i32, "lens_out", dev, n),
+        _status_ptr(status, dev), _flat(scratch, torch.uint8, "scratch", dev), scratch.numel(), _stream_ptr(stream)))
+
+
+def extend_page_table(held_lens, new_lens, free_pages, free_count, page_indptr, page_indices, token_indptr, slot_map, *, max_lens=None,
+                      lens_out=None, free_count_out=None, status=None, scratch=None, stream=None):
+    """psa_extend_page_table on torch CUDA tensors: new_lens more tokens for samples that hold held_lens, in existing page lists.
+    Outputs as for build_page_table; lens_out and free_count_out may be held_lens and free_count themselves."""
+    import torch
+    n, i32 = held_lens.numel(), torch.int32
+    p_held = _flat(held_lens, i32, "held_lens", held_lens.get_device())
+    p_new = _flat(new_lens, i32, "new_lens", held_lens.get_device(), n)
+    p_indptr, p_tokens = (_flat(t, i32, name, held_lens.get_device(), n + 1) for t, name in ((page_indptr, "page_indptr"), (token_indptr, "token_indptr")))
+    dev = _device_of(held_lens, "held_lens")
+    if scratch is None:
+        scratch = page_table_scratch(n)
+    _check(library().psa_extend_page_table(
+        p_held, p_new, _flat(max_lens, i32, "max_lens", dev, n), n, _flat(free_pages, i32, "free_pages", dev),
+        _flat(free_count, i32, "free_count", dev, 1), _flat(free_count if free_count_out is None else free_count_out, i32, "free_count_out", dev, 1),
+        p_indptr, _flat(page_indices, i32, "page_indices", dev), page_indices.numel(), p_tokens,
+        _flat(slot_map, torch.int64, "slot_map", dev), slot_map.numel(), _flat(lens_out, i32, "lens_out", dev, n),
+        _status_ptr(status, dev), _flat(scratch, torch.uint8, "scratch", dev), scratch.numel(), _stream_ptr(stream)))
+
+
+def _status_ptr(status, dev):
+    """A status word: a one-element int32 tensor, or a Plan (the word Plan.check_status reads)."""
+    import torch
+    if status is None:
+        return None
+    if isinstance(status, Plan):
+        if status.workspace is None:
+            raise ValueError("status: the plan has no workspace yet")
+        return _flat(status.workspace, torch.uint8, "status", dev)
+    return _flat(status, torch.int32, "status", dev, 1)
+
+
+def read_status(status, stream=None):
+    """psa_read_status: synchronise, raise if the one-element int32 tensor `status` holds an error, and clear it."""
+    import torch
+    _check(library().psa_read_status(_flat(status, torch.int32, "status", _device_of(status, "status"), 1), _stream_ptr(stream)))
+
+
+def kv4_cell_bytes(head_dim) -> int:
+    """Bytes of one (page, KV head) cell of the 4-bit cache."""
+    return int(library().psa_kv4_cell_bytes(int(head_dim)))
+
+
+def _kv4_args(k, v, slot_map, pool, names):
+    import torch
+    if k.dim() != 3 or k.shape != v.shape or k.stride() != v.stride() or k.dtype is not torch.bfloat16 or v.dtype is not torch.bfloat16:
+        raise ValueError(f"{names} must be bf16 [tokens, heads, head_dim] of the same shape and strides")
+    tokens, heads, dim = k.shape
+    if pool.dtype is not torch.uint8 or pool.dim() != 3 or pool.shape[1] != heads:
+        raise ValueError("pool must be uint8 [pages, heads, kv4_cell_bytes(head_dim)]")
+    if slot_map.dtype is not torch.int64 or slot_map.numel() < tokens or not slot_map.is_contiguous():
+        raise ValueError(f"slot_map must be contiguous int64 with at least {tokens} elements")
+    dev = _device_of(k, names)
+    if v.get_device() != dev or slot_map.get_device() != dev or pool.get_device() != dev:
+        raise ValueError("all tensors must be on the current CUDA device")
+    return tokens, heads, dim, _outer_strides(k, dim, names), _outer_strides(pool, 20 * dim, "pool"), dev
+
+
+def store_kv4(new_k, new_v, slot_map, pool, *, status=None, stream=None):
+    """psa_store_kv4: quantise new_k / new_v [T, Hkv, D] bf16 (any token and head stride) into the slots of a 4-bit pool
+    [pages, Hkv, kv4_cell_bytes(D)] uint8."""
+    t, h, d, kst, pst, dev = _kv4_args(new_k, new_v, slot_map, pool, "new_k and new_v")
+    _check(library().psa_store_kv4(new_k.data_ptr(), new_v.data_ptr(), kst, slot_map.data_ptr(), t, h, d, pool.data_ptr(), pst,
+                                   pool.shape[0], _status_ptr(status, dev), _stream_ptr(stream)))
+
+
+def load_kv4(pool, slot_map, out_k, out_v, *, status=None, stream=None):
+    """psa_load_kv4: the cached tokens of slot_map as bf16 rows out_k / out_v [T, Hkv, D]; rows of negative slots are left alone."""
+    t, h, d, kst, pst, dev = _kv4_args(out_k, out_v, slot_map, pool, "out_k and out_v")
+    _check(library().psa_load_kv4(pool.data_ptr(), pst, pool.shape[0], slot_map.data_ptr(), t, h, d, out_k.data_ptr(), out_v.data_ptr(),
+                                  kst, _status_ptr(status, dev), _stream_ptr(stream)))
+
+
+def decode_kv4(plan: Plan, q, prefix_k, prefix_v, pool, page_indptr, page_indices, suffix_lens, out, lse, *, prefix_strides=None,
+               stream=None, stage="all"):
+    """psa_decode_kv4 (or its suffix stage): decode with the samples' own tokens in a 4-bit pool [pages, Hkv, kv4_cell_bytes(D)]
+    uint8.  Everything else as for decode."""
+    import torch
+    if stage not in ("all", "suffix"):
+        raise ValueError(stage)
+    if pool.dtype is not torch.uint8 or pool.dim() != 3 or pool.shape[1] != plan.num_kv_heads:
+        raise ValueError("pool must be uint8 [pages, num_kv_heads, kv4_cell_bytes(head_dim)]")
+    pst = _outer_strides(pool, 20 * plan.head_dim, "pool")
+    rows = len(plan.suffix_len_bounds)
+    dev = _device_of(pool, "pool")
+    if plan.workspace is None:
+        plan.bind_workspace(stream=stream)
+    p_q = _flat(q, torch.bfloat16, "q", dev, rows * plan.num_q_heads * plan.head_dim)
+    table = (_flat(page_indptr, torch.int32, "page_indptr", dev, rows + 1), _flat(page_indices, torch.int32, "page_indices", dev),
+             _flat(suffix_lens, torch.int32, "suffix_lens", dev, rows))
+    ws = (_ptr(plan.workspace), plan.workspace.numel(), _stream_ptr(stream))
+    if stage == "suffix":
+        _check(library().psa_decode_suffix_kv4(plan.handle, p_q, pool.data_ptr(), pst, *table, *ws))
+        return
+    p_out = _flat(out, torch.float32 if plan.out_dtype == PSA_OUT_F32 else torch.bfloat16, "out", dev, rows * plan.num_q_heads * plan.head_dim)
+    p_lse = _flat(lse, torch.float32, "lse", dev, rows * plan.num_q_heads)
+    _check(library().psa_decode_kv4(plan.handle, p_q, _ptr(prefix_k), _ptr(prefix_v), _strides2(*(prefix_strides or default_prefix_strides(plan))),
+                                    pool.data_ptr(), pst, *table, p_out, p_lse, *ws))
+
+
+def _dtype_code(t, name):
+    import torch
+    if t.dtype is torch.bfloat16:
+        return PSA_OUT_BF16
+    if t.dtype is torch.float32:
+        return PSA_OUT_F32
+    raise ValueError(f"{name} must be bf16 or f32, not {t.dtype}")
+
+
+def process_logits(logits, out=None, *, repetition=None, frequency=None, presence=None, history=None, history_lens=None,
+                   prompt_bits=None, prompt_rows=None, bias_indptr=None, bias_ids=None, bias_values=None, mask_bits=None,
+                   mask_rows=None, stream=None):
+    """psa_process_logits on torch CUDA tensors: penalties for repeated tokens, biases and grammar masks.  logits and out [R, V] bf16
+    or f32 (rows may be padded; out may be logits; allocated when None); repetition / frequency / presence [R] f32; history
+    [R, capacity] int32 with history_lens [R]; prompt_bits / mask_bits [*, >= ceil(V / 32)] int32 bitmaps chosen per row by prompt_rows /
+    mask_rows [R] int32; bias_indptr [R+1], bias_ids int32 and bias_values f32.  Returns out."""
+    import torch
+    if logits.dim() != 2 or (out is not None and out.shape != logits.shape):
+        raise ValueError("logits must be [rows, vocab], and out of the same shape")
+    R, V = logits.shape
+    in_code = _dtype_code(logits, "logits")
+    if out is None:
+        out = torch.empty((R, (V + 7) // 8 * 8), dtype=logits.dtype, device=logits.device)[:, :V]
+    out_code = _dtype_code(out, "out")
+    if (logits.stride(1) != 1 or out.stride(1) != 1) and V > 1:
+        raise ValueError("logits and out must be contiguous along the vocabulary")
+    if (history is None) != (history_lens is None):
+        raise ValueError("history and history_lens go together")
+    if history is not None and (history.dtype is not torch.int32 or history.dim() != 2 or history.shape[0] < R or (history.stride(1) != 1 and history.shape[1] > 1)):
+        raise ValueError("history must be int32 [rows, capacity], contiguous along the second dimension")
+    if len({bias_indptr is None, bias_ids is None, bias_values is None}) != 1:
+        raise ValueError("bias_indptr, bias_ids and bias_values go together")
+    words = (V + 31) // 32
+    for bits, rows, name in ((prompt_bits, prompt_rows, "prompt"), (mask_bits, mask_rows, "mask")):
+        if bits is None:
+            if rows is not None:
+                raise ValueError(f"{name}_rows without {name}_bits")
+        elif bits.dtype is not torch.int32 or bits.dim() != 2 or bits.shape[1] < words or (bits.stride(1) != 1 and bits.shape[1] > 1):
+            raise ValueError(f"{name}_bits must be int32 [bitmaps, words >= {words}], contiguous along the second dimension")
+        elif rows is None and bits.shape[0] < R:
+            raise ValueError(f"{name}_bits needs one bitmap per row, or {name}_rows")
+    dev = _device_of(logits, "logits")
+    for t, name in ((out, "out"), (history, "history"), (prompt_bits, "prompt_bits"), (mask_bits, "mask_bits")):
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"{name} must be on the current CUDA device")
+    f32, i32 = torch.float32, torch.int32
+    rules = _LogitsRules()
+    rules.repetition = _flat(repetition, f32, "repetition", dev, R)
+    rules.frequency = _flat(frequency, f32, "frequency", dev, R)
+    rules.presence = _flat(presence, f32, "presence", dev, R)
+    if history is not None:
+        rules.history, rules.history_lens = history.data_ptr(), _flat(history_lens, i32, "history_lens", dev, R)
+        rules.history_stride, rules.history_capacity = _row_stride(history), history.shape[1]
+    if prompt_bits is not None:
+        rules.prompt_bits, rules.prompt_row_words, rules.num_prompt_bitmaps = prompt_bits.data_ptr(), _row_stride(prompt_bits), prompt_bits.shape[0]
+        rules.prompt_rows = _flat(prompt_rows, i32, "prompt_rows", dev, R)
+    if bias_indptr is not None:
+        rules.bias_indptr = _flat(bias_indptr, i32, "bias_indptr", dev, R + 1)
+        rules.bias_ids, rules.num_biases = _flat(bias_ids, i32, "bias_ids", dev), bias_ids.numel()
+        rules.bias_values = _flat(bias_values, f32, "bias_values", dev, bias_ids.numel())
+    if mask_bits is not None:
+        rules.mask_bits, rules.mask_row_words, rules.num_mask_bitmaps = mask_bits.data_ptr(), _row_stride(mask_bits), mask_bits.shape[0]
+        rules.mask_rows = _flat(mask_rows, i32, "mask_rows", dev, R)
+    in_stride, out_stride = (t.stride(0) if R > 1 else (V + 7) // 8 * 8 for t in (logits, out))
+    _check(library().psa_process_logits(logits.data_ptr(), in_code, in_stride, R, V, ctypes.byref(rules), out.data_ptr(), out_code, out_stride,
+                                        _stream_ptr(stream)))
+    return out
+
+
+def _row_stride(t):
+    """Row stride of a 2-d tensor with contiguous rows; one row has none of its own."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def mark_tokens(ids, indptr, vocab, bits=None, *, stream=None):
+    """psa_mark_tokens: bitmaps [rows, >= ceil(vocab / 32)] int32 of the tokens in ids[indptr[m] .. indptr[m + 1]).  Returns bits."""
+    import torch
+    rows, words = indptr.numel() - 1, (int(vocab) + 31) // 32
+    if rows < 0:
+        raise ValueError("indptr must hold rows + 1 elements")
+    if bits is None:
+        bits = torch.empty((rows, words), dtype=torch.int32, device=ids.device)
+    if bits.dtype is not torch.int32 or bits.dim() != 2 or bits.shape[0] < rows or bits.shape[1] < words or (bits.stride(1) != 1 and bits.shape[1] > 1):
+        raise ValueError(f"bits must be int32 [rows, words >= {words}], contiguous along the second dimension")
+    p_ids = _flat(ids, torch.int32, "ids", ids.get_device())
+    p_indptr = _flat(indptr, torch.int32, "indptr", ids.get_device())
+    dev = _device_of(ids, "ids")
+    if bits.get_device() != dev:
+        raise ValueError("bits must be on the current CUDA device")
+    _check(library().psa_mark_tokens(p_ids, ids.numel(), p_indptr, rows, int(vocab), bits.data_ptr(), _row_stride(bits), _stream_ptr(stream)))
+    return bits

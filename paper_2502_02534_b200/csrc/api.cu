@@ -281,6 +281,44 @@ psa_status_t psa_decode_suffix(const psa_plan_t *plan, const void *q, const void
                        workspace_bytes, cuda_stream, false);
 }
 
+static psa_status_t suffix_kv4_impl(const psa_plan_t *plan, const void *q, const void *kv4_pool, const int64_t pool_strides[2],
+                                    const int32_t *page_indptr, const int32_t *page_indices, const int32_t *suffix_lens,
+                                    void *workspace, size_t workspace_bytes, void *cuda_stream, bool after_prefix)
+{
+    TraceRange trace("psa suffix stage (4-bit)");
+    Carved c;
+    psa_status_t st = carve(plan, workspace, workspace_bytes, &c);
+    if (st != PSA_OK) return st;
+    if (plan->suffix_items.empty()) return PSA_OK;
+    if (!q || !kv4_pool || !pool_strides || !page_indptr || !page_indices || !suffix_lens)
+        return fail(PSA_ERR_INVALID_ARG, "null suffix argument");
+    if (!aligned(q, 16) || !aligned(kv4_pool, 16)) return fail(PSA_ERR_INVALID_ARG, "q and the pool must be 16-byte aligned");
+    for (int i = 0; i < 2; ++i)
+        if (pool_strides[i] < int64_t(psa_kv4_cell_bytes(plan->cfg.head_dim)) || pool_strides[i] % 16)
+            return fail(PSA_ERR_INVALID_ARG, "pool strides must be multiples of 16 bytes, at least one cell");
+    psa::SuffixKv4Args a{};
+    a.q = q; a.pool = kv4_pool;
+    a.stride_page = pool_strides[0]; a.stride_cell = pool_strides[1];
+    a.page_indptr = page_indptr; a.page_indices = page_indices; a.suffix_lens = suffix_lens;
+    a.num_q_heads = plan->cfg.num_q_heads; a.num_kv_heads = plan->cfg.num_kv_heads; a.head_dim = plan->cfg.head_dim;
+    a.sm_scale = plan->cfg.sm_scale;
+    a.items = c.suffix_items; a.sample_info = c.sample_info;
+    a.num_items = int32_t(plan->suffix_items.size()); a.chunk_tokens = plan->suffix_chunk_tokens;
+    a.partial_o = c.partial_o; a.partial_lse = c.partial_lse;
+    a.after_prefix = after_prefix;
+    std::string err;
+    if (psa::launch_suffix_kv4(a, cuda_stream, &err) != 0) return fail(PSA_ERR_CUDA, err);
+    return PSA_OK;
+}
+
+psa_status_t psa_decode_suffix_kv4(const psa_plan_t *plan, const void *q, const void *kv4_pool, const int64_t pool_strides[2],
+                                   const int32_t *page_indptr, const int32_t *page_indices, const int32_t *suffix_lens,
+                                   void *workspace, size_t workspace_bytes, void *cuda_stream)
+{
+    return suffix_kv4_impl(plan, q, kv4_pool, pool_strides, page_indptr, page_indices, suffix_lens, workspace, workspace_bytes,
+                           cuda_stream, false);
+}
+
 static psa_status_t merge_impl(const psa_plan_t *plan, const int32_t *suffix_lens, void *out, float *lse, void *workspace,
                                size_t workspace_bytes, void *cuda_stream, bool after_stage, bool wait_for_prefix_count = false)
 {
@@ -346,6 +384,25 @@ psa_status_t psa_decode(const psa_plan_t *plan, const void *q, const void *prefi
     if (st != PSA_OK) return st;
     st = suffix_impl(plan, q, suffix_k_pool, suffix_v_pool, pool_strides, page_indptr, page_indices, suffix_lens, workspace,
                      workspace_bytes, cuda_stream, have_prefix);
+    if (st != PSA_OK) return st;
+    return merge_impl(plan, suffix_lens, out, lse, workspace, workspace_bytes, cuda_stream, have_prefix || have_suffix,
+                      have_prefix && have_suffix);
+}
+
+psa_status_t psa_decode_kv4(const psa_plan_t *plan, const void *q, const void *prefix_k, const void *prefix_v,
+                            const int64_t prefix_strides[2], const void *kv4_pool, const int64_t pool_strides[2],
+                            const int32_t *page_indptr, const int32_t *page_indices, const int32_t *suffix_lens, void *out, float *lse,
+                            void *workspace, size_t workspace_bytes, void *cuda_stream)
+{
+    if (!plan) return fail(PSA_ERR_INVALID_ARG, "null plan");
+    TraceRange trace("psa_decode_kv4");
+    // the stages are chained exactly as in psa_decode
+    const bool have_prefix = !plan->prefix_items.empty(), have_suffix = !plan->suffix_items.empty();
+    psa_status_t st = prefix_impl(plan, q, prefix_k, prefix_v, prefix_strides, workspace, workspace_bytes, cuda_stream,
+                                  have_prefix && have_suffix);
+    if (st != PSA_OK) return st;
+    st = suffix_kv4_impl(plan, q, kv4_pool, pool_strides, page_indptr, page_indices, suffix_lens, workspace, workspace_bytes,
+                         cuda_stream, have_prefix);
     if (st != PSA_OK) return st;
     return merge_impl(plan, suffix_lens, out, lse, workspace, workspace_bytes, cuda_stream, have_prefix || have_suffix,
                       have_prefix && have_suffix);
@@ -445,6 +502,21 @@ psa_status_t psa_check_status(const psa_plan_t *plan, void *workspace, void *cud
         return fail(psa_status_t(word), "device-side status word was set");
     }
     return PSA_OK;
+}
+
+psa_status_t psa_read_status(int32_t *status, void *cuda_stream)
+{
+    if (!status || !aligned(status, 4)) return fail(PSA_ERR_INVALID_ARG, "status must be a 4-byte aligned device pointer");
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    int32_t word = 0;
+    cudaError_t e = cudaMemcpyAsync(&word, status, sizeof word, cudaMemcpyDeviceToHost, st);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+    if (e != cudaSuccess) return cuda_fail(e, "reading the status word");
+    if (word == 0) return PSA_OK;
+    e = cudaMemsetAsync(status, 0, sizeof word, st);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+    if (e != cudaSuccess) return cuda_fail(e, "clearing the status word");
+    return fail(psa_status_t(word), "device-side status word was set");
 }
 
 static psa_status_t append_impl(const psa_plan_t *plan, const void *new_k, const void *new_v, void *suffix_k_pool,

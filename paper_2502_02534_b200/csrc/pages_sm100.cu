@@ -1,0 +1,401 @@
+// Page tables and slot maps built on the device from request lengths.
+//
+// A sample s that holds S_s tokens and gets N_s new ones needs the pages ceil(S_s / 16) .. ceil((S_s + N_s) / 16) - 1 of
+// its list.  Pages come off a caller-owned stack in sample order: with need_s = the number of those pages and
+// P_s = sum of need over the samples before s, list entry j of sample s receives free_pages[count - 1 - (P_s + j - j0)].
+// Token i of sample s lands in slot page(pos / 16) * 16 + pos % 16, pos = S_s + i, and stands at token_indptr[s] + i of
+// the packed batch.  Everything is therefore three exclusive scans over the samples (tokens, list entries, pages) and
+// then one independent lookup per token and per list entry.
+//
+//   scan phase     one thread per sample, 1024 samples per block.  A block gets its starting sums by reducing the samples
+//                  before its own itself: no block waits for another one, and at the sizes of a decode batch (one to a
+//                  few blocks) that costs a few loads.
+//   spread phase   a warp takes 256 consecutive tokens (or list entries), finds the sample of the first and of the last
+//                  by a 32-way search over the scanned offsets (two rounds for 1024 samples), and writes 256 contiguous
+//                  bytes per instruction; within one sample the page id is shared by 16 lanes.
+//
+// Bound: 8 bytes written per token of capacity once there are many, launch latency when there are few.  The two phases
+// are one launch (one block) up to kOneBlockWork lookups and two launches above it.
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <string>
+
+#include "psa_internal.h"
+
+namespace psa {
+namespace {
+
+constexpr int kScanThreads = 1024;
+constexpr int kSpread = 256;                 // tokens or list entries a warp handles at a time
+constexpr int64_t kOneBlockWork = 16384;
+constexpr int kOneBlockSamples = 4096;
+
+struct PageTableArgs {
+    const int32_t *held;       // null: nothing is held yet (a table built from scratch)
+    const int32_t *new_lens;
+    const int32_t *limits;     // reserve_lens (build) / max_lens (extend), may be null
+    int32_t num_samples;
+    const int32_t *free_pages, *free_count;
+    int32_t *free_count_out;
+    int32_t *page_indptr;      // written when `build`, read otherwise
+    int32_t *page_indices;
+    int64_t num_entries;       // capacity of page_indices
+    int32_t *token_indptr;
+    int64_t *slot_map;
+    int64_t max_tokens;        // capacity of slot_map
+    int32_t *lens_out;         // may be null, may alias held / new_lens
+    int32_t *status;           // may be null
+    // scratch: head[0] = {pages on the stack, -}; rec[s] = {held, first page's rank on the stack or -1 (refused)};
+    // block_used[b] = pages handed out up to and including the last served sample of scan block b
+    int2 *head;
+    int2 *rec;
+    int32_t *block_used;
+    int32_t scan_blocks;
+    bool build;
+};
+
+struct Sums {
+    long long tokens, entries, pages;
+};
+
+// What a sample asks for, apart from whether the arrays have room for it.
+struct Ask {
+    int32_t held, count;       // tokens it holds, tokens it gets (0 where the input is negative)
+    int32_t entries;           // list entries it reserves (build)
+    int32_t pages;             // pages it needs; 0 when it is refused already
+    bool ok;
+};
+
+__device__ __forceinline__ Ask ask(const PageTableArgs &a, int s)
+{
+    Ask r;
+    const int32_t n = a.new_lens[s];
+    r.held = a.held ? a.held[s] : 0;
+    r.count = max(n, 0);
+    const long long end = (long long)(r.held) + r.count;
+    r.ok = n >= 0 && r.held >= 0 && end <= 0x7fffffffll;
+    if (a.build) {
+        const int32_t reserve = a.limits ? max(a.limits[s], 0) : r.count;
+        r.entries = int32_t(((long long)reserve + kPageSize - 1) / kPageSize);
+        r.ok = r.ok && end <= reserve;
+    } else {
+        r.entries = 0;
+        if (a.limits) r.ok = r.ok && (r.count == 0 || end <= a.limits[s]);
+        const long long first = a.page_indptr[s], last = a.page_indptr[s + 1];
+        r.ok = r.ok && (r.count == 0 || (first >= 0 && last <= a.num_entries && (end + kPageSize - 1) / kPageSize <= last - first));
+        // a partly filled page must be in the list already (a negative id marks an entry without a page)
+        if (r.ok && r.count > 0 && r.held % kPageSize != 0) r.ok = a.page_indices[first + r.held / kPageSize] >= 0;
+    }
+    r.pages = r.ok ? int32_t((end + kPageSize - 1) / kPageSize - ((long long)r.held + kPageSize - 1) / kPageSize) : 0;
+    return r;
+}
+
+__device__ __forceinline__ long long warp_inclusive(long long v, int lane)
+{
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long u = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += u;
+    }
+    return v;
+}
+__device__ __forceinline__ long long warp_total(long long v)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+// Samples [s0, s0 + 1024) with the sums of everything before them; returns the sums behind them.
+__device__ Sums scan_chunk(const PageTableArgs &a, int s0, const Sums &before, int avail, int *used_to)
+{
+    __shared__ long long warp_sums[3][32];
+    __shared__ int block_used;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int s = s0 + int(threadIdx.x);
+    Ask q{};
+    if (s < a.num_samples) q = ask(a, s);
+    const long long v[3] = {q.count, q.entries, q.pages};
+    long long incl[3];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        incl[i] = warp_inclusive(v[i], lane);
+        if (lane == 31) warp_sums[i][warp] = incl[i];
+    }
+    if (threadIdx.x == 0) block_used = 0;
+    __syncthreads();
+    if (warp < 3) warp_sums[warp][lane] = warp_inclusive(warp_sums[warp][lane], lane);
+    __syncthreads();
+    long long excl[3], total[3];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        excl[i] = (warp ? warp_sums[i][warp - 1] : 0) + incl[i] - v[i];
+        total[i] = warp_sums[i][31];
+    }
+    if (s < a.num_samples) {
+        const long long t0 = before.tokens + excl[0], e0 = before.entries + excl[1], p0 = before.pages + excl[2];
+        bool ok = q.ok && t0 + q.count <= a.max_tokens;
+        if (a.build) {
+            ok = ok && e0 + q.entries <= a.num_entries;
+            a.page_indptr[s] = int32_t(min(e0, (long long)a.num_entries));
+            if (s == a.num_samples - 1) a.page_indptr[s + 1] = int32_t(min(e0 + q.entries, (long long)a.num_entries));
+        }
+        ok = ok && (q.pages == 0 || p0 + q.pages <= avail);
+        a.token_indptr[s] = int32_t(min(t0, (long long)a.max_tokens));
+        if (s == a.num_samples - 1) a.token_indptr[s + 1] = int32_t(min(t0 + q.count, (long long)a.max_tokens));
+        a.rec[s] = make_int2(q.held, ok ? int32_t(min(p0, (long long)avail)) : -1);
+        if (ok && q.pages > 0) atomicMax(&block_used, int(p0 + q.pages));
+        if (!ok && a.status) atomicCAS(a.status, 0, int(PSA_ERR_BOUNDS));
+    }
+    __syncthreads();
+    *used_to = block_used;
+    __syncthreads();
+    return Sums{before.tokens + total[0], before.entries + total[1], before.pages + total[2]};
+}
+
+// Largest i in [lo, hi) with offsets[i] <= x; offsets ascend and offsets[lo] <= x.  All lanes of the warp search together.
+__device__ __forceinline__ int warp_find(const int32_t *offsets, int lo, int hi, long long x, int lane)
+{
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 31) / 32;
+        const int at = lo + lane * step;
+        const bool below = at < hi && (lane == 0 || offsets[at] <= x);
+        const int last = __popc(__ballot_sync(0xffffffffu, below)) - 1;
+        lo += last * step;
+        hi = min(hi, lo + step);
+    }
+    return lo;
+}
+__device__ __forceinline__ int lane_find(const int32_t *offsets, int lo, int hi, long long x)
+{
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (offsets[mid] <= x) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// Tokens [t0, t0 + 256) of the slot map.
+__device__ void spread_tokens(const PageTableArgs &a, long long t0, int avail, int lane)
+{
+    const int n = a.num_samples;
+    const long long total = n > 0 ? a.token_indptr[n] : 0;
+    const long long end = min(t0 + kSpread, (long long)a.max_tokens);
+    int s_lo = 0, s_hi = 0;
+    if (t0 < total) {
+        s_lo = warp_find(a.token_indptr, 0, n, t0, lane);
+        s_hi = warp_find(a.token_indptr, s_lo, n, min(end, total) - 1, lane);
+    }
+    for (long long t = t0 + lane; t < end; t += 32) {
+        long long slot = -1;
+        if (t < total) {
+            const int s = s_lo == s_hi ? s_lo : lane_find(a.token_indptr, s_lo, s_hi + 1, t);
+            const int2 rec = a.rec[s];
+            if (rec.y >= 0) {
+                const int pos = rec.x + int(t - a.token_indptr[s]);
+                const int j = pos / kPageSize, fresh = (rec.x + kPageSize - 1) / kPageSize;
+                const long long entry = (long long)a.page_indptr[s] + j;
+                int page;
+                if (j >= fresh) {
+                    page = a.free_pages[avail - 1 - (rec.y + j - fresh)];
+                    if (!a.build && pos % kPageSize == 0) a.page_indices[entry] = page;   // the first token of a fresh page files it
+                } else {
+                    page = a.page_indices[entry];
+                }
+                if (page >= 0) slot = (long long)page * kPageSize + pos % kPageSize;
+            }
+        }
+        a.slot_map[t] = slot;
+    }
+}
+
+// Entries [e0, e0 + 256) of a list array built from scratch: the pages of the tokens held, -1 in the rest.
+__device__ void spread_entries(const PageTableArgs &a, long long e0, int avail, int lane)
+{
+    const int n = a.num_samples;
+    const long long total = n > 0 ? a.page_indptr[n] : 0;
+    const long long end = min(e0 + kSpread, (long long)a.num_entries);
+    int s_lo = 0, s_hi = 0;
+    if (e0 < total) {
+        s_lo = warp_find(a.page_indptr, 0, n, e0, lane);
+        s_hi = warp_find(a.page_indptr, s_lo, n, min(end, total) - 1, lane);
+    }
+    for (long long e = e0 + lane; e < end; e += 32) {
+        int page = -1;
+        if (e < total) {
+            const int s = s_lo == s_hi ? s_lo : lane_find(a.page_indptr, s_lo, s_hi + 1, e);
+            const int2 rec = a.rec[s];
+            const int j = int(e - a.page_indptr[s]);
+            const int tokens = a.token_indptr[s + 1] - a.token_indptr[s];
+            if (rec.y >= 0 && j < (tokens + kPageSize - 1) / kPageSize) page = a.free_pages[avail - 1 - (rec.y + j)];
+        }
+        a.page_indices[e] = page;
+    }
+}
+
+// Everything behind the scans, shared out over `warps` warps.
+__device__ void spread(const PageTableArgs &a, int avail, long long warp, long long warps, int lane)
+{
+    const long long token_chunks = (a.max_tokens + kSpread - 1) / kSpread;
+    const long long entry_chunks = a.build ? (a.num_entries + kSpread - 1) / kSpread : 0;
+    for (long long c = warp; c < token_chunks + entry_chunks; c += warps) {
+        if (c < token_chunks) spread_tokens(a, c * kSpread, avail, lane);
+        else spread_entries(a, (c - token_chunks) * kSpread, avail, lane);
+    }
+    if (a.lens_out)
+        for (long long s = warp * 32 + lane; s < a.num_samples; s += warps * 32) {
+            const int2 rec = a.rec[s];
+            a.lens_out[s] = rec.y >= 0 ? rec.x + (a.token_indptr[s + 1] - a.token_indptr[s]) : rec.x;
+        }
+}
+
+// Small batches: both phases in one block.
+__global__ void __launch_bounds__(kScanThreads)
+page_table_one_block_kernel(PageTableArgs a)
+{
+    const int avail = max(*a.free_count, 0);
+    Sums sums{0, 0, 0};
+    int used = 0;
+    for (int s0 = 0; s0 < a.num_samples; s0 += kScanThreads) {
+        int u;
+        sums = scan_chunk(a, s0, sums, avail, &u);
+        used = max(used, u);
+    }
+    if (threadIdx.x == 0 && a.num_samples == 0) {
+        a.token_indptr[0] = 0;
+        if (a.build) a.page_indptr[0] = 0;
+    }
+    __syncthreads();   // also: every thread has read the stack's height before it is written, and the lengths before lens_out
+    if (threadIdx.x == 0) *a.free_count_out = avail - used;
+    spread(a, avail, threadIdx.x >> 5, kScanThreads / 32, threadIdx.x & 31);
+}
+
+__global__ void __launch_bounds__(kScanThreads)
+page_table_scan_kernel(PageTableArgs a)
+{
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    __shared__ long long part[3][32];
+    const int avail = max(*a.free_count, 0);
+    const int s0 = blockIdx.x * kScanThreads, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    Sums mine{0, 0, 0};
+    for (int s = threadIdx.x; s < s0; s += kScanThreads) {
+        const Ask q = ask(a, s);
+        mine.tokens += q.count; mine.entries += q.entries; mine.pages += q.pages;
+    }
+    const long long w[3] = {warp_total(mine.tokens), warp_total(mine.entries), warp_total(mine.pages)};
+    if (lane == 0) { part[0][warp] = w[0]; part[1][warp] = w[1]; part[2][warp] = w[2]; }
+    __syncthreads();
+    const Sums before{warp_total(part[0][lane]), warp_total(part[1][lane]), warp_total(part[2][lane])};
+    int used;
+    scan_chunk(a, s0, before, avail, &used);
+    if (threadIdx.x == 0) {
+        a.block_used[blockIdx.x] = used;
+        if (blockIdx.x == 0) {
+            a.head[0] = make_int2(avail, 0);
+            if (a.num_samples == 0) {
+                a.token_indptr[0] = 0;
+                if (a.build) a.page_indptr[0] = 0;
+            }
+        }
+    }
+}
+
+__global__ void __launch_bounds__(256)
+page_table_spread_kernel(PageTableArgs a)
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int avail = a.head[0].x;
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        int used = 0;
+        for (int b = 0; b < a.scan_blocks; ++b) used = max(used, a.block_used[b]);
+        *a.free_count_out = avail - used;
+    }
+    spread(a, avail, (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5), (long long)gridDim.x * (blockDim.x >> 5),
+           threadIdx.x & 31);
+}
+
+int scan_blocks_of(int num_samples) { return std::max(1, (num_samples + kScanThreads - 1) / kScanThreads); }
+
+psa_status_t run(PageTableArgs a, void *scratch, size_t scratch_bytes, void *cuda_stream)
+{
+    if (a.num_samples < 0 || a.max_tokens < 0 || a.num_entries < 0) return set_last_error(PSA_ERR_INVALID_ARG, "negative sizes");
+    if (a.num_samples > (1 << 20)) return set_last_error(PSA_ERR_UNSUPPORTED, "at most 2^20 samples per call");
+    if (a.max_tokens > 0x7fffffff || a.num_entries > 0x7fffffff)
+        return set_last_error(PSA_ERR_UNSUPPORTED, "slot_map and page_indices hold at most 2^31 - 1 entries");
+    if (!a.free_pages || !a.free_count || !a.free_count_out || !a.page_indptr || !a.token_indptr || (a.max_tokens > 0 && !a.slot_map) ||
+        (a.num_entries > 0 && !a.page_indices) || (a.num_samples > 0 && !a.new_lens) || (!a.build && a.num_samples > 0 && !a.held))
+        return set_last_error(PSA_ERR_INVALID_ARG, "null page table argument");
+    if (!scratch || reinterpret_cast<uintptr_t>(scratch) % 8 || scratch_bytes < psa_page_table_scratch_bytes(a.num_samples))
+        return set_last_error(PSA_ERR_WORKSPACE, "scratch must be 8-byte aligned and hold psa_page_table_scratch_bytes(num_samples)");
+    a.head = static_cast<int2 *>(scratch);
+    a.rec = a.head + 1;
+    a.block_used = reinterpret_cast<int32_t *>(a.rec + a.num_samples);
+    a.scan_blocks = scan_blocks_of(a.num_samples);
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const int64_t work = a.max_tokens + (a.build ? a.num_entries : 0);
+    cudaError_t e;
+    if (work <= kOneBlockWork && a.num_samples <= kOneBlockSamples) {
+        page_table_one_block_kernel<<<1, kScanThreads, 0, st>>>(a);
+        e = cudaGetLastError();
+    } else {
+        page_table_scan_kernel<<<a.scan_blocks, kScanThreads, 0, st>>>(a);
+        e = cudaGetLastError();
+        if (e == cudaSuccess) {
+            const int64_t warps = (work + kSpread - 1) / kSpread;
+            cudaLaunchConfig_t lc{};
+            lc.gridDim = dim3(unsigned(std::max<int64_t>(1, std::min<int64_t>((warps + 7) / 8, 148 * 8))));
+            lc.blockDim = dim3(256);
+            lc.stream = st;
+            cudaLaunchAttribute attr{};
+            attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+            attr.val.programmaticStreamSerializationAllowed = 1;
+            lc.attrs = &attr;
+            lc.numAttrs = 1;
+            e = cudaLaunchKernelEx(&lc, page_table_spread_kernel, a);
+        }
+    }
+    if (e != cudaSuccess) return set_last_error(PSA_ERR_CUDA, std::string("page table launch: ") + cudaGetErrorString(e));
+    return PSA_OK;
+}
+
+}  // namespace
+}  // namespace psa
+
+extern "C" size_t psa_page_table_scratch_bytes(int32_t num_samples)
+{
+    if (num_samples < 0) return 0;
+    return 8 * (size_t(num_samples) + 1) + 4 * size_t(psa::scan_blocks_of(num_samples));
+}
+
+extern "C" psa_status_t psa_build_page_table(const int32_t *seq_lens, const int32_t *reserve_lens, int32_t num_samples,
+                                             const int32_t *free_pages, const int32_t *free_count, int32_t *free_count_out,
+                                             int32_t *page_indptr, int32_t *page_indices, int64_t num_entries, int32_t *token_indptr,
+                                             int64_t *slot_map, int64_t max_tokens, int32_t *lens_out, int32_t *status, void *scratch,
+                                             size_t scratch_bytes, void *cuda_stream)
+{
+    psa::PageTableArgs a{};
+    a.new_lens = seq_lens; a.limits = reserve_lens; a.num_samples = num_samples;
+    a.free_pages = free_pages; a.free_count = free_count; a.free_count_out = free_count_out;
+    a.page_indptr = page_indptr; a.page_indices = page_indices; a.num_entries = num_entries;
+    a.token_indptr = token_indptr; a.slot_map = slot_map; a.max_tokens = max_tokens;
+    a.lens_out = lens_out; a.status = status; a.build = true;
+    return psa::run(a, scratch, scratch_bytes, cuda_stream);
+}
+
+extern "C" psa_status_t psa_extend_page_table(const int32_t *held_lens, const int32_t *new_lens, const int32_t *max_lens,
+                                              int32_t num_samples, const int32_t *free_pages, const int32_t *free_count,
+                                              int32_t *free_count_out, const int32_t *page_indptr, int32_t *page_indices,
+                                              int64_t num_entries, int32_t *token_indptr, int64_t *slot_map, int64_t max_tokens,
+                                              int32_t *lens_out, int32_t *status, void *scratch, size_t scratch_bytes,
+                                              void *cuda_stream)
+{
+    psa::PageTableArgs a{};
+    a.held = held_lens; a.new_lens = new_lens; a.limits = max_lens; a.num_samples = num_samples;
+    a.free_pages = free_pages; a.free_count = free_count; a.free_count_out = free_count_out;
+    a.page_indptr = const_cast<int32_t *>(page_indptr); a.page_indices = page_indices; a.num_entries = num_entries;   // read only: build is false
+    a.token_indptr = token_indptr; a.slot_map = slot_map; a.max_tokens = max_tokens;
+    a.lens_out = lens_out; a.status = status; a.build = false;
+    return psa::run(a, scratch, scratch_bytes, cuda_stream);
+}

@@ -173,6 +173,21 @@ struct SuffixArgs {
 };
 int launch_suffix(const SuffixArgs &a, void *stream, std::string *err);
 
+// The suffix stage over a 4-bit cache (kv4.h)
+struct SuffixKv4Args {
+    const void *q, *pool;
+    int64_t stride_page, stride_cell;  // bytes
+    const int32_t *page_indptr, *page_indices, *suffix_lens;  // device
+    int32_t num_q_heads, num_kv_heads, head_dim;
+    float sm_scale;
+    const SuffixItem *items;      // device
+    const SampleInfo *sample_info;// device
+    int32_t num_items, chunk_tokens;
+    float *partial_o, *partial_lse;
+    bool after_prefix = false;  // launched right behind the prefix stage of the same step: may overlap it
+};
+int launch_suffix_kv4(const SuffixKv4Args &a, void *stream, std::string *err);
+
 struct MergeArgs {
     const SampleInfo *sample_info;  // device
     const int32_t *suffix_lens;     // device

@@ -1,0 +1,449 @@
+// Suffix stage over a cache held in 4 bits (layout: kv4.h): each sample's G query rows of one KV head against its own
+// generated tokens, in 16-token pages scattered through a pool of cells.  Same place in a step, same partial results
+// and same online softmax (running maximum, row sum, un-normalised accumulator, one division at the end) as the bf16 stage.
+//
+// The cache is never expanded.  With value = s * code + b per (token, group of 32 channels),
+//     S[t, row]   = sum_g s[t, g] * (q[row, g] . code[t, g])  +  sum_g b[t, g] * (sum of q[row] over the group)
+//     O[row, ch]  = sum_t (p[row, t] * s[t, g]) * (code[t, ch] - 8)  +  sum_t p[row, t] * (b[t, g] + 8 s[t, g])
+// so scales multiply scores and probabilities, of which there are 8 per token, instead of 2 D channels per token, and the
+// matrix instructions run on the bare codes.  A code becomes a bf16 operand by ONE and-operation: the bit pattern of a small
+// whole number n is the subnormal bf16 n * 2^-133, exactly, and a nibble left in place at bits 4-7 is 16 n * 2^-133; the other
+// two nibbles of a 16-bit half need one shift for both.  2^64 on the other operand keeps the products in fp32's normal range,
+// and the powers of two come out again in constants (scores) or once at the end (outputs).  5 instructions unpack 8 codes.
+//   * scores: K codes come out of shared memory through ldmatrix with two 16-bit units = 8 channels of one token per
+//     register; the four masked forms of that register are A operands of two m16n8k16 products whose B operands hold q in the
+//     matching channel order (loaded that way once per block), odd nibbles' q divided by 16.
+//   * outputs: V codes come through ldmatrix.trans, so that a register holds one unit (4 channels) of two neighbouring tokens:
+//     each masked form is a row pair of V^T.  Odd nibbles are rows 8-15 of the product, 16 times too large until the end.
+//   * the offset term of the scores is one more product, parameters x (group sums of q, split into two bf16 numbers: 2^-16
+//     relative); the offset term of the outputs is one more product, parameters^T x p.
+//   * rounding: p * s and p are rounded to bf16 (2^-8 relative at most, zero mean) before they meet the codes and the offsets.  With
+//     codes centred on 8 both terms stay as small as the values themselves; uncentred, their errors would not cancel as the
+//     terms do.  The centring is a product with a constant -8 on the same rounded operand, hence exact.
+// Bound: HBM at 1.25 * D bytes per (token, KV head) while the unpacking and the products keep up; one block per (sample, KV
+// head, token chunk), 4 warps with a private ring of kStages cells each, filled by 16-byte cp.async.
+// Slots of the last page beyond the sample's length hold whatever the pool held: their scores are set to -inf and their
+// parameters to zero, so nothing of them (NaN bit patterns included) reaches a result.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include "kv4.h"
+
+namespace psa {
+namespace {
+
+constexpr int kWarps = 4;
+constexpr int kStages = 4;
+constexpr float kRescaleThreshold = 8.f;  // log2 units: the reference maximum may lag this far behind
+constexpr float kTwo64 = 18446744073709551616.f;
+constexpr float kUnscaleEven = 590295810358705651712.f;     // 2^69 = 2^133 / 2^64
+constexpr float kUnscaleOdd = 36893488147419103232.f;       // 2^65: odd nibbles stand 4 bits higher
+
+__device__ __forceinline__ uint32_t smem_u32(const void *p) { return uint32_t(__cvta_generic_to_shared(p)); }
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;\n" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;\n" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void ldmatrix_x4(uint32_t addr, uint32_t (&r)[4])
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];\n"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldmatrix_x4_trans(uint32_t addr, uint32_t (&r)[4])
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];\n"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldmatrix_x2(uint32_t addr, uint32_t &r0, uint32_t &r1)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x2.shared.b16 {%0,%1}, [%2];\n" : "=r"(r0), "=r"(r1) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldmatrix_x2_trans(uint32_t addr, uint32_t &r0, uint32_t &r1)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x2.trans.shared.b16 {%0,%1}, [%2];\n" : "=r"(r0), "=r"(r1) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void lds64(uint32_t addr, uint32_t &r0, uint32_t &r1)
+{
+    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];\n" : "=r"(r0), "=r"(r1) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t addr)
+{
+    uint32_t r;
+    asm volatile("ld.shared.u32 %0, [%1];\n" : "=r"(r) : "r"(addr) : "memory");
+    return r;
+}
+// D(16x8, f32) += A(16x16, bf16, row) * B(16x8, bf16, col)
+__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t movmatrix_trans(uint32_t a)
+{
+    uint32_t d;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;\n" : "=r"(d) : "r"(a));
+    return d;
+}
+__device__ __forceinline__ float fast_exp2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<uint32_t *>(&v);
+}
+__device__ __forceinline__ float lo_f32(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float hi_f32(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+template <int D>
+struct Kv4Smem {
+    static constexpr int kWarpBytes = kStages * Kv4Cell<D>::kBytes;
+    static constexpr int kTotal = kWarps * kWarpBytes;
+};
+
+template <int D, int G>
+__global__ void __launch_bounds__(kWarps * 32, 4)
+suffix_kv4_kernel(const __nv_bfloat16 *__restrict__ q, const unsigned char *__restrict__ pool, int64_t stride_page,
+                  int64_t stride_cell, const int32_t *__restrict__ page_indptr, const int32_t *__restrict__ page_indices,
+                  const int32_t *__restrict__ suffix_lens, const SuffixItem *__restrict__ items,
+                  const SampleInfo *__restrict__ sample_info, int num_q_heads, int chunk_tokens, float scale_log2,
+                  float *__restrict__ partial_o, float *__restrict__ partial_lse, int first_of_step)
+{
+    using C = Kv4Cell<D>;
+    using L = Kv4Smem<D>;
+    constexpr int NG = C::kGroups;
+    constexpr int kChunks = C::kBytes / 16;
+    extern __shared__ __align__(128) unsigned char smem_raw[];
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int4 item = __ldg(reinterpret_cast<const int4 *>(items + blockIdx.x));   // plan data, bound long before
+    const int s = item.x, kv = item.y, tok0 = item.z, prow0 = item.w;
+    // Alone (or first) in its step this grid is a programmatic dependent of whatever precedes it and waits before it touches
+    // anything that may have been written there; behind a prefix stage the prefix blocks have waited already.
+    if (first_of_step) {
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    }
+    int S = __ldg(suffix_lens + s);
+    S = min(S, __ldg(&sample_info[s].suf_len_bound));
+    const int n_tok = min(S - tok0, chunk_tokens);
+    if (n_tok <= 0) return;  // the merge stage derives the chunk count from the same length
+    const int n_pages = (n_tok + kPageSize - 1) / kPageSize;
+    const int my_pages = (n_pages - warp + kWarps - 1) / kWarps;  // pages warp, warp+4, ...
+    const int32_t *my_page_ids = page_indices + __ldg(page_indptr + s) + tok0 / kPageSize;
+
+    const uint32_t warp_smem = smem_u32(smem_raw) + warp * L::kWarpBytes;
+    const unsigned char *head = pool + int64_t(kv) * stride_cell + lane * 16;
+
+    // page ids 32 at a time per warp: lane l holds the id of page number 32 g + l, for the group in use and the next one
+    auto load_ids = [&](int g) {
+        const int i = g * 32 + lane;
+        return i < my_pages ? __ldg(my_page_ids + warp + i * kWarps) : 0;
+    };
+    int ids_cur = load_ids(0), ids_nxt = load_ids(1);
+    auto issue_page = [&](int i) {   // called with i = 0, 1, 2, ... in order
+        if (i > 0 && (i & 31) == 0) {
+            ids_cur = ids_nxt;
+            ids_nxt = load_ids((i >> 5) + 1);
+        }
+        const int64_t page = __shfl_sync(0xffffffffu, ids_cur, i & 31);
+        if (i < my_pages) {
+            const uint32_t dst = warp_smem + (i % kStages) * C::kBytes + lane * 16;
+            const unsigned char *src = head + page * stride_page;
+#pragma unroll
+            for (int c = 0; c < kChunks; c += 32)
+                if (c + 32 <= kChunks || lane < kChunks - c) cp_async16(dst + c * 16, src + c * 16);
+        }
+        cp_async_commit();  // an empty group keeps the group count uniform
+    };
+#pragma unroll
+    for (int i = 0; i < kStages - 1; ++i) issue_page(i);
+
+    // ---- Q as B operands (rows lane / 4; rows >= G stay zero).  c = lane % 4 owns channels 8 c .. 8 c + 7 of each group, in
+    // the order in which the masked registers of K present them: (0, 4), (1, 5)/16, (2, 6), (3, 7)/16.
+    const int qrow = lane >> 2, c4 = lane & 3;
+    uint32_t qb[NG][4];
+    uint32_t qs0 = 0u, qs1 = 0u;   // group sums of q (times the softmax scale), high and low bf16 part, where the offsets stand
+    {
+        float gsum[NG];
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            uint4 w{};
+            if (qrow < G) w = __ldg(reinterpret_cast<const uint4 *>(q + (size_t(s) * num_q_heads + size_t(kv) * G + qrow) * D + g * 32 + c4 * 8));
+            const float f[8] = {lo_f32(w.x), hi_f32(w.x), lo_f32(w.y), hi_f32(w.y), lo_f32(w.z), hi_f32(w.z), lo_f32(w.w), hi_f32(w.w)};
+            qb[g][0] = pack_bf16(f[0] * kTwo64, f[4] * kTwo64);
+            qb[g][1] = pack_bf16(f[1] * (kTwo64 / 16), f[5] * (kTwo64 / 16));
+            qb[g][2] = pack_bf16(f[2] * kTwo64, f[6] * kTwo64);
+            qb[g][3] = pack_bf16(f[3] * (kTwo64 / 16), f[7] * (kTwo64 / 16));
+            float t = ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+            t += __shfl_xor_sync(0xffffffffu, t, 1);
+            t += __shfl_xor_sync(0xffffffffu, t, 2);
+            gsum[g] = t * scale_log2;
+        }
+        // parameter row of a token, as pairs: D = 128: {s0 s1} {s2 s3} {b0 b1} {b2 b3};  D = 64: {s0 s1} {b0 b1} of K, then of V
+        constexpr int kFirst = D == 128 ? 2 : 1;
+#pragma unroll
+        for (int i = 0; i < NG / 2; ++i)
+            if (c4 == kFirst + i) {
+                qs0 = pack_bf16(gsum[2 * i], gsum[2 * i + 1]);
+                qs1 = pack_bf16(gsum[2 * i] - lo_f32(qs0), gsum[2 * i + 1] - hi_f32(qs0));
+            }
+    }
+    const float score_scale = scale_log2 * kUnscaleEven;
+
+    // A thread holds query rows r0 = 2 * (lane % 4) and r0 + 1: scores of tokens u and u + 8, outputs of channels 4 u .. 4 u + 3 of
+    // each group, u = lane / 4.
+    const int u = lane >> 2, r0 = c4 * 2;
+    float o[NG][2][4];   // [group][channels 4u, 4u + 1 | 4u + 2, 4u + 3][rows r0, r0 + 1 of the even, of the odd channel]
+    float ob[4] = {0.f, 0.f, 0.f, 0.f};   // parameters^T p: row u of the parameter row
+#pragma unroll
+    for (int g = 0; g < NG; ++g)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) o[g][h][0] = o[g][h][1] = o[g][h][2] = o[g][h][3] = 0.f;
+    float m_ref[2] = {-INFINITY, -INFINITY};
+    float l_part[2] = {0.f, 0.f};
+
+    // row addresses of the matrix loads inside a cell: matrix lane / 8, row lane % 8; matrices = (tokens 0-7, 8-15) x two groups
+    const int mat = lane >> 3, mrow = lane & 7;
+    const int mtok = (mat & 1) * 8 + mrow;
+    uint32_t code_at[NG / 2];
+#pragma unroll
+    for (int p = 0; p < NG / 2; ++p) code_at[p] = C::chunk(mtok, 2 * p + (mat >> 1));
+    const uint32_t pk_at = C::kParamOff + (lane & 15) * 16;
+    const uint32_t pv_at = pk_at + (D == 128 ? 16 * kPageSize : 0);
+
+    for (int i = 0; i < my_pages; ++i) {
+        __syncwarp();
+        issue_page(i + kStages - 1);   // refills the slot read in iteration i - 1
+        cp_async_wait<kStages - 1>();
+        __syncwarp();
+
+        const int valid = min(kPageSize, n_tok - (warp + i * kWarps) * kPageSize);
+        const uint32_t cell = warp_smem + (i % kStages) * C::kBytes;
+
+        // ---- scores of 16 tokens x 8 rows
+        float x[4] = {0.f, 0.f, 0.f, 0.f};   // the offset term, already in log2 units
+        {
+            uint32_t a0, a1;
+            ldmatrix_x2(cell + pk_at, a0, a1);
+            mma_bf16(x, a0, a1, a0, a1, qs0, qs1);
+        }
+        float acc[NG][4];
+#pragma unroll
+        for (int p = 0; p < NG / 2; ++p) {
+            uint32_t w[4];
+            ldmatrix_x4(cell + code_at[p], w);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int g = 2 * p + h;
+                const uint32_t lo = w[2 * h], hi = w[2 * h + 1], lo8 = lo >> 8, hi8 = hi >> 8;
+                acc[g][0] = acc[g][1] = acc[g][2] = acc[g][3] = 0.f;
+                mma_bf16(acc[g], lo & 0x000F000Fu, hi & 0x000F000Fu, lo & 0x00F000F0u, hi & 0x00F000F0u, qb[g][0], qb[g][1]);
+                mma_bf16(acc[g], lo8 & 0x000F000Fu, hi8 & 0x000F000Fu, lo8 & 0x00F000F0u, hi8 & 0x00F000F0u, qb[g][2], qb[g][3]);
+            }
+        }
+        {
+            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+            uint32_t sl[2], sh[2];   // scales of tokens u and u + 8
+            const uint32_t at = cell + C::params(0, 0) + u * 16;
+            if constexpr (D == 128) {
+                lds64(at, sl[0], sl[1]);
+                lds64(at + 128, sh[0], sh[1]);
+            } else {
+                sl[0] = lds32(at);
+                sh[0] = lds32(at + 128);
+            }
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                const float a = (g & 1) ? hi_f32(sl[g >> 1]) : lo_f32(sl[g >> 1]), b = (g & 1) ? hi_f32(sh[g >> 1]) : lo_f32(sh[g >> 1]);
+                sum[0] = fmaf(a, acc[g][0], sum[0]);
+                sum[1] = fmaf(a, acc[g][1], sum[1]);
+                sum[2] = fmaf(b, acc[g][2], sum[2]);
+                sum[3] = fmaf(b, acc[g][3], sum[3]);
+            }
+#pragma unroll
+            for (int t = 0; t < 4; ++t) x[t] = fmaf(sum[t], score_scale, x[t]);
+        }
+        if (valid < kPageSize) {
+            if (u >= valid) x[0] = x[1] = -INFINITY;
+            if (u + 8 >= valid) x[2] = x[3] = -INFINITY;
+        }
+        const float tmax0 = fmaxf(x[0], x[2]), tmax1 = fmaxf(x[1], x[3]);
+        if (__any_sync(0xffffffffu, tmax0 > m_ref[0] + kRescaleThreshold || tmax1 > m_ref[1] + kRescaleThreshold)) {
+            float rmax0 = tmax0, rmax1 = tmax1;   // over the 8 lanes that hold the same rows
+#pragma unroll
+            for (int sh = 4; sh < 32; sh <<= 1) {
+                rmax0 = fmaxf(rmax0, __shfl_xor_sync(0xffffffffu, rmax0, sh));
+                rmax1 = fmaxf(rmax1, __shfl_xor_sync(0xffffffffu, rmax1, sh));
+            }
+            const float m_new0 = fmaxf(m_ref[0], rmax0), m_new1 = fmaxf(m_ref[1], rmax1);
+            if (m_new0 > m_ref[0] || m_new1 > m_ref[1]) {
+                const float alpha0 = m_new0 > m_ref[0] ? fast_exp2(m_ref[0] - m_new0) : 1.f;  // m_ref = -inf gives 0
+                const float alpha1 = m_new1 > m_ref[1] ? fast_exp2(m_ref[1] - m_new1) : 1.f;
+                l_part[0] *= alpha0; l_part[1] *= alpha1;
+#pragma unroll
+                for (int g = 0; g < NG; ++g)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) { o[g][h][0] *= alpha0; o[g][h][1] *= alpha1; o[g][h][2] *= alpha0; o[g][h][3] *= alpha1; }
+                ob[0] *= alpha0; ob[1] *= alpha1;
+                m_ref[0] = m_new0; m_ref[1] = m_new1;
+            }
+        }
+        float p[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) p[t] = fast_exp2(x[t] - m_ref[t & 1]);  // masked slots: exp2(-inf) = 0
+        l_part[0] += p[0] + p[2];
+        l_part[1] += p[1] + p[3];
+
+        // ---- outputs.  The offset term: parameters^T (rows: the 8 units of a parameter row) x p
+        {
+            uint32_t a0, a2;
+            ldmatrix_x2_trans(cell + pv_at, a0, a2);
+            if (valid < kPageSize) {   // parameters of slots beyond the length: tokens 2 c4, 2 c4 + 1 and those + 8
+                a0 &= (r0 < valid ? 0x0000FFFFu : 0u) | (r0 + 1 < valid ? 0xFFFF0000u : 0u);
+                a2 &= (r0 + 8 < valid ? 0x0000FFFFu : 0u) | (r0 + 9 < valid ? 0xFFFF0000u : 0u);
+            }
+            mma_bf16(ob, a0, 0u, a2, 0u, movmatrix_trans(pack_bf16(p[0], p[1])), movmatrix_trans(pack_bf16(p[2], p[3])));
+        }
+        uint32_t sl[2] = {0u, 0u}, sh[2] = {0u, 0u};
+        {
+            const uint32_t at = cell + C::params(1, 0) + u * 16;
+            if constexpr (D == 128) {
+                lds64(at, sl[0], sl[1]);
+                lds64(at + 128, sh[0], sh[1]);
+            } else {
+                sl[0] = lds32(at);
+                sh[0] = lds32(at + 128);
+            }
+            if (valid < kPageSize) {
+                if (u >= valid) sl[0] = sl[1] = 0u;
+                if (u + 8 >= valid) sh[0] = sh[1] = 0u;
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) p[t] *= kTwo64;
+#pragma unroll
+        for (int pr = 0; pr < NG / 2; ++pr) {
+            uint32_t w[4];
+            ldmatrix_x4_trans(cell + C::kCodeBytes + code_at[pr], w);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int g = 2 * pr + h;
+                const float a = h ? hi_f32(sl[pr]) : lo_f32(sl[pr]), b = h ? hi_f32(sh[pr]) : lo_f32(sh[pr]);
+                const uint32_t pb0 = movmatrix_trans(pack_bf16(p[0] * a, p[1] * a)), pb1 = movmatrix_trans(pack_bf16(p[2] * b, p[3] * b));
+                const uint32_t lo = w[2 * h], hi = w[2 * h + 1], lo8 = lo >> 8, hi8 = hi >> 8;
+                mma_bf16(o[g][0], lo & 0x000F000Fu, lo & 0x00F000F0u, hi & 0x000F000Fu, hi & 0x00F000F0u, pb0, pb1);
+                mma_bf16(o[g][1], lo8 & 0x000F000Fu, lo8 & 0x00F000F0u, hi8 & 0x000F000Fu, hi8 & 0x00F000F0u, pb0, pb1);
+                // - 8 for every code, on the same rounded operand: rows 0-7 hold codes, rows 8-15 sixteen times codes
+                mma_bf16(o[g][0], 0x80088008u, 0x80808080u, 0x80088008u, 0x80808080u, pb0, pb1);
+                mma_bf16(o[g][1], 0x80088008u, 0x80808080u, 0x80088008u, 0x80808080u, pb0, pb1);
+            }
+        }
+    }
+    cp_async_wait<0>();
+
+    // ---- finish the row sums over the 8 lanes that share the rows, then combine the 4 warps through shared memory
+    float l_row[2] = {l_part[0], l_part[1]};
+#pragma unroll
+    for (int sh = 4; sh < 32; sh <<= 1) {
+        l_row[0] += __shfl_xor_sync(0xffffffffu, l_row[0], sh);
+        l_row[1] += __shfl_xor_sync(0xffffffffu, l_row[1], sh);
+    }
+    __syncthreads();  // every warp is done with its ring: reuse the memory
+    float *sm_o = reinterpret_cast<float *>(smem_raw);           // [kWarps][G][D]
+    float *sm_m = sm_o + kWarps * G * D;                          // [kWarps][G]
+    float *sm_l = sm_m + kWarps * G;                              // [kWarps][G]
+    // unit of V's scale and of its offset of group g in the parameter row
+    constexpr int kScaleUnit = D == 128 ? 0 : 4, kOffsetUnit = D == 128 ? 4 : 6;
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const float sum_s = __shfl_sync(0xffffffffu, ob[h], (kScaleUnit + g) * 4 + c4);
+            const float sum_b = __shfl_sync(0xffffffffu, ob[h], (kOffsetUnit + g) * 4 + c4);
+            const float base = fmaf(8.f, sum_s, sum_b);
+            if (r0 + h < G) {
+                const float4 v = make_float4(fmaf(o[g][0][h], kUnscaleEven, base), fmaf(o[g][0][2 + h], kUnscaleOdd, base),
+                                             fmaf(o[g][1][h], kUnscaleEven, base), fmaf(o[g][1][2 + h], kUnscaleOdd, base));
+                *reinterpret_cast<float4 *>(sm_o + (warp * G + r0 + h) * D + g * 32 + u * 4) = v;
+            }
+        }
+    }
+    if (u == 0) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (r0 + h < G) { sm_m[warp * G + r0 + h] = m_ref[h]; sm_l[warp * G + r0 + h] = l_row[h]; }
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < G * D; e += kWarps * 32) {
+        const int g = e / D, d = e % D;
+        float top = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, sm_m[w * G + g]);
+        float z = 0.f, acc = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            const float mw = sm_m[w * G + g];
+            const float f = mw == -INFINITY ? 0.f : fast_exp2(mw - top);
+            z += f * sm_l[w * G + g];
+            acc += f * sm_o[(w * G + g) * D + d];
+        }
+        partial_o[size_t(prow0 + g) * D + d] = acc / z;
+        if (d == 0) partial_lse[prow0 + g] = (top + log2f(z)) * 0.6931471805599453f;
+    }
+    if (!first_of_step) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
+template <int D, int G>
+int launch_one(const SuffixKv4Args &a, cudaStream_t st)
+{
+    using L = Kv4Smem<D>;
+    static_assert(L::kTotal >= int(sizeof(float)) * kWarps * G * (D + 2), "combine buffer must fit in the ring");
+    auto kern = suffix_kv4_kernel<D, G>;
+    static PerDeviceOnce once;   // per instantiation
+    const int cfg_rc = once.ensure([&] {
+        cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kTotal);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(kern, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+        return int(e);
+    });
+    if (cfg_rc != 0) return cfg_rc;
+    cudaLaunchConfig_t lc{};
+    lc.gridDim = dim3(a.num_items);
+    lc.blockDim = dim3(kWarps * 32);
+    lc.dynamicSmemBytes = L::kTotal;
+    lc.stream = st;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    lc.attrs = &attr;
+    lc.numAttrs = 1;
+    return int(cudaLaunchKernelEx(&lc, kern, static_cast<const __nv_bfloat16 *>(a.q), static_cast<const unsigned char *>(a.pool),
+                                  a.stride_page, a.stride_cell, a.page_indptr, a.page_indices, a.suffix_lens, a.items, a.sample_info,
+                                  a.num_q_heads, a.chunk_tokens, a.sm_scale * 1.4426950408889634f, a.partial_o, a.partial_lse,
+                                  a.after_prefix ? 0 : 1));
+}
+
+}  // namespace
+
+int launch_suffix_kv4(const SuffixKv4Args &a, void *stream, std::string *err)
+{
+    if (a.num_items == 0) return 0;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const int G = a.num_q_heads / a.num_kv_heads;
+    int rc = -1;
+#define PSA_CASE(DD, GG) if (a.head_dim == DD && G == GG) rc = launch_one<DD, GG>(a, st);
+    PSA_CASE(128, 1) PSA_CASE(128, 2) PSA_CASE(128, 4) PSA_CASE(128, 8)
+    PSA_CASE(64, 1) PSA_CASE(64, 2) PSA_CASE(64, 4) PSA_CASE(64, 8)
+#undef PSA_CASE
+    if (rc != 0 && err) *err = rc < 0 ? "suffix (4-bit): unsupported shape" : std::string("suffix (4-bit) launch: ") + cudaGetErrorString(cudaError_t(rc));
+    return rc;
+}
+
+}  // namespace psa
