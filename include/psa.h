@@ -450,9 +450,12 @@ psa_status_t psa_load_kv4(const void *pool, const int64_t pool_strides[2], int64
                           const int64_t kv_strides[2], int32_t *status, void *cuda_stream);
 /*
  * psa_decode / psa_decode_suffix with the samples' own tokens in such a pool (the shared prefix stays bf16).  Any plan serves
- * either cache; every other argument is that of psa_decode.  K and V enter the products as their exact codes; probabilities are
- * rounded to bf16 as in psa_decode.
+ * either cache with the same results up to rounding; psa_plan_create_kv4 makes, from a plan for psa_decode, the plan of the same
+ * problem (and forced knobs) whose pieces are sized for a 4-bit cache; it is bound, queried and destroyed like any other.  Every
+ * other argument is that of psa_decode.  K and V enter the products as their exact codes; probabilities are rounded to bf16 as in
+ * psa_decode.
  */
+psa_status_t psa_plan_create_kv4(const psa_plan_t *plan, psa_plan_t **out_plan);
 psa_status_t psa_decode_kv4(const psa_plan_t *plan, const void *q, const void *prefix_k, const void *prefix_v,
                             const int64_t prefix_strides[2], const void *kv4_pool, const int64_t pool_strides[2],
                             const int32_t *page_indptr, const int32_t *page_indices, const int32_t *suffix_lens,

@@ -21,7 +21,7 @@ EXPORTED_SYMBOLS = [
     "psa_decode", "psa_decode_static", "psa_static_check_status", "psa_static_selftest_bounded_wait", "psa_decode_prefix", "psa_decode_suffix", "psa_decode_merge",
     "psa_decode_host_staging_bytes", "psa_decode_host", "psa_check_status", "psa_selftest_bounded_wait", "psa_append_kv", "psa_append_kv_alloc", "psa_validate_page_table", "psa_sample_scratch_bytes", "psa_sample_tokens", "psa_sample_tokens_at", "psa_attn_task",
     "psa_page_table_scratch_bytes", "psa_build_page_table", "psa_extend_page_table", "psa_read_status", "psa_kv4_cell_bytes", "psa_store_kv4",
-    "psa_load_kv4", "psa_decode_kv4", "psa_decode_suffix_kv4", "psa_process_logits", "psa_mark_tokens",
+    "psa_load_kv4", "psa_plan_create_kv4", "psa_decode_kv4", "psa_decode_suffix_kv4", "psa_process_logits", "psa_mark_tokens",
     "psa_status_string", "psa_last_error_message", "psa_version",
 ]
 
@@ -147,6 +147,8 @@ def library():
         lib.psa_store_kv4.argtypes = [P, P, POINTER(c_int64), P, c_int64, c_int32, c_int32, P, POINTER(c_int64), c_int64, P, P]
         lib.psa_load_kv4.restype = c_int32
         lib.psa_load_kv4.argtypes = [P, POINTER(c_int64), c_int64, P, c_int64, c_int32, c_int32, P, P, POINTER(c_int64), P, P]
+        lib.psa_plan_create_kv4.restype = c_int32
+        lib.psa_plan_create_kv4.argtypes = [P, POINTER(c_void_p)]
         lib.psa_decode_kv4.restype = c_int32
         lib.psa_decode_kv4.argtypes = [P, P, P, P, POINTER(c_int64), P, POINTER(c_int64), P, P, P, P, P, P, c_size_t, P]
         lib.psa_decode_suffix_kv4.restype = c_int32
@@ -224,6 +226,19 @@ class Plan:
                                                ctypes.byref(handle)))
         self._h = handle
         self.workspace = None
+        self._kv4 = None
+
+    def for_kv4(self) -> "Plan":
+        """The plan of the same problem whose pieces are sized for a 4-bit cache (psa_plan_create_kv4), with a workspace of its own.
+        decode_kv4 uses it in place of this one; it is made once and kept."""
+        if self._kv4 is None:
+            handle = c_void_p()
+            _check(library().psa_plan_create_kv4(self._h, ctypes.byref(handle)))
+            plan = Plan.__new__(Plan)
+            plan.__dict__.update(self.__dict__, _h=handle, workspace=None)
+            plan._kv4 = plan
+            self._kv4 = plan
+        return self._kv4
 
     def __del__(self):
         if getattr(self, "_h", None):
@@ -280,6 +295,11 @@ class Plan:
         _check(library().psa_selftest_bounded_wait(_ptr(self.workspace), self.workspace.numel(), int(limit_ns), _stream_ptr(stream)))
 
     def check_status(self, stream=None):
+        """Raise if a step left a device-side error in the workspace (that of for_kv4 included), and clear it."""
+        if self._kv4 is not None and self._kv4 is not self and self._kv4.workspace is not None:
+            self._kv4.check_status(stream)
+            if self.workspace is None:
+                return
         _check(library().psa_check_status(self._h, _ptr(self.workspace), _stream_ptr(stream)))
 
 
@@ -591,11 +611,16 @@ def load_kv4(pool, slot_map, out_k, out_v, *, status=None, stream=None):
 
 def decode_kv4(plan: Plan, q, prefix_k, prefix_v, pool, page_indptr, page_indices, suffix_lens, out, lse, *, prefix_strides=None,
                stream=None, stage="all"):
-    """psa_decode_kv4 (or its suffix stage): decode with the samples' own tokens in a 4-bit pool [pages, Hkv, kv4_cell_bytes(D)]
-    uint8.  Everything else as for decode."""
+    """psa_decode_kv4 (or one of its stages): decode with the samples' own tokens in a 4-bit pool [pages, Hkv, kv4_cell_bytes(D)]
+    uint8.  Everything else as for decode; the work lists and the workspace are those of plan.for_kv4()."""
     import torch
-    if stage not in ("all", "suffix"):
+    if stage not in ("all", "prefix", "suffix", "merge"):
         raise ValueError(stage)
+    plan = plan.for_kv4()
+    if stage in ("prefix", "merge"):
+        decode(plan, q, prefix_k, prefix_v, None, None, page_indptr, page_indices, suffix_lens, out, lse, prefix_strides=prefix_strides,
+               stream=stream, stage=stage)
+        return
     if pool.dtype is not torch.uint8 or pool.dim() != 3 or pool.shape[1] != plan.num_kv_heads:
         raise ValueError("pool must be uint8 [pages, num_kv_heads, kv4_cell_bytes(head_dim)]")
     pst = _outer_strides(pool, 20 * plan.head_dim, "pool")

@@ -69,7 +69,7 @@ extern "C" {
 static psa_status_t create_impl(const psa_config_t *cfg, int32_t num_groups, const int32_t *first_sample,
                                 const int32_t *n_samples, const int32_t *token_len, int32_t num_samples,
                                 const int32_t *suffix_lens, psa_plan_t **out_plan, const int32_t *token_begin = nullptr,
-                                int64_t total_tokens = 0, bool causal = false)
+                                int64_t total_tokens = 0, bool causal = false, bool kv4 = false)
 {
     if (!cfg || !out_plan) return fail(PSA_ERR_INVALID_ARG, "null cfg or out_plan");
     *out_plan = nullptr;
@@ -85,7 +85,7 @@ static psa_status_t create_impl(const psa_config_t *cfg, int32_t num_groups, con
     if (!plan) return fail(PSA_ERR_INVALID_ARG, "out of host memory");
     std::string err;
     psa_status_t st = psa::build_plan(c, num_groups, first_sample, n_samples, token_len, token_begin, total_tokens, causal, num_samples,
-                                      suffix_lens, plan, &err);
+                                      suffix_lens, kv4, plan, &err);
     if (st != PSA_OK) {
         delete plan;
         return fail(st, err);
@@ -149,6 +149,15 @@ psa_status_t psa_plan_create_prefill(const psa_config_t *cfg, int32_t num_prompt
     if (c.prefix_rows_per_item == 0) c.prefix_rows_per_item = psa::kPrefixRowsPerItem;
     return create_impl(&c, int32_t(first.size()), first.data(), count.data(), len.data(), int32_t(total), zero_suffix.data(),
                        out_plan, begin.data(), total, true);
+}
+
+psa_status_t psa_plan_create_kv4(const psa_plan_t *plan, psa_plan_t **out_plan)
+{
+    if (!plan || !out_plan) return fail(PSA_ERR_INVALID_ARG, "null plan or out_plan");
+    *out_plan = nullptr;
+    if (plan->causal) return fail(PSA_ERR_INVALID_ARG, "a prefill plan has no suffix cache");
+    return create_impl(&plan->cfg, plan->num_prefixes, plan->group_first_sample.data(), plan->group_n_samples.data(),
+                       plan->group_token_len.data(), plan->num_samples, plan->suffix_len_bounds.data(), out_plan, nullptr, 0, false, true);
 }
 
 psa_status_t psa_plan_destroy(psa_plan_t *plan)

@@ -20,6 +20,14 @@ namespace {
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
+// How fast the suffix stage streams its cache, bytes per microsecond, on the whole machine and on one SM beside others
+// that are busy with prefix blocks.  bf16: bound by HBM (see below).  4-bit: bound by the SMs that unpack it (256 samples x
+// U[0,4096] tokens x 8 heads, 671 MB: 117 us on 148 SMs).
+struct SuffixRates {
+    double machine, per_sm;
+};
+constexpr SuffixRates kBf16Rates{6.4e6, 7.2e4}, kKv4Rates{5.7e6, 3.9e4};
+
 // Prefix: every (group, kv head, row group) streams ceil(L / 128) key tiles; with at most T tiles per item a
 // group of `tiles` tiles is cut into ceil(tiles / T) items.  Items are dispatched longest first to the SMs, so
 // the stage takes about max(longest item, sum of items / SMs); every split also costs a partial result per row
@@ -38,7 +46,7 @@ inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 // items of 64 tiles against 385 us as 128 items of 32 tiles.
 int choose_prefix_tiles_per_item(const std::vector<int64_t> &tiles, const std::vector<int64_t> &groups,
                                  const std::vector<int64_t> &partial_rows_per_split, double step_weight, int head_dim, int num_sms,
-                                 double sm_time_weight, bool owns_sm, double prefix_bytes, double suffix_bytes)
+                                 double sm_time_weight, bool owns_sm, double prefix_bytes, double suffix_bytes, const SuffixRates &rates)
 {
     int64_t max_tiles = 0;
     for (int64_t t : tiles) max_tiles = std::max(max_tiles, t);
@@ -85,7 +93,7 @@ int choose_prefix_tiles_per_item(const std::vector<int64_t> &tiles, const std::v
         }
         double cost = stage + partial;
         if (owns_sm && suffix_bytes > 0.0) {
-            const double step_us = 1.5, hbm = 6.4e6 /* bytes per us */, per_sm = 7.2e4;
+            const double step_us = 1.5, hbm = rates.machine, per_sm = rates.per_sm;
             const double t_prefix = stage * step_us;
             const double free_sms = std::max(0.0, double(num_sms) - items);
             const double rate = std::max(0.0, std::min(hbm - prefix_bytes / t_prefix, free_sms * per_sm));
@@ -132,11 +140,46 @@ int choose_suffix_chunk(const int32_t *lens, int n, int num_kv_heads, int num_sm
     return best;
 }
 
+// Suffix over a 4-bit cache.  A token costs a third of the bytes but about the same instructions, so the stage is bound by
+// its warps rather than by HBM: `slots` blocks share the SMs (four per SM, two where a small prefix block sits beside them,
+// none where a prefix block owns the SM) at a fair share of about 69 tokens per us each, an SM with fewer blocks runs each
+// of them faster (up to 2.2 times), and a block's start and end cost as much as 320 tokens.  Estimate in tokens:
+//     max( (sum of tokens + 320 per item) / min(slots, items),  longest item * max(blocks per SM / 4, 0.45) + 320 ).
+// Measured, suffix stage alone, chunks of 4096 / 1024 / 256 tokens: 64 samples x U[1,4096] x 8 heads 57.7 / 33.4 / 44.8 us (items of
+// 4096 leave a third of the machine idle at the end), 256 samples 120 / 143 / 246 us, 32 samples x U[0,1024] 11.5 / 11.5 / 10.1 us;
+// beside a 4096-token prefix the last one's step takes 16.8 us with 512-token chunks, 18.4 with 256, 18.5 with 832.
+int choose_kv4_chunk(const int32_t *lens, int n, int num_kv_heads, int num_sms, int prefix_items, bool prefix_owns_sm)
+{
+    const double overhead = 320.0;
+    const int beside = std::min(prefix_items, num_sms);
+    double slots = prefix_owns_sm ? 4.0 * (num_sms - beside) : 4.0 * num_sms - 2.0 * beside;
+    if (slots <= 0.0) slots = 4.0 * num_sms;   // every SM has its prefix block first and is free afterwards
+    double best_cost = std::numeric_limits<double>::infinity();
+    int best = 64;
+    for (int C = 64; C <= 8192; C += (C < 1024 ? 64 : (C < 4096 ? 256 : 1024))) {
+        double sum = 0.0, items = 0.0;
+        int64_t longest = 0;
+        for (int s = 0; s < n; ++s) {
+            const int64_t S = lens[s];
+            if (S <= 0) continue;
+            const int64_t chunks = ceil_div(S, C);
+            sum += double(num_kv_heads) * (double(S) + overhead * double(chunks));
+            items += double(num_kv_heads) * double(chunks);
+            longest = std::max<int64_t>(longest, std::min<int64_t>(S, C));
+        }
+        if (items == 0.0) break;
+        const double share = std::max(std::min(4.0, items * 4.0 / slots) / 4.0, 0.45);
+        const double cost = std::max(sum / std::min(slots, items), double(longest) * share + overhead);
+        if (cost < best_cost * 0.999) { best_cost = cost; best = C; }
+    }
+    return best;
+}
+
 }  // namespace
 
 psa_status_t build_plan(const psa_config_t &cfg, int32_t P, const int32_t *first_sample, const int32_t *n_samples,
                         const int32_t *prefix_lens, const int32_t *token_begin, int64_t total_tokens_arg, bool causal,
-                        int32_t num_samples, const int32_t *suffix_lens, psa_plan *plan, std::string *err)
+                        int32_t num_samples, const int32_t *suffix_lens, bool kv4, psa_plan *plan, std::string *err)
 {
     auto fail = [&](psa_status_t st, const char *msg) { if (err) *err = msg; return st; };
     if (cfg.num_q_heads <= 0 || cfg.num_kv_heads <= 0 || cfg.num_q_heads % cfg.num_kv_heads != 0)
@@ -198,10 +241,10 @@ psa_status_t build_plan(const psa_config_t &cfg, int32_t P, const int32_t *first
                                                            : (max_rows >= 2 * kPrefixRowsPerItem ? kPrefixRowsPerItem : kPrefixTileRows);
     const int samples_per_group = rows_per_item / G;
     bool any_suffix = false;
-    double suffix_kv_bytes = 0.0, prefix_kv_bytes = 0.0;   // K and V, bf16, all heads
+    double suffix_kv_bytes = 0.0, prefix_kv_bytes = 0.0;   // K and V, all heads
     for (int64_t s = 0; s < B; ++s) {
         any_suffix = any_suffix || suffix_lens[s] > 0;
-        suffix_kv_bytes += 4.0 * double(suffix_lens[s]) * cfg.num_kv_heads * cfg.head_dim;
+        suffix_kv_bytes += (kv4 ? 1.25 : 4.0) * double(suffix_lens[s]) * cfg.num_kv_heads * cfg.head_dim;
     }
     for (int p = 0; p < P; ++p)
         if (n_samples[p] > 0) prefix_kv_bytes += 4.0 * double(prefix_lens[p]) * cfg.num_kv_heads * cfg.head_dim;
@@ -215,7 +258,8 @@ psa_status_t build_plan(const psa_config_t &cfg, int32_t P, const int32_t *first
                       ? cfg.prefix_tiles_per_item
                       : choose_prefix_tiles_per_item(tiles, groups, rows_per_split, rows_per_item > kPrefixTileRows ? 1.3 : 1.0,
                                                      cfg.head_dim, cfg.num_sms, any_suffix ? 0.35 : 0.0,
-                                                     rows_per_item > kPrefixTileRows, prefix_kv_bytes, suffix_kv_bytes);
+                                                     rows_per_item > kPrefixTileRows, prefix_kv_bytes, suffix_kv_bytes,
+                                                     kv4 ? kKv4Rates : kBf16Rates);
     plan->prefix_tiles_per_item = T;
 
     plan->sample_info.assign(size_t(B), SampleInfo{});
@@ -277,7 +321,10 @@ psa_status_t build_plan(const psa_config_t &cfg, int32_t P, const int32_t *first
     });
 
     // ---- suffix items
-    const int C = cfg.suffix_chunk_tokens > 0 ? cfg.suffix_chunk_tokens : choose_suffix_chunk(suffix_lens, int(B), cfg.num_kv_heads, cfg.num_sms);
+    const int C = cfg.suffix_chunk_tokens > 0 ? cfg.suffix_chunk_tokens
+                  : kv4 ? choose_kv4_chunk(suffix_lens, int(B), cfg.num_kv_heads, cfg.num_sms, int(plan->prefix_items.size()),
+                                           plan->prefix_max_rows_per_item > kPrefixTileRows)
+                        : choose_suffix_chunk(suffix_lens, int(B), cfg.num_kv_heads, cfg.num_sms);
     plan->suffix_chunk_tokens = C;
     plan->suffix_items.clear();
     for (int64_t s = 0; s < B; ++s) {

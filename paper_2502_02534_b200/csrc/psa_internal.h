@@ -132,10 +132,10 @@ struct PerDeviceOnce {
 // Shared-prefix group g: `token_len[g]` consecutive tokens of the packed prefix arrays (groups back to back, in
 // order) attended by samples [first_sample[g], first_sample[g] + n_samples[g]).
 // token_begin == nullptr: group g starts where group g-1 ends.  causal: keys beyond a row's own packed token index
-// are masked (prefill: "samples" are the prompt's tokens).
+// are masked (prefill: "samples" are the prompt's tokens).  kv4: the suffix work is sized for a 4-bit cache.
 psa_status_t build_plan(const psa_config_t &cfg, int32_t num_groups, const int32_t *first_sample, const int32_t *n_samples,
                         const int32_t *token_len, const int32_t *token_begin, int64_t total_tokens, bool causal,
-                        int32_t num_samples, const int32_t *suffix_lens, psa_plan *plan, std::string *err);
+                        int32_t num_samples, const int32_t *suffix_lens, bool kv4, psa_plan *plan, std::string *err);
 
 // Launchers (one per .cu file). All enqueue on `stream` and return a CUDA error code (0 = ok).
 struct PrefixArgs {

@@ -9,12 +9,13 @@
 // matrix instructions run on the bare codes.  A code becomes a bf16 operand by ONE and-operation: the bit pattern of a small
 // whole number n is the subnormal bf16 n * 2^-133, exactly, and a nibble left in place at bits 4-7 is 16 n * 2^-133; the other
 // two nibbles of a 16-bit half need one shift for both.  2^64 on the other operand keeps the products in fp32's normal range,
-// and the powers of two come out again in constants (scores) or once at the end (outputs).  5 instructions unpack 8 codes.
+// and the powers of two come out again in constants (scores) or once at the end (outputs).  5 instructions unpack 8 codes of K.
 //   * scores: K codes come out of shared memory through ldmatrix with two 16-bit units = 8 channels of one token per
 //     register; the four masked forms of that register are A operands of two m16n8k16 products whose B operands hold q in the
 //     matching channel order (loaded that way once per block), odd nibbles' q divided by 16.
-//   * outputs: V codes come through ldmatrix.trans, so that a register holds one unit (4 channels) of two neighbouring tokens:
-//     each masked form is a row pair of V^T.  Odd nibbles are rows 8-15 of the product, 16 times too large until the end.
+//   * outputs: V codes come through ldmatrix.trans, so that a register holds one unit (4 channels) of two neighbouring tokens.
+//     Rows 0-7 of a product take whole bytes (even code + 16 * odd code, still a subnormal whole number), rows 8-15 the upper
+//     nibbles alone; the even channel is their difference, taken once at the end.  4 instructions per 8 codes.
 //   * the offset term of the scores is one more product, parameters x (group sums of q, split into two bf16 numbers: 2^-16
 //     relative); the offset term of the outputs is one more product, parameters^T x p.
 //   * rounding: p * s and p are rounded to bf16 (2^-8 relative at most, zero mean) before they meet the codes and the offsets.  With
@@ -26,6 +27,8 @@
 // parameters to zero, so nothing of them (NaN bit patterns included) reaches a result.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
+
+#include <type_traits>
 
 #include "kv4.h"
 
@@ -57,14 +60,6 @@ __device__ __forceinline__ void ldmatrix_x4_trans(uint32_t addr, uint32_t (&r)[4
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];\n"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
-__device__ __forceinline__ void ldmatrix_x2(uint32_t addr, uint32_t &r0, uint32_t &r1)
-{
-    asm volatile("ldmatrix.sync.aligned.m8n8.x2.shared.b16 {%0,%1}, [%2];\n" : "=r"(r0), "=r"(r1) : "r"(addr) : "memory");
-}
-__device__ __forceinline__ void ldmatrix_x2_trans(uint32_t addr, uint32_t &r0, uint32_t &r1)
-{
-    asm volatile("ldmatrix.sync.aligned.m8n8.x2.trans.shared.b16 {%0,%1}, [%2];\n" : "=r"(r0), "=r"(r1) : "r"(addr) : "memory");
-}
 __device__ __forceinline__ void lds64(uint32_t addr, uint32_t &r0, uint32_t &r1)
 {
     asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];\n" : "=r"(r0), "=r"(r1) : "r"(addr) : "memory");
@@ -75,17 +70,31 @@ __device__ __forceinline__ uint32_t lds32(uint32_t addr)
     asm volatile("ld.shared.u32 %0, [%1];\n" : "=r"(r) : "r"(addr) : "memory");
     return r;
 }
-// D(16x8, f32) += A(16x16, bf16, row) * B(16x8, bf16, col)
+// D(16x8, f32) = A(16x16, bf16, row) * B(16x8, bf16, col)
+__device__ __forceinline__ void mma_bf16_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};\n"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+// D = C + A * B
+__device__ __forceinline__ void mma_bf16_from(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, const float (&c)[4])
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};\n"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
+}
+// D += A * B
 __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ uint32_t movmatrix_trans(uint32_t a)
 {
     uint32_t d;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;\n" : "=r"(d) : "r"(a));
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;\n" : "=r"(d) : "r"(a));
     return d;
 }
 __device__ __forceinline__ float fast_exp2(float x)
@@ -201,13 +210,16 @@ suffix_kv4_kernel(const __nv_bfloat16 *__restrict__ q, const unsigned char *__re
     // A thread holds query rows r0 = 2 * (lane % 4) and r0 + 1: scores of tokens u and u + 8, outputs of channels 4 u .. 4 u + 3 of
     // each group, u = lane / 4.
     const int u = lane >> 2, r0 = c4 * 2;
-    float o[NG][2][4];   // [group][channels 4u, 4u + 1 | 4u + 2, 4u + 3][rows r0, r0 + 1 of the even, of the odd channel]
+    float o[NG][2][4];   // [group][channels 4u, 4u + 1 | 4u + 2, 4u + 3][rows r0, r0 + 1: even + 16 odd channel | 16 odd channel]
     float ob[4] = {0.f, 0.f, 0.f, 0.f};   // parameters^T p: row u of the parameter row
 #pragma unroll
     for (int g = 0; g < NG; ++g)
 #pragma unroll
         for (int h = 0; h < 2; ++h) o[g][h][0] = o[g][h][1] = o[g][h][2] = o[g][h][3] = 0.f;
-    float m_ref[2] = {-INFINITY, -INFINITY};
+    // Minus the reference maximum of rows r0, r0 + 1: what the scores' accumulators start from, so that the products deliver scores
+    // relative to it.
+    float base[4] = {0.f, 0.f, 0.f, 0.f};   // [0], [1] of tokens u, again for tokens u + 8
+    float limit = -INFINITY;   // scores above it move the reference; the first page's do in any case
     float l_part[2] = {0.f, 0.f};
 
     // row addresses of the matrix loads inside a cell: matrix lane / 8, row lane % 8; matrices = (tokens 0-7, 8-15) x two groups
@@ -216,41 +228,61 @@ suffix_kv4_kernel(const __nv_bfloat16 *__restrict__ q, const unsigned char *__re
     uint32_t code_at[NG / 2];
 #pragma unroll
     for (int p = 0; p < NG / 2; ++p) code_at[p] = C::chunk(mtok, 2 * p + (mat >> 1));
+    // parameter rows: K's as A rows (tokens 0-7, 8-15) with both halves of k alike; V's transposed, tokens 0-7 and 8-15 along k, the
+    // second half of the rows a copy that nobody reads
     const uint32_t pk_at = C::kParamOff + (lane & 15) * 16;
-    const uint32_t pv_at = pk_at + (D == 128 ? 16 * kPageSize : 0);
+    const uint32_t pv_at = C::params(D == 128 ? 1 : 0, 0) + ((mat >> 1) * 8 + mrow) * 16;
+    // the centring operand - (8 + 16 * 8) for bytes, - 16 * 8 for upper nibbles, kept in registers
+    uint32_t centre[4];
+    asm volatile("mov.b32 %0, 0x80888088;\n\tmov.b32 %1, 0x80808080;\n\tmov.b32 %2, 0x80888088;\n\tmov.b32 %3, 0x80808080;"
+                 : "=r"(centre[0]), "=r"(centre[1]), "=r"(centre[2]), "=r"(centre[3]));
 
-    for (int i = 0; i < my_pages; ++i) {
+    // page i of the warp; `last`: some of its slots may lie beyond the length
+    auto work = [&](int i, auto last) {
         __syncwarp();
-        issue_page(i + kStages - 1);   // refills the slot read in iteration i - 1
+        issue_page(i + kStages - 1);   // refills the slot read in the iteration before
         cp_async_wait<kStages - 1>();
         __syncwarp();
 
-        const int valid = min(kPageSize, n_tok - (warp + i * kWarps) * kPageSize);
         const uint32_t cell = warp_smem + (i % kStages) * C::kBytes;
-
-        // ---- scores of 16 tokens x 8 rows
-        float x[4] = {0.f, 0.f, 0.f, 0.f};   // the offset term, already in log2 units
-        {
-            uint32_t a0, a1;
-            ldmatrix_x2(cell + pk_at, a0, a1);
-            mma_bf16(x, a0, a1, a0, a1, qs0, qs1);
-        }
-        float acc[NG][4];
-#pragma unroll
-        for (int p = 0; p < NG / 2; ++p) {
-            uint32_t w[4];
-            ldmatrix_x4(cell + code_at[p], w);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int g = 2 * p + h;
-                const uint32_t lo = w[2 * h], hi = w[2 * h + 1], lo8 = lo >> 8, hi8 = hi >> 8;
-                acc[g][0] = acc[g][1] = acc[g][2] = acc[g][3] = 0.f;
-                mma_bf16(acc[g], lo & 0x000F000Fu, hi & 0x000F000Fu, lo & 0x00F000F0u, hi & 0x00F000F0u, qb[g][0], qb[g][1]);
-                mma_bf16(acc[g], lo8 & 0x000F000Fu, hi8 & 0x000F000Fu, lo8 & 0x00F000F0u, hi8 & 0x00F000F0u, qb[g][2], qb[g][3]);
+        const int valid = n_tok - (warp + i * kWarps) * kPageSize;   // at least 16 unless this is the last page
+        if constexpr (last.value) {
+            // slots beyond the length get zero as V's parameters
+            if ((lane & 15) >= valid) {
+                const uint32_t at = cell + C::params(1, 0) + (lane & 15) * 16;
+                if (D == 128) asm volatile("st.shared.v2.u32 [%0], {%1, %1};" ::"r"(at + (lane >> 4) * 8), "r"(0) : "memory");
+                else asm volatile("st.shared.u32 [%0], %1;" ::"r"(at + (lane >> 4) * 4), "r"(0) : "memory");
             }
+            __syncwarp();
         }
+
+        // ---- scores of 16 tokens x 8 rows, in log2 units relative to the row's reference
+        float x[4];
         {
-            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+            {
+                uint32_t a[4];
+                ldmatrix_x4(cell + pk_at, a);
+                mma_bf16_from(x, a[0], a[1], a[2], a[3], qs0, qs1, base);
+            }
+            float acc[NG][4];
+#pragma unroll
+            for (int p = 0; p < NG / 2; ++p) {
+                uint32_t w[4];
+                ldmatrix_x4(cell + code_at[p], w);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int g = 2 * p + h;
+                    const uint32_t lo = w[2 * h], hi = w[2 * h + 1];
+                    mma_bf16_first(acc[g], lo & 0x000F000Fu, hi & 0x000F000Fu, lo & 0x00F000F0u, hi & 0x00F000F0u, qb[g][0], qb[g][1]);
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int g = 2 * p + h;
+                    const uint32_t lo8 = w[2 * h] >> 8, hi8 = w[2 * h + 1] >> 8;
+                    mma_bf16(acc[g], lo8 & 0x000F000Fu, hi8 & 0x000F000Fu, lo8 & 0x00F000F0u, hi8 & 0x00F000F0u, qb[g][2], qb[g][3]);
+                }
+            }
+            float sum[4];
             uint32_t sl[2], sh[2];   // scales of tokens u and u + 8
             const uint32_t at = cell + C::params(0, 0) + u * 16;
             if constexpr (D == 128) {
@@ -263,57 +295,58 @@ suffix_kv4_kernel(const __nv_bfloat16 *__restrict__ q, const unsigned char *__re
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
                 const float a = (g & 1) ? hi_f32(sl[g >> 1]) : lo_f32(sl[g >> 1]), b = (g & 1) ? hi_f32(sh[g >> 1]) : lo_f32(sh[g >> 1]);
-                sum[0] = fmaf(a, acc[g][0], sum[0]);
-                sum[1] = fmaf(a, acc[g][1], sum[1]);
-                sum[2] = fmaf(b, acc[g][2], sum[2]);
-                sum[3] = fmaf(b, acc[g][3], sum[3]);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) sum[t] = g == 0 ? (t < 2 ? a : b) * acc[g][t] : fmaf(t < 2 ? a : b, acc[g][t], sum[t]);
             }
 #pragma unroll
             for (int t = 0; t < 4; ++t) x[t] = fmaf(sum[t], score_scale, x[t]);
         }
-        if (valid < kPageSize) {
+        if constexpr (last.value) {
             if (u >= valid) x[0] = x[1] = -INFINITY;
             if (u + 8 >= valid) x[2] = x[3] = -INFINITY;
         }
         const float tmax0 = fmaxf(x[0], x[2]), tmax1 = fmaxf(x[1], x[3]);
-        if (__any_sync(0xffffffffu, tmax0 > m_ref[0] + kRescaleThreshold || tmax1 > m_ref[1] + kRescaleThreshold)) {
+        if (__any_sync(0xffffffffu, fmaxf(tmax0, tmax1) > limit)) {
             float rmax0 = tmax0, rmax1 = tmax1;   // over the 8 lanes that hold the same rows
 #pragma unroll
             for (int sh = 4; sh < 32; sh <<= 1) {
                 rmax0 = fmaxf(rmax0, __shfl_xor_sync(0xffffffffu, rmax0, sh));
                 rmax1 = fmaxf(rmax1, __shfl_xor_sync(0xffffffffu, rmax1, sh));
             }
-            const float m_new0 = fmaxf(m_ref[0], rmax0), m_new1 = fmaxf(m_ref[1], rmax1);
-            if (m_new0 > m_ref[0] || m_new1 > m_ref[1]) {
-                const float alpha0 = m_new0 > m_ref[0] ? fast_exp2(m_ref[0] - m_new0) : 1.f;  // m_ref = -inf gives 0
-                const float alpha1 = m_new1 > m_ref[1] ? fast_exp2(m_ref[1] - m_new1) : 1.f;
+            // the reference moves to the row's maximum: down only the first time, when nothing has been summed yet
+            const bool first = i == 0;
+            const float d0 = first ? rmax0 : fmaxf(rmax0, 0.f), d1 = first ? rmax1 : fmaxf(rmax1, 0.f);
+            if (!first) {
+                const float alpha0 = fast_exp2(-d0), alpha1 = fast_exp2(-d1);
                 l_part[0] *= alpha0; l_part[1] *= alpha1;
 #pragma unroll
                 for (int g = 0; g < NG; ++g)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) { o[g][h][0] *= alpha0; o[g][h][1] *= alpha1; o[g][h][2] *= alpha0; o[g][h][3] *= alpha1; }
                 ob[0] *= alpha0; ob[1] *= alpha1;
-                m_ref[0] = m_new0; m_ref[1] = m_new1;
             }
+            x[0] -= d0; x[2] -= d0; x[1] -= d1; x[3] -= d1;
+            base[0] -= d0; base[1] -= d1;
+            base[2] = base[0]; base[3] = base[1];
+            limit = kRescaleThreshold;
         }
-        float p[4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) p[t] = fast_exp2(x[t] - m_ref[t & 1]);  // masked slots: exp2(-inf) = 0
-        l_part[0] += p[0] + p[2];
-        l_part[1] += p[1] + p[3];
 
-        // ---- outputs.  The offset term: parameters^T (rows: the 8 units of a parameter row) x p
         {
-            uint32_t a0, a2;
-            ldmatrix_x2_trans(cell + pv_at, a0, a2);
-            if (valid < kPageSize) {   // parameters of slots beyond the length: tokens 2 c4, 2 c4 + 1 and those + 8
-                a0 &= (r0 < valid ? 0x0000FFFFu : 0u) | (r0 + 1 < valid ? 0xFFFF0000u : 0u);
-                a2 &= (r0 + 8 < valid ? 0x0000FFFFu : 0u) | (r0 + 9 < valid ? 0xFFFF0000u : 0u);
+            float p[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) p[t] = fast_exp2(x[t]);  // masked slots: exp2(-inf) = 0
+            l_part[0] += p[0] + p[2];
+            l_part[1] += p[1] + p[3];
+
+            // ---- outputs.  The offset term: parameters^T (rows: the 8 units of a parameter row) x p
+            {
+                uint32_t a[4];
+                ldmatrix_x4_trans(cell + pv_at, a);
+                mma_bf16(ob, a[0], a[1], a[2], a[3], movmatrix_trans(pack_bf16(p[0], p[1])), movmatrix_trans(pack_bf16(p[2], p[3])));
             }
-            mma_bf16(ob, a0, 0u, a2, 0u, movmatrix_trans(pack_bf16(p[0], p[1])), movmatrix_trans(pack_bf16(p[2], p[3])));
-        }
-        uint32_t sl[2] = {0u, 0u}, sh[2] = {0u, 0u};
-        {
+#pragma unroll
+            for (int t = 0; t < 4; ++t) p[t] *= kTwo64;
+            uint32_t sl[2], sh[2];
             const uint32_t at = cell + C::params(1, 0) + u * 16;
             if constexpr (D == 128) {
                 lds64(at, sl[0], sl[1]);
@@ -322,31 +355,36 @@ suffix_kv4_kernel(const __nv_bfloat16 *__restrict__ q, const unsigned char *__re
                 sl[0] = lds32(at);
                 sh[0] = lds32(at + 128);
             }
-            if (valid < kPageSize) {
-                if (u >= valid) sl[0] = sl[1] = 0u;
-                if (u + 8 >= valid) sh[0] = sh[1] = 0u;
+#pragma unroll
+            for (int pr = 0; pr < NG / 2; ++pr) {
+                uint32_t w[4], pb0[2], pb1[2];
+                ldmatrix_x4_trans(cell + C::kCodeBytes + code_at[pr], w);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float a = h ? hi_f32(sl[pr]) : lo_f32(sl[pr]), b = h ? hi_f32(sh[pr]) : lo_f32(sh[pr]);
+                    pb0[h] = movmatrix_trans(pack_bf16(p[0] * a, p[1] * a));
+                    pb1[h] = movmatrix_trans(pack_bf16(p[2] * b, p[3] * b));
+                }
+                // rows 0-7: whole bytes (even code + 16 odd code), rows 8-15: their upper nibbles; bytes 0, 2 and bytes 1, 3
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t lo = w[2 * h], hi = w[2 * h + 1];
+                    const uint32_t lo1 = __byte_perm(lo, 0u, 0x4341), hi1 = __byte_perm(hi, 0u, 0x4341);
+                    mma_bf16(o[2 * pr + h][0], lo & 0x00FF00FFu, lo & 0x00F000F0u, hi & 0x00FF00FFu, hi & 0x00F000F0u, pb0[h], pb1[h]);
+                    mma_bf16(o[2 * pr + h][1], lo1, lo1 & 0x00F000F0u, hi1, hi1 & 0x00F000F0u, pb0[h], pb1[h]);
+                }
+                // - 8 for every code, on the same rounded operand
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    mma_bf16(o[2 * pr + h][0], centre[0], centre[1], centre[2], centre[3], pb0[h], pb1[h]);
+                    mma_bf16(o[2 * pr + h][1], centre[0], centre[1], centre[2], centre[3], pb0[h], pb1[h]);
+                }
             }
         }
-#pragma unroll
-        for (int t = 0; t < 4; ++t) p[t] *= kTwo64;
-#pragma unroll
-        for (int pr = 0; pr < NG / 2; ++pr) {
-            uint32_t w[4];
-            ldmatrix_x4_trans(cell + C::kCodeBytes + code_at[pr], w);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int g = 2 * pr + h;
-                const float a = h ? hi_f32(sl[pr]) : lo_f32(sl[pr]), b = h ? hi_f32(sh[pr]) : lo_f32(sh[pr]);
-                const uint32_t pb0 = movmatrix_trans(pack_bf16(p[0] * a, p[1] * a)), pb1 = movmatrix_trans(pack_bf16(p[2] * b, p[3] * b));
-                const uint32_t lo = w[2 * h], hi = w[2 * h + 1], lo8 = lo >> 8, hi8 = hi >> 8;
-                mma_bf16(o[g][0], lo & 0x000F000Fu, lo & 0x00F000F0u, hi & 0x000F000Fu, hi & 0x00F000F0u, pb0, pb1);
-                mma_bf16(o[g][1], lo8 & 0x000F000Fu, lo8 & 0x00F000F0u, hi8 & 0x000F000Fu, hi8 & 0x00F000F0u, pb0, pb1);
-                // - 8 for every code, on the same rounded operand: rows 0-7 hold codes, rows 8-15 sixteen times codes
-                mma_bf16(o[g][0], 0x80088008u, 0x80808080u, 0x80088008u, 0x80808080u, pb0, pb1);
-                mma_bf16(o[g][1], 0x80088008u, 0x80808080u, 0x80088008u, 0x80808080u, pb0, pb1);
-            }
-        }
-    }
+    };
+    int i = 0;
+    for (; i + 1 < my_pages; ++i) work(i, std::false_type{});
+    if (i < my_pages) work(i, std::true_type{});
     cp_async_wait<0>();
 
     // ---- finish the row sums over the 8 lanes that share the rows, then combine the 4 warps through shared memory
@@ -368,10 +406,10 @@ suffix_kv4_kernel(const __nv_bfloat16 *__restrict__ q, const unsigned char *__re
         for (int h = 0; h < 2; ++h) {
             const float sum_s = __shfl_sync(0xffffffffu, ob[h], (kScaleUnit + g) * 4 + c4);
             const float sum_b = __shfl_sync(0xffffffffu, ob[h], (kOffsetUnit + g) * 4 + c4);
-            const float base = fmaf(8.f, sum_s, sum_b);
+            const float offset = fmaf(8.f, sum_s, sum_b);
             if (r0 + h < G) {
-                const float4 v = make_float4(fmaf(o[g][0][h], kUnscaleEven, base), fmaf(o[g][0][2 + h], kUnscaleOdd, base),
-                                             fmaf(o[g][1][h], kUnscaleEven, base), fmaf(o[g][1][2 + h], kUnscaleOdd, base));
+                const float4 v = make_float4(fmaf(o[g][0][h] - o[g][0][2 + h], kUnscaleEven, offset), fmaf(o[g][0][2 + h], kUnscaleOdd, offset),
+                                             fmaf(o[g][1][h] - o[g][1][2 + h], kUnscaleEven, offset), fmaf(o[g][1][2 + h], kUnscaleOdd, offset));
                 *reinterpret_cast<float4 *>(sm_o + (warp * G + r0 + h) * D + g * 32 + u * 4) = v;
             }
         }
@@ -379,23 +417,28 @@ suffix_kv4_kernel(const __nv_bfloat16 *__restrict__ q, const unsigned char *__re
     if (u == 0) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
-            if (r0 + h < G) { sm_m[warp * G + r0 + h] = m_ref[h]; sm_l[warp * G + r0 + h] = l_row[h]; }
+            if (r0 + h < G) {
+                sm_m[warp * G + r0 + h] = my_pages > 0 ? -base[h] : -INFINITY;
+                sm_l[warp * G + r0 + h] = l_row[h];
+            }
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < G * D; e += kWarps * 32) {
-        const int g = e / D, d = e % D;
+    for (int e = threadIdx.x; e < G * D / 4; e += kWarps * 32) {
+        const int g = e / (D / 4), d = e % (D / 4) * 4;
         float top = -INFINITY;
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) top = fmaxf(top, sm_m[w * G + g]);
-        float z = 0.f, acc = 0.f;
+        float z = 0.f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
             const float mw = sm_m[w * G + g];
             const float f = mw == -INFINITY ? 0.f : fast_exp2(mw - top);
+            const float4 v = *reinterpret_cast<const float4 *>(sm_o + (w * G + g) * D + d);
             z += f * sm_l[w * G + g];
-            acc += f * sm_o[(w * G + g) * D + d];
+            acc.x += f * v.x; acc.y += f * v.y; acc.z += f * v.z; acc.w += f * v.w;
         }
-        partial_o[size_t(prow0 + g) * D + d] = acc / z;
+        *reinterpret_cast<float4 *>(partial_o + size_t(prow0 + g) * D + d) = make_float4(acc.x / z, acc.y / z, acc.z / z, acc.w / z);
         if (d == 0) partial_lse[prow0 + g] = (top + log2f(z)) * 0.6931471805599453f;
     }
     if (!first_of_step) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");

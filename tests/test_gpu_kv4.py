@@ -299,7 +299,7 @@ def test_a_group_that_is_not_finite_stays_in_its_sample_and_head():
 
 def test_pool_strides_stage_by_stage_and_far_pages():
     import torch
-    from paper_2502_02534_b200 import decode, decode_kv4
+    from paper_2502_02534_b200 import decode_kv4
     w = problem(128, 2, 2, [64], [4], [100, 3, 0, 48], seed=10)
     n = w["kv4_pool"].shape[0]
     whole, _ = run(w)
@@ -311,12 +311,10 @@ def test_pool_strides_stage_by_stage_and_far_pages():
     assert np.array_equal(out, whole)
     # the stages one by one give what the fused step gives
     plan, d = make_plan(w, "f32"), on_device(w)
-    plan.bind_workspace()
     o = torch.zeros((4, 4, 128), device="cuda")
     l = torch.zeros((4, 4), device="cuda")  # noqa: E741
-    decode(plan, d["q"], d["prefix_k"], d["prefix_v"], None, None, None, None, None, o, l, stage="prefix")
-    decode_kv4(plan, d["q"], None, None, d["pool"], d["page_indptr"], d["page_indices"], d["suffix_lens"], None, None, stage="suffix")
-    decode(plan, d["q"], None, None, None, None, None, None, d["suffix_lens"], o, l, stage="merge")
+    for stage in ("prefix", "suffix", "merge"):
+        decode_kv4(plan, d["q"], d["prefix_k"], d["prefix_v"], d["pool"], d["page_indptr"], d["page_indices"], d["suffix_lens"], o, l, stage=stage)
     assert np.array_equal(o.double().cpu().numpy(), whole)
     # pages beyond 2^32 bytes
     far = torch.empty((2 ** 32 // 5120 + n, 2, 2560), dtype=torch.uint8, device="cuda")
@@ -360,6 +358,38 @@ def test_captured_graph_and_two_streams():
     for (o, l), (ro, rl), plan in zip(outs, ref, plans):  # noqa: E741
         plan.check_status()
         assert np.array_equal(o.double().cpu().numpy(), ro) and np.array_equal(l.double().cpu().numpy(), rl)
+
+
+def test_one_plan_serves_both_caches_side_by_side_and_its_own_lists_serve_the_4_bit_one():
+    import torch
+    from paper_2502_02534_b200 import decode, library
+    from paper_2502_02534_b200.binding import _check, _strides2, default_pool_strides
+    w = problem(128, 4, 2, [300], [5], [400, 0, 33, 64, 1], seed=14)
+    plan, d = make_plan(w, "f32"), on_device(w)
+    plan.bind_workspace()
+    lists, before = plan.suffix_items().copy(), plan.workspace_bytes
+    out4, lse4 = run(w, plan=plan, d=d)
+    within_bounds(w, out4, lse4)
+    assert np.array_equal(plan.suffix_items(), lists) and plan.workspace_bytes == before
+    assert plan.for_kv4() is plan.for_kv4() and plan.for_kv4().for_kv4() is plan.for_kv4()
+    assert plan.for_kv4().workspace.data_ptr() != plan.workspace.data_ptr()
+    # a bf16 step on the same plan object, between two 4-bit ones
+    pages = w["kv4_pool"].shape[0]
+    pk, pv = (bf(wl.normal_bf16((pages, 2, 16, 128), 15, i)) for i in range(2))
+    o, l = torch.zeros((5, 8, 128), device="cuda"), torch.zeros((5, 8), device="cuda")  # noqa: E741
+    decode(plan, d["q"], d["prefix_k"], d["prefix_v"], pk, pv, d["page_indptr"], d["page_indices"], d["suffix_lens"], o, l)
+    first = o.clone()
+    assert np.array_equal(run(w, plan=plan, d=d)[0], out4)
+    decode(plan, d["q"], d["prefix_k"], d["prefix_v"], pk, pv, d["page_indptr"], d["page_indices"], d["suffix_lens"], o, l)
+    assert torch.equal(first, o) and default_pool_strides(plan)[2] == 128
+    # the plan made for bf16, handed to the 4-bit entry point itself
+    _check(library().psa_decode_kv4(plan.handle, d["q"].data_ptr(), d["prefix_k"].data_ptr(), d["prefix_v"].data_ptr(), _strides2(256, 128),
+                                    d["pool"].data_ptr(), _strides2(*d["pool"].stride()[:2]), d["page_indptr"].data_ptr(), d["page_indices"].data_ptr(),
+                                    d["suffix_lens"].data_ptr(), o.data_ptr(), l.data_ptr(), plan.workspace.data_ptr(), plan.workspace.numel(),
+                                    torch.cuda.current_stream().cuda_stream))
+    torch.cuda.synchronize()
+    plan.check_status()
+    within_bounds(w, o.double().cpu().numpy(), l.double().cpu().numpy())
 
 
 @pytest.mark.parametrize("seed", range(12))

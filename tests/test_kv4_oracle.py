@@ -121,7 +121,34 @@ def test_host_refusals():
         return lib.psa_decode_suffix_kv4(plan.handle, q, pool, st(*pst), FAKE, FAKE, FAKE, ws, size, None)
     assert decode(ws=None) == 3 and decode(size=n - 1) == 3 and decode(q=None) == 1 and decode(pool=None) == 1
     assert decode(pool=FAKE + 8) == 1 and decode(pst=(5120, 2552)) == 1 and decode(pst=(16, 2560)) == 1
+    handle = ctypes.c_void_p()
+    assert lib.psa_plan_create_kv4(None, ctypes.byref(handle)) == 1 and lib.psa_plan_create_kv4(plan.handle, None) == 1
+    causal = psa.Plan([], [], [], num_q_heads=8, num_kv_heads=2, head_dim=128, num_sms=148, prefill_prompt_lens=[40])
+    assert lib.psa_plan_create_kv4(causal.handle, ctypes.byref(handle)) == 1 and b"prefill" in lib.psa_last_error_message()
     assert lib.psa_decode_kv4(None, FAKE, FAKE, FAKE, st(256, 128), FAKE, st(5120, 2560), FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, n, None) == 1
+
+
+def test_the_4_bit_plan_covers_the_same_tokens_and_keeps_forced_knobs():
+    import paper_2502_02534_b200 as psa
+    rng = np.random.default_rng(0)
+    for _ in range(30):
+        P = int(rng.integers(1, 4))
+        n = rng.integers(0, 20, P)
+        lens = rng.integers(0, int(rng.choice([40, 700, 5000])), int(n.sum()))
+        kw = dict(num_q_heads=16, num_kv_heads=int(rng.choice([2, 8])), head_dim=128, num_sms=148)
+        plan = psa.Plan(rng.integers(0, 3000, P), n, lens, **kw)
+        four = plan.for_kv4()
+        C = four.info.suffix_chunk_tokens
+        want = {(s, h, t) for s in range(len(lens)) for h in range(kw["num_kv_heads"]) for t in range(0, int(lens[s]), C)}
+        items = four.suffix_items()
+        assert {tuple(int(x) for x in it[:3]) for it in items} == want and len(items) == len(want) and C % 64 == 0
+        rows = sorted(int(it[3]) for it in items)
+        G = 16 // kw["num_kv_heads"]
+        assert all(b - a >= G for a, b in zip(rows, rows[1:]))
+        keys = lambda p: sum(int(it[1]) * int(it[4]) for it in p.prefix_items())  # noqa: E731
+        assert keys(four) == keys(plan)
+        forced = psa.Plan(rng.integers(0, 3000, P), n, lens, suffix_chunk_tokens=192, prefix_tiles_per_item=3, **kw).for_kv4()
+        assert forced.info.suffix_chunk_tokens == 192 and forced.info.prefix_tiles_per_item <= 3
 
 
 def test_binding_refusals():
@@ -142,6 +169,6 @@ def test_binding_refusals():
         psa.decode_kv4(plan, k, k, k, pool[:, :1], slots, slots, slots, k, k)
     with pytest.raises(ValueError, match="current CUDA device"):
         psa.decode_kv4(plan, k, k, k, pool, slots, slots, slots, k, k)
-    with pytest.raises(ValueError):
-        psa.decode_kv4(plan, k, k, k, pool, slots, slots, slots, k, k, stage="merge")
+    with pytest.raises(ValueError, match="both"):
+        psa.decode_kv4(plan, k, k, k, pool, slots, slots, slots, k, k, stage="both")
     assert math.isclose(psa.kv4_cell_bytes(64), 1280)
