@@ -405,7 +405,7 @@ psa_status_t psa_attn_task(int32_t task, const void *q, const void *k, const voi
  * status PSA_ERR_BOUNDS -- when a length is negative, exceeds reserve_lens / max_lens or its list, when a page that it should hold
  * already is missing (a negative id), when its tokens or list entries do not fit max_tokens / num_entries (offsets are then cut
  * there), or when the stack has too few pages left; in that last case no later sample that needs a page gets one either.
- * At most 2^20 samples.  One launch for small batches, two otherwise; only enqueues work.
+ * At most 2^20 samples and 2^31 - 256 entries.  One launch for small batches, two otherwise; only enqueues work.
  */
 size_t psa_page_table_scratch_bytes(int32_t num_samples);
 psa_status_t psa_build_page_table(const int32_t *seq_lens, const int32_t *reserve_lens, int32_t num_samples, const int32_t *free_pages,

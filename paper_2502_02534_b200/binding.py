@@ -468,27 +468,44 @@ def host_staging_bytes(plan: Plan, n_prefix_tokens: int, n_pool_pages: int, n_pa
 
 # ---- page tables, the 4-bit cache and rules on logits.  These check the tensors they are given: type, layout, size, and that all of
 # ---- them live on the current CUDA device (ValueError otherwise); what the library itself refuses comes back as PsaError.
+# ---- The checks are written for the latency of a decode step: a handful of attribute reads per tensor, no per-call imports.
 
-def _flat(t, dtype, name, dev, size=None):
+_torch = None
+
+
+def _bind_torch():
+    """Module-level references for the functions below (torch is not needed to import this module)."""
+    global _torch, _i32_t, _i64_t, _u8_t, _bf16_t, _f32_t, _current_device, _raw_stream
+    import torch
+    _i32_t, _i64_t, _u8_t, _bf16_t, _f32_t = torch.int32, torch.int64, torch.uint8, torch.bfloat16, torch.float32
+    _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+    _torch = torch
+
+
+def _flat(t, dtype, name, dev, size=0):
     """Address of a contiguous tensor of at least `size` elements on device `dev` (None passes through)."""
     if t is None:
         return None
+    if t.dtype is dtype and t.get_device() == dev and t.is_contiguous() and t.numel() >= size:
+        return t.data_ptr()
     if t.dtype is not dtype:
         raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
-    if not t.is_contiguous() or (size is not None and t.numel() < size):
-        raise ValueError(f"{name} must be contiguous" + (f" and hold at least {size} elements" if size is not None else ""))
-    if t.get_device() != dev:
-        raise ValueError(f"{name} must be on the current CUDA device")
-    return t.data_ptr()
+    if not t.is_contiguous() or t.numel() < size:
+        raise ValueError(f"{name} must be contiguous" + (f" and hold at least {size} elements" if size else ""))
+    raise ValueError(f"{name} must be on the current CUDA device")
 
 
 def _device_of(t, name):
     """The device the call runs on: that of tensor `t`, which must be the current one."""
-    import torch
     dev = t.get_device()
-    if dev < 0 or dev != torch.cuda.current_device():
+    if dev < 0 or dev != _current_device():
         raise ValueError(f"{name} must be on the current CUDA device")
     return dev
+
+
+def _stream_on(stream, dev):
+    return _raw_stream(dev) if stream is None else _stream_ptr(stream)
 
 
 @functools.lru_cache(maxsize=256)
@@ -521,57 +538,64 @@ def build_page_table(seq_lens, free_pages, free_count, page_indptr, page_indices
     reserve_lens), pages from the stack free_pages[0 .. free_count), and the slot of every token.  Outputs: page_indptr [B+1],
     page_indices (any capacity), token_indptr [B+1], slot_map (any capacity), lens_out [B], free_count_out (free_count in place
     when None)."""
-    import torch
-    n, i32 = seq_lens.numel(), torch.int32
-    p_seq = _flat(seq_lens, i32, "seq_lens", seq_lens.get_device())
-    p_indptr, p_tokens = (_flat(t, i32, name, seq_lens.get_device(), n + 1) for t, name in ((page_indptr, "page_indptr"), (token_indptr, "token_indptr")))
+    if _torch is None:
+        _bind_torch()
+    i32, n, dev = _i32_t, seq_lens.numel(), seq_lens.get_device()
+    p_seq = _flat(seq_lens, i32, "seq_lens", dev)
+    p_indptr = _flat(page_indptr, i32, "page_indptr", dev, n + 1)
+    p_tokens = _flat(token_indptr, i32, "token_indptr", dev, n + 1)
     dev = _device_of(seq_lens, "seq_lens")
     if scratch is None:
         scratch = page_table_scratch(n)
+    p_count = _flat(free_count, i32, "free_count", dev, 1)
     _check(library().psa_build_page_table(
-        p_seq, _flat(reserve_lens, i32, "reserve_lens", dev, n), n, _flat(free_pages, i32, "free_pages", dev),
-        _flat(free_count, i32, "free_count", dev, 1), _flat(free_count if free_count_out is None else free_count_out, i32, "free_count_out", dev, 1),
-        p_indptr, _flat(page_indices, i32, "page_indices", dev), page_indices.numel(), p_tokens,
-        _flat(slot_map, torch.int64, "slot_map", dev), slot_map.numel(), _flat(lens_out, i32, "lens_out", dev, n),
-        _status_ptr(status, dev), _flat(scratch, torch.uint8, "scratch", dev), scratch.numel(), _stream_ptr(stream)))
+        p_seq, _flat(reserve_lens, i32, "reserve_lens", dev, n), n, _flat(free_pages, i32, "free_pages", dev), p_count,
+        p_count if free_count_out is None else _flat(free_count_out, i32, "free_count_out", dev, 1), p_indptr,
+        _flat(page_indices, i32, "page_indices", dev), page_indices.numel(), p_tokens, _flat(slot_map, _i64_t, "slot_map", dev), slot_map.numel(),
+        _flat(lens_out, i32, "lens_out", dev, n), _status_ptr(status, dev), _flat(scratch, _u8_t, "scratch", dev), scratch.numel(),
+        _stream_on(stream, dev)))
 
 
 def extend_page_table(held_lens, new_lens, free_pages, free_count, page_indptr, page_indices, token_indptr, slot_map, *, max_lens=None,
                       lens_out=None, free_count_out=None, status=None, scratch=None, stream=None):
     """psa_extend_page_table on torch CUDA tensors: new_lens more tokens for samples that hold held_lens, in existing page lists.
     Outputs as for build_page_table; lens_out and free_count_out may be held_lens and free_count themselves."""
-    import torch
-    n, i32 = held_lens.numel(), torch.int32
-    p_held = _flat(held_lens, i32, "held_lens", held_lens.get_device())
-    p_new = _flat(new_lens, i32, "new_lens", held_lens.get_device(), n)
-    p_indptr, p_tokens = (_flat(t, i32, name, held_lens.get_device(), n + 1) for t, name in ((page_indptr, "page_indptr"), (token_indptr, "token_indptr")))
+    if _torch is None:
+        _bind_torch()
+    i32, n, dev = _i32_t, held_lens.numel(), held_lens.get_device()
+    p_held = _flat(held_lens, i32, "held_lens", dev)
+    p_new = _flat(new_lens, i32, "new_lens", dev, n)
+    p_indptr = _flat(page_indptr, i32, "page_indptr", dev, n + 1)
+    p_tokens = _flat(token_indptr, i32, "token_indptr", dev, n + 1)
     dev = _device_of(held_lens, "held_lens")
     if scratch is None:
         scratch = page_table_scratch(n)
+    p_count = _flat(free_count, i32, "free_count", dev, 1)
     _check(library().psa_extend_page_table(
-        p_held, p_new, _flat(max_lens, i32, "max_lens", dev, n), n, _flat(free_pages, i32, "free_pages", dev),
-        _flat(free_count, i32, "free_count", dev, 1), _flat(free_count if free_count_out is None else free_count_out, i32, "free_count_out", dev, 1),
-        p_indptr, _flat(page_indices, i32, "page_indices", dev), page_indices.numel(), p_tokens,
-        _flat(slot_map, torch.int64, "slot_map", dev), slot_map.numel(), _flat(lens_out, i32, "lens_out", dev, n),
-        _status_ptr(status, dev), _flat(scratch, torch.uint8, "scratch", dev), scratch.numel(), _stream_ptr(stream)))
+        p_held, p_new, _flat(max_lens, i32, "max_lens", dev, n), n, _flat(free_pages, i32, "free_pages", dev), p_count,
+        p_count if free_count_out is None else _flat(free_count_out, i32, "free_count_out", dev, 1), p_indptr,
+        _flat(page_indices, i32, "page_indices", dev), page_indices.numel(), p_tokens, _flat(slot_map, _i64_t, "slot_map", dev), slot_map.numel(),
+        _flat(lens_out, i32, "lens_out", dev, n), _status_ptr(status, dev), _flat(scratch, _u8_t, "scratch", dev), scratch.numel(),
+        _stream_on(stream, dev)))
 
 
 def _status_ptr(status, dev):
     """A status word: a one-element int32 tensor, or a Plan (the word Plan.check_status reads)."""
-    import torch
     if status is None:
         return None
     if isinstance(status, Plan):
         if status.workspace is None:
             raise ValueError("status: the plan has no workspace yet")
-        return _flat(status.workspace, torch.uint8, "status", dev)
-    return _flat(status, torch.int32, "status", dev, 1)
+        return _flat(status.workspace, _u8_t, "status", dev)
+    return _flat(status, _i32_t, "status", dev, 1)
 
 
 def read_status(status, stream=None):
     """psa_read_status: synchronise, raise if the one-element int32 tensor `status` holds an error, and clear it."""
-    import torch
-    _check(library().psa_read_status(_flat(status, torch.int32, "status", _device_of(status, "status"), 1), _stream_ptr(stream)))
+    if _torch is None:
+        _bind_torch()
+    dev = _device_of(status, "status")
+    _check(library().psa_read_status(_flat(status, _i32_t, "status", dev, 1), _stream_on(stream, dev)))
 
 
 def kv4_cell_bytes(head_dim) -> int:
@@ -580,13 +604,13 @@ def kv4_cell_bytes(head_dim) -> int:
 
 
 def _kv4_args(k, v, slot_map, pool, names):
-    import torch
-    if k.dim() != 3 or k.shape != v.shape or k.stride() != v.stride() or k.dtype is not torch.bfloat16 or v.dtype is not torch.bfloat16:
+    shape = k.shape
+    if len(shape) != 3 or k.dtype is not _bf16_t or v.dtype is not _bf16_t or v.shape != shape or v.stride() != k.stride():
         raise ValueError(f"{names} must be bf16 [tokens, heads, head_dim] of the same shape and strides")
-    tokens, heads, dim = k.shape
-    if pool.dtype is not torch.uint8 or pool.dim() != 3 or pool.shape[1] != heads:
+    tokens, heads, dim = shape
+    if pool.dtype is not _u8_t or pool.dim() != 3 or pool.shape[1] != heads:
         raise ValueError("pool must be uint8 [pages, heads, kv4_cell_bytes(head_dim)]")
-    if slot_map.dtype is not torch.int64 or slot_map.numel() < tokens or not slot_map.is_contiguous():
+    if slot_map.dtype is not _i64_t or slot_map.numel() < tokens or not slot_map.is_contiguous():
         raise ValueError(f"slot_map must be contiguous int64 with at least {tokens} elements")
     dev = _device_of(k, names)
     if v.get_device() != dev or slot_map.get_device() != dev or pool.get_device() != dev:
@@ -597,57 +621,83 @@ def _kv4_args(k, v, slot_map, pool, names):
 def store_kv4(new_k, new_v, slot_map, pool, *, status=None, stream=None):
     """psa_store_kv4: quantise new_k / new_v [T, Hkv, D] bf16 (any token and head stride) into the slots of a 4-bit pool
     [pages, Hkv, kv4_cell_bytes(D)] uint8."""
+    if _torch is None:
+        _bind_torch()
     t, h, d, kst, pst, dev = _kv4_args(new_k, new_v, slot_map, pool, "new_k and new_v")
     _check(library().psa_store_kv4(new_k.data_ptr(), new_v.data_ptr(), kst, slot_map.data_ptr(), t, h, d, pool.data_ptr(), pst,
-                                   pool.shape[0], _status_ptr(status, dev), _stream_ptr(stream)))
+                                   pool.shape[0], _status_ptr(status, dev), _stream_on(stream, dev)))
 
 
 def load_kv4(pool, slot_map, out_k, out_v, *, status=None, stream=None):
     """psa_load_kv4: the cached tokens of slot_map as bf16 rows out_k / out_v [T, Hkv, D]; rows of negative slots are left alone."""
+    if _torch is None:
+        _bind_torch()
     t, h, d, kst, pst, dev = _kv4_args(out_k, out_v, slot_map, pool, "out_k and out_v")
     _check(library().psa_load_kv4(pool.data_ptr(), pst, pool.shape[0], slot_map.data_ptr(), t, h, d, out_k.data_ptr(), out_v.data_ptr(),
-                                  kst, _status_ptr(status, dev), _stream_ptr(stream)))
+                                  kst, _status_ptr(status, dev), _stream_on(stream, dev)))
 
 
 def decode_kv4(plan: Plan, q, prefix_k, prefix_v, pool, page_indptr, page_indices, suffix_lens, out, lse, *, prefix_strides=None,
                stream=None, stage="all"):
     """psa_decode_kv4 (or one of its stages): decode with the samples' own tokens in a 4-bit pool [pages, Hkv, kv4_cell_bytes(D)]
     uint8.  Everything else as for decode; the work lists and the workspace are those of plan.for_kv4()."""
-    import torch
+    if _torch is None:
+        _bind_torch()
     if stage not in ("all", "prefix", "suffix", "merge"):
         raise ValueError(stage)
-    plan = plan.for_kv4()
+    plan = plan._kv4 or plan.for_kv4()
     if stage in ("prefix", "merge"):
         decode(plan, q, prefix_k, prefix_v, None, None, page_indptr, page_indices, suffix_lens, out, lse, prefix_strides=prefix_strides,
                stream=stream, stage=stage)
         return
-    if pool.dtype is not torch.uint8 or pool.dim() != 3 or pool.shape[1] != plan.num_kv_heads:
+    if pool.dtype is not _u8_t or pool.dim() != 3 or pool.shape[1] != plan.num_kv_heads:
         raise ValueError("pool must be uint8 [pages, num_kv_heads, kv4_cell_bytes(head_dim)]")
     pst = _outer_strides(pool, 20 * plan.head_dim, "pool")
-    rows = len(plan.suffix_len_bounds)
+    rows, i32 = plan.suffix_len_bounds.size, _i32_t
     dev = _device_of(pool, "pool")
     if plan.workspace is None:
         plan.bind_workspace(stream=stream)
-    p_q = _flat(q, torch.bfloat16, "q", dev, rows * plan.num_q_heads * plan.head_dim)
-    table = (_flat(page_indptr, torch.int32, "page_indptr", dev, rows + 1), _flat(page_indices, torch.int32, "page_indices", dev),
-             _flat(suffix_lens, torch.int32, "suffix_lens", dev, rows))
-    ws = (_ptr(plan.workspace), plan.workspace.numel(), _stream_ptr(stream))
+    lib, ws, heads = library(), plan.workspace, rows * plan.num_q_heads
+    p_q = _flat(q, _bf16_t, "q", dev, heads * plan.head_dim)
+    p_indptr = _flat(page_indptr, i32, "page_indptr", dev, rows + 1)
+    p_indices = _flat(page_indices, i32, "page_indices", dev)
+    p_lens = _flat(suffix_lens, i32, "suffix_lens", dev, rows)
+    st = _stream_on(stream, dev)
     if stage == "suffix":
-        _check(library().psa_decode_suffix_kv4(plan.handle, p_q, pool.data_ptr(), pst, *table, *ws))
+        _check(lib.psa_decode_suffix_kv4(plan._h, p_q, pool.data_ptr(), pst, p_indptr, p_indices, p_lens, ws.data_ptr(), ws.numel(), st))
         return
-    p_out = _flat(out, torch.float32 if plan.out_dtype == PSA_OUT_F32 else torch.bfloat16, "out", dev, rows * plan.num_q_heads * plan.head_dim)
-    p_lse = _flat(lse, torch.float32, "lse", dev, rows * plan.num_q_heads)
-    _check(library().psa_decode_kv4(plan.handle, p_q, _ptr(prefix_k), _ptr(prefix_v), _strides2(*(prefix_strides or default_prefix_strides(plan))),
-                                    pool.data_ptr(), pst, *table, p_out, p_lse, *ws))
+    for t, name in ((prefix_k, "prefix_k"), (prefix_v, "prefix_v")):
+        if t is not None and (t.dtype is not _bf16_t or t.get_device() != dev):
+            raise ValueError(f"{name} must be bf16 on the current CUDA device")
+    p_out = _flat(out, _f32_t if plan.out_dtype == PSA_OUT_F32 else _bf16_t, "out", dev, heads * plan.head_dim)
+    p_lse = _flat(lse, _f32_t, "lse", dev, heads)
+    kst = _strides2(plan.num_kv_heads * plan.head_dim, plan.head_dim) if prefix_strides is None else _strides2(*prefix_strides)
+    _check(lib.psa_decode_kv4(plan._h, p_q, _ptr(prefix_k), _ptr(prefix_v), kst, pool.data_ptr(), pst, p_indptr, p_indices, p_lens,
+                              p_out, p_lse, ws.data_ptr(), ws.numel(), st))
 
 
 def _dtype_code(t, name):
-    import torch
-    if t.dtype is torch.bfloat16:
+    if t.dtype is _bf16_t:
         return PSA_OUT_BF16
-    if t.dtype is torch.float32:
+    if t.dtype is _f32_t:
         return PSA_OUT_F32
     raise ValueError(f"{name} must be bf16 or f32, not {t.dtype}")
+
+
+def _bitmap_args(bits, rows, words, R, name, dev):
+    """(address, row stride in words, number of bitmaps, address of the row numbers) of a set of bitmaps."""
+    if bits is None:
+        if rows is not None:
+            raise ValueError(f"{name}_rows without {name}_bits")
+        return None, 0, 0, None
+    count, width = bits.shape if bits.dim() == 2 else (0, -1)
+    if bits.dtype is not _i32_t or width < words or (bits.stride(1) != 1 and width > 1):
+        raise ValueError(f"{name}_bits must be int32 [bitmaps, words >= {words}], contiguous along the second dimension")
+    if rows is None and count < R:
+        raise ValueError(f"{name}_bits needs one bitmap per row, or {name}_rows")
+    if bits.get_device() != dev:
+        raise ValueError(f"{name}_bits must be on the current CUDA device")
+    return bits.data_ptr(), bits.stride(0) if count > 1 else width, count, _flat(rows, _i32_t, f"{name}_rows", dev, R)
 
 
 def process_logits(logits, out=None, *, repetition=None, frequency=None, presence=None, history=None, history_lens=None,
@@ -657,78 +707,72 @@ def process_logits(logits, out=None, *, repetition=None, frequency=None, presenc
     or f32 (rows may be padded; out may be logits; allocated when None); repetition / frequency / presence [R] f32; history
     [R, capacity] int32 with history_lens [R]; prompt_bits / mask_bits [*, >= ceil(V / 32)] int32 bitmaps chosen per row by prompt_rows /
     mask_rows [R] int32; bias_indptr [R+1], bias_ids int32 and bias_values f32.  Returns out."""
-    import torch
+    if _torch is None:
+        _bind_torch()
     if logits.dim() != 2 or (out is not None and out.shape != logits.shape):
         raise ValueError("logits must be [rows, vocab], and out of the same shape")
     R, V = logits.shape
     in_code = _dtype_code(logits, "logits")
     if out is None:
-        out = torch.empty((R, (V + 7) // 8 * 8), dtype=logits.dtype, device=logits.device)[:, :V]
+        out = _torch.empty((R, (V + 7) // 8 * 8), dtype=logits.dtype, device=logits.device)[:, :V]
     out_code = _dtype_code(out, "out")
-    if (logits.stride(1) != 1 or out.stride(1) != 1) and V > 1:
+    in_stride, step = logits.stride()
+    out_stride, out_step = out.stride()
+    if (step != 1 or out_step != 1) and V > 1:
         raise ValueError("logits and out must be contiguous along the vocabulary")
-    if (history is None) != (history_lens is None):
+    if R <= 1:      # one row has no stride of its own
+        in_stride = out_stride = (V + 7) // 8 * 8
+    dev = logits.get_device()
+    h_ptr, h_lens, h_stride, h_cap = None, None, 0, 0
+    if history is not None and history_lens is not None:
+        if history.dtype is not _i32_t or history.dim() != 2 or history.shape[0] < R or (history.stride(1) != 1 and history.shape[1] > 1):
+            raise ValueError("history must be int32 [rows, capacity], contiguous along the second dimension")
+        h_cap = history.shape[1]
+        h_stride = history.stride(0) if history.shape[0] > 1 else h_cap
+        if history.get_device() != dev:
+            raise ValueError("history must be on the current CUDA device")
+        h_ptr, h_lens = history.data_ptr(), _flat(history_lens, _i32_t, "history_lens", dev, R)
+    elif history is not history_lens:
         raise ValueError("history and history_lens go together")
-    if history is not None and (history.dtype is not torch.int32 or history.dim() != 2 or history.shape[0] < R or (history.stride(1) != 1 and history.shape[1] > 1)):
-        raise ValueError("history must be int32 [rows, capacity], contiguous along the second dimension")
-    if len({bias_indptr is None, bias_ids is None, bias_values is None}) != 1:
+    b_indptr, b_ids, b_values, b_count = None, None, None, 0
+    if bias_indptr is not None and bias_ids is not None and bias_values is not None:
+        b_count = bias_ids.numel()
+        b_indptr = _flat(bias_indptr, _i32_t, "bias_indptr", dev, R + 1)
+        b_ids = _flat(bias_ids, _i32_t, "bias_ids", dev)
+        b_values = _flat(bias_values, _f32_t, "bias_values", dev, b_count)
+    elif not (bias_indptr is bias_ids is bias_values):
         raise ValueError("bias_indptr, bias_ids and bias_values go together")
     words = (V + 31) // 32
-    for bits, rows, name in ((prompt_bits, prompt_rows, "prompt"), (mask_bits, mask_rows, "mask")):
-        if bits is None:
-            if rows is not None:
-                raise ValueError(f"{name}_rows without {name}_bits")
-        elif bits.dtype is not torch.int32 or bits.dim() != 2 or bits.shape[1] < words or (bits.stride(1) != 1 and bits.shape[1] > 1):
-            raise ValueError(f"{name}_bits must be int32 [bitmaps, words >= {words}], contiguous along the second dimension")
-        elif rows is None and bits.shape[0] < R:
-            raise ValueError(f"{name}_bits needs one bitmap per row, or {name}_rows")
-    dev = _device_of(logits, "logits")
-    for t, name in ((out, "out"), (history, "history"), (prompt_bits, "prompt_bits"), (mask_bits, "mask_bits")):
-        if t is not None and t.get_device() != dev:
-            raise ValueError(f"{name} must be on the current CUDA device")
-    f32, i32 = torch.float32, torch.int32
-    rules = _LogitsRules()
-    rules.repetition = _flat(repetition, f32, "repetition", dev, R)
-    rules.frequency = _flat(frequency, f32, "frequency", dev, R)
-    rules.presence = _flat(presence, f32, "presence", dev, R)
-    if history is not None:
-        rules.history, rules.history_lens = history.data_ptr(), _flat(history_lens, i32, "history_lens", dev, R)
-        rules.history_stride, rules.history_capacity = _row_stride(history), history.shape[1]
-    if prompt_bits is not None:
-        rules.prompt_bits, rules.prompt_row_words, rules.num_prompt_bitmaps = prompt_bits.data_ptr(), _row_stride(prompt_bits), prompt_bits.shape[0]
-        rules.prompt_rows = _flat(prompt_rows, i32, "prompt_rows", dev, R)
-    if bias_indptr is not None:
-        rules.bias_indptr = _flat(bias_indptr, i32, "bias_indptr", dev, R + 1)
-        rules.bias_ids, rules.num_biases = _flat(bias_ids, i32, "bias_ids", dev), bias_ids.numel()
-        rules.bias_values = _flat(bias_values, f32, "bias_values", dev, bias_ids.numel())
-    if mask_bits is not None:
-        rules.mask_bits, rules.mask_row_words, rules.num_mask_bitmaps = mask_bits.data_ptr(), _row_stride(mask_bits), mask_bits.shape[0]
-        rules.mask_rows = _flat(mask_rows, i32, "mask_rows", dev, R)
-    in_stride, out_stride = (t.stride(0) if R > 1 else (V + 7) // 8 * 8 for t in (logits, out))
+    prompt = _bitmap_args(prompt_bits, prompt_rows, words, R, "prompt", dev)
+    mask = _bitmap_args(mask_bits, mask_rows, words, R, "mask", dev)
+    f32 = _f32_t
+    rules = _LogitsRules(_flat(repetition, f32, "repetition", dev, R), _flat(frequency, f32, "frequency", dev, R),
+                         _flat(presence, f32, "presence", dev, R), h_ptr, h_lens, h_stride, h_cap, *prompt, b_indptr, b_ids, b_values, b_count, *mask)
+    if out.get_device() != _device_of(logits, "logits"):
+        raise ValueError("out must be on the current CUDA device")
     _check(library().psa_process_logits(logits.data_ptr(), in_code, in_stride, R, V, ctypes.byref(rules), out.data_ptr(), out_code, out_stride,
-                                        _stream_ptr(stream)))
+                                        _stream_on(stream, dev)))
     return out
-
-
-def _row_stride(t):
-    """Row stride of a 2-d tensor with contiguous rows; one row has none of its own."""
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
 def mark_tokens(ids, indptr, vocab, bits=None, *, stream=None):
     """psa_mark_tokens: bitmaps [rows, >= ceil(vocab / 32)] int32 of the tokens in ids[indptr[m] .. indptr[m + 1]).  Returns bits."""
-    import torch
-    rows, words = indptr.numel() - 1, (int(vocab) + 31) // 32
+    if _torch is None:
+        _bind_torch()
+    vocab = int(vocab)
+    rows, words = indptr.numel() - 1, (vocab + 31) // 32
     if rows < 0:
         raise ValueError("indptr must hold rows + 1 elements")
     if bits is None:
-        bits = torch.empty((rows, words), dtype=torch.int32, device=ids.device)
-    if bits.dtype is not torch.int32 or bits.dim() != 2 or bits.shape[0] < rows or bits.shape[1] < words or (bits.stride(1) != 1 and bits.shape[1] > 1):
+        bits = _torch.empty((rows, words), dtype=_i32_t, device=ids.device)
+    count, width = bits.shape if bits.dim() == 2 else (0, -1)
+    if bits.dtype is not _i32_t or count < rows or width < words or (bits.stride(1) != 1 and width > 1):
         raise ValueError(f"bits must be int32 [rows, words >= {words}], contiguous along the second dimension")
-    p_ids = _flat(ids, torch.int32, "ids", ids.get_device())
-    p_indptr = _flat(indptr, torch.int32, "indptr", ids.get_device())
-    dev = _device_of(ids, "ids")
-    if bits.get_device() != dev:
+    dev = ids.get_device()
+    p_ids = _flat(ids, _i32_t, "ids", dev)
+    p_indptr = _flat(indptr, _i32_t, "indptr", dev)
+    if bits.get_device() != _device_of(ids, "ids"):
         raise ValueError("bits must be on the current CUDA device")
-    _check(library().psa_mark_tokens(p_ids, ids.numel(), p_indptr, rows, int(vocab), bits.data_ptr(), _row_stride(bits), _stream_ptr(stream)))
+    _check(library().psa_mark_tokens(p_ids, ids.numel(), p_indptr, rows, vocab, bits.data_ptr(), bits.stride(0) if count > 1 else width,
+                                     _stream_on(stream, dev)))
     return bits

@@ -7,11 +7,11 @@
 // roundings are IEEE fp32, so the codes do not depend on who computes them.  A group whose range is not finite (a NaN, an
 // infinity, or a range beyond fp32) gets s = NaN: it reads back as NaN.
 //
-// Work: 16 bytes of bf16 (8 channels) per thread and row, four threads per group, K and V of a row in the same thread;
+// Work: 16 bytes of bf16 (8 channels) per thread and row, four threads per group, K and V of kRows rows in the same thread;
 // the group's minimum and maximum need two shuffles.  The quotient is one multiplication by the correctly rounded 1 / s and
 // one residual step, which rounds exactly like the division (Markstein) as long as nothing under- or overflows; other
-// groups take the division itself.  Both kernels are bound by HBM: 4 bytes read and 1.25 written per channel pair of K and
-// V, or the reverse.
+// groups take the division itself.  Both kernels are bound by HBM: 4 bytes read and 1.25 written per channel of K and V, or the
+// reverse.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -23,6 +23,8 @@ namespace psa {
 namespace {
 
 constexpr int kKv4Threads = 256;
+constexpr int kRows = 2;                     // rows a thread has in flight
+constexpr float kFifteenth = 1.f / 15.f;
 
 struct Kv4Args {
     const __nv_bfloat16 *in_k, *in_v;   // store: [T, Hkv, D]
@@ -31,6 +33,7 @@ struct Kv4Args {
     const int64_t *slot_map;
     int64_t num_tokens;
     int num_kv_heads;
+    uint32_t heads_magic, heads_shift;  // row / num_kv_heads = mulhi(row, magic) >> shift for row < 2^31
     unsigned char *pool;
     int64_t stride_page, stride_cell;   // bytes: page to page, KV head to KV head
     int64_t num_pool_pages;
@@ -68,7 +71,11 @@ __device__ __forceinline__ Quantised quantise(uint4 x)
     lo = min2_nan(lo, (lo >> 16) | (lo << 16));
     hi = max2_nan(hi, (hi >> 16) | (hi << 16));
     const float b = lo_f32(lo);
-    float s = __bfloat162float(__float2bfloat16_rn(__fdiv_rn(hi_f32(hi) - b, 15.f)));
+    // (max - min) / 15, rounded like the division: a multiplication by 1 / 15 and one residual step, unless the range is extreme
+    const float range = hi_f32(hi) - b;
+    float s0 = __fmul_rn(range, kFifteenth);
+    s0 = range > 1e-30f && range < 1e30f ? __fmaf_rn(__fmaf_rn(-s0, 15.f, range), kFifteenth, s0) : __fdiv_rn(range, 15.f);
+    const float s = __bfloat162float(__float2bfloat16_rn(s0));
     Quantised q;
     q.offset = uint16_t(lo);
     if (!(s <= 3.0e38f)) {   // NaN or infinite
@@ -79,7 +86,11 @@ __device__ __forceinline__ Quantised quantise(uint4 x)
     q.scale = uint16_t(__float_as_uint(s) >> 16);
     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
     if (s > 1e-30f && s < 1e30f) {
-        const float inv = __frcp_rn(s);
+        // 1 / s to the last bit: s has 8 significant bits, so its reciprocal lies at least 2^-33 from a rounding border, and one
+        // Newton step from an approximation good to 2^-22 ends within 2^-43
+        float inv;
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
+        inv = __fmaf_rn(__fmaf_rn(-s, inv, 1.f), inv, inv);
         // code + 1.5 * 2^23: adding that constant rounds to the nearest whole number, ties to even, into the low bits
         uint32_t acc = 0;
 #pragma unroll
@@ -117,6 +128,11 @@ __device__ __forceinline__ unsigned char *cell_of(const Kv4Args &a, int64_t slot
     return a.pool + page * a.stride_page + int64_t(head) * a.stride_cell;
 }
 
+__device__ __forceinline__ uint32_t token_of(const Kv4Args &a, uint32_t row)
+{
+    return a.num_kv_heads == 1 ? row : __umulhi(row, a.heads_magic) >> a.heads_shift;
+}
+
 template <int D>
 __global__ void __launch_bounds__(kKv4Threads)
 store_kv4_kernel(Kv4Args a)
@@ -124,25 +140,33 @@ store_kv4_kernel(Kv4Args a)
     using C = Kv4Cell<D>;
     constexpr int kPerRow = D / 8;                       // threads of one (token, head) row; rows never straddle a warp
     const int lane = threadIdx.x % kPerRow, g = lane >> 2;
-    const int64_t rows = a.num_tokens * a.num_kv_heads;
-    const int64_t per_grid = int64_t(gridDim.x) * (kKv4Threads / kPerRow);
-    const int64_t rounds = (rows + per_grid - 1) / per_grid;   // the same for all threads: the shuffles are warp-wide
-    int64_t row = int64_t(blockIdx.x) * (kKv4Threads / kPerRow) + threadIdx.x / kPerRow;
-    for (int64_t i = 0; i < rounds; ++i, row += per_grid) {
-        const bool live = row < rows;
-        const int64_t t = live ? row / a.num_kv_heads : 0;
-        const int head = live ? int(row - t * a.num_kv_heads) : 0;
-        const int64_t slot = live ? a.slot_map[t] : -1;
-        uint4 k{}, v{};
-        if (slot >= 0) {
-            const int64_t at = t * a.stride_tok + head * a.stride_head + lane * 8;
-            k = __ldg(reinterpret_cast<const uint4 *>(a.in_k + at));
-            v = __ldg(reinterpret_cast<const uint4 *>(a.in_v + at));
+    const uint32_t rows = uint32_t(a.num_tokens) * uint32_t(a.num_kv_heads);     // below 2^31
+    const uint32_t base = blockIdx.x * uint32_t(kKv4Threads / kPerRow * kRows) + threadIdx.x / kPerRow;
+    uint4 k[kRows], v[kRows];
+    int64_t slot[kRows];
+    int head[kRows];
+    // K and V are requested before the slots are known: a row that is skipped costs its bytes, every other one a round trip less
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        const uint32_t row = base + i * (kKv4Threads / kPerRow);
+        slot[i] = -1;
+        head[i] = 0;
+        k[i] = v[i] = uint4{};
+        if (row < rows) {
+            const uint32_t t = token_of(a, row);
+            head[i] = int(row - t * uint32_t(a.num_kv_heads));
+            const int64_t at = int64_t(t) * a.stride_tok + head[i] * a.stride_head + lane * 8;
+            k[i] = __ldg(reinterpret_cast<const uint4 *>(a.in_k + at));
+            v[i] = __ldg(reinterpret_cast<const uint4 *>(a.in_v + at));
+            slot[i] = a.slot_map[t];
         }
-        const Quantised qk = quantise(k), qv = quantise(v);
-        unsigned char *cell = cell_of(a, slot, head);
+    }
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        const Quantised qk = quantise(k[i]), qv = quantise(v[i]);
+        unsigned char *cell = cell_of(a, slot[i], head[i]);
         if (!cell) continue;
-        const int tok = int(slot % kPageSize);
+        const int tok = int(slot[i] % kPageSize);
         const int at = C::chunk(tok, g) + (lane & 3) * 4;
         *reinterpret_cast<uint32_t *>(cell + at) = qk.codes;
         *reinterpret_cast<uint32_t *>(cell + C::kCodeBytes + at) = qv.codes;
@@ -176,23 +200,40 @@ load_kv4_kernel(Kv4Args a)
     using C = Kv4Cell<D>;
     constexpr int kPerRow = D / 8;
     const int lane = threadIdx.x % kPerRow, g = lane >> 2;
-    const int64_t rows = a.num_tokens * a.num_kv_heads;
-    const int64_t per_grid = int64_t(gridDim.x) * (kKv4Threads / kPerRow);
-    for (int64_t row = int64_t(blockIdx.x) * (kKv4Threads / kPerRow) + threadIdx.x / kPerRow; row < rows; row += per_grid) {
-        const int64_t t = row / a.num_kv_heads;
-        const int head = int(row - t * a.num_kv_heads);
-        const int64_t slot = a.slot_map[t];
-        const unsigned char *cell = cell_of(a, slot, head);
-        if (!cell) continue;
-        const int tok = int(slot % kPageSize);
-        const int at = C::chunk(tok, g) + (lane & 3) * 4;
-        const uint32_t ck = *reinterpret_cast<const uint32_t *>(cell + at), cv = *reinterpret_cast<const uint32_t *>(cell + C::kCodeBytes + at);
-        const uint16_t *pk = reinterpret_cast<const uint16_t *>(cell + C::params(0, tok)) + g;
-        const uint16_t *pv = reinterpret_cast<const uint16_t *>(cell + C::params(1, tok)) + g;
-        const uint4 k = dequantise(ck, pk[0], pk[C::kGroups]), v = dequantise(cv, pv[0], pv[C::kGroups]);
-        const int64_t to = t * a.stride_tok + head * a.stride_head + lane * 8;
-        *reinterpret_cast<uint4 *>(a.out_k + to) = k;
-        *reinterpret_cast<uint4 *>(a.out_v + to) = v;
+    const uint32_t rows = uint32_t(a.num_tokens) * uint32_t(a.num_kv_heads);
+    const uint32_t base = blockIdx.x * uint32_t(kKv4Threads / kPerRow * kRows) + threadIdx.x / kPerRow;
+    const unsigned char *cell[kRows];
+    int tok[kRows];
+    int64_t to[kRows];
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        const uint32_t row = base + i * (kKv4Threads / kPerRow);
+        cell[i] = nullptr;
+        if (row < rows) {
+            const uint32_t t = token_of(a, row);
+            const int head = int(row - t * uint32_t(a.num_kv_heads));
+            const int64_t slot = a.slot_map[t];
+            cell[i] = cell_of(a, slot, head);
+            tok[i] = int(slot % kPageSize);
+            to[i] = int64_t(t) * a.stride_tok + head * a.stride_head + lane * 8;
+        }
+    }
+    uint32_t ck[kRows], cv[kRows], sk[kRows], sv[kRows], bk[kRows], bv[kRows];
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        if (!cell[i]) continue;
+        const int at = C::chunk(tok[i], g) + (lane & 3) * 4;
+        ck[i] = *reinterpret_cast<const uint32_t *>(cell[i] + at);
+        cv[i] = *reinterpret_cast<const uint32_t *>(cell[i] + C::kCodeBytes + at);
+        const uint16_t *pk = reinterpret_cast<const uint16_t *>(cell[i] + C::params(0, tok[i])) + g;
+        const uint16_t *pv = reinterpret_cast<const uint16_t *>(cell[i] + C::params(1, tok[i])) + g;
+        sk[i] = pk[0]; bk[i] = pk[C::kGroups]; sv[i] = pv[0]; bv[i] = pv[C::kGroups];
+    }
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        if (!cell[i]) continue;
+        *reinterpret_cast<uint4 *>(a.out_k + to[i]) = dequantise(ck[i], sk[i], bk[i]);
+        *reinterpret_cast<uint4 *>(a.out_v + to[i]) = dequantise(cv[i], sv[i], bv[i]);
     }
 }
 
@@ -202,7 +243,8 @@ psa_status_t check(const Kv4Args &a, const void *k, const void *v, const int64_t
 {
     if (a.num_tokens < 0 || a.num_kv_heads <= 0 || a.num_pool_pages < 0) return set_last_error(PSA_ERR_INVALID_ARG, "negative sizes or no KV head");
     if (head_dim != 64 && head_dim != 128) return set_last_error(PSA_ERR_UNSUPPORTED, "head_dim must be 64 or 128");
-    if (a.num_tokens > 0x7fffffff || a.num_kv_heads > 65536) return set_last_error(PSA_ERR_UNSUPPORTED, "problem too large");
+    if (a.num_kv_heads > 65536 || a.num_tokens > 0x7fffffff / a.num_kv_heads)
+        return set_last_error(PSA_ERR_UNSUPPORTED, "at most 2^31 - 1 rows (tokens x KV heads) per call");
     if (a.num_tokens == 0) return PSA_OK;
     if (!k || !v || !kv_strides || !a.slot_map || !pool_strides || (a.num_pool_pages > 0 && !a.pool))
         return set_last_error(PSA_ERR_INVALID_ARG, "null K/V cache argument");
@@ -217,10 +259,13 @@ psa_status_t check(const Kv4Args &a, const void *k, const void *v, const int64_t
 }
 
 template <class K64, class K128>
-psa_status_t launch(const Kv4Args &a, int head_dim, K64 k64, K128 k128, void *cuda_stream, const char *what)
+psa_status_t launch(Kv4Args a, int head_dim, K64 k64, K128 k128, void *cuda_stream, const char *what)
 {
-    const int64_t threads = a.num_tokens * a.num_kv_heads * (head_dim / 8);
-    const unsigned blocks = unsigned(std::min<int64_t>((threads + kKv4Threads - 1) / kKv4Threads, 148 * 64));
+    const int64_t rows_per_block = kKv4Threads / (head_dim / 8) * kRows;
+    const unsigned blocks = unsigned((a.num_tokens * a.num_kv_heads + rows_per_block - 1) / rows_per_block);
+    // division by the head count (Granlund and Montgomery): magic = ceil(2^(32 + shift) / heads), 2^shift < heads <= 2^(shift + 1)
+    while ((2u << a.heads_shift) < unsigned(a.num_kv_heads)) ++a.heads_shift;
+    a.heads_magic = uint32_t(((uint64_t(1) << (32 + a.heads_shift)) + unsigned(a.num_kv_heads) - 1) / unsigned(a.num_kv_heads));
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     if (head_dim == 64) k64<<<blocks, kKv4Threads, 0, st>>>(a);
     else k128<<<blocks, kKv4Threads, 0, st>>>(a);

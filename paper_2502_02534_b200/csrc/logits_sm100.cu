@@ -1,13 +1,13 @@
 // Rules applied to logits before a token is drawn: penalties for repeated tokens, additive biases, grammar masks.
 //
 // For logit x of token i in row r, with c = how often i stands in the row's generated tokens:
-//     x <- x > 0 ? x / repetition : x * repetition       if c > 0 or i is in the row's prompt set
+//     x <- x > 0 ? x / repetition : x * repetition       if c > 0 or i is in the row's prompt set   (by 1 / repetition, rounded once)
 //     x <- x - frequency * c - presence * [c > 0]
 //     x <- x + (sum of the row's biases for i, added in list order)
 //     x <- -inf                                          if the row's mask has bit i clear
 // in fp32, rounded once to the output type.
 //
-// One block per (row, tile of kTile logits).  The tile's logits are requested first, into registers; while they are on
+// One block per (row, tile of kTile logits).  The tile's logits and bitmaps are requested first, into registers; while they are on
 // their way the block walks the row's generated tokens and biases twice: the first walk marks the tile's touched tokens in
 // a bitmap and zeroes exactly their counters (nothing else of the counter arrays is ever read, so they need no clearing), the
 // second adds up.  A thread then handles eight consecutive logits at a time: one byte each of the touched bitmap, the
@@ -28,8 +28,11 @@ namespace {
 constexpr int kRuleThreads = 256;
 constexpr int kVec = 8;                                    // logits a thread handles together
 constexpr int kRounds = 2;
+constexpr int kKeep = 4;                                   // generated tokens a thread remembers between the two walks
 constexpr int kTile = kRuleThreads * kVec * kRounds;       // 4096 logits
 constexpr int kMarkTile = 32768;                           // tokens of one block's bitmap
+constexpr int kMarkThreads = 1024;
+constexpr int kMarkBatch = 8;
 
 struct RulesArgs {
     psa_logits_rules_t r;
@@ -146,67 +149,81 @@ rules_kernel(RulesArgs a)
     const void *in = static_cast<const unsigned char *>(a.logits) + int64_t(row) * a.row_stride * (kInF32 ? 4 : 2);
     void *out = static_cast<unsigned char *>(a.out) + int64_t(row) * a.out_stride * (kOutF32 ? 4 : 2);
 
+    // ---- everything that does not depend on the lists is requested first: the row's numbers, its logits, its bitmaps
+    const int32_t *said = a.r.history ? a.r.history + int64_t(row) * a.r.history_stride : nullptr;
+    const int said_len = said ? a.r.history_lens[row] : 0;
+    int b0 = 0, b1 = 0;
+    if (a.r.bias_indptr) { b0 = a.r.bias_indptr[row]; b1 = a.r.bias_indptr[row + 1]; }
+    const float rep_in = a.r.repetition ? a.r.repetition[row] : 1.f;
+    const float freq = a.r.frequency ? a.r.frequency[row] : 0.f;
+    const float pres = a.r.presence ? a.r.presence[row] : 0.f;
+    const int64_t prompt_row = a.r.prompt_rows && a.r.prompt_bits ? a.r.prompt_rows[row] : row;
+    const int64_t mask_row = a.r.mask_rows && a.r.mask_bits ? a.r.mask_rows[row] : row;
     Vec8<kInF32> v[kRounds];
 #pragma unroll
     for (int k = 0; k < kRounds; ++k) {
         const int i = base + (k * kRuleThreads + tid) * kVec;
         if (i + kVec <= limit) v[k].load(in, i);
     }
+    const unsigned char *prompt = nullptr, *mask = nullptr;
+    if (a.r.prompt_bits && prompt_row >= 0 && prompt_row < a.r.num_prompt_bitmaps)
+        prompt = reinterpret_cast<const unsigned char *>(a.r.prompt_bits + prompt_row * a.r.prompt_row_words);
+    if (a.r.mask_bits && mask_row >= 0 && mask_row < a.r.num_mask_bitmaps)
+        mask = reinterpret_cast<const unsigned char *>(a.r.mask_bits + mask_row * a.r.mask_row_words);
+    uint32_t seen[kRounds], allowed[kRounds];   // one bit per logit
+#pragma unroll
+    for (int k = 0; k < kRounds; ++k) {
+        const int i = base + (k * kRuleThreads + tid) * kVec;
+        seen[k] = prompt && i < limit ? __ldg(prompt + (i >> 3)) : 0u;
+        allowed[k] = mask && i < limit ? __ldg(mask + (i >> 3)) : 0xFFu;
+    }
 
     // ---- the row's lists
-    const int32_t *said = a.r.history ? a.r.history + int64_t(row) * a.r.history_stride : nullptr;
-    const int n_said = said ? max(0, min(a.r.history_lens[row], a.r.history_capacity)) : 0;
-    int b0 = 0, b1 = 0;
-    if (a.r.bias_indptr) { b0 = max(0, a.r.bias_indptr[row]); b1 = min(a.r.num_biases, a.r.bias_indptr[row + 1]); }
+    const int n_said = max(0, min(said_len, a.r.history_capacity));
+    b0 = max(0, b0);
+    b1 = min(a.r.num_biases, b1);
     const bool lists = n_said > 0 || b1 > b0;   // the same for the whole block
     if (lists) {
+        int kept[kKeep];   // this thread's first generated tokens, as positions in the tile (-1: elsewhere)
         for (int w = tid; w < kTile / 32; w += kRuleThreads) sm.touched[w] = 0u;
+        auto place = [&](const int32_t *list, int e, int n) {
+            const int id = e < n ? list[e] : -1;
+            return id >= base && id < limit ? id - base : -1;
+        };
+#pragma unroll
+        for (int j = 0; j < kKeep; ++j) kept[j] = place(said, tid + j * kRuleThreads, n_said);
         __syncthreads();
-        for (int e = tid; e < n_said; e += kRuleThreads) {
-            const int id = said[e];
-            if (id >= base && id < limit) {
-                sm.count[id - base] = 0; sm.bias[id - base] = 0.f;
-                atomicOr(&sm.touched[(id - base) >> 5], 1u << ((id - base) & 31));
+        auto touch = [&](int at) {
+            if (at >= 0) {
+                sm.count[at] = 0; sm.bias[at] = 0.f;
+                atomicOr(&sm.touched[at >> 5], 1u << (at & 31));
             }
-        }
-        for (int e = b0 + tid; e < b1; e += kRuleThreads) {
-            const int id = a.r.bias_ids[e];
-            if (id >= base && id < limit) {
-                sm.count[id - base] = 0; sm.bias[id - base] = 0.f;
-                atomicOr(&sm.touched[(id - base) >> 5], 1u << ((id - base) & 31));
-            }
-        }
+        };
+#pragma unroll
+        for (int j = 0; j < kKeep; ++j) touch(kept[j]);
+        for (int e = tid + kKeep * kRuleThreads; e < n_said; e += kRuleThreads) touch(place(said, e, n_said));
+        for (int e = b0 + tid; e < b1; e += kRuleThreads) touch(place(a.r.bias_ids, e, b1));
         __syncthreads();
-        for (int e = tid; e < n_said; e += kRuleThreads) {
-            const int id = said[e];
-            if (id >= base && id < limit) atomicAdd(&sm.count[id - base], 1);
+#pragma unroll
+        for (int j = 0; j < kKeep; ++j)
+            if (kept[j] >= 0) atomicAdd(&sm.count[kept[j]], 1);
+        for (int e = tid + kKeep * kRuleThreads; e < n_said; e += kRuleThreads) {
+            const int at = place(said, e, n_said);
+            if (at >= 0) atomicAdd(&sm.count[at], 1);
         }
         if (tid < 32 && b1 > b0) add_biases(a, sm, b0, b1, base, limit, tid);
         __syncthreads();
     }
 
-    const float rep_in = a.r.repetition ? a.r.repetition[row] : 1.f;
     const float rep = rep_in > 0.f ? rep_in : 1.f;   // not a penalty: off
-    const float freq = a.r.frequency ? a.r.frequency[row] : 0.f;
-    const float pres = a.r.presence ? a.r.presence[row] : 0.f;
-    const unsigned char *prompt = nullptr, *mask = nullptr;
-    if (a.r.prompt_bits) {
-        const int64_t p = a.r.prompt_rows ? a.r.prompt_rows[row] : row;
-        if (p >= 0 && p < a.r.num_prompt_bitmaps) prompt = reinterpret_cast<const unsigned char *>(a.r.prompt_bits + p * a.r.prompt_row_words);
-    }
-    if (a.r.mask_bits) {
-        const int64_t p = a.r.mask_rows ? a.r.mask_rows[row] : row;
-        if (p >= 0 && p < a.r.num_mask_bitmaps) mask = reinterpret_cast<const unsigned char *>(a.r.mask_bits + p * a.r.mask_row_words);
-    }
+    const float inv_rep = __fdiv_rn(1.f, rep);
     const unsigned char *touched = reinterpret_cast<const unsigned char *>(sm.touched);
-
-    // one logit whose token is touched, in the prompt, or masked
-    auto apply = [&](float x, int local, bool hit, bool in_prompt, bool allowed) {
-        const int c = hit ? sm.count[local] : 0;
-        if (c > 0 || in_prompt) x = x > 0.f ? __fdiv_rn(x, rep) : x * rep;
+    // a logit whose token is in one of the row's lists
+    auto listed = [&](float x, int local, bool in_prompt) {
+        const int c = sm.count[local];
+        if (c > 0 || in_prompt) x *= x > 0.f ? inv_rep : rep;
         if (c > 0) x = x - freq * float(c) - pres;
-        if (hit) x += sm.bias[local];
-        return allowed ? x : -INFINITY;
+        return x + sm.bias[local];
     };
 
 #pragma unroll
@@ -215,43 +232,61 @@ rules_kernel(RulesArgs a)
         const int i = base + local0;
         if (i >= limit) continue;
         const uint32_t hits = lists ? touched[local0 >> 3] : 0u;
-        const uint32_t seen = prompt ? __ldg(prompt + (i >> 3)) : 0u;
-        const uint32_t allowed = mask ? __ldg(mask + (i >> 3)) : 0xFFu;
-        if (i + kVec <= limit) {
-            float x[8];
+        const uint32_t prompt_only = seen[k] & ~hits, ok = allowed[k];
+        float x[8];
+        const bool whole = i + kVec <= limit;
+        if (whole) {
             v[k].get(x);
-            if ((hits | seen) != 0u || allowed != 0xFFu) {
+        } else {   // the ragged end of a row: neither read nor written beyond the vocabulary
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    x[e] = apply(x[e], local0 + e, (hits >> e) & 1u, (seen >> e) & 1u, (allowed >> e) & 1u);
-            }
+            for (int e = 0; e < 8; ++e) x[e] = i + e < limit ? load_one<kInF32>(in, i + e) : 0.f;
+        }
+        if (hits) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (hits & (1u << e)) x[e] = listed(x[e], local0 + e, seen[k] & (1u << e));
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (prompt_only & (1u << e)) x[e] *= x[e] > 0.f ? inv_rep : rep;
+            if (!(ok & (1u << e))) x[e] = -INFINITY;
+        }
+        if (whole) {
             Vec8<kOutF32> o;
             o.set(x);
             o.store(out, i);
-        } else {   // the ragged end of a row: neither read nor written beyond the vocabulary
-            for (int e = 0; i + e < limit; ++e)
-                store_one<kOutF32>(out, i + e, apply(load_one<kInF32>(in, i + e), local0 + e, (hits >> e) & 1u, (seen >> e) & 1u, (allowed >> e) & 1u));
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (i + e < limit) store_one<kOutF32>(out, i + e, x[e]);
         }
     }
 }
 
 // Token sets as bitmaps: one block per (row, kMarkTile tokens) walks the row's list and sets bits in shared memory.
-__global__ void __launch_bounds__(1024)
+__global__ void __launch_bounds__(kMarkThreads)
 mark_kernel(const int32_t *__restrict__ ids, int num_ids, const int32_t *__restrict__ indptr, int vocab, uint32_t *__restrict__ bits, int64_t row_words)
 {
     __shared__ uint32_t tile[kMarkTile / 32];
     const int row = blockIdx.y, base = blockIdx.x * kMarkTile;
     const int limit = min(vocab, base + kMarkTile);
-    for (int w = threadIdx.x; w < kMarkTile / 32; w += blockDim.x) tile[w] = 0u;
+    for (int w = threadIdx.x; w < kMarkTile / 32; w += kMarkThreads) tile[w] = 0u;
     __syncthreads();
     const int first = max(0, indptr[row]), last = min(num_ids, indptr[row + 1]);
-    for (int e = first + threadIdx.x; e < last; e += blockDim.x) {
-        const int id = ids[e];
-        if (id >= base && id < limit) atomicOr(&tile[(id - base) >> 5], 1u << ((id - base) & 31));
+    for (int64_t e0 = first; e0 < last; e0 += kMarkBatch * kMarkThreads) {
+        int id[kMarkBatch];   // that many loads in flight per thread
+#pragma unroll
+        for (int j = 0; j < kMarkBatch; ++j) {
+            const int64_t e = e0 + j * kMarkThreads + threadIdx.x;
+            id[j] = e < last ? ids[e] : -1;
+        }
+#pragma unroll
+        for (int j = 0; j < kMarkBatch; ++j)
+            if (id[j] >= base && id[j] < limit) atomicOr(&tile[(id[j] - base) >> 5], 1u << ((id[j] - base) & 31));
     }
     __syncthreads();
     uint32_t *to = bits + int64_t(row) * row_words + base / 32;
-    for (int w = threadIdx.x; w < (limit - base + 31) / 32; w += blockDim.x) to[w] = tile[w];
+    for (int w = threadIdx.x; w < (limit - base + 31) / 32; w += kMarkThreads) to[w] = tile[w];
 }
 
 bool misaligned(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n != 0; }
@@ -319,7 +354,7 @@ extern "C" psa_status_t psa_mark_tokens(const int32_t *ids, int32_t num_ids, con
     if (vocab > (1 << 30)) return set_last_error(PSA_ERR_UNSUPPORTED, "vocab must be at most 2^30");
     if ((!ids && num_ids > 0) || !indptr || !bits) return set_last_error(PSA_ERR_INVALID_ARG, "null argument");
     if (row_words < (int64_t(vocab) + 31) / 32) return set_last_error(PSA_ERR_INVALID_ARG, "bitmap rows must hold at least ceil(vocab / 32) words");
-    psa::mark_kernel<<<dim3((vocab + psa::kMarkTile - 1) / psa::kMarkTile, num_rows), 1024, 0, static_cast<cudaStream_t>(cuda_stream)>>>(
+    psa::mark_kernel<<<dim3((vocab + psa::kMarkTile - 1) / psa::kMarkTile, num_rows), psa::kMarkThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(
         ids, num_ids, indptr, vocab, bits, row_words);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return set_last_error(PSA_ERR_CUDA, std::string("mark launch: ") + cudaGetErrorString(e));

@@ -10,12 +10,12 @@
 //   scan phase     one thread per sample, 1024 samples per block.  A block gets its starting sums by reducing the samples
 //                  before its own itself: no block waits for another one, and at the sizes of a decode batch (one to a
 //                  few blocks) that costs a few loads.
-//   spread phase   a warp takes 256 consecutive tokens (or list entries), finds the sample of the first and of the last
-//                  by a 32-way search over the scanned offsets (two rounds for 1024 samples), and writes 256 contiguous
-//                  bytes per instruction; within one sample the page id is shared by 16 lanes.
+//   spread phase   a warp takes kSpread consecutive tokens (or list entries) and finds the samples of the first and the last
+//                  by a 32-way search over the scanned offsets (two rounds for 1024 samples).  A few long samples are walked
+//                  one after the other with everything about them in registers; many short ones are looked up lane by lane.
 //
-// Bound: 8 bytes written per token of capacity once there are many, launch latency when there are few.  The two phases
-// are one launch (one block) up to kOneBlockWork lookups and two launches above it.
+// Bound: 8 bytes written per token of capacity once there are many, the latency of a few dependent loads when there are few.  The
+// two phases are one launch of one block, with the offsets in shared memory, up to kOneBlockWork lookups; two launches above it.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -27,9 +27,11 @@ namespace psa {
 namespace {
 
 constexpr int kScanThreads = 1024;
-constexpr int kSpread = 256;                 // tokens or list entries a warp handles at a time
+constexpr int kSpread = 1024;                // most tokens or list entries a warp handles at a time
+constexpr int64_t kMostEntries = 0x7fffff00; // 32-bit positions, with room for one more stride of a loop
+constexpr int kWalk = 8;                     // samples in such a piece that are walked one after the other
 constexpr int64_t kOneBlockWork = 16384;
-constexpr int kOneBlockSamples = 4096;
+constexpr int kOneBlockSamples = 2048;       // offsets and records of these fit in 32 KB of shared memory
 
 struct PageTableArgs {
     const int32_t *held;       // null: nothing is held yet (a table built from scratch)
@@ -55,6 +57,12 @@ struct PageTableArgs {
     bool build;
 };
 
+// Where the spread phase finds the scanned offsets and records: global memory, or shared memory in the one-block kernel.
+struct Tables {
+    const int32_t *token_indptr, *page_indptr;
+    const int2 *rec;
+};
+
 struct Sums {
     long long tokens, entries, pages;
 };
@@ -64,6 +72,7 @@ struct Ask {
     int32_t held, count;       // tokens it holds, tokens it gets (0 where the input is negative)
     int32_t entries;           // list entries it reserves (build)
     int32_t pages;             // pages it needs; 0 when it is refused already
+    int32_t list;              // where its list starts (extend)
     bool ok;
 };
 
@@ -73,6 +82,7 @@ __device__ __forceinline__ Ask ask(const PageTableArgs &a, int s)
     const int32_t n = a.new_lens[s];
     r.held = a.held ? a.held[s] : 0;
     r.count = max(n, 0);
+    r.list = 0;
     const long long end = (long long)(r.held) + r.count;
     r.ok = n >= 0 && r.held >= 0 && end <= 0x7fffffffll;
     if (a.build) {
@@ -81,8 +91,9 @@ __device__ __forceinline__ Ask ask(const PageTableArgs &a, int s)
         r.ok = r.ok && end <= reserve;
     } else {
         r.entries = 0;
+        r.list = a.page_indptr[s];
         if (a.limits) r.ok = r.ok && (r.count == 0 || end <= a.limits[s]);
-        const long long first = a.page_indptr[s], last = a.page_indptr[s + 1];
+        const long long first = r.list, last = a.page_indptr[s + 1];
         r.ok = r.ok && (r.count == 0 || (first >= 0 && last <= a.num_entries && (end + kPageSize - 1) / kPageSize <= last - first));
         // a partly filled page must be in the list already (a negative id marks an entry without a page)
         if (r.ok && r.count > 0 && r.held % kPageSize != 0) r.ok = a.page_indices[first + r.held / kPageSize] >= 0;
@@ -108,7 +119,12 @@ __device__ __forceinline__ long long warp_total(long long v)
 }
 
 // Samples [s0, s0 + 1024) with the sums of everything before them; returns the sums behind them.
-__device__ Sums scan_chunk(const PageTableArgs &a, int s0, const Sums &before, int avail, int *used_to)
+// `copy` (shared memory, may be null) receives what the spread phase reads besides the output arrays.
+struct TableCopy {
+    int32_t *token_indptr, *page_indptr;
+    int2 *rec;
+};
+__device__ Sums scan_chunk(const PageTableArgs &a, int s0, const Sums &before, int avail, int *used_to, const TableCopy *copy)
 {
     __shared__ long long warp_sums[3][32];
     __shared__ int block_used;
@@ -136,15 +152,25 @@ __device__ Sums scan_chunk(const PageTableArgs &a, int s0, const Sums &before, i
     if (s < a.num_samples) {
         const long long t0 = before.tokens + excl[0], e0 = before.entries + excl[1], p0 = before.pages + excl[2];
         bool ok = q.ok && t0 + q.count <= a.max_tokens;
+        const int32_t e_cut = int32_t(min(e0, (long long)a.num_entries)), e_end = int32_t(min(e0 + q.entries, (long long)a.num_entries));
+        const int32_t t_cut = int32_t(min(t0, (long long)a.max_tokens)), t_end = int32_t(min(t0 + q.count, (long long)a.max_tokens));
+        ok = ok && (!a.build || e0 + q.entries <= a.num_entries) && (q.pages == 0 || p0 + q.pages <= avail);
+        const int2 rec = make_int2(q.held, ok ? int32_t(min(p0, (long long)avail)) : -1);
+        const bool end = s == a.num_samples - 1;
+        a.token_indptr[s] = t_cut;
+        if (end) a.token_indptr[s + 1] = t_end;
         if (a.build) {
-            ok = ok && e0 + q.entries <= a.num_entries;
-            a.page_indptr[s] = int32_t(min(e0, (long long)a.num_entries));
-            if (s == a.num_samples - 1) a.page_indptr[s + 1] = int32_t(min(e0 + q.entries, (long long)a.num_entries));
+            a.page_indptr[s] = e_cut;
+            if (end) a.page_indptr[s + 1] = e_end;
         }
-        ok = ok && (q.pages == 0 || p0 + q.pages <= avail);
-        a.token_indptr[s] = int32_t(min(t0, (long long)a.max_tokens));
-        if (s == a.num_samples - 1) a.token_indptr[s + 1] = int32_t(min(t0 + q.count, (long long)a.max_tokens));
-        a.rec[s] = make_int2(q.held, ok ? int32_t(min(p0, (long long)avail)) : -1);
+        if (copy) {
+            copy->token_indptr[s] = t_cut;
+            copy->page_indptr[s] = a.build ? e_cut : q.list;
+            copy->rec[s] = rec;
+            if (end) { copy->token_indptr[s + 1] = t_end; copy->page_indptr[s + 1] = a.build ? e_end : 0; }
+        } else {
+            a.rec[s] = rec;
+        }
         if (ok && q.pages > 0) atomicMax(&block_used, int(p0 + q.pages));
         if (!ok && a.status) atomicCAS(a.status, 0, int(PSA_ERR_BOUNDS));
     }
@@ -177,77 +203,83 @@ __device__ __forceinline__ int lane_find(const int32_t *offsets, int lo, int hi,
     return lo;
 }
 
-// Tokens [t0, t0 + 256) of the slot map.
-__device__ void spread_tokens(const PageTableArgs &a, long long t0, int avail, int lane)
+// Token t of sample s (record rec, first token at t_first, list at e_first): its slot; files a fresh page in the list.
+__device__ __forceinline__ long long slot_of(const PageTableArgs &a, int t, int2 rec, int t_first, int e_first, int avail)
+{
+    const int pos = rec.x + (t - t_first);
+    const int j = pos / kPageSize, fresh = (rec.x + kPageSize - 1) / kPageSize;
+    int page;
+    if (j >= fresh) {
+        page = a.free_pages[avail - 1 - (rec.y + j - fresh)];
+        if (!a.build && pos % kPageSize == 0) a.page_indices[(long long)e_first + j] = page;   // the first token of a fresh page files it
+    } else {
+        page = a.page_indices[(long long)e_first + j];
+    }
+    return page >= 0 ? (long long)page * kPageSize + pos % kPageSize : -1;
+}
+
+// Tokens [t0, t0 + piece) of the slot map.
+__device__ void spread_tokens(const PageTableArgs &a, const Tables &tab, long long t0, int piece, int avail, int lane)
 {
     const int n = a.num_samples;
-    const long long total = n > 0 ? a.token_indptr[n] : 0;
-    const long long end = min(t0 + kSpread, (long long)a.max_tokens);
-    int s_lo = 0, s_hi = 0;
-    if (t0 < total) {
-        s_lo = warp_find(a.token_indptr, 0, n, t0, lane);
-        s_hi = warp_find(a.token_indptr, s_lo, n, min(end, total) - 1, lane);
-    }
-    for (long long t = t0 + lane; t < end; t += 32) {
-        long long slot = -1;
-        if (t < total) {
-            const int s = s_lo == s_hi ? s_lo : lane_find(a.token_indptr, s_lo, s_hi + 1, t);
-            const int2 rec = a.rec[s];
-            if (rec.y >= 0) {
-                const int pos = rec.x + int(t - a.token_indptr[s]);
-                const int j = pos / kPageSize, fresh = (rec.x + kPageSize - 1) / kPageSize;
-                const long long entry = (long long)a.page_indptr[s] + j;
-                int page;
-                if (j >= fresh) {
-                    page = a.free_pages[avail - 1 - (rec.y + j - fresh)];
-                    if (!a.build && pos % kPageSize == 0) a.page_indices[entry] = page;   // the first token of a fresh page files it
-                } else {
-                    page = a.page_indices[entry];
-                }
-                if (page >= 0) slot = (long long)page * kPageSize + pos % kPageSize;
+    const int total = n > 0 ? tab.token_indptr[n] : 0;
+    const int end = int(min(t0 + piece, (long long)a.max_tokens)), live = min(end, total);
+    int t = int(t0);
+    if (t < live) {
+        const int s_lo = warp_find(tab.token_indptr, 0, n, t, lane);
+        const int s_hi = tab.token_indptr[s_lo + 1] >= live ? s_lo : warp_find(tab.token_indptr, s_lo, n, live - 1, lane);
+        if (s_hi - s_lo < kWalk) {
+            for (int s = s_lo; s <= s_hi; ++s) {
+                const int2 rec = tab.rec[s];
+                const int t_first = tab.token_indptr[s], stop = min(live, tab.token_indptr[s + 1]), e_first = tab.page_indptr[s];
+                for (int i = t + lane; i < stop; i += 32) a.slot_map[i] = rec.y >= 0 ? slot_of(a, i, rec, t_first, e_first, avail) : -1;
+                t = max(t, stop);
             }
+        } else {
+            for (int i = t + lane; i < live; i += 32) {
+                const int s = lane_find(tab.token_indptr, s_lo, s_hi + 1, i);
+                const int2 rec = tab.rec[s];
+                a.slot_map[i] = rec.y >= 0 ? slot_of(a, i, rec, tab.token_indptr[s], tab.page_indptr[s], avail) : -1;
+            }
+            t = live;
         }
-        a.slot_map[t] = slot;
     }
+    for (int i = t + lane; i < end; i += 32) a.slot_map[i] = -1;
 }
 
-// Entries [e0, e0 + 256) of a list array built from scratch: the pages of the tokens held, -1 in the rest.
-__device__ void spread_entries(const PageTableArgs &a, long long e0, int avail, int lane)
+// Entries [e0, e0 + piece) of a list array built from scratch: the pages of the tokens held, -1 in the rest.
+__device__ void spread_entries(const PageTableArgs &a, const Tables &tab, long long e0, int piece, int avail, int lane)
 {
     const int n = a.num_samples;
-    const long long total = n > 0 ? a.page_indptr[n] : 0;
-    const long long end = min(e0 + kSpread, (long long)a.num_entries);
-    int s_lo = 0, s_hi = 0;
-    if (e0 < total) {
-        s_lo = warp_find(a.page_indptr, 0, n, e0, lane);
-        s_hi = warp_find(a.page_indptr, s_lo, n, min(end, total) - 1, lane);
+    const int total = n > 0 ? tab.page_indptr[n] : 0;
+    const int end = int(min(e0 + piece, (long long)a.num_entries)), live = min(end, total);
+    auto entry = [&](int e, int s) {
+        const int2 rec = tab.rec[s];
+        const int j = e - tab.page_indptr[s], tokens = tab.token_indptr[s + 1] - tab.token_indptr[s];
+        return rec.y >= 0 && j < (tokens + kPageSize - 1) / kPageSize ? a.free_pages[avail - 1 - (rec.y + j)] : -1;
+    };
+    int e = int(e0);
+    if (e < live) {
+        const int s_lo = warp_find(tab.page_indptr, 0, n, e, lane), s_hi = warp_find(tab.page_indptr, s_lo, n, live - 1, lane);
+        for (int i = e + lane; i < live; i += 32) a.page_indices[i] = entry(i, s_lo == s_hi ? s_lo : lane_find(tab.page_indptr, s_lo, s_hi + 1, i));
+        e = live;
     }
-    for (long long e = e0 + lane; e < end; e += 32) {
-        int page = -1;
-        if (e < total) {
-            const int s = s_lo == s_hi ? s_lo : lane_find(a.page_indptr, s_lo, s_hi + 1, e);
-            const int2 rec = a.rec[s];
-            const int j = int(e - a.page_indptr[s]);
-            const int tokens = a.token_indptr[s + 1] - a.token_indptr[s];
-            if (rec.y >= 0 && j < (tokens + kPageSize - 1) / kPageSize) page = a.free_pages[avail - 1 - (rec.y + j)];
-        }
-        a.page_indices[e] = page;
-    }
+    for (int i = e + lane; i < end; i += 32) a.page_indices[i] = -1;
 }
 
-// Everything behind the scans, shared out over `warps` warps.
-__device__ void spread(const PageTableArgs &a, int avail, long long warp, long long warps, int lane)
+// Everything behind the scans, shared out over `warps` warps in pieces of `piece`.
+__device__ void spread(const PageTableArgs &a, const Tables &tab, int piece, int avail, long long warp, long long warps, int lane)
 {
-    const long long token_chunks = (a.max_tokens + kSpread - 1) / kSpread;
-    const long long entry_chunks = a.build ? (a.num_entries + kSpread - 1) / kSpread : 0;
-    for (long long c = warp; c < token_chunks + entry_chunks; c += warps) {
-        if (c < token_chunks) spread_tokens(a, c * kSpread, avail, lane);
-        else spread_entries(a, (c - token_chunks) * kSpread, avail, lane);
+    const long long token_pieces = (a.max_tokens + piece - 1) / piece;
+    const long long entry_pieces = a.build ? (a.num_entries + piece - 1) / piece : 0;
+    for (long long c = warp; c < token_pieces + entry_pieces; c += warps) {
+        if (c < token_pieces) spread_tokens(a, tab, c * piece, piece, avail, lane);
+        else spread_entries(a, tab, (c - token_pieces) * piece, piece, avail, lane);
     }
     if (a.lens_out)
         for (long long s = warp * 32 + lane; s < a.num_samples; s += warps * 32) {
-            const int2 rec = a.rec[s];
-            a.lens_out[s] = rec.y >= 0 ? rec.x + (a.token_indptr[s + 1] - a.token_indptr[s]) : rec.x;
+            const int2 rec = tab.rec[s];
+            a.lens_out[s] = rec.y >= 0 ? rec.x + (tab.token_indptr[s + 1] - tab.token_indptr[s]) : rec.x;
         }
 }
 
@@ -255,12 +287,15 @@ __device__ void spread(const PageTableArgs &a, int avail, long long warp, long l
 __global__ void __launch_bounds__(kScanThreads)
 page_table_one_block_kernel(PageTableArgs a)
 {
+    __shared__ int32_t tokens[kOneBlockSamples + 1], pages[kOneBlockSamples + 1];
+    __shared__ int2 rec[kOneBlockSamples];
+    const TableCopy copy{tokens, pages, rec};
     const int avail = max(*a.free_count, 0);
     Sums sums{0, 0, 0};
     int used = 0;
     for (int s0 = 0; s0 < a.num_samples; s0 += kScanThreads) {
         int u;
-        sums = scan_chunk(a, s0, sums, avail, &u);
+        sums = scan_chunk(a, s0, sums, avail, &u, &copy);
         used = max(used, u);
     }
     if (threadIdx.x == 0 && a.num_samples == 0) {
@@ -269,7 +304,8 @@ page_table_one_block_kernel(PageTableArgs a)
     }
     __syncthreads();   // also: every thread has read the stack's height before it is written, and the lengths before lens_out
     if (threadIdx.x == 0) *a.free_count_out = avail - used;
-    spread(a, avail, threadIdx.x >> 5, kScanThreads / 32, threadIdx.x & 31);
+    const int piece = max(32, int((a.max_tokens + (a.build ? a.num_entries : 0)) / (kScanThreads / 32)));
+    spread(a, Tables{tokens, pages, rec}, min(piece, kSpread), avail, threadIdx.x >> 5, kScanThreads / 32, threadIdx.x & 31);
 }
 
 __global__ void __launch_bounds__(kScanThreads)
@@ -289,7 +325,7 @@ page_table_scan_kernel(PageTableArgs a)
     __syncthreads();
     const Sums before{warp_total(part[0][lane]), warp_total(part[1][lane]), warp_total(part[2][lane])};
     int used;
-    scan_chunk(a, s0, before, avail, &used);
+    scan_chunk(a, s0, before, avail, &used, nullptr);
     if (threadIdx.x == 0) {
         a.block_used[blockIdx.x] = used;
         if (blockIdx.x == 0) {
@@ -312,7 +348,7 @@ page_table_spread_kernel(PageTableArgs a)
         for (int b = 0; b < a.scan_blocks; ++b) used = max(used, a.block_used[b]);
         *a.free_count_out = avail - used;
     }
-    spread(a, avail, (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5), (long long)gridDim.x * (blockDim.x >> 5),
+    spread(a, Tables{a.token_indptr, a.page_indptr, a.rec}, kSpread, avail, (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5), (long long)gridDim.x * (blockDim.x >> 5),
            threadIdx.x & 31);
 }
 
@@ -322,8 +358,8 @@ psa_status_t run(PageTableArgs a, void *scratch, size_t scratch_bytes, void *cud
 {
     if (a.num_samples < 0 || a.max_tokens < 0 || a.num_entries < 0) return set_last_error(PSA_ERR_INVALID_ARG, "negative sizes");
     if (a.num_samples > (1 << 20)) return set_last_error(PSA_ERR_UNSUPPORTED, "at most 2^20 samples per call");
-    if (a.max_tokens > 0x7fffffff || a.num_entries > 0x7fffffff)
-        return set_last_error(PSA_ERR_UNSUPPORTED, "slot_map and page_indices hold at most 2^31 - 1 entries");
+    if (a.max_tokens > kMostEntries || a.num_entries > kMostEntries)
+        return set_last_error(PSA_ERR_UNSUPPORTED, "slot_map and page_indices hold at most 2^31 - 256 entries");
     if (!a.free_pages || !a.free_count || !a.free_count_out || !a.page_indptr || !a.token_indptr || (a.max_tokens > 0 && !a.slot_map) ||
         (a.num_entries > 0 && !a.page_indices) || (a.num_samples > 0 && !a.new_lens) || (!a.build && a.num_samples > 0 && !a.held))
         return set_last_error(PSA_ERR_INVALID_ARG, "null page table argument");

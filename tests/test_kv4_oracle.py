@@ -108,7 +108,7 @@ def test_host_refusals():
     def store(k=FAKE, v=FAKE, kst=(256, 128), slots=FAKE, t=4, h=2, d=128, pool=FAKE, pst=(5120, 2560), pages=3):
         return lib.psa_store_kv4(k, v, st(*kst), slots, t, h, d, pool, st(*pst), pages, None, None)
     assert store(t=-1) == 1 and store(h=0) == 1 and store(pages=-1) == 1
-    assert store(d=96) == 2 and store(t=1 << 31) == 2
+    assert store(d=96) == 2 and store(t=1 << 31) == 2 and store(t=1 << 30) == 2 and store(h=65537) == 2
     assert store(k=None) == 1 and store(v=None) == 1 and store(slots=None) == 1 and store(pool=None) == 1
     assert store(k=FAKE + 8) == 1 and store(pool=FAKE + 4) == 1
     assert store(kst=(0, 128)) == 1 and store(kst=(256, 4)) == 1 and store(pst=(5120, 2552)) == 1 and store(pst=(2544, 2560)) == 1
