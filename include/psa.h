@@ -437,7 +437,7 @@ psa_status_t psa_read_status(int32_t *status, void *cuda_stream);
  * psa_store_kv4 quantises token t of new_k / new_v (bf16, element (t, head, d) at t*kv_strides[0] + head*kv_strides[1] + d) into
  * slot_map[t] (page * 16 + position, as the page tables above give them); a negative slot is skipped, one beyond num_pool_pages is
  * skipped and raises PSA_ERR_BOUNDS in *status (device, may be NULL).  The slots of one call must be distinct.
- * psa_load_kv4 reads the tokens of slot_map back into bf16 rows (s * code + b in fp32, rounded once), for instance to make a
+ * psa_load_kv4 reads the tokens of slot_map back into bf16 rows (s * code + b, rounded once), for instance to make a
  * finished sample part of a shared prefix; rows of skipped slots are left as they were.
  * D in {64, 128}; K, V and the pool 16-byte aligned, kv_strides multiples of 8 elements.  Only enqueue one kernel.
  */
@@ -472,7 +472,7 @@ psa_status_t psa_decode_suffix_kv4(const psa_plan_t *plan, const void *q, const 
  *     x <- x + (the row's biases for i, added in list order)
  *     x <- -inf                                               if the row's mask has bit i clear
  * in fp32, rounded once to the output type.  Every pointer is device memory and may be NULL, which leaves that rule out:
- *   repetition, frequency, presence  [R] f32 (a repetition that is not > 0 counts as 1)
+ *   repetition, frequency, presence  [R] f32 (a repetition that is not positive and finite counts as 1)
  *   history        int32, row r at r*history_stride; the first history_lens[r] (0 .. history_capacity, clamped) entries are the
  *                  row's generated tokens
  *   prompt_bits    num_prompt_bitmaps bitmaps of prompt_row_words uint32 each, bit i % 32 of word i / 32 = token i; row r uses bitmap
@@ -483,7 +483,9 @@ psa_status_t psa_decode_suffix_kv4(const psa_plan_t *plan, const void *q, const 
  *   mask_bits      bitmaps like prompt_bits (set = allowed): num_mask_bitmaps of mask_row_words words; mask_rows as prompt_rows
  * Token ids outside 0 .. vocab-1 are ignored.  A row whose mask allows nothing becomes -inf throughout.  Types, alignment and strides
  * as for psa_sample_tokens, for input and output each; out may be logits (same type and stride).  NaN logits stay NaN unless
- * masked.  Only enqueues one kernel.
+ * masked.  scratch: device, 4-byte aligned, psa_process_logits_scratch_bytes(num_rows, vocab) bytes (0 for small vocabularies),
+ * needed with history or biases only; overwritten by every call (calls that share it must be ordered on one stream).  Only enqueues
+ * one or two kernels.
  */
 typedef struct {
     const float *repetition, *frequency, *presence;
@@ -502,8 +504,10 @@ typedef struct {
     int32_t num_mask_bitmaps;
     const int32_t *mask_rows;
 } psa_logits_rules_t;
+size_t psa_process_logits_scratch_bytes(int32_t num_rows, int32_t vocab);
 psa_status_t psa_process_logits(const void *logits, int32_t logits_dtype, int64_t row_stride, int32_t num_rows, int32_t vocab,
-                                const psa_logits_rules_t *rules, void *out, int32_t out_dtype, int64_t out_row_stride, void *cuda_stream);
+                                const psa_logits_rules_t *rules, void *out, int32_t out_dtype, int64_t out_row_stride,
+                                void *scratch, size_t scratch_bytes, void *cuda_stream);
 /*
  * Token sets as bitmaps: bit i of row m (bits + m*row_words, i as above) is set when token i is among ids[indptr[m] .. indptr[m+1])
  * (int32 device, indptr [num_rows+1], cut to 0 .. num_ids), all others are cleared (the ceil(vocab / 32) words of a row are written whole).  Ids outside 0 .. vocab-1 are ignored.  For the

@@ -20,6 +20,17 @@ def f64_to_bf16(x):
     return np.where(np.isnan(x), np.uint16(0x7FC0), r)
 
 
+def f64_to_bf16_once(x):
+    """fp64 -> bf16 bits in one rounding to nearest even (to odd in fp32 first, which keeps every tie and every side of it)."""
+    x = np.asarray(x, np.float64)
+    with np.errstate(invalid="ignore", over="ignore"):
+        f = x.astype(np.float32)
+        toward = np.where(np.abs(f.astype(np.float64)) > np.abs(x), np.nextafter(f, np.float32(0)), f)       # truncated
+        inexact = np.isfinite(x) & (toward.astype(np.float64) != x)
+        u = toward.view(np.uint32) | inexact.astype(np.uint32)
+    return f64_to_bf16(u.view(np.float32))
+
+
 def quantise(bits):
     """bits [..., D] bf16 -> (codes [..., D] uint8, scale and offset bf16 bits [..., D / 32])."""
     with np.errstate(all="ignore"):

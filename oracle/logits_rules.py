@@ -16,7 +16,7 @@ def process(logits, repetition=None, frequency=None, presence=None, history=None
             count[t] = count.get(t, 0) + 1
         prompt = prompt_sets[r] if prompt_sets is not None and prompt_sets[r] is not None else set()
         rep = float(repetition[r]) if repetition is not None else 1.0
-        rep = rep if rep > 0 else 1.0
+        rep = rep if 0 < rep < float("inf") else 1.0
         with np.errstate(invalid="ignore"):
             for t in set(count) | {t for t in prompt if 0 <= t < V}:
                 out[r, t] = out[r, t] / rep if out[r, t] > 0 else out[r, t] * rep

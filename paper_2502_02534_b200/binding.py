@@ -21,7 +21,7 @@ EXPORTED_SYMBOLS = [
     "psa_decode", "psa_decode_static", "psa_static_check_status", "psa_static_selftest_bounded_wait", "psa_decode_prefix", "psa_decode_suffix", "psa_decode_merge",
     "psa_decode_host_staging_bytes", "psa_decode_host", "psa_check_status", "psa_selftest_bounded_wait", "psa_append_kv", "psa_append_kv_alloc", "psa_validate_page_table", "psa_sample_scratch_bytes", "psa_sample_tokens", "psa_sample_tokens_at", "psa_attn_task",
     "psa_page_table_scratch_bytes", "psa_build_page_table", "psa_extend_page_table", "psa_read_status", "psa_kv4_cell_bytes", "psa_store_kv4",
-    "psa_load_kv4", "psa_plan_create_kv4", "psa_decode_kv4", "psa_decode_suffix_kv4", "psa_process_logits", "psa_mark_tokens",
+    "psa_load_kv4", "psa_plan_create_kv4", "psa_decode_kv4", "psa_decode_suffix_kv4", "psa_process_logits_scratch_bytes", "psa_process_logits", "psa_mark_tokens",
     "psa_status_string", "psa_last_error_message", "psa_version",
 ]
 
@@ -153,8 +153,10 @@ def library():
         lib.psa_decode_kv4.argtypes = [P, P, P, P, POINTER(c_int64), P, POINTER(c_int64), P, P, P, P, P, P, c_size_t, P]
         lib.psa_decode_suffix_kv4.restype = c_int32
         lib.psa_decode_suffix_kv4.argtypes = [P, P, P, POINTER(c_int64), P, P, P, P, c_size_t, P]
+        lib.psa_process_logits_scratch_bytes.restype = c_size_t
+        lib.psa_process_logits_scratch_bytes.argtypes = [c_int32, c_int32]
         lib.psa_process_logits.restype = c_int32
-        lib.psa_process_logits.argtypes = [P, c_int32, c_int64, c_int32, c_int32, POINTER(_LogitsRules), P, c_int32, c_int64, P]
+        lib.psa_process_logits.argtypes = [P, c_int32, c_int64, c_int32, c_int32, POINTER(_LogitsRules), P, c_int32, c_int64, P, c_size_t, P]
         lib.psa_mark_tokens.restype = c_int32
         lib.psa_mark_tokens.argtypes = [P, c_int32, P, c_int32, c_int32, P, c_int64, P]
         lib.psa_status_string.restype = c_char_p
@@ -702,11 +704,12 @@ def _bitmap_args(bits, rows, words, R, name, dev):
 
 def process_logits(logits, out=None, *, repetition=None, frequency=None, presence=None, history=None, history_lens=None,
                    prompt_bits=None, prompt_rows=None, bias_indptr=None, bias_ids=None, bias_values=None, mask_bits=None,
-                   mask_rows=None, stream=None):
+                   mask_rows=None, scratch=None, stream=None):
     """psa_process_logits on torch CUDA tensors: penalties for repeated tokens, biases and grammar masks.  logits and out [R, V] bf16
     or f32 (rows may be padded; out may be logits; allocated when None); repetition / frequency / presence [R] f32; history
     [R, capacity] int32 with history_lens [R]; prompt_bits / mask_bits [*, >= ceil(V / 32)] int32 bitmaps chosen per row by prompt_rows /
-    mask_rows [R] int32; bias_indptr [R+1], bias_ids int32 and bias_values f32.  Returns out."""
+    mask_rows [R] int32; bias_indptr [R+1], bias_ids int32 and bias_values f32; scratch uint8 (psa_process_logits_scratch_bytes, for callers
+    that must not allocate).  Returns out."""
     if _torch is None:
         _bind_torch()
     if logits.dim() != 2 or (out is not None and out.shape != logits.shape):
@@ -750,8 +753,13 @@ def process_logits(logits, out=None, *, repetition=None, frequency=None, presenc
                          _flat(presence, f32, "presence", dev, R), h_ptr, h_lens, h_stride, h_cap, *prompt, b_indptr, b_ids, b_values, b_count, *mask)
     if out.get_device() != _device_of(logits, "logits"):
         raise ValueError("out must be on the current CUDA device")
-    _check(library().psa_process_logits(logits.data_ptr(), in_code, in_stride, R, V, ctypes.byref(rules), out.data_ptr(), out_code, out_stride,
-                                        _stream_on(stream, dev)))
+    lib, need = library(), 0
+    if h_cap > 0 or b_count > 0:
+        need = lib.psa_process_logits_scratch_bytes(R, V)
+        if need and scratch is None:
+            scratch = _torch.empty(need, dtype=_u8_t, device=logits.device)
+    _check(lib.psa_process_logits(logits.data_ptr(), in_code, in_stride, R, V, ctypes.byref(rules), out.data_ptr(), out_code, out_stride,
+                                  _flat(scratch, _u8_t, "scratch", dev, need) if need else None, need, _stream_on(stream, dev)))
     return out
 
 

@@ -7,11 +7,11 @@
 // roundings are IEEE fp32, so the codes do not depend on who computes them.  A group whose range is not finite (a NaN, an
 // infinity, or a range beyond fp32) gets s = NaN: it reads back as NaN.
 //
-// Work: 16 bytes of bf16 (8 channels) per thread and row, four threads per group, K and V of kRows rows in the same thread;
-// the group's minimum and maximum need two shuffles.  The quotient is one multiplication by the correctly rounded 1 / s and
-// one residual step, which rounds exactly like the division (Markstein) as long as nothing under- or overflows; other
-// groups take the division itself.  Both kernels are bound by HBM: 4 bytes read and 1.25 written per channel of K and V, or the
-// reverse.
+// Work: a thread takes half a group (16 channels, 32 bytes of bf16) of K and of V of one row, so that the group's minimum and
+// maximum need one shuffle and the indices are worked out once per 64 bytes.  The quotient is one multiplication by the correctly
+// rounded 1 / s and one residual step, which rounds exactly like the division (Markstein) as long as nothing under- or overflows;
+// groups of extreme range, and those that are not finite, take the division itself.  Both kernels are bound by HBM: 4 bytes read and
+// 1.25 written per channel of K and V, or the reverse.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -22,8 +22,9 @@
 namespace psa {
 namespace {
 
-constexpr int kKv4Threads = 256;
-constexpr int kRows = 2;                     // rows a thread has in flight
+constexpr int kKv4Threads = 128;
+constexpr int kPer = 16, kStoreRows = 1;     // channels of a thread that quantises, and rows it has in flight
+constexpr int kLoadPer = 8, kLoadRows = 2;   // channels of a thread that reads back, and rows it has in flight
 constexpr float kFifteenth = 1.f / 15.f;
 
 struct Kv4Args {
@@ -55,63 +56,95 @@ __device__ __forceinline__ uint32_t max2_nan(uint32_t a, uint32_t b)
 __device__ __forceinline__ float lo_f32(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_f32(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
+// Two fp32 operations at once (each rounded like the single one).
+struct F2 {
+    float x, y;
+};
+__device__ __forceinline__ F2 add2(F2 a, F2 b)
+{
+    F2 d;
+    asm("{\n\t.reg .b64 p, q;\n\tmov.b64 p, {%2, %3};\n\tmov.b64 q, {%4, %5};\n\tadd.rn.f32x2 p, p, q;\n\tmov.b64 {%0, %1}, p;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b)
+{
+    F2 d;
+    asm("{\n\t.reg .b64 p, q;\n\tmov.b64 p, {%2, %3};\n\tmov.b64 q, {%4, %5};\n\tmul.rn.f32x2 p, p, q;\n\tmov.b64 {%0, %1}, p;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c)
+{
+    F2 d;
+    asm("{\n\t.reg .b64 p, q, r;\n\tmov.b64 p, {%2, %3};\n\tmov.b64 q, {%4, %5};\n\tmov.b64 r, {%6, %7};\n\tfma.rn.f32x2 p, p, q, r;\n\t"
+        "mov.b64 {%0, %1}, p;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+
 struct Quantised {
-    uint32_t codes;          // 8 nibbles
-    uint16_t scale, offset;  // bf16 bits, the same in the four threads of a group
+    uint32_t codes[kPer / 8];  // nibbles
+    uint16_t scale, offset;    // bf16 bits, the same in all threads of a group
 };
 
-__device__ __forceinline__ Quantised quantise(uint4 x)
+// Any group, by IEEE divisions; `w` this thread's channels.
+__device__ __forceinline__ void quantise_any(const uint32_t (&w)[kPer / 2], float range, float b, Quantised &q)
 {
-    uint32_t lo = min2_nan(min2_nan(x.x, x.y), min2_nan(x.z, x.w)), hi = max2_nan(max2_nan(x.x, x.y), max2_nan(x.z, x.w));
+    const float s = __bfloat162float(__float2bfloat16_rn(__fdiv_rn(range, 15.f)));
+    const bool finite = s <= 3.0e38f;
+    q.scale = finite ? uint16_t(__float_as_uint(s) >> 16) : uint16_t(0x7FC0);   // NaN or infinite: the group reads back as NaN
 #pragma unroll
-    for (int o = 1; o < 4; o <<= 1) {
-        lo = min2_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-        hi = max2_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+    for (int i = 0; i < kPer / 8; ++i) q.codes[i] = 0u;
+    if (!finite || !(s > 0.f)) return;
+#pragma unroll
+    for (int i = kPer - 1; i >= 0; --i) {
+        const float r = ((i & 1) ? hi_f32(w[i >> 1]) : lo_f32(w[i >> 1])) - b;
+        q.codes[i >> 3] = q.codes[i >> 3] * 16u + uint32_t(fminf(rintf(__fdiv_rn(r, s)), 15.f));
     }
-    lo = min2_nan(lo, (lo >> 16) | (lo << 16));
-    hi = max2_nan(hi, (hi >> 16) | (hi << 16));
-    const float b = lo_f32(lo);
-    // (max - min) / 15, rounded like the division: a multiplication by 1 / 15 and one residual step, unless the range is extreme
-    const float range = hi_f32(hi) - b;
-    float s0 = __fmul_rn(range, kFifteenth);
-    s0 = range > 1e-30f && range < 1e30f ? __fmaf_rn(__fmaf_rn(-s0, 15.f, range), kFifteenth, s0) : __fdiv_rn(range, 15.f);
-    const float s = __bfloat162float(__float2bfloat16_rn(s0));
+}
+
+__device__ __forceinline__ Quantised quantise(const uint32_t (&w)[kPer / 2])
+{
+    uint32_t lo = w[0], hi = w[0];
+#pragma unroll
+    for (int i = 1; i < kPer / 2; ++i) { lo = min2_nan(lo, w[i]); hi = max2_nan(hi, w[i]); }
+    lo = min2_nan(lo, __byte_perm(lo, 0u, 0x1032));
+    hi = max2_nan(hi, __byte_perm(hi, 0u, 0x1032));
+    // both halves alike: the minimum and minus the maximum go through one shuffle and one minimum a step
+    uint32_t both = __byte_perm(lo, hi ^ 0x80008000u, 0x5410);
+#pragma unroll
+    for (int o = 1; o < kKv4Group / kPer; o <<= 1) both = min2_nan(both, __shfl_xor_sync(0xffffffffu, both, o));
+    const float b = lo_f32(both), range = -hi_f32(both) - b;
+    // range / 15, rounded like the division
+    const float s0 = __fmul_rn(range, kFifteenth);
+    const float s = __bfloat162float(__float2bfloat16_rn(__fmaf_rn(__fmaf_rn(-s0, 15.f, range), kFifteenth, s0)));
     Quantised q;
-    q.offset = uint16_t(lo);
-    if (!(s <= 3.0e38f)) {   // NaN or infinite
-        q.scale = 0x7FC0;
-        q.codes = 0;
-        return q;
-    }
-    q.scale = uint16_t(__float_as_uint(s) >> 16);
-    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    q.offset = uint16_t(both);
     if (s > 1e-30f && s < 1e30f) {
+        q.scale = uint16_t(__float_as_uint(s) >> 16);
         // 1 / s to the last bit: s has 8 significant bits, so its reciprocal lies at least 2^-33 from a rounding border, and one
         // Newton step from an approximation good to 2^-22 ends within 2^-43
         float inv;
         asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
         inv = __fmaf_rn(__fmaf_rn(-s, inv, 1.f), inv, inv);
         // code + 1.5 * 2^23: adding that constant rounds to the nearest whole number, ties to even, into the low bits
-        uint32_t acc = 0;
+        const F2 nb{-b, -b}, i2{inv, inv}, ns{-s, -s}, magic{12582912.f, 12582912.f};
 #pragma unroll
-        for (int i = 7; i >= 0; --i) {
-            const float r = ((i & 1) ? hi_f32(w[i >> 1]) : lo_f32(w[i >> 1])) - b;
-            const float q0 = __fmul_rn(r, inv);
-            const float q1 = __fmaf_rn(__fmaf_rn(-q0, s, r), inv, q0);
-            acc = acc * 16u + __float_as_uint(__fadd_rn(q1, 12582912.f));
-        }
-        constexpr uint32_t kBias = 0x4B400000u;
-        constexpr uint32_t kBiasSum = kBias * 0x11111111u;   // of the eight biases, each shifted by its nibble
-        q.codes = acc - kBiasSum;
-    } else {
-        q.codes = 0;
-        if (s > 0.f) {
+        for (int h = 0; h < kPer / 8; ++h) {
+            uint32_t c = 0u;
 #pragma unroll
-            for (int i = 7; i >= 0; --i) {
-                const float r = ((i & 1) ? hi_f32(w[i >> 1]) : lo_f32(w[i >> 1])) - b;
-                q.codes = q.codes * 16u + uint32_t(fminf(rintf(__fdiv_rn(r, s)), 15.f));
+            for (int i = 4 * h + 3; i >= 4 * h; --i) {
+                const F2 r = add2(F2{lo_f32(w[i]), hi_f32(w[i])}, nb);
+                const F2 q0 = mul2(r, i2);
+                const F2 code = add2(fma2(fma2(q0, ns, r), i2, q0), magic);
+                c = (c * 16u + __float_as_uint(code.y)) * 16u + __float_as_uint(code.x);
             }
+            constexpr uint32_t kBiasSum = 0x4B400000u * 0x11111111u;   // of the eight constants, each shifted by its nibble
+            q.codes[h] = c - kBiasSum;
         }
+    } else {
+        quantise_any(w, range, b, q);
     }
     return q;
 }
@@ -133,64 +166,96 @@ __device__ __forceinline__ uint32_t token_of(const Kv4Args &a, uint32_t row)
     return a.num_kv_heads == 1 ? row : __umulhi(row, a.heads_magic) >> a.heads_shift;
 }
 
+// Rows (token, KV head) are dealt out in order, `per` channels a thread; a row never straddles a warp.
+template <int D, int per>
+struct MyRow {
+    static constexpr int kThreads = D / per;
+    static constexpr int kPerBlock = kKv4Threads / kThreads;
+    uint32_t token;
+    int head;
+    __device__ __forceinline__ MyRow(const Kv4Args &a, uint32_t row)
+    {
+        token = token_of(a, row);
+        head = int(row - token * uint32_t(a.num_kv_heads));
+    }
+    __device__ __forceinline__ int64_t at(const Kv4Args &a) const
+    {
+        return int64_t(token) * a.stride_tok + head * a.stride_head + threadIdx.x % kThreads * per;
+    }
+};
+
 template <int D>
 __global__ void __launch_bounds__(kKv4Threads)
 store_kv4_kernel(Kv4Args a)
 {
     using C = Kv4Cell<D>;
-    constexpr int kPerRow = D / 8;                       // threads of one (token, head) row; rows never straddle a warp
-    const int lane = threadIdx.x % kPerRow, g = lane >> 2;
+    using R = MyRow<D, kPer>;
+    constexpr int kWords = kPer / 2;
     const uint32_t rows = uint32_t(a.num_tokens) * uint32_t(a.num_kv_heads);     // below 2^31
-    const uint32_t base = blockIdx.x * uint32_t(kKv4Threads / kPerRow * kRows) + threadIdx.x / kPerRow;
-    uint4 k[kRows], v[kRows];
-    int64_t slot[kRows];
-    int head[kRows];
+    const uint32_t base = blockIdx.x * uint32_t(R::kPerBlock * kStoreRows) + threadIdx.x / R::kThreads;
+    const int lane = threadIdx.x % R::kThreads, group = lane / (kKv4Group / kPer), part = lane % (kKv4Group / kPer);
+    uint32_t k[kStoreRows][kWords], v[kStoreRows][kWords];
+    int64_t slot[kStoreRows];
+    int head[kStoreRows];
     // K and V are requested before the slots are known: a row that is skipped costs its bytes, every other one a round trip less
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-        const uint32_t row = base + i * (kKv4Threads / kPerRow);
+    for (int i = 0; i < kStoreRows; ++i) {
+        const uint32_t row = base + i * R::kPerBlock;
         slot[i] = -1;
         head[i] = 0;
-        k[i] = v[i] = uint4{};
+#pragma unroll
+        for (int j = 0; j < kWords; ++j) k[i][j] = v[i][j] = 0u;
         if (row < rows) {
-            const uint32_t t = token_of(a, row);
-            head[i] = int(row - t * uint32_t(a.num_kv_heads));
-            const int64_t at = int64_t(t) * a.stride_tok + head[i] * a.stride_head + lane * 8;
-            k[i] = __ldg(reinterpret_cast<const uint4 *>(a.in_k + at));
-            v[i] = __ldg(reinterpret_cast<const uint4 *>(a.in_v + at));
-            slot[i] = a.slot_map[t];
+            const R r(a, row);
+            head[i] = r.head;
+            const uint4 *pk = reinterpret_cast<const uint4 *>(a.in_k + r.at(a)), *pv = reinterpret_cast<const uint4 *>(a.in_v + r.at(a));
+#pragma unroll
+            for (int j = 0; j < kWords / 4; ++j) {
+                *reinterpret_cast<uint4 *>(&k[i][4 * j]) = __ldg(pk + j);
+                *reinterpret_cast<uint4 *>(&v[i][4 * j]) = __ldg(pv + j);
+            }
+            slot[i] = a.slot_map[r.token];
         }
     }
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
+    for (int i = 0; i < kStoreRows; ++i) {
         const Quantised qk = quantise(k[i]), qv = quantise(v[i]);
         unsigned char *cell = cell_of(a, slot[i], head[i]);
         if (!cell) continue;
-        const int tok = int(slot[i] % kPageSize);
-        const int at = C::chunk(tok, g) + (lane & 3) * 4;
-        *reinterpret_cast<uint32_t *>(cell + at) = qk.codes;
-        *reinterpret_cast<uint32_t *>(cell + C::kCodeBytes + at) = qv.codes;
-        // the four threads of a group file its four parameters
-        const int which = (lane >> 1) & 1, offset = lane & 1;
-        const uint16_t value = which ? (offset ? qv.offset : qv.scale) : (offset ? qk.offset : qk.scale);
-        *reinterpret_cast<uint16_t *>(cell + C::params(which, tok) + 2 * (offset * C::kGroups + g)) = value;
+        const int tok = int(slot[i] & (kPageSize - 1));
+        uint32_t *codes = reinterpret_cast<uint32_t *>(cell + C::chunk(tok, group) + part * (kPer / 2));
+        uint32_t *codes_v = reinterpret_cast<uint32_t *>(reinterpret_cast<unsigned char *>(codes) + C::kCodeBytes);
+        if constexpr (kPer == 16) {
+            *reinterpret_cast<uint2 *>(codes) = make_uint2(qk.codes[0], qk.codes[1]);
+            *reinterpret_cast<uint2 *>(codes_v) = make_uint2(qv.codes[0], qv.codes[1]);
+        } else {
+            codes[0] = qk.codes[0];
+            codes_v[0] = qv.codes[0];
+        }
+        // the first thread of a group files K's parameters, the second V's
+        if (part < 2) {
+            unsigned char *params = cell + C::params(part, tok) + 2 * group;
+            *reinterpret_cast<uint16_t *>(params) = part ? qv.scale : qk.scale;
+            *reinterpret_cast<uint16_t *>(params + 2 * C::kGroups) = part ? qv.offset : qk.offset;
+        }
     }
 }
 
-__device__ __forceinline__ uint32_t pack2(float lo, float hi)
-{
-    __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<uint32_t *>(&v);
-}
-// eight channels: s * code + b in fp32, rounded once to bf16
+// Eight channels: s * code + b, rounded once to bf16.  A nibble or'ed into the mantissa of 128 is 128 + code; subtracting 128 is exact.
 __device__ __forceinline__ uint4 dequantise(uint32_t codes, uint32_t scale, uint32_t offset)
 {
-    const float s = __uint_as_float(scale << 16), b = __uint_as_float(offset << 16);
-    float f[8];
+    const uint32_t s2 = scale * 0x10001u, b2 = offset * 0x10001u;
+    const uint32_t even = codes & 0x0F0F0F0Fu, odd = (codes >> 4) & 0x0F0F0F0Fu;   // byte i: channels 2 i and 2 i + 1
+    uint32_t w[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        f[i] = __fmaf_rn(__uint_as_float(((codes >> (4 * i)) & 15u) | 0x4B000000u) - 8388608.f, s, b);
-    return make_uint4(pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7]));
+    for (int i = 0; i < 4; ++i) {
+        // byte i of each into the halves' low bytes; the high bytes are whatever, and replaced
+        const uint32_t pair = (__byte_perm(even, odd, uint32_t(i | (i << 4) | ((4 + i) << 8) | ((4 + i) << 12))) & 0x000F000Fu) | 0x43004300u;
+        uint32_t c;
+        asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(c) : "r"(pair), "r"(0x43004300u));
+        asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(w[i]) : "r"(c), "r"(s2), "r"(b2));
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 template <int D>
@@ -198,39 +263,38 @@ __global__ void __launch_bounds__(kKv4Threads)
 load_kv4_kernel(Kv4Args a)
 {
     using C = Kv4Cell<D>;
-    constexpr int kPerRow = D / 8;
-    const int lane = threadIdx.x % kPerRow, g = lane >> 2;
+    using R = MyRow<D, kLoadPer>;
     const uint32_t rows = uint32_t(a.num_tokens) * uint32_t(a.num_kv_heads);
-    const uint32_t base = blockIdx.x * uint32_t(kKv4Threads / kPerRow * kRows) + threadIdx.x / kPerRow;
-    const unsigned char *cell[kRows];
-    int tok[kRows];
-    int64_t to[kRows];
+    const uint32_t base = blockIdx.x * uint32_t(R::kPerBlock * kLoadRows) + threadIdx.x / R::kThreads;
+    const int lane = threadIdx.x % R::kThreads, group = lane >> 2;
+    const unsigned char *cell[kLoadRows];
+    int tok[kLoadRows];
+    int64_t to[kLoadRows];
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-        const uint32_t row = base + i * (kKv4Threads / kPerRow);
+    for (int i = 0; i < kLoadRows; ++i) {
+        const uint32_t row = base + i * R::kPerBlock;
         cell[i] = nullptr;
         if (row < rows) {
-            const uint32_t t = token_of(a, row);
-            const int head = int(row - t * uint32_t(a.num_kv_heads));
-            const int64_t slot = a.slot_map[t];
-            cell[i] = cell_of(a, slot, head);
-            tok[i] = int(slot % kPageSize);
-            to[i] = int64_t(t) * a.stride_tok + head * a.stride_head + lane * 8;
+            const R r(a, row);
+            const int64_t slot = a.slot_map[r.token];
+            cell[i] = cell_of(a, slot, r.head);
+            tok[i] = int(slot & (kPageSize - 1));
+            to[i] = r.at(a);
         }
     }
-    uint32_t ck[kRows], cv[kRows], sk[kRows], sv[kRows], bk[kRows], bv[kRows];
+    uint32_t ck[kLoadRows], cv[kLoadRows], sk[kLoadRows], sv[kLoadRows], bk[kLoadRows], bv[kLoadRows];
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
+    for (int i = 0; i < kLoadRows; ++i) {
         if (!cell[i]) continue;
-        const int at = C::chunk(tok[i], g) + (lane & 3) * 4;
-        ck[i] = *reinterpret_cast<const uint32_t *>(cell[i] + at);
-        cv[i] = *reinterpret_cast<const uint32_t *>(cell[i] + C::kCodeBytes + at);
-        const uint16_t *pk = reinterpret_cast<const uint16_t *>(cell[i] + C::params(0, tok[i])) + g;
-        const uint16_t *pv = reinterpret_cast<const uint16_t *>(cell[i] + C::params(1, tok[i])) + g;
+        const unsigned char *codes = cell[i] + C::chunk(tok[i], group) + (lane & 3) * 4;
+        ck[i] = *reinterpret_cast<const uint32_t *>(codes);
+        cv[i] = *reinterpret_cast<const uint32_t *>(codes + C::kCodeBytes);
+        const uint16_t *pk = reinterpret_cast<const uint16_t *>(cell[i] + C::params(0, tok[i])) + group;
+        const uint16_t *pv = reinterpret_cast<const uint16_t *>(cell[i] + C::params(1, tok[i])) + group;
         sk[i] = pk[0]; bk[i] = pk[C::kGroups]; sv[i] = pv[0]; bv[i] = pv[C::kGroups];
     }
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
+    for (int i = 0; i < kLoadRows; ++i) {
         if (!cell[i]) continue;
         *reinterpret_cast<uint4 *>(a.out_k + to[i]) = dequantise(ck[i], sk[i], bk[i]);
         *reinterpret_cast<uint4 *>(a.out_v + to[i]) = dequantise(cv[i], sv[i], bv[i]);
@@ -259,9 +323,8 @@ psa_status_t check(const Kv4Args &a, const void *k, const void *v, const int64_t
 }
 
 template <class K64, class K128>
-psa_status_t launch(Kv4Args a, int head_dim, K64 k64, K128 k128, void *cuda_stream, const char *what)
+psa_status_t launch(Kv4Args a, int head_dim, K64 k64, K128 k128, int64_t rows_per_block, void *cuda_stream, const char *what)
 {
-    const int64_t rows_per_block = kKv4Threads / (head_dim / 8) * kRows;
     const unsigned blocks = unsigned((a.num_tokens * a.num_kv_heads + rows_per_block - 1) / rows_per_block);
     // division by the head count (Granlund and Montgomery): magic = ceil(2^(32 + shift) / heads), 2^shift < heads <= 2^(shift + 1)
     while ((2u << a.heads_shift) < unsigned(a.num_kv_heads)) ++a.heads_shift;
@@ -291,7 +354,7 @@ extern "C" psa_status_t psa_store_kv4(const void *new_k, const void *new_v, cons
     a.in_k = static_cast<const __nv_bfloat16 *>(new_k); a.in_v = static_cast<const __nv_bfloat16 *>(new_v);
     a.stride_tok = kv_strides[0]; a.stride_head = kv_strides[1];
     a.stride_page = pool_strides[0]; a.stride_cell = pool_strides[1];
-    return psa::launch(a, head_dim, psa::store_kv4_kernel<64>, psa::store_kv4_kernel<128>, cuda_stream, "store launch: ");
+    return psa::launch(a, head_dim, psa::store_kv4_kernel<64>, psa::store_kv4_kernel<128>, psa::kKv4Threads / (head_dim / psa::kPer) * psa::kStoreRows, cuda_stream, "store launch: ");
 }
 
 extern "C" psa_status_t psa_load_kv4(const void *pool, const int64_t pool_strides[2], int64_t num_pool_pages, const int64_t *slot_map,
@@ -306,5 +369,6 @@ extern "C" psa_status_t psa_load_kv4(const void *pool, const int64_t pool_stride
     a.out_k = static_cast<__nv_bfloat16 *>(out_k); a.out_v = static_cast<__nv_bfloat16 *>(out_v);
     a.stride_tok = kv_strides[0]; a.stride_head = kv_strides[1];
     a.stride_page = pool_strides[0]; a.stride_cell = pool_strides[1];
-    return psa::launch(a, head_dim, psa::load_kv4_kernel<64>, psa::load_kv4_kernel<128>, cuda_stream, "load launch: ");
+    return psa::launch(a, head_dim, psa::load_kv4_kernel<64>, psa::load_kv4_kernel<128>,
+                       psa::kKv4Threads / (head_dim / psa::kLoadPer) * psa::kLoadRows, cuda_stream, "load launch: ");
 }

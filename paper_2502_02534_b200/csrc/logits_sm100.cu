@@ -7,30 +7,38 @@
 //     x <- -inf                                          if the row's mask has bit i clear
 // in fp32, rounded once to the output type.
 //
-// One block per (row, tile of kTile logits).  The tile's logits and bitmaps are requested first, into registers; while they are on
-// their way the block walks the row's generated tokens and biases twice: the first walk marks the tile's touched tokens in
-// a bitmap and zeroes exactly their counters (nothing else of the counter arrays is ever read, so they need no clearing), the
-// second adds up.  A thread then handles eight consecutive logits at a time: one byte each of the touched bitmap, the
-// prompt set and the mask tell whether there is anything to do, and the common answer (no) costs a conversion.
-// Each block reads and writes only its own tile, so the output may be the input.
-// Bound: HBM, one read and one write of every logit; the walks read a few KB per block from L2.
+// A row touches a few hundred of its many tokens through its lists (generated tokens, biases), all others only through the two
+// bitmaps.  So the work is split:
+//   lists    one block per row counts the generated tokens and adds up the biases in a hash table in shared memory, works out the
+//            logit of every token in it, writes it to the output, and marks the token in a bitmap;
+//   stream   every other logit: a thread takes eight consecutive ones, and one byte each of the marks, the prompt set and the mask
+//            tell what there is to do.  Marked logits are taken from the output as they are, so that the output may be the input.
+// Up to kWholeRow tokens the block that did a row's lists streams the row as well (one launch, marks in shared memory); above it
+// the stream is a launch of its own with many blocks per row, and the marks are in the caller's scratch memory.  Without lists
+// there is only the stream.  Lists of more entries than half the table are done in ranges of as many tokens as it has slots,
+// indexed directly.
+// Bound: HBM, one read and one write of every logit (and 3 bits).  Counting inside the blocks of the stream instead, tile by tile,
+// costs barriers and dependent loads in each of them: 46 us against the figure below for 256 rows x 131072 bf16 logits.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
 #include <algorithm>
 #include <string>
+#include <type_traits>
 
 #include "psa_internal.h"
 
 namespace psa {
 namespace {
 
-constexpr int kRuleThreads = 256;
+constexpr int kListThreads = 512;
+constexpr int kStreamThreads = 256;
 constexpr int kVec = 8;                                    // logits a thread handles together
-constexpr int kRounds = 2;
-constexpr int kKeep = 4;                                   // generated tokens a thread remembers between the two walks
-constexpr int kTile = kRuleThreads * kVec * kRounds;       // 4096 logits
-constexpr int kMarkTile = 32768;                           // tokens of one block's bitmap
+constexpr int kStreamTile = kStreamThreads * kVec;         // logits a block of the stream takes at a time
+constexpr int kStreamRun = 4, kStreamDepth = 4;            // tiles of a block; of them in flight
+constexpr int kWholeRow = 8192;                            // vocabularies up to this are streamed by the row's own block
+constexpr int kSlotsFew = 2048, kSlotsMany = 8192;         // hash table sizes
+constexpr int kMarkTile = 65536;                           // tokens of one block's bitmap
 constexpr int kMarkThreads = 1024;
 constexpr int kMarkBatch = 8;
 
@@ -40,12 +48,9 @@ struct RulesArgs {
     void *out;
     int64_t row_stride, out_stride;
     int vocab;
-};
-
-struct RulesSmem {
-    uint32_t touched[kTile / 32];
-    int32_t count[kTile];
-    float bias[kTile];
+    uint32_t *marks;      // [rows][words]; null: no lists, or kept in shared memory
+    int64_t mark_words;
+    int log2_slots;       // of the largest table
 };
 
 template <bool kF32>
@@ -113,153 +118,340 @@ __device__ __forceinline__ void store_one(void *base, int64_t i, float x)
     else static_cast<__nv_bfloat16 *>(base)[i] = __float2bfloat16_rn(x);
 }
 
-// Biases of one row that fall into [base, base + kTile): added to their cells in list order, by one warp.  Equal ids inside
-// the 32 entries of a step are summed by the first lane that has them, so the order of the additions is that of the list.
-__device__ void add_biases(const RulesArgs &a, RulesSmem &sm, int first, int last, int base, int limit, int lane)
+// What a row needs besides its logits.
+struct Row {
+    float rep, inv_rep;
+    const unsigned char *prompt, *mask;   // bitmaps, may be null
+    __device__ Row(const RulesArgs &a, int row)
+    {
+        const float r = a.r.repetition ? a.r.repetition[row] : 1.f;
+        rep = r > 0.f && r < INFINITY ? r : 1.f;   // not a penalty: off
+        inv_rep = __fdiv_rn(1.f, rep);
+        prompt = rep != 1.f ? bitmap(a.r.prompt_bits, a.r.prompt_row_words, a.r.num_prompt_bitmaps, a.r.prompt_rows, row) : nullptr;
+        mask = bitmap(a.r.mask_bits, a.r.mask_row_words, a.r.num_mask_bitmaps, a.r.mask_rows, row);
+    }
+    static __device__ const unsigned char *bitmap(const uint32_t *bits, int64_t words, int count, const int32_t *rows, int row)
+    {
+        if (!bits) return nullptr;
+        const int64_t p = rows ? rows[row] : row;
+        return p >= 0 && p < count ? reinterpret_cast<const unsigned char *>(bits + p * words) : nullptr;
+    }
+    __device__ __forceinline__ static bool has(const unsigned char *bits, int i) { return (__ldg(bits + (i >> 3)) >> (i & 7)) & 1; }
+    __device__ __forceinline__ float penalised(float x) const { return x * (x > 0.f ? inv_rep : rep); }
+};
+
+// two products at once
+__device__ __forceinline__ void mul2(float &a, float &b, float x, float y, float f)
 {
-    for (int e0 = first; e0 < last; e0 += 32) {
+    asm("{\n\t.reg .b64 p, q;\n\tmov.b64 p, {%2, %3};\n\tmov.b64 q, {%4, %4};\n\tmul.rn.f32x2 p, p, q;\n\tmov.b64 {%0, %1}, p;\n\t}"
+        : "=f"(a), "=f"(b) : "f"(x), "f"(y), "f"(f));
+}
+// The penalty for all eight logits.  With repetition above 1 both of its branches give the smaller one of x / repetition and
+// x * repetition, below 1 the larger one: two products and a minimum, without a comparison.
+template <bool kUp>
+__device__ __forceinline__ void penalise8(float (&y)[8], const float (&x)[8], const Row &row)
+{
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+        float a0, a1, b0, b1;
+        mul2(a0, a1, x[e], x[e + 1], row.inv_rep);
+        mul2(b0, b1, x[e], x[e + 1], row.rep);
+        y[e] = kUp ? fmaxf(a0, b0) : fminf(a0, b0);
+        y[e + 1] = kUp ? fmaxf(a1, b1) : fminf(a1, b1);
+    }
+}
+// Four bits to the top bits of the four bytes of a word: the shifted copies in the product do not overlap.
+__device__ __forceinline__ uint32_t spread4(uint32_t nibble) { return nibble * 0x10204080u; }
+// All ones in the 16-bit halves of a word whose bits among the eight of `lo` (bits 0-3) and `hi` (bits 4-7) are set: logits 2 p and
+// 2 p + 1.  prmt with the top selector bit repeats a byte's sign.
+template <int p>
+__device__ __forceinline__ uint32_t halves(uint32_t lo, uint32_t hi)
+{
+    uint32_t m;
+    asm("prmt.b32 %0, %1, 0, %2;" : "=r"(m) : "r"(p < 2 ? lo : hi), "n"(p % 2 ? 0xBBAA : 0x9988));
+    return m;
+}
+__device__ __forceinline__ uint32_t blend(uint32_t mask, uint32_t set, uint32_t clear) { return (set & mask) | (clear & ~mask); }
+
+// Eight consecutive logits that lie inside the row.  `marked`: those that are in the output already.  bf16 to bf16 stays packed: the
+// three selections are made on pairs.
+template <bool kInF32, bool kOutF32, bool kUp>
+__device__ __forceinline__ void stream8(const Row &row, void *out, int i, const Vec8<kInF32> &v, uint32_t marked, uint32_t seen, uint32_t allowed)
+{
+    float x[8];
+    Vec8<kOutF32> o;
+    if constexpr (!kInF32 && !kOutF32) {
+        uint32_t w[4] = {v.a.x, v.a.y, v.a.z, v.a.w};
+        if (row.prompt) {
+            float y[8];
+            v.get(x);
+            penalise8<kUp>(y, x, row);
+            o.set(y);
+            const uint32_t lo = spread4(seen & 15u), hi = spread4(seen >> 4);
+            w[0] = blend(halves<0>(lo, hi), o.a.x, w[0]);
+            w[1] = blend(halves<1>(lo, hi), o.a.y, w[1]);
+            w[2] = blend(halves<2>(lo, hi), o.a.z, w[2]);
+            w[3] = blend(halves<3>(lo, hi), o.a.w, w[3]);
+        }
+        if (row.mask) {
+            const uint32_t lo = spread4(allowed & 15u), hi = spread4(allowed >> 4), none = 0xFF80FF80u;   // - infinity twice
+            w[0] = blend(halves<0>(lo, hi), w[0], none);
+            w[1] = blend(halves<1>(lo, hi), w[1], none);
+            w[2] = blend(halves<2>(lo, hi), w[2], none);
+            w[3] = blend(halves<3>(lo, hi), w[3], none);
+        }
+        if (marked) {
+            o.load(out, i);
+            const uint32_t lo = spread4(marked & 15u), hi = spread4(marked >> 4);
+            w[0] = blend(halves<0>(lo, hi), o.a.x, w[0]);
+            w[1] = blend(halves<1>(lo, hi), o.a.y, w[1]);
+            w[2] = blend(halves<2>(lo, hi), o.a.z, w[2]);
+            w[3] = blend(halves<3>(lo, hi), o.a.w, w[3]);
+        }
+        o.a = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+        v.get(x);
+        if (row.prompt) {
+            float y[8];
+            penalise8<kUp>(y, x, row);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = seen & (1u << e) ? y[e] : x[e];
+        }
+        if (row.mask) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = allowed & (1u << e) ? x[e] : -INFINITY;
+        }
+        if (marked) {
+            float y[8];
+            o.load(out, i);
+            o.get(y);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = marked & (1u << e) ? y[e] : x[e];
+        }
+        o.set(x);
+    }
+    o.store(out, i);
+}
+
+// The last logits of a row whose vocabulary is not a multiple of eight, by one thread: neither read nor written beyond it.
+template <bool kInF32, bool kOutF32>
+__device__ __forceinline__ void stream_rest(const Row &row, const void *in, void *out, int vocab, const unsigned char *marks)
+{
+    for (int i = vocab & ~7; i < vocab; ++i) {
+        if (marks && (marks[i >> 3] >> (i & 7)) & 1) continue;
+        float x = load_one<kInF32>(in, i);
+        if (row.prompt && Row::has(row.prompt, i)) x = row.penalised(x);
+        store_one<kOutF32>(out, i, row.mask && !Row::has(row.mask, i) ? -INFINITY : x);
+    }
+}
+
+__device__ __forceinline__ const void *row_of(const void *p, int64_t stride, int row, bool f32)
+{
+    return static_cast<const unsigned char *>(p) + int64_t(row) * stride * (f32 ? 4 : 2);
+}
+
+// One block per (row, run of kStreamRun tiles).  A thread copies its own groups of the next kStreamDepth - 1 tiles ahead of itself into
+// shared memory (cp.async), so that enough bytes are on their way without registers or barriers.
+template <bool kInF32, bool kOutF32>
+__global__ void __launch_bounds__(kStreamThreads)
+rules_stream_kernel(RulesArgs a)
+{
+    constexpr int kBytes = kVec * (kInF32 ? 4 : 2);
+    __shared__ __align__(16) unsigned char ring[kStreamDepth][kStreamThreads * kBytes];
+    const int row = blockIdx.y;
+    const int first = blockIdx.x * (kStreamRun * kStreamTile) + threadIdx.x * kVec;
+    const int n = min(kStreamRun, ((a.vocab & ~7) - first + kStreamTile - 1) / kStreamTile);   // whole groups of this thread; may be <= 0
+    const unsigned char *in = static_cast<const unsigned char *>(row_of(a.logits, a.row_stride, row, kInF32));
+    void *out = const_cast<void *>(row_of(a.out, a.out_stride, row, kOutF32));
+    // Behind the lists of the same call the inputs are complete already (that grid has waited for them) and stay as they are unless
+    // they are the output; only the marks and the logits written there have to be waited for.
+    const bool early = a.marks != nullptr && a.logits != a.out;
+    if (!early) asm volatile("griddepcontrol.wait;" ::: "memory");
+    auto request = [&](int t) {
+        if (t < n) {
+            const uint32_t to = uint32_t(__cvta_generic_to_shared(&ring[t % kStreamDepth][threadIdx.x * kBytes]));
+            const unsigned char *from = in + int64_t(first + t * kStreamTile) * (kBytes / kVec);
+#pragma unroll
+            for (int c = 0; c < kBytes; c += 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + c), "l"(from + c) : "memory");
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int t = 0; t < kStreamDepth - 1; ++t) request(t);
+    const Row r(a, row);
+    const unsigned char *marks = a.marks ? reinterpret_cast<const unsigned char *>(a.marks + row * a.mark_words) : nullptr;
+    uint32_t seen, allowed, marked;
+    auto bits = [&](int t) {
+        const int at = (first + t * kStreamTile) >> 3;
+        seen = r.prompt && t < n ? __ldg(r.prompt + at) : 0u;
+        allowed = r.mask && t < n ? __ldg(r.mask + at) : 0u;
+        marked = marks && t < n ? marks[at] : 0u;
+    };
+    if (early) asm volatile("griddepcontrol.wait;" ::: "memory");
+    bits(0);
+    auto work = [&](auto up) {
+        for (int t = 0; t < n; ++t) {
+            request(t + kStreamDepth - 1);
+            const uint32_t s = seen, ok = allowed, m = marked;
+            bits(t + 1);
+            asm volatile("cp.async.wait_group %0;" ::"n"(kStreamDepth - 1) : "memory");
+            Vec8<kInF32> v;
+            v.load(&ring[t % kStreamDepth][threadIdx.x * kBytes], 0);
+            stream8<kInF32, kOutF32, up.value>(r, out, first + t * kStreamTile, v, m, s, ok);
+        }
+    };
+    if (r.rep < 1.f) work(std::true_type{});
+    else work(std::false_type{});
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) stream_rest<kInF32, kOutF32>(r, in, out, a.vocab, marks);
+}
+
+// Where a token's counters are: hashed with linear probing (the table is at most half full), or directly at id - r0.
+struct Table {
+    int32_t *key, *count;
+    float *value;
+    int log2_slots, r0, r1;   // tokens [r0, r1) belong to the table
+    bool hashed;
+    __device__ __forceinline__ int slots() const { return 1 << log2_slots; }
+    __device__ __forceinline__ int add(int id) const
+    {
+        if (id < r0 || id >= r1) return -1;
+        if (!hashed) {
+            key[id - r0] = id;
+            return id - r0;
+        }
+        for (int h = int((uint32_t(id) * 2654435761u) >> (32 - log2_slots));; h = (h + 1) & (slots() - 1)) {
+            const int old = atomicCAS(key + h, -1, id);
+            if (old == -1 || old == id) return h;
+        }
+    }
+    __device__ __forceinline__ int find(int id) const   // of a token that has been added
+    {
+        if (id < r0 || id >= r1) return -1;
+        if (!hashed) return id - r0;
+        int h = int((uint32_t(id) * 2654435761u) >> (32 - log2_slots));
+        while (key[h] != id) h = (h + 1) & (slots() - 1);
+        return h;
+    }
+};
+
+// Adds a row's biases to their tokens' values in list order, by one warp.  Equal tokens inside the 32 entries of a step are summed
+// by the first lane that has them, so the order of the additions is that of the list.
+__device__ void add_biases(const int32_t *ids, const float *values, int n, const Table &t, int lane)
+{
+    for (int e0 = 0; e0 < n; e0 += 32) {
         const int e = e0 + lane;
-        const int id = e < last ? a.r.bias_ids[e] : -1;
-        const float v = e < last ? a.r.bias_values[e] : 0.f;
-        const bool mine = id >= base && id < limit;
-        const uint32_t same = __match_any_sync(0xffffffffu, mine ? id : -1);
-        const bool leader = mine && (__ffs(same) - 1) == lane;
-        float sum = leader ? sm.bias[id - base] : 0.f;
+        const int at = e < n ? t.find(ids[e]) : -1;
+        const float v = e < n ? values[e] : 0.f;
+        const uint32_t same = __match_any_sync(0xffffffffu, at);
+        const bool leader = at >= 0 && (__ffs(same) - 1) == lane;
+        float sum = leader ? t.value[at] : 0.f;
         // every lane takes part in the shuffles; at most 32 rounds, one without duplicates
-        uint32_t rest = mine ? same : 0u;
+        uint32_t rest = at >= 0 ? same : 0u;
         while (__any_sync(0xffffffffu, rest != 0u)) {
             const int from = rest ? __ffs(rest) - 1 : 0;
             const float u = __shfl_sync(0xffffffffu, v, from);
             if (rest) sum += u;
             rest &= rest - 1u;
         }
-        if (leader) sm.bias[id - base] = sum;
+        if (leader) t.value[at] = sum;
         __syncwarp();
     }
 }
 
-template <bool kInF32, bool kOutF32>
-__global__ void __launch_bounds__(kRuleThreads)
-rules_kernel(RulesArgs a)
+template <bool kInF32, bool kOutF32, bool kWhole>
+__global__ void __launch_bounds__(kListThreads)
+rules_lists_kernel(RulesArgs a)
 {
-    extern __shared__ __align__(16) unsigned char smem_raw[];
-    RulesSmem &sm = *reinterpret_cast<RulesSmem *>(smem_raw);
-    const int row = blockIdx.y, base = blockIdx.x * kTile, tid = threadIdx.x;
-    const int limit = min(a.vocab, base + kTile);
-    const void *in = static_cast<const unsigned char *>(a.logits) + int64_t(row) * a.row_stride * (kInF32 ? 4 : 2);
-    void *out = static_cast<unsigned char *>(a.out) + int64_t(row) * a.out_stride * (kOutF32 ? 4 : 2);
-
-    // ---- everything that does not depend on the lists is requested first: the row's numbers, its logits, its bitmaps
+    extern __shared__ __align__(16) int32_t table_smem[];
+    __shared__ uint32_t own_marks[kWhole ? kWholeRow / 32 : 1];
+    const int row = blockIdx.x, tid = threadIdx.x;
+    if (!kWhole) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the stream sets itself up beside this and waits
+    const void *in = row_of(a.logits, a.row_stride, row, kInF32);
+    void *out = const_cast<void *>(row_of(a.out, a.out_stride, row, kOutF32));
     const int32_t *said = a.r.history ? a.r.history + int64_t(row) * a.r.history_stride : nullptr;
-    const int said_len = said ? a.r.history_lens[row] : 0;
-    int b0 = 0, b1 = 0;
-    if (a.r.bias_indptr) { b0 = a.r.bias_indptr[row]; b1 = a.r.bias_indptr[row + 1]; }
-    const float rep_in = a.r.repetition ? a.r.repetition[row] : 1.f;
+    const int n_said = said ? max(0, min(a.r.history_lens[row], a.r.history_capacity)) : 0;
+    int b0 = 0, n_bias = 0;
+    if (a.r.bias_indptr) {
+        b0 = max(0, a.r.bias_indptr[row]);
+        n_bias = max(0, min(a.r.num_biases, a.r.bias_indptr[row + 1]) - b0);
+    }
+    const Row r(a, row);
     const float freq = a.r.frequency ? a.r.frequency[row] : 0.f;
     const float pres = a.r.presence ? a.r.presence[row] : 0.f;
-    const int64_t prompt_row = a.r.prompt_rows && a.r.prompt_bits ? a.r.prompt_rows[row] : row;
-    const int64_t mask_row = a.r.mask_rows && a.r.mask_bits ? a.r.mask_rows[row] : row;
-    Vec8<kInF32> v[kRounds];
+    Vec8<kInF32> v[kWhole ? kWholeRow / kVec / kListThreads : 1];
+    if constexpr (kWhole) {
 #pragma unroll
-    for (int k = 0; k < kRounds; ++k) {
-        const int i = base + (k * kRuleThreads + tid) * kVec;
-        if (i + kVec <= limit) v[k].load(in, i);
+        for (int k = 0; k < kWholeRow / kVec / kListThreads; ++k) {
+            const int i = (k * kListThreads + tid) * kVec;
+            if (i + kVec <= a.vocab) v[k].load(in, i);
+        }
     }
-    const unsigned char *prompt = nullptr, *mask = nullptr;
-    if (a.r.prompt_bits && prompt_row >= 0 && prompt_row < a.r.num_prompt_bitmaps)
-        prompt = reinterpret_cast<const unsigned char *>(a.r.prompt_bits + prompt_row * a.r.prompt_row_words);
-    if (a.r.mask_bits && mask_row >= 0 && mask_row < a.r.num_mask_bitmaps)
-        mask = reinterpret_cast<const unsigned char *>(a.r.mask_bits + mask_row * a.r.mask_row_words);
-    uint32_t seen[kRounds], allowed[kRounds];   // one bit per logit
-#pragma unroll
-    for (int k = 0; k < kRounds; ++k) {
-        const int i = base + (k * kRuleThreads + tid) * kVec;
-        seen[k] = prompt && i < limit ? __ldg(prompt + (i >> 3)) : 0u;
-        allowed[k] = mask && i < limit ? __ldg(mask + (i >> 3)) : 0xFFu;
-    }
+    uint32_t *marks = kWhole ? own_marks : a.marks + row * a.mark_words;
+    for (int w = tid; w < (a.vocab + 31) / 32; w += kListThreads) marks[w] = 0u;
 
-    // ---- the row's lists
-    const int n_said = max(0, min(said_len, a.r.history_capacity));
-    b0 = max(0, b0);
-    b1 = min(a.r.num_biases, b1);
-    const bool lists = n_said > 0 || b1 > b0;   // the same for the whole block
-    if (lists) {
-        int kept[kKeep];   // this thread's first generated tokens, as positions in the tile (-1: elsewhere)
-        for (int w = tid; w < kTile / 32; w += kRuleThreads) sm.touched[w] = 0u;
-        auto place = [&](const int32_t *list, int e, int n) {
-            const int id = e < n ? list[e] : -1;
-            return id >= base && id < limit ? id - base : -1;
-        };
-#pragma unroll
-        for (int j = 0; j < kKeep; ++j) kept[j] = place(said, tid + j * kRuleThreads, n_said);
+    // the smallest table that stays half empty, or all there is, indexed directly
+    const uint32_t entries = uint32_t(n_said) + uint32_t(n_bias);
+    Table t;
+    t.log2_slots = max(9, 32 - __clz(2 * entries));
+    t.hashed = entries < (1u << 30) && t.log2_slots <= a.log2_slots;
+    if (!t.hashed) t.log2_slots = a.log2_slots;
+    t.key = table_smem; t.count = t.key + t.slots(); t.value = reinterpret_cast<float *>(t.count + t.slots());
+    for (int64_t r0 = 0; r0 < a.vocab; r0 += t.slots()) {
+        t.r0 = t.hashed ? 0 : int(r0);
+        t.r1 = t.hashed ? a.vocab : int(min((int64_t)a.vocab, r0 + t.slots()));
+        for (int h = tid; h < t.slots(); h += kListThreads) {
+            t.key[h] = -1;
+            t.count[h] = 0;
+            t.value[h] = 0.f;
+        }
         __syncthreads();
-        auto touch = [&](int at) {
-            if (at >= 0) {
-                sm.count[at] = 0; sm.bias[at] = 0.f;
-                atomicOr(&sm.touched[at >> 5], 1u << (at & 31));
+        for (int e = tid; e < n_said; e += kListThreads) {
+            const int at = t.add(said[e]);
+            if (at >= 0) atomicAdd(t.count + at, 1);
+        }
+        for (int e = tid; e < n_bias; e += kListThreads) t.add(a.r.bias_ids[b0 + e]);
+        __syncthreads();
+        if (n_bias > 0) {   // the same for the whole block
+            if (tid < 32) add_biases(a.r.bias_ids + b0, a.r.bias_values + b0, n_bias, t, tid);
+            __syncthreads();
+        }
+        for (int h0 = tid; h0 < t.slots(); h0 += 4 * kListThreads) {   // the scattered reads of four tokens at once
+            int id[4];
+            float x[4];
+            bool in_prompt[4], allowed[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int h = h0 + k * kListThreads;
+                id[k] = h < t.slots() ? t.key[h] : -1;
+                x[k] = id[k] >= 0 ? load_one<kInF32>(in, id[k]) : 0.f;
+                in_prompt[k] = id[k] >= 0 && r.prompt && Row::has(r.prompt, id[k]);
+                allowed[k] = id[k] < 0 || !r.mask || Row::has(r.mask, id[k]);
             }
-        };
 #pragma unroll
-        for (int j = 0; j < kKeep; ++j) touch(kept[j]);
-        for (int e = tid + kKeep * kRuleThreads; e < n_said; e += kRuleThreads) touch(place(said, e, n_said));
-        for (int e = b0 + tid; e < b1; e += kRuleThreads) touch(place(a.r.bias_ids, e, b1));
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < kKeep; ++j)
-            if (kept[j] >= 0) atomicAdd(&sm.count[kept[j]], 1);
-        for (int e = tid + kKeep * kRuleThreads; e < n_said; e += kRuleThreads) {
-            const int at = place(said, e, n_said);
-            if (at >= 0) atomicAdd(&sm.count[at], 1);
+            for (int k = 0; k < 4; ++k) {
+                if (id[k] < 0) continue;
+                const int h = h0 + k * kListThreads, c = t.count[h];
+                if (c > 0 || in_prompt[k]) x[k] = r.penalised(x[k]);
+                if (c > 0) x[k] = x[k] - freq * float(c) - pres;
+                store_one<kOutF32>(out, id[k], allowed[k] ? x[k] + t.value[h] : -INFINITY);
+                atomicOr(marks + (id[k] >> 5), 1u << (id[k] & 31));
+            }
         }
-        if (tid < 32 && b1 > b0) add_biases(a, sm, b0, b1, base, limit, tid);
         __syncthreads();
+        if (t.hashed) break;
     }
-
-    const float rep = rep_in > 0.f ? rep_in : 1.f;   // not a penalty: off
-    const float inv_rep = __fdiv_rn(1.f, rep);
-    const unsigned char *touched = reinterpret_cast<const unsigned char *>(sm.touched);
-    // a logit whose token is in one of the row's lists
-    auto listed = [&](float x, int local, bool in_prompt) {
-        const int c = sm.count[local];
-        if (c > 0 || in_prompt) x *= x > 0.f ? inv_rep : rep;
-        if (c > 0) x = x - freq * float(c) - pres;
-        return x + sm.bias[local];
-    };
-
+    if constexpr (kWhole) {
+        const unsigned char *bytes = reinterpret_cast<const unsigned char *>(own_marks);
 #pragma unroll
-    for (int k = 0; k < kRounds; ++k) {
-        const int local0 = (k * kRuleThreads + tid) * kVec;
-        const int i = base + local0;
-        if (i >= limit) continue;
-        const uint32_t hits = lists ? touched[local0 >> 3] : 0u;
-        const uint32_t prompt_only = seen[k] & ~hits, ok = allowed[k];
-        float x[8];
-        const bool whole = i + kVec <= limit;
-        if (whole) {
-            v[k].get(x);
-        } else {   // the ragged end of a row: neither read nor written beyond the vocabulary
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = i + e < limit ? load_one<kInF32>(in, i + e) : 0.f;
+        for (int k = 0; k < kWholeRow / kVec / kListThreads; ++k) {
+            const int i = (k * kListThreads + tid) * kVec;
+            if (i + kVec > a.vocab) continue;
+            const uint32_t seen = r.prompt ? __ldg(r.prompt + (i >> 3)) : 0u, allowed = r.mask ? __ldg(r.mask + (i >> 3)) : 0u;
+            if (r.rep < 1.f) stream8<kInF32, kOutF32, true>(r, out, i, v[k], bytes[i >> 3], seen, allowed);
+            else stream8<kInF32, kOutF32, false>(r, out, i, v[k], bytes[i >> 3], seen, allowed);
         }
-        if (hits) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (hits & (1u << e)) x[e] = listed(x[e], local0 + e, seen[k] & (1u << e));
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            if (prompt_only & (1u << e)) x[e] *= x[e] > 0.f ? inv_rep : rep;
-            if (!(ok & (1u << e))) x[e] = -INFINITY;
-        }
-        if (whole) {
-            Vec8<kOutF32> o;
-            o.set(x);
-            o.store(out, i);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (i + e < limit) store_one<kOutF32>(out, i + e, x[e]);
-        }
+        if (tid == 0) stream_rest<kInF32, kOutF32>(r, in, out, a.vocab, bytes);
     }
 }
 
@@ -293,23 +485,48 @@ bool misaligned(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p)
 bool known_dtype(int32_t d) { return d == PSA_OUT_BF16 || d == PSA_OUT_F32; }
 
 template <bool kInF32, bool kOutF32>
-cudaError_t launch_rules(const RulesArgs &a, int rows, cudaStream_t st)
+cudaError_t launch_rules(const RulesArgs &a, int rows, bool lists, cudaStream_t st)
 {
-    static PerDeviceOnce once;
-    const int rc = once.ensure([] {
-        return int(cudaFuncSetAttribute(rules_kernel<kInF32, kOutF32>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(sizeof(RulesSmem))));
-    });
-    if (rc != 0) return cudaError_t(rc);
-    rules_kernel<kInF32, kOutF32><<<dim3((a.vocab + kTile - 1) / kTile, rows), kRuleThreads, sizeof(RulesSmem), st>>>(a);
-    return cudaGetLastError();
+    const size_t table = size_t(12) << a.log2_slots;
+    if (lists) {
+        const bool whole = a.vocab <= kWholeRow;
+        static PerDeviceOnce once;
+        const int rc = once.ensure([] {
+            cudaError_t e = cudaFuncSetAttribute(rules_lists_kernel<kInF32, kOutF32, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, 12 * kSlotsMany);
+            if (e == cudaSuccess)
+                e = cudaFuncSetAttribute(rules_lists_kernel<kInF32, kOutF32, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, 12 * kSlotsMany);
+            return int(e);
+        });
+        if (rc != 0) return cudaError_t(rc);
+        if (whole) rules_lists_kernel<kInF32, kOutF32, true><<<rows, kListThreads, table, st>>>(a);
+        else rules_lists_kernel<kInF32, kOutF32, false><<<rows, kListThreads, table, st>>>(a);
+        const cudaError_t e = cudaGetLastError();
+        if (whole || e != cudaSuccess) return e;
+    }
+    cudaLaunchConfig_t lc{};
+    lc.gridDim = dim3((a.vocab + kStreamRun * kStreamTile - 1) / (kStreamRun * kStreamTile), rows);
+    lc.blockDim = dim3(kStreamThreads);
+    lc.stream = st;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    lc.attrs = &attr;
+    lc.numAttrs = 1;
+    return cudaLaunchKernelEx(&lc, rules_stream_kernel<kInF32, kOutF32>, a);
 }
 
 }  // namespace
 }  // namespace psa
 
+extern "C" size_t psa_process_logits_scratch_bytes(int32_t num_rows, int32_t vocab)
+{
+    if (num_rows <= 0 || vocab <= psa::kWholeRow) return 0;
+    return size_t(num_rows) * ((size_t(vocab) + 31) / 32) * 4;
+}
+
 extern "C" psa_status_t psa_process_logits(const void *logits, int32_t logits_dtype, int64_t row_stride, int32_t num_rows, int32_t vocab,
                                            const psa_logits_rules_t *rules, void *out, int32_t out_dtype, int64_t out_row_stride,
-                                           void *cuda_stream)
+                                           void *scratch, size_t scratch_bytes, void *cuda_stream)
 {
     using psa::set_last_error;
     if (num_rows < 0 || vocab < 0) return set_last_error(PSA_ERR_INVALID_ARG, "negative num_rows or vocab");
@@ -332,13 +549,23 @@ extern "C" psa_status_t psa_process_logits(const void *logits, int32_t logits_dt
     const int64_t words = (int64_t(vocab) + 31) / 32;
     if ((r.prompt_bits && r.prompt_row_words < words) || (r.mask_bits && r.mask_row_words < words))
         return set_last_error(PSA_ERR_INVALID_ARG, "bitmap rows must hold at least ceil(vocab / 32) words");
-    psa::RulesArgs a{r, logits, out, row_stride, out_row_stride, vocab};
+    const bool lists = (r.history && r.history_capacity > 0) || (r.bias_indptr && r.num_biases > 0);
+    psa::RulesArgs a{r, logits, out, row_stride, out_row_stride, vocab, nullptr, words, 0};
+    if (lists && vocab > psa::kWholeRow) {
+        if (!scratch || reinterpret_cast<uintptr_t>(scratch) % 4 || scratch_bytes < psa_process_logits_scratch_bytes(num_rows, vocab))
+            return set_last_error(PSA_ERR_WORKSPACE, "scratch must be 4-byte aligned and hold psa_process_logits_scratch_bytes(num_rows, vocab)");
+        a.marks = static_cast<uint32_t *>(scratch);
+    }
+    // the small table serves lists of fewer than 1024 entries, and leaves room for more blocks beside it
+    const int64_t most = int64_t(r.history ? r.history_capacity : 0) + (r.bias_indptr ? r.num_biases : 0);
+    a.log2_slots = most < psa::kSlotsFew / 2 ? 11 : 13;
+    static_assert(psa::kSlotsFew == 1 << 11 && psa::kSlotsMany == 1 << 13, "table sizes");
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     cudaError_t e;
     if (logits_dtype == PSA_OUT_F32)
-        e = out_dtype == PSA_OUT_F32 ? psa::launch_rules<true, true>(a, num_rows, st) : psa::launch_rules<true, false>(a, num_rows, st);
+        e = out_dtype == PSA_OUT_F32 ? psa::launch_rules<true, true>(a, num_rows, lists, st) : psa::launch_rules<true, false>(a, num_rows, lists, st);
     else
-        e = out_dtype == PSA_OUT_F32 ? psa::launch_rules<false, true>(a, num_rows, st) : psa::launch_rules<false, false>(a, num_rows, st);
+        e = out_dtype == PSA_OUT_F32 ? psa::launch_rules<false, true>(a, num_rows, lists, st) : psa::launch_rules<false, false>(a, num_rows, lists, st);
     if (e != cudaSuccess) return set_last_error(PSA_ERR_CUDA, std::string("logits launch: ") + cudaGetErrorString(e));
     return PSA_OK;
 }

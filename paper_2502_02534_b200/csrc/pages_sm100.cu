@@ -27,7 +27,7 @@ namespace psa {
 namespace {
 
 constexpr int kScanThreads = 1024;
-constexpr int kSpread = 1024;                // most tokens or list entries a warp handles at a time
+constexpr int kSpread = 1024;                // most tokens or list entries a warp handles at a time (their pages fit 3 registers a lane)
 constexpr int64_t kMostEntries = 0x7fffff00; // 32-bit positions, with room for one more stride of a loop
 constexpr int kWalk = 8;                     // samples in such a piece that are walked one after the other
 constexpr int64_t kOneBlockWork = 16384;
@@ -203,22 +203,13 @@ __device__ __forceinline__ int lane_find(const int32_t *offsets, int lo, int hi,
     return lo;
 }
 
-// Token t of sample s (record rec, first token at t_first, list at e_first): its slot; files a fresh page in the list.
-__device__ __forceinline__ long long slot_of(const PageTableArgs &a, int t, int2 rec, int t_first, int e_first, int avail)
+// Page of entry j of a sample's list (record rec, list at e_first); entries from `fresh` on come off the stack.
+__device__ __forceinline__ int page_of(const PageTableArgs &a, int j, int fresh, int2 rec, int e_first, int avail)
 {
-    const int pos = rec.x + (t - t_first);
-    const int j = pos / kPageSize, fresh = (rec.x + kPageSize - 1) / kPageSize;
-    int page;
-    if (j >= fresh) {
-        page = a.free_pages[avail - 1 - (rec.y + j - fresh)];
-        if (!a.build && pos % kPageSize == 0) a.page_indices[(long long)e_first + j] = page;   // the first token of a fresh page files it
-    } else {
-        page = a.page_indices[(long long)e_first + j];
-    }
-    return page >= 0 ? (long long)page * kPageSize + pos % kPageSize : -1;
+    return j >= fresh ? a.free_pages[avail - 1 - (rec.y + j - fresh)] : a.page_indices[(long long)e_first + j];
 }
 
-// Tokens [t0, t0 + piece) of the slot map.
+// Tokens [t0, t0 + piece) of the slot map, piece <= kSpread.
 __device__ void spread_tokens(const PageTableArgs &a, const Tables &tab, long long t0, int piece, int avail, int lane)
 {
     const int n = a.num_samples;
@@ -232,14 +223,57 @@ __device__ void spread_tokens(const PageTableArgs &a, const Tables &tab, long lo
             for (int s = s_lo; s <= s_hi; ++s) {
                 const int2 rec = tab.rec[s];
                 const int t_first = tab.token_indptr[s], stop = min(live, tab.token_indptr[s + 1]), e_first = tab.page_indptr[s];
-                for (int i = t + lane; i < stop; i += 32) a.slot_map[i] = rec.y >= 0 ? slot_of(a, i, rec, t_first, e_first, avail) : -1;
+                if (rec.y < 0) {
+                    for (int i = t + lane; i < stop; i += 32) a.slot_map[i] = -1;
+                } else if (t < stop) {
+                    // the pages of up to 1024 tokens: 65 at most, fetched at once, two a lane and one more
+                    const int pos0 = rec.x + (t - t_first), pos1 = pos0 + (stop - t);
+                    const int j0 = pos0 / kPageSize, j1 = (pos1 - 1) / kPageSize, fresh = (rec.x + kPageSize - 1) / kPageSize;
+                    int page[3];
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) {
+                        const int j = j0 + k * 32 + lane;
+                        page[k] = j <= j1 ? page_of(a, j, fresh, rec, e_first, avail) : -1;
+                    }
+                    if (!a.build)   // the piece that holds a fresh page's first token files the page
+#pragma unroll
+                        for (int k = 0; k < 3; ++k) {
+                            const int j = j0 + k * 32 + lane;
+                            if (j <= j1 && j >= fresh && j * kPageSize >= pos0) a.page_indices[(long long)e_first + j] = page[k];
+                        }
+                    for (int base = 0; base < pos1 - pos0; base += 32) {
+                        const int pos = pos0 + base + lane, at = min(pos, pos1 - 1) / kPageSize - j0;
+                        const int p0 = __shfl_sync(0xffffffffu, page[0], at & 31), p1 = __shfl_sync(0xffffffffu, page[1], at & 31);
+                        const int p2 = __shfl_sync(0xffffffffu, page[2], at & 31);
+                        const int p = at < 32 ? p0 : at < 64 ? p1 : p2;
+                        if (pos < pos1) a.slot_map[t + base + lane] = p >= 0 ? (long long)p * kPageSize + pos % kPageSize : -1;
+                    }
+                }
                 t = max(t, stop);
             }
         } else {
-            for (int i = t + lane; i < live; i += 32) {
-                const int s = lane_find(tab.token_indptr, s_lo, s_hi + 1, i);
-                const int2 rec = tab.rec[s];
-                a.slot_map[i] = rec.y >= 0 ? slot_of(a, i, rec, tab.token_indptr[s], tab.page_indptr[s], avail) : -1;
+            for (int i0 = t; i0 < live; i0 += 4 * 32) {   // four lookups in flight per lane
+                int page[4], in_page[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int i = i0 + k * 32 + lane;
+                    page[k] = -1;
+                    in_page[k] = 0;
+                    if (i < live) {
+                        const int s = lane_find(tab.token_indptr, s_lo, s_hi + 1, i);
+                        const int2 rec = tab.rec[s];
+                        if (rec.y >= 0) {
+                            const int pos = rec.x + (i - tab.token_indptr[s]), j = pos / kPageSize, fresh = (rec.x + kPageSize - 1) / kPageSize;
+                            const int e_first = tab.page_indptr[s];
+                            in_page[k] = pos % kPageSize;
+                            page[k] = page_of(a, j, fresh, rec, e_first, avail);
+                            if (!a.build && j >= fresh && in_page[k] == 0) a.page_indices[(long long)e_first + j] = page[k];
+                        }
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (i0 + k * 32 + lane < live) a.slot_map[i0 + k * 32 + lane] = page[k] >= 0 ? (long long)page[k] * kPageSize + in_page[k] : -1;
             }
             t = live;
         }
@@ -261,7 +295,17 @@ __device__ void spread_entries(const PageTableArgs &a, const Tables &tab, long l
     int e = int(e0);
     if (e < live) {
         const int s_lo = warp_find(tab.page_indptr, 0, n, e, lane), s_hi = warp_find(tab.page_indptr, s_lo, n, live - 1, lane);
-        for (int i = e + lane; i < live; i += 32) a.page_indices[i] = entry(i, s_lo == s_hi ? s_lo : lane_find(tab.page_indptr, s_lo, s_hi + 1, i));
+        for (int i0 = e; i0 < live; i0 += 4 * 32) {   // four lookups in flight per lane
+            int page[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int i = i0 + k * 32 + lane;
+                page[k] = i < live ? entry(i, s_lo == s_hi ? s_lo : lane_find(tab.page_indptr, s_lo, s_hi + 1, i)) : -1;
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (i0 + k * 32 + lane < live) a.page_indices[i0 + k * 32 + lane] = page[k];
+        }
         e = live;
     }
     for (int i = e + lane; i < end; i += 32) a.page_indices[i] = -1;

@@ -43,7 +43,7 @@ def case(R, V, seed, said=40, n_bias=12, hot=True):
     masks = [set(rng.integers(0, V, max(1, V // 3)).tolist()), set(), set(range(V))]
     mask_rows = rng.integers(-1, 4, R)                                # -1 and 3: none; 1: nothing allowed
     return dict(x=x, history=history, lens=lens, biases=biases, prompts=prompts, prompt_rows=prompt_rows, masks=masks, mask_rows=mask_rows,
-                rep=rng.choice([1.0, 1.3, 0.8, 0.0, np.nan, -2.0], R).astype(np.float32), freq=rng.choice([0, 0.25, -0.1], R).astype(np.float32),
+                rep=rng.choice([1.0, 1.3, 0.8, 0.0, np.nan, -2.0, np.inf], R).astype(np.float32), freq=rng.choice([0, 0.25, -0.1], R).astype(np.float32),
                 pres=rng.choice([0, 0.4], R).astype(np.float32))
 
 
@@ -128,9 +128,9 @@ def test_infinite_and_nan_logits():
     run(c, 600, "f32", "f32", ALL)
 
 
-def test_many_repeats_long_lists_and_the_same_result_each_time():
-    V = 20000
-    c = case(3, V, 7, said=5000, n_bias=700)
+@pytest.mark.parametrize("V,said", [(20000, 5000), (20000, 1500), (3000, 6000), (8192, 1030), (8193, 1025)])
+def test_many_repeats_long_lists_and_the_same_result_each_time(V, said):
+    c = case(3, V, 7, said=said, n_bias=700)
     c["biases"][2] = [(11, float(np.float32(v))) for v in np.random.default_rng(0).normal(0, 100, 900)]      # one token, 900 biases, in list order
     first = run(c, V, "f32", "f32", ALL)
     for _ in range(5):
@@ -155,6 +155,20 @@ def test_lengths_beyond_the_capacity_are_cut_and_lists_stay_inside_their_arrays(
     cut = dict(c, lens=np.array([c["history"].shape[1], 0, c["history"].shape[1]]), biases=[flat[:2], flat[2:], []])
     seen = c["x"].astype(np.float64)
     compare(got, reference(cut, seen, ("freq", "history", "bias")), seen, cut, "f32")
+
+
+def test_scratch_of_the_callers_is_used_and_too_little_of_it_refused():
+    import torch
+    from paper_2502_02534_b200 import library, process_logits
+    c = case(3, 9000, 12)
+    _, x = padded(c["x"], "f32")
+    kw = arguments(c, 9000, ALL)
+    need = library().psa_process_logits_scratch_bytes(3, 9000)
+    scratch = torch.full((need + 64,), 255, dtype=torch.uint8, device="cuda")
+    a, b = process_logits(x, scratch=scratch, **kw), process_logits(x, **kw)
+    assert torch.equal(a.isnan(), b.isnan()) and torch.equal(a.nan_to_num(), b.nan_to_num()) and (scratch[need:] == 255).all()
+    with pytest.raises(ValueError, match="scratch"):
+        process_logits(x, scratch=scratch[:need - 1], **kw)
 
 
 def test_processed_logits_are_what_sampling_draws_from():
