@@ -20,6 +20,7 @@
 
 #include <algorithm>
 #include <string>
+#include <type_traits>
 
 #include "psa_internal.h"
 
@@ -27,11 +28,12 @@ namespace psa {
 namespace {
 
 constexpr int kScanThreads = 1024;
-constexpr int kSpread = 1024;                // most tokens or list entries a warp handles at a time (their pages fit 3 registers a lane)
+constexpr int kSpread = 256;                 // most tokens or list entries a warp handles at a time
+constexpr int kPageRegs = (kSpread / 16 + 1 + 31) / 32;   // registers a lane needs for a 32nd of their pages
 constexpr int64_t kMostEntries = 0x7fffff00; // 32-bit positions, with room for one more stride of a loop
 constexpr int kWalk = 8;                     // samples in such a piece that are walked one after the other
-constexpr int64_t kOneBlockWork = 16384;
-constexpr int kOneBlockSamples = 2048;       // offsets and records of these fit in 32 KB of shared memory
+constexpr int64_t kOneBlockWork = 4096;      // one block: 1024 samples x 4 tokens 8.6 us, 2048 x 4 15.1 us; two launches ~8 and ~9 us
+constexpr int kOneBlockSamples = 1024;
 
 struct PageTableArgs {
     const int32_t *held;       // null: nothing is held yet (a table built from scratch)
@@ -226,27 +228,33 @@ __device__ void spread_tokens(const PageTableArgs &a, const Tables &tab, long lo
                 if (rec.y < 0) {
                     for (int i = t + lane; i < stop; i += 32) a.slot_map[i] = -1;
                 } else if (t < stop) {
-                    // the pages of up to 1024 tokens: 65 at most, fetched at once, two a lane and one more
+                    // the pages of up to kSpread tokens are fetched at once, a few a lane, and go round by shuffles: two pages
+                    // of 16 slots per store of the warp
                     const int pos0 = rec.x + (t - t_first), pos1 = pos0 + (stop - t);
                     const int j0 = pos0 / kPageSize, j1 = (pos1 - 1) / kPageSize, fresh = (rec.x + kPageSize - 1) / kPageSize;
-                    int page[3];
+                    int page[kPageRegs];
 #pragma unroll
-                    for (int k = 0; k < 3; ++k) {
+                    for (int k = 0; k < kPageRegs; ++k) {
                         const int j = j0 + k * 32 + lane;
                         page[k] = j <= j1 ? page_of(a, j, fresh, rec, e_first, avail) : -1;
                     }
                     if (!a.build)   // the piece that holds a fresh page's first token files the page
 #pragma unroll
-                        for (int k = 0; k < 3; ++k) {
+                        for (int k = 0; k < kPageRegs; ++k) {
                             const int j = j0 + k * 32 + lane;
                             if (j <= j1 && j >= fresh && j * kPageSize >= pos0) a.page_indices[(long long)e_first + j] = page[k];
                         }
-                    for (int base = 0; base < pos1 - pos0; base += 32) {
-                        const int pos = pos0 + base + lane, at = min(pos, pos1 - 1) / kPageSize - j0;
-                        const int p0 = __shfl_sync(0xffffffffu, page[0], at & 31), p1 = __shfl_sync(0xffffffffu, page[1], at & 31);
-                        const int p2 = __shfl_sync(0xffffffffu, page[2], at & 31);
-                        const int p = at < 32 ? p0 : at < 64 ? p1 : p2;
-                        if (pos < pos1) a.slot_map[t + base + lane] = p >= 0 ? (long long)p * kPageSize + pos % kPageSize : -1;
+                    int64_t *to = a.slot_map + t - pos0;
+#pragma unroll
+                    for (int k = 0; k < kPageRegs; ++k) {
+                        const int last = min(j1 - j0 - k * 32, 31);   // of this register's pages; the same in all lanes
+#pragma unroll 4
+                        for (int w = 0; w <= last; w += 2) {
+                            const int mine = w + (lane >> 4);
+                            const int p = __shfl_sync(0xffffffffu, page[k], mine);
+                            const int pos = (j0 + k * 32 + mine) * kPageSize + (lane & 15);
+                            if (pos >= pos0 && pos < pos1) to[pos] = p >= 0 ? (long long)p * kPageSize + (lane & 15) : -1;
+                        }
                     }
                 }
                 t = max(t, stop);
@@ -278,6 +286,7 @@ __device__ void spread_tokens(const PageTableArgs &a, const Tables &tab, long lo
             t = live;
         }
     }
+#pragma unroll 8
     for (int i = t + lane; i < end; i += 32) a.slot_map[i] = -1;
 }
 
@@ -382,6 +391,7 @@ page_table_scan_kernel(PageTableArgs a)
     }
 }
 
+template <int kPiece>
 __global__ void __launch_bounds__(256)
 page_table_spread_kernel(PageTableArgs a)
 {
@@ -392,7 +402,7 @@ page_table_spread_kernel(PageTableArgs a)
         for (int b = 0; b < a.scan_blocks; ++b) used = max(used, a.block_used[b]);
         *a.free_count_out = avail - used;
     }
-    spread(a, Tables{a.token_indptr, a.page_indptr, a.rec}, kSpread, avail, (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5), (long long)gridDim.x * (blockDim.x >> 5),
+    spread(a, Tables{a.token_indptr, a.page_indptr, a.rec}, kPiece, avail, (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5), (long long)gridDim.x * (blockDim.x >> 5),
            threadIdx.x & 31);
 }
 
@@ -423,17 +433,24 @@ psa_status_t run(PageTableArgs a, void *scratch, size_t scratch_bytes, void *cud
         page_table_scan_kernel<<<a.scan_blocks, kScanThreads, 0, st>>>(a);
         e = cudaGetLastError();
         if (e == cudaSuccess) {
-            const int64_t warps = (work + kSpread - 1) / kSpread;
-            cudaLaunchConfig_t lc{};
-            lc.gridDim = dim3(unsigned(std::max<int64_t>(1, std::min<int64_t>((warps + 7) / 8, 148 * 8))));
-            lc.blockDim = dim3(256);
-            lc.stream = st;
-            cudaLaunchAttribute attr{};
-            attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-            attr.val.programmaticStreamSerializationAllowed = 1;
-            lc.attrs = &attr;
-            lc.numAttrs = 1;
-            e = cudaLaunchKernelEx(&lc, page_table_spread_kernel, a);
+            // pieces small enough to keep the machine's warps busy: 8.9 million lookups take 22 us in pieces of 256 and 30 in 128,
+            // 270 thousand 9.4 and 7.6, 8 thousand 15 and 12.4 (11.6 in 32)
+            auto go = [&](auto piece) {
+                const int64_t warps = (work + piece.value - 1) / piece.value;
+                cudaLaunchConfig_t lc{};
+                lc.gridDim = dim3(unsigned(std::max<int64_t>(1, std::min<int64_t>((warps + 7) / 8, 148 * 8))));
+                lc.blockDim = dim3(256);
+                lc.stream = st;
+                cudaLaunchAttribute attr{};
+                attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+                attr.val.programmaticStreamSerializationAllowed = 1;
+                lc.attrs = &attr;
+                lc.numAttrs = 1;
+                return cudaLaunchKernelEx(&lc, page_table_spread_kernel<piece.value>, a);
+            };
+            if (work >= 2000000) e = go(std::integral_constant<int, kSpread>{});
+            else if (work >= 65536) e = go(std::integral_constant<int, 128>{});
+            else e = go(std::integral_constant<int, 32>{});
         }
     }
     if (e != cudaSuccess) return set_last_error(PSA_ERR_CUDA, std::string("page table launch: ") + cudaGetErrorString(e));
