@@ -1,7 +1,6 @@
 from __future__ import annotations
 
 import ctypes
-import functools
 from ctypes import POINTER, c_char_p, c_float, c_int32, c_int64, c_size_t, c_void_p
 from dataclasses import dataclass
 from pathlib import Path
@@ -468,64 +467,47 @@ def host_staging_bytes(plan: Plan, n_prefix_tokens: int, n_pool_pages: int, n_pa
     return int(library().psa_decode_host_staging_bytes(plan.handle, n_prefix_tokens, n_pool_pages, n_page_indices))
 
 
-# ---- page tables, the 4-bit cache and rules on logits.  These check the tensors they are given: type, layout, size, and that all of
-# ---- them live on the current CUDA device (ValueError otherwise); what the library itself refuses comes back as PsaError.
-# ---- The checks are written for the latency of a decode step: a handful of attribute reads per tensor, no per-call imports.
+# ---- page tables, the 4-bit cache and rules on logits.  Their tensors are checked (type, layout, size, and that all of them live on the
+# ---- current CUDA device: ValueError otherwise) and marshalled by the native module _torch_calls; what the library itself refuses comes
+# ---- back as PsaError.
 
-_torch = None
+_CALLS_PATH = _HERE / "_torch_calls.so"
+_calls = None
 
 
-def _bind_torch():
-    """Module-level references for the functions below (torch is not needed to import this module)."""
-    global _torch, _i32_t, _i64_t, _u8_t, _bf16_t, _f32_t, _current_device, _raw_stream
+def _native():
+    """Load _torch_calls.so.  Raises if it has not been built: there is no other implementation."""
+    global _calls
+    if _calls is None:
+        import importlib.util
+        import torch  # noqa: F401  (the module's own libraries)
+        library()
+        if not _CALLS_PATH.exists():
+            raise ImportError(f"{_CALLS_PATH} is missing: build it with `python -m paper_2502_02534_b200.build`")
+        spec = importlib.util.spec_from_file_location("_torch_calls", _CALLS_PATH)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        module.attach(str(_LIB_PATH))
+        _calls = module
+    return _calls
+
+
+def _scratch(nbytes, like, stream):
+    """A scratch tensor for one call on `stream` (None: the current one)."""
     import torch
-    _i32_t, _i64_t, _u8_t, _bf16_t, _f32_t = torch.int32, torch.int64, torch.uint8, torch.bfloat16, torch.float32
-    _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
-    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
-    _torch = torch
+    t = torch.empty(int(nbytes), dtype=torch.uint8, device=like.device)
+    if stream is not None and t.is_cuda:      # allocated on the current stream, used on another one: not to be reused before that is done
+        t.record_stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
+    return t
 
 
-def _flat(t, dtype, name, dev, size=0):
-    """Address of a contiguous tensor of at least `size` elements on device `dev` (None passes through)."""
-    if t is None:
-        return None
-    if t.dtype is dtype and t.get_device() == dev and t.is_contiguous() and t.numel() >= size:
-        return t.data_ptr()
-    if t.dtype is not dtype:
-        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
-    if not t.is_contiguous() or t.numel() < size:
-        raise ValueError(f"{name} must be contiguous" + (f" and hold at least {size} elements" if size else ""))
-    raise ValueError(f"{name} must be on the current CUDA device")
-
-
-def _device_of(t, name):
-    """The device the call runs on: that of tensor `t`, which must be the current one."""
-    dev = t.get_device()
-    if dev < 0 or dev != _current_device():
-        raise ValueError(f"{name} must be on the current CUDA device")
-    return dev
-
-
-def _stream_on(stream, dev):
-    return _raw_stream(dev) if stream is None else _stream_ptr(stream)
-
-
-@functools.lru_cache(maxsize=256)
-def _strides2(a, b):
-    return (c_int64 * 2)(a, b)
-
-
-def _outer_strides(t, inner, name):
-    """Strides of dimensions 0 and 1 of a 3-d tensor whose last dimension is contiguous; a dimension of one element has none of its own."""
-    s0, s1, s2 = t.stride()
-    n0, n1, n2 = t.shape
-    if n2 != inner or (s2 != 1 and n2 > 1):
-        raise ValueError(f"{name} must be [.., .., {inner}] with a contiguous last dimension")
-    if n1 <= 1:
-        s1 = inner
-    if n0 <= 1:
-        s0 = max(1, n1) * max(s1, inner)
-    return _strides2(s0, s1)
+def _status_tensor(status):
+    """A status word: a one-element int32 tensor, or a Plan (the word Plan.check_status reads)."""
+    if isinstance(status, Plan):
+        if status.workspace is None:
+            raise ValueError("status: the plan has no workspace yet")
+        return status.workspace
+    return status
 
 
 def page_table_scratch(num_samples):
@@ -540,64 +522,36 @@ def build_page_table(seq_lens, free_pages, free_count, page_indptr, page_indices
     reserve_lens), pages from the stack free_pages[0 .. free_count), and the slot of every token.  Outputs: page_indptr [B+1],
     page_indices (any capacity), token_indptr [B+1], slot_map (any capacity), lens_out [B], free_count_out (free_count in place
     when None)."""
-    if _torch is None:
-        _bind_torch()
-    i32, n, dev = _i32_t, seq_lens.numel(), seq_lens.get_device()
-    p_seq = _flat(seq_lens, i32, "seq_lens", dev)
-    p_indptr = _flat(page_indptr, i32, "page_indptr", dev, n + 1)
-    p_tokens = _flat(token_indptr, i32, "token_indptr", dev, n + 1)
-    dev = _device_of(seq_lens, "seq_lens")
+    if status is not None:
+        status = _status_tensor(status)
     if scratch is None:
-        scratch = page_table_scratch(n)
-    p_count = _flat(free_count, i32, "free_count", dev, 1)
-    _check(library().psa_build_page_table(
-        p_seq, _flat(reserve_lens, i32, "reserve_lens", dev, n), n, _flat(free_pages, i32, "free_pages", dev), p_count,
-        p_count if free_count_out is None else _flat(free_count_out, i32, "free_count_out", dev, 1), p_indptr,
-        _flat(page_indices, i32, "page_indices", dev), page_indices.numel(), p_tokens, _flat(slot_map, _i64_t, "slot_map", dev), slot_map.numel(),
-        _flat(lens_out, i32, "lens_out", dev, n), _status_ptr(status, dev), _flat(scratch, _u8_t, "scratch", dev), scratch.numel(),
-        _stream_on(stream, dev)))
+        scratch = _scratch(library().psa_page_table_scratch_bytes(seq_lens.numel()), seq_lens, stream)
+    rc = (_calls or _native()).build_page_table(seq_lens, reserve_lens, free_pages, free_count, free_count_out, page_indptr, page_indices,
+                                                token_indptr, slot_map, lens_out, status, scratch, stream)
+    if rc:
+        _check(rc)
 
 
 def extend_page_table(held_lens, new_lens, free_pages, free_count, page_indptr, page_indices, token_indptr, slot_map, *, max_lens=None,
                       lens_out=None, free_count_out=None, status=None, scratch=None, stream=None):
     """psa_extend_page_table on torch CUDA tensors: new_lens more tokens for samples that hold held_lens, in existing page lists.
     Outputs as for build_page_table; lens_out and free_count_out may be held_lens and free_count themselves."""
-    if _torch is None:
-        _bind_torch()
-    i32, n, dev = _i32_t, held_lens.numel(), held_lens.get_device()
-    p_held = _flat(held_lens, i32, "held_lens", dev)
-    p_new = _flat(new_lens, i32, "new_lens", dev, n)
-    p_indptr = _flat(page_indptr, i32, "page_indptr", dev, n + 1)
-    p_tokens = _flat(token_indptr, i32, "token_indptr", dev, n + 1)
-    dev = _device_of(held_lens, "held_lens")
+    if status is not None:
+        status = _status_tensor(status)
     if scratch is None:
-        scratch = page_table_scratch(n)
-    p_count = _flat(free_count, i32, "free_count", dev, 1)
-    _check(library().psa_extend_page_table(
-        p_held, p_new, _flat(max_lens, i32, "max_lens", dev, n), n, _flat(free_pages, i32, "free_pages", dev), p_count,
-        p_count if free_count_out is None else _flat(free_count_out, i32, "free_count_out", dev, 1), p_indptr,
-        _flat(page_indices, i32, "page_indices", dev), page_indices.numel(), p_tokens, _flat(slot_map, _i64_t, "slot_map", dev), slot_map.numel(),
-        _flat(lens_out, i32, "lens_out", dev, n), _status_ptr(status, dev), _flat(scratch, _u8_t, "scratch", dev), scratch.numel(),
-        _stream_on(stream, dev)))
-
-
-def _status_ptr(status, dev):
-    """A status word: a one-element int32 tensor, or a Plan (the word Plan.check_status reads)."""
-    if status is None:
-        return None
-    if isinstance(status, Plan):
-        if status.workspace is None:
-            raise ValueError("status: the plan has no workspace yet")
-        return _flat(status.workspace, _u8_t, "status", dev)
-    return _flat(status, _i32_t, "status", dev, 1)
+        scratch = _scratch(library().psa_page_table_scratch_bytes(held_lens.numel()), held_lens, stream)
+    rc = (_calls or _native()).extend_page_table(held_lens, new_lens, max_lens, free_pages, free_count, free_count_out, page_indptr, page_indices,
+                                                 token_indptr, slot_map, lens_out, status, scratch, stream)
+    if rc:
+        _check(rc)
 
 
 def read_status(status, stream=None):
     """psa_read_status: synchronise, raise if the one-element int32 tensor `status` holds an error, and clear it."""
-    if _torch is None:
-        _bind_torch()
-    dev = _device_of(status, "status")
-    _check(library().psa_read_status(_flat(status, _i32_t, "status", dev, 1), _stream_on(stream, dev)))
+    import torch
+    if status.dtype is not torch.int32 or status.numel() < 1 or not status.is_cuda:
+        raise ValueError("status must be a one-element int32 CUDA tensor")
+    _check(library().psa_read_status(status.data_ptr(), _stream_ptr(stream)))
 
 
 def kv4_cell_bytes(head_dim) -> int:
@@ -605,101 +559,57 @@ def kv4_cell_bytes(head_dim) -> int:
     return int(library().psa_kv4_cell_bytes(int(head_dim)))
 
 
-def _kv4_args(k, v, slot_map, pool, names):
-    shape = k.shape
-    if len(shape) != 3 or k.dtype is not _bf16_t or v.dtype is not _bf16_t or v.shape != shape or v.stride() != k.stride():
-        raise ValueError(f"{names} must be bf16 [tokens, heads, head_dim] of the same shape and strides")
-    tokens, heads, dim = shape
-    if pool.dtype is not _u8_t or pool.dim() != 3 or pool.shape[1] != heads:
-        raise ValueError("pool must be uint8 [pages, heads, kv4_cell_bytes(head_dim)]")
-    if slot_map.dtype is not _i64_t or slot_map.numel() < tokens or not slot_map.is_contiguous():
-        raise ValueError(f"slot_map must be contiguous int64 with at least {tokens} elements")
-    dev = _device_of(k, names)
-    if v.get_device() != dev or slot_map.get_device() != dev or pool.get_device() != dev:
-        raise ValueError("all tensors must be on the current CUDA device")
-    return tokens, heads, dim, _outer_strides(k, dim, names), _outer_strides(pool, 20 * dim, "pool"), dev
-
-
 def store_kv4(new_k, new_v, slot_map, pool, *, status=None, stream=None):
     """psa_store_kv4: quantise new_k / new_v [T, Hkv, D] bf16 (any token and head stride) into the slots of a 4-bit pool
     [pages, Hkv, kv4_cell_bytes(D)] uint8."""
-    if _torch is None:
-        _bind_torch()
-    t, h, d, kst, pst, dev = _kv4_args(new_k, new_v, slot_map, pool, "new_k and new_v")
-    _check(library().psa_store_kv4(new_k.data_ptr(), new_v.data_ptr(), kst, slot_map.data_ptr(), t, h, d, pool.data_ptr(), pst,
-                                   pool.shape[0], _status_ptr(status, dev), _stream_on(stream, dev)))
+    if status is not None:
+        status = _status_tensor(status)
+    rc = (_calls or _native()).store_kv4(new_k, new_v, slot_map, pool, status, stream)
+    if rc:
+        _check(rc)
 
 
 def load_kv4(pool, slot_map, out_k, out_v, *, status=None, stream=None):
     """psa_load_kv4: the cached tokens of slot_map as bf16 rows out_k / out_v [T, Hkv, D]; rows of negative slots are left alone."""
-    if _torch is None:
-        _bind_torch()
-    t, h, d, kst, pst, dev = _kv4_args(out_k, out_v, slot_map, pool, "out_k and out_v")
-    _check(library().psa_load_kv4(pool.data_ptr(), pst, pool.shape[0], slot_map.data_ptr(), t, h, d, out_k.data_ptr(), out_v.data_ptr(),
-                                  kst, _status_ptr(status, dev), _stream_on(stream, dev)))
+    if status is not None:
+        status = _status_tensor(status)
+    rc = (_calls or _native()).load_kv4(out_k, out_v, slot_map, pool, status, stream)
+    if rc:
+        _check(rc)
 
 
 def decode_kv4(plan: Plan, q, prefix_k, prefix_v, pool, page_indptr, page_indices, suffix_lens, out, lse, *, prefix_strides=None,
                stream=None, stage="all"):
     """psa_decode_kv4 (or one of its stages): decode with the samples' own tokens in a 4-bit pool [pages, Hkv, kv4_cell_bytes(D)]
     uint8.  Everything else as for decode; the work lists and the workspace are those of plan.for_kv4()."""
-    if _torch is None:
-        _bind_torch()
-    if stage not in ("all", "prefix", "suffix", "merge"):
-        raise ValueError(stage)
     plan = plan._kv4 or plan.for_kv4()
+    if stage != "all":
+        return _decode_kv4_stage(plan, q, prefix_k, prefix_v, pool, page_indptr, page_indices, suffix_lens, out, lse, prefix_strides, stream, stage)
+    if plan.workspace is None:
+        if not pool.is_cuda:
+            raise ValueError("pool must be on the current CUDA device")
+        plan.bind_workspace(stream=stream)
+    head_dim = plan.head_dim
+    s0, s1 = (plan.num_kv_heads * head_dim, head_dim) if prefix_strides is None else prefix_strides
+    rc = (_calls or _native()).decode_kv4(plan._h.value, plan.suffix_len_bounds.size, plan.num_q_heads, plan.num_kv_heads, head_dim, plan.out_dtype, q, prefix_k,
+                                          prefix_v, s0, s1, pool, page_indptr, page_indices, suffix_lens, out, lse, plan.workspace, stream)
+    if rc:
+        _check(rc)
+
+
+def _decode_kv4_stage(plan, q, prefix_k, prefix_v, pool, page_indptr, page_indices, suffix_lens, out, lse, prefix_strides, stream, stage):
+    """One stage of a 4-bit step, for tests and per-kernel timing."""
     if stage in ("prefix", "merge"):
-        decode(plan, q, prefix_k, prefix_v, None, None, page_indptr, page_indices, suffix_lens, out, lse, prefix_strides=prefix_strides,
-               stream=stream, stage=stage)
-        return
-    if pool.dtype is not _u8_t or pool.dim() != 3 or pool.shape[1] != plan.num_kv_heads:
-        raise ValueError("pool must be uint8 [pages, num_kv_heads, kv4_cell_bytes(head_dim)]")
-    pst = _outer_strides(pool, 20 * plan.head_dim, "pool")
-    rows, i32 = plan.suffix_len_bounds.size, _i32_t
-    dev = _device_of(pool, "pool")
+        return decode(plan, q, prefix_k, prefix_v, None, None, page_indptr, page_indices, suffix_lens, out, lse, prefix_strides=prefix_strides,
+                      stream=stream, stage=stage)
+    if stage != "suffix":
+        raise ValueError(stage)
+    if pool.dim() != 3 or pool.element_size() != 1 or pool.stride(2) != 1 or not pool.is_cuda:
+        raise ValueError("pool must be uint8 [pages, num_kv_heads, kv4_cell_bytes(head_dim)] on the current CUDA device")
     if plan.workspace is None:
         plan.bind_workspace(stream=stream)
-    lib, ws, heads = library(), plan.workspace, rows * plan.num_q_heads
-    p_q = _flat(q, _bf16_t, "q", dev, heads * plan.head_dim)
-    p_indptr = _flat(page_indptr, i32, "page_indptr", dev, rows + 1)
-    p_indices = _flat(page_indices, i32, "page_indices", dev)
-    p_lens = _flat(suffix_lens, i32, "suffix_lens", dev, rows)
-    st = _stream_on(stream, dev)
-    if stage == "suffix":
-        _check(lib.psa_decode_suffix_kv4(plan._h, p_q, pool.data_ptr(), pst, p_indptr, p_indices, p_lens, ws.data_ptr(), ws.numel(), st))
-        return
-    for t, name in ((prefix_k, "prefix_k"), (prefix_v, "prefix_v")):
-        if t is not None and (t.dtype is not _bf16_t or t.get_device() != dev):
-            raise ValueError(f"{name} must be bf16 on the current CUDA device")
-    p_out = _flat(out, _f32_t if plan.out_dtype == PSA_OUT_F32 else _bf16_t, "out", dev, heads * plan.head_dim)
-    p_lse = _flat(lse, _f32_t, "lse", dev, heads)
-    kst = _strides2(plan.num_kv_heads * plan.head_dim, plan.head_dim) if prefix_strides is None else _strides2(*prefix_strides)
-    _check(lib.psa_decode_kv4(plan._h, p_q, _ptr(prefix_k), _ptr(prefix_v), kst, pool.data_ptr(), pst, p_indptr, p_indices, p_lens,
-                              p_out, p_lse, ws.data_ptr(), ws.numel(), st))
-
-
-def _dtype_code(t, name):
-    if t.dtype is _bf16_t:
-        return PSA_OUT_BF16
-    if t.dtype is _f32_t:
-        return PSA_OUT_F32
-    raise ValueError(f"{name} must be bf16 or f32, not {t.dtype}")
-
-
-def _bitmap_args(bits, rows, words, R, name, dev):
-    """(address, row stride in words, number of bitmaps, address of the row numbers) of a set of bitmaps."""
-    if bits is None:
-        if rows is not None:
-            raise ValueError(f"{name}_rows without {name}_bits")
-        return None, 0, 0, None
-    count, width = bits.shape if bits.dim() == 2 else (0, -1)
-    if bits.dtype is not _i32_t or width < words or (bits.stride(1) != 1 and width > 1):
-        raise ValueError(f"{name}_bits must be int32 [bitmaps, words >= {words}], contiguous along the second dimension")
-    if rows is None and count < R:
-        raise ValueError(f"{name}_bits needs one bitmap per row, or {name}_rows")
-    if bits.get_device() != dev:
-        raise ValueError(f"{name}_bits must be on the current CUDA device")
-    return bits.data_ptr(), bits.stride(0) if count > 1 else width, count, _flat(rows, _i32_t, f"{name}_rows", dev, R)
+    _check(library().psa_decode_suffix_kv4(plan.handle, _ptr(q), _ptr(pool), _strides(pool.stride()[:2], 2), _ptr(page_indptr), _ptr(page_indices),
+                                           _ptr(suffix_lens), _ptr(plan.workspace), plan.workspace.numel(), _stream_ptr(stream)))
 
 
 def process_logits(logits, out=None, *, repetition=None, frequency=None, presence=None, history=None, history_lens=None,
@@ -710,77 +620,27 @@ def process_logits(logits, out=None, *, repetition=None, frequency=None, presenc
     [R, capacity] int32 with history_lens [R]; prompt_bits / mask_bits [*, >= ceil(V / 32)] int32 bitmaps chosen per row by prompt_rows /
     mask_rows [R] int32; bias_indptr [R+1], bias_ids int32 and bias_values f32; scratch uint8 (psa_process_logits_scratch_bytes, for callers
     that must not allocate).  Returns out."""
-    if _torch is None:
-        _bind_torch()
-    if logits.dim() != 2 or (out is not None and out.shape != logits.shape):
-        raise ValueError("logits must be [rows, vocab], and out of the same shape")
-    R, V = logits.shape
-    in_code = _dtype_code(logits, "logits")
+    rows, vocab = logits.shape
     if out is None:
-        out = _torch.empty((R, (V + 7) // 8 * 8), dtype=logits.dtype, device=logits.device)[:, :V]
-    out_code = _dtype_code(out, "out")
-    in_stride, step = logits.stride()
-    out_stride, out_step = out.stride()
-    if (step != 1 or out_step != 1) and V > 1:
-        raise ValueError("logits and out must be contiguous along the vocabulary")
-    if R <= 1:      # one row has no stride of its own
-        in_stride = out_stride = (V + 7) // 8 * 8
-    dev = logits.get_device()
-    h_ptr, h_lens, h_stride, h_cap = None, None, 0, 0
-    if history is not None and history_lens is not None:
-        if history.dtype is not _i32_t or history.dim() != 2 or history.shape[0] < R or (history.stride(1) != 1 and history.shape[1] > 1):
-            raise ValueError("history must be int32 [rows, capacity], contiguous along the second dimension")
-        h_cap = history.shape[1]
-        h_stride = history.stride(0) if history.shape[0] > 1 else h_cap
-        if history.get_device() != dev:
-            raise ValueError("history must be on the current CUDA device")
-        h_ptr, h_lens = history.data_ptr(), _flat(history_lens, _i32_t, "history_lens", dev, R)
-    elif history is not history_lens:
-        raise ValueError("history and history_lens go together")
-    b_indptr, b_ids, b_values, b_count = None, None, None, 0
-    if bias_indptr is not None and bias_ids is not None and bias_values is not None:
-        b_count = bias_ids.numel()
-        b_indptr = _flat(bias_indptr, _i32_t, "bias_indptr", dev, R + 1)
-        b_ids = _flat(bias_ids, _i32_t, "bias_ids", dev)
-        b_values = _flat(bias_values, _f32_t, "bias_values", dev, b_count)
-    elif not (bias_indptr is bias_ids is bias_values):
-        raise ValueError("bias_indptr, bias_ids and bias_values go together")
-    words = (V + 31) // 32
-    prompt = _bitmap_args(prompt_bits, prompt_rows, words, R, "prompt", dev)
-    mask = _bitmap_args(mask_bits, mask_rows, words, R, "mask", dev)
-    f32 = _f32_t
-    rules = _LogitsRules(_flat(repetition, f32, "repetition", dev, R), _flat(frequency, f32, "frequency", dev, R),
-                         _flat(presence, f32, "presence", dev, R), h_ptr, h_lens, h_stride, h_cap, *prompt, b_indptr, b_ids, b_values, b_count, *mask)
-    if out.get_device() != _device_of(logits, "logits"):
-        raise ValueError("out must be on the current CUDA device")
-    lib, need = library(), 0
-    if h_cap > 0 or b_count > 0:
-        need = lib.psa_process_logits_scratch_bytes(R, V)
-        if need and scratch is None:
-            scratch = _torch.empty(need, dtype=_u8_t, device=logits.device)
-    _check(lib.psa_process_logits(logits.data_ptr(), in_code, in_stride, R, V, ctypes.byref(rules), out.data_ptr(), out_code, out_stride,
-                                  _flat(scratch, _u8_t, "scratch", dev, need) if need else None, need, _stream_on(stream, dev)))
+        import torch
+        out = torch.empty((rows, (vocab + 7) // 8 * 8), dtype=logits.dtype, device=logits.device)[:, :vocab]
+    if scratch is None and vocab > 4096 and (history is not None or bias_ids is not None):
+        need = library().psa_process_logits_scratch_bytes(rows, vocab)
+        if need:
+            scratch = _scratch(need, logits, stream)
+    rc = (_calls or _native()).process_logits(logits, out, repetition, frequency, presence, history, history_lens, prompt_bits, prompt_rows, bias_indptr,
+                                              bias_ids, bias_values, mask_bits, mask_rows, scratch, stream)
+    if rc:
+        _check(rc)
     return out
 
 
 def mark_tokens(ids, indptr, vocab, bits=None, *, stream=None):
     """psa_mark_tokens: bitmaps [rows, >= ceil(vocab / 32)] int32 of the tokens in ids[indptr[m] .. indptr[m + 1]).  Returns bits."""
-    if _torch is None:
-        _bind_torch()
-    vocab = int(vocab)
-    rows, words = indptr.numel() - 1, (vocab + 31) // 32
-    if rows < 0:
-        raise ValueError("indptr must hold rows + 1 elements")
     if bits is None:
-        bits = _torch.empty((rows, words), dtype=_i32_t, device=ids.device)
-    count, width = bits.shape if bits.dim() == 2 else (0, -1)
-    if bits.dtype is not _i32_t or count < rows or width < words or (bits.stride(1) != 1 and width > 1):
-        raise ValueError(f"bits must be int32 [rows, words >= {words}], contiguous along the second dimension")
-    dev = ids.get_device()
-    p_ids = _flat(ids, _i32_t, "ids", dev)
-    p_indptr = _flat(indptr, _i32_t, "indptr", dev)
-    if bits.get_device() != _device_of(ids, "ids"):
-        raise ValueError("bits must be on the current CUDA device")
-    _check(library().psa_mark_tokens(p_ids, ids.numel(), p_indptr, rows, vocab, bits.data_ptr(), bits.stride(0) if count > 1 else width,
-                                     _stream_on(stream, dev)))
+        import torch
+        bits = torch.empty((max(0, indptr.numel() - 1), (int(vocab) + 31) // 32), dtype=torch.int32, device=ids.device)
+    rc = (_calls or _native()).mark_tokens(ids, indptr, vocab, bits, stream)
+    if rc:
+        _check(rc)
     return bits

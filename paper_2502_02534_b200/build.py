@@ -1,9 +1,10 @@
-"""Compile the CUDA library in-tree for sm_100a with nvcc (works without a GPU)."""
+"""Compile the CUDA library in-tree for sm_100a with nvcc (works without a GPU), and the native marshalling of torch tensors with g++."""
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 from pathlib import Path
 
@@ -11,6 +12,7 @@ HERE = Path(__file__).resolve().parent
 CSRC = HERE / "csrc"
 INCLUDE = HERE.parent / "include"
 LIB = HERE / "libpsa.so"
+CALLS = HERE / "_torch_calls.so"      # a Python extension module (csrc/torch_calls.cpp)
 SOURCES = ["api.cu", "plan.cpp", "prefix_sm100.cu", "suffix_sm100.cu", "merge_sm100.cu", "static_workspace.cu", "append_sm100.cu", "sample_sm100.cu", "attn_tasks.cu",
            "pages_sm100.cu", "kv4_sm100.cu", "suffix_kv4_sm100.cu", "logits_sm100.cu"]
 NVCC_FLAGS = [
@@ -47,8 +49,27 @@ def build(force: bool = False, verbose: bool = False) -> Path:
                 raise RuntimeError(f"nvcc failed on {src}:\n{logs[src]}")
         return obj
 
-    with ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
+    def compile_calls():
+        src = CSRC / "torch_calls.cpp"
+        if not (force or _stale(CALLS, [src, *INCLUDE.glob("*.h")])):
+            return
+        import torch
+        torch_dir = Path(torch.__file__).resolve().parent
+        tmp = CALLS.with_suffix(f".tmp{os.getpid()}.so")
+        cuda = Path(_nvcc()).resolve().parent.parent / "include"
+        cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f"-I{INCLUDE}",
+               "-isystem", str(torch_dir / "include"), "-isystem", str(torch_dir / "include/torch/csrc/api/include"),
+               "-isystem", sysconfig.get_path("include"), "-isystem", str(cuda), str(src), "-o", str(tmp),
+               f"-L{torch_dir / 'lib'}", "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-ldl"]
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        if r.returncode != 0:
+            raise RuntimeError(f"g++ failed on {src.name}:\n{r.stderr}")
+        os.replace(tmp, CALLS)
+
+    with ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
+        calls = ex.submit(compile_calls)
         objs = list(ex.map(compile_one, SOURCES))
+        calls.result()
     if force or _stale(LIB, objs):
         tmp = LIB.with_suffix(f".tmp{os.getpid()}.so")
         cmd = [_nvcc(), "-shared", "-gencode", "arch=compute_100a,code=sm_100a", "-o", str(tmp), *map(str, objs), "-ldl"]

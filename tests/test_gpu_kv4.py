@@ -363,7 +363,7 @@ def test_captured_graph_and_two_streams():
 def test_one_plan_serves_both_caches_side_by_side_and_its_own_lists_serve_the_4_bit_one():
     import torch
     from paper_2502_02534_b200 import decode, library
-    from paper_2502_02534_b200.binding import _check, _strides2, default_pool_strides
+    from paper_2502_02534_b200.binding import _check, _strides, default_pool_strides
     w = problem(128, 4, 2, [300], [5], [400, 0, 33, 64, 1], seed=14)
     plan, d = make_plan(w, "f32"), on_device(w)
     plan.bind_workspace()
@@ -383,8 +383,8 @@ def test_one_plan_serves_both_caches_side_by_side_and_its_own_lists_serve_the_4_
     decode(plan, d["q"], d["prefix_k"], d["prefix_v"], pk, pv, d["page_indptr"], d["page_indices"], d["suffix_lens"], o, l)
     assert torch.equal(first, o) and default_pool_strides(plan)[2] == 128
     # the plan made for bf16, handed to the 4-bit entry point itself
-    _check(library().psa_decode_kv4(plan.handle, d["q"].data_ptr(), d["prefix_k"].data_ptr(), d["prefix_v"].data_ptr(), _strides2(256, 128),
-                                    d["pool"].data_ptr(), _strides2(*d["pool"].stride()[:2]), d["page_indptr"].data_ptr(), d["page_indices"].data_ptr(),
+    _check(library().psa_decode_kv4(plan.handle, d["q"].data_ptr(), d["prefix_k"].data_ptr(), d["prefix_v"].data_ptr(), _strides((256, 128), 2),
+                                    d["pool"].data_ptr(), _strides(d["pool"].stride()[:2], 2), d["page_indptr"].data_ptr(), d["page_indices"].data_ptr(),
                                     d["suffix_lens"].data_ptr(), o.data_ptr(), l.data_ptr(), plan.workspace.data_ptr(), plan.workspace.numel(),
                                     torch.cuda.current_stream().cuda_stream))
     torch.cuda.synchronize()

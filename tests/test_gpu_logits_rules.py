@@ -159,7 +159,7 @@ def test_lengths_beyond_the_capacity_are_cut_and_lists_stay_inside_their_arrays(
 
 def test_scratch_of_the_callers_is_used_and_too_little_of_it_refused():
     import torch
-    from paper_2502_02534_b200 import library, process_logits
+    from paper_2502_02534_b200 import PsaError, library, process_logits
     c = case(3, 9000, 12)
     _, x = padded(c["x"], "f32")
     kw = arguments(c, 9000, ALL)
@@ -167,8 +167,9 @@ def test_scratch_of_the_callers_is_used_and_too_little_of_it_refused():
     scratch = torch.full((need + 64,), 255, dtype=torch.uint8, device="cuda")
     a, b = process_logits(x, scratch=scratch, **kw), process_logits(x, **kw)
     assert torch.equal(a.isnan(), b.isnan()) and torch.equal(a.nan_to_num(), b.nan_to_num()) and (scratch[need:] == 255).all()
-    with pytest.raises(ValueError, match="scratch"):
+    with pytest.raises(PsaError) as e:
         process_logits(x, scratch=scratch[:need - 1], **kw)
+    assert e.value.status == 3
 
 
 def test_processed_logits_are_what_sampling_draws_from():
