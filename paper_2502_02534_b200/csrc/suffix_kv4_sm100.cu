@@ -16,8 +16,8 @@
 //   * outputs: V codes come through ldmatrix.trans, so that a register holds one unit (4 channels) of two neighbouring tokens.
 //     Rows 0-7 of a product take whole bytes (even code + 16 * odd code, still a subnormal whole number), rows 8-15 the upper
 //     nibbles alone; the even channel is their difference, taken once at the end.  4 instructions per 8 codes.
-//   * the offset term of the scores is one more product, parameters x (group sums of q, split into two bf16 numbers: 2^-16
-//     relative); the offset term of the outputs is one more product, parameters^T x p.
+//   * the offset term of the scores is one and a half more products, parameters x (group sums of q, split into three bf16 numbers:
+//     2^-24 relative); the offset term of the outputs is one more product, parameters^T x p.
 //   * rounding: p * s and p are rounded to bf16 (2^-8 relative at most, zero mean) before they meet the codes and the offsets.  With
 //     codes centred on 8 both terms stay as small as the values themselves; uncentred, their errors would not cancel as the
 //     terms do.  The centring is a product with a constant -8 on the same rounded operand, hence exact.
@@ -90,6 +90,12 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// D(16x8, f32) += A(16x8, bf16, row) * B(8x8, bf16, col)
+__device__ __forceinline__ void mma_bf16_k8(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t b0)
+{
+    asm("mma.sync.aligned.m16n8k8.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%0,%1,%2,%3};\n"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(b0));
 }
 __device__ __forceinline__ uint32_t movmatrix_trans(uint32_t a)
 {
@@ -179,7 +185,7 @@ suffix_kv4_kernel(const __nv_bfloat16 *__restrict__ q, const unsigned char *__re
     // the order in which the masked registers of K present them: (0, 4), (1, 5)/16, (2, 6), (3, 7)/16.
     const int qrow = lane >> 2, c4 = lane & 3;
     uint32_t qb[NG][4];
-    uint32_t qs0 = 0u, qs1 = 0u;   // group sums of q (times the softmax scale), high and low bf16 part, where the offsets stand
+    uint32_t qs0 = 0u, qs1 = 0u, qs2 = 0u;   // group sums of q (times the softmax scale) as three bf16 parts, where the offsets stand
     {
         float gsum[NG];
 #pragma unroll
@@ -202,7 +208,9 @@ suffix_kv4_kernel(const __nv_bfloat16 *__restrict__ q, const unsigned char *__re
         for (int i = 0; i < NG / 2; ++i)
             if (c4 == kFirst + i) {
                 qs0 = pack_bf16(gsum[2 * i], gsum[2 * i + 1]);
-                qs1 = pack_bf16(gsum[2 * i] - lo_f32(qs0), gsum[2 * i + 1] - hi_f32(qs0));
+                const float r0 = gsum[2 * i] - lo_f32(qs0), r1 = gsum[2 * i + 1] - hi_f32(qs0);
+                qs1 = pack_bf16(r0, r1);
+                qs2 = pack_bf16(r0 - lo_f32(qs1), r1 - hi_f32(qs1));
             }
     }
     const float score_scale = scale_log2 * kUnscaleEven;
@@ -263,6 +271,7 @@ suffix_kv4_kernel(const __nv_bfloat16 *__restrict__ q, const unsigned char *__re
                 uint32_t a[4];
                 ldmatrix_x4(cell + pk_at, a);
                 mma_bf16_from(x, a[0], a[1], a[2], a[3], qs0, qs1, base);
+                mma_bf16_k8(x, a[0], a[1], qs2);
             }
             float acc[NG][4];
 #pragma unroll

@@ -214,13 +214,13 @@ def run(w, out_dtype="f32", plan=None, d=None, **kw):
 
 
 def within_bounds(w, out, lse, out_dtype="f32"):
-    """Scores: each group sum of q is split into two bf16 numbers, residual 2^-16 of it, and a score is a chain of fp32 sums (at most
+    """Scores: each group sum of q is split into three bf16 numbers, residual 2^-24 of it, and a score is a chain of fp32 sums (at most
     D / 16 + 8 of them, each within 2^-23 of the absolute terms: matrix instructions may truncate).  Probabilities: bf16, half a step is
     2^-8 of each term; the shared prefix's truncated bf16 probabilities are within 2^-7; 2^-18 covers exp2, fp32 sums and the merge."""
     ref_o, ref_l, mag_o, mag_l = kv4.attend(w)
     empty = np.isneginf(ref_l)
     assert np.array_equal(np.isneginf(lse), empty) and np.isfinite(out).all()
-    score = mag_l * (2.0 ** -16 + (w["head_dim"] / 16 + 8) * 2.0 ** -23)
+    score = mag_l * (2.0 ** -24 + (w["head_dim"] / 16 + 8) * 2.0 ** -23)
     tol_l = score + np.abs(np.where(empty, 0, ref_l)) * 2.0 ** -22 + 2.0 ** -18
     if w["prefix_lens"].sum():
         tol_l = tol_l + 2.0 ** -14      # the prefix kernels' cubic for exp2: 7.5e-5 relative at most
