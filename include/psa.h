@@ -481,10 +481,11 @@ psa_status_t psa_decode_suffix_kv4(const psa_plan_t *plan, const void *q, const 
  *   bias_indptr    [R+1] int32, bias_ids int32, bias_values f32 of num_biases entries: bias_indptr[r] .. bias_indptr[r+1]-1 (cut to
  *                  0 .. num_biases) belong to row r
  *   mask_bits      bitmaps like prompt_bits (set = allowed): num_mask_bitmaps of mask_row_words words; mask_rows as prompt_rows
- * Token ids outside 0 .. vocab-1 are ignored.  A row whose mask allows nothing becomes -inf throughout.  Types, alignment and strides
- * as for psa_sample_tokens, for input and output each; out may be logits (same type and stride).  NaN logits stay NaN unless
- * masked.  scratch: device, 4-byte aligned, psa_process_logits_scratch_bytes(num_rows, vocab) bytes (0 for small vocabularies),
- * needed with history or biases only; overwritten by every call (calls that share it must be ordered on one stream).  Only enqueues
+ * Token ids outside 0 .. vocab-1 are ignored; vocab <= 2^24.  A row whose mask allows nothing becomes -inf throughout.  Types, alignment and strides
+ * as for psa_sample_tokens, for input and output each; out may be logits (same type and stride), otherwise the two do not overlap.
+ * NaN logits stay NaN unless masked.  scratch: device, 4-byte aligned, psa_process_logits_scratch_bytes(num_rows, vocab) bytes (0 for
+ * small vocabularies), needed in place with history or biases only; overwritten by every such call (calls that share it must be
+ * ordered on one stream).  Only enqueues
  * one or two kernels.
  */
 typedef struct {

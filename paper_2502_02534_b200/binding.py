@@ -227,17 +227,19 @@ class Plan:
                                                ctypes.byref(handle)))
         self._h = handle
         self.workspace = None
-        self._kv4 = None
+        self._kv4 = None            # the plan for_kv4 returns, once made
+        self._is_kv4 = False
 
     def for_kv4(self) -> "Plan":
         """The plan of the same problem whose pieces are sized for a 4-bit cache (psa_plan_create_kv4), with a workspace of its own.
         decode_kv4 uses it in place of this one; it is made once and kept."""
+        if self._is_kv4:
+            return self
         if self._kv4 is None:
             handle = c_void_p()
             _check(library().psa_plan_create_kv4(self._h, ctypes.byref(handle)))
             plan = Plan.__new__(Plan)
-            plan.__dict__.update(self.__dict__, _h=handle, workspace=None)
-            plan._kv4 = plan
+            plan.__dict__.update(self.__dict__, _h=handle, workspace=None, _is_kv4=True)
             self._kv4 = plan
         return self._kv4
 
@@ -297,7 +299,7 @@ class Plan:
 
     def check_status(self, stream=None):
         """Raise if a step left a device-side error in the workspace (that of for_kv4 included), and clear it."""
-        if self._kv4 is not None and self._kv4 is not self and self._kv4.workspace is not None:
+        if self._kv4 is not None and self._kv4.workspace is not None:
             self._kv4.check_status(stream)
             if self.workspace is None:
                 return
@@ -502,11 +504,14 @@ def _scratch(nbytes, like, stream):
 
 
 def _status_tensor(status):
-    """A status word: a one-element int32 tensor, or a Plan (the word Plan.check_status reads)."""
+    """A status word: a one-element int32 tensor, or a Plan (a word that Plan.check_status reads)."""
     if isinstance(status, Plan):
-        if status.workspace is None:
+        workspace = status.workspace
+        if workspace is None and status._kv4 is not None:
+            workspace = status._kv4.workspace
+        if workspace is None:
             raise ValueError("status: the plan has no workspace yet")
-        return status.workspace
+        return workspace
     return status
 
 
@@ -581,7 +586,8 @@ def load_kv4(pool, slot_map, out_k, out_v, *, status=None, stream=None):
 def decode_kv4(plan: Plan, q, prefix_k, prefix_v, pool, page_indptr, page_indices, suffix_lens, out, lse, *, prefix_strides=None,
                stream=None, stage="all"):
     """psa_decode_kv4 (or one of its stages): decode with the samples' own tokens in a 4-bit pool [pages, Hkv, kv4_cell_bytes(D)]
-    uint8.  Everything else as for decode; the work lists and the workspace are those of plan.for_kv4()."""
+    uint8.  Everything else as for decode; the work lists and the workspace are those of plan.for_kv4(), made at the first call (which
+    therefore comes before any stream capture)."""
     plan = plan._kv4 or plan.for_kv4()
     if stage != "all":
         return _decode_kv4_stage(plan, q, prefix_k, prefix_v, pool, page_indptr, page_indices, suffix_lens, out, lse, prefix_strides, stream, stage)
@@ -624,7 +630,7 @@ def process_logits(logits, out=None, *, repetition=None, frequency=None, presenc
     if out is None:
         import torch
         out = torch.empty((rows, (vocab + 7) // 8 * 8), dtype=logits.dtype, device=logits.device)[:, :vocab]
-    if scratch is None and vocab > 4096 and (history is not None or bias_ids is not None):
+    if scratch is None and vocab > 4096 and (history is not None or bias_ids is not None) and out.data_ptr() == logits.data_ptr():
         need = library().psa_process_logits_scratch_bytes(rows, vocab)
         if need:
             scratch = _scratch(need, logits, stream)

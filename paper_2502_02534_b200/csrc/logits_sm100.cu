@@ -9,16 +9,17 @@
 //
 // A row touches a few hundred of its many tokens through its lists (generated tokens, biases), all others only through the two
 // bitmaps.  So the work is split:
-//   lists    one block per row counts the generated tokens and adds up the biases in a hash table in shared memory, works out the
-//            logit of every token in it, writes it to the output, and marks the token in a bitmap;
-//   stream   every other logit: a thread takes eight consecutive ones, and one byte each of the marks, the prompt set and the mask
-//            tell what there is to do.  Marked logits are taken from the output as they are, so that the output may be the input.
-// Up to kWholeRow tokens the block that did a row's lists streams the row as well (one launch, marks in shared memory); above it
-// the stream is a launch of its own with many blocks per row, and the marks are in the caller's scratch memory.  Without lists
-// there is only the stream.  Lists of more entries than half the table are done in ranges of as many tokens as it has slots,
-// indexed directly.
-// Bound: HBM, one read and one write of every logit (and 3 bits).  Counting inside the blocks of the stream instead, tile by tile,
-// costs barriers and dependent loads in each of them: 46 us against the figure below for 256 rows x 131072 bf16 logits.
+//   lists    one block per row counts the generated tokens and adds up the biases in a hash table in shared memory, and works out the
+//            logit of every token in it;
+//   stream   every other logit: a thread takes eight consecutive ones, and one byte each of the prompt set and the mask tell what there
+//            is to do.
+// Up to kWholeRow tokens the block that did a row's lists streams the row as well (one launch).  Above it the stream is a launch of
+// its own with many blocks per row, and the lists' launch follows it: it counts while the stream is still running and writes its few
+// logits over the stream's when that is done.  In place that order would lose the inputs, so the lists go first, mark their tokens
+// in a bitmap in the caller's scratch memory, and the stream leaves marked logits as they are.
+// Lists of more entries than half the table are done in ranges of as many tokens as it has slots, indexed directly.
+// Bound: HBM, one read and one write of every logit (and 2 bits).  Counting inside the blocks of the stream instead, tile by tile,
+// costs barriers and dependent loads in each of them: 46 us for 256 rows x 131072 bf16 logits.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -48,7 +49,7 @@ struct RulesArgs {
     void *out;
     int64_t row_stride, out_stride;
     int vocab;
-    uint32_t *marks;      // [rows][words]; null: no lists, or kept in shared memory
+    uint32_t *marks;      // [rows][words], in place only
     int64_t mark_words;
     int log2_slots;       // of the largest table
 };
@@ -263,10 +264,8 @@ rules_stream_kernel(RulesArgs a)
     const int n = min(kStreamRun, ((a.vocab & ~7) - first + kStreamTile - 1) / kStreamTile);   // whole groups of this thread; may be <= 0
     const unsigned char *in = static_cast<const unsigned char *>(row_of(a.logits, a.row_stride, row, kInF32));
     void *out = const_cast<void *>(row_of(a.out, a.out_stride, row, kOutF32));
-    // Behind the lists of the same call the inputs are complete already (that grid has waited for them) and stay as they are unless
-    // they are the output; only the marks and the logits written there have to be waited for.
-    const bool early = a.marks != nullptr && a.logits != a.out;
-    if (!early) asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");                // for whatever wrote the inputs, or (in place) for the lists
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the lists' launch may count beside this one
     auto request = [&](int t) {
         if (t < n) {
             const uint32_t to = uint32_t(__cvta_generic_to_shared(&ring[t % kStreamDepth][threadIdx.x * kBytes]));
@@ -287,7 +286,6 @@ rules_stream_kernel(RulesArgs a)
         allowed = r.mask && t < n ? __ldg(r.mask + at) : 0u;
         marked = marks && t < n ? marks[at] : 0u;
     };
-    if (early) asm volatile("griddepcontrol.wait;" ::: "memory");
     bits(0);
     auto work = [&](auto up) {
         for (int t = 0; t < n; ++t) {
@@ -366,7 +364,10 @@ rules_lists_kernel(RulesArgs a)
     extern __shared__ __align__(16) int32_t table_smem[];
     __shared__ uint32_t own_marks[kWhole ? kWholeRow / 32 : 1];
     const int row = blockIdx.x, tid = threadIdx.x;
-    if (!kWhole) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the stream sets itself up beside this and waits
+    // Not the whole row, not in place: this runs under the stream of the same call, which has waited for the inputs and does not write
+    // them; only this kernel's writes have to wait for it.
+    const bool after = !kWhole && a.marks == nullptr;
+    if (!after) asm volatile("griddepcontrol.wait;" ::: "memory");
     const void *in = row_of(a.logits, a.row_stride, row, kInF32);
     void *out = const_cast<void *>(row_of(a.out, a.out_stride, row, kOutF32));
     const int32_t *said = a.r.history ? a.r.history + int64_t(row) * a.r.history_stride : nullptr;
@@ -387,8 +388,9 @@ rules_lists_kernel(RulesArgs a)
             if (i + kVec <= a.vocab) v[k].load(in, i);
         }
     }
-    uint32_t *marks = kWhole ? own_marks : a.marks + row * a.mark_words;
-    for (int w = tid; w < (a.vocab + 31) / 32; w += kListThreads) marks[w] = 0u;
+    uint32_t *marks = kWhole ? own_marks : after ? nullptr : a.marks + row * a.mark_words;
+    if (marks)
+        for (int w = tid; w < (a.vocab + 31) / 32; w += kListThreads) marks[w] = 0u;
 
     // the smallest table that stays half empty, or all there is, indexed directly
     const uint32_t entries = uint32_t(n_said) + uint32_t(n_bias);
@@ -434,10 +436,13 @@ rules_lists_kernel(RulesArgs a)
                 const int h = h0 + k * kListThreads, c = t.count[h];
                 if (c > 0 || in_prompt[k]) x[k] = r.penalised(x[k]);
                 if (c > 0) x[k] = x[k] - freq * float(c) - pres;
-                store_one<kOutF32>(out, id[k], allowed[k] ? x[k] + t.value[h] : -INFINITY);
-                atomicOr(marks + (id[k] >> 5), 1u << (id[k] & 31));
+                t.value[h] = allowed[k] ? x[k] + t.value[h] : -INFINITY;
+                if (marks) atomicOr(marks + (id[k] >> 5), 1u << (id[k] & 31));
             }
         }
+        if (after) asm volatile("griddepcontrol.wait;" ::: "memory");
+        for (int h = tid; h < t.slots(); h += kListThreads)   // the slots this thread has just worked out
+            if (t.key[h] >= 0) store_one<kOutF32>(out, t.key[h], t.value[h]);
         __syncthreads();
         if (t.hashed) break;
     }
@@ -484,35 +489,45 @@ mark_kernel(const int32_t *__restrict__ ids, int num_ids, const int32_t *__restr
 bool misaligned(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n != 0; }
 bool known_dtype(int32_t d) { return d == PSA_OUT_BF16 || d == PSA_OUT_F32; }
 
-template <bool kInF32, bool kOutF32>
-cudaError_t launch_rules(const RulesArgs &a, int rows, bool lists, cudaStream_t st)
+// A launch that sets itself up under the tail of the one before it and waits there (griddepcontrol.wait) for its results.
+template <class Kernel>
+cudaError_t launch_behind(Kernel kernel, dim3 grid, int threads, size_t smem, cudaStream_t st, const RulesArgs &a)
 {
-    const size_t table = size_t(12) << a.log2_slots;
-    if (lists) {
-        const bool whole = a.vocab <= kWholeRow;
-        static PerDeviceOnce once;
-        const int rc = once.ensure([] {
-            cudaError_t e = cudaFuncSetAttribute(rules_lists_kernel<kInF32, kOutF32, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, 12 * kSlotsMany);
-            if (e == cudaSuccess)
-                e = cudaFuncSetAttribute(rules_lists_kernel<kInF32, kOutF32, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, 12 * kSlotsMany);
-            return int(e);
-        });
-        if (rc != 0) return cudaError_t(rc);
-        if (whole) rules_lists_kernel<kInF32, kOutF32, true><<<rows, kListThreads, table, st>>>(a);
-        else rules_lists_kernel<kInF32, kOutF32, false><<<rows, kListThreads, table, st>>>(a);
-        const cudaError_t e = cudaGetLastError();
-        if (whole || e != cudaSuccess) return e;
-    }
     cudaLaunchConfig_t lc{};
-    lc.gridDim = dim3((a.vocab + kStreamRun * kStreamTile - 1) / (kStreamRun * kStreamTile), rows);
-    lc.blockDim = dim3(kStreamThreads);
+    lc.gridDim = grid;
+    lc.blockDim = dim3(threads);
+    lc.dynamicSmemBytes = smem;
     lc.stream = st;
     cudaLaunchAttribute attr{};
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr.val.programmaticStreamSerializationAllowed = 1;
     lc.attrs = &attr;
     lc.numAttrs = 1;
-    return cudaLaunchKernelEx(&lc, rules_stream_kernel<kInF32, kOutF32>, a);
+    return cudaLaunchKernelEx(&lc, kernel, a);
+}
+
+template <bool kInF32, bool kOutF32>
+cudaError_t launch_rules(const RulesArgs &a, int rows, bool lists, cudaStream_t st)
+{
+    const auto whole = rules_lists_kernel<kInF32, kOutF32, true>, part = rules_lists_kernel<kInF32, kOutF32, false>;
+    const auto stream = rules_stream_kernel<kInF32, kOutF32>;
+    if (lists) {
+        static PerDeviceOnce once;
+        const int rc = once.ensure([&] {
+            cudaError_t e = cudaFuncSetAttribute(whole, cudaFuncAttributeMaxDynamicSharedMemorySize, 12 * kSlotsMany);
+            if (e == cudaSuccess) e = cudaFuncSetAttribute(part, cudaFuncAttributeMaxDynamicSharedMemorySize, 12 * kSlotsMany);
+            return int(e);
+        });
+        if (rc != 0) return cudaError_t(rc);
+    }
+    const size_t table = size_t(12) << a.log2_slots;
+    const dim3 tiles((a.vocab + kStreamRun * kStreamTile - 1) / (kStreamRun * kStreamTile), rows);
+    if (lists && a.vocab <= kWholeRow) return launch_behind(whole, dim3(rows), kListThreads, table, st, a);
+    cudaError_t e = cudaSuccess;
+    if (lists && a.marks) e = launch_behind(part, dim3(rows), kListThreads, table, st, a);
+    if (e == cudaSuccess) e = launch_behind(stream, tiles, kStreamThreads, 0, st, a);
+    if (e == cudaSuccess && lists && !a.marks) e = launch_behind(part, dim3(rows), kListThreads, table, st, a);
+    return e;
 }
 
 }  // namespace
@@ -533,7 +548,7 @@ extern "C" psa_status_t psa_process_logits(const void *logits, int32_t logits_dt
     if (num_rows == 0) return PSA_OK;
     if (vocab == 0) return set_last_error(PSA_ERR_INVALID_ARG, "vocab must be positive");
     if (num_rows > 65535) return set_last_error(PSA_ERR_UNSUPPORTED, "at most 65535 rows per call");
-    if (vocab > (1 << 30)) return set_last_error(PSA_ERR_UNSUPPORTED, "vocab must be at most 2^30");
+    if (vocab > (1 << 24)) return set_last_error(PSA_ERR_UNSUPPORTED, "vocab must be at most 2^24");
     if (!psa::known_dtype(logits_dtype) || !psa::known_dtype(out_dtype))
         return set_last_error(PSA_ERR_UNSUPPORTED, "dtypes must be PSA_OUT_BF16 or PSA_OUT_F32");
     if (!logits || !out || !rules) return set_last_error(PSA_ERR_INVALID_ARG, "null argument");
@@ -551,7 +566,7 @@ extern "C" psa_status_t psa_process_logits(const void *logits, int32_t logits_dt
         return set_last_error(PSA_ERR_INVALID_ARG, "bitmap rows must hold at least ceil(vocab / 32) words");
     const bool lists = (r.history && r.history_capacity > 0) || (r.bias_indptr && r.num_biases > 0);
     psa::RulesArgs a{r, logits, out, row_stride, out_row_stride, vocab, nullptr, words, 0};
-    if (lists && vocab > psa::kWholeRow) {
+    if (lists && vocab > psa::kWholeRow && logits == out) {
         if (!scratch || reinterpret_cast<uintptr_t>(scratch) % 4 || scratch_bytes < psa_process_logits_scratch_bytes(num_rows, vocab))
             return set_last_error(PSA_ERR_WORKSPACE, "scratch must be 4-byte aligned and hold psa_process_logits_scratch_bytes(num_rows, vocab)");
         a.marks = static_cast<uint32_t *>(scratch);
@@ -578,7 +593,7 @@ extern "C" psa_status_t psa_mark_tokens(const int32_t *ids, int32_t num_ids, con
     if (num_rows == 0) return PSA_OK;
     if (vocab == 0) return set_last_error(PSA_ERR_INVALID_ARG, "vocab must be positive");
     if (num_rows > 65535) return set_last_error(PSA_ERR_UNSUPPORTED, "at most 65535 rows per call");
-    if (vocab > (1 << 30)) return set_last_error(PSA_ERR_UNSUPPORTED, "vocab must be at most 2^30");
+    if (vocab > (1 << 24)) return set_last_error(PSA_ERR_UNSUPPORTED, "vocab must be at most 2^24");
     if ((!ids && num_ids > 0) || !indptr || !bits) return set_last_error(PSA_ERR_INVALID_ARG, "null argument");
     if (row_words < (int64_t(vocab) + 31) / 32) return set_last_error(PSA_ERR_INVALID_ARG, "bitmap rows must hold at least ceil(vocab / 32) words");
     psa::mark_kernel<<<dim3((vocab + psa::kMarkTile - 1) / psa::kMarkTile, num_rows), psa::kMarkThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(

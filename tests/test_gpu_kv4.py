@@ -392,6 +392,35 @@ def test_one_plan_serves_both_caches_side_by_side_and_its_own_lists_serve_the_4_
     within_bounds(w, o.double().cpu().numpy(), l.double().cpu().numpy())
 
 
+def test_a_cascade_of_shared_prefixes():
+    """Two levels of shared tokens above the 4-bit suffixes, against the oracle on the same keys copied out per sample."""
+    cfg = wl.PsaConfig("kv4cascade", 2, 3, 8, 2, 128, (1, 1), (0, 1), seed=21)
+    lens = [30, 0, 17, 64, 5, 100]
+    base = problem(128, 4, 2, [100, 40], [3, 3], lens, seed=21)
+    c = wl.make_cascade_workload(cfg, 150, lengths=([100, 40], [3, 3], lens))
+    c.update({k: base[k] for k in ("q", "page_indptr", "page_indices", "kv4_pool", "suffix_lens")})
+    flat = wl.flatten_cascade(c)
+    out, lse = run(c)
+    within_bounds(flat, out, lse)
+
+
+def test_explicit_streams_of_both_kinds_and_temporary_scratch():
+    import torch
+    from paper_2502_02534_b200 import extend_page_table, process_logits
+    side = torch.cuda.Stream()
+    held, new = i32([3, 17]), i32([2, 20])
+    for stream in (side, side.cuda_stream, 0):
+        indices, slots = i32([4, -1, 5, 6, -1]), i64(np.zeros(22))
+        torch.cuda.synchronize()
+        extend_page_table(held, new, i32([7, 8, 9]), i32([3]), i32([0, 2, 5]), indices, i32([0, 0, 0]), slots, stream=stream)
+        x = torch.ones((2, 9000), device="cuda")
+        torch.cuda.synchronize()
+        process_logits(x, x, presence=torch.ones(2, device="cuda"), history=i32([[5], [6]]), history_lens=i32([1, 1]), stream=stream)
+        torch.cuda.synchronize()
+        assert indices.tolist() == [4, -1, 5, 6, 9] and slots.tolist() == [67, 68] + list(range(97, 112)) + list(range(144, 149))
+        assert x.sum().item() == 18000 - 2 and x[0, 5] == 0 and x[1, 6] == 0
+
+
 @pytest.mark.parametrize("seed", range(12))
 def test_seeded_draws(seed):
     rng = np.random.default_rng(1000 + seed)

@@ -112,10 +112,11 @@ def test_each_rule_alone(use):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-def test_in_place_equals_out_of_place(dtype):
-    c = case(9, 9001, 5)
-    a = run(c, 9001, dtype, dtype, ALL)
-    b = run(c, 9001, dtype, dtype, ALL, in_place=True)
+@pytest.mark.parametrize("V", [9001, 8192, 8193, 700, 40000])
+def test_in_place_equals_out_of_place(dtype, V):
+    c = case(9, V, 5)
+    a = run(c, V, dtype, dtype, ALL)
+    b = run(c, V, dtype, dtype, ALL, in_place=True)
     assert np.array_equal(a, b, equal_nan=True)
 
 
@@ -165,11 +166,12 @@ def test_scratch_of_the_callers_is_used_and_too_little_of_it_refused():
     kw = arguments(c, 9000, ALL)
     need = library().psa_process_logits_scratch_bytes(3, 9000)
     scratch = torch.full((need + 64,), 255, dtype=torch.uint8, device="cuda")
-    a, b = process_logits(x, scratch=scratch, **kw), process_logits(x, **kw)
-    assert torch.equal(a.isnan(), b.isnan()) and torch.equal(a.nan_to_num(), b.nan_to_num()) and (scratch[need:] == 255).all()
+    b = process_logits(x, **kw)
     with pytest.raises(PsaError) as e:
-        process_logits(x, scratch=scratch[:need - 1], **kw)
+        process_logits(x, x, scratch=scratch[:need - 1], **kw)
     assert e.value.status == 3
+    a = process_logits(x, x, scratch=scratch, **kw)
+    assert a is x and torch.equal(a.isnan(), b.isnan()) and torch.equal(a.nan_to_num(), b.nan_to_num()) and (scratch[need:] == 255).all()
 
 
 def test_processed_logits_are_what_sampling_draws_from():
