@@ -10,12 +10,17 @@
 //   scan phase     one thread per sample, 1024 samples per block.  A block gets its starting sums by reducing the samples
 //                  before its own itself: no block waits for another one, and at the sizes of a decode batch (one to a
 //                  few blocks) that costs a few loads.
-//   spread phase   a warp takes kSpread consecutive tokens (or list entries) and finds the samples of the first and the last
-//                  by a 32-way search over the scanned offsets (two rounds for 1024 samples).  A few long samples are walked
-//                  one after the other with everything about them in registers; many short ones are looked up lane by lane.
+//   spread phase   a warp takes a run of pieces of up to kSpread tokens and finds the samples of a piece's first and last token
+//                  by a 32-way search over the scanned offsets (two rounds for 1024 samples), the first one only where the
+//                  sample of the piece before has ended.  A few long samples are walked one after the other with everything
+//                  about them in registers, their pages one a lane; many short ones are looked up lane by lane.
 //
 // Bound: 8 bytes written per token of capacity once there are many, the latency of a few dependent loads when there are few.  The
 // two phases are one launch of one block, with the offsets in shared memory, up to kOneBlockWork lookups; two launches above it.
+// Measured: 256 samples x 1 token 5.5 us, an empty launch being about 2; 2048 samples x U[0, 4096] tokens, capacity 8.4 million, 19.5 us
+// for 70 MB (3.6 TB/s; a plain fill of as many bytes takes 10.5, the scan before it 5).  Pieces dealt out in turn instead of in runs
+// cost a search each: 22.4 us.  Every block scanning up to 2048 samples for itself, without the launch before it: 27 us, and 13.9
+// instead of 10.9 us for 2048 samples x 1 token.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -29,10 +34,10 @@ namespace {
 
 constexpr int kScanThreads = 1024;
 constexpr int kSpread = 256;                 // most tokens or list entries a warp handles at a time
-constexpr int kPageRegs = (kSpread / 16 + 1 + 31) / 32;   // registers a lane needs for a 32nd of their pages
+static_assert(kSpread / kPageSize < 32, "a warp holds the pages of a piece, one a lane");
 constexpr int64_t kMostEntries = 0x7fffff00; // 32-bit positions, with room for one more stride of a loop
 constexpr int kWalk = 8;                     // samples in such a piece that are walked one after the other
-constexpr int64_t kOneBlockWork = 4096;      // one block: 1024 samples x 4 tokens 8.6 us, 2048 x 4 15.1 us; two launches ~8 and ~9 us
+constexpr int64_t kOneBlockWork = 4096;      // one block: 1024 samples x 4 tokens 8.7 us, 2048 x 4 15.1; two launches 9.7 and 11.3
 constexpr int kOneBlockSamples = 1024;
 
 struct PageTableArgs {
@@ -211,49 +216,57 @@ __device__ __forceinline__ int page_of(const PageTableArgs &a, int j, int fresh,
     return j >= fresh ? a.free_pages[avail - 1 - (rec.y + j - fresh)] : a.page_indices[(long long)e_first + j];
 }
 
+// The sample that a warp's last token belonged to.  A warp takes its pieces in order, so a long sample is looked up once.
+struct Here {
+    int s = 0;
+    int t_first = 0, t_next = -1;   // its tokens; an empty range before any other at first
+    int e_first = 0;
+    int2 rec{};
+    __device__ __forceinline__ void load(const Tables &tab, int sample)
+    {
+        s = sample;
+        t_first = tab.token_indptr[s];
+        t_next = tab.token_indptr[s + 1];
+        e_first = tab.page_indptr[s];
+        rec = tab.rec[s];
+    }
+};
+
 // Tokens [t0, t0 + piece) of the slot map, piece <= kSpread.
-__device__ void spread_tokens(const PageTableArgs &a, const Tables &tab, long long t0, int piece, int avail, int lane)
+__device__ void spread_tokens(const PageTableArgs &a, const Tables &tab, long long t0, int piece, int avail, int lane, Here &at)
 {
     const int n = a.num_samples;
     const int total = n > 0 ? tab.token_indptr[n] : 0;
     const int end = int(min(t0 + piece, (long long)a.max_tokens)), live = min(end, total);
     int t = int(t0);
     if (t < live) {
-        const int s_lo = warp_find(tab.token_indptr, 0, n, t, lane);
-        const int s_hi = tab.token_indptr[s_lo + 1] >= live ? s_lo : warp_find(tab.token_indptr, s_lo, n, live - 1, lane);
+        if (t >= at.t_next) at.load(tab, warp_find(tab.token_indptr, at.s, n, t, lane));
+        const int s_lo = at.s, s_hi = at.t_next >= live ? s_lo : warp_find(tab.token_indptr, s_lo, n, live - 1, lane);
         if (s_hi - s_lo < kWalk) {
             for (int s = s_lo; s <= s_hi; ++s) {
-                const int2 rec = tab.rec[s];
-                const int t_first = tab.token_indptr[s], stop = min(live, tab.token_indptr[s + 1]), e_first = tab.page_indptr[s];
+                if (s != s_lo) at.load(tab, s);
+                const int2 rec = at.rec;
+                const int t_first = at.t_first, stop = min(live, at.t_next), e_first = at.e_first;
                 if (rec.y < 0) {
                     for (int i = t + lane; i < stop; i += 32) a.slot_map[i] = -1;
                 } else if (t < stop) {
-                    // the pages of up to kSpread tokens are fetched at once, a few a lane, and go round by shuffles: two pages
-                    // of 16 slots per store of the warp
-                    const int pos0 = rec.x + (t - t_first), pos1 = pos0 + (stop - t);
-                    const int j0 = pos0 / kPageSize, j1 = (pos1 - 1) / kPageSize, fresh = (rec.x + kPageSize - 1) / kPageSize;
-                    int page[kPageRegs];
+                    // the pages of up to kSpread tokens are fetched at once, one a lane, and go round by shuffles.  32 tokens further
+                    // on are two pages further on, at the same place in the page.
+                    const int len = stop - t, pos0 = rec.x + (t - t_first), j0 = pos0 / kPageSize, j1 = (pos0 + len - 1) / kPageSize;
+                    const int fresh = (rec.x + kPageSize - 1) / kPageSize, j = j0 + lane;
+                    const int page = j <= j1 ? page_of(a, j, fresh, rec, e_first, avail) : 0;
+                    if (!a.build && j <= j1 && j >= fresh && j * kPageSize >= pos0)   // the piece that holds a fresh page's first token files it
+                        a.page_indices[(long long)e_first + j] = page;
+                    const int from = (pos0 % kPageSize + lane) / kPageSize, in_page = (pos0 + lane) % kPageSize;
+                    int64_t *to = a.slot_map + t + lane;
+                    if (len == kSpread && !__any_sync(0xffffffffu, page < 0)) {   // the middle of a long sample
 #pragma unroll
-                    for (int k = 0; k < kPageRegs; ++k) {
-                        const int j = j0 + k * 32 + lane;
-                        page[k] = j <= j1 ? page_of(a, j, fresh, rec, e_first, avail) : -1;
-                    }
-                    if (!a.build)   // the piece that holds a fresh page's first token files the page
-#pragma unroll
-                        for (int k = 0; k < kPageRegs; ++k) {
-                            const int j = j0 + k * 32 + lane;
-                            if (j <= j1 && j >= fresh && j * kPageSize >= pos0) a.page_indices[(long long)e_first + j] = page[k];
-                        }
-                    int64_t *to = a.slot_map + t - pos0;
-#pragma unroll
-                    for (int k = 0; k < kPageRegs; ++k) {
-                        const int last = min(j1 - j0 - k * 32, 31);   // of this register's pages; the same in all lanes
-#pragma unroll 4
-                        for (int w = 0; w <= last; w += 2) {
-                            const int mine = w + (lane >> 4);
-                            const int p = __shfl_sync(0xffffffffu, page[k], mine);
-                            const int pos = (j0 + k * 32 + mine) * kPageSize + (lane & 15);
-                            if (pos >= pos0 && pos < pos1) to[pos] = p >= 0 ? (long long)p * kPageSize + (lane & 15) : -1;
+                        for (int k = 0; k < kSpread / 32; ++k)
+                            to[k * 32] = (long long)__shfl_sync(0xffffffffu, page, from + 2 * k) * kPageSize + in_page;
+                    } else {
+                        for (int k = 0; k * 32 < len; ++k) {
+                            const int p = __shfl_sync(0xffffffffu, page, from + 2 * k);
+                            if (k * 32 + lane < len) to[k * 32] = p >= 0 ? (long long)p * kPageSize + in_page : -1;
                         }
                     }
                 }
@@ -286,8 +299,13 @@ __device__ void spread_tokens(const PageTableArgs &a, const Tables &tab, long lo
             t = live;
         }
     }
-#pragma unroll 8
-    for (int i = t + lane; i < end; i += 32) a.slot_map[i] = -1;
+    int64_t *to = a.slot_map + t + lane;
+    if (end - t == kSpread) {
+#pragma unroll
+        for (int k = 0; k < kSpread / 32; ++k) to[k * 32] = -1;
+    } else {
+        for (int i = t + lane; i < end; i += 32, to += 32) *to = -1;
+    }
 }
 
 // Entries [e0, e0 + piece) of a list array built from scratch: the pages of the tokens held, -1 in the rest.
@@ -323,12 +341,12 @@ __device__ void spread_entries(const PageTableArgs &a, const Tables &tab, long l
 // Everything behind the scans, shared out over `warps` warps in pieces of `piece`.
 __device__ void spread(const PageTableArgs &a, const Tables &tab, int piece, int avail, long long warp, long long warps, int lane)
 {
-    const long long token_pieces = (a.max_tokens + piece - 1) / piece;
+    const long long token_pieces = (a.max_tokens + piece - 1) / piece, per_warp = (token_pieces + warps - 1) / warps;
+    Here at;
+    for (long long c = warp * per_warp, stop = min(c + per_warp, token_pieces); c < stop; ++c) spread_tokens(a, tab, c * piece, piece, avail, lane, at);
+    // the last warps, whose tokens are the least likely to exist, begin with the list entries
     const long long entry_pieces = a.build ? (a.num_entries + piece - 1) / piece : 0;
-    for (long long c = warp; c < token_pieces + entry_pieces; c += warps) {
-        if (c < token_pieces) spread_tokens(a, tab, c * piece, piece, avail, lane);
-        else spread_entries(a, tab, (c - token_pieces) * piece, piece, avail, lane);
-    }
+    for (long long c = warps - 1 - warp; c < entry_pieces; c += warps) spread_entries(a, tab, c * piece, piece, avail, lane);
     if (a.lens_out)
         for (long long s = warp * 32 + lane; s < a.num_samples; s += warps * 32) {
             const int2 rec = tab.rec[s];
@@ -392,7 +410,7 @@ page_table_scan_kernel(PageTableArgs a)
 }
 
 template <int kPiece>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, 6)
 page_table_spread_kernel(PageTableArgs a)
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -433,12 +451,12 @@ psa_status_t run(PageTableArgs a, void *scratch, size_t scratch_bytes, void *cud
         page_table_scan_kernel<<<a.scan_blocks, kScanThreads, 0, st>>>(a);
         e = cudaGetLastError();
         if (e == cudaSuccess) {
-            // pieces small enough to keep the machine's warps busy: 8.9 million lookups take 22 us in pieces of 256 and 30 in 128,
-            // 270 thousand 9.4 and 7.6, 8 thousand 15 and 12.4 (11.6 in 32)
+            // pieces small enough to keep the machine's warps busy: 8.9 million lookups take 19.5 us in pieces of 256 and 26 in 128,
+            // 270 thousand 9.4 and 7.7, 8 thousand 15 and 12.4 (11.3 in 32)
             auto go = [&](auto piece) {
                 const int64_t warps = (work + piece.value - 1) / piece.value;
                 cudaLaunchConfig_t lc{};
-                lc.gridDim = dim3(unsigned(std::max<int64_t>(1, std::min<int64_t>((warps + 7) / 8, 148 * 8))));
+                lc.gridDim = dim3(unsigned(std::max<int64_t>(1, std::min<int64_t>((warps + 7) / 8, 148 * 6))));
                 lc.blockDim = dim3(256);
                 lc.stream = st;
                 cudaLaunchAttribute attr{};
