@@ -39,6 +39,7 @@ constexpr int kStreamTile = kStreamThreads * kVec;         // logits a block of 
 constexpr int kStreamRun = 4, kStreamDepth = 4;            // tiles of a block; of them in flight
 constexpr int kWholeRow = 8192;                            // vocabularies up to this are streamed by the row's own block
 constexpr int kSlotsFew = 2048, kSlotsMany = 8192;         // hash table sizes
+constexpr int kOwn = kSlotsMany / 2 / kListThreads;         // list entries a thread keeps in registers
 constexpr int kMarkTile = 65536;                           // tokens of one block's bitmap
 constexpr int kMarkThreads = 1024;
 constexpr int kMarkBatch = 8;
@@ -311,8 +312,10 @@ struct Table {
     int log2_slots, r0, r1;   // tokens [r0, r1) belong to the table
     bool hashed;
     __device__ __forceinline__ int slots() const { return 1 << log2_slots; }
-    __device__ __forceinline__ int add(int id) const
+    // slot of a token (-1: none of the table's); `mine`: the caller has brought it in
+    __device__ __forceinline__ int add(int id, bool &mine) const
     {
+        mine = false;
         if (id < r0 || id >= r1) return -1;
         if (!hashed) {
             key[id - r0] = id;
@@ -320,7 +323,16 @@ struct Table {
         }
         for (int h = int((uint32_t(id) * 2654435761u) >> (32 - log2_slots));; h = (h + 1) & (slots() - 1)) {
             const int old = atomicCAS(key + h, -1, id);
-            if (old == -1 || old == id) return h;
+            mine = old == -1;
+            if (mine || old == id) return h;
+        }
+    }
+    __device__ __forceinline__ void clear(int tid, int threads) const   // slots() is a multiple of 4
+    {
+        for (int h = tid; h < slots() / 4; h += threads) {
+            reinterpret_cast<int4 *>(key)[h] = make_int4(-1, -1, -1, -1);
+            reinterpret_cast<int4 *>(count)[h] = make_int4(0, 0, 0, 0);
+            reinterpret_cast<float4 *>(value)[h] = make_float4(0.f, 0.f, 0.f, 0.f);
         }
     }
     __device__ __forceinline__ int find(int id) const   // of a token that has been added
@@ -358,7 +370,7 @@ __device__ void add_biases(const int32_t *ids, const float *values, int n, const
 }
 
 template <bool kInF32, bool kOutF32, bool kWhole>
-__global__ void __launch_bounds__(kListThreads)
+__global__ void __launch_bounds__(kListThreads, 2)
 rules_lists_kernel(RulesArgs a)
 {
     extern __shared__ __align__(16) int32_t table_smem[];
@@ -399,52 +411,79 @@ rules_lists_kernel(RulesArgs a)
     t.hashed = entries < (1u << 30) && t.log2_slots <= a.log2_slots;
     if (!t.hashed) t.log2_slots = a.log2_slots;
     t.key = table_smem; t.count = t.key + t.slots(); t.value = reinterpret_cast<float *>(t.count + t.slots());
-    for (int64_t r0 = 0; r0 < a.vocab; r0 += t.slots()) {
-        t.r0 = t.hashed ? 0 : int(r0);
-        t.r1 = t.hashed ? a.vocab : int(min((int64_t)a.vocab, r0 + t.slots()));
-        for (int h = tid; h < t.slots(); h += kListThreads) {
-            t.key[h] = -1;
-            t.count[h] = 0;
-            t.value[h] = 0.f;
+    // logit x of a token that stands in the lists c times, apart from its biases
+    auto ruled = [&](float x, int c, bool in_prompt) {
+        if (c > 0 || in_prompt) x = r.penalised(x);
+        return c > 0 ? x - freq * float(c) - pres : x;
+    };
+    if (t.hashed) {
+        // At most kOwn entries a thread.  The thread that brings a token into the table reads its logit and bits at once and keeps
+        // them in registers, with the other entries' reads and with the biases still under way.
+        t.r0 = 0; t.r1 = a.vocab;
+        int id[kOwn], at[kOwn];
+#pragma unroll
+        for (int k = 0; k < kOwn; ++k) {
+            const int e = tid + k * kListThreads;
+            id[k] = -1;
+            if (k * kListThreads < int(entries) && e < int(entries)) id[k] = e < n_said ? said[e] : a.r.bias_ids[b0 + e - n_said];
         }
+        t.clear(tid, kListThreads);
         __syncthreads();
-        for (int e = tid; e < n_said; e += kListThreads) {
-            const int at = t.add(said[e]);
-            if (at >= 0) atomicAdd(t.count + at, 1);
+        float x[kOwn];
+        uint32_t in_prompt = 0u, allowed = ~0u;   // a bit per k
+#pragma unroll
+        for (int k = 0; k < kOwn; ++k) {
+            at[k] = -1;
+            if (k * kListThreads >= int(entries)) continue;
+            bool mine;
+            const int h = t.add(id[k], mine);
+            if (h >= 0 && tid + k * kListThreads < n_said) atomicAdd(t.count + h, 1);
+            if (mine) {
+                at[k] = h;
+                x[k] = load_one<kInF32>(in, id[k]);
+                if (r.prompt && Row::has(r.prompt, id[k])) in_prompt |= 1u << k;
+                if (r.mask && !Row::has(r.mask, id[k])) allowed &= ~(1u << k);
+                if (marks) atomicOr(marks + (id[k] >> 5), 1u << (id[k] & 31));
+            }
         }
-        for (int e = tid; e < n_bias; e += kListThreads) t.add(a.r.bias_ids[b0 + e]);
         __syncthreads();
         if (n_bias > 0) {   // the same for the whole block
             if (tid < 32) add_biases(a.r.bias_ids + b0, a.r.bias_values + b0, n_bias, t, tid);
             __syncthreads();
         }
-        for (int h0 = tid; h0 < t.slots(); h0 += 4 * kListThreads) {   // the scattered reads of four tokens at once
-            int id[4];
-            float x[4];
-            bool in_prompt[4], allowed[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int h = h0 + k * kListThreads;
-                id[k] = h < t.slots() ? t.key[h] : -1;
-                x[k] = id[k] >= 0 ? load_one<kInF32>(in, id[k]) : 0.f;
-                in_prompt[k] = id[k] >= 0 && r.prompt && Row::has(r.prompt, id[k]);
-                allowed[k] = id[k] < 0 || !r.mask || Row::has(r.mask, id[k]);
-            }
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if (id[k] < 0) continue;
-                const int h = h0 + k * kListThreads, c = t.count[h];
-                if (c > 0 || in_prompt[k]) x[k] = r.penalised(x[k]);
-                if (c > 0) x[k] = x[k] - freq * float(c) - pres;
-                t.value[h] = allowed[k] ? x[k] + t.value[h] : -INFINITY;
-                if (marks) atomicOr(marks + (id[k] >> 5), 1u << (id[k] & 31));
-            }
-        }
         if (after) asm volatile("griddepcontrol.wait;" ::: "memory");
-        for (int h = tid; h < t.slots(); h += kListThreads)   // the slots this thread has just worked out
-            if (t.key[h] >= 0) store_one<kOutF32>(out, t.key[h], t.value[h]);
-        __syncthreads();
-        if (t.hashed) break;
+#pragma unroll
+        for (int k = 0; k < kOwn; ++k)
+            if (at[k] >= 0)
+                store_one<kOutF32>(out, id[k], allowed & (1u << k) ? ruled(x[k], t.count[at[k]], in_prompt & (1u << k)) + t.value[at[k]] : -INFINITY);
+        if (kWhole) __syncthreads();   // the marks
+    } else {
+        for (int64_t r0 = 0; r0 < a.vocab; r0 += t.slots()) {
+            t.r0 = int(r0);
+            t.r1 = int(min((int64_t)a.vocab, r0 + t.slots()));
+            t.clear(tid, kListThreads);
+            __syncthreads();
+            bool mine;
+            for (int e = tid; e < n_said; e += kListThreads) {
+                const int h = t.add(said[e], mine);
+                if (h >= 0) atomicAdd(t.count + h, 1);
+            }
+            for (int e = tid; e < n_bias; e += kListThreads) t.add(a.r.bias_ids[b0 + e], mine);
+            __syncthreads();
+            if (n_bias > 0) {
+                if (tid < 32) add_biases(a.r.bias_ids + b0, a.r.bias_values + b0, n_bias, t, tid);
+                __syncthreads();
+            }
+            if (after) asm volatile("griddepcontrol.wait;" ::: "memory");
+            for (int h = tid; h < t.slots(); h += kListThreads) {
+                const int token = t.key[h];
+                if (token < 0) continue;
+                const float x = ruled(load_one<kInF32>(in, token), t.count[h], r.prompt && Row::has(r.prompt, token));
+                store_one<kOutF32>(out, token, !r.mask || Row::has(r.mask, token) ? x + t.value[h] : -INFINITY);
+                if (marks) atomicOr(marks + (token >> 5), 1u << (token & 31));
+            }
+            __syncthreads();
+        }
     }
     if constexpr (kWhole) {
         const unsigned char *bytes = reinterpret_cast<const unsigned char *>(own_marks);
