@@ -483,10 +483,7 @@ psa_status_t psa_decode_suffix_kv4(const psa_plan_t *plan, const void *q, const 
  *   mask_bits      bitmaps like prompt_bits (set = allowed): num_mask_bitmaps of mask_row_words words; mask_rows as prompt_rows
  * Token ids outside 0 .. vocab-1 are ignored; vocab <= 2^24.  A row whose mask allows nothing becomes -inf throughout.  Types, alignment and strides
  * as for psa_sample_tokens, for input and output each; out may be logits (same type and stride), otherwise the two do not overlap.
- * NaN logits stay NaN unless masked.  scratch: device, 4-byte aligned, psa_process_logits_scratch_bytes(num_rows, vocab) bytes (0 for
- * small vocabularies), needed in place with history or biases only; overwritten by every such call (calls that share it must be
- * ordered on one stream).  Only enqueues
- * one or two kernels.
+ * NaN logits stay NaN unless masked.  Needs no scratch memory; only enqueues one or two kernels.
  */
 typedef struct {
     const float *repetition, *frequency, *presence;
@@ -505,10 +502,9 @@ typedef struct {
     int32_t num_mask_bitmaps;
     const int32_t *mask_rows;
 } psa_logits_rules_t;
-size_t psa_process_logits_scratch_bytes(int32_t num_rows, int32_t vocab);
 psa_status_t psa_process_logits(const void *logits, int32_t logits_dtype, int64_t row_stride, int32_t num_rows, int32_t vocab,
                                 const psa_logits_rules_t *rules, void *out, int32_t out_dtype, int64_t out_row_stride,
-                                void *scratch, size_t scratch_bytes, void *cuda_stream);
+                                void *cuda_stream);
 /*
  * Token sets as bitmaps: bit i of row m (bits + m*row_words, i as above) is set when token i is among ids[indptr[m] .. indptr[m+1])
  * (int32 device, indptr [num_rows+1], cut to 0 .. num_ids), all others are cleared (the ceil(vocab / 32) words of a row are written whole).  Ids outside 0 .. vocab-1 are ignored.  For the

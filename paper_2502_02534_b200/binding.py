@@ -20,7 +20,7 @@ EXPORTED_SYMBOLS = [
     "psa_decode", "psa_decode_static", "psa_static_check_status", "psa_static_selftest_bounded_wait", "psa_decode_prefix", "psa_decode_suffix", "psa_decode_merge",
     "psa_decode_host_staging_bytes", "psa_decode_host", "psa_check_status", "psa_selftest_bounded_wait", "psa_append_kv", "psa_append_kv_alloc", "psa_validate_page_table", "psa_sample_scratch_bytes", "psa_sample_tokens", "psa_sample_tokens_at", "psa_attn_task",
     "psa_page_table_scratch_bytes", "psa_build_page_table", "psa_extend_page_table", "psa_read_status", "psa_kv4_cell_bytes", "psa_store_kv4",
-    "psa_load_kv4", "psa_plan_create_kv4", "psa_decode_kv4", "psa_decode_suffix_kv4", "psa_process_logits_scratch_bytes", "psa_process_logits", "psa_mark_tokens",
+    "psa_load_kv4", "psa_plan_create_kv4", "psa_decode_kv4", "psa_decode_suffix_kv4", "psa_process_logits", "psa_mark_tokens",
     "psa_status_string", "psa_last_error_message", "psa_version",
 ]
 
@@ -152,10 +152,8 @@ def library():
         lib.psa_decode_kv4.argtypes = [P, P, P, P, POINTER(c_int64), P, POINTER(c_int64), P, P, P, P, P, P, c_size_t, P]
         lib.psa_decode_suffix_kv4.restype = c_int32
         lib.psa_decode_suffix_kv4.argtypes = [P, P, P, POINTER(c_int64), P, P, P, P, c_size_t, P]
-        lib.psa_process_logits_scratch_bytes.restype = c_size_t
-        lib.psa_process_logits_scratch_bytes.argtypes = [c_int32, c_int32]
         lib.psa_process_logits.restype = c_int32
-        lib.psa_process_logits.argtypes = [P, c_int32, c_int64, c_int32, c_int32, POINTER(_LogitsRules), P, c_int32, c_int64, P, c_size_t, P]
+        lib.psa_process_logits.argtypes = [P, c_int32, c_int64, c_int32, c_int32, POINTER(_LogitsRules), P, c_int32, c_int64, P]
         lib.psa_mark_tokens.restype = c_int32
         lib.psa_mark_tokens.argtypes = [P, c_int32, P, c_int32, c_int32, P, c_int64, P]
         lib.psa_status_string.restype = c_char_p
@@ -620,22 +618,17 @@ def _decode_kv4_stage(plan, q, prefix_k, prefix_v, pool, page_indptr, page_indic
 
 def process_logits(logits, out=None, *, repetition=None, frequency=None, presence=None, history=None, history_lens=None,
                    prompt_bits=None, prompt_rows=None, bias_indptr=None, bias_ids=None, bias_values=None, mask_bits=None,
-                   mask_rows=None, scratch=None, stream=None):
+                   mask_rows=None, stream=None):
     """psa_process_logits on torch CUDA tensors: penalties for repeated tokens, biases and grammar masks.  logits and out [R, V] bf16
     or f32 (rows may be padded; out may be logits; allocated when None); repetition / frequency / presence [R] f32; history
     [R, capacity] int32 with history_lens [R]; prompt_bits / mask_bits [*, >= ceil(V / 32)] int32 bitmaps chosen per row by prompt_rows /
-    mask_rows [R] int32; bias_indptr [R+1], bias_ids int32 and bias_values f32; scratch uint8 (psa_process_logits_scratch_bytes, for callers
-    that must not allocate).  Returns out."""
+    mask_rows [R] int32; bias_indptr [R+1], bias_ids int32 and bias_values f32.  Returns out."""
     rows, vocab = logits.shape
     if out is None:
         import torch
         out = torch.empty((rows, (vocab + 7) // 8 * 8), dtype=logits.dtype, device=logits.device)[:, :vocab]
-    if scratch is None and vocab > 4096 and (history is not None or bias_ids is not None) and out.data_ptr() == logits.data_ptr():
-        need = library().psa_process_logits_scratch_bytes(rows, vocab)
-        if need:
-            scratch = _scratch(need, logits, stream)
     rc = (_calls or _native()).process_logits(logits, out, repetition, frequency, presence, history, history_lens, prompt_bits, prompt_rows, bias_indptr,
-                                              bias_ids, bias_values, mask_bits, mask_rows, scratch, stream)
+                                              bias_ids, bias_values, mask_bits, mask_rows, stream)
     if rc:
         _check(rc)
     return out

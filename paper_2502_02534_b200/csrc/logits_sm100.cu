@@ -40,6 +40,15 @@ constexpr int kStreamRun = 4, kStreamDepth = 4;            // tiles of a block; 
 constexpr int kWholeRow = 8192;                            // vocabularies up to this are streamed by the row's own block
 constexpr int kSlotsFew = 2048, kSlotsMany = 8192;         // hash table sizes
 constexpr int kOwn = kSlotsMany / 2 / kListThreads;         // list entries a thread keeps in registers
+constexpr int kThreads = 256, kTile = kThreads * kVec;     // one launch: threads of a block, logits it takes at a time,
+constexpr int kRun = 4;                                    // tiles of it,
+__host__ __device__ constexpr int run_depth(bool f32) { return f32 ? 3 : 4; }   // of them in flight
+constexpr int run_bytes(bool f32) { return run_depth(f32) * kTile * (f32 ? 4 : 2); }
+constexpr int kLog2RunSlots = 11, kRunSlots = 1 << kLog2RunSlots;   // its table, at most half full; also a slot for every token of a tile
+constexpr int kHits = kRunSlots / 2 - 1;                   // list entries inside the run that the hash table takes
+constexpr int kRunOwn = (kHits + kThreads - 1) / kThreads;
+static_assert(kRunSlots == kTile && kRun * kTile <= 0x8000, "a slot for every token, 15 bits for a place in the run");
+constexpr int64_t kFewLogits = 12 << 20;                   // one launch up to this many (64 rows x 131072: 14.1 us, two launches 15.4; 256 rows 48 and 37)
 constexpr int kMarkTile = 65536;                           // tokens of one block's bitmap
 constexpr int kMarkThreads = 1024;
 constexpr int kMarkBatch = 8;
@@ -50,8 +59,6 @@ struct RulesArgs {
     void *out;
     int64_t row_stride, out_stride;
     int vocab;
-    uint32_t *marks;      // [rows][words], in place only
-    int64_t mark_words;
     int log2_slots;       // of the largest table
 };
 
@@ -175,10 +182,9 @@ __device__ __forceinline__ uint32_t halves(uint32_t lo, uint32_t hi)
 }
 __device__ __forceinline__ uint32_t blend(uint32_t mask, uint32_t set, uint32_t clear) { return (set & mask) | (clear & ~mask); }
 
-// Eight consecutive logits that lie inside the row.  `marked`: those that are in the output already.  bf16 to bf16 stays packed: the
-// three selections are made on pairs.
+// Eight consecutive logits that lie inside the row.  bf16 to bf16 stays packed: the selections are made on pairs.
 template <bool kInF32, bool kOutF32, bool kUp>
-__device__ __forceinline__ void stream8(const Row &row, void *out, int i, const Vec8<kInF32> &v, uint32_t marked, uint32_t seen, uint32_t allowed)
+__device__ __forceinline__ void stream8(const Row &row, void *out, int i, const Vec8<kInF32> &v, uint32_t seen, uint32_t allowed)
 {
     float x[8];
     Vec8<kOutF32> o;
@@ -202,14 +208,6 @@ __device__ __forceinline__ void stream8(const Row &row, void *out, int i, const 
             w[2] = blend(halves<2>(lo, hi), w[2], none);
             w[3] = blend(halves<3>(lo, hi), w[3], none);
         }
-        if (marked) {
-            o.load(out, i);
-            const uint32_t lo = spread4(marked & 15u), hi = spread4(marked >> 4);
-            w[0] = blend(halves<0>(lo, hi), o.a.x, w[0]);
-            w[1] = blend(halves<1>(lo, hi), o.a.y, w[1]);
-            w[2] = blend(halves<2>(lo, hi), o.a.z, w[2]);
-            w[3] = blend(halves<3>(lo, hi), o.a.w, w[3]);
-        }
         o.a = make_uint4(w[0], w[1], w[2], w[3]);
     } else {
         v.get(x);
@@ -223,13 +221,6 @@ __device__ __forceinline__ void stream8(const Row &row, void *out, int i, const 
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = allowed & (1u << e) ? x[e] : -INFINITY;
         }
-        if (marked) {
-            float y[8];
-            o.load(out, i);
-            o.get(y);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = marked & (1u << e) ? y[e] : x[e];
-        }
         o.set(x);
     }
     o.store(out, i);
@@ -237,10 +228,9 @@ __device__ __forceinline__ void stream8(const Row &row, void *out, int i, const 
 
 // The last logits of a row whose vocabulary is not a multiple of eight, by one thread: neither read nor written beyond it.
 template <bool kInF32, bool kOutF32>
-__device__ __forceinline__ void stream_rest(const Row &row, const void *in, void *out, int vocab, const unsigned char *marks)
+__device__ __forceinline__ void stream_rest(const Row &row, const void *in, void *out, int vocab)
 {
     for (int i = vocab & ~7; i < vocab; ++i) {
-        if (marks && (marks[i >> 3] >> (i & 7)) & 1) continue;
         float x = load_one<kInF32>(in, i);
         if (row.prompt && Row::has(row.prompt, i)) x = row.penalised(x);
         store_one<kOutF32>(out, i, row.mask && !Row::has(row.mask, i) ? -INFINITY : x);
@@ -265,7 +255,7 @@ rules_stream_kernel(RulesArgs a)
     const int n = min(kStreamRun, ((a.vocab & ~7) - first + kStreamTile - 1) / kStreamTile);   // whole groups of this thread; may be <= 0
     const unsigned char *in = static_cast<const unsigned char *>(row_of(a.logits, a.row_stride, row, kInF32));
     void *out = const_cast<void *>(row_of(a.out, a.out_stride, row, kOutF32));
-    asm volatile("griddepcontrol.wait;" ::: "memory");                // for whatever wrote the inputs, or (in place) for the lists
+    asm volatile("griddepcontrol.wait;" ::: "memory");                // for whatever wrote the inputs
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the lists' launch may count beside this one
     auto request = [&](int t) {
         if (t < n) {
@@ -279,30 +269,28 @@ rules_stream_kernel(RulesArgs a)
 #pragma unroll
     for (int t = 0; t < kStreamDepth - 1; ++t) request(t);
     const Row r(a, row);
-    const unsigned char *marks = a.marks ? reinterpret_cast<const unsigned char *>(a.marks + row * a.mark_words) : nullptr;
-    uint32_t seen, allowed, marked;
+    uint32_t seen, allowed;
     auto bits = [&](int t) {
         const int at = (first + t * kStreamTile) >> 3;
         seen = r.prompt && t < n ? __ldg(r.prompt + at) : 0u;
         allowed = r.mask && t < n ? __ldg(r.mask + at) : 0u;
-        marked = marks && t < n ? marks[at] : 0u;
     };
     bits(0);
     auto work = [&](auto up) {
         for (int t = 0; t < n; ++t) {
             request(t + kStreamDepth - 1);
-            const uint32_t s = seen, ok = allowed, m = marked;
+            const uint32_t s = seen, ok = allowed;
             bits(t + 1);
             asm volatile("cp.async.wait_group %0;" ::"n"(kStreamDepth - 1) : "memory");
             Vec8<kInF32> v;
             v.load(&ring[t % kStreamDepth][threadIdx.x * kBytes], 0);
-            stream8<kInF32, kOutF32, up.value>(r, out, first + t * kStreamTile, v, m, s, ok);
+            stream8<kInF32, kOutF32, up.value>(r, out, first + t * kStreamTile, v, s, ok);
         }
     };
     if (r.rep < 1.f) work(std::true_type{});
     else work(std::false_type{});
     asm volatile("cp.async.wait_group 0;" ::: "memory");
-    if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) stream_rest<kInF32, kOutF32>(r, in, out, a.vocab, marks);
+    if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) stream_rest<kInF32, kOutF32>(r, in, out, a.vocab);
 }
 
 // Where a token's counters are: hashed with linear probing (the table is at most half full), or directly at id - r0.
@@ -374,12 +362,9 @@ __global__ void __launch_bounds__(kListThreads, 2)
 rules_lists_kernel(RulesArgs a)
 {
     extern __shared__ __align__(16) int32_t table_smem[];
-    __shared__ uint32_t own_marks[kWhole ? kWholeRow / 32 : 1];
     const int row = blockIdx.x, tid = threadIdx.x;
-    // Not the whole row, not in place: this runs under the stream of the same call, which has waited for the inputs and does not write
-    // them; only this kernel's writes have to wait for it.
-    const bool after = !kWhole && a.marks == nullptr;
-    if (!after) asm volatile("griddepcontrol.wait;" ::: "memory");
+    // Beside a stream: that has waited for the inputs and does not write them; only this kernel's writes have to wait for it.
+    if (kWhole) asm volatile("griddepcontrol.wait;" ::: "memory");
     const void *in = row_of(a.logits, a.row_stride, row, kInF32);
     void *out = const_cast<void *>(row_of(a.out, a.out_stride, row, kOutF32));
     const int32_t *said = a.r.history ? a.r.history + int64_t(row) * a.r.history_stride : nullptr;
@@ -400,9 +385,24 @@ rules_lists_kernel(RulesArgs a)
             if (i + kVec <= a.vocab) v[k].load(in, i);
         }
     }
-    uint32_t *marks = kWhole ? own_marks : after ? nullptr : a.marks + row * a.mark_words;
-    if (marks)
-        for (int w = tid; w < (a.vocab + 31) / 32; w += kListThreads) marks[w] = 0u;
+    // everything but the lists' tokens, whose logits have been read by then
+    auto rest = [&] {
+        if constexpr (kWhole) {
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < kWholeRow / kVec / kListThreads; ++k) {
+                const int i = (k * kListThreads + tid) * kVec;
+                if (i + kVec > a.vocab) continue;
+                const uint32_t seen = r.prompt ? __ldg(r.prompt + (i >> 3)) : 0u, allowed = r.mask ? __ldg(r.mask + (i >> 3)) : 0u;
+                if (r.rep < 1.f) stream8<kInF32, kOutF32, true>(r, out, i, v[k], seen, allowed);
+                else stream8<kInF32, kOutF32, false>(r, out, i, v[k], seen, allowed);
+            }
+            if (tid == 0) stream_rest<kInF32, kOutF32>(r, in, out, a.vocab);
+            __syncthreads();
+        } else {
+            asm volatile("griddepcontrol.wait;" ::: "memory");
+        }
+    };
 
     // the smallest table that stays half empty, or all there is, indexed directly
     const uint32_t entries = uint32_t(n_said) + uint32_t(n_bias);
@@ -443,7 +443,6 @@ rules_lists_kernel(RulesArgs a)
                 x[k] = load_one<kInF32>(in, id[k]);
                 if (r.prompt && Row::has(r.prompt, id[k])) in_prompt |= 1u << k;
                 if (r.mask && !Row::has(r.mask, id[k])) allowed &= ~(1u << k);
-                if (marks) atomicOr(marks + (id[k] >> 5), 1u << (id[k] & 31));
             }
         }
         __syncthreads();
@@ -451,12 +450,11 @@ rules_lists_kernel(RulesArgs a)
             if (tid < 32) add_biases(a.r.bias_ids + b0, a.r.bias_values + b0, n_bias, t, tid);
             __syncthreads();
         }
-        if (after) asm volatile("griddepcontrol.wait;" ::: "memory");
+        rest();
 #pragma unroll
         for (int k = 0; k < kOwn; ++k)
             if (at[k] >= 0)
                 store_one<kOutF32>(out, id[k], allowed & (1u << k) ? ruled(x[k], t.count[at[k]], in_prompt & (1u << k)) + t.value[at[k]] : -INFINITY);
-        if (kWhole) __syncthreads();   // the marks
     } else {
         for (int64_t r0 = 0; r0 < a.vocab; r0 += t.slots()) {
             t.r0 = int(r0);
@@ -474,28 +472,185 @@ rules_lists_kernel(RulesArgs a)
                 if (tid < 32) add_biases(a.r.bias_ids + b0, a.r.bias_values + b0, n_bias, t, tid);
                 __syncthreads();
             }
-            if (after) asm volatile("griddepcontrol.wait;" ::: "memory");
             for (int h = tid; h < t.slots(); h += kListThreads) {
                 const int token = t.key[h];
                 if (token < 0) continue;
                 const float x = ruled(load_one<kInF32>(in, token), t.count[h], r.prompt && Row::has(r.prompt, token));
-                store_one<kOutF32>(out, token, !r.mask || Row::has(r.mask, token) ? x + t.value[h] : -INFINITY);
-                if (marks) atomicOr(marks + (token >> 5), 1u << (token & 31));
+                t.value[h] = !r.mask || Row::has(r.mask, token) ? x + t.value[h] : -INFINITY;
             }
+            rest();   // a whole row has one range
+            for (int h = tid; h < t.slots(); h += kListThreads)
+                if (t.key[h] >= 0) store_one<kOutF32>(out, t.key[h], t.value[h]);
             __syncthreads();
         }
     }
-    if constexpr (kWhole) {
-        const unsigned char *bytes = reinterpret_cast<const unsigned char *>(own_marks);
+}
+
+// One block per (row, run of kRun tiles).  A thread copies its own groups of the next kDepth - 1 tiles ahead of itself into shared memory
+// (cp.async), so that enough bytes are on their way without registers or barriers.
+template <bool kInF32, bool kOutF32>
+__global__ void __launch_bounds__(kThreads, 4)
+rules_run_kernel(RulesArgs a)
+{
+    constexpr int kBytes = kVec * (kInF32 ? 4 : 2), kDepth = run_depth(kInF32);
+    extern __shared__ __align__(16) unsigned char ring[];   // [kDepth][kThreads * kBytes]
+    __shared__ __align__(16) int32_t keys[kRunSlots], counts[kRunSlots];
+    __shared__ __align__(16) float values[kRunSlots];
+    __shared__ uint16_t hits[kHits];   // the run's list entries: token - c0, and whether it is a bias
+    __shared__ int num_hits;
+    const int row = blockIdx.y, tid = threadIdx.x;
+    const int c0 = blockIdx.x * (kRun * kTile), c1 = min(a.vocab, c0 + kRun * kTile), tiles = (c1 - c0 + kTile - 1) / kTile;
+    const int first = c0 + tid * kVec, whole = a.vocab & ~7;
+    const void *in = row_of(a.logits, a.row_stride, row, kInF32);
+    void *out = const_cast<void *>(row_of(a.out, a.out_stride, row, kOutF32));
+    if (tid == 0) num_hits = 0;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    auto request = [&](int t) {
+        const int i = first + t * kTile;
+        if (t < tiles && i < whole) {
+            const uint32_t to = uint32_t(__cvta_generic_to_shared(ring + (t % kDepth * kThreads + tid) * kBytes));
+            const unsigned char *from = static_cast<const unsigned char *>(in) + int64_t(i) * (kBytes / kVec);
 #pragma unroll
-        for (int k = 0; k < kWholeRow / kVec / kListThreads; ++k) {
-            const int i = (k * kListThreads + tid) * kVec;
-            if (i + kVec > a.vocab) continue;
-            const uint32_t seen = r.prompt ? __ldg(r.prompt + (i >> 3)) : 0u, allowed = r.mask ? __ldg(r.mask + (i >> 3)) : 0u;
-            if (r.rep < 1.f) stream8<kInF32, kOutF32, true>(r, out, i, v[k], bytes[i >> 3], seen, allowed);
-            else stream8<kInF32, kOutF32, false>(r, out, i, v[k], bytes[i >> 3], seen, allowed);
+            for (int c = 0; c < kBytes; c += 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + c), "l"(from + c) : "memory");
         }
-        if (tid == 0) stream_rest<kInF32, kOutF32>(r, in, out, a.vocab, bytes);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int t = 0; t < kDepth - 1; ++t) request(t);
+    const Row r(a, row);
+    const int32_t *said = a.r.history ? a.r.history + int64_t(row) * a.r.history_stride : nullptr;
+    const int n_said = said ? max(0, min(a.r.history_lens[row], a.r.history_capacity)) : 0;
+    int b0 = 0, n_bias = 0;
+    if (a.r.bias_indptr) {
+        b0 = max(0, a.r.bias_indptr[row]);
+        n_bias = max(0, min(a.r.num_biases, a.r.bias_indptr[row + 1]) - b0);
+    }
+    uint32_t seen, allowed;
+    auto bits = [&](int t) {
+        const int i = first + t * kTile;
+        const bool there = t < tiles && i < whole;
+        seen = r.prompt && there ? __ldg(r.prompt + (i >> 3)) : 0u;
+        allowed = r.mask && there ? __ldg(r.mask + (i >> 3)) : 0u;
+    };
+    bits(0);
+    auto stream = [&](int t) {
+        request(t + kDepth - 1);
+        const uint32_t s = seen, ok = allowed;
+        bits(t + 1);
+        asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
+        const int i = first + t * kTile;
+        if (i < whole) {
+            Vec8<kInF32> v;
+            v.load(ring + (t % kDepth * kThreads + tid) * kBytes, 0);
+            if (r.rep < 1.f) stream8<kInF32, kOutF32, true>(r, out, i, v, s, ok);
+            else stream8<kInF32, kOutF32, false>(r, out, i, v, s, ok);
+        }
+        if (t == tiles - 1 && c1 == a.vocab && tid == 0) stream_rest<kInF32, kOutF32>(r, in, out, a.vocab);
+    };
+    if (n_said + n_bias == 0) {   // the same for the whole block, as everything below
+        for (int t = 0; t < tiles; ++t) stream(t);
+        return;
+    }
+
+    const float freq = a.r.frequency ? a.r.frequency[row] : 0.f;
+    const float pres = a.r.presence ? a.r.presence[row] : 0.f;
+    // logit x of a token that stands in the lists c times, apart from its biases
+    auto ruled = [&](float x, int c, bool in_prompt) {
+        if (c > 0 || in_prompt) x = r.penalised(x);
+        return c > 0 ? x - freq * float(c) - pres : x;
+    };
+    __syncthreads();   // num_hits
+    bool biased = false;
+    auto gather = [&](const int32_t *ids, int n, uint32_t flag) {
+        for (int e0 = tid; e0 < n; e0 += 4 * kThreads) {
+            int id[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) id[k] = e0 + k * kThreads < n ? ids[e0 + k * kThreads] : -1;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (id[k] >= c0 && id[k] < c1) {
+                    const int at = atomicAdd(&num_hits, 1);
+                    if (at < kHits) hits[at] = uint16_t(uint32_t(id[k] - c0) | flag);
+                    biased = biased || flag != 0u;
+                }
+        }
+    };
+    gather(said, n_said, 0u);
+    gather(a.r.bias_ids + b0, n_bias, 0x8000u);
+    biased = __syncthreads_or(biased);
+    const int n_hits = num_hits;
+    Table t;
+    t.key = keys; t.count = counts; t.value = values;
+    if (n_hits <= kHits) {
+        // The thread that brings a token into the table reads its logit and bits at once and keeps them in registers.
+        t.hashed = true;
+        t.log2_slots = max(6, 32 - __clz(2 * n_hits));
+        t.r0 = c0; t.r1 = c1;
+        t.clear(tid, kThreads);
+        __syncthreads();
+        int id[kRunOwn], at[kRunOwn];
+        float x[kRunOwn];
+        uint32_t in_prompt = 0u, open = ~0u;   // a bit per k
+#pragma unroll
+        for (int k = 0; k < kRunOwn; ++k) {
+            at[k] = -1;
+            if (k * kThreads >= n_hits) continue;
+            const int e = tid + k * kThreads;
+            if (e < n_hits) {
+                const uint32_t hit = hits[e];
+                bool mine;
+                id[k] = c0 + int(hit & 0x7FFFu);
+                const int h = t.add(id[k], mine);
+                if (!(hit & 0x8000u)) atomicAdd(t.count + h, 1);
+                if (mine) {
+                    at[k] = h;
+                    x[k] = load_one<kInF32>(in, id[k]);
+                    if (r.prompt && Row::has(r.prompt, id[k])) in_prompt |= 1u << k;
+                    if (r.mask && !Row::has(r.mask, id[k])) open &= ~(1u << k);
+                }
+            }
+        }
+        __syncthreads();
+        if (biased && tid < 32) add_biases(a.r.bias_ids + b0, a.r.bias_values + b0, n_bias, t, tid);
+        for (int g = 0; g < tiles; ++g) stream(g);
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kRunOwn; ++k)
+            if (at[k] >= 0)
+                store_one<kOutF32>(out, id[k], open & (1u << k) ? ruled(x[k], t.count[at[k]], in_prompt & (1u << k)) + t.value[at[k]] : -INFINITY);
+    } else {
+        // tile by tile, with a counter for every token of it
+        t.hashed = false;
+        t.log2_slots = kLog2RunSlots;
+        for (int g = 0; g < tiles; ++g) {
+            t.r0 = c0 + g * kTile;
+            t.r1 = min(c1, t.r0 + kTile);
+            t.clear(tid, kThreads);
+            __syncthreads();
+            bool mine;
+            for (int e = tid; e < n_said; e += kThreads) {
+                const int h = t.add(said[e], mine);
+                if (h >= 0) atomicAdd(t.count + h, 1);
+            }
+            for (int e = tid; e < n_bias; e += kThreads) t.add(a.r.bias_ids[b0 + e], mine);
+            __syncthreads();
+            if (biased) {
+                if (tid < 32) add_biases(a.r.bias_ids + b0, a.r.bias_values + b0, n_bias, t, tid);
+                __syncthreads();
+            }
+            for (int h = tid; h < kTile; h += kThreads) {
+                const int token = t.key[h];
+                if (token < 0) continue;
+                const float x = ruled(load_one<kInF32>(in, token), t.count[h], r.prompt && Row::has(r.prompt, token));
+                t.value[h] = !r.mask || Row::has(r.mask, token) ? x + t.value[h] : -INFINITY;
+            }
+            __syncthreads();   // in place: the logits have been read
+            stream(g);
+            __syncthreads();
+            for (int h = tid; h < kTile; h += kThreads)
+                if (t.key[h] >= 0) store_one<kOutF32>(out, t.key[h], t.value[h]);
+            __syncthreads();
+        }
     }
 }
 
@@ -550,37 +705,33 @@ cudaError_t launch_rules(const RulesArgs &a, int rows, bool lists, cudaStream_t 
 {
     const auto whole = rules_lists_kernel<kInF32, kOutF32, true>, part = rules_lists_kernel<kInF32, kOutF32, false>;
     const auto stream = rules_stream_kernel<kInF32, kOutF32>;
+    const auto run = rules_run_kernel<kInF32, kOutF32>;
     if (lists) {
         static PerDeviceOnce once;
         const int rc = once.ensure([&] {
             cudaError_t e = cudaFuncSetAttribute(whole, cudaFuncAttributeMaxDynamicSharedMemorySize, 12 * kSlotsMany);
             if (e == cudaSuccess) e = cudaFuncSetAttribute(part, cudaFuncAttributeMaxDynamicSharedMemorySize, 12 * kSlotsMany);
+            if (e == cudaSuccess) e = cudaFuncSetAttribute(run, cudaFuncAttributeMaxDynamicSharedMemorySize, run_bytes(kInF32));
             return int(e);
         });
         if (rc != 0) return cudaError_t(rc);
     }
     const size_t table = size_t(12) << a.log2_slots;
-    const dim3 tiles((a.vocab + kStreamRun * kStreamTile - 1) / (kStreamRun * kStreamTile), rows);
     if (lists && a.vocab <= kWholeRow) return launch_behind(whole, dim3(rows), kListThreads, table, st, a);
-    cudaError_t e = cudaSuccess;
-    if (lists && a.marks) e = launch_behind(part, dim3(rows), kListThreads, table, st, a);
-    if (e == cudaSuccess) e = launch_behind(stream, tiles, kStreamThreads, 0, st, a);
-    if (e == cudaSuccess && lists && !a.marks) e = launch_behind(part, dim3(rows), kListThreads, table, st, a);
+    if (lists && (a.logits == a.out || int64_t(rows) * a.vocab <= kFewLogits || (a.r.history && a.r.history_capacity >= kSlotsMany / 2)))
+        return launch_behind(run, dim3((a.vocab + kRun * kTile - 1) / (kRun * kTile), rows), kThreads, run_bytes(kInF32), st, a);
+    const dim3 tiles((a.vocab + kStreamRun * kStreamTile - 1) / (kStreamRun * kStreamTile), rows);
+    cudaError_t e = launch_behind(stream, tiles, kStreamThreads, 0, st, a);
+    if (e == cudaSuccess && lists) e = launch_behind(part, dim3(rows), kListThreads, table, st, a);
     return e;
 }
 
 }  // namespace
 }  // namespace psa
 
-extern "C" size_t psa_process_logits_scratch_bytes(int32_t num_rows, int32_t vocab)
-{
-    if (num_rows <= 0 || vocab <= psa::kWholeRow) return 0;
-    return size_t(num_rows) * ((size_t(vocab) + 31) / 32) * 4;
-}
-
 extern "C" psa_status_t psa_process_logits(const void *logits, int32_t logits_dtype, int64_t row_stride, int32_t num_rows, int32_t vocab,
                                            const psa_logits_rules_t *rules, void *out, int32_t out_dtype, int64_t out_row_stride,
-                                           void *scratch, size_t scratch_bytes, void *cuda_stream)
+                                           void *cuda_stream)
 {
     using psa::set_last_error;
     if (num_rows < 0 || vocab < 0) return set_last_error(PSA_ERR_INVALID_ARG, "negative num_rows or vocab");
@@ -604,12 +755,7 @@ extern "C" psa_status_t psa_process_logits(const void *logits, int32_t logits_dt
     if ((r.prompt_bits && r.prompt_row_words < words) || (r.mask_bits && r.mask_row_words < words))
         return set_last_error(PSA_ERR_INVALID_ARG, "bitmap rows must hold at least ceil(vocab / 32) words");
     const bool lists = (r.history && r.history_capacity > 0) || (r.bias_indptr && r.num_biases > 0);
-    psa::RulesArgs a{r, logits, out, row_stride, out_row_stride, vocab, nullptr, words, 0};
-    if (lists && vocab > psa::kWholeRow && logits == out) {
-        if (!scratch || reinterpret_cast<uintptr_t>(scratch) % 4 || scratch_bytes < psa_process_logits_scratch_bytes(num_rows, vocab))
-            return set_last_error(PSA_ERR_WORKSPACE, "scratch must be 4-byte aligned and hold psa_process_logits_scratch_bytes(num_rows, vocab)");
-        a.marks = static_cast<uint32_t *>(scratch);
-    }
+    psa::RulesArgs a{r, logits, out, row_stride, out_row_stride, vocab, 0};
     // the small table serves lists of fewer than 1024 entries, and leaves room for more blocks beside it
     const int64_t most = int64_t(r.history ? r.history_capacity : 0) + (r.bias_indptr ? r.num_biases : 0);
     a.log2_slots = most < psa::kSlotsFew / 2 ? 11 : 13;

@@ -297,10 +297,10 @@ struct Bitmaps {
 };
 
 // logits, out, repetition, frequency, presence, history, history_lens, prompt_bits, prompt_rows, bias_indptr, bias_ids, bias_values, mask_bits,
-// mask_rows, scratch, stream
+// mask_rows, stream
 psa_status_t process_logits(PyObject *const *args, Py_ssize_t given)
 {
-    Call c(args, given, 16);
+    Call c(args, given, 15);
     const at::Tensor &logits = c.tensor(0, "logits"), &out = c.tensor(1, "out");
     if (logits.dim() != 2 || out.sizes() != logits.sizes()) throw Refused("logits must be [rows, vocab], and out of the same shape");
     const int32_t in_code = dtype_code(logits, "logits"), out_code = dtype_code(out, "out");
@@ -335,11 +335,8 @@ psa_status_t process_logits(PyObject *const *args, Py_ssize_t given)
         r.bias_values = c.flat<float>(11, at::kFloat, "bias_values", n);
         r.num_biases = int32_t(n);
     }
-    void *scratch = c.flat(14, at::kByte, "scratch");
-    const size_t scratch_bytes = scratch ? size_t(c.numel(14)) : 0;
-    void *stream = c.stream(15);
-    return api.process_logits(logits.data_ptr(), in_code, in_stride, int32_t(R), int32_t(V), &r, out.data_ptr(), out_code, out_stride, scratch,
-                              scratch_bytes, stream);
+    void *stream = c.stream(14);
+    return api.process_logits(logits.data_ptr(), in_code, in_stride, int32_t(R), int32_t(V), &r, out.data_ptr(), out_code, out_stride, stream);
 }
 
 // ids, indptr, vocab, bits, stream

@@ -158,20 +158,48 @@ def test_lengths_beyond_the_capacity_are_cut_and_lists_stay_inside_their_arrays(
     compare(got, reference(cut, seen, ("freq", "history", "bias")), seen, cut, "f32")
 
 
-def test_scratch_of_the_callers_is_used_and_too_little_of_it_refused():
+@pytest.mark.parametrize("vocab", [9000, 20000])
+@pytest.mark.parametrize("history", [300, 1100, 5000, 40000])
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_long_histories_in_place_and_out_of_place(vocab, history, kind):
+    """Lists that fill, overflow and far exceed a block's table, in every launch form, against the definition."""
+    from paper_2502_02534_b200 import process_logits
+    c = case(3, vocab, 12)
+    rng = np.random.default_rng(vocab + history)
+    # half of the tokens among 600 neighbours, so that one block's run gets most of them
+    c["history"] = np.where(rng.random((3, history)) < .5, rng.integers(8000, 8600, (3, history)), rng.integers(0, vocab, (3, history))).astype(np.int32)
+    c["lens"] = np.array([history, history // 2, history - 1], np.int32)
+    _, x = padded(c["x"], kind)
+    seen = x.double().cpu().numpy()
+    kw = arguments(c, vocab, ALL)
+    want = reference(c, seen, ALL)
+    compare(process_logits(x, **kw).double().cpu().numpy(), want, seen, c, kind)
+    assert process_logits(x, x, **kw) is x
+    compare(x.double().cpu().numpy(), want, seen, c, kind)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_many_rows_are_the_same_rows(kind):
+    """More logits than one launch takes: rows must come out as they do alone, and as the definition has them; one row's biases
+    outnumber the table."""
     import torch
-    from paper_2502_02534_b200 import PsaError, library, process_logits
-    c = case(3, 9000, 12)
-    _, x = padded(c["x"], "f32")
-    kw = arguments(c, 9000, ALL)
-    need = library().psa_process_logits_scratch_bytes(3, 9000)
-    scratch = torch.full((need + 64,), 255, dtype=torch.uint8, device="cuda")
-    b = process_logits(x, **kw)
-    with pytest.raises(PsaError) as e:
-        process_logits(x, x, scratch=scratch[:need - 1], **kw)
-    assert e.value.status == 3
-    a = process_logits(x, x, scratch=scratch, **kw)
-    assert a is x and torch.equal(a.isnan(), b.isnan()) and torch.equal(a.nan_to_num(), b.nan_to_num()) and (scratch[need:] == 255).all()
+    from paper_2502_02534_b200 import process_logits
+    R, V = 97, 131075
+    assert R * V > 12 << 20
+    c = case(R, V, 14, said=700)
+    rng = np.random.default_rng(5)
+    c["biases"][2] = [(int(i), float(np.float32(v))) for i, v in zip(rng.integers(0, V, 9000), rng.normal(0, 3, 9000))]
+    _, x = padded(c["x"], kind)
+    kw = arguments(c, V, ALL)
+    got = process_logits(x, **kw)
+    few = [0, 1, 2, 5, 96]
+    part = {k: ([v[i] for i in few] if k in ("biases",) else v[few] if k in ("x", "history", "lens", "prompt_rows", "mask_rows", "rep", "freq", "pres") else v)
+            for k, v in c.items()}
+    alone = process_logits(x[few].contiguous() if V % 8 == 0 else padded(c["x"][few], kind)[1], **arguments(part, V, ALL))
+    assert torch.equal(got[few].nan_to_num(7.0), alone.nan_to_num(7.0))
+    seen = x[few].double().cpu().numpy()
+    compare(alone.double().cpu().numpy(), reference(part, seen, ALL), seen, part, kind)
+    assert process_logits(x, x, **kw) is x and torch.equal(x.nan_to_num(7.0), got.nan_to_num(7.0))
 
 
 def test_processed_logits_are_what_sampling_draws_from():

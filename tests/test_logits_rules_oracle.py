@@ -35,9 +35,9 @@ def test_host_refusals():
     from paper_2502_02534_b200.binding import _LogitsRules
     lib = psa.library()
 
-    def call(rules=None, logits=FAKE, code=0, stride=104, rows=2, vocab=100, out=FAKE + 4096, out_code=0, out_stride=104, scratch=None, size=0):
+    def call(rules=None, logits=FAKE, code=0, stride=104, rows=2, vocab=100, out=FAKE + 4096, out_code=0, out_stride=104):
         r = _LogitsRules(**(rules or {}))
-        return lib.psa_process_logits(logits, code, stride, rows, vocab, ctypes.byref(r), out, out_code, out_stride, scratch, size, None)
+        return lib.psa_process_logits(logits, code, stride, rows, vocab, ctypes.byref(r), out, out_code, out_stride, None)
     assert call(rows=-1) == 1 and call(vocab=-1) == 1 and call(vocab=0) == 1 and call(rows=0) == 0
     assert call(rows=65536) == 2 and call(vocab=(1 << 24) + 1, stride=1 << 25, out_stride=1 << 25) == 2 and call(code=2) == 2 and call(out_code=-1) == 2
     assert call(logits=None) == 1 and call(out=None) == 1 and call(logits=FAKE + 8) == 1 and call(out=FAKE + 2) == 1
@@ -46,11 +46,7 @@ def test_host_refusals():
     assert call(dict(history=FAKE)) == 1 and call(dict(history=FAKE, history_lens=FAKE, history_capacity=8, history_stride=4)) == 1
     assert call(dict(bias_indptr=FAKE, num_biases=3)) == 1 and call(dict(num_biases=-1)) == 1
     assert call(dict(prompt_bits=FAKE, prompt_row_words=3)) == 1 and call(dict(mask_bits=FAKE, mask_row_words=3)) == 1
-    assert lib.psa_process_logits(FAKE, 0, 104, 2, 100, None, FAKE, 0, 104, None, 0, None) == 1
-    big = dict(rules=dict(history=FAKE, history_lens=FAKE, history_capacity=4, history_stride=4), vocab=20000, stride=20000, out_stride=20000, out=FAKE)
-    need = lib.psa_process_logits_scratch_bytes(2, 20000)
-    assert need == 2 * 625 * 4 and lib.psa_process_logits_scratch_bytes(2, 100) == 0 and lib.psa_process_logits_scratch_bytes(-1, 20000) == 0
-    assert call(**big) == 3 and call(**big, scratch=FAKE, size=need - 1) == 3 and call(**big, scratch=FAKE + 2, size=need) == 3
+    assert lib.psa_process_logits(FAKE, 0, 104, 2, 100, None, FAKE, 0, 104, None) == 1
 
     def mark(ids=FAKE, n=4, indptr=FAKE, rows=2, vocab=100, bits=FAKE, words=4):
         return lib.psa_mark_tokens(ids, n, indptr, rows, vocab, bits, words, None)
