@@ -12,6 +12,8 @@
 // rounded 1 / s and one residual step, which rounds exactly like the division (Markstein) as long as nothing under- or overflows;
 // groups of extreme range, and those that are not finite, take the division itself.  Both kernels are bound by HBM: 4 bytes read and
 // 1.25 written per channel of K and V, or the reverse.
+// Measured, 65536 tokens x 8 heads of 128 channels (353 MB): store 57 us (6.2 TB/s, 0.95 of the measured copy rate), load 63 us (5.6
+// TB/s).  Store with 8 channels a thread 73-76 us (the indices twice), with grid-wide loops 85-102.
 #include <cuda_runtime.h>
 
 #include <algorithm>

@@ -13,13 +13,21 @@
 //            logit of every token in it;
 //   stream   every other logit: a thread takes eight consecutive ones, and one byte each of the prompt set and the mask tell what there
 //            is to do.
-// Up to kWholeRow tokens the block that did a row's lists streams the row as well (one launch).  Above it the stream is a launch of
-// its own with many blocks per row, and the lists' launch follows it: it counts while the stream is still running and writes its few
-// logits over the stream's when that is done.  In place that order would lose the inputs, so the lists go first, mark their tokens
-// in a bitmap in the caller's scratch memory, and the stream leaves marked logits as they are.
-// Lists of more entries than half the table are done in ranges of as many tokens as it has slots, indexed directly.
-// Bound: HBM, one read and one write of every logit (and 2 bits).  Counting inside the blocks of the stream instead, tile by tile,
-// costs barriers and dependent loads in each of them: 46 us for 256 rows x 131072 bf16 logits.
+// Three forms of it:
+//   whole    vocabularies up to kWholeRow: the block that did a row's lists streams the row as well, before it writes the lists' logits.
+//   run      a block per row and run of kRun tiles picks the entries of its own tokens out of the row's lists, streams the run and writes
+//            the lists' logits over it.  One launch, everything written where it was just read; but every block reads all the lists
+//            and waits for them.  For few logits, for long histories, and in place.
+//   two      the stream as a launch of its own, and the lists' launch behind it: that counts while the stream is still running and
+//            writes its few logits over the stream's when that is done.  For large batches with histories of fewer than 4096 tokens.
+// Lists of more entries than half the table are done with a counter for every token of a tile (run) or of as many tokens as the table
+// has slots (two).
+// Bound: HBM, one read and one write of every logit (and 2 bits).  Measured: 256 rows x 131072 bf16 logits, 1024 generated tokens and 32
+// biases each, 134.9 MB: two 36 us, run 48; the stream alone 24.3 (a plain copy of as many bytes takes 22.3), and the lists' 278 thousand
+// scattered logits, each a sector of its own, 12 behind it.  8 rows of that: run 6.4, two 7.9; 64 rows 14.2 and 15.4; 256 rows with 4096
+// generated tokens each 77 and 134.  8 rows x 3001: whole 4.7 us.
+// Tried for the largest case: lists by warps beside the streaming ones of a block 40-59 us; a resident stream of 5 blocks an SM with the
+// lists beside it from the start 42; groups of rows streamed and followed by their lists 35-42.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -48,7 +56,7 @@ constexpr int kLog2RunSlots = 11, kRunSlots = 1 << kLog2RunSlots;   // its table
 constexpr int kHits = kRunSlots / 2 - 1;                   // list entries inside the run that the hash table takes
 constexpr int kRunOwn = (kHits + kThreads - 1) / kThreads;
 static_assert(kRunSlots == kTile && kRun * kTile <= 0x8000, "a slot for every token, 15 bits for a place in the run");
-constexpr int64_t kFewLogits = 12 << 20;                   // one launch up to this many (64 rows x 131072: 14.1 us, two launches 15.4; 256 rows 48 and 37)
+constexpr int64_t kFewLogits = 12 << 20;                   // form run up to this many
 constexpr int kMarkTile = 65536;                           // tokens of one block's bitmap
 constexpr int kMarkThreads = 1024;
 constexpr int kMarkBatch = 8;
@@ -363,7 +371,7 @@ rules_lists_kernel(RulesArgs a)
 {
     extern __shared__ __align__(16) int32_t table_smem[];
     const int row = blockIdx.x, tid = threadIdx.x;
-    // Beside a stream: that has waited for the inputs and does not write them; only this kernel's writes have to wait for it.
+    // Behind a stream: that has waited for the inputs and does not write them; only this kernel's writes have to wait for it.
     if (kWhole) asm volatile("griddepcontrol.wait;" ::: "memory");
     const void *in = row_of(a.logits, a.row_stride, row, kInF32);
     void *out = const_cast<void *>(row_of(a.out, a.out_stride, row, kOutF32));
@@ -654,7 +662,8 @@ rules_run_kernel(RulesArgs a)
     }
 }
 
-// Token sets as bitmaps: one block per (row, kMarkTile tokens) walks the row's list and sets bits in shared memory.
+// Token sets as bitmaps: one block per (row, kMarkTile tokens) walks the row's list and sets bits in shared memory.  Bound by latency and, with
+// long lists, by the shared atomics: 64 rows x 32768 ids, vocabulary 131072 (two blocks a row, each reading the whole list) 5.4 us, floor 1.1.
 __global__ void __launch_bounds__(kMarkThreads)
 mark_kernel(const int32_t *__restrict__ ids, int num_ids, const int32_t *__restrict__ indptr, int vocab, uint32_t *__restrict__ bits, int64_t row_words)
 {

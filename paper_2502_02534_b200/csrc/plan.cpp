@@ -145,9 +145,9 @@ int choose_suffix_chunk(const int32_t *lens, int n, int num_kv_heads, int num_sm
 // none where a prefix block owns the SM) at a fair share of about 69 tokens per us each, an SM with fewer blocks runs each
 // of them faster (up to 2.2 times), and a block's start and end cost as much as 320 tokens.  Estimate in tokens:
 //     max( (sum of tokens + 320 per item) / min(slots, items),  longest item * max(blocks per SM / 4, 0.45) + 320 ).
-// Measured, suffix stage alone, chunks of 4096 / 1024 / 256 tokens: 64 samples x U[1,4096] x 8 heads 57.7 / 33.4 / 44.8 us (items of
-// 4096 leave a third of the machine idle at the end), 256 samples 120 / 143 / 246 us, 32 samples x U[0,1024] 11.5 / 11.5 / 10.1 us;
-// beside a 4096-token prefix the last one's step takes 16.8 us with 512-token chunks, 18.4 with 256, 18.5 with 832.
+// Measured, suffix stage alone: 64 samples x U[1,4096] x 8 heads, chunks of 4096 / 1792 (chosen) / 1024 / 512 tokens: 59.8 / 35.2 / 34.2 /
+// 37.2 us (items of 4096 leave a third of the machine idle at the end); 256 samples, 4096 (chosen) / 1024: 118 / 136; 32 samples x
+// U[0,1024], 1024 / 512 / 384 (chosen) / 256: 10.9 / 11.4 / 10.5 / 9.2, and their whole step beside a 4096-token prefix 18.0 / 16.4 / 16.4 / 16.9.
 int choose_kv4_chunk(const int32_t *lens, int n, int num_kv_heads, int num_sms, int prefix_items, bool prefix_owns_sm)
 {
     const double overhead = 320.0;

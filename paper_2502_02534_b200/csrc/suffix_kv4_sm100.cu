@@ -23,6 +23,11 @@
 //     terms do.  The centring is a product with a constant -8 on the same rounded operand, hence exact.
 // Bound: HBM at 1.25 * D bytes per (token, KV head) while the unpacking and the products keep up; one block per (sample, KV
 // head, token chunk), 4 warps with a private ring of kStages cells each, filled by 16-byte cp.async.
+// Measured: 256 samples x U[0, 4096] tokens x 8 heads of 128 channels, 671 MB: 118 us (5.7 TB/s, 0.87 of the measured copy rate) at
+// 1965 MHz; the copies alone take 105, the arithmetic alone 110 (284 instructions per page and warp: issue slots 60 % busy, ALU 50 %,
+// tensor pipe 45 %).  In long loops under the power limit the clock falls to 1630 MHz and the time follows it, to 141 us.
+// Four blocks an SM of 126 registers: five or six (96, 80 registers) spill, 137 and 184 us; two pages at a time 120-124; 2 or 8 warps a
+// block 121-124; q re-read from shared memory 121-126.
 // Slots of the last page beyond the sample's length hold whatever the pool held: their scores are set to -inf and their
 // parameters to zero, so nothing of them (NaN bit patterns included) reaches a result.
 #include <cuda_bf16.h>
@@ -36,7 +41,7 @@ namespace psa {
 namespace {
 
 constexpr int kWarps = 4;
-constexpr int kStages = 4;
+constexpr int kStages = 4;                // 40 KB a block at D = 128, four blocks an SM
 constexpr float kRescaleThreshold = 8.f;  // log2 units: the reference maximum may lag this far behind
 constexpr float kTwo64 = 18446744073709551616.f;
 constexpr float kUnscaleEven = 590295810358705651712.f;     // 2^69 = 2^133 / 2^64
