@@ -57,7 +57,7 @@ constexpr int kHits = kRunSlots / 2 - 1;                   // list entries insid
 constexpr int kRunOwn = (kHits + kThreads - 1) / kThreads;
 static_assert(kRunSlots == kTile && kRun * kTile <= 0x8000, "a slot for every token, 15 bits for a place in the run");
 constexpr int64_t kFewLogits = 12 << 20;                   // form run up to this many
-constexpr int kMarkTile = 65536;                           // tokens of one block's bitmap
+constexpr int kMarkTile = 131072;                          // tokens of one block's bitmap
 constexpr int kMarkThreads = 1024;
 constexpr int kMarkBatch = 8;
 
@@ -662,8 +662,9 @@ rules_run_kernel(RulesArgs a)
     }
 }
 
-// Token sets as bitmaps: one block per (row, kMarkTile tokens) walks the row's list and sets bits in shared memory.  Bound by latency and, with
-// long lists, by the shared atomics: 64 rows x 32768 ids, vocabulary 131072 (two blocks a row, each reading the whole list) 5.4 us, floor 1.1.
+// Token sets as bitmaps: one block per (row, kMarkTile tokens) walks the row's list and sets bits in shared memory.  Bound by the shared
+// atomics of one block, 16-byte loads change nothing: 64 rows x 32768 ids, vocabulary 131072, 5.4 us (floor 1.1); 256 rows 9.1, and 14.4
+// with tiles of half the size, whose blocks read every list twice.
 __global__ void __launch_bounds__(kMarkThreads)
 mark_kernel(const int32_t *__restrict__ ids, int num_ids, const int32_t *__restrict__ indptr, int vocab, uint32_t *__restrict__ bits, int64_t row_words)
 {

@@ -241,7 +241,7 @@ def test_a_replayed_graph_follows_its_inputs():
     compare(out.double().cpu().numpy(), reference(mixed, seen, ALL), seen, mixed, "f32")
 
 
-@pytest.mark.parametrize("rows,vocab", [(1, 1), (1, 31), (3, 32), (5, 33), (4, 32767), (3, 32768), (2, 32769), (2, 131072), (6, 100003)])
+@pytest.mark.parametrize("rows,vocab", [(1, 1), (1, 31), (3, 32), (5, 33), (4, 32767), (3, 32768), (2, 32769), (2, 131072), (2, 131073), (3, 300001), (6, 100003)])
 def test_mark(rows, vocab):
     import torch
     from paper_2502_02534_b200 import mark_tokens
