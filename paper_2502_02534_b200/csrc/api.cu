@@ -236,6 +236,7 @@ static psa_status_t prefix_impl(const psa_plan_t *plan, const void *q, const voi
     a.max_rows_per_item = plan->prefix_max_rows_per_item; a.max_tiles_per_item = plan->prefix_tiles_per_item;
     a.causal = plan->causal;
     a.kernel_choice = plan->cfg.prefix_kernel;
+    a.kv4 = plan->kv4;
     a.no_suffix_stage = plan->suffix_items.empty();
     a.partial_o = c.partial_o; a.partial_lse = c.partial_lse; a.status = c.status;
     a.launch_counter = count_blocks ? c.status + psa::kPrefixLaunchWord : nullptr;

@@ -204,6 +204,7 @@ psa_status_t build_plan(const psa_config_t &cfg, int32_t P, const int32_t *first
 
     plan->cfg = cfg;
     plan->causal = causal;
+    plan->kv4 = kv4;
     plan->group = G;
     plan->num_prefixes = P;
     plan->group_first_sample.assign(first_sample, first_sample + P);

@@ -95,6 +95,7 @@ struct psa_plan {
     int32_t prefix_tiles_per_item = 0;
     int32_t prefix_max_rows_per_item = 0;
     bool causal = false;          // a prefill plan
+    bool kv4 = false;             // a plan for a 4-bit suffix cache
     int32_t suffix_chunk_tokens = 0;
     int64_t num_partial_rows = 0;
     psa::WorkspaceLayout ws;
@@ -149,6 +150,7 @@ struct PrefixArgs {
     int32_t max_rows_per_item, max_tiles_per_item;  // over all items of the plan
     bool causal = false;  // prefill: row (token) i sees keys up to its own packed token index
     int32_t kernel_choice = 0;   // PSA_PREFIX_KERNEL_*: 0 = by the shape of the items
+    bool kv4 = false;               // the plan's suffixes are held in 4 bits
     bool no_suffix_stage = false;   // the plan has no suffix work at all: the prefix grid has the SMs to itself
     float *partial_o, *partial_lse;  // device
     int32_t *status;                 // device

@@ -430,3 +430,24 @@ def test_seeded_draws(seed):
     w = problem(D, G, Hkv, rng.integers(0, 200, P) * int(rng.integers(0, 2)), n, rng.integers(0, int(rng.choice([20, 300, 1200])), int(n.sum())), seed=seed)
     dt = str(rng.choice(["f32", "bf16"]))
     within_bounds(w, *run(w, dt, suffix_chunk_tokens=int(rng.choice([0, 64, 128]))), dt)
+
+
+@pytest.mark.parametrize("D,n_samples", [(128, 8), (128, 64), (64, 64)])
+def test_weights_of_the_prefix_carry_no_bias(D, n_samples):
+    """V = 1: the outputs are the rounded weights over their sum.  A weight is off by at most 2^-8, evenly, so the mean of 8192 of them
+    with an effective number of 8192 / e moves by 2^-8 / sqrt(3) / 55 = 4e-5; a weight lost to 2^-8 in one direction would show as 1e-3."""
+    import torch
+    from paper_2502_02534_b200 import Plan, decode_kv4, kv4_cell_bytes
+    g = torch.Generator(device="cuda").manual_seed(D + n_samples)
+    lens = np.zeros(n_samples, np.int32)
+    plan = Plan(np.array([8192], np.int32), np.array([n_samples], np.int32), lens, num_q_heads=8, num_kv_heads=2, head_dim=D,
+                sm_scale=D ** -.5, out_dtype="f32")
+    plan.bind_workspace()
+    q = torch.randn((n_samples, 8, D), generator=g, device="cuda").bfloat16()
+    k = torch.randn((8192, 2, D), generator=g, device="cuda").bfloat16()
+    out, lse = torch.empty((n_samples, 8, D), device="cuda"), torch.empty((n_samples, 8), device="cuda")
+    pool = torch.zeros((1, 2, kv4_cell_bytes(D)), dtype=torch.uint8, device="cuda")
+    decode_kv4(plan, q, k, torch.ones_like(k), pool, i32(np.zeros(n_samples + 1)), i32([0]), i32(lens), out, lse)
+    torch.cuda.synchronize()
+    assert abs(out.double().mean().item() - 1) < 2e-4
+    assert (out.double() - 1).abs().max().item() < 8e-4
