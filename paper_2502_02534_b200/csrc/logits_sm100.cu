@@ -15,19 +15,20 @@
 //            is to do.
 // Three forms of it:
 //   whole    vocabularies up to kWholeRow: the block that did a row's lists streams the row as well, before it writes the lists' logits.
+//   two      the stream as a launch of its own, and the lists' launch behind it: that counts while the stream is still running and
+//            writes its few logits over the stream's when that is done.
 //   run      a block per row and run of kRun tiles picks the entries of its own tokens out of the row's lists, streams the run and writes
 //            the lists' logits over it.  One launch, everything written where it was just read; but every block reads all the lists
-//            and waits for them.  For few logits, for long histories, and in place.
-//   two      the stream as a launch of its own, and the lists' launch behind it: that counts while the stream is still running and
-//            writes its few logits over the stream's when that is done.  For large batches with histories of fewer than 4096 tokens.
-// Lists of more entries than half the table are done with a counter for every token of a tile (run) or of as many tokens as the table
-// has slots (two).
-// Bound: HBM, one read and one write of every logit (and 2 bits).  Measured: 256 rows x 131072 bf16 logits, 1024 generated tokens and 32
-// biases each, 134.9 MB: two 36 us, run 48; the stream alone 24.3 (a plain copy of as many bytes takes 22.3), and the lists' 278 thousand
-// scattered logits, each a sector of its own, 12 behind it.  8 rows of that: run 6.4, two 7.9; 64 rows 14.2 and 15.4; 256 rows with 4096
-// generated tokens each 77 and 134.  8 rows x 3001: whole 4.7 us.
+//            and waits for them.  In place, and for lists that the row's table does not take.
+// Lists of more entries than the table takes are done with a counter for every token of a tile (run) or of as many tokens as the table
+// has slots (two, whole).
+// Bound: HBM, one read and one write of every logit (and 2 bits).  Measured: 256 rows x 131072 bf16 logits, U[0, 1024] generated tokens and
+// U[0, 64] biases each, 134.9 MB: two 28.4 us (31.2 over three sets of inputs in turn), run 48; the stream alone 24.3, a plain copy 22.3.
+// What the lists add is their latency, not their traffic: a table half full instead of a quarter 32.2 us, linear probing 38, 96 KB of
+// table instead of 48 (fewer blocks beside the stream's) 33.9, stream blocks of 4 or 16 tiles instead of 8 33.7 and 34.5.
+// 8 / 64 rows of that: two 6.6 / 11.2, run 6.3 / 13.9; 256 rows with 3500 generated tokens each 49 and 76.  8 rows x 3001: whole 4.4 us.
 // Tried for the largest case: lists by warps beside the streaming ones of a block 40-59 us; a resident stream of 5 blocks an SM with the
-// lists beside it from the start 42; groups of rows streamed and followed by their lists 35-42.
+// lists beside it from the start 42; groups of rows streamed and followed by their lists 35-42; prefetching the lists into L2: no change.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -44,10 +45,12 @@ constexpr int kListThreads = 512;
 constexpr int kStreamThreads = 256;
 constexpr int kVec = 8;                                    // logits a thread handles together
 constexpr int kStreamTile = kStreamThreads * kVec;         // logits a block of the stream takes at a time
-constexpr int kStreamRun = 4, kStreamDepth = 4;            // tiles of a block; of them in flight
+constexpr int kStreamRun = 8, kStreamDepth = 4;            // tiles of a block; of them in flight
 constexpr int kWholeRow = 8192;                            // vocabularies up to this are streamed by the row's own block
-constexpr int kSlotsFew = 2048, kSlotsMany = 8192;         // hash table sizes
-constexpr int kOwn = kSlotsMany / 2 / kListThreads;         // list entries a thread keeps in registers
+constexpr int kLog2Few = 11, kLog2Many = 13;                // sizes of the row's hash table
+__host__ __device__ constexpr int64_t table_takes(int log2_slots) { return int64_t(1) << (log2_slots - 1); }   // entries: half full
+constexpr int kOwn = 8;                                    // list entries a thread keeps in registers
+constexpr int kLongHistory = kOwn * kListThreads;
 constexpr int kThreads = 256, kTile = kThreads * kVec;     // one launch: threads of a block, logits it takes at a time,
 constexpr int kRun = 4;                                    // tiles of it,
 __host__ __device__ constexpr int run_depth(bool f32) { return f32 ? 3 : 4; }   // of them in flight
@@ -56,7 +59,6 @@ constexpr int kLog2RunSlots = 11, kRunSlots = 1 << kLog2RunSlots;   // its table
 constexpr int kHits = kRunSlots / 2 - 1;                   // list entries inside the run that the hash table takes
 constexpr int kRunOwn = (kHits + kThreads - 1) / kThreads;
 static_assert(kRunSlots == kTile && kRun * kTile <= 0x8000, "a slot for every token, 15 bits for a place in the run");
-constexpr int64_t kFewLogits = 12 << 20;                   // form run up to this many
 constexpr int kMarkTile = 131072;                          // tokens of one block's bitmap
 constexpr int kMarkThreads = 1024;
 constexpr int kMarkBatch = 8;
@@ -301,7 +303,7 @@ rules_stream_kernel(RulesArgs a)
     if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) stream_rest<kInF32, kOutF32>(r, in, out, a.vocab);
 }
 
-// Where a token's counters are: hashed with linear probing (the table is at most half full), or directly at id - r0.
+// Where a token's counters are: hashed with linear probing (the table is never full), or directly at id - r0.
 struct Table {
     int32_t *key, *count;
     float *value;
@@ -317,7 +319,7 @@ struct Table {
             key[id - r0] = id;
             return id - r0;
         }
-        for (int h = int((uint32_t(id) * 2654435761u) >> (32 - log2_slots));; h = (h + 1) & (slots() - 1)) {
+        for (int h = int((uint32_t(id) * 2654435761u) >> (32 - log2_slots)), k = 1;; h = (h + k++) & (slots() - 1)) {
             const int old = atomicCAS(key + h, -1, id);
             mine = old == -1;
             if (mine || old == id) return h;
@@ -336,7 +338,7 @@ struct Table {
         if (id < r0 || id >= r1) return -1;
         if (!hashed) return id - r0;
         int h = int((uint32_t(id) * 2654435761u) >> (32 - log2_slots));
-        while (key[h] != id) h = (h + 1) & (slots() - 1);
+        for (int k = 1; key[h] != id; ++k) h = (h + k) & (slots() - 1);
         return h;
     }
 };
@@ -366,7 +368,7 @@ __device__ void add_biases(const int32_t *ids, const float *values, int n, const
 }
 
 template <bool kInF32, bool kOutF32, bool kWhole>
-__global__ void __launch_bounds__(kListThreads, 2)
+__global__ void __launch_bounds__(kListThreads, kWhole ? 2 : 3)
 rules_lists_kernel(RulesArgs a)
 {
     extern __shared__ __align__(16) int32_t table_smem[];
@@ -415,8 +417,9 @@ rules_lists_kernel(RulesArgs a)
     // the smallest table that stays half empty, or all there is, indexed directly
     const uint32_t entries = uint32_t(n_said) + uint32_t(n_bias);
     Table t;
-    t.log2_slots = max(9, 32 - __clz(2 * entries));
-    t.hashed = entries < (1u << 30) && t.log2_slots <= a.log2_slots;
+    t.log2_slots = max(9, entries > 1u ? 33 - __clz(entries - 1u) : 0);
+    if (t.log2_slots < a.log2_slots) ++t.log2_slots;   // a quarter full, where there is room
+    t.hashed = entries <= kLongHistory && t.log2_slots <= a.log2_slots;
     if (!t.hashed) t.log2_slots = a.log2_slots;
     t.key = table_smem; t.count = t.key + t.slots(); t.value = reinterpret_cast<float *>(t.count + t.slots());
     // logit x of a token that stands in the lists c times, apart from its biases
@@ -711,7 +714,7 @@ cudaError_t launch_behind(Kernel kernel, dim3 grid, int threads, size_t smem, cu
 }
 
 template <bool kInF32, bool kOutF32>
-cudaError_t launch_rules(const RulesArgs &a, int rows, bool lists, cudaStream_t st)
+cudaError_t launch_rules(const RulesArgs &a, int rows, bool lists, bool long_lists, cudaStream_t st)
 {
     const auto whole = rules_lists_kernel<kInF32, kOutF32, true>, part = rules_lists_kernel<kInF32, kOutF32, false>;
     const auto stream = rules_stream_kernel<kInF32, kOutF32>;
@@ -719,8 +722,8 @@ cudaError_t launch_rules(const RulesArgs &a, int rows, bool lists, cudaStream_t 
     if (lists) {
         static PerDeviceOnce once;
         const int rc = once.ensure([&] {
-            cudaError_t e = cudaFuncSetAttribute(whole, cudaFuncAttributeMaxDynamicSharedMemorySize, 12 * kSlotsMany);
-            if (e == cudaSuccess) e = cudaFuncSetAttribute(part, cudaFuncAttributeMaxDynamicSharedMemorySize, 12 * kSlotsMany);
+            cudaError_t e = cudaFuncSetAttribute(whole, cudaFuncAttributeMaxDynamicSharedMemorySize, 12 << kLog2Many);
+            if (e == cudaSuccess) e = cudaFuncSetAttribute(part, cudaFuncAttributeMaxDynamicSharedMemorySize, 12 << kLog2Many);
             if (e == cudaSuccess) e = cudaFuncSetAttribute(run, cudaFuncAttributeMaxDynamicSharedMemorySize, run_bytes(kInF32));
             return int(e);
         });
@@ -728,7 +731,7 @@ cudaError_t launch_rules(const RulesArgs &a, int rows, bool lists, cudaStream_t 
     }
     const size_t table = size_t(12) << a.log2_slots;
     if (lists && a.vocab <= kWholeRow) return launch_behind(whole, dim3(rows), kListThreads, table, st, a);
-    if (lists && (a.logits == a.out || int64_t(rows) * a.vocab <= kFewLogits || (a.r.history && a.r.history_capacity >= kSlotsMany / 2)))
+    if (lists && (a.logits == a.out || long_lists))
         return launch_behind(run, dim3((a.vocab + kRun * kTile - 1) / (kRun * kTile), rows), kThreads, run_bytes(kInF32), st, a);
     const dim3 tiles((a.vocab + kStreamRun * kStreamTile - 1) / (kStreamRun * kStreamTile), rows);
     cudaError_t e = launch_behind(stream, tiles, kStreamThreads, 0, st, a);
@@ -766,16 +769,20 @@ extern "C" psa_status_t psa_process_logits(const void *logits, int32_t logits_dt
         return set_last_error(PSA_ERR_INVALID_ARG, "bitmap rows must hold at least ceil(vocab / 32) words");
     const bool lists = (r.history && r.history_capacity > 0) || (r.bias_indptr && r.num_biases > 0);
     psa::RulesArgs a{r, logits, out, row_stride, out_row_stride, vocab, 0};
-    // the small table serves lists of fewer than 1024 entries, and leaves room for more blocks beside it
-    const int64_t most = int64_t(r.history ? r.history_capacity : 0) + (r.bias_indptr ? r.num_biases : 0);
-    a.log2_slots = most < psa::kSlotsFew / 2 ? 11 : 13;
-    static_assert(psa::kSlotsFew == 1 << 11 && psa::kSlotsMany == 1 << 13, "table sizes");
+    // A table as small as the lists allow, since it decides how many of their blocks fit beside the stream's (256 rows x 131072, up
+    // to 1088 entries a row: 96 KB 33.9 us, 48 KB 31.2).  For whole rows it takes all entries there can be or has a slot for every token; else it
+    // takes four times the mean number of biases, and rows with more are done in ranges.
+    const int64_t said = r.history ? r.history_capacity : 0, biases = r.bias_indptr ? r.num_biases : 0;
+    const int64_t most = said + (vocab <= psa::kWholeRow ? biases : std::min(biases, std::max<int64_t>(512, 4 * biases / num_rows)));
+    a.log2_slots = psa::kLog2Few;
+    while (a.log2_slots < psa::kLog2Many && most > psa::table_takes(a.log2_slots)) ++a.log2_slots;
+    static_assert(psa::kWholeRow <= 1 << psa::kLog2Many, "a slot for every token");
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     cudaError_t e;
     if (logits_dtype == PSA_OUT_F32)
-        e = out_dtype == PSA_OUT_F32 ? psa::launch_rules<true, true>(a, num_rows, lists, st) : psa::launch_rules<true, false>(a, num_rows, lists, st);
+        e = out_dtype == PSA_OUT_F32 ? psa::launch_rules<true, true>(a, num_rows, lists, most > psa::table_takes(psa::kLog2Many), st) : psa::launch_rules<true, false>(a, num_rows, lists, most > psa::table_takes(psa::kLog2Many), st);
     else
-        e = out_dtype == PSA_OUT_F32 ? psa::launch_rules<false, true>(a, num_rows, lists, st) : psa::launch_rules<false, false>(a, num_rows, lists, st);
+        e = out_dtype == PSA_OUT_F32 ? psa::launch_rules<false, true>(a, num_rows, lists, most > psa::table_takes(psa::kLog2Many), st) : psa::launch_rules<false, false>(a, num_rows, lists, most > psa::table_takes(psa::kLog2Many), st);
     if (e != cudaSuccess) return set_last_error(PSA_ERR_CUDA, std::string("logits launch: ") + cudaGetErrorString(e));
     return PSA_OK;
 }
