@@ -262,3 +262,35 @@ def test_mark(rows, vocab):
     got = mark_tokens(dev(ids), dev(cut), vocab)
     ref = lr.bitmaps([ids[max(0, cut[m]):min(len(ids), cut[m + 1])].tolist() for m in range(rows)], vocab)
     assert np.array_equal(got.cpu().numpy().view(np.uint32), ref)
+
+
+def test_captured_calls_on_two_streams_follow_their_inputs():
+    """The two launches of a large vocabulary, captured twice over the same lists and replayed side by side with other logits."""
+    import torch
+    from paper_2502_02534_b200 import process_logits
+    V = 20001
+    c = case(5, V, 31)
+    kw = arguments(c, V, ALL)
+    graphs, xs, outs, streams = [], [], [], [torch.cuda.Stream(), torch.cuda.Stream()]
+    for st in streams:
+        xs.append(padded(c["x"], "f32")[1])
+        outs.append(padded(np.zeros_like(c["x"]), "f32")[1])
+        process_logits(xs[-1], outs[-1], **kw)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=st):
+            for _ in range(3):
+                process_logits(xs[-1], outs[-1], **kw)
+        graphs.append(g)
+    others = [case(5, V, 40 + i)["x"] for i in range(2)]
+    for x, o in zip(xs, others):
+        x.copy_(torch.from_numpy(o))
+    torch.cuda.synchronize()
+    for st, g in zip(streams, graphs):
+        with torch.cuda.stream(st):
+            for _ in range(4):
+                g.replay()
+    torch.cuda.synchronize()
+    for o, out in zip(others, outs):
+        seen = o.astype(np.float64)
+        compare(out.double().cpu().numpy(), reference(c, seen, ALL), seen, c, "f32")
