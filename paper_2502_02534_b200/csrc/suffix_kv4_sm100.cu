@@ -27,7 +27,8 @@
 // 1965 MHz; the copies alone take 105, the arithmetic alone 110 (284 instructions per page and warp: issue slots 60 % busy, ALU 50 %,
 // tensor pipe 45 %).  In long loops under the power limit the clock falls to 1630 MHz and the time follows it, to 141 us.
 // Four blocks an SM of 126 registers: five or six (96, 80 registers) spill, 137 and 184 us; two pages at a time 120-124; 2 or 8 warps a
-// block 121-124; q re-read from shared memory 121-126.
+// block 121-124; q re-read from shared memory 121-126; 3 or 5 stages 120-121; one bulk copy a page with a barrier of its own 126; packed
+// two-wide fp32 operations 118-119.
 // Slots of the last page beyond the sample's length hold whatever the pool held: their scores are set to -inf and their
 // parameters to zero, so nothing of them (NaN bit patterns included) reaches a result.
 #include <cuda_bf16.h>
