@@ -694,6 +694,16 @@ mark_kernel(const int32_t *__restrict__ ids, int num_ids, const int32_t *__restr
 }
 
 bool misaligned(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n != 0; }
+// Whether rows of `width` bytes every `stride` bytes from p share memory with rows of `width2` every `stride2` from q.  Different strides
+// count as sharing wherever the two ranges do.
+bool rows_overlap(const void *p, int64_t stride, int64_t width, const void *q, int64_t stride2, int64_t width2, int64_t rows)
+{
+    const int64_t gap = int64_t(reinterpret_cast<uintptr_t>(q)) - int64_t(reinterpret_cast<uintptr_t>(p));
+    if (gap >= (rows - 1) * stride + width || -gap >= (rows - 1) * stride2 + width2) return false;
+    if (stride != stride2 || rows == 1) return true;
+    const int64_t d = ((gap % stride) + stride) % stride;   // from a row of p to the next row of q
+    return d < width || stride - d < width2;
+}
 bool known_dtype(int32_t d) { return d == PSA_OUT_BF16 || d == PSA_OUT_F32; }
 
 // A launch that sets itself up under the tail of the one before it and waits there (griddepcontrol.wait) for its results.
@@ -759,6 +769,9 @@ extern "C" psa_status_t psa_process_logits(const void *logits, int32_t logits_dt
         return set_last_error(PSA_ERR_INVALID_ARG, "logits and out must be 16-byte aligned with row strides >= vocab that are multiples of 8 elements");
     if (logits == out && (logits_dtype != out_dtype || row_stride != out_row_stride))
         return set_last_error(PSA_ERR_INVALID_ARG, "in place, input and output must have the same type and stride");
+    const int64_t in_size = logits_dtype == PSA_OUT_F32 ? 4 : 2, out_size = out_dtype == PSA_OUT_F32 ? 4 : 2;
+    if (logits != out && psa::rows_overlap(logits, row_stride * in_size, vocab * in_size, out, out_row_stride * out_size, vocab * out_size, num_rows))
+        return set_last_error(PSA_ERR_INVALID_ARG, "logits and out must be the same array or not overlap");
     const psa_logits_rules_t &r = *rules;
     if ((r.history && !r.history_lens) || r.history_capacity < 0 || (r.history && r.history_stride < r.history_capacity))
         return set_last_error(PSA_ERR_INVALID_ARG, "history needs history_lens and a stride of at least its capacity");

@@ -294,3 +294,20 @@ def test_captured_calls_on_two_streams_follow_their_inputs():
     for o, out in zip(others, outs):
         seen = o.astype(np.float64)
         compare(out.double().cpu().numpy(), reference(c, seen, ALL), seen, c, "f32")
+
+
+def test_logits_and_out_side_by_side_in_one_buffer():
+    import torch
+    from paper_2502_02534_b200 import PsaError, process_logits
+    c = case(4, 9000, 51)
+    kw = arguments(c, 9000, ALL)
+    buf = torch.zeros((4, 18000), device="cuda")
+    x, out = buf[:, :9000], buf[:, 9000:]
+    x.copy_(torch.from_numpy(c["x"]))
+    process_logits(x, out, **kw)
+    seen = x.double().cpu().numpy()
+    compare(out.double().cpu().numpy(), reference(c, seen, ALL), seen, c, "f32")
+    process_logits(out, x, **kw)
+    for other in (buf[:, 8000:17000], buf[:, 8:9008]):
+        with pytest.raises((PsaError, ValueError), match="overlap"):
+            process_logits(x, other, **kw)
