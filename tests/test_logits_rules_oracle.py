@@ -45,7 +45,7 @@ def test_host_refusals():
     assert call(out=FAKE, out_code=1) == 1 and call(out=FAKE, out_stride=112) == 1                 # in place, but not the same array
     # shifted by a row or by less than a row (bf16: 208 bytes from row to row, 200 of them used), either way round, and f32 into the end of them
     assert call(out=FAKE + 208) == 1 and call(out=FAKE + 16) == 1 and call(out=FAKE - 208) == 1 and call(out=FAKE - 16) == 1
-    assert call(out=FAKE + 400, out_code=1) == 1 and call(out=FAKE + 304, stride=408, out_stride=408) == 1
+    assert call(out=FAKE + 400, out_code=1) == 1 and call(out=FAKE + 720, stride=408, out_stride=408) == 1
     assert call(dict(history=FAKE)) == 1 and call(dict(history=FAKE, history_lens=FAKE, history_capacity=8, history_stride=4)) == 1
     assert call(dict(bias_indptr=FAKE, num_biases=3)) == 1 and call(dict(num_biases=-1)) == 1
     assert call(dict(prompt_bits=FAKE, prompt_row_words=3)) == 1 and call(dict(mask_bits=FAKE, mask_row_words=3)) == 1
