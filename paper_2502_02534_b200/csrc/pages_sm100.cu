@@ -131,14 +131,12 @@ struct TableCopy {
     int32_t *token_indptr, *page_indptr;
     int2 *rec;
 };
-__device__ Sums scan_chunk(const PageTableArgs &a, int s0, const Sums &before, int avail, int *used_to, const TableCopy *copy)
+__device__ Sums scan_chunk(const PageTableArgs &a, int s0, const Ask &q, const Sums &before, int avail, int *used_to, const TableCopy *copy)
 {
     __shared__ long long warp_sums[3][32];
     __shared__ int block_used;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int s = s0 + int(threadIdx.x);
-    Ask q{};
-    if (s < a.num_samples) q = ask(a, s);
     const long long v[3] = {q.count, q.entries, q.pages};
     long long incl[3];
 #pragma unroll
@@ -366,7 +364,8 @@ page_table_one_block_kernel(PageTableArgs a)
     int used = 0;
     for (int s0 = 0; s0 < a.num_samples; s0 += kScanThreads) {
         int u;
-        sums = scan_chunk(a, s0, sums, avail, &u, &copy);
+        const int s = s0 + int(threadIdx.x);
+        sums = scan_chunk(a, s0, s < a.num_samples ? ask(a, s) : Ask{}, sums, avail, &u, &copy);
         used = max(used, u);
     }
     if (threadIdx.x == 0 && a.num_samples == 0) {
@@ -386,6 +385,8 @@ page_table_scan_kernel(PageTableArgs a)
     __shared__ long long part[3][32];
     const int avail = max(*a.free_count, 0);
     const int s0 = blockIdx.x * kScanThreads, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int own = s0 + int(threadIdx.x);
+    const Ask asked = own < a.num_samples ? ask(a, own) : Ask{};   // under way together with the samples before
     Sums mine{0, 0, 0};
     for (int s = threadIdx.x; s < s0; s += kScanThreads) {
         const Ask q = ask(a, s);
@@ -396,7 +397,7 @@ page_table_scan_kernel(PageTableArgs a)
     __syncthreads();
     const Sums before{warp_total(part[0][lane]), warp_total(part[1][lane]), warp_total(part[2][lane])};
     int used;
-    scan_chunk(a, s0, before, avail, &used, nullptr);
+    scan_chunk(a, s0, asked, before, avail, &used, nullptr);
     if (threadIdx.x == 0) {
         a.block_used[blockIdx.x] = used;
         if (blockIdx.x == 0) {
