@@ -20,7 +20,7 @@
 // Measured: 256 samples x 1 token 5.5 us, an empty launch being about 2; 2048 samples x U[0, 4096] tokens, capacity 8.4 million, 19.5 us
 // for 70 MB (3.6 TB/s; a plain fill of as many bytes takes 10.5, the scan before it 5).  Pieces dealt out in turn instead of in runs
 // cost a search each: 22.4 us.  Every block scanning up to 2048 samples for itself, without the launch before it: 27 us, and 13.9
-// instead of 10.9 us for 2048 samples x 1 token.
+// instead of 10.7 us for 2048 samples x 1 token.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -37,7 +37,7 @@ constexpr int kSpread = 256;                 // most tokens or list entries a wa
 static_assert(kSpread / kPageSize < 32, "a warp holds the pages of a piece, one a lane");
 constexpr int64_t kMostEntries = 0x7fffff00; // 32-bit positions, with room for one more stride of a loop
 constexpr int kWalk = 8;                     // samples in such a piece that are walked one after the other
-constexpr int64_t kOneBlockWork = 4096;      // one block: 1024 samples x 4 tokens 8.7 us, 2048 x 4 15.1; two launches 9.7 and 11.3
+constexpr int64_t kOneBlockWork = 4096;      // one block: 1024 samples x 4 tokens 8.7 us, 2048 x 4 15.1; two launches 9.7 and 10.8
 constexpr int kOneBlockSamples = 1024;
 
 struct PageTableArgs {
@@ -453,7 +453,7 @@ psa_status_t run(PageTableArgs a, void *scratch, size_t scratch_bytes, void *cud
         e = cudaGetLastError();
         if (e == cudaSuccess) {
             // pieces small enough to keep the machine's warps busy: 8.9 million lookups take 19.5 us in pieces of 256 and 26 in 128,
-            // 270 thousand 9.4 and 7.7, 8 thousand 15 and 12.4 (11.3 in 32)
+            // 270 thousand 9.4 and 7.7, 8 thousand 15 and 12.4 (10.8 in 32)
             auto go = [&](auto piece) {
                 const int64_t warps = (work + piece.value - 1) / piece.value;
                 cudaLaunchConfig_t lc{};
