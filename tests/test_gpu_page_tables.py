@@ -67,7 +67,7 @@ def run_extend(held, new, max_lens, free, count, indptr, indices, tokens, in_pla
 
 @pytest.mark.parametrize("in_place", [False, True])
 @pytest.mark.parametrize("n,longest,pad_tokens", [(0, 1, 0), (1, 0, 5), (1, 1, 0), (1, 17, 3), (7, 40, 1), (33, 500, 100), (1024, 30, 7), (1025, 40, 0),
-                                                  (2500, 70, 300), (5000, 3, 1), (40, 4000, 17)])
+                                                  (2500, 70, 300), (5000, 3, 1), (40, 4000, 17), (500, 9000, 5000), (16000, 290, 3)])
 def test_build(n, longest, pad_tokens, in_place):
     rng = np.random.default_rng(n * 31 + longest)
     seq = rng.integers(0, longest + 1, n)
@@ -93,7 +93,7 @@ def lists(rng, n, longest, slack):
 
 @pytest.mark.parametrize("in_place", [False, True])
 @pytest.mark.parametrize("n,longest,new_max,slack", [(1, 0, 1, 1), (1, 40, 33, 4), (9, 64, 1, 1), (256, 300, 1, 1), (300, 100, 40, 3), (1500, 60, 20, 2),
-                                                     (6000, 20, 3, 1), (20, 2000, 2000, 130)])
+                                                     (6000, 20, 3, 1), (20, 2000, 2000, 130), (300, 3000, 15001, 1000), (9000, 100, 480, 40)])
 def test_extend(n, longest, new_max, slack, in_place):
     rng = np.random.default_rng(n + 7 * longest)
     held, indptr, indices, free = lists(rng, n, longest, slack)
