@@ -17,16 +17,16 @@
 //   whole    vocabularies up to kWholeRow: the block that did a row's lists streams the row as well, before it writes the lists' logits.
 //   two      the stream as a launch of its own, and the lists' launch behind it: that counts while the stream is still running and
 //            writes its few logits over the stream's when that is done.
-//   run      a block per row and run of kRun tiles picks the entries of its own tokens out of the row's lists, streams the run and writes
+//   run      a block per row and run of 4 to 16 tiles picks the entries of its own tokens out of the row's lists, streams the run and writes
 //            the lists' logits over it.  One launch, everything written where it was just read; but every block reads all the lists
 //            and waits for them.  In place, and for lists that the row's table does not take.
 // Lists of more entries than the table takes are done with a counter for every token of a tile (run) or of as many tokens as the table
 // has slots (two, whole).
 // Bound: HBM, one read and one write of every logit (and 2 bits).  Measured: 256 rows x 131072 bf16 logits, U[0, 1024] generated tokens and
-// U[0, 64] biases each, 134.9 MB: two 28.4 us (31.2 over three sets of inputs in turn), run 48; the stream alone 24.3, a plain copy 22.3.
+// U[0, 64] biases each, 134.9 MB: two 28.4 us (31.2 over three sets of inputs in turn), run 39.5; the stream alone 24.3, a plain copy 22.3.
 // What the lists add is their latency, not their traffic: a table half full instead of a quarter 32.2 us, linear probing 38, 96 KB of
 // table instead of 48 (fewer blocks beside the stream's) 33.9, stream blocks of 4 or 16 tiles instead of 8 33.7 and 34.5.
-// 8 / 64 rows of that: two 6.6 / 11.2, run 6.3 / 13.9; 256 rows with 3500 generated tokens each 49 and 76.  8 rows x 3001: whole 4.4 us.
+// 8 / 64 rows of that: two 6.6 / 11.2, run 6.1 / 11.8; 256 rows with up to 3500 generated tokens each 49 and 76.  8 rows x 3001: whole 4.4 us.
 // Tried for the largest case: lists by warps beside the streaming ones of a block 40-59 us; a resident stream of 5 blocks an SM with the
 // lists beside it from the start 42; groups of rows streamed and followed by their lists 35-42; prefetching the lists into L2: no change.
 #include <cuda_bf16.h>
@@ -52,13 +52,13 @@ __host__ __device__ constexpr int64_t table_takes(int log2_slots) { return int64
 constexpr int kOwn = 8;                                    // list entries a thread keeps in registers
 constexpr int kLongHistory = kOwn * kListThreads;
 constexpr int kThreads = 256, kTile = kThreads * kVec;     // one launch: threads of a block, logits it takes at a time,
-constexpr int kRun = 4;                                    // tiles of it,
+constexpr int kLeastRun = 4, kMostRun = 16;                // tiles of it,
 __host__ __device__ constexpr int run_depth(bool f32) { return f32 ? 3 : 4; }   // of them in flight
 constexpr int run_bytes(bool f32) { return run_depth(f32) * kTile * (f32 ? 4 : 2); }
 constexpr int kLog2RunSlots = 11, kRunSlots = 1 << kLog2RunSlots;   // its table, at most half full; also a slot for every token of a tile
 constexpr int kHits = kRunSlots / 2 - 1;                   // list entries inside the run that the hash table takes
 constexpr int kRunOwn = (kHits + kThreads - 1) / kThreads;
-static_assert(kRunSlots == kTile && kRun * kTile <= 0x8000, "a slot for every token, 15 bits for a place in the run");
+static_assert(kRunSlots == kTile && kMostRun * kTile <= 0x8000, "a slot for every token, 15 bits for a place in the run");
 constexpr int kMarkTile = 131072;                          // tokens of one block's bitmap
 constexpr int kMarkThreads = 1024;
 constexpr int kMarkBatch = 8;
@@ -70,6 +70,7 @@ struct RulesArgs {
     int64_t row_stride, out_stride;
     int vocab;
     int log2_slots;       // of the largest table
+    int run;              // tiles of a block
 };
 
 template <bool kF32>
@@ -497,7 +498,7 @@ rules_lists_kernel(RulesArgs a)
     }
 }
 
-// One block per (row, run of kRun tiles).  A thread copies its own groups of the next kDepth - 1 tiles ahead of itself into shared memory
+// One block per (row, run of a.run tiles).  A thread copies its own groups of the next kDepth - 1 tiles ahead of itself into shared memory
 // (cp.async), so that enough bytes are on their way without registers or barriers.
 template <bool kInF32, bool kOutF32>
 __global__ void __launch_bounds__(kThreads, 4)
@@ -510,7 +511,7 @@ rules_run_kernel(RulesArgs a)
     __shared__ uint16_t hits[kHits];   // the run's list entries: token - c0, and whether it is a bias
     __shared__ int num_hits;
     const int row = blockIdx.y, tid = threadIdx.x;
-    const int c0 = blockIdx.x * (kRun * kTile), c1 = min(a.vocab, c0 + kRun * kTile), tiles = (c1 - c0 + kTile - 1) / kTile;
+    const int c0 = blockIdx.x * (a.run * kTile), c1 = min(a.vocab, c0 + a.run * kTile), tiles = (c1 - c0 + kTile - 1) / kTile;
     const int first = c0 + tid * kVec, whole = a.vocab & ~7;
     const void *in = row_of(a.logits, a.row_stride, row, kInF32);
     void *out = const_cast<void *>(row_of(a.out, a.out_stride, row, kOutF32));
@@ -595,7 +596,7 @@ rules_run_kernel(RulesArgs a)
     if (n_hits <= kHits) {
         // The thread that brings a token into the table reads its logit and bits at once and keeps them in registers.
         t.hashed = true;
-        t.log2_slots = max(6, 32 - __clz(2 * n_hits));
+        t.log2_slots = min(kLog2RunSlots, max(6, 33 - __clz(2 * n_hits)));   // a quarter full, where there is room
         t.r0 = c0; t.r1 = c1;
         t.clear(tid, kThreads);
         __syncthreads();
@@ -741,8 +742,17 @@ cudaError_t launch_rules(const RulesArgs &a, int rows, bool lists, bool long_lis
     }
     const size_t table = size_t(12) << a.log2_slots;
     if (lists && a.vocab <= kWholeRow) return launch_behind(whole, dim3(rows), kListThreads, table, st, a);
-    if (lists && (a.logits == a.out || long_lists))
-        return launch_behind(run, dim3((a.vocab + kRun * kTile - 1) / (kRun * kTile), rows), kThreads, run_bytes(kInF32), st, a);
+    if (lists && (a.logits == a.out || long_lists)) {
+        // Long runs, since every block reads all of its row's lists: 256 rows x 131072 in place take 44.5 us in runs of 4 tiles, 34.7 in 8 and
+        // 31.2 in 16.  But two or three blocks for every SM (64 rows: 14.0, 12.3, 13.2; 8 rows: 6.7, 8.2, 10.4), and no more entries in
+        // a run than its table takes (8192 generated tokens: 87, 97, 132).
+        RulesArgs b = a;
+        const int64_t said = a.r.history ? a.r.history_capacity : 0;
+        auto blocks = [&](int tiles) { return (a.vocab + tiles * kTile - 1) / (tiles * kTile); };
+        b.run = kLeastRun;
+        while (b.run < kMostRun && int64_t(blocks(2 * b.run)) * rows >= 3 * 148 && said * (2 * b.run * kTile) / a.vocab <= kHits / 2) b.run *= 2;
+        return launch_behind(run, dim3(blocks(b.run), rows), kThreads, run_bytes(kInF32), st, b);
+    }
     const dim3 tiles((a.vocab + kStreamRun * kStreamTile - 1) / (kStreamRun * kStreamTile), rows);
     cudaError_t e = launch_behind(stream, tiles, kStreamThreads, 0, st, a);
     if (e == cudaSuccess && lists) e = launch_behind(part, dim3(rows), kListThreads, table, st, a);
@@ -781,7 +791,7 @@ extern "C" psa_status_t psa_process_logits(const void *logits, int32_t logits_dt
     if ((r.prompt_bits && r.prompt_row_words < words) || (r.mask_bits && r.mask_row_words < words))
         return set_last_error(PSA_ERR_INVALID_ARG, "bitmap rows must hold at least ceil(vocab / 32) words");
     const bool lists = (r.history && r.history_capacity > 0) || (r.bias_indptr && r.num_biases > 0);
-    psa::RulesArgs a{r, logits, out, row_stride, out_row_stride, vocab, 0};
+    psa::RulesArgs a{r, logits, out, row_stride, out_row_stride, vocab, 0, 0};
     // A table as small as the lists allow, since it decides how many of their blocks fit beside the stream's (256 rows x 131072, up
     // to 1088 entries a row: 96 KB 33.9 us, 48 KB 31.2).  For whole rows it takes all entries there can be or has a slot for every token; else it
     // takes four times the mean number of biases, and rows with more are done in ranges.
