@@ -800,12 +800,13 @@ extern "C" psa_status_t psa_process_logits(const void *logits, int32_t logits_dt
     a.log2_slots = psa::kLog2Few;
     while (a.log2_slots < psa::kLog2Many && most > psa::table_takes(a.log2_slots)) ++a.log2_slots;
     static_assert(psa::kWholeRow <= 1 << psa::kLog2Many, "a slot for every token");
+    const bool long_lists = most > psa::table_takes(psa::kLog2Many);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     cudaError_t e;
     if (logits_dtype == PSA_OUT_F32)
-        e = out_dtype == PSA_OUT_F32 ? psa::launch_rules<true, true>(a, num_rows, lists, most > psa::table_takes(psa::kLog2Many), st) : psa::launch_rules<true, false>(a, num_rows, lists, most > psa::table_takes(psa::kLog2Many), st);
+        e = out_dtype == PSA_OUT_F32 ? psa::launch_rules<true, true>(a, num_rows, lists, long_lists, st) : psa::launch_rules<true, false>(a, num_rows, lists, long_lists, st);
     else
-        e = out_dtype == PSA_OUT_F32 ? psa::launch_rules<false, true>(a, num_rows, lists, most > psa::table_takes(psa::kLog2Many), st) : psa::launch_rules<false, false>(a, num_rows, lists, most > psa::table_takes(psa::kLog2Many), st);
+        e = out_dtype == PSA_OUT_F32 ? psa::launch_rules<false, true>(a, num_rows, lists, long_lists, st) : psa::launch_rules<false, false>(a, num_rows, lists, long_lists, st);
     if (e != cudaSuccess) return set_last_error(PSA_ERR_CUDA, std::string("logits launch: ") + cudaGetErrorString(e));
     return PSA_OK;
 }
