@@ -16,8 +16,8 @@
 //   * outputs: V codes come through ldmatrix.trans, so that a register holds one unit (4 channels) of two neighbouring tokens.
 //     Rows 0-7 of a product take whole bytes (even code + 16 * odd code, still a subnormal whole number), rows 8-15 the upper
 //     nibbles alone; the even channel is their difference, taken once at the end.  4 instructions per 8 codes.
-//   * the offset term of the scores is one and a half more products, parameters x (group sums of q, split into three bf16 numbers:
-//     2^-24 relative); the offset term of the outputs is one more product, parameters^T x p.
+//   * the offset term of the scores is one and a half more products (one for D = 64), parameters x (group sums of q, split into three bf16
+//     numbers: 2^-24 relative); the offset term of the outputs is one more product, parameters^T x p.
 //   * rounding: p * s and p are rounded to bf16 (2^-8 relative at most, zero mean) before they meet the codes and the offsets.  With
 //     codes centred on 8 both terms stay as small as the values themselves; uncentred, their errors would not cancel as the
 //     terms do.  The centring is a product with a constant -8 on the same rounded operand, hence exact.
@@ -26,6 +26,7 @@
 // Measured: 256 samples x U[0, 4096] tokens x 8 heads of 128 channels, 671 MB: 118 us (5.7 TB/s, 0.87 of the measured copy rate) at
 // 1965 MHz; the copies alone take 105, the arithmetic alone 110 (284 instructions per page and warp: issue slots 60 % busy, ALU 50 %,
 // tensor pipe 45 %).  In long loops under the power limit the clock falls to 1630 MHz and the time follows it, to 141 us.
+// The same with heads of 64 channels, 350 MB: 76 us (4.6 TB/s, 0.70 of the copy rate): a page has half the bytes and more than half the instructions.
 // Four blocks an SM of 126 registers: five or six (96, 80 registers) spill, 137 and 184 us; two pages at a time 120-124; 2 or 8 warps a
 // block 121-124; q re-read from shared memory 121-126; 3 or 5 stages 120-121; one bulk copy a page with a barrier of its own 126; packed
 // two-wide fp32 operations 118-119.
@@ -209,15 +210,16 @@ suffix_kv4_kernel(const __nv_bfloat16 *__restrict__ q, const unsigned char *__re
             gsum[g] = t * scale_log2;
         }
         // parameter row of a token, as pairs: D = 128: {s0 s1} {s2 s3} {b0 b1} {b2 b3};  D = 64: {s0 s1} {b0 b1} of K, then of V
-        constexpr int kFirst = D == 128 ? 2 : 1;
 #pragma unroll
-        for (int i = 0; i < NG / 2; ++i)
-            if (c4 == kFirst + i) {
-                qs0 = pack_bf16(gsum[2 * i], gsum[2 * i + 1]);
-                const float r0 = gsum[2 * i] - lo_f32(qs0), r1 = gsum[2 * i + 1] - hi_f32(qs0);
-                qs1 = pack_bf16(r0, r1);
-                qs2 = pack_bf16(r0 - lo_f32(qs1), r1 - hi_f32(qs1));
-            }
+        for (int i = 0; i < NG / 2; ++i) {
+            const uint32_t part0 = pack_bf16(gsum[2 * i], gsum[2 * i + 1]);
+            const float r0 = gsum[2 * i] - lo_f32(part0), r1 = gsum[2 * i + 1] - hi_f32(part0);
+            const uint32_t part1 = pack_bf16(r0, r1), part2 = pack_bf16(r0 - lo_f32(part1), r1 - hi_f32(part1));
+            if (D == 128 && c4 == 2 + i) { qs0 = part0; qs1 = part1; qs2 = part2; }
+            // K's half of the row twice along k, and again in the second half of k: the three parts stand in one product
+            if (D == 64 && c4 == 1) { qs0 = part0; qs1 = part2; }
+            if (D == 64 && c4 == 3) qs0 = part1;
+        }
     }
     const float score_scale = scale_log2 * kUnscaleEven;
 
@@ -243,8 +245,9 @@ suffix_kv4_kernel(const __nv_bfloat16 *__restrict__ q, const unsigned char *__re
 #pragma unroll
     for (int p = 0; p < NG / 2; ++p) code_at[p] = C::chunk(mtok, 2 * p + (mat >> 1));
     // parameter rows: K's as A rows (tokens 0-7, 8-15) with both halves of k alike; V's transposed, tokens 0-7 and 8-15 along k, the
-    // second half of the rows a copy that nobody reads
-    const uint32_t pk_at = C::kParamOff + (lane & 15) * 16;
+    // second half of the rows a copy that nobody reads.  D = 64: V's half of a row must stay out of the scores, since a zero in q would not
+    // keep a NaN among its parameters out; each thread reads its two registers of K's half.
+    const uint32_t pk_at = C::kParamOff + (D == 128 ? (lane & 15) * 16 : u * 16 + (c4 & 1) * 4);
     const uint32_t pv_at = C::params(D == 128 ? 1 : 0, 0) + ((mat >> 1) * 8 + mrow) * 16;
     // the centring operand - (8 + 16 * 8) for bytes, - 16 * 8 for upper nibbles, kept in registers
     uint32_t centre[4];
@@ -274,10 +277,15 @@ suffix_kv4_kernel(const __nv_bfloat16 *__restrict__ q, const unsigned char *__re
         float x[4];
         {
             {
-                uint32_t a[4];
-                ldmatrix_x4(cell + pk_at, a);
-                mma_bf16_from(x, a[0], a[1], a[2], a[3], qs0, qs1, base);
-                mma_bf16_k8(x, a[0], a[1], qs2);
+                if constexpr (D == 128) {
+                    uint32_t a[4];
+                    ldmatrix_x4(cell + pk_at, a);
+                    mma_bf16_from(x, a[0], a[1], a[2], a[3], qs0, qs1, base);
+                    mma_bf16_k8(x, a[0], a[1], qs2);
+                } else {
+                    const uint32_t a0 = lds32(cell + pk_at), a1 = lds32(cell + pk_at + 128);
+                    mma_bf16_from(x, a0, a1, a0, a1, qs0, qs1, base);
+                }
             }
             float acc[NG][4];
 #pragma unroll
