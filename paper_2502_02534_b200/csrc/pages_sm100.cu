@@ -208,6 +208,9 @@ __device__ __forceinline__ int lane_find(const int32_t *offsets, int lo, int hi,
     return lo;
 }
 
+// Pages of n >= 0 tokens; n may be the largest 32-bit number.
+__device__ __forceinline__ int pages_of(int n) { return n / kPageSize + (n % kPageSize != 0); }
+
 // Page of entry j of a sample's list (record rec, list at e_first); entries from `fresh` on come off the stack.
 __device__ __forceinline__ int page_of(const PageTableArgs &a, int j, int fresh, int2 rec, int e_first, int avail)
 {
@@ -251,11 +254,11 @@ __device__ void spread_tokens(const PageTableArgs &a, const Tables &tab, long lo
                     // the pages of up to kSpread tokens are fetched at once, one a lane, and go round by shuffles.  32 tokens further
                     // on are two pages further on, at the same place in the page.
                     const int len = stop - t, pos0 = rec.x + (t - t_first), j0 = pos0 / kPageSize, j1 = (pos0 + len - 1) / kPageSize;
-                    const int fresh = (rec.x + kPageSize - 1) / kPageSize, j = j0 + lane;
+                    const int fresh = pages_of(rec.x), j = j0 + lane;
                     const int page = j <= j1 ? page_of(a, j, fresh, rec, e_first, avail) : 0;
                     if (!a.build && j <= j1 && j >= fresh && j * kPageSize >= pos0)   // the piece that holds a fresh page's first token files it
                         a.page_indices[(long long)e_first + j] = page;
-                    const int from = (pos0 % kPageSize + lane) / kPageSize, in_page = (pos0 + lane) % kPageSize;
+                    const int in_first = pos0 % kPageSize + lane, from = in_first / kPageSize, in_page = in_first % kPageSize;
                     int64_t *to = a.slot_map + t + lane;
                     if (len == kSpread && !__any_sync(0xffffffffu, page < 0)) {   // the middle of a long sample
 #pragma unroll
@@ -282,7 +285,7 @@ __device__ void spread_tokens(const PageTableArgs &a, const Tables &tab, long lo
                         const int s = lane_find(tab.token_indptr, s_lo, s_hi + 1, i);
                         const int2 rec = tab.rec[s];
                         if (rec.y >= 0) {
-                            const int pos = rec.x + (i - tab.token_indptr[s]), j = pos / kPageSize, fresh = (rec.x + kPageSize - 1) / kPageSize;
+                            const int pos = rec.x + (i - tab.token_indptr[s]), j = pos / kPageSize, fresh = pages_of(rec.x);
                             const int e_first = tab.page_indptr[s];
                             in_page[k] = pos % kPageSize;
                             page[k] = page_of(a, j, fresh, rec, e_first, avail);
@@ -315,7 +318,7 @@ __device__ void spread_entries(const PageTableArgs &a, const Tables &tab, long l
     auto entry = [&](int e, int s) {
         const int2 rec = tab.rec[s];
         const int j = e - tab.page_indptr[s], tokens = tab.token_indptr[s + 1] - tab.token_indptr[s];
-        return rec.y >= 0 && j < (tokens + kPageSize - 1) / kPageSize ? a.free_pages[avail - 1 - (rec.y + j)] : -1;
+        return rec.y >= 0 && j < pages_of(tokens) ? a.free_pages[avail - 1 - (rec.y + j)] : -1;
     };
     int e = int(e0);
     if (e < live) {
