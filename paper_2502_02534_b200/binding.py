@@ -1,6 +1,7 @@
 from __future__ import annotations
 
 import ctypes
+from contextlib import nullcontext
 from ctypes import POINTER, c_char_p, c_float, c_int32, c_int64, c_size_t, c_void_p
 from dataclasses import dataclass
 from pathlib import Path
@@ -191,6 +192,40 @@ def _stream_ptr(stream):
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
+def _on(stream):
+    """The context in which what a call on `stream` needs is allocated (None: the current stream).  A block of the caching allocator belongs
+    to the stream it was allocated on: one of the current stream's may still be written by work enqueued there before it was freed,
+    which a call on another stream does not wait for."""
+    if stream is None:
+        return nullcontext()
+    import torch
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+    return torch.cuda.stream(stream)
+
+
+def _new(shape, dtype, device, stream):
+    """A tensor that a call on `stream` writes and returns: allocated for that stream, and not given back to it before the current stream's
+    use of it is over."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with _on(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if t.is_cuda:
+        t.record_stream(torch.cuda.current_stream(t.device))
+    return t
+
+
+def _scratch(nbytes, like, stream):
+    """A scratch tensor for one call on `stream` (None: the current one)."""
+    import torch
+    if stream is None:
+        return torch.empty(int(nbytes), dtype=torch.uint8, device=like.device)
+    with _on(stream):
+        return torch.empty(int(nbytes), dtype=torch.uint8, device=like.device)
+
+
 def _i32(a):
     return np.ascontiguousarray(np.asarray(a, dtype=np.int32))
 
@@ -279,7 +314,8 @@ class Plan:
         """Allocate (through torch) or adopt a device workspace and upload the work lists into it."""
         import torch
         if workspace is None:
-            workspace = torch.empty(max(256, self.workspace_bytes), dtype=torch.uint8, device="cuda")
+            with _on(stream):
+                workspace = torch.empty(max(256, self.workspace_bytes), dtype=torch.uint8, device="cuda")
         _check(library().psa_plan_bind_workspace(self._h, _ptr(workspace), workspace.numel(), _stream_ptr(stream)))
         self.workspace = workspace
         return workspace
@@ -408,9 +444,9 @@ def sample_tokens_at(logits, temperature, seeds, step_device, advance=1, tokens=
     if logits.stride(1) != 1:
         raise ValueError("logits must be contiguous along the vocabulary")
     if tokens is None:
-        tokens = torch.empty(B, dtype=torch.int32, device=logits.device)
+        tokens = _new(B, torch.int32, logits.device, stream)
     if scratch is None:
-        scratch = torch.empty(max(8, int(lib.psa_sample_scratch_bytes(B))), dtype=torch.uint8, device=logits.device)
+        scratch = _scratch(max(8, int(lib.psa_sample_scratch_bytes(B))), logits, stream)
     _check(lib.psa_sample_tokens_at(_ptr(logits), dtype, logits.stride(0), B, V, _ptr(temperature), _ptr(seeds), _ptr(step_device),
                                     int(advance), _ptr(tokens), _ptr(scratch), scratch.numel(), _stream_ptr(stream)))
     return tokens
@@ -426,10 +462,10 @@ def sample_tokens(logits, temperature, seeds, step, tokens=None, scratch=None, *
     if logits.stride(1) != 1:
         raise ValueError("logits must be contiguous along the vocabulary")
     if tokens is None:
-        tokens = torch.empty(B, dtype=torch.int32, device=logits.device)
+        tokens = _new(B, torch.int32, logits.device, stream)
     need = int(lib.psa_sample_scratch_bytes(B))
     if scratch is None:
-        scratch = torch.empty(max(8, need), dtype=torch.uint8, device=logits.device)
+        scratch = _scratch(max(8, need), logits, stream)
     _check(lib.psa_sample_tokens(_ptr(logits), dtype, logits.stride(0), B, V, _ptr(temperature), _ptr(seeds), int(step) & 0xFFFFFFFF,
                                  _ptr(tokens), _ptr(scratch), scratch.numel(), _stream_ptr(stream)))
     return tokens
@@ -440,9 +476,7 @@ def attn_task(task, q, k, v, sm_scale, *, stream=None):
     import torch
     R, D = q.shape
     M = k.shape[0]
-    out = torch.empty((R, D), dtype=torch.float32, device=q.device)
-    m = torch.empty(R, dtype=torch.float32, device=q.device)
-    l = torch.empty(R, dtype=torch.float32, device=q.device)
+    out, m, l = (_new(shape, torch.float32, q.device, stream) for shape in ((R, D), R, R))  # noqa: E741
     _check(library().psa_attn_task(int(task), _ptr(q), _ptr(k) if M else None, _ptr(v) if M else None, R, M, D, float(sm_scale),
                                    _ptr(out), _ptr(m), _ptr(l), _stream_ptr(stream)))
     return out, m, l
@@ -490,15 +524,6 @@ def _native():
         module.attach(str(_LIB_PATH))
         _calls = module
     return _calls
-
-
-def _scratch(nbytes, like, stream):
-    """A scratch tensor for one call on `stream` (None: the current one)."""
-    import torch
-    t = torch.empty(int(nbytes), dtype=torch.uint8, device=like.device)
-    if stream is not None and t.is_cuda:      # allocated on the current stream, used on another one: not to be reused before that is done
-        t.record_stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
-    return t
 
 
 def _status_tensor(status):
@@ -625,8 +650,7 @@ def process_logits(logits, out=None, *, repetition=None, frequency=None, presenc
     mask_rows [R] int32; bias_indptr [R+1], bias_ids int32 and bias_values f32.  Returns out."""
     rows, vocab = logits.shape
     if out is None:
-        import torch
-        out = torch.empty((rows, (vocab + 7) // 8 * 8), dtype=logits.dtype, device=logits.device)[:, :vocab]
+        out = _new((rows, (vocab + 7) // 8 * 8), logits.dtype, logits.device, stream)[:, :vocab]
     rc = (_calls or _native()).process_logits(logits, out, repetition, frequency, presence, history, history_lens, prompt_bits, prompt_rows, bias_indptr,
                                               bias_ids, bias_values, mask_bits, mask_rows, stream)
     if rc:
@@ -638,7 +662,7 @@ def mark_tokens(ids, indptr, vocab, bits=None, *, stream=None):
     """psa_mark_tokens: bitmaps [rows, >= ceil(vocab / 32)] int32 of the tokens in ids[indptr[m] .. indptr[m + 1]).  Returns bits."""
     if bits is None:
         import torch
-        bits = torch.empty((max(0, indptr.numel() - 1), (int(vocab) + 31) // 32), dtype=torch.int32, device=ids.device)
+        bits = _new((max(0, indptr.numel() - 1), (int(vocab) + 31) // 32), torch.int32, ids.device, stream)
     rc = (_calls or _native()).mark_tokens(ids, indptr, vocab, bits, stream)
     if rc:
         _check(rc)
