@@ -272,9 +272,14 @@ class Plan:
             handle = c_void_p()
             _check(library().psa_plan_create_kv4(self._h, ctypes.byref(handle)))
             plan = Plan.__new__(Plan)
-            plan.__dict__.update(self.__dict__, _h=handle, workspace=None, _is_kv4=True)
+            plan.__dict__.update(self.__dict__, _h=handle, workspace=None, _is_kv4=True, _prefix_tokens=self._prefix_tokens_read())
             self._kv4 = plan
         return self._kv4
+
+    def _prefix_tokens_read(self) -> int:
+        """Packed prefix tokens up to the last one that a sample attends over."""
+        samples, lens = self.groups[1:] if hasattr(self, "groups") else (self.n_samples, self.prefix_lens)
+        return int(np.cumsum(lens, dtype=np.int64)[(samples > 0) & (lens > 0)].max(initial=0))
 
     def __del__(self):
         if getattr(self, "_h", None):
@@ -609,7 +614,8 @@ def load_kv4(pool, slot_map, out_k, out_v, *, status=None, stream=None):
 def decode_kv4(plan: Plan, q, prefix_k, prefix_v, pool, page_indptr, page_indices, suffix_lens, out, lse, *, prefix_strides=None,
                stream=None, stage="all"):
     """psa_decode_kv4 (or one of its stages): decode with the samples' own tokens in a 4-bit pool [pages, Hkv, kv4_cell_bytes(D)]
-    uint8.  Everything else as for decode; the work lists and the workspace are those of plan.for_kv4(), made at the first call (which
+    uint8.  prefix_k and prefix_v are [tokens, Hkv, D] of any token and head stride (prefix_strides: those of the packed array in their
+    storage, for tensors of another form).  Everything else as for decode; the work lists and the workspace are those of plan.for_kv4(), made at the first call (which
     therefore comes before any stream capture)."""
     plan = plan._kv4 or plan.for_kv4()
     if stage != "all":
@@ -619,9 +625,10 @@ def decode_kv4(plan: Plan, q, prefix_k, prefix_v, pool, page_indptr, page_indice
             raise ValueError("pool must be on the current CUDA device")
         plan.bind_workspace(stream=stream)
     head_dim = plan.head_dim
-    s0, s1 = (plan.num_kv_heads * head_dim, head_dim) if prefix_strides is None else prefix_strides
-    rc = (_calls or _native()).decode_kv4(plan._h.value, plan.suffix_len_bounds.size, plan.num_q_heads, plan.num_kv_heads, head_dim, plan.out_dtype, q, prefix_k,
-                                          prefix_v, s0, s1, pool, page_indptr, page_indices, suffix_lens, out, lse, plan.workspace, stream)
+    s0, s1 = (None, None) if prefix_strides is None else prefix_strides
+    rc = (_calls or _native()).decode_kv4(plan._h.value, plan.suffix_len_bounds.size, plan.num_q_heads, plan.num_kv_heads, head_dim, plan.out_dtype,
+                                          plan._prefix_tokens, q, prefix_k, prefix_v, s0, s1, pool, page_indptr, page_indices, suffix_lens, out, lse,
+                                          plan.workspace, stream)
     if rc:
         _check(rc)
 
@@ -629,6 +636,8 @@ def decode_kv4(plan: Plan, q, prefix_k, prefix_v, pool, page_indptr, page_indice
 def _decode_kv4_stage(plan, q, prefix_k, prefix_v, pool, page_indptr, page_indices, suffix_lens, out, lse, prefix_strides, stream, stage):
     """One stage of a 4-bit step, for tests and per-kernel timing."""
     if stage in ("prefix", "merge"):
+        if prefix_strides is None and prefix_k is not None and prefix_k.dim() == 3:      # a dimension of one element has no stride of its own
+            prefix_strides = [st if n > 1 else d for st, n, d in zip(prefix_k.stride(), prefix_k.shape, default_prefix_strides(plan))]
         return decode(plan, q, prefix_k, prefix_v, None, None, page_indptr, page_indices, suffix_lens, out, lse, prefix_strides=prefix_strides,
                       stream=stream, stage=stage)
     if stage != "suffix":

@@ -233,36 +233,63 @@ psa_status_t load_kv4(PyObject *const *args, Py_ssize_t given)
                         c.kv_strides, c.status, c.stream);
 }
 
-// plan handle, samples, query heads, KV heads, head dim, f32 output?, q, prefix_k, prefix_v, prefix stride 0, prefix stride 1, pool, page_indptr,
-// page_indices, suffix_lens, out, lse, workspace, stream
+// The shared prefix, bf16: K and V with the same token and head stride (elements), `tokens` rows of `heads` x `dim` of each inside its storage.
+struct Prefix {
+    const void *k = nullptr, *v = nullptr;
+    int64_t strides[2];
+    // tensors at `at` and `at` + 1, strides behind them (None: the tensors' own where they are [tokens, heads, dim], else contiguous)
+    Prefix(Call &c, int at, int64_t tokens, int64_t heads, int64_t dim)
+    {
+        const bool own = c.none(at + 2);
+        strides[0] = own ? heads * dim : c.integer(at + 2);
+        strides[1] = own ? dim : c.integer(at + 3);
+        const at::Tensor *first = nullptr;
+        for (int i = 0; i < 2; ++i) {
+            if (c.none(at + i)) continue;
+            const char *name = i ? "prefix_v" : "prefix_k";
+            const at::Tensor &t = c.tensor(at + i, name);
+            if (t.scalar_type() != at::kBFloat16) throw Refused("prefix_k and prefix_v must be torch.bfloat16");
+            (i ? v : k) = t.data_ptr();
+            if (tokens == 0) continue;   // nothing is read
+            if (own) {
+                int64_t mine[2] = {heads * dim, dim};
+                if (t.dim() == 3 && t.size(1) == heads && t.size(2) == dim) outer_strides(t, dim, name, mine);
+                else if (!t.is_contiguous()) throw Refused(std::string(name) + " must be [tokens, heads, head_dim] or contiguous, unless prefix_strides are given");
+                if (t.numel() < tokens * heads * dim) throw Refused(std::string(name) + " must hold at least " + std::to_string(tokens) + " tokens");
+                if (first && (mine[0] != strides[0] || mine[1] != strides[1])) throw Refused("prefix_k and prefix_v must have the same strides");
+                strides[0] = mine[0]; strides[1] = mine[1];
+                first = &t;
+            }
+            const __int128 last = __int128(tokens - 1) * strides[0] + __int128(heads - 1) * strides[1] + dim;   // the library refuses strides below 1
+            if (last > int64_t(t.storage().nbytes() / 2) - t.storage_offset())
+                throw Refused(std::string(name) + " must hold at least " + std::to_string(tokens) + " tokens at these strides");
+        }
+    }
+};
+
+// plan handle, samples, query heads, KV heads, head dim, f32 output?, prefix tokens that are read, q, prefix_k, prefix_v, prefix stride 0,
+// prefix stride 1, pool, page_indptr, page_indices, suffix_lens, out, lse, workspace, stream
 psa_status_t decode_kv4(PyObject *const *args, Py_ssize_t given)
 {
-    Call c(args, given, 19);
+    Call c(args, given, 20);
     const auto *plan = reinterpret_cast<const psa_plan_t *>(PyLong_AsVoidPtr(args[0]));
     const int64_t rows = c.integer(1), heads = c.integer(2), kv = c.integer(3), dim = c.integer(4);
-    const at::Tensor &pool = c.tensor(11, "pool");
+    const at::Tensor &pool = c.tensor(12, "pool");
     if (pool.scalar_type() != at::kByte || pool.dim() != 3 || pool.size(1) != kv)
         throw Refused("pool must be uint8 [pages, num_kv_heads, kv4_cell_bytes(head_dim)]");
     int64_t pool_strides[2];
     outer_strides(pool, 20 * dim, "pool", pool_strides);
-    const void *q = c.needed(6, at::kBFloat16, "q", rows * heads * dim);
-    const void *prefix[2] = {nullptr, nullptr};
-    for (int i = 0; i < 2; ++i)   // any strides: not necessarily contiguous
-        if (!c.none(7 + i)) {
-            const at::Tensor &t = c.tensor(7 + i, i ? "prefix_v" : "prefix_k");
-            if (t.scalar_type() != at::kBFloat16) throw Refused("prefix_k and prefix_v must be torch.bfloat16");
-            prefix[i] = t.data_ptr();
-        }
-    const int64_t prefix_strides[2] = {c.integer(9), c.integer(10)};
-    const auto *indptr = c.needed<int32_t>(12, at::kInt, "page_indptr", rows + 1);
-    const auto *indices = c.needed<int32_t>(13, at::kInt, "page_indices");
-    const auto *lens = c.needed<int32_t>(14, at::kInt, "suffix_lens", rows);
-    void *out = c.needed(15, c.integer(5) ? at::kFloat : at::kBFloat16, "out", rows * heads * dim);
-    auto *lse = c.needed<float>(16, at::kFloat, "lse", rows * heads);
-    void *workspace = c.needed(17, at::kByte, "workspace");
-    void *stream = c.stream(18);
-    return api.decode_kv4(plan, q, prefix[0], prefix[1], prefix_strides, pool.data_ptr(), pool_strides, indptr, indices, lens, out, lse, workspace,
-                          size_t(c.numel(17)), stream);
+    const void *q = c.needed(7, at::kBFloat16, "q", rows * heads * dim);
+    const Prefix prefix(c, 8, c.integer(6), kv, dim);
+    const auto *indptr = c.needed<int32_t>(13, at::kInt, "page_indptr", rows + 1);
+    const auto *indices = c.needed<int32_t>(14, at::kInt, "page_indices");
+    const auto *lens = c.needed<int32_t>(15, at::kInt, "suffix_lens", rows);
+    void *out = c.needed(16, c.integer(5) ? at::kFloat : at::kBFloat16, "out", rows * heads * dim);
+    auto *lse = c.needed<float>(17, at::kFloat, "lse", rows * heads);
+    void *workspace = c.needed(18, at::kByte, "workspace");
+    void *stream = c.stream(19);
+    return api.decode_kv4(plan, q, prefix.k, prefix.v, prefix.strides, pool.data_ptr(), pool_strides, indptr, indices, lens, out, lse, workspace,
+                          size_t(c.numel(18)), stream);
 }
 
 int32_t dtype_code(const at::Tensor &t, const char *name)
