@@ -265,7 +265,8 @@ class Plan:
 
     def for_kv4(self) -> "Plan":
         """The plan of the same problem whose pieces are sized for a 4-bit cache (psa_plan_create_kv4), with a workspace of its own.
-        decode_kv4 uses it in place of this one; it is made once and kept."""
+        decode_kv4 uses it in place of this one; it is made once and kept.  `plan.for_kv4().bind_workspace()` makes it ready for a capture or
+        gives it a workspace of the caller's."""
         if self._is_kv4:
             return self
         if self._kv4 is None:
@@ -615,15 +616,16 @@ def decode_kv4(plan: Plan, q, prefix_k, prefix_v, pool, page_indptr, page_indice
                stream=None, stage="all"):
     """psa_decode_kv4 (or one of its stages): decode with the samples' own tokens in a 4-bit pool [pages, Hkv, kv4_cell_bytes(D)]
     uint8.  prefix_k and prefix_v are [tokens, Hkv, D] of any token and head stride (prefix_strides: those of the packed array in their
-    storage, for tensors of another form).  Everything else as for decode; the work lists and the workspace are those of plan.for_kv4(), made at the first call (which
-    therefore comes before any stream capture)."""
+    storage, for tensors of another form).  Everything else as for decode; the work lists
+    and the workspace are those of plan.for_kv4(), made at the first call unless plan.for_kv4().bind_workspace() has been called before: one of
+    the two has to come before a stream capture."""
     plan = plan._kv4 or plan.for_kv4()
     if stage != "all":
         return _decode_kv4_stage(plan, q, prefix_k, prefix_v, pool, page_indptr, page_indices, suffix_lens, out, lse, prefix_strides, stream, stage)
     if plan.workspace is None:
         if not pool.is_cuda:
             raise ValueError("pool must be on the current CUDA device")
-        plan.bind_workspace(stream=stream)
+        _bind_kv4(plan, stream)
     head_dim = plan.head_dim
     s0, s1 = (None, None) if prefix_strides is None else prefix_strides
     rc = (_calls or _native()).decode_kv4(plan._h.value, plan.suffix_len_bounds.size, plan.num_q_heads, plan.num_kv_heads, head_dim, plan.out_dtype,
@@ -633,9 +635,21 @@ def decode_kv4(plan: Plan, q, prefix_k, prefix_v, pool, page_indptr, page_indice
         _check(rc)
 
 
+def _bind_kv4(plan, stream):
+    """Bind a workspace to a 4-bit plan outside a capture.  Inside one the upload would run at every replay instead of now, out of memory that
+    the plan may have freed by then, and an eager call before the first replay would find no work lists."""
+    import torch
+    with _on(stream):
+        if torch.cuda.is_current_stream_capturing():
+            raise ValueError("the 4-bit plan has no workspace yet: call plan.for_kv4().bind_workspace(), or decode_kv4 once, before the capture")
+    plan.bind_workspace(stream=stream)
+
+
 def _decode_kv4_stage(plan, q, prefix_k, prefix_v, pool, page_indptr, page_indices, suffix_lens, out, lse, prefix_strides, stream, stage):
     """One stage of a 4-bit step, for tests and per-kernel timing."""
     if stage in ("prefix", "merge"):
+        if plan.workspace is None:
+            _bind_kv4(plan, stream)
         if prefix_strides is None and prefix_k is not None and prefix_k.dim() == 3:      # a dimension of one element has no stride of its own
             prefix_strides = [st if n > 1 else d for st, n, d in zip(prefix_k.stride(), prefix_k.shape, default_prefix_strides(plan))]
         return decode(plan, q, prefix_k, prefix_v, None, None, page_indptr, page_indices, suffix_lens, out, lse, prefix_strides=prefix_strides,
@@ -645,7 +659,7 @@ def _decode_kv4_stage(plan, q, prefix_k, prefix_v, pool, page_indptr, page_indic
     if pool.dim() != 3 or pool.element_size() != 1 or pool.stride(2) != 1 or not pool.is_cuda:
         raise ValueError("pool must be uint8 [pages, num_kv_heads, kv4_cell_bytes(head_dim)] on the current CUDA device")
     if plan.workspace is None:
-        plan.bind_workspace(stream=stream)
+        _bind_kv4(plan, stream)
     _check(library().psa_decode_suffix_kv4(plan.handle, _ptr(q), _ptr(pool), _strides(pool.stride()[:2], 2), _ptr(page_indptr), _ptr(page_indices),
                                            _ptr(suffix_lens), _ptr(plan.workspace), plan.workspace.numel(), _stream_ptr(stream)))
 
