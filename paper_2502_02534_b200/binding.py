@@ -594,7 +594,7 @@ def kv4_cell_bytes(head_dim) -> int:
 
 
 def store_kv4(new_k, new_v, slot_map, pool, *, status=None, stream=None):
-    """psa_store_kv4: quantise new_k / new_v [T, Hkv, D] bf16 (any token and head stride) into the slots of a 4-bit pool
+    """psa_store_kv4: quantise new_k / new_v [T, Hkv, D] bf16 (any token and head stride, the same for both) into the slots of a 4-bit pool
     [pages, Hkv, kv4_cell_bytes(D)] uint8."""
     if status is not None:
         status = _status_tensor(status)

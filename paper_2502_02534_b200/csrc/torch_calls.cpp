@@ -204,7 +204,7 @@ struct Kv4Call {
         Call c(args, given, 6);
         k = &c.tensor(0, names);
         v = &c.tensor(1, names);
-        if (k->dim() != 3 || k->scalar_type() != at::kBFloat16 || v->scalar_type() != at::kBFloat16 || k->sizes() != v->sizes() || k->strides() != v->strides())
+        if (k->dim() != 3 || k->scalar_type() != at::kBFloat16 || v->scalar_type() != at::kBFloat16 || k->sizes() != v->sizes())
             throw Refused(std::string(names) + " must be bf16 [tokens, heads, head_dim] of the same shape and strides");
         tokens = k->size(0);
         if (k->size(1) > 0x7fffffff || k->size(2) > 0xffff) throw Refused(std::string(names) + " are too large");
@@ -214,7 +214,10 @@ struct Kv4Call {
         pool = &c.tensor(3, "pool");
         if (pool->scalar_type() != at::kByte || pool->dim() != 3 || pool->size(1) != heads)
             throw Refused("pool must be uint8 [pages, heads, kv4_cell_bytes(head_dim)]");
+        int64_t v_strides[2];
         outer_strides(*k, dim, names, kv_strides);
+        outer_strides(*v, dim, names, v_strides);
+        if (tokens > 0 && (kv_strides[0] != v_strides[0] || kv_strides[1] != v_strides[1])) throw Refused(std::string(names) + " must have the same strides");
         outer_strides(*pool, 20 * dim, "pool", pool_strides);
         status = c.status(4);
         stream = c.stream(5);
