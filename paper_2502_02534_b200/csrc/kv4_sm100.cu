@@ -316,6 +316,7 @@ psa_status_t check(const Kv4Args &a, const void *k, const void *v, const int64_t
         return set_last_error(PSA_ERR_INVALID_ARG, "null K/V cache argument");
     if (misaligned(k, 16) || misaligned(v, 16) || misaligned(a.pool, 16))
         return set_last_error(PSA_ERR_INVALID_ARG, "K, V and the pool must be 16-byte aligned");
+    if (misaligned(a.status, 4)) return set_last_error(PSA_ERR_INVALID_ARG, "the status word must be 4-byte aligned");
     for (int i = 0; i < 2; ++i) {
         if (kv_strides[i] <= 0 || kv_strides[i] % 8) return set_last_error(PSA_ERR_INVALID_ARG, "K/V strides must be positive multiples of 8 elements");
         if (pool_strides[i] < 20 * head_dim || pool_strides[i] % 16)

@@ -439,6 +439,7 @@ psa_status_t run(PageTableArgs a, void *scratch, size_t scratch_bytes, void *cud
     if (!a.free_pages || !a.free_count || !a.free_count_out || !a.page_indptr || !a.token_indptr || (a.max_tokens > 0 && !a.slot_map) ||
         (a.num_entries > 0 && !a.page_indices) || (a.num_samples > 0 && !a.new_lens) || (!a.build && a.num_samples > 0 && !a.held))
         return set_last_error(PSA_ERR_INVALID_ARG, "null page table argument");
+    if (reinterpret_cast<uintptr_t>(a.status) % 4) return set_last_error(PSA_ERR_INVALID_ARG, "the status word must be 4-byte aligned");
     if (!scratch || reinterpret_cast<uintptr_t>(scratch) % 8 || scratch_bytes < psa_page_table_scratch_bytes(a.num_samples))
         return set_last_error(PSA_ERR_WORKSPACE, "scratch must be 8-byte aligned and hold psa_page_table_scratch_bytes(num_samples)");
     a.head = static_cast<int2 *>(scratch);

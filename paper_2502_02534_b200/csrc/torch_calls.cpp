@@ -88,7 +88,7 @@ public:
         if (v == -1 && PyErr_Occurred()) throw Refused("");
         return v;
     }
-    // a status word: an int32 tensor, or the workspace of a plan (uint8), whose first word it is
+    // a status word: an int32 tensor, or the workspace of a plan (uint8), whose first word it is; the library checks its alignment
     int32_t *status(int i)
     {
         if (none(i)) return nullptr;
