@@ -453,7 +453,9 @@ psa_status_t psa_load_kv4(const void *pool, const int64_t pool_strides[2], int64
  * either cache with the same results up to rounding; psa_plan_create_kv4 makes, from a plan for psa_decode, the plan of the same
  * problem (and forced knobs) whose pieces are sized for a 4-bit cache; it is bound, queried and destroyed like any other.  Every
  * other argument is that of psa_decode.  K and V enter the products as their exact codes; probabilities are rounded to bf16 as in
- * psa_decode.
+ * psa_decode.  Magnitudes it takes: components of q below 2^64, scales of K up to 2^50, scales of V from 2^-57 to 2^55 (V's values up
+ * to 5e17).  V groups of smaller scale lose bits of their codes, those of larger scale may come out infinite or NaN, although
+ * psa_store_kv4 and psa_load_kv4 take any.
  */
 psa_status_t psa_plan_create_kv4(const psa_plan_t *plan, psa_plan_t **out_plan);
 psa_status_t psa_decode_kv4(const psa_plan_t *plan, const void *q, const void *prefix_k, const void *prefix_v,

@@ -10,6 +10,8 @@
 // whole number n is the subnormal bf16 n * 2^-133, exactly, and a nibble left in place at bits 4-7 is 16 n * 2^-133; the other
 // two nibbles of a 16-bit half need one shift for both.  2^64 on the other operand keeps the products in fp32's normal range,
 // and the powers of two come out again in constants (scores) or once at the end (outputs).  5 instructions unpack 8 codes of K.
+// That bounds the magnitudes: q * 2^64 and p * s * 2^64, with p up to 2^8 while the reference lags, are finite bf16 numbers for q below
+// 2^64 and scales of V up to 2^55; p * s * 2^-69 is a normal fp32 number for p = 1 and scales of V from 2^-57 on.
 //   * scores: K codes come out of shared memory through ldmatrix with two 16-bit units = 8 channels of one token per
 //     register; the four masked forms of that register are A operands of two m16n8k16 products whose B operands hold q in the
 //     matching channel order (loaded that way once per block), odd nibbles' q divided by 16.
