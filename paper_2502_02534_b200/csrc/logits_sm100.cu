@@ -19,14 +19,20 @@
 //            writes its few logits over the stream's when that is done.
 //   run      a block per row and run of 4 to 16 tiles picks the entries of its own tokens out of the row's lists, streams the run and writes
 //            the lists' logits over it.  One launch, everything written where it was just read; but every block reads all the lists
-//            and waits for them.  In place, and for lists that the row's table does not take.
-// Lists of more entries than the table takes are done with a counter for every token of a tile (run) or of as many tokens as the table
-// has slots (two, whole).
+//            and waits for them.  In place, for lists that the row's table does not take, and for many biases.
+// Lists of more entries than the table takes are done tile by tile with a slot for every token (run), with a slot for every token of the row
+// (whole), or in ranges of tokens whose entries the table takes (two).  The table of "two" is sized for the history and four times the mean
+// number of biases, since its size costs every row; a row with more biases takes a few passes over its lists.
 // Bound: HBM, one read and one write of every logit (and 2 bits).  Measured: 256 rows x 131072 bf16 logits, U[0, 1024] generated tokens and
-// U[0, 64] biases each, 134.9 MB: two 28.4 us (31.2 over three sets of inputs in turn), run 39.5; the stream alone 24.3, a plain copy 22.3.
+// U[0, 64] biases each, 134.9 MB: two 28.2 us (31.3 over three sets of inputs in turn), run 40.0, in place 29.4; the stream alone 24.3, a
+// plain copy 22.3.
 // What the lists add is their latency, not their traffic: a table half full instead of a quarter 32.2 us, linear probing 38, 96 KB of
 // table instead of 48 (fewer blocks beside the stream's) 33.9, stream blocks of 4 or 16 tiles instead of 8 33.7 and 34.5.
-// 8 / 64 rows of that: two 6.6 / 11.2, run 6.1 / 11.8; 256 rows with up to 3500 generated tokens each 49 and 76.  8 rows x 3001: whole 4.4 us.
+// 8 / 64 / 128 rows of that: two 6.9 / 10.0 / 14.2, run 6.6 / 10.5 / 18.2, in place 6.7 / 10.6 / 18.5; 256 rows with up to 3500 generated tokens
+// each: two 52, run 79, in place 70.  8 rows x 3001: whole 3.9 us.
+// Biases of one row alone, 256 rows, none / 1000 / 3000 / 8000 / 30000: two 20 / 54 / 100 / 318 / 2430, in place 16 / 18 / 30 / 257 / 795 us.  The
+// same number in every row, no history, 128 / 256 / 512: two 23 / 28 / 36, run 31 / 29 / 32; 64 rows 7.2 / 10.7 / 16.4 and 8.6 / 8.1 / 9.2; 8 rows
+// 5.8 / 9.2 / 14.8 and 4.9 / 4.5 / 4.9.
 // Tried for the largest case: lists by warps beside the streaming ones of a block 40-59 us; a resident stream of 5 blocks an SM with the
 // lists beside it from the start 42; groups of rows streamed and followed by their lists 35-42; prefetching the lists into L2: no change.
 #include <cuda_bf16.h>
@@ -49,6 +55,9 @@ constexpr int kStreamRun = 8, kStreamDepth = 4;            // tiles of a block; 
 constexpr int kWholeRow = 8192;                            // vocabularies up to this are streamed by the row's own block
 constexpr int kLog2Few = 11, kLog2Many = 13;                // sizes of the row's hash table
 __host__ __device__ constexpr int64_t table_takes(int log2_slots) { return int64_t(1) << (log2_slots - 1); }   // entries: half full
+constexpr int kFewBiases = 128;                            // more of them in a row are added up by the whole block, where it can
+constexpr int kManyBiases = 256;                           // more of them a row on average: one launch
+constexpr int kParts = 512;                                // of the vocabulary, whose entries are counted where there are too many for the table
 constexpr int kOwn = 8;                                    // list entries a thread keeps in registers
 constexpr int kLongHistory = kOwn * kListThreads;
 constexpr int kThreads = 256, kTile = kThreads * kVec;     // one launch: threads of a block, logits it takes at a time,
@@ -344,27 +353,83 @@ struct Table {
     }
 };
 
-// Adds a row's biases to their tokens' values in list order, by one warp.  Equal tokens inside the 32 entries of a step are summed
-// by the first lane that has them, so the order of the additions is that of the list.
+// Hands every id of a list to one of the block's threads, which has four reads in flight; -1 behind the list.
+template <int kBlock, class Take>
+__device__ __forceinline__ void for_all(const int32_t *ids, int n, Take take)
+{
+    for (int e0 = threadIdx.x; e0 < n; e0 += 4 * kBlock) {
+        int id[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) id[k] = e0 + k * kBlock < n ? ids[e0 + k * kBlock] : -1;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) take(id[k]);
+    }
+}
+
+// Adds 32 biases to their tokens' values, by one warp; at: slot of a lane's token, -1 for none.  Equal tokens are summed by the first lane
+// that has them, so the order of the additions is that of the lanes.
+__device__ __forceinline__ void add_32(const Table &t, int at, float v, int lane)
+{
+    const uint32_t same = __match_any_sync(0xffffffffu, at);
+    const bool leader = at >= 0 && (__ffs(same) - 1) == lane;
+    float sum = leader ? t.value[at] : 0.f;
+    // every lane takes part in the shuffles; at most 32 rounds, one without duplicates
+    uint32_t rest = at >= 0 ? same : 0u;
+    while (__any_sync(0xffffffffu, rest != 0u)) {
+        const int from = rest ? __ffs(rest) - 1 : 0;
+        const float u = __shfl_sync(0xffffffffu, v, from);
+        if (rest) sum += u;
+        rest &= rest - 1u;
+    }
+    if (leader) t.value[at] = sum;
+    __syncwarp();
+}
+// Adds a row's biases to their tokens' values in list order, by one warp.
 __device__ void add_biases(const int32_t *ids, const float *values, int n, const Table &t, int lane)
 {
     for (int e0 = 0; e0 < n; e0 += 32) {
         const int e = e0 + lane;
         const int at = e < n ? t.find(ids[e]) : -1;
         const float v = e < n ? values[e] : 0.f;
-        const uint32_t same = __match_any_sync(0xffffffffu, at);
-        const bool leader = at >= 0 && (__ffs(same) - 1) == lane;
-        float sum = leader ? t.value[at] : 0.f;
-        // every lane takes part in the shuffles; at most 32 rounds, one without duplicates
-        uint32_t rest = at >= 0 ? same : 0u;
-        while (__any_sync(0xffffffffu, rest != 0u)) {
-            const int from = rest ? __ffs(rest) - 1 : 0;
-            const float u = __shfl_sync(0xffffffffu, v, from);
-            if (rest) sum += u;
-            rest &= rest - 1u;
+        add_32(t, at, v, lane);
+    }
+}
+// The same by a whole block, for long lists: the entries that concern the table are brought together in list order, so that the warp that
+// adds them up meets no others and does not wait for memory.  The caller synchronises the block before and after it.
+template <int kBlock>
+struct Together {   // in shared memory that is free meanwhile
+    float value[kBlock];
+    uint16_t slot[kBlock];
+    int32_t count[kBlock / 32];
+};
+template <int kBlock>
+__device__ __forceinline__ void add_many_biases(const int32_t *ids, const float *values, int n, const Table &t, Together<kBlock> &to)
+{
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    int id = tid < n ? ids[tid] : -1;
+    float v = tid < n ? values[tid] : 0.f;
+    for (int e0 = 0; e0 < n; e0 += kBlock) {
+        const int at = t.find(id);
+        const float mine = v;
+        const int next = e0 + kBlock + tid;
+        id = next < n ? ids[next] : -1;
+        v = next < n ? values[next] : 0.f;
+        const uint32_t have = __ballot_sync(0xffffffffu, at >= 0);
+        if (lane == 0) to.count[warp] = __popc(have);
+        __syncthreads();   // also: the warp that adds is done with the entries before
+        int before = 0, total = 0;
+        for (int w = 0; w < kBlock / 32; ++w) {
+            before += w < warp ? to.count[w] : 0;
+            total += to.count[w];
         }
-        if (leader) t.value[at] = sum;
-        __syncwarp();
+        if (at >= 0) {
+            const int i = before + __popc(have & ((1u << lane) - 1u));
+            to.slot[i] = uint16_t(at);
+            to.value[i] = mine;
+        }
+        __syncthreads();
+        if (warp == 0)
+            for (int i = lane; i - lane < total; i += 32) add_32(t, i < total ? int(to.slot[i]) : -1, i < total ? to.value[i] : 0.f, lane);
     }
 }
 
@@ -468,9 +533,20 @@ rules_lists_kernel(RulesArgs a)
             if (at[k] >= 0)
                 store_one<kOutF32>(out, id[k], allowed & (1u << k) ? ruled(x[k], t.count[at[k]], in_prompt & (1u << k)) + t.value[at[k]] : -INFINITY);
     } else {
-        for (int64_t r0 = 0; r0 < a.vocab; r0 += t.slots()) {
-            t.r0 = int(r0);
-            t.r1 = int(min((int64_t)a.vocab, r0 + t.slots()));
+        // what the table has come to: its tokens' logits, written when the stream is done with theirs
+        auto finish = [&] {
+            for (int h = tid; h < t.slots(); h += kListThreads) {
+                const int token = t.key[h];
+                if (token < 0) continue;
+                const float x = ruled(load_one<kInF32>(in, token), t.count[h], r.prompt && Row::has(r.prompt, token));
+                t.value[h] = !r.mask || Row::has(r.mask, token) ? x + t.value[h] : -INFINITY;
+            }
+            rest();
+            for (int h = tid; h < t.slots(); h += kListThreads)
+                if (t.key[h] >= 0) store_one<kOutF32>(out, t.key[h], t.value[h]);
+        };
+        if constexpr (kWhole) {
+            t.r0 = 0; t.r1 = a.vocab;
             t.clear(tid, kListThreads);
             __syncthreads();
             bool mine;
@@ -484,16 +560,53 @@ rules_lists_kernel(RulesArgs a)
                 if (tid < 32) add_biases(a.r.bias_ids + b0, a.r.bias_values + b0, n_bias, t, tid);
                 __syncthreads();
             }
-            for (int h = tid; h < t.slots(); h += kListThreads) {
-                const int token = t.key[h];
-                if (token < 0) continue;
-                const float x = ruled(load_one<kInF32>(in, token), t.count[h], r.prompt && Row::has(r.prompt, token));
-                t.value[h] = !r.mask || Row::has(r.mask, token) ? x + t.value[h] : -INFINITY;
-            }
-            rest();   // a whole row has one range
-            for (int h = tid; h < t.slots(); h += kListThreads)
-                if (t.key[h] >= 0) store_one<kOutF32>(out, t.key[h], t.value[h]);
+            finish();
+        } else {
+            // Ranges of as many neighbouring parts of the vocabulary as the table takes the entries of, so about entries / most passes over
+            // the lists, where a slot for every token would need vocab / slots of them.  Half of the table, three quarters full; the other half of
+            // the memory holds what else is needed.
+            --t.log2_slots;
+            t.count = t.key + t.slots(); t.value = reinterpret_cast<float *>(t.count + t.slots());
+            const int most = t.slots() / 4 * 3;
+            int *in_part = reinterpret_cast<int *>(t.value + t.slots());
+            auto &to = *reinterpret_cast<Together<kListThreads> *>(in_part + kParts);
+            static_assert(4 * kParts + sizeof(to) <= (12 << kLog2Few) / 2 && kParts <= kListThreads, "in the other half");
+            int log2_part = t.log2_slots;
+            while ((a.vocab - 1) >> log2_part >= kParts) ++log2_part;
+            const int parts = ((a.vocab - 1) >> log2_part) + 1;
+            if (tid < kParts) in_part[tid] = 0;
             __syncthreads();
+            auto tally = [&](int id) {
+                if (id >= 0 && id < a.vocab) atomicAdd(in_part + (id >> log2_part), 1);
+            };
+            for_all<kListThreads>(said, n_said, tally);
+            for_all<kListThreads>(a.r.bias_ids + b0, n_bias, tally);
+            __syncthreads();
+            // a part that alone has more entries gets a slot for every token, as many tokens at a time as there are slots
+            for (int p = 0, q, r0 = 0, r1; p < parts; p = q, r0 = r1) {
+                int sum = in_part[p];
+                for (q = p + 1; q < parts && sum + in_part[q] <= most; ++q) sum += in_part[q];
+                r0 = max(r0, p << log2_part);
+                r1 = min(a.vocab, q << log2_part);
+                if (sum > most && r1 - r0 > t.slots()) { r1 = r0 + t.slots(); q = p; }
+                if (sum == 0) continue;
+                t.r0 = r0; t.r1 = r1; t.hashed = sum <= most;
+                t.clear(tid, kListThreads);
+                __syncthreads();
+                bool mine;
+                for_all<kListThreads>(said, n_said, [&](int id) {
+                    const int h = t.add(id, mine);
+                    if (h >= 0) atomicAdd(t.count + h, 1);
+                });
+                for_all<kListThreads>(a.r.bias_ids + b0, n_bias, [&](int id) { t.add(id, mine); });
+                __syncthreads();
+                if (n_bias > 0) {
+                    add_many_biases<kListThreads>(a.r.bias_ids + b0, a.r.bias_values + b0, n_bias, t, to);
+                    __syncthreads();
+                }
+                finish();
+                __syncthreads();
+            }
         }
     }
 }
@@ -508,7 +621,9 @@ rules_run_kernel(RulesArgs a)
     extern __shared__ __align__(16) unsigned char ring[];   // [kDepth][kThreads * kBytes]
     __shared__ __align__(16) int32_t keys[kRunSlots], counts[kRunSlots];
     __shared__ __align__(16) float values[kRunSlots];
-    __shared__ uint16_t hits[kHits];   // the run's list entries: token - c0, and whether it is a bias
+    __shared__ __align__(16) uint16_t hits[kHits];   // the run's list entries: token - c0, and whether it is a bias
+    auto &to = *reinterpret_cast<Together<kThreads> *>(hits);   // once they have been read
+    static_assert(sizeof(to) <= sizeof hits, "in its place");
     __shared__ int num_hits;
     const int row = blockIdx.y, tid = threadIdx.x;
     const int c0 = blockIdx.x * (a.run * kTile), c1 = min(a.vocab, c0 + a.run * kTile), tiles = (c1 - c0 + kTile - 1) / kTile;
@@ -623,7 +738,8 @@ rules_run_kernel(RulesArgs a)
             }
         }
         __syncthreads();
-        if (biased && tid < 32) add_biases(a.r.bias_ids + b0, a.r.bias_values + b0, n_bias, t, tid);
+        if (biased && n_bias > kFewBiases) add_many_biases<kThreads>(a.r.bias_ids + b0, a.r.bias_values + b0, n_bias, t, to);
+        else if (biased && tid < 32) add_biases(a.r.bias_ids + b0, a.r.bias_values + b0, n_bias, t, tid);
         for (int g = 0; g < tiles; ++g) stream(g);
         __syncthreads();
 #pragma unroll
@@ -647,9 +763,11 @@ rules_run_kernel(RulesArgs a)
             for (int e = tid; e < n_bias; e += kThreads) t.add(a.r.bias_ids[b0 + e], mine);
             __syncthreads();
             if (biased) {
-                if (tid < 32) add_biases(a.r.bias_ids + b0, a.r.bias_values + b0, n_bias, t, tid);
+                if (n_bias > kFewBiases) add_many_biases<kThreads>(a.r.bias_ids + b0, a.r.bias_values + b0, n_bias, t, to);
+                else if (tid < 32) add_biases(a.r.bias_ids + b0, a.r.bias_values + b0, n_bias, t, tid);
                 __syncthreads();
             }
+#pragma unroll 8
             for (int h = tid; h < kTile; h += kThreads) {
                 const int token = t.key[h];
                 if (token < 0) continue;
@@ -659,6 +777,7 @@ rules_run_kernel(RulesArgs a)
             __syncthreads();   // in place: the logits have been read
             stream(g);
             __syncthreads();
+#pragma unroll 8
             for (int h = tid; h < kTile; h += kThreads)
                 if (t.key[h] >= 0) store_one<kOutF32>(out, t.key[h], t.value[h]);
             __syncthreads();
@@ -742,10 +861,10 @@ cudaError_t launch_rules(const RulesArgs &a, int rows, bool lists, bool long_lis
     }
     const size_t table = size_t(12) << a.log2_slots;
     if (lists && a.vocab <= kWholeRow) return launch_behind(whole, dim3(rows), kListThreads, table, st, a);
-    if (lists && (a.logits == a.out || long_lists)) {
+    if (lists && (a.logits == a.out || long_lists || a.r.num_biases > int64_t(kManyBiases) * rows)) {
         // Long runs, since every block reads all of its row's lists: 256 rows x 131072 in place take 44.5 us in runs of 4 tiles, 34.7 in 8 and
-        // 31.2 in 16.  But two or three blocks for every SM (64 rows: 14.0, 12.3, 13.2; 8 rows: 6.7, 8.2, 10.4), and no more entries in
-        // a run than its table takes (8192 generated tokens: 87, 97, 132).
+        // 31.2 in 16 (three sets of inputs in turn).  But two or three blocks for every SM (64 rows: 14.0, 12.3, 13.2; 8 rows: 6.7, 8.2, 10.4),
+        // and no more entries in a run than its table takes (8192 generated tokens: 87, 97, 132).
         RulesArgs b = a;
         const int64_t said = a.r.history ? a.r.history_capacity : 0;
         auto blocks = [&](int tiles) { return (a.vocab + tiles * kTile - 1) / (tiles * kTile); };
