@@ -607,6 +607,7 @@ rules_lists_kernel(RulesArgs a)
                 finish();
                 __syncthreads();
             }
+            rest();   // where no entry is a token's: this grid must not end before the stream has
         }
     }
 }
@@ -787,7 +788,8 @@ rules_run_kernel(RulesArgs a)
 
 // Token sets as bitmaps: one block per (row, kMarkTile tokens) walks the row's list and sets bits in shared memory.  Bound by the shared
 // atomics of one block, 16-byte loads change nothing: 64 rows x 32768 ids, vocabulary 131072, 5.4 us (floor 1.1); 256 rows 9.1, and 14.4
-// with tiles of half the size, whose blocks read every list twice.
+// with tiles of half the size, whose blocks read every list twice.  Larger vocabularies are where that begins (131073 / 151936 tokens): 64 rows x
+// 32768 ids 6.2 -> 6.7 / 7.4 us as calls, 256 x 4096 6.2 -> 8.1 / 8.3.
 __global__ void __launch_bounds__(kMarkThreads)
 mark_kernel(const int32_t *__restrict__ ids, int num_ids, const int32_t *__restrict__ indptr, int vocab, uint32_t *__restrict__ bits, int64_t row_words)
 {

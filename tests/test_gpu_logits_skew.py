@@ -111,3 +111,25 @@ def test_one_long_row_does_not_hold_up_the_call():
     none = time(one(0))
     assert time(one(2000)) < 10 * none and time(one(3000)) < 15 * none
     assert time(one(2000) + 8) < 10 * time(np.full(R, 16))
+
+
+@pytest.mark.parametrize("n", [1000, 5000])
+def test_a_long_row_none_of_whose_entries_is_a_token(n):
+    """Nothing to write for that row; calls behind it, on its output, find it complete."""
+    import torch
+    from paper_2502_02534_b200 import process_logits
+    R, V = 300, 131072
+    c = np.zeros(R, int)
+    c[7] = n
+    kw = dict(bias_indptr=dev(np.concatenate([[0], np.cumsum(c)])), bias_ids=dev(np.where(np.arange(n) % 2, -1 - np.arange(n), V + np.arange(n))),
+              bias_values=torch.ones(n, device="cuda"), prompt_bits=torch.full((1, V // 32), -1, dtype=torch.int32, device="cuda"),
+              prompt_rows=dev(np.zeros(R)), repetition=torch.full((R,), 2.0, device="cuda"))
+    x = torch.randn((R, V), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").abs()
+    want = x * 0.125
+    a, b = torch.empty_like(x), torch.empty_like(x)
+    for _ in range(5):
+        a.zero_(); b.zero_()
+        process_logits(x, a, **kw)
+        process_logits(a, b, **kw)
+        process_logits(b, a, **kw)
+        assert torch.equal(a, want)
