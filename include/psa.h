@@ -473,7 +473,8 @@ psa_status_t psa_decode_suffix_kv4(const psa_plan_t *plan, const void *q, const 
  *     x <- x - frequency[r] * c - presence[r] * [c > 0]
  *     x <- x + (the row's biases for i, added in list order)
  *     x <- -inf                                               if the row's mask has bit i clear
- * in fp32, rounded once to the output type.  Every pointer is device memory and may be NULL, which leaves that rule out:
+ * in fp32, rounded once to the output type; the quotient is x times 1 / repetition, both rounded to fp32.  Every pointer is device
+ * memory and may be NULL, which leaves that rule out:
  *   repetition, frequency, presence  [R] f32 (a repetition that is not positive and finite counts as 1)
  *   history        int32, row r at r*history_stride; the first history_lens[r] (0 .. history_capacity, clamped) entries are the
  *                  row's generated tokens
@@ -483,7 +484,7 @@ psa_status_t psa_decode_suffix_kv4(const psa_plan_t *plan, const void *q, const 
  *   bias_indptr    [R+1] int32, bias_ids int32, bias_values f32 of num_biases entries: bias_indptr[r] .. bias_indptr[r+1]-1 (cut to
  *                  0 .. num_biases) belong to row r
  *   mask_bits      bitmaps like prompt_bits (set = allowed): num_mask_bitmaps of mask_row_words words; mask_rows as prompt_rows
- * Token ids outside 0 .. vocab-1 are ignored; vocab <= 2^24.  A row whose mask allows nothing becomes -inf throughout.  Types, alignment and strides
+ * Token ids outside 0 .. vocab-1 are ignored; vocab <= 2^24, num_rows <= 65535.  A row whose mask allows nothing becomes -inf throughout.  Types, alignment and strides
  * as for psa_sample_tokens, for input and output each; out may be logits (same type and stride), otherwise the two do not overlap.
  * NaN logits stay NaN unless masked.  Needs no scratch memory; only enqueues one or two kernels.
  */

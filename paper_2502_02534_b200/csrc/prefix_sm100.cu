@@ -557,7 +557,7 @@ prefix_body(const CUtensorMap *pmap_q, const CUtensorMap *pmap_k, const CUtensor
                 return true;
             };
 
-            float tile_sum = 0.f;   // the row's sum over this tile (times 1 + 2^-9, see exp_in_place)
+            float tile_sum = 0.f;   // the row's sum over this tile (times the factor of truncation, see exp_in_place)
             if constexpr (kTwo) {
                 // ---- S in registers; P (bf16) is written back over the first 64 columns of S.
                 // Common case: ONE pass that exponentiates against the current reference maximum while tracking the
@@ -578,7 +578,7 @@ prefix_body(const CUtensorMap *pmap_q, const CUtensorMap *pmap_k, const CUtensor
                 };
                 // sreg: 128 scores -> 64 words of packed bf16 P (in sreg[0], sreg[1]); returns the row's sum of the tile.
                 // bf16 by truncation (a byte permute on the integer pipe: the special-function unit does the
-                // exponentials and nothing else), unbiased by exponentiating x + log2(1 + 2^-9); no running maximum: a
+                // exponentials and nothing else), unbiased by exponentiating x + trunc_bias (log2 of the factor); no running maximum: a
                 // tile sum above kKeys * 2^8 is what tells that some exponent exceeded the threshold.
                 auto exp_in_place = [&]() -> float {
                     const float off = trunc_bias - (m_ref == -INFINITY ? 0.f : m_ref);   // no key seen yet: exponentiate against 0
@@ -688,7 +688,7 @@ prefix_body(const CUtensorMap *pmap_q, const CUtensorMap *pmap_k, const CUtensor
         // ring is idle by now) so that every global store instruction writes one full 4*D-byte row.
         // The release of the last V buffer follows the last MMA of the block (of both row tiles): O is final
         // and nothing reads the ring any more, so the staging tile may overlay it.
-        l_sum *= trunc_unbias;   // the row sums carry the factor (1 + 2^-9) of the truncation trick
+        l_sum *= trunc_unbias;   // the row sums carry the factor that makes up for truncation
         if (ok) ok = mbar_wait(bar_empty((2 * n_tiles - 1) % ring), ((2 * n_tiles - 1) / ring) & 1, abort_flag);
         float *stage = reinterpret_cast<float *>(smem + L::kRingOff + t * L::kStageBytes);
         if (ok) {
@@ -1040,8 +1040,8 @@ prefix_body2(const CUtensorMap *pmap_q, const CUtensorMap *pmap_k, const CUtenso
             // The special-function unit is the scarce pipe here (one exponential per score), so nothing else may use
             // it: bf16 comes from TRUNCATING p (a byte permute on the integer pipe) instead of a rounding conversion,
             // and the bias of truncation (half a unit in the last place on average) is cancelled by exponentiating
-            // x + log2(1 + 2^-9): every p -- and with it the row sum, which is corrected once in the epilogue --
-            // carries the factor (1 + 2^-9).  No running maximum either: if every exponent is below the threshold the
+            // x + trunc_bias, log2 of a factor: every p -- and with it the row sum, which is corrected once in the
+            // epilogue by trunc_unbias -- carries that factor.  No running maximum either: if every exponent is below the threshold the
             // tile sum is at most 64 * 2^8, so a sum above that bound is what sends the tile to the slow path.
             auto exp_in_place = [&]() -> float {
                 const float off = trunc_bias - (m_ref == -INFINITY ? 0.f : m_ref);   // a row that has seen no key yet: exponentiate against 0
@@ -1112,7 +1112,7 @@ prefix_body2(const CUtensorMap *pmap_q, const CUtensorMap *pmap_k, const CUtenso
         }
         // ---- epilogue.  Every MMA of the block is complete (O final, Q and the rings idle): the staging tile(s) may
         // overlay them, so that every global store instruction writes one full row.
-        l_sum *= trunc_unbias;   // the row sums carry the factor (1 + 2^-9) of the truncation trick
+        l_sum *= trunc_unbias;   // the row sums carry the factor that makes up for truncation
         const bool active = kPing || t < n_streams;
         if (active) {
             if (ok) ok = mbar_wait(bar(L::kBarDone), 0, abort_flag);
