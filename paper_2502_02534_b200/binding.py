@@ -193,37 +193,34 @@ def _stream_ptr(stream):
 
 
 def _on(stream):
-    """The context in which what a call on `stream` needs is allocated (None: the current stream).  A block of the caching allocator belongs
-    to the stream it was allocated on: one of the current stream's may still be written by work enqueued there before it was freed,
-    which a call on another stream does not wait for."""
+    """The context of a stream, given as torch's, as its handle or as an object that has one (None: the current stream)."""
     if stream is None:
         return nullcontext()
     import torch
-    if isinstance(stream, int):
-        stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+    if not isinstance(stream, torch.cuda.Stream):
+        handle = _stream_ptr(stream)
+        stream = torch.cuda.ExternalStream(handle) if handle else torch.cuda.default_stream()
     return torch.cuda.stream(stream)
 
 
-def _new(shape, dtype, device, stream):
-    """A tensor that a call on `stream` writes and returns: allocated for that stream, and not given back to it before the current stream's
-    use of it is over."""
+_TYPE_CODES = {"int32": 1, "uint8": 2, "float32": 3}
+
+
+def _new(shape, like, stream, dtype=None):
+    """A tensor that a call on `stream` writes and returns, on the device and (dtype None) of the type of `like`.  Allocated for that stream, as
+    the native module's `empty` says."""
+    if stream is not None:
+        return (_calls or _native()).empty(like, _TYPE_CODES.get(dtype, 0), shape, stream, True)
     import torch
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    with _on(stream):
-        t = torch.empty(shape, dtype=dtype, device=device)
-    if t.is_cuda:
-        t.record_stream(torch.cuda.current_stream(t.device))
-    return t
+    return torch.empty(shape, dtype=getattr(torch, dtype) if dtype else like.dtype, device=like.device)
 
 
 def _scratch(nbytes, like, stream):
     """A scratch tensor for one call on `stream` (None: the current one)."""
+    if stream is not None:
+        return (_calls or _native()).empty(like, 2, (int(nbytes),), stream, False)
     import torch
-    if stream is None:
-        return torch.empty(int(nbytes), dtype=torch.uint8, device=like.device)
-    with _on(stream):
-        return torch.empty(int(nbytes), dtype=torch.uint8, device=like.device)
+    return torch.empty(int(nbytes), dtype=torch.uint8, device=like.device)
 
 
 def _i32(a):
@@ -450,7 +447,7 @@ def sample_tokens_at(logits, temperature, seeds, step_device, advance=1, tokens=
     if logits.stride(1) != 1:
         raise ValueError("logits must be contiguous along the vocabulary")
     if tokens is None:
-        tokens = _new(B, torch.int32, logits.device, stream)
+        tokens = _new((B,), logits, stream, "int32")
     if scratch is None:
         scratch = _scratch(max(8, int(lib.psa_sample_scratch_bytes(B))), logits, stream)
     _check(lib.psa_sample_tokens_at(_ptr(logits), dtype, logits.stride(0), B, V, _ptr(temperature), _ptr(seeds), _ptr(step_device),
@@ -468,7 +465,7 @@ def sample_tokens(logits, temperature, seeds, step, tokens=None, scratch=None, *
     if logits.stride(1) != 1:
         raise ValueError("logits must be contiguous along the vocabulary")
     if tokens is None:
-        tokens = _new(B, torch.int32, logits.device, stream)
+        tokens = _new((B,), logits, stream, "int32")
     need = int(lib.psa_sample_scratch_bytes(B))
     if scratch is None:
         scratch = _scratch(max(8, need), logits, stream)
@@ -479,10 +476,9 @@ def sample_tokens(logits, temperature, seeds, step, tokens=None, scratch=None, *
 
 def attn_task(task, q, k, v, sm_scale, *, stream=None):
     """psa_attn_task on torch CUDA tensors: q [R, D], k / v [M, D] bf16.  Returns (out [R, D] f32, m [R], l [R])."""
-    import torch
     R, D = q.shape
     M = k.shape[0]
-    out, m, l = (_new(shape, torch.float32, q.device, stream) for shape in ((R, D), R, R))  # noqa: E741
+    out, m, l = (_new(shape, q, stream, "float32") for shape in ((R, D), (R,), (R,)))  # noqa: E741
     _check(library().psa_attn_task(int(task), _ptr(q), _ptr(k) if M else None, _ptr(v) if M else None, R, M, D, float(sm_scale),
                                    _ptr(out), _ptr(m), _ptr(l), _stream_ptr(stream)))
     return out, m, l
@@ -673,7 +669,7 @@ def process_logits(logits, out=None, *, repetition=None, frequency=None, presenc
     mask_rows [R] int32; bias_indptr [R+1], bias_ids int32 and bias_values f32.  Returns out."""
     rows, vocab = logits.shape
     if out is None:
-        out = _new((rows, (vocab + 7) // 8 * 8), logits.dtype, logits.device, stream)[:, :vocab]
+        out = _new((rows, (vocab + 7) // 8 * 8), logits, stream)[:, :vocab]
     rc = (_calls or _native()).process_logits(logits, out, repetition, frequency, presence, history, history_lens, prompt_bits, prompt_rows, bias_indptr,
                                               bias_ids, bias_values, mask_bits, mask_rows, stream)
     if rc:
@@ -684,8 +680,7 @@ def process_logits(logits, out=None, *, repetition=None, frequency=None, presenc
 def mark_tokens(ids, indptr, vocab, bits=None, *, stream=None):
     """psa_mark_tokens: bitmaps [rows, >= ceil(vocab / 32)] int32 of the tokens in ids[indptr[m] .. indptr[m + 1]).  Returns bits."""
     if bits is None:
-        import torch
-        bits = _new((max(0, indptr.numel() - 1), (int(vocab) + 31) // 32), torch.int32, ids.device, stream)
+        bits = _new((max(0, indptr.numel() - 1), (int(vocab) + 31) // 32), ids, stream, "int32")
     rc = (_calls or _native()).mark_tokens(ids, indptr, vocab, bits, stream)
     if rc:
         _check(rc)

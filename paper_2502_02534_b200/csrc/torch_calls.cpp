@@ -1,13 +1,15 @@
 // Native argument marshalling for the entry points that a decode step calls with a dozen tensors each: page tables, the 4-bit
 // cache, rules on logits.  It reads types, layouts, devices and addresses out of the tensors directly and calls the C ABI
 // (include/psa.h), so that a call costs about as much as its launch; the same checks made attribute by attribute in Python
-// took 6 to 11 us a call.  No arithmetic and no memory management happens here.
+// took 6 to 11 us a call.  No arithmetic happens here, and the only memory is what a call on an explicit stream needs.
 //
 // What a caller got wrong about its tensors (type, layout, size, device) is raised as ValueError; the library's own status comes back as
 // an integer, which the Python side turns into PsaError.
 #include <Python.h>
 
+#include <ATen/ops/empty.h>
 #include <c10/cuda/CUDAFunctions.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -102,11 +104,15 @@ public:
         if (odd_) throw Refused(std::string(odd_) + " must be on the current CUDA device");
         if (device_ != c10::cuda::current_device()) throw Refused("the tensors must be on the current CUDA device");
         if (none(i)) return c10::cuda::getCurrentCUDAStream(c10::DeviceIndex(device_)).stream();
-        if (PyLong_Check(args_[i])) return PyLong_AsVoidPtr(args_[i]);
-        PyObject *handle = PyObject_GetAttrString(args_[i], "cuda_stream");
-        if (!handle) throw Refused("");
-        void *p = PyLong_AsVoidPtr(handle);
-        Py_DECREF(handle);
+        return handle(args_[i]);
+    }
+    // a stream given as its handle or as an object that has one
+    static void *handle(PyObject *stream)
+    {
+        PyObject *h = PyLong_Check(stream) ? Py_NewRef(stream) : PyObject_GetAttrString(stream, "cuda_stream");
+        if (!h) throw Refused("");
+        void *p = PyLong_AsVoidPtr(h);
+        Py_DECREF(h);
         if (!p && PyErr_Occurred()) throw Refused("");
         return p;
     }
@@ -386,6 +392,42 @@ psa_status_t mark_tokens(PyObject *const *args, Py_ssize_t given)
                            bits.size(0) > 1 ? bits.stride(0) : bits.size(1), stream);
 }
 
+// tensor, type code (0: the tensor's, 1: int32, 2: uint8, 3: float32), sizes, stream, whether it is returned: a new tensor where the given one
+// is, allocated for the stream.  A block of the caching allocator belongs to the stream it was allocated on: one of the current stream's may
+// still be written by work enqueued there before it was freed, which a call on another stream does not wait for.  What is returned is not given
+// back to its stream before the current stream's use of it is over.
+PyObject *empty(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    try {
+        if (n != 5 || !THPVariable_Check(args[0]) || !PyTuple_Check(args[2])) throw Refused("wrong arguments");
+        const at::Tensor &like = THPVariable_Unpack(args[0]);
+        const long code = PyLong_AsLong(args[1]);
+        int64_t sizes[2] = {0, 0};
+        const Py_ssize_t dims = PyTuple_GET_SIZE(args[2]);
+        if (dims > 2) throw Refused("wrong arguments");
+        for (Py_ssize_t i = 0; i < dims; ++i) sizes[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(args[2], i));
+        if (PyErr_Occurred()) return nullptr;
+        const auto type = code == 1 ? at::kInt : code == 2 ? at::kByte : code == 3 ? at::kFloat : like.scalar_type();
+        const auto make = [&] { return at::empty(at::IntArrayRef(sizes, size_t(dims)), at::TensorOptions().dtype(type).device(like.device())); };
+        if (!like.is_cuda()) return THPVariable_Wrap(make());
+        void *const handle = Call::handle(args[3]);
+        const c10::DeviceIndex device = like.get_device();
+        const auto current = c10::cuda::getCurrentCUDAStream(device);
+        const c10::cuda::CUDAStreamGuard guard(handle ? c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(handle), device)
+                                                      : c10::cuda::getDefaultCUDAStream(device));
+        const at::Tensor t = make();
+        if (args[4] == Py_True) t.record_stream(current);
+        return THPVariable_Wrap(t);
+    } catch (const Refused &e) {
+        if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, e.what());
+    } catch (const std::exception &e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+    } catch (...) {
+        PyErr_SetString(PyExc_RuntimeError, "unknown error while allocating a call's memory");
+    }
+    return nullptr;
+}
+
 // path of the C library, which has been loaded already
 PyObject *attach(PyObject *, PyObject *path)
 {
@@ -416,6 +458,7 @@ PyMethodDef method(const char *name)
 PyMethodDef methods[] = {
     method<build_page_table>("build_page_table"), method<extend_page_table>("extend_page_table"), method<store_kv4>("store_kv4"),
     method<load_kv4>("load_kv4"), method<decode_kv4>("decode_kv4"), method<process_logits>("process_logits"), method<mark_tokens>("mark_tokens"),
+    {"empty", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&empty)), METH_FASTCALL, nullptr},
     {"attach", attach, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_torch_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -138,3 +138,20 @@ def test_sampling():
         side.synchronize()
         torch.cuda.synchronize()
         assert torch.equal(got, want)
+
+
+def test_streams_of_every_kind():
+    """A torch stream, a handle, an object that carries one, the current stream by name, and the default stream."""
+    import torch
+    from types import SimpleNamespace
+    from paper_2502_02534_b200 import mark_tokens, process_logits
+    c = case(5, 9000, 3)
+    _, x = padded(c["x"], "f32")
+    kw = arguments(c, 9000, ALL)
+    want, bits = process_logits(x, **kw).clone(), mark_tokens(dev([3, 4]), dev([0, 2]), 100).clone()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for stream in (side, side.cuda_stream, SimpleNamespace(cuda_stream=side.cuda_stream), torch.cuda.current_stream(), 0, torch.cuda.ExternalStream(side.cuda_stream)):
+        got, marked = process_logits(x, stream=stream, **kw), mark_tokens(dev([3, 4]), dev([0, 2]), 100, stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(got.nan_to_num(7.0), want.nan_to_num(7.0)) and torch.equal(marked, bits)
