@@ -83,7 +83,7 @@ def test_large_vocabularies(V, said, n, kind, rows):
 
 
 def test_one_long_row_does_not_hold_up_the_call():
-    """256 rows x 131072, 2000 and 3000 biases in one row: a few times the call without them (it was 30 and 46 times), with and without the
+    """256 rows x 131072, 2000 and 3000 biases in one row: a few times the call without them (one warp walking the whole list for every 2048 tokens: 30 and 46 times), with and without the
     same number spread over the rows."""
     import torch
     from paper_2502_02534_b200 import process_logits
