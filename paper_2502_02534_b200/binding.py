@@ -275,9 +275,10 @@ class Plan:
         return self._kv4
 
     def _prefix_tokens_read(self) -> int:
-        """Packed prefix tokens up to the last one that a sample attends over."""
+        """Tokens the packed prefix arrays must hold: all of them (a tile of keys reaches into the next prompt's), or none if no sample attends
+        over any."""
         samples, lens = self.groups[1:] if hasattr(self, "groups") else (self.n_samples, self.prefix_lens)
-        return int(np.cumsum(lens, dtype=np.int64)[(samples > 0) & (lens > 0)].max(initial=0))
+        return int(lens.sum(dtype=np.int64)) if ((samples > 0) & (lens > 0)).any() else 0
 
     def __del__(self):
         if getattr(self, "_h", None):

@@ -276,7 +276,7 @@ struct Prefix {
     }
 };
 
-// plan handle, samples, query heads, KV heads, head dim, f32 output?, prefix tokens that are read, q, prefix_k, prefix_v, prefix stride 0,
+// plan handle, samples, query heads, KV heads, head dim, f32 output?, tokens of the packed prefix, q, prefix_k, prefix_v, prefix stride 0,
 // prefix stride 1, pool, page_indptr, page_indices, suffix_lens, out, lse, workspace, stream
 psa_status_t decode_kv4(PyObject *const *args, Py_ssize_t given)
 {

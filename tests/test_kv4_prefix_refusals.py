@@ -28,9 +28,12 @@ def test_layouts_that_are_read_as_they_lie():
             call([40], [2], k, v, **kw)
     with pytest.raises(ValueError, match="current CUDA device"):
         call([0], [2], None, bf(1), )
-    # the last prompt has no samples: its tokens are not read
+    # prompts without samples: nothing is read if there are no others ...
     with pytest.raises(ValueError, match="current CUDA device"):
-        call([40, 1000], [2, 0], bf(40, H, D), bf(40, H, D))
+        call([0, 1000], [2, 0], bf(1), bf(1))
+    # ... otherwise a tile of the last prompt's keys may reach into theirs
+    with pytest.raises(ValueError, match="current CUDA device"):
+        call([40, 1000], [2, 0], bf(1040, H, D), bf(1040, H, D))
     with pytest.raises(ValueError, match="current CUDA device"):
         call([], [], bf(60, H, D), bf(60, H, D), groups=([0, 0], [2, 1], [40, 20]))
 
@@ -48,5 +51,7 @@ def test_refusals():
                             (fused[1:, 0], fused[:, H], dict(prefix_strides=((2 * H + 3) * D, D)), "prefix_k must hold")):
         with pytest.raises(ValueError, match=match):
             call([40], [2], k, v, **kw)
+    with pytest.raises(ValueError, match="at least 1040"):
+        call([40, 1000], [2, 0], bf(1039, H, D), bf(1040, H, D))
     with pytest.raises(ValueError, match="at least 60"):
         call([], [], bf(59, H, D), bf(60, H, D), groups=([0, 0], [2, 1], [40, 20]))
