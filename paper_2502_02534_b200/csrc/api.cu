@@ -4,6 +4,7 @@
 
 #include <algorithm>
 #include <cstring>
+#include <memory>
 #include <new>
 #include <string>
 #include <vector>
@@ -22,6 +23,19 @@ psa_status_t fail(psa_status_t st, const std::string &msg)
 psa_status_t cuda_fail(cudaError_t e, const char *what)
 {
     return fail(PSA_ERR_CUDA, std::string(what) + ": " + cudaGetErrorString(e));
+}
+// What became of an entry point that makes a plan, inside its handler: no exception leaves the library.
+psa_status_t failed_by_exception()
+{
+    try {
+        throw;
+    } catch (const std::bad_alloc &) {
+        return fail(PSA_ERR_INVALID_ARG, "out of host memory");
+    } catch (const std::exception &e) {
+        return fail(PSA_ERR_INVALID_ARG, e.what());
+    } catch (...) {
+        return fail(PSA_ERR_INVALID_ARG, "unknown exception");
+    }
 }
 bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
@@ -81,22 +95,18 @@ static psa_status_t create_impl(const psa_config_t *cfg, int32_t num_groups, con
         if (e != cudaSuccess) return cuda_fail(e, "querying the SM count");
         c.num_sms = sms;
     }
-    psa_plan *plan = new (std::nothrow) psa_plan();
-    if (!plan) return fail(PSA_ERR_INVALID_ARG, "out of host memory");
+    auto plan = std::make_unique<psa_plan>();
     std::string err;
     psa_status_t st = psa::build_plan(c, num_groups, first_sample, n_samples, token_len, token_begin, total_tokens, causal, num_samples,
-                                      suffix_lens, kv4, plan, &err);
-    if (st != PSA_OK) {
-        delete plan;
-        return fail(st, err);
-    }
-    *out_plan = plan;
+                                      suffix_lens, kv4, plan.get(), &err);
+    if (st != PSA_OK) return fail(st, err);
+    *out_plan = plan.release();
     return PSA_OK;
 }
 
 psa_status_t psa_plan_create(const psa_config_t *cfg, int32_t num_prefixes, const int32_t *prefix_lens,
                              const int32_t *n_samples_per_prefix, const int32_t *suffix_lens, psa_plan_t **out_plan)
-{
+try {
     if (num_prefixes < 0 || (num_prefixes > 0 && !n_samples_per_prefix)) return fail(PSA_ERR_INVALID_ARG, "null length arrays");
     // prompt p is the prefix group of the next n_samples_per_prefix[p] samples
     std::vector<int32_t> first(static_cast<size_t>(num_prefixes), 0);
@@ -108,18 +118,22 @@ psa_status_t psa_plan_create(const psa_config_t *cfg, int32_t num_prefixes, cons
         if (B > (1 << 24)) return fail(PSA_ERR_UNSUPPORTED, "problem too large");
     }
     return create_impl(cfg, num_prefixes, first.data(), n_samples_per_prefix, prefix_lens, int32_t(B), suffix_lens, out_plan);
+} catch (...) {
+    return failed_by_exception();
 }
 
 psa_status_t psa_plan_create_cascade(const psa_config_t *cfg, int32_t num_groups, const int32_t *group_first_sample,
                                      const int32_t *group_n_samples, const int32_t *group_token_len, int32_t num_samples,
                                      const int32_t *suffix_lens, psa_plan_t **out_plan)
-{
+try {
     return create_impl(cfg, num_groups, group_first_sample, group_n_samples, group_token_len, num_samples, suffix_lens, out_plan);
+} catch (...) {
+    return failed_by_exception();
 }
 
 psa_status_t psa_plan_create_prefill(const psa_config_t *cfg, int32_t num_prompts, const int32_t *prompt_lens,
                                      psa_plan_t **out_plan)
-{
+try {
     if (!cfg || !out_plan) return fail(PSA_ERR_INVALID_ARG, "null cfg or out_plan");
     if (num_prompts < 0 || (num_prompts > 0 && !prompt_lens)) return fail(PSA_ERR_INVALID_ARG, "null prompt_lens");
     if (cfg->num_kv_heads <= 0 || cfg->num_q_heads <= 0 || cfg->num_q_heads % cfg->num_kv_heads)
@@ -149,15 +163,19 @@ psa_status_t psa_plan_create_prefill(const psa_config_t *cfg, int32_t num_prompt
     if (c.prefix_rows_per_item == 0) c.prefix_rows_per_item = psa::kPrefixRowsPerItem;
     return create_impl(&c, int32_t(first.size()), first.data(), count.data(), len.data(), int32_t(total), zero_suffix.data(),
                        out_plan, begin.data(), total, true);
+} catch (...) {
+    return failed_by_exception();
 }
 
 psa_status_t psa_plan_create_kv4(const psa_plan_t *plan, psa_plan_t **out_plan)
-{
+try {
     if (!plan || !out_plan) return fail(PSA_ERR_INVALID_ARG, "null plan or out_plan");
     *out_plan = nullptr;
     if (plan->causal) return fail(PSA_ERR_INVALID_ARG, "a prefill plan has no suffix cache");
     return create_impl(&plan->cfg, plan->num_prefixes, plan->group_first_sample.data(), plan->group_n_samples.data(),
                        plan->group_token_len.data(), plan->num_samples, plan->suffix_len_bounds.data(), out_plan, nullptr, 0, false, true);
+} catch (...) {
+    return failed_by_exception();
 }
 
 psa_status_t psa_plan_destroy(psa_plan_t *plan)
