@@ -32,7 +32,7 @@
 // each: two 52, run 79, in place 70.  8 rows x 3001: whole 3.9 us.
 // Biases of one row alone, 256 rows, none / 1000 / 3000 / 8000 / 30000: two 20 / 54 / 100 / 318 / 2430, in place 16 / 18 / 30 / 257 / 795 us.  The
 // same number in every row, no history, 128 / 256 / 512: two 23 / 28 / 36, run 31 / 29 / 32; 64 rows 7.2 / 10.7 / 16.4 and 8.6 / 8.1 / 9.2; 8 rows
-// 5.8 / 9.2 / 14.8 and 4.9 / 4.5 / 4.9.
+// 5.8 / 9.2 / 14.8 and 4.9 / 4.5 / 4.9.  Whole rows of 8000 tokens, none / 1000 / 8000 biases in one row: 5 / 21 / 97.
 // Tried for the largest case: lists by warps beside the streaming ones of a block 40-59 us; a resident stream of 5 blocks an SM with the
 // lists beside it from the start 42; groups of rows streamed and followed by their lists 35-42; prefetching the lists into L2: no change.
 #include <cuda_bf16.h>
