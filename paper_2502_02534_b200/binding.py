@@ -613,9 +613,9 @@ def decode_kv4(plan: Plan, q, prefix_k, prefix_v, pool, page_indptr, page_indice
                stream=None, stage="all"):
     """psa_decode_kv4 (or one of its stages): decode with the samples' own tokens in a 4-bit pool [pages, Hkv, kv4_cell_bytes(D)]
     uint8.  prefix_k and prefix_v are [tokens, Hkv, D] of any token and head stride (prefix_strides: those of the packed array in their
-    storage, for tensors of another form).  Everything else as for decode; the work lists
-    and the workspace are those of plan.for_kv4(), made at the first call unless plan.for_kv4().bind_workspace() has been called before: one of
-    the two has to come before a stream capture."""
+    storage, for tensors of another form).  Everything else as for decode; the work lists and the workspace are those of plan.for_kv4(),
+    made at the first call unless plan.for_kv4().bind_workspace() has been called before: one of the two has to come before a stream
+    capture."""
     plan = plan._kv4 or plan.for_kv4()
     if stage != "all":
         return _decode_kv4_stage(plan, q, prefix_k, prefix_v, pool, page_indptr, page_indices, suffix_lens, out, lse, prefix_strides, stream, stage)
@@ -647,8 +647,9 @@ def _decode_kv4_stage(plan, q, prefix_k, prefix_v, pool, page_indptr, page_indic
     if stage in ("prefix", "merge"):
         if plan.workspace is None:
             _bind_kv4(plan, stream)
-        if prefix_strides is None and prefix_k is not None and prefix_k.dim() == 3:      # a dimension of one element has no stride of its own
-            prefix_strides = [st if n > 1 else d for st, n, d in zip(prefix_k.stride(), prefix_k.shape, default_prefix_strides(plan))]
+        if stage == "prefix":
+            s0, s1 = (None, None) if prefix_strides is None else prefix_strides
+            prefix_strides = (_calls or _native()).prefix_strides(plan._prefix_tokens, plan.num_kv_heads, plan.head_dim, prefix_k, prefix_v, s0, s1, stream)
         return decode(plan, q, prefix_k, prefix_v, None, None, page_indptr, page_indices, suffix_lens, out, lse, prefix_strides=prefix_strides,
                       stream=stream, stage=stage)
     if stage != "suffix":

@@ -133,11 +133,11 @@ void outer_strides(const at::Tensor &t, int64_t inner, const char *name, int64_t
     s[0] = t.size(0) > 1 ? t.stride(0) : std::max<int64_t>(1, t.size(1)) * std::max(s[1], inner);
 }
 
-template <psa_status_t (*body)(PyObject *const *, Py_ssize_t)>
-PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n)
+template <class Body>
+PyObject *guarded(Body body)
 {
     try {
-        return PyLong_FromLong(body(args, n));
+        return body();
     } catch (const Refused &e) {
         if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, e.what());
     } catch (const std::exception &e) {
@@ -146,6 +146,11 @@ PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n)
         PyErr_SetString(PyExc_RuntimeError, "unknown error while reading the tensors of a call");
     }
     return nullptr;
+}
+template <psa_status_t (*body)(PyObject *const *, Py_ssize_t)>
+PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&] { return PyLong_FromLong(body(args, n)); });
 }
 
 // seq_lens, reserve_lens, free_pages, free_count, free_count_out, page_indptr, page_indices, token_indptr, slot_map, lens_out, status,
@@ -276,6 +281,17 @@ struct Prefix {
     }
 };
 
+// tokens of the packed prefix, KV heads, head dim, prefix_k, prefix_v, prefix stride 0, prefix stride 1, stream: the strides that decode_kv4 would use
+PyObject *prefix_strides(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&] {
+        Call c(args, n, 8);
+        const Prefix prefix(c, 3, c.integer(0), c.integer(1), c.integer(2));
+        if (!c.none(3) || !c.none(4)) c.stream(7);
+        return Py_BuildValue("LL", static_cast<long long>(prefix.strides[0]), static_cast<long long>(prefix.strides[1]));
+    });
+}
+
 // plan handle, samples, query heads, KV heads, head dim, f32 output?, tokens of the packed prefix, q, prefix_k, prefix_v, prefix stride 0,
 // prefix stride 1, pool, page_indptr, page_indices, suffix_lens, out, lse, workspace, stream
 psa_status_t decode_kv4(PyObject *const *args, Py_ssize_t given)
@@ -398,7 +414,7 @@ psa_status_t mark_tokens(PyObject *const *args, Py_ssize_t given)
 // back to its stream before the current stream's use of it is over.
 PyObject *empty(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
-    try {
+    return guarded([&]() -> PyObject * {
         if (n != 5 || !THPVariable_Check(args[0]) || !PyTuple_Check(args[2])) throw Refused("wrong arguments");
         const at::Tensor &like = THPVariable_Unpack(args[0]);
         const long code = PyLong_AsLong(args[1]);
@@ -418,14 +434,7 @@ PyObject *empty(PyObject *, PyObject *const *args, Py_ssize_t n)
         const at::Tensor t = make();
         if (args[4] == Py_True) t.record_stream(current);
         return THPVariable_Wrap(t);
-    } catch (const Refused &e) {
-        if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, e.what());
-    } catch (const std::exception &e) {
-        PyErr_SetString(PyExc_RuntimeError, e.what());
-    } catch (...) {
-        PyErr_SetString(PyExc_RuntimeError, "unknown error while allocating a call's memory");
-    }
-    return nullptr;
+    });
 }
 
 // path of the C library, which has been loaded already
@@ -458,6 +467,7 @@ PyMethodDef method(const char *name)
 PyMethodDef methods[] = {
     method<build_page_table>("build_page_table"), method<extend_page_table>("extend_page_table"), method<store_kv4>("store_kv4"),
     method<load_kv4>("load_kv4"), method<decode_kv4>("decode_kv4"), method<process_logits>("process_logits"), method<mark_tokens>("mark_tokens"),
+    {"prefix_strides", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&prefix_strides)), METH_FASTCALL, nullptr},
     {"empty", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&empty)), METH_FASTCALL, nullptr},
     {"attach", attach, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr},
 };

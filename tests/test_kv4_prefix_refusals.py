@@ -49,8 +49,9 @@ def test_refusals():
                             (bf(40, H, D), bf(40, H, D), dict(prefix_strides=(2 * H * D, D)), "at these strides"),
                             (bf(40, H, D), bf(40, H, D), dict(prefix_strides=(2 ** 62, D)), "at these strides"),
                             (fused[1:, 0], fused[:, H], dict(prefix_strides=((2 * H + 3) * D, D)), "prefix_k must hold")):
-        with pytest.raises(ValueError, match=match):
-            call([40], [2], k, v, **kw)
+        for stage in ("all", "prefix"):
+            with pytest.raises(ValueError, match=match):
+                call([40], [2], k, v, stage=stage, **kw)
     with pytest.raises(ValueError, match="at least 1040"):
         call([40, 1000], [2, 0], bf(1039, H, D), bf(1040, H, D))
     with pytest.raises(ValueError, match="at least 60"):
