@@ -517,6 +517,49 @@ psa_status_t psa_mark_tokens(const int32_t *ids, int32_t num_ids, const int32_t 
                              int64_t row_words, void *cuda_stream);
 
 /*
+ * psa_store_kv writes token t of new_k / new_v (bf16, element (t, head, d) at t*kv_strides[0] + head*kv_strides[1] + d) into
+ * slot_map[t] (page * 16 + position, as psa_build_page_table and psa_extend_page_table give them) of the pools of psa_decode and
+ * psa_attend_paged (pool_strides as for psa_attend_paged); a negative slot is skipped, one beyond num_pool_pages is skipped and raises
+ * PSA_ERR_BOUNDS in *status (device, may be NULL).  The slots of one call must be distinct.  D in {64, 128}; pointers 16-byte aligned,
+ * strides multiples of 8 elements.  Enqueues one kernel.
+ */
+psa_status_t psa_store_kv(const void *new_k, const void *new_v, const int64_t kv_strides[2], const int64_t *slot_map, int64_t num_tokens,
+                          int32_t num_kv_heads, int32_t head_dim, void *k_pool, void *v_pool, const int64_t pool_strides[3],
+                          int64_t num_pool_pages, int32_t *status, void *cuda_stream);
+/*
+ * Several new tokens per sample at once, over a cache in pages: a new turn of a running sample, drafted tokens to be verified, an
+ * answer to be scored, a long prompt in chunks.  psa_extend_page_table gives the tokens their slots, psa_store_kv writes them, and
+ * psa_attend_paged attends: sample s holds S = kv_lens[s] tokens, the n = q_indptr[s+1] - q_indptr[s] new ones last, and new token i
+ * sees the tokens up to its own position S - n + i,
+ *     out[row, h, :] = softmax_{j <= S - n + i}( sm_scale * q[row, h, :] . k_j ) . v_j ,   lse = ln sum_j exp(...),   row = q_indptr[s] + i.
+ * A row that sees nothing (S < n) gets out = 0 and lse = -inf.  n may be 0, 1 (a decode step) or anything else.
+ *   q              [num_tokens, Hq, D] bf16 device; element (row, h, d) at row*q_strides[0] + h*q_strides[1] + d.
+ *   q_indptr       [B+1] int32 device, not descending; NULL: one token per sample.  Rows from q_indptr[B] on are left as they are.
+ *   k_pool, v_pool bf16 device; (page, head, slot, d) at page*pool_strides[0] + head*pool_strides[1] + slot*pool_strides[2] + d.
+ *   page_indptr, page_indices, kv_lens   as for psa_decode (int32 device), num_entries entries in page_indices.
+ *   prior_out, prior_lse   or NULL: the same rows attended over other keys (their shared prompt, by psa_decode with a plan whose
+ *                  samples are these rows), [num_tokens, Hq, D] of prior_dtype and [num_tokens, Hq] f32; the two are joined as
+ *                  psa_decode joins its stages.  They may be out and lse themselves (same type), otherwise they do not overlap.
+ *   out, lse       [num_tokens, Hq, D] of out_dtype, [num_tokens, Hq] f32, contiguous.
+ *   status         int32 device or NULL: receives PSA_ERR_BOUNDS (see psa_read_status) for a page id outside 0 .. num_pool_pages-1 (its
+ *                  keys count as zeros), a list that is too short for kv_lens or a negative length (the sample counts as empty), and
+ *                  q_indptr that descends; PSA_ERR_TIMEOUT if a wait inside the kernel ran out.
+ *   scratch        device, 256-byte aligned, psa_attend_paged_scratch_bytes(...) bytes, overwritten by every call (calls that share it
+ *                  must be ordered on one stream).
+ * What stands in the pages behind a sample's last token does not matter, NaN included.  Within the new tokens V has to be finite
+ * where earlier rows are to be: a tile's products are taken with weight 0 for what a row does not see.
+ * D in {64, 128}, Hq / Hkv in {1, 2, 4, 8}; pointers 16-byte aligned, strides multiples of 8 elements; at most 2^20 samples and 2^24
+ * new tokens.  Weights are rounded to bf16 as in psa_decode.  Enqueues three kernels.
+ */
+size_t psa_attend_paged_scratch_bytes(int64_t num_tokens, int32_t num_samples, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim);
+psa_status_t psa_attend_paged(const void *q, const int64_t q_strides[2], const int32_t *q_indptr, int64_t num_tokens, int32_t num_samples,
+                              int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, float sm_scale, const void *k_pool,
+                              const void *v_pool, const int64_t pool_strides[3], int64_t num_pool_pages, const int32_t *page_indptr,
+                              const int32_t *page_indices, int64_t num_entries, const int32_t *kv_lens, const void *prior_out,
+                              int32_t prior_dtype, const float *prior_lse, void *out, int32_t out_dtype, float *lse, int32_t *status,
+                              void *scratch, size_t scratch_bytes, void *cuda_stream);
+
+/*
  * Self-test of the device-side error path (no counterpart in the paper).  Enqueues one tiny kernel whose only
  * wait is on a barrier that nothing completes; the wait gives up after `limit_ns` (<= 1 s), the kernel writes
  * PSA_ERR_TIMEOUT into the status word of `workspace` and exits normally.  psa_check_status then reports and

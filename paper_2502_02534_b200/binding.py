@@ -22,6 +22,7 @@ EXPORTED_SYMBOLS = [
     "psa_decode_host_staging_bytes", "psa_decode_host", "psa_check_status", "psa_selftest_bounded_wait", "psa_append_kv", "psa_append_kv_alloc", "psa_validate_page_table", "psa_sample_scratch_bytes", "psa_sample_tokens", "psa_sample_tokens_at", "psa_attn_task",
     "psa_page_table_scratch_bytes", "psa_build_page_table", "psa_extend_page_table", "psa_read_status", "psa_kv4_cell_bytes", "psa_store_kv4",
     "psa_load_kv4", "psa_plan_create_kv4", "psa_decode_kv4", "psa_decode_suffix_kv4", "psa_process_logits", "psa_mark_tokens",
+    "psa_store_kv", "psa_attend_paged_scratch_bytes", "psa_attend_paged",
     "psa_status_string", "psa_last_error_message", "psa_version",
 ]
 
@@ -157,6 +158,13 @@ def library():
         lib.psa_process_logits.argtypes = [P, c_int32, c_int64, c_int32, c_int32, POINTER(_LogitsRules), P, c_int32, c_int64, P]
         lib.psa_mark_tokens.restype = c_int32
         lib.psa_mark_tokens.argtypes = [P, c_int32, P, c_int32, c_int32, P, c_int64, P]
+        lib.psa_store_kv.restype = c_int32
+        lib.psa_store_kv.argtypes = [P, P, POINTER(c_int64), P, c_int64, c_int32, c_int32, P, P, POINTER(c_int64), c_int64, P, P]
+        lib.psa_attend_paged_scratch_bytes.restype = c_size_t
+        lib.psa_attend_paged_scratch_bytes.argtypes = [c_int64, c_int32, c_int32, c_int32, c_int32]
+        lib.psa_attend_paged.restype = c_int32
+        lib.psa_attend_paged.argtypes = [P, POINTER(c_int64), P, c_int64, c_int32, c_int32, c_int32, c_int32, c_float, P, P, POINTER(c_int64), c_int64, P, P,
+                                         c_int64, P, P, c_int32, P, P, c_int32, P, P, P, c_size_t, P]
         lib.psa_status_string.restype = c_char_p
         lib.psa_status_string.argtypes = [c_int32]
         lib.psa_last_error_message.restype = c_char_p
@@ -687,3 +695,51 @@ def mark_tokens(ids, indptr, vocab, bits=None, *, stream=None):
     if rc:
         _check(rc)
     return bits
+
+
+# ---- several new tokens per sample over the bf16 cache, checked and marshalled as above
+
+def store_kv(new_k, new_v, slot_map, k_pool, v_pool, *, status=None, stream=None):
+    """psa_store_kv: write new_k / new_v [T, Hkv, D] bf16 (any token and head stride, the same for both) into the slots of the pools
+    [pages, Hkv, 16, D] bf16 (any strides, the same for both; the last dimension contiguous)."""
+    if status is not None:
+        status = _status_tensor(status)
+    rc = (_calls or _native()).store_kv(new_k, new_v, slot_map, k_pool, v_pool, status, stream)
+    if rc:
+        _check(rc)
+
+
+def attend_paged_scratch(num_tokens, num_samples, num_q_heads, num_kv_heads, head_dim):
+    """Scratch tensor for attend_paged, to be kept by callers that must not allocate (uint8)."""
+    import torch
+    return torch.empty(int(library().psa_attend_paged_scratch_bytes(num_tokens, num_samples, num_q_heads, num_kv_heads, head_dim)), dtype=torch.uint8, device="cuda")
+
+
+def attend_paged(q, k_pool, v_pool, page_indptr, page_indices, kv_lens, q_indptr=None, out=None, lse=None, *, sm_scale=None, prior_out=None,
+                 prior_lse=None, status=None, scratch=None, stream=None):
+    """psa_attend_paged on torch CUDA tensors: the new tokens q [T, Hq, D] bf16 (any token and head stride) of every sample, rows
+    q_indptr[s] .. q_indptr[s + 1] (one each when None), over the sample's kv_lens[s] tokens in pages, which end with the new ones; each sees
+    what stands up to itself.  prior_out / prior_lse: the same rows over other keys, joined with the result.  out [T, Hq, D] bf16 or f32
+    (bf16 when None), lse [T, Hq] f32.  Returns (out, lse)."""
+    if q.dim() != 3 or k_pool.dim() != 4:
+        raise ValueError("q must be [tokens, heads, head_dim] and the pools [pages, heads, 16, head_dim]")
+    if status is not None:
+        status = _status_tensor(status)
+    if out is None:
+        out = _new3(q, stream)
+    if lse is None:
+        lse = _new(tuple(q.shape[:2]), q, stream, "float32")
+    if scratch is None:
+        nbytes = library().psa_attend_paged_scratch_bytes(q.shape[0], kv_lens.numel(), q.shape[1], k_pool.shape[1], q.shape[2])
+        scratch = _scratch(nbytes, q, stream)
+    rc = (_calls or _native()).attend_paged(q, k_pool, v_pool, page_indptr, page_indices, kv_lens, q_indptr, out, lse,
+                                            q.shape[-1] ** -0.5 if sm_scale is None else sm_scale, prior_out, prior_lse, status, scratch, stream)
+    if rc:
+        _check(rc)
+    return out, lse
+
+
+def _new3(like, stream):
+    """_new of the shape and type of the three-dimensional `like`."""
+    T, H, D = like.shape
+    return _new((T * H, D), like, stream).view(T, H, D)

@@ -1,0 +1,218 @@
+// What the kernels over chunks of new tokens share (attention: chunk_sm100.cu; weights of cached tokens: weights_sm100.cu): a call's
+// arguments, the checks of a sample's entries, and how the work is cut into equal shares.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include "psa_internal.h"
+
+namespace psa {
+
+constexpr int kScheduleThreads = 1024;
+constexpr int kGroupRows = 256;                              // rows of a group: two row tiles of 128
+constexpr int kMostBlocks = 160;                             // persistent blocks, at most one per SM
+constexpr int64_t kMostChunkPages = int64_t(1) << 27, kMostChunkEntries = (int64_t(1) << 31) - 256;
+
+struct ChunkHeader {
+    long long per_head;    // cost of one KV head's groups
+    int32_t groups, blocks;
+};
+// Up to kGroupRows rows of one sample: consecutive new tokens and the group's query heads, head fastest.
+struct ChunkGroup {
+    long long cum;         // cost of the groups before it
+    int32_t q0, n_tok;     // rows of q
+    int32_t pos0, keys;    // position of the first token (negative: it sees nothing), keys that the last one sees
+    int32_t list0, pad;    // where the sample's pages start in page_indices
+};
+static_assert(sizeof(ChunkGroup) == 32, "");
+
+struct ChunkArgs {
+    int64_t num_tokens, num_entries;
+    int32_t num_samples, num_q_heads, num_kv_heads, group, num_pool_pages;
+    const int32_t *q_indptr, *kv_lens, *page_indptr, *page_indices;
+    int32_t *status;
+    float scale_log2;
+    const void *prior_out;
+    const float *prior_lse;
+    void *out;
+    float *lse;
+    bool prior_f32, out_f32;
+    // scratch
+    int32_t blocks, max_groups, slot_rows;
+    ChunkHeader *header;
+    ChunkGroup *groups;
+    float *partial_lse, *partial_o;    // [2 * blocks, slot_rows] log2, [2 * blocks, slot_rows, D] normalised
+};
+
+#ifdef __CUDACC__
+__device__ __forceinline__ void raise(int32_t *status, int code)
+{
+    if (status) atomicCAS(status, 0, code);
+}
+
+// A sample's entries, made safe: n new tokens from row q0 on, len keys in pages from list0 on.  What does not hold together raises
+// PSA_ERR_BOUNDS; a sample whose keys do not fit its list counts as empty.
+struct ChunkSample { int q0, n, len, list0; };
+__device__ __forceinline__ ChunkSample chunk_sample(const ChunkArgs &a, int s)
+{
+    const int tokens = int(a.num_tokens);
+    int b0 = s, b1 = s + 1;
+    if (a.q_indptr) {
+        const int r0 = a.q_indptr[s], r1 = a.q_indptr[s + 1];
+        b0 = min(max(r0, 0), tokens);
+        b1 = min(max(r1, b0), tokens);
+        if (b0 != r0 || b1 != r1) raise(a.status, PSA_ERR_BOUNDS);
+    }
+    if (b1 == b0) return {b0, 0, 0, 0};
+    const int l0 = a.page_indptr[s], l1 = a.page_indptr[s + 1];
+    int len = a.kv_lens[s];
+    if (l0 < 0 || l1 < l0 || l1 > a.num_entries || len < 0 || len > (long long)(l1 - l0) * kPageSize) {
+        raise(a.status, PSA_ERR_BOUNDS);
+        len = 0;
+    }
+    return {b0, b1 - b0, len, l0};
+}
+__device__ __forceinline__ ChunkGroup chunk_group(const ChunkSample &c, int i, int per_group)
+{
+    ChunkGroup g{};
+    const int first = i * per_group;
+    g.q0 = c.q0 + first;
+    g.n_tok = min(per_group, c.n - first);
+    g.pos0 = c.len - c.n + first;
+    g.keys = max(0, g.pos0 + g.n_tok);
+    g.list0 = c.list0;
+    return g;
+}
+
+// Cost of a piece in quarters of a key tile of two row tiles.  A single row tile's key tile costs three: half the arithmetic, but as many
+// bytes.  kPieceCost: loading Q, the first tiles' way, the epilogue.
+constexpr int kPieceCost = 4;
+constexpr int kLeastCost = 12;    // a share is not made smaller than this
+__device__ __forceinline__ int chunk_tiles(int keys) { return (keys + 127) >> 7; }
+__device__ __forceinline__ int chunk_weight(const ChunkGroup &g, int group) { return g.n_tok * group > 128 ? 4 : 3; }
+__device__ __forceinline__ long long chunk_cost(const ChunkGroup &g, int group)
+{
+    return kPieceCost + (long long)chunk_tiles(g.keys) * chunk_weight(g, group);
+}
+// shares of [0, total): share i of n starts here
+__device__ __forceinline__ long long share_begin(long long total, int i, int n) { return total / n * i + total % n * i / n; }
+// the first key tile of a group at `base` that belongs behind x
+__device__ __forceinline__ int tile_at(const ChunkGroup &g, int group, long long base, long long x)
+{
+    const long long y = x - base - kPieceCost;
+    if (y <= 0) return 0;
+    const int tiles = chunk_tiles(g.keys), w = chunk_weight(g, group);
+    return y >= (long long)tiles * w ? tiles : int(uint32_t(y) / uint32_t(w));
+}
+// the head and group that x lies in, searched by a whole warp
+__device__ __forceinline__ void locate(const ChunkArgs &a, const ChunkHeader &h, long long x, int lane, int *head, int *group)
+{
+    *head = int(x / h.per_head);
+    const long long y = x - *head * h.per_head;
+    int lo = 0, hi = h.groups;
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 31) >> 5, at = lo + lane * step;
+        const unsigned below = __ballot_sync(0xffffffffu, at < hi && a.groups[at].cum <= y);
+        lo += (__popc(below) - 1) * step;
+        hi = min(hi, lo + step);
+    }
+    *group = lo;
+}
+
+struct ChunkPiece {
+    ChunkGroup g;
+    int head, t0, t1;      // key tiles
+    bool split;            // not the whole group: the result is partial and goes to `slot`
+    int slot;
+};
+// The pieces of one block's share, in order.
+struct ChunkWalk {
+    const ChunkArgs &a;
+    ChunkHeader h;
+    long long x0 = 0, x1 = 0;
+    int block, head, gi = 0;
+    __device__ __forceinline__ ChunkWalk(const ChunkArgs &args, int b, int lane) : a(args), h(*args.header), block(b)
+    {
+        head = a.num_kv_heads;
+        if (block >= h.blocks || h.groups == 0) return;
+        const long long total = h.per_head * a.num_kv_heads;
+        x0 = share_begin(total, block, h.blocks);
+        x1 = share_begin(total, block + 1, h.blocks);
+        locate(a, h, x0, lane, &head, &gi);
+    }
+    __device__ __forceinline__ bool next(ChunkPiece &p)
+    {
+        for (;;) {
+            if (gi >= h.groups) {
+                gi = 0;
+                ++head;
+            }
+            if (head >= a.num_kv_heads) return false;
+            p.g = a.groups[gi];
+            const long long base = head * h.per_head + p.g.cum;
+            if (base >= x1) {
+                head = a.num_kv_heads;
+                return false;
+            }
+            ++gi;
+            p.head = head;
+            const int tiles = chunk_tiles(p.g.keys);
+            p.t0 = tile_at(p.g, a.group, base, x0);
+            p.t1 = tile_at(p.g, a.group, base, x1);
+            p.split = false;
+            p.slot = 0;
+            if (tiles == 0) {
+                if (base < x0) continue;     // the share where it starts has it
+                return true;
+            }
+            if (p.t1 <= p.t0) continue;
+            p.split = p.t0 > 0 || p.t1 < tiles;
+            p.slot = 2 * block + (p.t0 > 0 ? 0 : 1);
+            return true;
+        }
+    }
+};
+
+// Two partial results of a row joined: their shares and the joint log2-sum-exp.
+struct Joined { float first, second, lse2; };
+__device__ __forceinline__ Joined join(float a2, float b2)
+{
+    const float top = fmaxf(a2, b2);
+    if (top == -INFINITY) return {0.f, 0.f, -INFINITY};
+    const float wa = exp2f(a2 - top), wb = exp2f(b2 - top), sum = wa + wb;
+    return {wa / sum, wb / sum, top + log2f(sum)};
+}
+// 32 columns of the earlier result
+__device__ __forceinline__ void add_prior(const ChunkArgs &a, size_t at, float w, float (&v)[32])
+{
+    if (a.prior_f32) {
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) {
+            const float4 p = *reinterpret_cast<const float4 *>(static_cast<const float *>(a.prior_out) + at + i);
+            v[i] = fmaf(w, p.x, v[i]); v[i + 1] = fmaf(w, p.y, v[i + 1]); v[i + 2] = fmaf(w, p.z, v[i + 2]); v[i + 3] = fmaf(w, p.w, v[i + 3]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 32; i += 8) {
+            const uint4 p = *reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(a.prior_out) + at + i);
+            const uint32_t u[4] = {p.x, p.y, p.z, p.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                v[i + 2 * k] = fmaf(w, __uint_as_float(u[k] << 16), v[i + 2 * k]);
+                v[i + 2 * k + 1] = fmaf(w, __uint_as_float(u[k] & 0xffff0000u), v[i + 2 * k + 1]);
+            }
+        }
+    }
+}
+#endif
+
+// chunk_sm100.cu: places in a call's scratch memory (sets the pointers; returns the bytes), checks, tensor maps of q and the pools
+size_t chunk_layout(ChunkArgs &a, void *scratch, int head_dim);
+psa_status_t chunk_check(const ChunkArgs &a, const void *q, const int64_t q_strides[2], const void *pool, const int64_t pool_strides[3], int head_dim);
+psa_status_t chunk_maps(const ChunkArgs &a, const void *q, const int64_t q_strides[2], const void *const *pools, int num_pools,
+                        const int64_t pool_strides[3], int head_dim, CUtensorMap *maps);
+int multiprocessors();   // of the current device; 0: there is none
+
+}  // namespace psa

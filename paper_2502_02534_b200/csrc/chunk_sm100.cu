@@ -1,0 +1,812 @@
+// Attention of several new tokens per sample over a paged K/V cache (psa_attend_paged).
+//
+// Sample s holds S keys in its pages, the last n of them its new tokens; new token i stands at position S - n + i and sees the keys up to
+// its own:   out = softmax_{j <= S - n + i}(sm_scale q.k_j) . v_j,   lse = ln sum exp.   Optionally an earlier partial result of the same
+// rows over other keys (prior_out, prior_lse) is folded in:  L = ln(e^lse + e^prior_lse),  out = e^(lse - L) out + e^(prior_lse - L) prior_out.
+//
+// Three launches.  chunk_schedule_kernel cuts every sample's new tokens into GROUPS of up to 256 rows (256 / G tokens x G query heads) and
+// writes their running costs (key tiles).  chunk_kernel is persistent: block i takes the i-th equal share of all (KV head, group, key
+// tile) units, in order, so every SM has the same work whatever the lengths are, and a group is cut only where a share ends.  What is cut
+// leaves partial results, two slots a block at most, which chunk_merge_kernel joins; groups that were not cut are finished in place.
+//
+// chunk_kernel, 10 warps: 0-3 and 4-7 softmax warpgroups (streams 0 and 1), 8 TMA producer, 9 MMA issuer (one lane) and owner of the
+// tensor memory.  Key tiles of 128 keys arrive page by page (one TMA box of 16 tokens x 64 channels each) in a ring; S = Q K^T goes to
+// tensor memory, a warpgroup (thread = row) turns it into P (bf16, over S), O += P V.  More than 128 rows: each stream has a row tile and
+// both read every key tile.  Up to 128 rows: the streams take alternate key tiles of the one row tile, each with an accumulator of its
+// own, joined at the end.  P is handed over in halves of 64 keys, so that the first half's products run under the second half's
+// exponentials.  The reference maximum moves only when a half's exponents exceed it by 2^8 (which its sum tells).
+//
+// What does not exist is never used: products stop at the last page, rows of V behind the last key are zeroed in shared memory (they may
+// hold anything), scores behind a row's last key become -inf.  Page ids outside the pool read as zeros (TMA bounds) and raise
+// PSA_ERR_BOUNDS.  Every wait is bounded.
+#include <cuda_bf16.h>
+
+#include <algorithm>
+
+#include "chunk.h"
+#include "psa_internal.h"
+#include "tensor_core.cuh"
+
+namespace psa {
+namespace {
+
+constexpr int kTileKeys = 128;
+constexpr int kRowTile = 128;
+constexpr int kPagesPerTile = kTileKeys / kPageSize;
+constexpr float kThreshold = 8.f;                      // log2 units
+constexpr float kHalfSumLimit = 64.f * 256.f * 1.01f;  // 64 exponentials of at most 2^8
+// P is truncated to bf16; exponents carry log2 of 1 / (1 - 2^-8 / (2 ln 2)), what truncation loses on average, and the sums are freed of it
+constexpr float kBias = 0.0040709119f, kUnbias = 0.99718224f;
+constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
+
+__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void grid_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+// ------------------------------------------------------------------------------------------------------------- schedule
+// Running sums over the samples by one block; every thread takes samples of its own (a sample's groups one after another).
+__global__ void __launch_bounds__(kScheduleThreads)
+chunk_schedule_kernel(ChunkArgs a)
+{
+    __shared__ long long sum_cost[kScheduleThreads / 32];
+    __shared__ int sum_groups[kScheduleThreads / 32];
+    grid_release();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int per_group = kGroupRows / a.group;   // tokens
+    long long carry_cost = 0;
+    int carry_groups = 0;
+    for (int s0 = 0; s0 < a.num_samples; s0 += kScheduleThreads) {
+        const int s = s0 + int(threadIdx.x);
+        ChunkSample c{};
+        int groups = 0;
+        long long cost = 0;
+        if (s < a.num_samples) {
+            c = chunk_sample(a, s);
+            groups = (c.n + per_group - 1) / per_group;
+            for (int i = 0; i < groups; ++i) cost += chunk_cost(chunk_group(c, i, per_group), a.group);
+        }
+        // exclusive scans over the block
+        long long x = cost;
+        int y = groups;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const long long ux = __shfl_up_sync(0xffffffffu, x, d);
+            const int uy = __shfl_up_sync(0xffffffffu, y, d);
+            if (lane >= d) { x += ux; y += uy; }
+        }
+        if (lane == 31) { sum_cost[warp] = x; sum_groups[warp] = y; }
+        __syncthreads();
+        long long before_cost = carry_cost;
+        int before_groups = carry_groups;
+        for (int w = 0; w < kScheduleThreads / 32; ++w) {
+            if (w < warp) { before_cost += sum_cost[w]; before_groups += sum_groups[w]; }
+            carry_cost += sum_cost[w];
+            carry_groups += sum_groups[w];
+        }
+        __syncthreads();
+        long long at = before_cost + x - cost;
+        int to = before_groups + y - groups;
+        for (int i = 0; i < groups; ++i, ++to) {
+            ChunkGroup g = chunk_group(c, i, per_group);
+            g.cum = at;
+            at += chunk_cost(g, a.group);
+            if (to < a.max_groups) a.groups[to] = g;
+        }
+    }
+    if (threadIdx.x == 0) {
+        if (carry_groups > a.max_groups) {   // q_indptr that runs backwards: more rows than there are
+            raise(a.status, PSA_ERR_BOUNDS);
+            carry_groups = 0;
+            carry_cost = 0;
+        }
+        const long long total = carry_cost * a.num_kv_heads;
+        ChunkHeader h{};
+        h.per_head = carry_cost;
+        h.groups = carry_groups;
+        h.blocks = int(max(1ll, min((long long)a.blocks, total / kLeastCost)));
+        *a.header = h;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------------- attention
+template <int D>
+struct ChunkSmem {
+    static constexpr int kHalves = D / 64;
+    static constexpr int kHalfBytes = 128 * 128;                 // 128 rows x 64 bf16
+    static constexpr int kTileBytes = kHalves * kHalfBytes;      // a tile of Q, K or V
+    static constexpr int kRing = D == 128 ? 5 : 10;
+    static constexpr int kBarQFull = 0, kBarQEmpty = 2, kBarFull = 4, kBarEmpty = kBarFull + kRing, kBarS = kBarEmpty + kRing, kBarP = kBarS + 2,
+                         kBarHalf = kBarP + 4, kBarDone = kBarHalf + 2, kBarMet = kBarDone + 2, kBarDrain = kBarMet + 1, kNumBars = kBarDrain + 1;
+    static constexpr int kTmemPtrOff = 8 * kNumBars, kAbortOff = kTmemPtrOff + 4;
+    static constexpr int kExchangeOff = 1024;                    // (m, l) of both streams' rows
+    static constexpr int kQOff = 3072;
+    static constexpr int kRingOff = kQOff + 2 * kTileBytes;
+    static constexpr int kTotal = kRingOff + kRing * kTileBytes;
+    static_assert(kAbortOff + 4 <= kExchangeOff && kTotal <= 227 * 1024, "shared memory plan");
+};
+
+// Element m of the order in which K and V tiles travel: alternating with two row tiles, K two tiles ahead with one.
+struct Travel { int tile; bool is_v; };
+__device__ __forceinline__ Travel travel(int m, int n, bool two)
+{
+    if (two || n == 1) return {m >> 1, (m & 1) != 0};
+    if (m < 2) return {m, false};
+    const int r = m - 2, both = 2 * (n - 2);
+    if (r < both) return {(r >> 1) + (r & 1) * 2, (r & 1) == 0};
+    return {n - 2 + r - both, true};
+}
+// place of V tile i in that order
+__device__ __forceinline__ int v_place(int i, int n, bool two) { return two ? 2 * i + 1 : i < n - 1 ? 2 * i + 2 : 2 * n - 1; }
+
+// 32 columns of one row to global memory
+__device__ __forceinline__ void store_f32(float *to, const float (&v)[32])
+{
+#pragma unroll
+    for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4 *>(to + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+}
+__device__ __forceinline__ void store_bf16(__nv_bfloat16 *to, const float (&v)[32])
+{
+#pragma unroll
+    for (int i = 0; i < 32; i += 8) {
+        uint32_t w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const __nv_bfloat162 p = __floats2bfloat162_rn(v[i + 2 * k], v[i + 2 * k + 1]);
+            w[k] = reinterpret_cast<const uint32_t &>(p);
+        }
+        *reinterpret_cast<uint4 *>(to + i) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+template <int D>
+__global__ void __launch_bounds__(320, 1)
+chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+             const ChunkArgs a)
+{
+    using L = ChunkSmem<D>;
+    constexpr int kProducerWarp = 8, kMmaWarp = 9;
+    constexpr int kKSteps = D / 16;
+    constexpr uint32_t kIdescQK = make_idesc(kTileKeys, false), kIdescPV = make_idesc(D, true);
+    constexpr uint32_t kColO = 256;                    // S[t] at 128 t, O[t] at 256 + t D
+
+    extern __shared__ __align__(1024) unsigned char smem[];
+    const uint32_t sbase = smem_u32(smem);
+    if (sbase & 1023u) {   // swizzled tiles need a 1024-byte aligned base; refuse to run rather than read garbage
+        if (threadIdx.x == 0) raise(a.status, PSA_ERR_BOUNDS);
+        return;
+    }
+    volatile uint32_t *tmem_ptr = reinterpret_cast<volatile uint32_t *>(smem + L::kTmemPtrOff);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + L::kAbortOff);
+    auto bar = [&](int i) { return sbase + 8 * i; };
+    auto bar_p = [&](int t, int h) { return bar(L::kBarP + 2 * t + h); };
+    auto warp_wait = [&](uint32_t b, uint32_t parity) {   // the whole warp goes on, or the whole warp gives up
+        return __all_sync(0xffffffffu, mbar_wait(b, parity, abort_flag)) != 0;
+    };
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        *abort_flag = 0;
+        for (int i = 0; i < L::kNumBars; ++i) mbar_init(bar(i), i >= L::kBarP && i < L::kBarHalf ? 128 : i == L::kBarMet ? 256 : 1);
+        fence_barrier_init();
+    }
+    if (warp == kMmaWarp) {
+        tmem_alloc(smem_u32(const_cast<uint32_t *>(tmem_ptr)), 512);
+        tmem_relinquish();
+    }
+    if (warp == kProducerWarp && elect_one()) { prefetch_tensormap(&map_q); prefetch_tensormap(&map_k); prefetch_tensormap(&map_v); }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_ptr;
+    grid_wait();
+    grid_release();
+
+    ChunkWalk walk(a, blockIdx.x, lane);
+    ChunkPiece pc;
+
+    if (warp == kProducerWarp) {
+        // ------------------------------------------------------------ TMA producer, one box per lane
+        uint32_t e = 0, q_uses[2] = {0, 0}, q_sel = 0;
+        bool ok = true;
+        while (ok && walk.next(pc)) {
+            const int n = pc.t1 - pc.t0;
+            if (n == 0) continue;
+            const bool two = pc.g.n_tok * a.group > kRowTile;
+            auto page_of = [&](int m) {   // this lane's page of element m
+                const int page = (pc.t0 + travel(m, n, two).tile) * kPagesPerTile + lane / L::kHalves;
+                if (lane >= kPagesPerTile * L::kHalves || page * kPageSize >= pc.g.keys) return 0;
+                return a.page_indices[pc.g.list0 + page];   // inside the list: the schedule saw to that
+            };
+            int id = page_of(0);
+            for (int m = 0; ok && m < 2 * n; ++m, ++e) {
+                const Travel tr = travel(m, n, two);
+                const int next = m + 1 < 2 * n ? page_of(m + 1) : 0;
+                const int slot = e % L::kRing, use = e / L::kRing;
+                if (use > 0 && !(ok = warp_wait(bar(L::kBarEmpty + slot), (use - 1) & 1))) break;
+                const int left = pc.g.keys - (pc.t0 + tr.tile) * kTileKeys;
+                const int pages = min(kPagesPerTile, (left + kPageSize - 1) / kPageSize);
+                const uint32_t full = bar(L::kBarFull + slot), dst = sbase + L::kRingOff + slot * L::kTileBytes;
+                if (lane == 0) mbar_expect_tx(full, pages * kPageSize * D * 2);
+                __syncwarp();
+                if (lane < pages * L::kHalves) {
+                    const int p = lane / L::kHalves, h = lane % L::kHalves;
+                    if (id < 0 || id >= a.num_pool_pages) {
+                        raise(a.status, PSA_ERR_BOUNDS);
+                        id = a.num_pool_pages;   // outside the map: zeros
+                    }
+                    tma_load_4d(dst + h * L::kHalfBytes + p * kPageSize * 128, tr.is_v ? &map_v : &map_k, full, h * 64, 0, pc.head, id);
+                }
+                id = next;
+                if (m == 0) {   // Q behind the first K tile
+                    const int tiles = two ? 2 : 1;
+                    for (int t = 0; ok && t < tiles; ++t) {
+                        const int b = two ? t : int(q_sel);
+                        if (q_uses[b] > 0 && !(ok = warp_wait(bar(L::kBarQEmpty + b), (q_uses[b] - 1) & 1))) break;
+                        ++q_uses[b];
+                        if (lane == 0) {
+                            mbar_expect_tx(bar(L::kBarQFull + b), L::kTileBytes);
+                            for (int h = 0; h < L::kHalves; ++h)
+                                tma_load_4d(sbase + L::kQOff + b * L::kTileBytes + h * L::kHalfBytes, &map_q, bar(L::kBarQFull + b), h * 64, 0, pc.head,
+                                            pc.g.q0 + t * (kRowTile / a.group));
+                        }
+                    }
+                    if (!two) q_sel ^= 1;
+                }
+            }
+        }
+    } else if (warp == kMmaWarp) {
+        // ------------------------------------------------------------ MMA issuer.  Unit u of a piece: stream u & 1, key tile u / 2 (two row
+        // tiles) or u (one).  QK^T runs two units ahead of PV.
+        if (elect_one()) {
+            constexpr uint64_t kHi = uint64_t(smem_desc_hi(1024)) << 32;
+            const uint64_t q_desc = kHi | smem_desc_lo(sbase + L::kQOff, 16);
+            const uint64_t k_desc = kHi | smem_desc_lo(sbase + L::kRingOff, 16);               // K-major
+            const uint64_t v_desc = kHi | smem_desc_lo(sbase + L::kRingOff, L::kHalfBytes);    // MN-major, halves kHalfBytes apart
+            uint32_t e = 0, q_uses[2] = {0, 0}, q_sel = 0, uses[2] = {0, 0};
+            bool ok = true;
+            auto landed = [&]() {   // waits for the next element; its slot
+                const int slot = e % L::kRing;
+                ok = mbar_wait(bar(L::kBarFull + slot), (e / L::kRing) & 1, abort_flag);
+                ++e;
+                return slot;
+            };
+            while (ok && walk.next(pc)) {
+                const int n = pc.t1 - pc.t0;
+                if (n == 0) continue;
+                const bool two = pc.g.n_tok * a.group > kRowTile;
+                const int units = two ? 2 * n : n;
+                const int qb = two ? 0 : int(q_sel);
+                for (int t = 0; ok && t < (two ? 2 : 1); ++t) {
+                    ok = mbar_wait(bar(L::kBarQFull + qb + t), q_uses[qb + t] & 1, abort_flag);
+                    ++q_uses[qb + t];
+                }
+                if (!two) q_sel ^= 1;
+                int k_slot = 0, v_slot = 0;
+                auto issue_qk = [&](int u) {
+                    const int t = u & 1;
+                    if (!two || t == 0) k_slot = landed();
+                    if (!ok) return;
+                    tc_fence_after();
+                    const uint64_t q = q_desc + uint32_t(two ? t : qb) * (L::kTileBytes >> 4);
+                    const uint64_t k = k_desc + uint32_t(k_slot) * (L::kTileBytes >> 4);
+                    const uint32_t d = tmem_base + uint32_t(t) * 128;
+#pragma unroll
+                    for (int i = 0; i < kKSteps; ++i) {
+                        const uint32_t off = ((i / 4) * L::kHalfBytes + (i % 4) * 32) >> 4;
+                        if (i == 0) mma_ss<false>(d, q + off, k + off, kIdescQK);
+                        else mma_ss<true>(d, q + off, k + off, kIdescQK);
+                    }
+                    tc_commit(bar(L::kBarS + t));
+                    if (!two || t == 1) tc_commit(bar(L::kBarEmpty + k_slot));
+                    if (two ? u + 2 >= units : u + 1 == units) tc_commit(bar(L::kBarQEmpty + (two ? t : qb)));
+                };
+                for (int u = 0; ok && u < 2 && u < units; ++u) issue_qk(u);
+                for (int u = 0; ok && u < units; ++u) {
+                    const int t = u & 1, tile = pc.t0 + (two ? u >> 1 : u);
+                    if (!two || t == 0) v_slot = landed();
+                    if (!ok) break;
+                    const int steps = min(kPagesPerTile, (pc.g.keys - tile * kTileKeys + kPageSize - 1) / kPageSize);   // of 16 keys
+                    const uint64_t v = v_desc + uint32_t(v_slot) * (L::kTileBytes >> 4);
+                    const uint32_t p = tmem_base + uint32_t(t) * 128, o = tmem_base + kColO + t * D;
+                    const bool first = u < 2;
+                    if (!(ok = mbar_wait(bar_p(t, 0), uses[t] & 1, abort_flag))) break;
+                    tc_fence_after();
+                    mma_ts_p(o, p, v, kIdescPV, first ? 0u : 1u);
+#pragma unroll
+                    for (int i = 1; i < 4; ++i)
+                        if (i < steps) mma_ts(o, p + i * 8, v + ((i * 2048) >> 4), kIdescPV);
+                    tc_commit(bar(L::kBarHalf + t));
+                    if (!(ok = mbar_wait(bar_p(t, 1), uses[t] & 1, abort_flag))) break;
+                    tc_fence_after();
+#pragma unroll
+                    for (int i = 4; i < 8; ++i)
+                        if (i < steps) mma_ts(o, p + i * 8, v + ((i * 2048) >> 4), kIdescPV);
+                    if (!two || t == 1) tc_commit(bar(L::kBarEmpty + v_slot));
+                    ++uses[t];
+                    if (u + 2 < units) issue_qk(u + 2);   // over P of this unit: ordered behind the products just issued
+                    else tc_commit(bar(L::kBarDone + t));
+                }
+            }
+        }
+    } else {
+        // ------------------------------------------------------------ softmax warpgroups and epilogue
+        const int t = warp >> 2;
+        const int row = (warp & 3) * 32 + lane;        // TMEM lane
+        const uint32_t lane_addr = uint32_t((warp & 3) * 32) << 16;
+        const uint32_t s_addr = tmem_base + lane_addr + uint32_t(t) * 128;
+        const uint32_t o_base = tmem_base + lane_addr + kColO;
+        float *exchange = reinterpret_cast<float *>(smem + L::kExchangeOff);   // [stream][m, l][row]
+        uint32_t e = 0, uses = 0, met = 0, done[2] = {0, 0};
+        bool ok = true;
+        while (ok && walk.next(pc)) {
+            const int n = pc.t1 - pc.t0;
+            const int rows = pc.g.n_tok * a.group;
+            const bool two = rows > kRowTile;
+            const int in_group = (two ? t * kRowTile : 0) + row;
+            const bool mine = in_group < rows;
+            const bool active = __any_sync(0xffffffffu, mine);
+            const int token = in_group / a.group;
+            const int sees = mine ? max(0, min(pc.g.keys, pc.g.pos0 + token + 1)) : 0;   // keys the row sees
+            const int my_uses = two ? n : (n - t + 1) / 2;
+            const int tiles = (pc.g.keys + kTileKeys - 1) / kTileKeys;
+            float m_ref = -INFINITY, l_sum = 0.f;
+
+            for (int j = 0; j < my_uses; ++j, ++uses) {
+                const int local = two ? j : 2 * j + t, tile = pc.t0 + local;
+                if (!(ok = warp_wait(bar(L::kBarS + t), uses & 1))) break;
+                tc_fence_after();
+                const int keys_here = pc.g.keys - tile * kTileKeys;
+                if (tile == tiles - 1 && keys_here % kPageSize) {
+                    // rows of V behind the last key may hold anything, and 0 x NaN is NaN: zero what the products will read of them
+                    const uint32_t at = e + v_place(local, n, two);
+                    const int slot = at % L::kRing;
+                    if (!(ok = warp_wait(bar(L::kBarFull + slot), (at / L::kRing) & 1))) break;
+                    const int chunks = (kPageSize - keys_here % kPageSize) * 8;
+                    for (int i = row; i < chunks * L::kHalves; i += 128) {
+                        const int h = i / chunks, c = i % chunks;
+                        *reinterpret_cast<uint4 *>(smem + L::kRingOff + slot * L::kTileBytes + h * L::kHalfBytes + keys_here * 128 + c * 16) = make_uint4(0, 0, 0, 0);
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                }
+                if (!active) {   // no row of this warp exists: whatever stands in these lanes of P stays in their lanes of O
+                    mbar_arrive(bar_p(t, 0));
+                    mbar_arrive(bar_p(t, 1));
+                    continue;
+                }
+                const int valid = sees - tile * kTileKeys;
+                uint32_t s0[2][32], s1[2][32];
+                auto load = [&](int h, uint32_t (&r)[2][32]) {
+                    tmem_ld32(s_addr + h * 64, r[0]);
+                    tmem_ld32(s_addr + h * 64 + 32, r[1]);
+                };
+                auto mask = [&](int v, uint32_t (&r)[2][32]) {
+                    if (__any_sync(0xffffffffu, v < 64)) {
+#pragma unroll
+                        for (int i = 0; i < 64; ++i)
+                            if (i >= v) r[i / 32][i % 32] = 0xff800000u;
+                    }
+                };
+                // 64 scores -> 32 words of bf16 P in r[0]; returns their sum
+                auto exponentials = [&](uint32_t (&r)[2][32]) -> float {
+                    const float off = kBias - (m_ref == -INFINITY ? 0.f : m_ref);
+                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int i = 0; i < 64; i += 2) {
+                        const bool poly = ((i >> 1) % 3) == 2;   // a third by polynomial, where the special-function unit is the bound
+                        const float x0 = fmaf(__uint_as_float(r[i / 32][i % 32]), a.scale_log2, off);
+                        const float x1 = fmaf(__uint_as_float(r[i / 32][i % 32 + 1]), a.scale_log2, off);
+                        const float p0 = poly ? poly_exp2(x0) : fast_exp2(x0), p1 = poly ? poly_exp2(x1) : fast_exp2(x1);
+                        sum[(i >> 1) & 3] += p0 + p1;
+                        r[0][i / 2] = __byte_perm(__float_as_uint(p0), __float_as_uint(p1), 0x7632);
+                    }
+                    return (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                };
+                auto half = [&](int h, uint32_t (&r)[2][32]) -> bool {
+                    const int v = valid - 64 * h;
+                    mask(v, r);
+                    float sum = 0.f;
+                    bool redo = __any_sync(0xffffffffu, m_ref == -INFINITY && v > 0);   // nothing to exponentiate against yet
+                    if (!redo) {
+                        sum = exponentials(r);
+                        redo = __any_sync(0xffffffffu, !(sum <= kHalfSumLimit));
+                        if (redo) {
+                            load(h, r);
+                            tmem_wait_ld();
+                            mask(v, r);
+                        }
+                    }
+                    if (redo) {
+                        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                        for (int i = 0; i < 64; ++i) mx[i & 3] = fmaxf(mx[i & 3], __uint_as_float(r[i / 32][i % 32]));
+                        const float top = a.scale_log2 * fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+                        const bool need = top > m_ref + kThreshold;
+                        if (__any_sync(0xffffffffu, need)) {
+                            const float alpha = need ? fast_exp2(m_ref - top) : 1.f;
+                            if (j > 0 || h == 1) {
+                                // O[t] is at rest: S of this unit was made behind the products before it; the first half's products of
+                                // this very unit are waited for
+                                if (h == 1) {
+                                    if (!warp_wait(bar(L::kBarHalf + t), uses & 1)) return false;
+                                    tc_fence_after();
+                                }
+                                uint32_t o[32];
+#pragma unroll 1
+                                for (int c = 0; c < D / 32; ++c) {
+                                    tmem_ld32(o_base + t * D + c * 32, o);
+                                    tmem_wait_ld();
+#pragma unroll
+                                    for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+                                    tmem_st32(o_base + t * D + c * 32, o);
+                                }
+                                tmem_wait_st();
+                            }
+                            l_sum *= alpha;
+                            if (need) m_ref = top;
+                        }
+                        sum = exponentials(r);
+                    }
+                    tmem_st32(s_addr + h * 32, r[0]);
+                    l_sum += sum;
+                    tmem_wait_st();
+                    tc_fence_before();
+                    mbar_arrive(bar_p(t, h));
+                    return true;
+                };
+                load(0, s0);
+                tmem_wait_ld();
+                load(1, s1);
+                if (!(ok = half(0, s0))) break;
+                tmem_wait_ld();
+                if (!(ok = half(1, s1))) break;
+            }
+            if (!ok) break;
+            e += 2 * n;
+
+            // ---- epilogue
+            l_sum *= kUnbias;
+            const int streams = n == 0 ? 0 : two || n > 1 ? 2 : 1;
+            if (two || n == 0) {
+                if (n > 0) {
+                    if (!(ok = warp_wait(bar(L::kBarDone + t), done[t]++ & 1))) break;
+                    done[1 - t]++;
+                }
+            } else {
+                for (int i = 0; ok && i < streams; ++i) ok = warp_wait(bar(L::kBarDone + i), done[i]++ & 1);
+                if (!ok) break;
+            }
+            tc_fence_after();
+            float share[2] = {0.f, 0.f};   // of each stream's accumulator in the result
+            float lse2;
+            if (two || n == 0) {
+                share[t] = l_sum == 0.f ? 0.f : 1.f / l_sum;
+                lse2 = l_sum == 0.f ? -INFINITY : m_ref + log2f(l_sum);
+            } else {
+                exchange[t * 256 + row] = m_ref;
+                exchange[t * 256 + 128 + row] = l_sum;
+                mbar_arrive(bar(L::kBarMet));
+                if (!(ok = warp_wait(bar(L::kBarMet), met++ & 1))) break;
+                const float m[2] = {exchange[row], exchange[256 + row]}, l[2] = {exchange[128 + row], exchange[384 + row]};
+                const float top = fmaxf(m[0], m[1]);
+                const float w0 = l[0] == 0.f ? 0.f : fast_exp2(m[0] - top), w1 = l[1] == 0.f ? 0.f : fast_exp2(m[1] - top);
+                const float total = w0 * l[0] + w1 * l[1];
+                share[0] = total == 0.f ? 0.f : w0 / total;
+                share[1] = total == 0.f ? 0.f : w1 / total;
+                lse2 = total == 0.f ? -INFINITY : top + log2f(total);
+            }
+            // this warpgroup's columns: all of its own row tile, or half of the shared one
+            const int c0 = two ? 0 : t * (D / 64), c1 = two ? D / 32 : (t + 1) * (D / 64);
+            const size_t out_row = size_t(pc.g.q0 + token) * a.num_q_heads + pc.head * a.group + in_group % a.group;
+            const size_t part_row = size_t(pc.slot) * a.slot_rows + in_group;
+            float from_prior = 0.f;
+            if (mine && !pc.split && a.prior_lse) {
+                const Joined jn = join(lse2, a.prior_lse[out_row] * kLog2e);
+                share[0] *= jn.first;
+                share[1] *= jn.first;
+                from_prior = jn.second;
+                lse2 = jn.lse2;
+            }
+            for (int c = c0; active && c < c1; ++c) {
+                __syncwarp();
+                float v[32];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] = 0.f;
+                for (int i = 0; i < 2; ++i) {
+                    if (two ? i != t : i >= streams) continue;
+                    if (n == 0) continue;
+                    uint32_t o[32];
+                    tmem_ld32(o_base + i * D + c * 32, o);
+                    tmem_wait_ld();
+                    if (share[i] != 0.f)
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) v[k] = fmaf(__uint_as_float(o[k]), share[i], v[k]);
+                }
+                if (!mine) continue;
+                if (pc.split) {
+                    store_f32(a.partial_o + part_row * D + c * 32, v);
+                    continue;
+                }
+                if (from_prior != 0.f) add_prior(a, out_row * D + c * 32, from_prior, v);
+                if (a.out_f32) store_f32(static_cast<float *>(a.out) + out_row * D + c * 32, v);
+                else store_bf16(static_cast<__nv_bfloat16 *>(a.out) + out_row * D + c * 32, v);
+            }
+            tc_fence_before();
+            if (!two) {
+                // each warpgroup has read both accumulators, the exchanged sums and prior_lse (which lse may be): none of them is written
+                // before both are done
+                mbar_arrive(bar(L::kBarMet));
+                if (!(ok = warp_wait(bar(L::kBarMet), met++ & 1))) break;
+            }
+            if (mine && (two || t == 0)) {
+                if (pc.split) a.partial_lse[part_row] = lse2;
+                else a.lse[out_row] = lse2 * kLn2;
+            }
+        }
+        if (!ok) *abort_flag = 1;
+    }
+
+    // ---------------------------------------------------------------- teardown
+    tc_fence_before();
+    __syncthreads();
+    if (*abort_flag) {
+        if (threadIdx.x == 0) raise(a.status, PSA_ERR_TIMEOUT);
+        // let copies that were already issued land before the block's shared memory is released
+        if (warp == kProducerWarp && lane == 0) {
+            const unsigned long long t0 = global_timer_ns();
+            while (global_timer_ns() - t0 < 2000000ull) { }
+        }
+        // products queued before the issuing thread gave up may still run: one more commit completes when all of them have retired
+        if (warp == kMmaWarp && elect_one()) {
+            tc_commit(bar(L::kBarDrain));
+            const unsigned long long t0 = global_timer_ns();
+            while (!mbar_try_wait(bar(L::kBarDrain), 0) && global_timer_ns() - t0 < 2000000ull) { }
+        }
+        __syncthreads();
+    }
+    if (warp == kMmaWarp) {
+        tc_fence_after();
+        tmem_dealloc(tmem_base, 512);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------------- merge
+// Block (cut, slice): the group that the end of share `cut` falls into, if that is the first cut inside it; a warp per row.
+template <int D>
+__global__ void __launch_bounds__(128)
+chunk_merge_kernel(const ChunkArgs a)
+{
+    grid_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const ChunkHeader h = *a.header;
+    const int cut = blockIdx.x;                 // between blocks cut and cut + 1
+    if (cut + 1 >= h.blocks || h.groups == 0) return;
+    const long long total = h.per_head * a.num_kv_heads;
+    const long long x = share_begin(total, cut + 1, h.blocks);
+    int head, gi;
+    locate(a, h, x, lane, &head, &gi);
+    if (head >= a.num_kv_heads) return;
+    const ChunkGroup g = a.groups[gi];
+    const long long base = head * h.per_head + g.cum;
+    const int tiles = chunk_tiles(g.keys), t_cut = tile_at(g, a.group, base, x);
+    if (t_cut <= 0 || t_cut >= tiles) return;                                              // nothing is cut here
+    if (cut > 0 && tile_at(g, a.group, base, share_begin(total, cut, h.blocks)) > 0) return;   // an earlier cut's group
+    // pieces: blocks cut, cut + 1, ... until the group ends
+    const int rows = g.n_tok * a.group;
+    constexpr int kPer = D / 32;
+    for (int r = blockIdx.y * (blockDim.x >> 5) + warp; r < rows; r += gridDim.y * (blockDim.x >> 5)) {
+        float top = -INFINITY, sum = 0.f, acc[kPer];
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) acc[i] = 0.f;
+        for (int b = cut; b < h.blocks; ++b) {
+            const int t0 = tile_at(g, a.group, base, share_begin(total, b, h.blocks)), t1 = tile_at(g, a.group, base, share_begin(total, b + 1, h.blocks));
+            if (t1 > t0) {
+                const size_t at = size_t(2 * b + (t0 > 0 ? 0 : 1)) * a.slot_rows + r;
+                const float lse2 = a.partial_lse[at];
+                float o[kPer];
+                const float *from = a.partial_o + at * D + lane * kPer;
+                if constexpr (kPer == 4) {
+                    const float4 q = *reinterpret_cast<const float4 *>(from);
+                    o[0] = q.x; o[1] = q.y; o[2] = q.z; o[3] = q.w;
+                } else {
+                    const float2 q = *reinterpret_cast<const float2 *>(from);
+                    o[0] = q.x; o[1] = q.y;
+                }
+                if (lse2 != -INFINITY) {
+                    const float next = fmaxf(top, lse2);
+                    const float keep = top == -INFINITY ? 0.f : exp2f(top - next), w = exp2f(lse2 - next);
+                    sum = sum * keep + w;
+#pragma unroll
+                    for (int i = 0; i < kPer; ++i) acc[i] = acc[i] * keep + w * o[i];
+                    top = next;
+                }
+            }
+            if (t1 >= tiles) break;
+        }
+        float lse2 = sum == 0.f ? -INFINITY : top + log2f(sum);
+        float share = sum == 0.f ? 0.f : 1.f / sum, from_prior = 0.f;
+        const size_t row = size_t(g.q0 + r / a.group) * a.num_q_heads + head * a.group + r % a.group;
+        if (a.prior_lse) {
+            const Joined jn = join(lse2, a.prior_lse[row] * kLog2e);
+            share *= jn.first;
+            from_prior = jn.second;
+            lse2 = jn.lse2;
+        }
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const size_t at = row * D + lane * kPer + i;
+            float v = acc[i] * share;
+            if (from_prior != 0.f)
+                v = fmaf(from_prior, a.prior_f32 ? static_cast<const float *>(a.prior_out)[at] : __bfloat162float(static_cast<const __nv_bfloat16 *>(a.prior_out)[at]), v);
+            if (a.out_f32) static_cast<float *>(a.out)[at] = v;
+            else static_cast<__nv_bfloat16 *>(a.out)[at] = __float2bfloat16_rn(v);
+        }
+        __syncwarp();   // lse may be prior_lse: every lane has read it
+        if (lane == 0) a.lse[row] = lse2 * kLn2;
+    }
+}
+
+template <class K, class... A>
+cudaError_t launch_dependent(K kernel, dim3 grid, int threads, int smem, cudaStream_t st, A... args)
+{
+    cudaLaunchConfig_t lc{};
+    lc.gridDim = grid;
+    lc.blockDim = dim3(threads);
+    lc.dynamicSmemBytes = smem;
+    lc.stream = st;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    lc.attrs = &attr;
+    lc.numAttrs = 1;
+    return cudaLaunchKernelEx(&lc, kernel, args...);
+}
+
+template <int D>
+cudaError_t launch(const ChunkArgs &a, const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorMap &mv, cudaStream_t st)
+{
+    static PerDeviceOnce once;
+    if (const int rc = once.ensure([] { return int(cudaFuncSetAttribute(chunk_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, ChunkSmem<D>::kTotal)); }))
+        return cudaError_t(rc);
+    chunk_schedule_kernel<<<1, kScheduleThreads, 0, st>>>(a);
+    cudaError_t e = cudaGetLastError();
+    if (e == cudaSuccess) e = launch_dependent(chunk_kernel<D>, dim3(a.blocks), 320, ChunkSmem<D>::kTotal, st, mq, mk, mv, a);
+    if (e == cudaSuccess && a.blocks > 1) e = launch_dependent(chunk_merge_kernel<D>, dim3(a.blocks - 1, (a.slot_rows + 31) / 32), 128, 0, st, a);
+    return e;
+}
+
+bool misaligned(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n != 0; }
+
+}  // namespace
+
+size_t chunk_layout(ChunkArgs &a, void *scratch, int head_dim)
+{
+    const int per_group = kGroupRows / a.group;
+    a.max_groups = int(a.num_tokens / per_group + a.num_samples);
+    a.slot_rows = int(std::min<int64_t>(kGroupRows, a.num_tokens * a.group));
+    size_t off = 0;
+    auto take = [&](size_t bytes) { const size_t at = off; off = (off + bytes + 255) / 256 * 256; return static_cast<unsigned char *>(scratch) + at; };
+    a.header = reinterpret_cast<ChunkHeader *>(take(sizeof(ChunkHeader)));
+    a.groups = reinterpret_cast<ChunkGroup *>(take(sizeof(ChunkGroup) * size_t(a.max_groups)));
+    if (head_dim > 0) {
+        a.partial_lse = reinterpret_cast<float *>(take(4 * size_t(2 * a.blocks) * a.slot_rows));
+        a.partial_o = reinterpret_cast<float *>(take(4 * size_t(2 * a.blocks) * a.slot_rows * head_dim));
+    }
+    return off;
+}
+
+psa_status_t chunk_check(const ChunkArgs &a, const void *q, const int64_t q_strides[2], const void *pool, const int64_t pool_strides[3], int head_dim)
+{
+    if (a.num_tokens < 0 || a.num_samples < 0 || a.num_pool_pages < 0 || a.num_entries < 0 || a.num_kv_heads <= 0 || a.num_q_heads <= 0)
+        return set_last_error(PSA_ERR_INVALID_ARG, "negative sizes or no heads");
+    if (head_dim != 64 && head_dim != 128) return set_last_error(PSA_ERR_UNSUPPORTED, "head_dim must be 64 or 128");
+    if (a.num_q_heads % a.num_kv_heads || (a.group != 1 && a.group != 2 && a.group != 4 && a.group != 8))
+        return set_last_error(PSA_ERR_UNSUPPORTED, "num_q_heads / num_kv_heads must be 1, 2, 4 or 8");
+    if (a.num_samples > (1 << 20)) return set_last_error(PSA_ERR_UNSUPPORTED, "at most 2^20 samples per call");
+    if (a.num_tokens > (1 << 24)) return set_last_error(PSA_ERR_UNSUPPORTED, "at most 2^24 new tokens per call");
+    if (a.num_pool_pages > kMostChunkPages || a.num_entries > kMostChunkEntries)
+        return set_last_error(PSA_ERR_UNSUPPORTED, "at most 2^27 pages and 2^31 - 256 list entries");
+    if (misaligned(a.status, 4)) return set_last_error(PSA_ERR_INVALID_ARG, "the status word must be 4-byte aligned");
+    if (a.num_tokens == 0 || a.num_samples == 0) return PSA_OK;
+    if (!q || !q_strides || !pool_strides || !a.page_indptr || !a.kv_lens || (a.num_entries > 0 && !a.page_indices) || (a.num_pool_pages > 0 && !pool) ||
+        (!a.q_indptr && a.num_samples != a.num_tokens))
+        return set_last_error(PSA_ERR_INVALID_ARG, "null paged attention argument");
+    if (misaligned(q, 16) || misaligned(pool, 16)) return set_last_error(PSA_ERR_INVALID_ARG, "q and the pools must be 16-byte aligned");
+    for (int i = 0; i < 3; ++i) {
+        if (pool_strides[i] <= 0 || pool_strides[i] % 8 || pool_strides[i] >= (int64_t(1) << 38))
+            return set_last_error(PSA_ERR_INVALID_ARG, "pool strides must be positive multiples of 8 elements below 2^38");
+        if (i < 2 && (q_strides[i] <= 0 || q_strides[i] % 8 || q_strides[i] >= (int64_t(1) << 38)))
+            return set_last_error(PSA_ERR_INVALID_ARG, "q strides must be positive multiples of 8 elements below 2^38");
+    }
+    return PSA_OK;
+}
+
+psa_status_t chunk_maps(const ChunkArgs &a, const void *q, const int64_t q_strides[2], const void *const *pools, int num_pools, const int64_t pool_strides[3],
+                        int head_dim, CUtensorMap *maps)
+{
+    std::string err;
+    EncodeFn fn = get_encode_fn(&err);
+    if (!fn) return set_last_error(PSA_ERR_CUDA, err);
+    {   // Q as (d, g, kv head, token): a box of (64, G, 1, 128 / G) is one 64-wide half of a row tile, g fastest
+        const cuuint64_t dims[4] = {cuuint64_t(head_dim), cuuint64_t(a.group), cuuint64_t(a.num_kv_heads), cuuint64_t(a.num_tokens)};
+        const cuuint64_t strides[3] = {cuuint64_t(q_strides[1]) * 2, cuuint64_t(q_strides[1]) * a.group * 2, cuuint64_t(q_strides[0]) * 2};
+        const cuuint32_t box[4] = {64, cuuint32_t(a.group), 1, cuuint32_t(kRowTile / a.group)};
+        if (!encode(fn, &maps[0], q, 4, dims, strides, box, &err)) return set_last_error(PSA_ERR_CUDA, err);
+    }
+    for (int i = 0; i < num_pools; ++i) {   // a pool as (d, slot, kv head, page): a box is one 64-wide half of a page
+        const cuuint64_t dims[4] = {cuuint64_t(head_dim), kPageSize, cuuint64_t(a.num_kv_heads), cuuint64_t(a.num_pool_pages)};
+        const cuuint64_t strides[3] = {cuuint64_t(pool_strides[2]) * 2, cuuint64_t(pool_strides[1]) * 2, cuuint64_t(pool_strides[0]) * 2};
+        const cuuint32_t box[4] = {64, kPageSize, 1, 1};
+        if (!encode(fn, &maps[1 + i], pools[i], 4, dims, strides, box, &err)) return set_last_error(PSA_ERR_CUDA, err);
+    }
+    return PSA_OK;
+}
+
+int multiprocessors()
+{
+    static std::atomic<int> known[PerDeviceOnce::kMaxDevices];
+    int dev = 0;
+    if (PerDeviceOnce::device_ordinal(&dev)) return 0;
+    if (dev < 0 || dev >= PerDeviceOnce::kMaxDevices) return 0;
+    int n = known[dev].load(std::memory_order_relaxed);
+    if (n == 0) {
+        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+        known[dev].store(n, std::memory_order_relaxed);
+    }
+    return n;
+}
+
+}  // namespace psa
+
+extern "C" size_t psa_attend_paged_scratch_bytes(int64_t num_tokens, int32_t num_samples, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim)
+{
+    if (num_tokens < 0 || num_samples < 0 || num_kv_heads <= 0 || num_q_heads < num_kv_heads || num_tokens > (1 << 24) || head_dim < 0 || head_dim > 1024) return 0;
+    psa::ChunkArgs a{};
+    a.num_tokens = num_tokens; a.num_samples = num_samples;
+    a.group = std::min(8, num_q_heads / num_kv_heads);
+    a.blocks = psa::kMostBlocks;
+    return psa::chunk_layout(a, nullptr, head_dim);
+}
+
+extern "C" psa_status_t psa_attend_paged(const void *q, const int64_t q_strides[2], const int32_t *q_indptr, int64_t num_tokens, int32_t num_samples,
+                                         int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, float sm_scale, const void *k_pool,
+                                         const void *v_pool, const int64_t pool_strides[3], int64_t num_pool_pages, const int32_t *page_indptr,
+                                         const int32_t *page_indices, int64_t num_entries, const int32_t *kv_lens, const void *prior_out,
+                                         int32_t prior_dtype, const float *prior_lse, void *out, int32_t out_dtype, float *lse, int32_t *status,
+                                         void *scratch, size_t scratch_bytes, void *cuda_stream)
+{
+    using namespace psa;
+    ChunkArgs a{};
+    a.num_tokens = num_tokens; a.num_samples = num_samples; a.num_q_heads = num_q_heads; a.num_kv_heads = num_kv_heads;
+    a.group = num_kv_heads > 0 ? num_q_heads / num_kv_heads : 0;
+    a.num_pool_pages = int32_t(std::min<int64_t>(num_pool_pages, kMostChunkPages + 1)); a.num_entries = num_entries;
+    a.q_indptr = q_indptr; a.kv_lens = kv_lens; a.page_indptr = page_indptr; a.page_indices = page_indices;
+    a.status = status;
+    a.scale_log2 = sm_scale * kLog2e;
+    a.prior_out = prior_out; a.prior_lse = prior_lse; a.prior_f32 = prior_dtype == PSA_OUT_F32;
+    a.out = out; a.lse = lse; a.out_f32 = out_dtype == PSA_OUT_F32;
+    psa_status_t rc = chunk_check(a, q, q_strides, k_pool, pool_strides, head_dim);
+    if (rc != PSA_OK) return rc;
+    if ((out_dtype != PSA_OUT_BF16 && out_dtype != PSA_OUT_F32) || (prior_out && prior_dtype != PSA_OUT_BF16 && prior_dtype != PSA_OUT_F32))
+        return set_last_error(PSA_ERR_UNSUPPORTED, "out and prior_out must be bf16 or f32");
+    if (!(sm_scale > 0.f) || sm_scale > 1e30f) return set_last_error(PSA_ERR_INVALID_ARG, "sm_scale must be positive and finite");
+    if ((prior_out == nullptr) != (prior_lse == nullptr)) return set_last_error(PSA_ERR_INVALID_ARG, "prior_out and prior_lse go together");
+    if (num_tokens == 0 || num_samples == 0) return PSA_OK;
+    if ((num_pool_pages > 0 && !v_pool) || !out || !lse) return set_last_error(PSA_ERR_INVALID_ARG, "null paged attention argument");
+    if (misaligned(v_pool, 16) || misaligned(out, 16) || misaligned(prior_out, 16) || misaligned(lse, 4) || misaligned(prior_lse, 4))
+        return set_last_error(PSA_ERR_INVALID_ARG, "pools, out and prior_out must be 16-byte aligned, lse 4-byte aligned");
+    if (prior_out == out && prior_out && prior_dtype != out_dtype) return set_last_error(PSA_ERR_INVALID_ARG, "prior_out may be out only with the same type");
+    if (num_pool_pages == 0) return set_last_error(PSA_ERR_INVALID_ARG, "the pool has no pages");
+    if (!scratch || misaligned(scratch, 256) ||
+        scratch_bytes < psa_attend_paged_scratch_bytes(num_tokens, num_samples, num_q_heads, num_kv_heads, head_dim))
+        return set_last_error(PSA_ERR_WORKSPACE, "scratch must be 256-byte aligned and hold psa_attend_paged_scratch_bytes");
+    a.blocks = std::min(multiprocessors(), kMostBlocks);
+    if (a.blocks <= 0) return set_last_error(PSA_ERR_CUDA, "no CUDA device");
+    chunk_layout(a, scratch, head_dim);
+    CUtensorMap maps[3];
+    const void *pools[2] = {k_pool, v_pool};
+    rc = chunk_maps(a, q, q_strides, pools, 2, pool_strides, head_dim, maps);
+    if (rc != PSA_OK) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const cudaError_t e = head_dim == 128 ? launch<128>(a, maps[0], maps[1], maps[2], st) : launch<64>(a, maps[0], maps[1], maps[2], st);
+    if (e != cudaSuccess) return set_last_error(PSA_ERR_CUDA, std::string("paged attention launch: ") + cudaGetErrorString(e));
+    return PSA_OK;
+}

@@ -35,6 +35,8 @@ struct Api {
     decltype(&psa_decode_kv4) decode_kv4;
     decltype(&psa_process_logits) process_logits;
     decltype(&psa_mark_tokens) mark_tokens;
+    decltype(&psa_store_kv) store_kv;
+    decltype(&psa_attend_paged) attend_paged;
 } api{};
 
 const char *name_of(at::ScalarType t)
@@ -88,6 +90,12 @@ public:
     {
         const long long v = PyLong_AsLongLong(args_[i]);
         if (v == -1 && PyErr_Occurred()) throw Refused("");
+        return v;
+    }
+    double real(int i) const
+    {
+        const double v = PyFloat_AsDouble(args_[i]);
+        if (v == -1.0 && PyErr_Occurred()) throw Refused("");
         return v;
     }
     // a status word: an int32 tensor, or the workspace of a plan (uint8), whose first word it is; the library checks its alignment
@@ -317,11 +325,111 @@ psa_status_t decode_kv4(PyObject *const *args, Py_ssize_t given)
                           size_t(c.numel(18)), stream);
 }
 
+// A bf16 cache in pages: pools [pages, heads, 16, dim], the last dimension contiguous, any strides before it (the same for K and V).
+struct Pools {
+    int64_t strides[3], pages;
+    static void read(const at::Tensor &t, int64_t heads, int64_t dim, const char *name, int64_t (&s)[3])
+    {
+        if (t.scalar_type() != at::kBFloat16 || t.dim() != 4 || t.size(1) != heads || t.size(2) != 16 || t.size(3) != dim || t.stride(3) != 1)
+            throw Refused(std::string(name) + " must be bf16 [pages, " + std::to_string(heads) + ", 16, " + std::to_string(dim) + "] with a contiguous last dimension");
+        s[2] = t.stride(2);
+        s[1] = heads > 1 ? t.stride(1) : 16 * dim;
+        s[0] = t.size(0) > 1 ? t.stride(0) : heads * 16 * dim;
+    }
+    Pools(const at::Tensor &k, const at::Tensor *v, int64_t heads, int64_t dim) : pages(k.size(0))
+    {
+        read(k, heads, dim, "k_pool", strides);
+        if (!v) return;
+        int64_t mine[3];
+        read(*v, heads, dim, "v_pool", mine);
+        if (v->size(0) != pages || mine[0] != strides[0] || mine[1] != strides[1] || mine[2] != strides[2])
+            throw Refused("k_pool and v_pool must have the same shape and strides");
+    }
+};
+
+// new_k, new_v, slot_map, k_pool, v_pool, status, stream
+psa_status_t store_kv(PyObject *const *args, Py_ssize_t given)
+{
+    Call c(args, given, 7);
+    const at::Tensor &k = c.tensor(0, "new_k"), &v = c.tensor(1, "new_v");
+    if (k.dim() != 3 || k.scalar_type() != at::kBFloat16 || v.scalar_type() != at::kBFloat16 || k.sizes() != v.sizes())
+        throw Refused("new_k and new_v must be bf16 [tokens, heads, head_dim] of the same shape and strides");
+    const int64_t tokens = k.size(0), heads = k.size(1), dim = k.size(2);
+    if (heads > 0x7fffffff || dim > 0xffff) throw Refused("new_k and new_v are too large");
+    int64_t strides[2], v_strides[2];
+    outer_strides(k, dim, "new_k", strides);
+    outer_strides(v, dim, "new_v", v_strides);
+    if (tokens > 0 && (strides[0] != v_strides[0] || strides[1] != v_strides[1])) throw Refused("new_k and new_v must have the same strides");
+    const auto *slots = c.needed<int64_t>(2, at::kLong, "slot_map", tokens);
+    const at::Tensor &k_pool = c.tensor(3, "k_pool"), &v_pool = c.tensor(4, "v_pool");
+    const Pools pools(k_pool, &v_pool, heads, dim);
+    int32_t *status = c.status(5);
+    void *stream = c.stream(6);
+    return api.store_kv(k.data_ptr(), v.data_ptr(), strides, slots, tokens, int32_t(heads), int32_t(dim), k_pool.data_ptr(), v_pool.data_ptr(),
+                        pools.strides, pools.pages, status, stream);
+}
+
 int32_t dtype_code(const at::Tensor &t, const char *name)
 {
     if (t.scalar_type() == at::kBFloat16) return PSA_OUT_BF16;
     if (t.scalar_type() == at::kFloat) return PSA_OUT_F32;
     throw Refused(std::string(name) + " must be bf16 or f32, not " + name_of(t.scalar_type()));
+}
+
+// Rows of q over samples in pages: what attention and the weights of cached tokens have in common.
+struct Rows {
+    const at::Tensor *q;
+    int64_t strides[2], tokens, heads, dim, samples, entries;
+    const int32_t *q_indptr, *lens, *indptr, *indices;
+    // tensors of q, page_indptr, page_indices, kv_lens, q_indptr from `at` on
+    Rows(Call &c, int at, int q_indptr_at)
+    {
+        q = &c.tensor(0, "q");
+        if (q->dim() != 3 || q->scalar_type() != at::kBFloat16) throw Refused("q must be bf16 [tokens, heads, head_dim]");
+        tokens = q->size(0); heads = q->size(1); dim = q->size(2);
+        if (heads > 0xffff || dim > 0xffff || tokens > 0x7fffffff) throw Refused("q is too large");
+        outer_strides(*q, dim, "q", strides);
+        lens = c.needed<int32_t>(at + 2, at::kInt, "kv_lens");
+        samples = c.numel(at + 2);
+        if (samples > 0x7fffffff) throw Refused("too many samples");
+        indptr = c.needed<int32_t>(at, at::kInt, "page_indptr", samples + 1);
+        indices = c.needed<int32_t>(at + 1, at::kInt, "page_indices");
+        entries = c.numel(at + 1);
+        q_indptr = c.flat<int32_t>(q_indptr_at, at::kInt, "q_indptr", samples + 1);
+        if (!q_indptr && samples != tokens) throw Refused("without q_indptr there is one row of q per sample");
+    }
+};
+
+// q, k_pool, v_pool, page_indptr, page_indices, kv_lens, q_indptr, out, lse, sm_scale, prior_out, prior_lse, status, scratch, stream
+psa_status_t attend_paged(PyObject *const *args, Py_ssize_t given)
+{
+    Call c(args, given, 15);
+    const Rows r(c, 3, 6);
+    const at::Tensor &k_pool = c.tensor(1, "k_pool"), &v_pool = c.tensor(2, "v_pool");
+    if (k_pool.dim() != 4) throw Refused("k_pool must be bf16 [pages, heads, 16, head_dim]");
+    const int64_t kv = k_pool.size(1);
+    const Pools pools(k_pool, &v_pool, kv, r.dim);
+    const at::Tensor &out = c.tensor(7, "out");
+    const int32_t out_code = dtype_code(out, "out");
+    if (!out.is_contiguous() || out.sizes() != r.q->sizes()) throw Refused("out must be contiguous and of q's shape");
+    auto *lse = c.needed<float>(8, at::kFloat, "lse", r.tokens * r.heads);
+    const double scale = c.real(9);
+    const void *prior = nullptr;
+    int32_t prior_code = 0;
+    if (c.none(10) != c.none(11)) throw Refused("prior_out and prior_lse go together");
+    if (!c.none(10)) {
+        const at::Tensor &p = c.tensor(10, "prior_out");
+        prior_code = dtype_code(p, "prior_out");
+        if (!p.is_contiguous() || p.sizes() != r.q->sizes()) throw Refused("prior_out must be contiguous and of q's shape");
+        prior = p.data_ptr();
+    }
+    const auto *prior_lse = c.flat<float>(11, at::kFloat, "prior_lse", r.tokens * r.heads);
+    int32_t *status = c.status(12);
+    void *scratch = c.needed(13, at::kByte, "scratch");
+    void *stream = c.stream(14);
+    return api.attend_paged(r.q->data_ptr(), r.strides, r.q_indptr, r.tokens, int32_t(r.samples), int32_t(r.heads), int32_t(std::min<int64_t>(kv, 0x7fffffff)),
+                            int32_t(r.dim), float(scale), k_pool.data_ptr(), v_pool.data_ptr(), pools.strides, pools.pages, r.indptr, r.indices, r.entries,
+                            r.lens, prior, prior_code, prior_lse, out.data_ptr(), out_code, lse, status, scratch, size_t(c.numel(13)), stream);
 }
 
 struct Bitmaps {
@@ -451,7 +559,8 @@ PyObject *attach(PyObject *, PyObject *path)
         {"psa_build_page_table", reinterpret_cast<void **>(&api.build_page_table)}, {"psa_extend_page_table", reinterpret_cast<void **>(&api.extend_page_table)},
         {"psa_store_kv4", reinterpret_cast<void **>(&api.store_kv4)},               {"psa_load_kv4", reinterpret_cast<void **>(&api.load_kv4)},
         {"psa_decode_kv4", reinterpret_cast<void **>(&api.decode_kv4)},             {"psa_process_logits", reinterpret_cast<void **>(&api.process_logits)},
-        {"psa_mark_tokens", reinterpret_cast<void **>(&api.mark_tokens)},
+        {"psa_mark_tokens", reinterpret_cast<void **>(&api.mark_tokens)},           {"psa_store_kv", reinterpret_cast<void **>(&api.store_kv)},
+        {"psa_attend_paged", reinterpret_cast<void **>(&api.attend_paged)},
     };
     for (const auto &w : wanted)
         if (!(*w.to = dlsym(lib, w.name))) return PyErr_Format(PyExc_ImportError, "%s lacks %s", p, w.name);
@@ -467,6 +576,7 @@ PyMethodDef method(const char *name)
 PyMethodDef methods[] = {
     method<build_page_table>("build_page_table"), method<extend_page_table>("extend_page_table"), method<store_kv4>("store_kv4"),
     method<load_kv4>("load_kv4"), method<decode_kv4>("decode_kv4"), method<process_logits>("process_logits"), method<mark_tokens>("mark_tokens"),
+    method<store_kv>("store_kv"), method<attend_paged>("attend_paged"),
     {"prefix_strides", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&prefix_strides)), METH_FASTCALL, nullptr},
     {"empty", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&empty)), METH_FASTCALL, nullptr},
     {"attach", attach, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr},
