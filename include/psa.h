@@ -543,7 +543,7 @@ psa_status_t psa_store_kv(const void *new_k, const void *new_v, const int64_t kv
  *   out, lse       [num_tokens, Hq, D] of out_dtype, [num_tokens, Hq] f32, contiguous.
  *   status         int32 device or NULL: receives PSA_ERR_BOUNDS (see psa_read_status) for a page id outside 0 .. num_pool_pages-1 (its
  *                  keys count as zeros), a list that is too short for kv_lens or a negative length (the sample counts as empty), and
- *                  q_indptr that descends; PSA_ERR_TIMEOUT if a wait inside the kernel ran out.
+ *                  q_indptr that descends (a sample of more than 2^30 tokens counts as a list that is too short); PSA_ERR_TIMEOUT if a wait inside the kernel ran out.
  *   scratch        device, 256-byte aligned, psa_attend_paged_scratch_bytes(...) bytes, overwritten by every call (calls that share it
  *                  must be ordered on one stream).
  * What stands in the pages behind a sample's last token does not matter, NaN included.  Within the new tokens V has to be finite
@@ -558,6 +558,67 @@ psa_status_t psa_attend_paged(const void *q, const int64_t q_strides[2], const i
                               const int32_t *page_indices, int64_t num_entries, const int32_t *kv_lens, const void *prior_out,
                               int32_t prior_dtype, const float *prior_lse, void *out, int32_t out_dtype, float *lse, int32_t *status,
                               void *scratch, size_t scratch_bytes, void *cuda_stream);
+
+/*
+ * The attention weight each cached token received, for keeping a cache within bounds: for KV head h and the token at position j < kv_lens[s]
+ * of a sample with new tokens,
+ *     weights_out[cell] = (j is one of the new tokens ? 0 : weights[cell]) + sum exp( sm_scale * q[row, g, :] . k_j - lse[row, g] )
+ * over the sample's rows that see j (as in psa_attend_paged) and the query heads g that read h; cell = (page, h, j % 16) of an array
+ * [num_pool_pages, Hkv, 16] f32, contiguous, in the order of the pool.  weights_out may be weights.  Cells of other tokens and samples are
+ * left as they are, so a page from the free stack needs no clearing.
+ *   lse            [num_tokens, Hq] f32: what psa_attend_paged or psa_decode returned for the rows (over all they attended to, a shared
+ *                  prompt included); rows with -inf give no weight.
+ * Scores and sums are fp32, added in a fixed order.  The other arguments, limits and status reports are those of psa_attend_paged; a
+ * sample's list must not hold a page twice.  Enqueues three kernels.
+ */
+size_t psa_accumulate_weights_scratch_bytes(int64_t num_tokens, int32_t num_samples);
+psa_status_t psa_accumulate_weights(const void *q, const int64_t q_strides[2], const int32_t *q_indptr, int64_t num_tokens, int32_t num_samples,
+                                    int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, float sm_scale, const float *lse,
+                                    const void *k_pool, const int64_t pool_strides[3], int64_t num_pool_pages, const int32_t *page_indptr,
+                                    const int32_t *page_indices, int64_t num_entries, const int32_t *kv_lens, const float *weights,
+                                    float *weights_out, int32_t *status, void *scratch, size_t scratch_bytes, void *cuda_stream);
+
+/*
+ * Pages that leave a cache which has grown beyond its budget, chosen by the weights above.  A page weighs as much as its heaviest cell
+ * (max over KV heads and its 16 slots; NaN cells do not count, a page of nothing else weighs less than any).  Sample s holds
+ * P = ceil(kv_lens[s] / 16) pages; if P > budgets[s], its min(recent, budgets[s]) newest pages stay and of the others the heaviest, so that
+ * budgets[s] >= 1 are left (of equal weights the older page stays).  The list closes up in order -- K and V do not move --, entries
+ * budgets[s] .. P - 1 become -1, the length drops by 16 a page (the newest page, the only one that may be part full, stays: recent >= 1), and
+ * the ids that left are pushed onto the stack of psa_extend_page_table, in sample order, oldest page first:
+ * free_pages[*free_count .. *free_count_out).
+ *   weights           [num_pool_pages, Hkv, 16] f32 device, 16-byte aligned;  budgets [B] int32 device, pages.
+ *   free_pages        int32 device, in/out, room for free_capacity ids.
+ *   page_indices_out  [num_entries] int32 device: all of page_indices with the lists changed; may be page_indices.
+ *   lens_out          [B] int32 device or NULL; may be kv_lens.   free_count_out  may be free_count.
+ *   status            receives PSA_ERR_BOUNDS: a sample with a negative length or one beyond its list, or a budget below 1, is left as it is;
+ *                     a page id outside the pool weighs less than any other and is pushed as -1; if the stack has no room for all that
+ *                     would leave (or its height is out of range), nothing leaves.
+ *   scratch           device, 16-byte aligned, psa_evict_pages_scratch_bytes(B, num_entries) bytes, as above.
+ * Pages must belong to one list only.  The cache may be of either kind (ids are shared).  Enqueues two kernels.
+ */
+size_t psa_evict_pages_scratch_bytes(int32_t num_samples, int64_t num_entries);
+psa_status_t psa_evict_pages(const float *weights, int64_t num_pool_pages, int32_t num_kv_heads, const int32_t *page_indptr,
+                             const int32_t *page_indices, int64_t num_entries, const int32_t *kv_lens, const int32_t *budgets,
+                             int32_t num_samples, int32_t recent, int32_t *free_pages, int64_t free_capacity, const int32_t *free_count,
+                             int32_t *page_indices_out, int32_t *lens_out, int32_t *free_count_out, int32_t *status, void *scratch,
+                             size_t scratch_bytes, void *cuda_stream);
+
+/*
+ * What a row of logits says about a given token: with x = logits[r] / T_r and p = softmax(x),
+ *     logprobs[r] = ln p[tokens[r]],   entropy[r] = -sum_i p_i ln p_i,
+ *     top_ids[r, 0 .. top), top_logprobs[r, 0 .. top) = the `top` likeliest tokens in order (equal logits: the lower token first).
+ * For scoring answers (the paper keeps what scores well: Algorithm 1), verifying drafted tokens and reporting alternatives.
+ *   logits        as for psa_sample_tokens: bf16 or f32, 16-byte aligned, row_stride a multiple of 8, >= vocab.
+ *   tokens        [R] int32 device; NULL leaves logprobs out.  A token outside 0 .. vocab-1 gets -inf.
+ *   temperature   [R] f32 device or NULL (1); what is not positive and finite counts as 1.
+ *   logprobs, entropy [R] f32, top_ids int32 and top_logprobs f32 [R, top] with rows top_stride apart; each may be NULL.
+ * -inf logits (masked tokens) have probability 0 and log probability -inf, and come last, by token; a row of nothing else has entropy 0.
+ * A NaN or +inf logit makes the row's numbers NaN; NaN tokens are not listed (-1 where too few are left).
+ * top <= 64 and <= vocab <= 2^24, R <= 65535.  fp32 throughout; a fixed order of summation.  Needs no scratch memory; enqueues one kernel.
+ */
+psa_status_t psa_token_logprobs(const void *logits, int32_t logits_dtype, int64_t row_stride, int32_t num_rows, int32_t vocab,
+                                const int32_t *tokens, const float *temperature, float *logprobs, float *entropy, int32_t top,
+                                int32_t *top_ids, float *top_logprobs, int64_t top_stride, void *cuda_stream);
 
 /*
  * Self-test of the device-side error path (no counterpart in the paper).  Enqueues one tiny kernel whose only

@@ -49,3 +49,43 @@ def attend(q, k_pool, v_pool, page_indptr, page_indices, kv_lens, q_indptr, sm_s
                 size[row, h] = mine * size[row, h]
                 lse[row, h] = both
     return out, lse, size
+
+
+def accumulate(weights, q, lse, k_pool, page_indptr, page_indices, kv_lens, q_indptr, sm_scale):
+    """The array [pages, heads, 16] after a call, float64: cells of samples with new tokens get their sums, the new tokens' own from zero."""
+    got = weights.astype(np.float64)
+    group = q.shape[1] // k_pool.shape[1]
+    for s, length in enumerate(kv_lens):
+        a, b = int(q_indptr[s]), int(q_indptr[s + 1])
+        pages = page_indices[page_indptr[s]:page_indptr[s + 1]]
+        if a == b:
+            continue
+        for head in range(k_pool.shape[1]):
+            k = tokens_of(k_pool, pages, head, int(length))
+            for j in range(int(length)):
+                total = 0.0 if j >= int(length) - (b - a) else float(weights[pages[j // PAGE], head, j % PAGE])
+                first = max(a, a + j - (int(length) - (b - a)))
+                x = (q[first:b, head * group:(head + 1) * group].astype(np.float64) @ k[j]) * sm_scale - lse[first:b, head * group:(head + 1) * group]
+                got[pages[j // PAGE], head, j % PAGE] = total + np.exp(x).sum()
+    return got
+
+
+def evict(weights, page_indptr, page_indices, kv_lens, budgets, recent, free_pages, free_count):
+    """(page_indices, kv_lens, free_pages, free_count) after a call."""
+    out, lens, stack = np.array(page_indices), np.array(kv_lens), [int(p) for p in free_pages[:free_count]]
+    for s, length in enumerate(kv_lens):
+        held = -(-int(length) // PAGE)
+        mine = [int(p) for p in page_indices[page_indptr[s]:page_indptr[s] + held]]
+        budget = int(budgets[s])
+        if held <= budget:
+            continue
+        newest = min(recent, budget)
+        older = list(range(held - newest))
+        heavy = [np.nanmax(np.where(np.isnan(weights[p]), -np.inf, weights[p])) + 0.0 for p in mine]
+        stay = sorted(sorted(older, key=lambda i: (-heavy[i], i))[:budget - newest]) + list(range(held - newest, held))
+        stack += [mine[i] for i in older if i not in set(stay)]
+        out[page_indptr[s]:page_indptr[s] + held] = [mine[i] for i in stay] + [-1] * (held - budget)
+        lens[s] = int(length) - PAGE * (held - budget)
+    free = np.array(free_pages)
+    free[:len(stack)] = stack
+    return out, lens, free, len(stack)

@@ -23,6 +23,7 @@ EXPORTED_SYMBOLS = [
     "psa_page_table_scratch_bytes", "psa_build_page_table", "psa_extend_page_table", "psa_read_status", "psa_kv4_cell_bytes", "psa_store_kv4",
     "psa_load_kv4", "psa_plan_create_kv4", "psa_decode_kv4", "psa_decode_suffix_kv4", "psa_process_logits", "psa_mark_tokens",
     "psa_store_kv", "psa_attend_paged_scratch_bytes", "psa_attend_paged",
+    "psa_accumulate_weights_scratch_bytes", "psa_accumulate_weights", "psa_evict_pages_scratch_bytes", "psa_evict_pages", "psa_token_logprobs",
     "psa_status_string", "psa_last_error_message", "psa_version",
 ]
 
@@ -165,6 +166,17 @@ def library():
         lib.psa_attend_paged.restype = c_int32
         lib.psa_attend_paged.argtypes = [P, POINTER(c_int64), P, c_int64, c_int32, c_int32, c_int32, c_int32, c_float, P, P, POINTER(c_int64), c_int64, P, P,
                                          c_int64, P, P, c_int32, P, P, c_int32, P, P, P, c_size_t, P]
+        lib.psa_accumulate_weights_scratch_bytes.restype = c_size_t
+        lib.psa_accumulate_weights_scratch_bytes.argtypes = [c_int64, c_int32]
+        lib.psa_accumulate_weights.restype = c_int32
+        lib.psa_accumulate_weights.argtypes = [P, POINTER(c_int64), P, c_int64, c_int32, c_int32, c_int32, c_int32, c_float, P, P, POINTER(c_int64), c_int64, P,
+                                               P, c_int64, P, P, P, P, P, c_size_t, P]
+        lib.psa_evict_pages_scratch_bytes.restype = c_size_t
+        lib.psa_evict_pages_scratch_bytes.argtypes = [c_int32, c_int64]
+        lib.psa_evict_pages.restype = c_int32
+        lib.psa_evict_pages.argtypes = [P, c_int64, c_int32, P, P, c_int64, P, P, c_int32, c_int32, P, c_int64, P, P, P, P, P, P, c_size_t, P]
+        lib.psa_token_logprobs.restype = c_int32
+        lib.psa_token_logprobs.argtypes = [P, c_int32, c_int64, c_int32, c_int32, P, P, P, P, c_int32, P, P, c_int64, P]
         lib.psa_status_string.restype = c_char_p
         lib.psa_status_string.argtypes = [c_int32]
         lib.psa_last_error_message.restype = c_char_p
@@ -743,3 +755,64 @@ def _new3(like, stream):
     """_new of the shape and type of the three-dimensional `like`."""
     T, H, D = like.shape
     return _new((T * H, D), like, stream).view(T, H, D)
+
+
+def accumulate_weights_scratch(num_tokens, num_samples):
+    """Scratch tensor for accumulate_weights, to be kept by callers that must not allocate (uint8)."""
+    import torch
+    return torch.empty(int(library().psa_accumulate_weights_scratch_bytes(num_tokens, num_samples)), dtype=torch.uint8, device="cuda")
+
+
+def accumulate_weights(q, lse, k_pool, page_indptr, page_indices, kv_lens, q_indptr, weights, *, weights_out=None, sm_scale=None, status=None,
+                       scratch=None, stream=None):
+    """psa_accumulate_weights on torch CUDA tensors: add to weights [pages, Hkv, 16] f32 (or write to weights_out) the attention weight that
+    the rows q [T, Hq, D] with log-sum-exps lse [T, Hq] f32 gave to every cached token they see; new tokens start from zero.  Rows and
+    samples as for attend_paged."""
+    if status is not None:
+        status = _status_tensor(status)
+    if scratch is None:
+        scratch = _scratch(library().psa_accumulate_weights_scratch_bytes(q.shape[0], kv_lens.numel()), q, stream)
+    rc = (_calls or _native()).accumulate_weights(q, lse, k_pool, page_indptr, page_indices, kv_lens, q_indptr, weights, weights_out,
+                                                  q.shape[-1] ** -0.5 if sm_scale is None else sm_scale, status, scratch, stream)
+    if rc:
+        _check(rc)
+
+
+def evict_pages_scratch(num_samples, num_entries):
+    """Scratch tensor for evict_pages, to be kept by callers that must not allocate (uint8)."""
+    import torch
+    return torch.empty(int(library().psa_evict_pages_scratch_bytes(num_samples, num_entries)), dtype=torch.uint8, device="cuda")
+
+
+def evict_pages(weights, page_indptr, page_indices, kv_lens, budgets, recent, free_pages, free_count, *, page_indices_out=None, lens_out=None,
+                free_count_out=None, status=None, scratch=None, stream=None):
+    """psa_evict_pages on torch CUDA tensors (int32; weights [pages, Hkv, 16] f32): samples of more than budgets[s] pages keep their `recent`
+    newest and the heaviest others; ids that leave go onto the stack free_pages[0 .. free_count).  Lists, lengths and count are updated in
+    place where no output is given."""
+    if status is not None:
+        status = _status_tensor(status)
+    if scratch is None:
+        scratch = _scratch(library().psa_evict_pages_scratch_bytes(kv_lens.numel(), page_indices.numel()), weights, stream)
+    rc = (_calls or _native()).evict_pages(weights, page_indptr, page_indices, kv_lens, budgets, recent, free_pages, free_count, page_indices_out,
+                                           lens_out, free_count_out, status, scratch, stream)
+    if rc:
+        _check(rc)
+
+
+def token_logprobs(logits, tokens, top=0, *, temperature=None, logprobs=None, entropy=None, top_ids=None, top_logprobs=None, stream=None):
+    """psa_token_logprobs on torch CUDA tensors: of every row of logits [R, V] (bf16 or f32; rows may be padded) at temperature [R] f32 the
+    log probability of tokens [R] int32, the entropy, and the `top` likeliest tokens with theirs.  Returns (logprobs [R], entropy [R],
+    top_ids [R, top] int32, top_logprobs [R, top])."""
+    rows = logits.shape[0]
+    if logprobs is None:
+        logprobs = _new((rows,), logits, stream, "float32")
+    if entropy is None:
+        entropy = _new((rows,), logits, stream, "float32")
+    if top_ids is None:
+        top_ids = _new((rows, top), logits, stream, "int32")
+    if top_logprobs is None:
+        top_logprobs = _new((rows, top), logits, stream, "float32")
+    rc = (_calls or _native()).token_logprobs(logits, tokens, top, temperature, logprobs, entropy, top_ids, top_logprobs, stream)
+    if rc:
+        _check(rc)
+    return logprobs, entropy, top_ids, top_logprobs

@@ -14,7 +14,8 @@ INCLUDE = HERE.parent / "include"
 LIB = HERE / "libpsa.so"
 CALLS = HERE / "_torch_calls.so"      # a Python extension module (csrc/torch_calls.cpp)
 SOURCES = ["api.cu", "plan.cpp", "prefix_sm100.cu", "suffix_sm100.cu", "merge_sm100.cu", "static_workspace.cu", "append_sm100.cu", "sample_sm100.cu", "attn_tasks.cu",
-           "pages_sm100.cu", "kv4_sm100.cu", "suffix_kv4_sm100.cu", "logits_sm100.cu", "chunk_sm100.cu", "store_sm100.cu"]
+           "pages_sm100.cu", "kv4_sm100.cu", "suffix_kv4_sm100.cu", "logits_sm100.cu", "chunk_sm100.cu", "store_sm100.cu", "weights_sm100.cu", "evict_sm100.cu",
+           "logprobs_sm100.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-Xcompiler", "-fPIC", "-Xptxas", "-v", f"-I{INCLUDE}", f"-I{CSRC}",

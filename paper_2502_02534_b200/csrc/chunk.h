@@ -13,6 +13,7 @@ namespace psa {
 constexpr int kScheduleThreads = 1024;
 constexpr int kGroupRows = 256;                              // rows of a group: two row tiles of 128
 constexpr int kMostBlocks = 160;                             // persistent blocks, at most one per SM
+constexpr int kMostTokens = 1 << 30;                         // of one sample
 constexpr int64_t kMostChunkPages = int64_t(1) << 27, kMostChunkEntries = (int64_t(1) << 31) - 256;
 
 struct ChunkHeader {
@@ -47,6 +48,25 @@ struct ChunkArgs {
 };
 
 #ifdef __CUDACC__
+__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void grid_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+// A launch whose set-up may overlap the tail of the one before; its kernel calls grid_wait before it touches memory.
+template <class K, class... A>
+cudaError_t launch_dependent(K kernel, dim3 grid, int threads, int smem, cudaStream_t st, A... args)
+{
+    cudaLaunchConfig_t lc{};
+    lc.gridDim = grid;
+    lc.blockDim = dim3(threads);
+    lc.dynamicSmemBytes = smem;
+    lc.stream = st;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    lc.attrs = &attr;
+    lc.numAttrs = 1;
+    return cudaLaunchKernelEx(&lc, kernel, args...);
+}
+
 __device__ __forceinline__ void raise(int32_t *status, int code)
 {
     if (status) atomicCAS(status, 0, code);
@@ -68,7 +88,7 @@ __device__ __forceinline__ ChunkSample chunk_sample(const ChunkArgs &a, int s)
     if (b1 == b0) return {b0, 0, 0, 0};
     const int l0 = a.page_indptr[s], l1 = a.page_indptr[s + 1];
     int len = a.kv_lens[s];
-    if (l0 < 0 || l1 < l0 || l1 > a.num_entries || len < 0 || len > (long long)(l1 - l0) * kPageSize) {
+    if (l0 < 0 || l1 < l0 || l1 > a.num_entries || len < 0 || len > kMostTokens || len > (long long)(l1 - l0) * kPageSize) {
         raise(a.status, PSA_ERR_BOUNDS);
         len = 0;
     }
@@ -107,14 +127,15 @@ __device__ __forceinline__ int tile_at(const ChunkGroup &g, int group, long long
     return y >= (long long)tiles * w ? tiles : int(uint32_t(y) / uint32_t(w));
 }
 // the head and group that x lies in, searched by a whole warp
-__device__ __forceinline__ void locate(const ChunkArgs &a, const ChunkHeader &h, long long x, int lane, int *head, int *group)
+template <class Group>
+__device__ __forceinline__ void locate(const Group *groups, const ChunkHeader &h, long long x, int lane, int *head, int *group)
 {
     *head = int(x / h.per_head);
     const long long y = x - *head * h.per_head;
     int lo = 0, hi = h.groups;
     while (hi - lo > 1) {
         const int step = (hi - lo + 31) >> 5, at = lo + lane * step;
-        const unsigned below = __ballot_sync(0xffffffffu, at < hi && a.groups[at].cum <= y);
+        const unsigned below = __ballot_sync(0xffffffffu, at < hi && groups[at].cum <= y);
         lo += (__popc(below) - 1) * step;
         hi = min(hi, lo + step);
     }
@@ -140,7 +161,7 @@ struct ChunkWalk {
         const long long total = h.per_head * a.num_kv_heads;
         x0 = share_begin(total, block, h.blocks);
         x1 = share_begin(total, block + 1, h.blocks);
-        locate(a, h, x0, lane, &head, &gi);
+        locate(a.groups, h, x0, lane, &head, &gi);
     }
     __device__ __forceinline__ bool next(ChunkPiece &p)
     {
@@ -211,8 +232,8 @@ __device__ __forceinline__ void add_prior(const ChunkArgs &a, size_t at, float w
 // chunk_sm100.cu: places in a call's scratch memory (sets the pointers; returns the bytes), checks, tensor maps of q and the pools
 size_t chunk_layout(ChunkArgs &a, void *scratch, int head_dim);
 psa_status_t chunk_check(const ChunkArgs &a, const void *q, const int64_t q_strides[2], const void *pool, const int64_t pool_strides[3], int head_dim);
-psa_status_t chunk_maps(const ChunkArgs &a, const void *q, const int64_t q_strides[2], const void *const *pools, int num_pools,
-                        const int64_t pool_strides[3], int head_dim, CUtensorMap *maps);
+psa_status_t chunk_q_map(const ChunkArgs &a, const void *q, const int64_t q_strides[2], int head_dim, int rows, CUtensorMap *map);
+psa_status_t chunk_pool_map(const ChunkArgs &a, const void *pool, const int64_t pool_strides[3], int head_dim, CUtensorMap *map);
 int multiprocessors();   // of the current device; 0: there is none
 
 }  // namespace psa

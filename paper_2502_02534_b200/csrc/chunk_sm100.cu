@@ -39,8 +39,6 @@ constexpr float kHalfSumLimit = 64.f * 256.f * 1.01f;  // 64 exponentials of at 
 constexpr float kBias = 0.0040709119f, kUnbias = 0.99718224f;
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 
-__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-__device__ __forceinline__ void grid_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // ------------------------------------------------------------------------------------------------------------- schedule
 // Running sums over the samples by one block; every thread takes samples of its own (a sample's groups one after another).
@@ -394,7 +392,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
                         const bool poly = ((i >> 1) % 3) == 2;   // a third by polynomial, where the special-function unit is the bound
                         const float x0 = fmaf(__uint_as_float(r[i / 32][i % 32]), a.scale_log2, off);
                         const float x1 = fmaf(__uint_as_float(r[i / 32][i % 32 + 1]), a.scale_log2, off);
-                        const float p0 = poly ? poly_exp2(x0) : fast_exp2(x0), p1 = poly ? poly_exp2(x1) : fast_exp2(x1);
+                        const float p0 = poly ? poly_exp2_fine<4>(x0) : fast_exp2(x0), p1 = poly ? poly_exp2_fine<4>(x1) : fast_exp2(x1);
                         sum[(i >> 1) & 3] += p0 + p1;
                         r[0][i / 2] = __byte_perm(__float_as_uint(p0), __float_as_uint(p1), 0x7632);
                     }
@@ -582,7 +580,7 @@ chunk_merge_kernel(const ChunkArgs a)
     const long long total = h.per_head * a.num_kv_heads;
     const long long x = share_begin(total, cut + 1, h.blocks);
     int head, gi;
-    locate(a, h, x, lane, &head, &gi);
+    locate(a.groups, h, x, lane, &head, &gi);
     if (head >= a.num_kv_heads) return;
     const ChunkGroup g = a.groups[gi];
     const long long base = head * h.per_head + g.cum;
@@ -644,22 +642,6 @@ chunk_merge_kernel(const ChunkArgs a)
     }
 }
 
-template <class K, class... A>
-cudaError_t launch_dependent(K kernel, dim3 grid, int threads, int smem, cudaStream_t st, A... args)
-{
-    cudaLaunchConfig_t lc{};
-    lc.gridDim = grid;
-    lc.blockDim = dim3(threads);
-    lc.dynamicSmemBytes = smem;
-    lc.stream = st;
-    cudaLaunchAttribute attr{};
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    lc.attrs = &attr;
-    lc.numAttrs = 1;
-    return cudaLaunchKernelEx(&lc, kernel, args...);
-}
-
 template <int D>
 cudaError_t launch(const ChunkArgs &a, const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorMap &mv, cudaStream_t st)
 {
@@ -719,24 +701,27 @@ psa_status_t chunk_check(const ChunkArgs &a, const void *q, const int64_t q_stri
     return PSA_OK;
 }
 
-psa_status_t chunk_maps(const ChunkArgs &a, const void *q, const int64_t q_strides[2], const void *const *pools, int num_pools, const int64_t pool_strides[3],
-                        int head_dim, CUtensorMap *maps)
+psa_status_t chunk_q_map(const ChunkArgs &a, const void *q, const int64_t q_strides[2], int head_dim, int rows, CUtensorMap *map)
 {
+    // Q as (d, g, kv head, token): a box of (64, G, 1, rows / G) is one 64-wide half of a row tile, g fastest
+    const cuuint64_t dims[4] = {cuuint64_t(head_dim), cuuint64_t(a.group), cuuint64_t(a.num_kv_heads), cuuint64_t(a.num_tokens)};
+    const cuuint64_t strides[3] = {cuuint64_t(q_strides[1]) * 2, cuuint64_t(q_strides[1]) * a.group * 2, cuuint64_t(q_strides[0]) * 2};
+    const cuuint32_t box[4] = {64, cuuint32_t(a.group), 1, cuuint32_t(rows / a.group)};
     std::string err;
     EncodeFn fn = get_encode_fn(&err);
-    if (!fn) return set_last_error(PSA_ERR_CUDA, err);
-    {   // Q as (d, g, kv head, token): a box of (64, G, 1, 128 / G) is one 64-wide half of a row tile, g fastest
-        const cuuint64_t dims[4] = {cuuint64_t(head_dim), cuuint64_t(a.group), cuuint64_t(a.num_kv_heads), cuuint64_t(a.num_tokens)};
-        const cuuint64_t strides[3] = {cuuint64_t(q_strides[1]) * 2, cuuint64_t(q_strides[1]) * a.group * 2, cuuint64_t(q_strides[0]) * 2};
-        const cuuint32_t box[4] = {64, cuuint32_t(a.group), 1, cuuint32_t(kRowTile / a.group)};
-        if (!encode(fn, &maps[0], q, 4, dims, strides, box, &err)) return set_last_error(PSA_ERR_CUDA, err);
-    }
-    for (int i = 0; i < num_pools; ++i) {   // a pool as (d, slot, kv head, page): a box is one 64-wide half of a page
-        const cuuint64_t dims[4] = {cuuint64_t(head_dim), kPageSize, cuuint64_t(a.num_kv_heads), cuuint64_t(a.num_pool_pages)};
-        const cuuint64_t strides[3] = {cuuint64_t(pool_strides[2]) * 2, cuuint64_t(pool_strides[1]) * 2, cuuint64_t(pool_strides[0]) * 2};
-        const cuuint32_t box[4] = {64, kPageSize, 1, 1};
-        if (!encode(fn, &maps[1 + i], pools[i], 4, dims, strides, box, &err)) return set_last_error(PSA_ERR_CUDA, err);
-    }
+    if (!fn || !encode(fn, map, q, 4, dims, strides, box, &err)) return set_last_error(PSA_ERR_CUDA, err);
+    return PSA_OK;
+}
+
+psa_status_t chunk_pool_map(const ChunkArgs &a, const void *pool, const int64_t pool_strides[3], int head_dim, CUtensorMap *map)
+{
+    // a pool as (d, slot, kv head, page): a box is one 64-wide half of a page
+    const cuuint64_t dims[4] = {cuuint64_t(head_dim), kPageSize, cuuint64_t(a.num_kv_heads), cuuint64_t(a.num_pool_pages)};
+    const cuuint64_t strides[3] = {cuuint64_t(pool_strides[2]) * 2, cuuint64_t(pool_strides[1]) * 2, cuuint64_t(pool_strides[0]) * 2};
+    const cuuint32_t box[4] = {64, kPageSize, 1, 1};
+    std::string err;
+    EncodeFn fn = get_encode_fn(&err);
+    if (!fn || !encode(fn, map, pool, 4, dims, strides, box, &err)) return set_last_error(PSA_ERR_CUDA, err);
     return PSA_OK;
 }
 
@@ -802,8 +787,9 @@ extern "C" psa_status_t psa_attend_paged(const void *q, const int64_t q_strides[
     if (a.blocks <= 0) return set_last_error(PSA_ERR_CUDA, "no CUDA device");
     chunk_layout(a, scratch, head_dim);
     CUtensorMap maps[3];
-    const void *pools[2] = {k_pool, v_pool};
-    rc = chunk_maps(a, q, q_strides, pools, 2, pool_strides, head_dim, maps);
+    rc = chunk_q_map(a, q, q_strides, head_dim, kRowTile, &maps[0]);
+    if (rc == PSA_OK) rc = chunk_pool_map(a, k_pool, pool_strides, head_dim, &maps[1]);
+    if (rc == PSA_OK) rc = chunk_pool_map(a, v_pool, pool_strides, head_dim, &maps[2]);
     if (rc != PSA_OK) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     const cudaError_t e = head_dim == 128 ? launch<128>(a, maps[0], maps[1], maps[2], st) : launch<64>(a, maps[0], maps[1], maps[2], st);

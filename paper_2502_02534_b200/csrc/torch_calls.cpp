@@ -37,6 +37,9 @@ struct Api {
     decltype(&psa_mark_tokens) mark_tokens;
     decltype(&psa_store_kv) store_kv;
     decltype(&psa_attend_paged) attend_paged;
+    decltype(&psa_accumulate_weights) accumulate_weights;
+    decltype(&psa_evict_pages) evict_pages;
+    decltype(&psa_token_logprobs) token_logprobs;
 } api{};
 
 const char *name_of(at::ScalarType t)
@@ -432,6 +435,88 @@ psa_status_t attend_paged(PyObject *const *args, Py_ssize_t given)
                             r.lens, prior, prior_code, prior_lse, out.data_ptr(), out_code, lse, status, scratch, size_t(c.numel(13)), stream);
 }
 
+// weights of cached tokens: f32 [pages, heads, 16], contiguous
+float *cell_weights(Call &c, int i, const char *name, int64_t pages, int64_t heads)
+{
+    const at::Tensor &t = c.tensor(i, name);
+    if (t.scalar_type() != at::kFloat || t.dim() != 3 || t.size(0) != pages || t.size(1) != heads || t.size(2) != 16 || !t.is_contiguous())
+        throw Refused(std::string(name) + " must be f32 [" + std::to_string(pages) + ", " + std::to_string(heads) + ", 16], contiguous");
+    return static_cast<float *>(t.data_ptr());
+}
+
+// q, lse, k_pool, page_indptr, page_indices, kv_lens, q_indptr, weights, weights_out, sm_scale, status, scratch, stream
+psa_status_t accumulate_weights(PyObject *const *args, Py_ssize_t given)
+{
+    Call c(args, given, 13);
+    const Rows r(c, 3, 6);
+    const auto *lse = c.needed<float>(1, at::kFloat, "lse", r.tokens * r.heads);
+    const at::Tensor &k_pool = c.tensor(2, "k_pool");
+    if (k_pool.dim() != 4) throw Refused("k_pool must be bf16 [pages, heads, 16, head_dim]");
+    const int64_t kv = k_pool.size(1);
+    const Pools pools(k_pool, nullptr, kv, r.dim);
+    const float *weights = cell_weights(c, 7, "weights", pools.pages, kv);
+    float *weights_out = c.none(8) ? const_cast<float *>(weights) : cell_weights(c, 8, "weights_out", pools.pages, kv);
+    const double scale = c.real(9);
+    int32_t *status = c.status(10);
+    void *scratch = c.needed(11, at::kByte, "scratch");
+    void *stream = c.stream(12);
+    return api.accumulate_weights(r.q->data_ptr(), r.strides, r.q_indptr, r.tokens, int32_t(r.samples), int32_t(r.heads),
+                                  int32_t(std::min<int64_t>(kv, 0x7fffffff)), int32_t(r.dim), float(scale), lse, k_pool.data_ptr(), pools.strides,
+                                  pools.pages, r.indptr, r.indices, r.entries, r.lens, weights, weights_out, status, scratch, size_t(c.numel(11)), stream);
+}
+
+// weights, page_indptr, page_indices, kv_lens, budgets, recent, free_pages, free_count, page_indices_out, lens_out, free_count_out, status,
+// scratch, stream
+psa_status_t evict_pages(PyObject *const *args, Py_ssize_t given)
+{
+    Call c(args, given, 14);
+    const at::Tensor &t = c.tensor(0, "weights");
+    if (t.dim() != 3) throw Refused("weights must be f32 [pages, heads, 16], contiguous");
+    const float *weights = cell_weights(c, 0, "weights", t.size(0), t.size(1));
+    const auto *lens = c.needed<int32_t>(3, at::kInt, "kv_lens");
+    const int64_t n = c.numel(3);
+    if (n > 0x7fffffff || t.size(1) > 0x7fffffff) throw Refused("too many samples or heads");
+    const auto *indptr = c.needed<int32_t>(1, at::kInt, "page_indptr", n + 1);
+    auto *indices = c.needed<int32_t>(2, at::kInt, "page_indices");
+    const int64_t entries = c.numel(2);
+    const auto *budgets = c.needed<int32_t>(4, at::kInt, "budgets", n);
+    const int64_t recent = c.integer(5);
+    if (recent < 1 || recent > 0x7fffffff) throw Refused("recent must be at least 1");
+    auto *free_pages = c.needed<int32_t>(6, at::kInt, "free_pages");
+    auto *count = c.needed<int32_t>(7, at::kInt, "free_count", 1);
+    auto *indices_out = c.flat<int32_t>(8, at::kInt, "page_indices_out", entries);
+    auto *lens_out = c.flat<int32_t>(9, at::kInt, "lens_out", n);
+    auto *count_out = c.flat<int32_t>(10, at::kInt, "free_count_out", 1);
+    int32_t *status = c.status(11);
+    void *scratch = c.needed(12, at::kByte, "scratch");
+    void *stream = c.stream(13);
+    return api.evict_pages(weights, t.size(0), int32_t(t.size(1)), indptr, indices, entries, lens, budgets, int32_t(n), int32_t(recent), free_pages,
+                           c.numel(6), count, indices_out ? indices_out : indices, lens_out ? lens_out : const_cast<int32_t *>(lens),
+                           count_out ? count_out : count, status, scratch, size_t(c.numel(12)), stream);
+}
+
+// logits, tokens, top, temperature, logprobs, entropy, top_ids, top_logprobs, stream
+psa_status_t token_logprobs(PyObject *const *args, Py_ssize_t given)
+{
+    Call c(args, given, 9);
+    const at::Tensor &logits = c.tensor(0, "logits");
+    if (logits.dim() != 2) throw Refused("logits must be [rows, vocab]");
+    const int32_t code = dtype_code(logits, "logits");
+    const int64_t R = logits.size(0), V = logits.size(1), top = c.integer(2);
+    if (R > 0x7fffffff || V > 0x7fffffff || top < 0 || top > 0x7fffffff) throw Refused("logits or top are too large");
+    if (V > 1 && logits.stride(1) != 1) throw Refused("logits must be contiguous along the vocabulary");
+    const int64_t stride = R > 1 ? logits.stride(0) : (V + 7) / 8 * 8;   // one row has no stride of its own
+    const auto *tokens = c.flat<int32_t>(1, at::kInt, "tokens", R);
+    const auto *temperature = c.flat<float>(3, at::kFloat, "temperature", R);
+    auto *logprobs = c.flat<float>(4, at::kFloat, "logprobs", R);
+    auto *entropy = c.flat<float>(5, at::kFloat, "entropy", R);
+    auto *ids = c.flat<int32_t>(6, at::kInt, "top_ids", R * top);
+    auto *top_logprobs = c.flat<float>(7, at::kFloat, "top_logprobs", R * top);
+    void *stream = c.stream(8);
+    return api.token_logprobs(logits.data_ptr(), code, stride, int32_t(R), int32_t(V), tokens, temperature, logprobs, entropy, int32_t(top), ids,
+                              top_logprobs, top, stream);
+}
+
 struct Bitmaps {
     const uint32_t *bits = nullptr;
     const int32_t *rows = nullptr;
@@ -560,7 +645,8 @@ PyObject *attach(PyObject *, PyObject *path)
         {"psa_store_kv4", reinterpret_cast<void **>(&api.store_kv4)},               {"psa_load_kv4", reinterpret_cast<void **>(&api.load_kv4)},
         {"psa_decode_kv4", reinterpret_cast<void **>(&api.decode_kv4)},             {"psa_process_logits", reinterpret_cast<void **>(&api.process_logits)},
         {"psa_mark_tokens", reinterpret_cast<void **>(&api.mark_tokens)},           {"psa_store_kv", reinterpret_cast<void **>(&api.store_kv)},
-        {"psa_attend_paged", reinterpret_cast<void **>(&api.attend_paged)},
+        {"psa_attend_paged", reinterpret_cast<void **>(&api.attend_paged)},         {"psa_accumulate_weights", reinterpret_cast<void **>(&api.accumulate_weights)},
+        {"psa_evict_pages", reinterpret_cast<void **>(&api.evict_pages)},           {"psa_token_logprobs", reinterpret_cast<void **>(&api.token_logprobs)},
     };
     for (const auto &w : wanted)
         if (!(*w.to = dlsym(lib, w.name))) return PyErr_Format(PyExc_ImportError, "%s lacks %s", p, w.name);
@@ -576,7 +662,8 @@ PyMethodDef method(const char *name)
 PyMethodDef methods[] = {
     method<build_page_table>("build_page_table"), method<extend_page_table>("extend_page_table"), method<store_kv4>("store_kv4"),
     method<load_kv4>("load_kv4"), method<decode_kv4>("decode_kv4"), method<process_logits>("process_logits"), method<mark_tokens>("mark_tokens"),
-    method<store_kv>("store_kv"), method<attend_paged>("attend_paged"),
+    method<store_kv>("store_kv"), method<attend_paged>("attend_paged"), method<accumulate_weights>("accumulate_weights"),
+    method<evict_pages>("evict_pages"), method<token_logprobs>("token_logprobs"),
     {"prefix_strides", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&prefix_strides)), METH_FASTCALL, nullptr},
     {"empty", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&empty)), METH_FASTCALL, nullptr},
     {"attach", attach, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr},

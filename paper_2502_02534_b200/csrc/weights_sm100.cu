@@ -1,0 +1,589 @@
+// The attention weight that every cached token received (psa_accumulate_weights): for KV head h and the key at position j of a sample,
+//     w[j] <- w[j] + sum over rows that see j, and the head's query heads, of 2^(c s_j - lse2),     s = q.k,  c = sm_scale log2 e,
+// with the rows' finished log-sum-exp as given; the new tokens' own weights start from zero.
+//
+// The transpose of attention's scores: S^T = K Q^T puts a key on every tensor-memory lane and the rows along its columns, so a thread sums
+// its own key's weights in a register -- no exchange, no atomics, one order of summation whatever the scheduling.  Two key tiles (a PAIR
+// of 128 keys each) stay in shared memory while the rows' tiles stream past both.  One exponential per key and row is the bound for
+// chunks; for a few rows (a decode step) it is reading K once.
+//
+// Work units are (KV head, sample, key pair, row tile); a share is a run of them, as in chunk.h.  A pair's rows may be cut between shares:
+// each then leaves 256 partial sums, which weights_merge_kernel adds in order.
+//
+// 10 warps: 0-3 and 4-7 take the first and second key tile of a pair (thread = key), 8 producer (TMA; also the rows' log-sum-exps), 9 MMA
+// issuer and owner of the tensor memory.  Two score buffers of 128 columns for each key tile.  Every wait is bounded.
+#include <algorithm>
+
+#include "chunk.h"
+#include "psa_internal.h"
+#include "tensor_core.cuh"
+
+namespace psa {
+namespace {
+
+constexpr int kPairKeys = 256, kTileKeys = 128, kRowTile = 128, kFewRows = 16;
+constexpr int kPairCost = 4, kRowCost = 2, kLeastShare = 8;
+constexpr float kLog2e = 1.4426950408889634f;
+
+// Consecutive pairs of one sample that the same row tiles see.
+struct WeightsGroup {
+    long long cum;
+    int32_t q0, n;           // rows of q: first token, tokens
+    int32_t pos0, len;
+    int32_t list0, first_pair, pairs, first_tile;   // first_tile: the first row tile that sees them
+};
+static_assert(sizeof(WeightsGroup) == 40, "");
+struct WeightsArgs {
+    ChunkArgs c;             // q, samples, pages, status, shares
+    WeightsGroup *groups;
+    const float *lse, *weights;
+    float *weights_out;
+    float *partial;          // [2 * blocks, 256]
+};
+
+__device__ __forceinline__ int row_tiles(int n, int group) { return (n * group + kRowTile - 1) / kRowTile; }
+__device__ __forceinline__ int pair_cost(const WeightsGroup &g, int group) { return kPairCost + kRowCost * (row_tiles(g.n, group) - g.first_tile); }
+
+// ------------------------------------------------------------------------------------------------------------- schedule
+struct Cut {
+    int diagonal;            // first pair that some row does not see
+    int pairs, tiles;
+    long long cost;
+};
+__device__ __forceinline__ int first_tile_of(const ChunkSample &s, int pair, int group)   // first row tile that sees the pair's first key
+{
+    const long long i = max(0ll, (long long)pair * kPairKeys - (s.len - s.n));
+    return int(i * group / kRowTile);
+}
+__device__ __forceinline__ Cut cut_of(const ChunkSample &s, int group)
+{
+    Cut c{};
+    if (s.n == 0 || s.len == 0) return c;
+    c.pairs = (s.len + kPairKeys - 1) / kPairKeys;
+    c.tiles = row_tiles(s.n, group);
+    c.diagonal = s.len < s.n ? 0 : min(c.pairs, (s.len - s.n) / kPairKeys + 1);
+    c.cost = (long long)c.diagonal * (kPairCost + kRowCost * c.tiles);
+    for (int p = c.diagonal; p < c.pairs; ++p) c.cost += kPairCost + kRowCost * (c.tiles - first_tile_of(s, p, group));
+    return c;
+}
+__global__ void __launch_bounds__(kScheduleThreads)
+weights_schedule_kernel(WeightsArgs w)
+{
+    __shared__ long long sum_cost[kScheduleThreads / 32];
+    __shared__ int sum_groups[kScheduleThreads / 32];
+    grid_release();
+    const ChunkArgs &a = w.c;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    long long carry_cost = 0;
+    int carry_groups = 0;
+    for (int s0 = 0; s0 < a.num_samples; s0 += kScheduleThreads) {
+        const int s = s0 + int(threadIdx.x);
+        ChunkSample cs{};
+        Cut c{};
+        if (s < a.num_samples) {
+            cs = chunk_sample(a, s);
+            c = cut_of(cs, a.group);
+        }
+        const int groups = (c.diagonal > 0) + c.pairs - c.diagonal;
+        long long x = c.cost;
+        int y = groups;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const long long ux = __shfl_up_sync(0xffffffffu, x, d);
+            const int uy = __shfl_up_sync(0xffffffffu, y, d);
+            if (lane >= d) { x += ux; y += uy; }
+        }
+        if (lane == 31) { sum_cost[warp] = x; sum_groups[warp] = y; }
+        __syncthreads();
+        long long at = carry_cost + x - c.cost;
+        int to = carry_groups + y - groups;
+        for (int k = 0; k < kScheduleThreads / 32; ++k) {
+            if (k < warp) { at += sum_cost[k]; to += sum_groups[k]; }
+            carry_cost += sum_cost[k];
+            carry_groups += sum_groups[k];
+        }
+        __syncthreads();
+        WeightsGroup g{};
+        g.q0 = cs.q0; g.n = cs.n; g.pos0 = cs.len - cs.n; g.len = cs.len; g.list0 = cs.list0;
+        auto put = [&](int first, int pairs, int first_tile) {
+            g.cum = at; g.first_pair = first; g.pairs = pairs; g.first_tile = first_tile;
+            if (to < a.max_groups) w.groups[to] = g;
+            ++to;
+            at += (long long)pairs * pair_cost(g, a.group);
+        };
+        if (c.diagonal > 0) put(0, c.diagonal, 0);
+        for (int p = c.diagonal; p < c.pairs; ++p) put(p, 1, first_tile_of(cs, p, a.group));
+    }
+    if (threadIdx.x == 0) {
+        if (carry_groups > a.max_groups) {   // q_indptr that runs backwards: more rows than there are
+            raise(a.status, PSA_ERR_BOUNDS);
+            carry_groups = 0;
+            carry_cost = 0;
+        }
+        ChunkHeader h{};
+        h.per_head = carry_cost;
+        h.groups = carry_groups;
+        h.blocks = int(max(1ll, min((long long)a.blocks, carry_cost * a.num_kv_heads / kLeastShare)));
+        *a.header = h;
+    }
+}
+
+// A place inside a group: the pair, and how many of its row tiles lie before it.
+struct Place { int pair, rows; };
+__device__ __forceinline__ Place place_of(const WeightsGroup &g, int group, long long y)   // y: cost from the group's begin
+{
+    const int cost = pair_cost(g, group);
+    if (y <= 0) return {0, 0};
+    if (y >= (long long)cost * g.pairs) return {g.pairs, 0};
+    const int pair = int(y / cost), rest = int(y - (long long)pair * cost);
+    const int rows = max(0, rest - kPairCost) / kRowCost;
+    return {pair, rows};
+}
+struct WeightsPiece {
+    WeightsGroup g;
+    int head;
+    Place from, to;          // [from, to)
+};
+struct WeightsWalk {
+    const WeightsArgs &w;
+    ChunkHeader h;
+    long long x0 = 0, x1 = 0;
+    int head, gi = 0;
+    __device__ __forceinline__ WeightsWalk(const WeightsArgs &args, int block, int lane) : w(args), h(*args.c.header)
+    {
+        head = w.c.num_kv_heads;
+        if (block >= h.blocks || h.groups == 0) return;
+        const long long total = h.per_head * w.c.num_kv_heads;
+        x0 = share_begin(total, block, h.blocks);
+        x1 = share_begin(total, block + 1, h.blocks);
+        locate(w.groups, h, x0, lane, &head, &gi);
+    }
+    __device__ __forceinline__ bool next(WeightsPiece &p)
+    {
+        for (;;) {
+            if (gi >= h.groups) {
+                gi = 0;
+                ++head;
+            }
+            if (head >= w.c.num_kv_heads) return false;
+            p.g = w.groups[gi];
+            const long long base = head * h.per_head + p.g.cum;
+            if (base >= x1) {
+                head = w.c.num_kv_heads;
+                return false;
+            }
+            ++gi;
+            p.head = head;
+            p.from = place_of(p.g, w.c.group, x0 - base);
+            p.to = place_of(p.g, w.c.group, x1 - base);
+            if (p.from.pair < p.to.pair || p.from.rows < p.to.rows) return true;
+        }
+    }
+};
+// One key's finished sum to its cell: new tokens start from zero.
+__device__ __forceinline__ void finish(const WeightsArgs &w, const WeightsGroup &g, int head, int pos, float sum)
+{
+    if (pos >= g.len) return;
+    const int page = w.c.page_indices[g.list0 + pos / kPageSize];
+    if (page < 0 || page >= w.c.num_pool_pages) return;   // reported by the load of its keys
+    const size_t at = (size_t(page) * w.c.num_kv_heads + head) * kPageSize + pos % kPageSize;
+    w.weights_out[at] = (pos < g.pos0 ? w.weights[at] : 0.f) + sum;
+}
+// The pairs of a piece, with the row tiles of each: pair, [r0, r1) counted from the row tiles that see it
+template <class F>
+__device__ __forceinline__ void each_pair(const WeightsPiece &p, int count, F f)
+{
+    for (int pair = p.from.pair; pair <= p.to.pair; ++pair) {
+        const int r0 = pair == p.from.pair ? p.from.rows : 0, r1 = pair == p.to.pair ? p.to.rows : count;
+        if (r0 < r1 && !f(pair, r0, r1)) return;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------------- sums
+template <int D>
+struct WeightsSmem {
+    static constexpr int kHalves = D / 64;
+    static constexpr int kHalfBytes = 128 * 128;
+    static constexpr int kTileBytes = kHalves * kHalfBytes;
+    static constexpr int kKRing = D == 128 ? 4 : 8, kQRing = D == 128 ? 3 : 6;   // tiles; K comes in pairs
+    static constexpr int kLseRing = 4;
+    static constexpr int kBarKFull = 0, kBarKEmpty = kBarKFull + kKRing, kBarQFull = kBarKEmpty + kKRing, kBarQEmpty = kBarQFull + kQRing,
+                         kBarLFull = kBarQEmpty + kQRing, kBarLEmpty = kBarLFull + kLseRing, kBarS = kBarLEmpty + kLseRing, kBarSFree = kBarS + 4,
+                         kBarDrain = kBarSFree + 4, kNumBars = kBarDrain + 1;
+    static constexpr int kTmemPtrOff = 8 * kNumBars, kAbortOff = kTmemPtrOff + 4;
+    static constexpr int kLseOff = 1024;
+    static constexpr int kQOff = kLseOff + kLseRing * 512;
+    static constexpr int kKOff = kQOff + kQRing * kTileBytes;
+    static constexpr int kTotal = kKOff + kKRing * kTileBytes;
+    static_assert(kAbortOff + 4 <= kLseOff && kQOff % 1024 == 0 && kTotal <= 227 * 1024, "shared memory plan");
+};
+
+template <int D>
+__global__ void __launch_bounds__(320, 1)
+weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_few, const __grid_constant__ CUtensorMap map_k,
+               const WeightsArgs w)
+{
+    using L = WeightsSmem<D>;
+    constexpr int kProducerWarp = 8, kMmaWarp = 9, kKSteps = D / 16;
+    const ChunkArgs &a = w.c;
+    extern __shared__ __align__(1024) unsigned char smem[];
+    const uint32_t sbase = smem_u32(smem);
+    if (sbase & 1023u) {
+        if (threadIdx.x == 0) raise(a.status, PSA_ERR_BOUNDS);
+        return;
+    }
+    volatile uint32_t *tmem_ptr = reinterpret_cast<volatile uint32_t *>(smem + L::kTmemPtrOff);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + L::kAbortOff);
+    auto bar = [&](int i) { return sbase + 8 * i; };
+    auto warp_wait = [&](uint32_t b, uint32_t parity) {   // the whole warp goes on, or the whole warp gives up
+        return __all_sync(0xffffffffu, mbar_wait(b, parity, abort_flag)) != 0;
+    };
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        *abort_flag = 0;
+        for (int i = 0; i < L::kNumBars; ++i) {
+            // a log-sum-exp slot is filled by 32 lanes and read by 8 warps, a score buffer is read by 4
+            const int count = i >= L::kBarLFull && i < L::kBarLEmpty ? 32 : i >= L::kBarLEmpty && i < L::kBarS ? 8 : i >= L::kBarSFree && i < L::kBarDrain ? 4 : 1;
+            mbar_init(bar(i), count);
+        }
+        fence_barrier_init();
+    }
+    if (warp == kMmaWarp) {
+        tmem_alloc(smem_u32(const_cast<uint32_t *>(tmem_ptr)), 512);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_ptr;
+    grid_wait();
+    grid_release();
+
+    WeightsWalk walk(w, blockIdx.x, lane);
+    WeightsPiece pc;
+    bool ok = true;
+
+    // The order of things, which every role follows: for each pair of a piece its K tiles, then its row tiles one by one.  A sample with
+    // one row tile has it loaded once for all pairs of a piece.
+    if (warp == kProducerWarp) {
+        uint32_t ke = 0, qe = 0, le = 0;
+        const int shift = __ffs(a.group) - 1;
+        while (ok && walk.next(pc)) {
+            const WeightsGroup &g = pc.g;
+            const int tiles = row_tiles(g.n, a.group), count = tiles - g.first_tile;
+            const bool few = g.n * a.group <= kFewRows;
+            bool have_q = false;
+            auto load_q = [&](int tile) {
+                const int slot = qe % L::kQRing, use = qe / L::kQRing;
+                if (use > 0 && !(ok = warp_wait(bar(L::kBarQEmpty + slot), (use - 1) & 1))) return;
+                ++qe;
+                if (lane == 0) {
+                    const uint32_t full = bar(L::kBarQFull + slot), dst = sbase + L::kQOff + slot * L::kTileBytes;
+                    mbar_expect_tx(full, (few ? kFewRows : kRowTile) * D * 2);
+                    for (int h = 0; h < L::kHalves; ++h)
+                        tma_load_4d(dst + h * L::kHalfBytes, few ? &map_few : &map_q, full, h * 64, 0, pc.head, g.q0 + tile * (kRowTile / a.group));
+                }
+                // minus the rows' log-sum-exps, in log2; what does not exist or saw nothing gives no weight
+                const int ls = le % L::kLseRing, lu = le / L::kLseRing;
+                if (lu > 0 && !(ok = warp_wait(bar(L::kBarLEmpty + ls), (lu - 1) & 1))) return;
+                ++le;
+                float4 v;
+                float *pv = reinterpret_cast<float *>(&v);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = tile * kRowTile + lane * 4 + i;
+                    float off = -INFINITY;
+                    if (r < g.n * a.group) {
+                        const float x = w.lse[size_t(g.q0 + (r >> shift)) * a.num_q_heads + pc.head * a.group + (r & (a.group - 1))];
+                        off = x == -INFINITY ? -INFINITY : -x * kLog2e;
+                    }
+                    pv[i] = off;
+                }
+                *reinterpret_cast<float4 *>(smem + L::kLseOff + ls * 512 + lane * 16) = v;
+                mbar_arrive(bar(L::kBarLFull + ls));
+            };
+            each_pair(pc, count, [&](int pair, int r0, int r1) {
+                for (int t = 0; t < 2; ++t, ++ke) {
+                    const int key0 = (g.first_pair + pair) * kPairKeys + t * kTileKeys;
+                    const int pages = min(8, max(0, (g.len - key0 + kPageSize - 1) / kPageSize));
+                    int id = 0;
+                    if (lane < pages * L::kHalves) id = a.page_indices[g.list0 + key0 / kPageSize + lane / L::kHalves];
+                    const int slot = ke % L::kKRing, use = ke / L::kKRing;
+                    if (use > 0 && !(ok = warp_wait(bar(L::kBarKEmpty + slot), (use - 1) & 1))) return false;
+                    const uint32_t full = bar(L::kBarKFull + slot), dst = sbase + L::kKOff + slot * L::kTileBytes;
+                    if (lane == 0) mbar_expect_tx(full, pages * kPageSize * D * 2);   // no page: the barrier completes at once
+                    __syncwarp();
+                    if (lane < pages * L::kHalves) {
+                        const int p = lane / L::kHalves, h = lane % L::kHalves;
+                        if (id < 0 || id >= a.num_pool_pages) {
+                            raise(a.status, PSA_ERR_BOUNDS);
+                            id = a.num_pool_pages;   // outside the map: zeros
+                        }
+                        tma_load_4d(dst + h * L::kHalfBytes + p * kPageSize * 128, &map_k, full, h * 64, 0, pc.head, id);
+                    }
+                }
+                if (tiles == 1) {
+                    if (!have_q) load_q(0);
+                    have_q = true;
+                } else {
+                    for (int r = r0; ok && r < r1; ++r) load_q(g.first_tile + r);
+                }
+                return ok;
+            });
+        }
+    } else if (warp == kMmaWarp) {
+        if (elect_one()) {
+            constexpr uint64_t kHi = uint64_t(smem_desc_hi(1024)) << 32;
+            const uint64_t q_desc = kHi | smem_desc_lo(sbase + L::kQOff, 16), k_desc = kHi | smem_desc_lo(sbase + L::kKOff, 16);
+            constexpr uint32_t kIdesc = make_idesc(kRowTile, false), kIdescFew = make_idesc(kFewRows, false);
+            uint32_t ke = 0, qe = 0, se = 0;
+            while (ok && walk.next(pc)) {
+                const int tiles = row_tiles(pc.g.n, a.group), count = tiles - pc.g.first_tile;
+                const bool few = pc.g.n * a.group <= kFewRows;
+                bool have_q = false;
+                int q_slot = 0;
+                each_pair(pc, count, [&](int pair, int r0, int r1) {
+                    int k_slot[2];
+                    for (int t = 0; t < 2; ++t, ++ke) {
+                        k_slot[t] = ke % L::kKRing;
+                        if (!(ok = mbar_wait(bar(L::kBarKFull + k_slot[t]), (ke / L::kKRing) & 1, abort_flag))) return false;
+                    }
+                    for (int r = r0; r < r1; ++r, ++se) {
+                        if (tiles > 1 || !have_q) {
+                            q_slot = qe % L::kQRing;
+                            if (!(ok = mbar_wait(bar(L::kBarQFull + q_slot), (qe / L::kQRing) & 1, abort_flag))) return false;
+                            ++qe;
+                            have_q = true;
+                        }
+                        for (int t = 0; t < 2; ++t) {
+                            const int b = 2 * t + int(se & 1);
+                            if (se >= 2 && !(ok = mbar_wait(bar(L::kBarSFree + b), ((se >> 1) - 1) & 1, abort_flag))) return false;
+                            tc_fence_after();
+                            const uint64_t k = k_desc + uint32_t(k_slot[t]) * (L::kTileBytes >> 4), q = q_desc + uint32_t(q_slot) * (L::kTileBytes >> 4);
+                            const uint32_t d = tmem_base + uint32_t(b) * 128, idesc = few ? kIdescFew : kIdesc;
+#pragma unroll
+                            for (int i = 0; i < kKSteps; ++i) {
+                                const uint32_t off = ((i / 4) * L::kHalfBytes + (i % 4) * 32) >> 4;
+                                if (i == 0) mma_ss<false>(d, k + off, q + off, idesc);
+                                else mma_ss<true>(d, k + off, q + off, idesc);
+                            }
+                            tc_commit(bar(L::kBarS + b));
+                            if (r + 1 == r1) tc_commit(bar(L::kBarKEmpty + k_slot[t]));
+                        }
+                        if (tiles > 1) tc_commit(bar(L::kBarQEmpty + q_slot));
+                    }
+                    return true;
+                });
+                if (ok && tiles == 1 && have_q) tc_commit(bar(L::kBarQEmpty + q_slot));
+            }
+        }
+    } else {
+        const int t = warp >> 2, key = (warp & 3) * 32 + lane;       // key tile of the pair, key inside it
+        const uint32_t lane_addr = uint32_t((warp & 3) * 32) << 16;
+        uint32_t se = 0, le = 0;
+        while (ok && walk.next(pc)) {
+            const WeightsGroup &g = pc.g;
+            const int tiles = row_tiles(g.n, a.group), count = tiles - g.first_tile;
+            const bool few = g.n * a.group <= kFewRows;
+            bool have_q = false;
+            int ls = 0;
+            each_pair(pc, count, [&](int pair, int r0, int r1) {
+                const int pos = (g.first_pair + pair) * kPairKeys + t * kTileKeys + key;
+                const int first_row = max(0, min(pos - g.pos0, g.n)) * a.group, rows = g.n * a.group;   // below 2^28
+                float total = 0.f;
+                for (int r = r0; r < r1; ++r, ++se) {
+                    if (tiles > 1 || !have_q) {
+                        ls = le % L::kLseRing;
+                        if (!(ok = warp_wait(bar(L::kBarLFull + ls), (le / L::kLseRing) & 1))) return false;
+                        ++le;
+                        have_q = true;
+                    }
+                    const int b = 2 * t + int(se & 1);
+                    if (!(ok = warp_wait(bar(L::kBarS + b), (se >> 1) & 1))) return false;
+                    tc_fence_after();
+                    const uint32_t s_addr = tmem_base + lane_addr + uint32_t(b) * 128;
+                    const float4 *off = reinterpret_cast<const float4 *>(smem + L::kLseOff + ls * 512);
+                    const int row0 = (g.first_tile + r) * kRowTile;
+                    const int lo = first_row - row0, hi = rows - row0;   // rows [lo, hi) give weight
+                    const bool whole = __all_sync(0xffffffffu, lo <= 0 && hi >= 128);
+                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                    auto add = [&](const uint32_t *s, int c, int n, bool masked, bool exact) {
+#pragma unroll
+                        for (int i = 0; i < n; i += 4) {
+                            const float4 o = off[(c + i) / 4];
+                            const float ov[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                float x = fmaf(__uint_as_float(s[i + k]), a.scale_log2, ov[k]);
+                                if (masked && (c + i + k < lo || c + i + k >= hi)) x = -INFINITY;
+                                sum[k] += !exact && k == 3 ? poly_exp2_fine<5>(x) : fast_exp2(x);
+                            }
+                        }
+                    };
+                    if (few) {
+                        uint32_t s[16];
+                        tmem_ld16(s_addr, s);
+                        tmem_wait_ld();
+                        add(s, 0, 16, true, true);
+                    } else {
+                        uint32_t s[2][32];
+                        tmem_ld32(s_addr, s[0]);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            if (c < 3) tmem_ld32(s_addr + (c + 1) * 32, s[(c + 1) & 1]);
+                            if (whole) add(s[c & 1], c * 32, 32, false, false);
+                            else add(s[c & 1], c * 32, 32, true, true);
+                            tmem_wait_ld();
+                        }
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) {
+                        mbar_arrive(bar(L::kBarSFree + b));
+                        if (tiles > 1) mbar_arrive(bar(L::kBarLEmpty + ls));
+                    }
+                    total += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                }
+                const bool cut = r0 > 0 || r1 < count;
+                if (cut) w.partial[size_t(2 * blockIdx.x + (r0 > 0 ? 0 : 1)) * kPairKeys + t * kTileKeys + key] = total;
+                else finish(w, g, pc.head, pos, total);
+                return true;
+            });
+            if (ok && tiles == 1 && have_q && lane == 0) mbar_arrive(bar(L::kBarLEmpty + ls));
+        }
+        if (!ok) *abort_flag = 1;
+    }
+
+    // ---------------------------------------------------------------- teardown
+    tc_fence_before();
+    __syncthreads();
+    if (*abort_flag) {
+        if (threadIdx.x == 0) raise(a.status, PSA_ERR_TIMEOUT);
+        // let copies that were already issued land before the block's shared memory is released
+        if (warp == kProducerWarp && lane == 0) {
+            const unsigned long long t0 = global_timer_ns();
+            while (global_timer_ns() - t0 < 2000000ull) { }
+        }
+        if (warp == kMmaWarp && elect_one()) {   // products still queued
+            tc_commit(bar(L::kBarDrain));
+            const unsigned long long t0 = global_timer_ns();
+            while (!mbar_try_wait(bar(L::kBarDrain), 0) && global_timer_ns() - t0 < 2000000ull) { }
+        }
+        __syncthreads();
+    }
+    if (warp == kMmaWarp) {
+        tc_fence_after();
+        tmem_dealloc(tmem_base, 512);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------------- merge
+// Block `cut`: the pair that the end of share `cut` falls into, if that is the first cut inside it; a thread per key.
+__global__ void __launch_bounds__(kPairKeys)
+weights_merge_kernel(const WeightsArgs w)
+{
+    grid_wait();
+    const ChunkHeader h = *w.c.header;
+    const int cut = blockIdx.x;
+    if (cut + 1 >= h.blocks || h.groups == 0) return;
+    const long long total = h.per_head * w.c.num_kv_heads;
+    const long long x = share_begin(total, cut + 1, h.blocks);
+    int head, gi;
+    locate(w.groups, h, x, threadIdx.x & 31, &head, &gi);
+    if (head >= w.c.num_kv_heads) return;
+    const WeightsGroup g = w.groups[gi];
+    const long long base = head * h.per_head + g.cum;
+    const int count = row_tiles(g.n, w.c.group) - g.first_tile;
+    const Place at = place_of(g, w.c.group, x - base);
+    if (at.pair >= g.pairs || at.rows <= 0 || at.rows >= count) return;                 // nothing is cut here
+    if (cut > 0) {
+        const Place before = place_of(g, w.c.group, share_begin(total, cut, h.blocks) - base);
+        if (before.pair == at.pair && before.rows > 0) return;                          // an earlier cut's pair
+    }
+    float sum = 0.f;
+    for (int b = cut; b < h.blocks; ++b) {
+        const Place from = place_of(g, w.c.group, share_begin(total, b, h.blocks) - base), to = place_of(g, w.c.group, share_begin(total, b + 1, h.blocks) - base);
+        const int r0 = from.pair == at.pair ? from.rows : 0, r1 = to.pair == at.pair ? to.rows : count;
+        if (r0 < r1) sum += w.partial[size_t(2 * b + (r0 > 0 ? 0 : 1)) * kPairKeys + threadIdx.x];
+        if (r1 >= count) break;
+    }
+    finish(w, g, head, (g.first_pair + at.pair) * kPairKeys + int(threadIdx.x), sum);
+}
+
+template <int D>
+cudaError_t launch(const WeightsArgs &w, const CUtensorMap *maps, cudaStream_t st)
+{
+    static PerDeviceOnce once;
+    if (const int rc = once.ensure([] { return int(cudaFuncSetAttribute(weights_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, WeightsSmem<D>::kTotal)); }))
+        return cudaError_t(rc);
+    weights_schedule_kernel<<<1, kScheduleThreads, 0, st>>>(w);
+    cudaError_t e = cudaGetLastError();
+    if (e == cudaSuccess) e = launch_dependent(weights_kernel<D>, dim3(w.c.blocks), 320, WeightsSmem<D>::kTotal, st, maps[0], maps[1], maps[2], w);
+    if (e == cudaSuccess && w.c.blocks > 1) e = launch_dependent(weights_merge_kernel, dim3(w.c.blocks - 1), kPairKeys, 0, st, w);
+    return e;
+}
+
+bool misaligned(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n != 0; }
+
+size_t layout(WeightsArgs &w, void *scratch)
+{
+    ChunkArgs &a = w.c;
+    a.max_groups = int(a.num_tokens / kPairKeys + 3 * int64_t(a.num_samples));
+    size_t off = 0;
+    auto take = [&](size_t bytes) { const size_t at = off; off = (off + bytes + 255) / 256 * 256; return static_cast<unsigned char *>(scratch) + at; };
+    a.header = reinterpret_cast<ChunkHeader *>(take(sizeof(ChunkHeader)));
+    w.groups = reinterpret_cast<WeightsGroup *>(take(sizeof(WeightsGroup) * size_t(a.max_groups)));
+    w.partial = reinterpret_cast<float *>(take(4 * size_t(2 * a.blocks) * kPairKeys));
+    return off;
+}
+
+}  // namespace
+}  // namespace psa
+
+extern "C" size_t psa_accumulate_weights_scratch_bytes(int64_t num_tokens, int32_t num_samples)
+{
+    if (num_tokens < 0 || num_samples < 0 || num_tokens > (1 << 24) || num_samples > (1 << 20)) return 0;
+    psa::WeightsArgs w{};
+    w.c.num_tokens = num_tokens; w.c.num_samples = num_samples; w.c.blocks = psa::kMostBlocks;
+    return psa::layout(w, nullptr);
+}
+
+extern "C" psa_status_t psa_accumulate_weights(const void *q, const int64_t q_strides[2], const int32_t *q_indptr, int64_t num_tokens, int32_t num_samples,
+                                               int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, float sm_scale, const float *lse,
+                                               const void *k_pool, const int64_t pool_strides[3], int64_t num_pool_pages, const int32_t *page_indptr,
+                                               const int32_t *page_indices, int64_t num_entries, const int32_t *kv_lens, const float *weights,
+                                               float *weights_out, int32_t *status, void *scratch, size_t scratch_bytes, void *cuda_stream)
+{
+    using namespace psa;
+    WeightsArgs w{};
+    ChunkArgs &a = w.c;
+    a.num_tokens = num_tokens; a.num_samples = num_samples; a.num_q_heads = num_q_heads; a.num_kv_heads = num_kv_heads;
+    a.group = num_kv_heads > 0 ? num_q_heads / num_kv_heads : 0;
+    a.num_pool_pages = int32_t(std::min<int64_t>(num_pool_pages, kMostChunkPages + 1)); a.num_entries = num_entries;
+    a.q_indptr = q_indptr; a.kv_lens = kv_lens; a.page_indptr = page_indptr; a.page_indices = page_indices;
+    a.status = status;
+    a.scale_log2 = sm_scale * kLog2e;
+    w.lse = lse; w.weights = weights; w.weights_out = weights_out;
+    psa_status_t rc = chunk_check(a, q, q_strides, k_pool, pool_strides, head_dim);
+    if (rc != PSA_OK) return rc;
+    if (!(sm_scale > 0.f) || sm_scale > 1e30f) return set_last_error(PSA_ERR_INVALID_ARG, "sm_scale must be positive and finite");
+    if (num_tokens == 0 || num_samples == 0) return PSA_OK;
+    if (!lse || !weights || !weights_out) return set_last_error(PSA_ERR_INVALID_ARG, "null lse or weights");
+    if (misaligned(lse, 4) || misaligned(weights, 4) || misaligned(weights_out, 4)) return set_last_error(PSA_ERR_INVALID_ARG, "lse and weights must be 4-byte aligned");
+    if (num_pool_pages == 0) return set_last_error(PSA_ERR_INVALID_ARG, "the pool has no pages");
+    if (!scratch || misaligned(scratch, 256) || scratch_bytes < psa_accumulate_weights_scratch_bytes(num_tokens, num_samples))
+        return set_last_error(PSA_ERR_WORKSPACE, "scratch must be 256-byte aligned and hold psa_accumulate_weights_scratch_bytes");
+    a.blocks = std::min(multiprocessors(), kMostBlocks);
+    if (a.blocks <= 0) return set_last_error(PSA_ERR_CUDA, "no CUDA device");
+    layout(w, scratch);
+    CUtensorMap maps[3];
+    rc = chunk_q_map(a, q, q_strides, head_dim, kRowTile, &maps[0]);
+    if (rc == PSA_OK) rc = chunk_q_map(a, q, q_strides, head_dim, kFewRows, &maps[1]);
+    if (rc == PSA_OK) rc = chunk_pool_map(a, k_pool, pool_strides, head_dim, &maps[2]);
+    if (rc != PSA_OK) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const cudaError_t e = head_dim == 128 ? launch<128>(w, maps, st) : launch<64>(w, maps, st);
+    if (e != cudaSuccess) return set_last_error(PSA_ERR_CUDA, std::string("cached weights launch: ") + cudaGetErrorString(e));
+    return PSA_OK;
+}
