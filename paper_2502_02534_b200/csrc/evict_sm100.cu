@@ -4,9 +4,9 @@
 // whatever they weigh, of the others the heaviest up to the budget (equal weights: the older page stays).  K and V do not move: the list
 // closes up in order, and the ids that leave go onto the stack of free pages.
 //
-// Two launches.  evict_plan_kernel (one block) reads lengths and budgets, checks them and runs the sum of pages that go, so that every
-// sample knows its place on the stack (and lengths and count may be updated in place).  evict_kernel has a block per sample: weights are
-// read once (all of the bytes that matter), as ordered 32-bit keys in shared memory; the border between what stays and goes is found by
+// A running sum of the pages that go gives every sample its place on the stack.  Where lengths and count are not updated in place each
+// block runs it for itself, from all samples' lengths and budgets; otherwise, and for many samples, evict_plan_kernel (one block) does so
+// before.  evict_kernel has a block per sample: weights are read once (all of the bytes that matter), as ordered 32-bit keys in shared memory; the border between what stays and goes is found by
 // four histograms of 8 bits; one scan closes up the list.
 #include <cuda_runtime.h>
 
@@ -20,6 +20,7 @@ namespace psa {
 namespace {
 
 constexpr int kPlanThreads = 1024, kThreads = 512, kWarps = kThreads / 32;
+constexpr int kAlone = 1024;        // samples up to which every block sums up the others for itself
 constexpr int kSharedKeys = 8192;   // longer lists keep their keys in the scratch memory
 
 struct EvictSample {
@@ -58,17 +59,18 @@ __device__ __forceinline__ EvictSample sample_of(const EvictArgs &a, int s)
     return e;
 }
 
-__global__ void __launch_bounds__(kPlanThreads)
-evict_plan_kernel(EvictArgs a)
+// What every sample does, and whether anything leaves at all, by one block: of all samples (kAll; entry s goes to plan[s], outputs are
+// written), or of sample `only` as every block of the other form needs it.
+template <bool kAll, int kBlock>
+__device__ __forceinline__ EvictSample plan(const EvictArgs &a, int only, int *height_out)
 {
-    grid_release();
-    __shared__ long long part[kPlanThreads / 32];
-    __shared__ int refused;
+    __shared__ long long part[kBlock / 32];
+    __shared__ EvictSample chosen;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int height = *a.free_count;
+    *height_out = height;
     long long carry = 0;
-    if (threadIdx.x == 0) refused = height < 0 || height > a.free_capacity;
-    for (int s0 = 0; s0 < a.num_samples; s0 += kPlanThreads) {
+    for (int s0 = 0; s0 < a.num_samples; s0 += kBlock) {
         const int s = s0 + int(threadIdx.x);
         EvictSample e{};
         if (s < a.num_samples) e = sample_of(a, s);
@@ -82,29 +84,49 @@ evict_plan_kernel(EvictArgs a)
         if (lane == 31) part[warp] = x;
         __syncthreads();
         long long before = carry + x - go;
-        for (int k = 0; k < kPlanThreads / 32; ++k) {
+#pragma unroll
+        for (int k = 0; k < kBlock / 32; ++k) {
             if (k < warp) before += part[k];
             carry += part[k];
         }
         __syncthreads();
         e.to = int(min(before, 0x7fffffffll));
-        if (s < a.num_samples) a.plan[s] = e;
+        if (kAll) {
+            if (s < a.num_samples) a.plan[s] = e;
+        } else if (s == only) {
+            chosen = e;
+        }
     }
-    __syncthreads();
-    if (threadIdx.x == 0 && carry > a.free_capacity - height) refused = 1;   // no room on the stack for all of them: nothing goes
-    __syncthreads();
-    const bool none = refused != 0;
-    for (int s = threadIdx.x; s < a.num_samples; s += kPlanThreads) {   // the thread's own entries
-        EvictSample &e = a.plan[s];
-        if (none) e.budget = e.pages;
-        const int len = a.kv_lens[s];
-        if (a.lens_out) a.lens_out[s] = len - (e.pages - e.budget) * kPageSize;
+    // a height that cannot be, or no room on the stack for all of them: nothing goes
+    const bool none = height < 0 || height > a.free_capacity || carry > a.free_capacity - height;
+    if (kAll) {
+        for (int s = threadIdx.x; s < a.num_samples; s += kBlock) {   // the thread's own entries
+            EvictSample &e = a.plan[s];
+            if (none) e.budget = e.pages;
+            const int len = a.kv_lens[s];
+            if (a.lens_out) a.lens_out[s] = len - (e.pages - e.budget) * kPageSize;
+        }
+    } else {
+        __syncthreads();
     }
-    if (threadIdx.x == 0) {
+    if (threadIdx.x == 0 && (kAll || only == 0)) {
         if (none) raise(a.status, PSA_ERR_BOUNDS);
-        *a.height = height;
         *a.free_count_out = none ? height : int(height + carry);
     }
+    if (kAll) return {};
+    EvictSample e = chosen;
+    if (none) e.budget = e.pages;
+    if (threadIdx.x == 0 && a.lens_out) a.lens_out[only] = a.kv_lens[only] - (e.pages - e.budget) * kPageSize;
+    return e;
+}
+
+__global__ void __launch_bounds__(kPlanThreads)
+evict_plan_kernel(EvictArgs a)
+{
+    grid_release();
+    int height;
+    plan<true, kPlanThreads>(a, 0, &height);
+    if (threadIdx.x == 0) *a.height = height;
 }
 
 // larger weight, larger key; NaN never gets here
@@ -114,6 +136,7 @@ __device__ __forceinline__ uint32_t ordered(float x)
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
+template <bool kPlanned>
 __global__ void __launch_bounds__(kThreads)
 evict_kernel(EvictArgs a)
 {
@@ -121,7 +144,7 @@ evict_kernel(EvictArgs a)
     __shared__ uint32_t bins[256];
     __shared__ uint32_t part[kWarps];
     __shared__ uint32_t found[2];
-    grid_wait();
+    if (kPlanned) grid_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     // entries that belong to no list
     if (a.indices_out != a.page_indices) {
@@ -131,7 +154,14 @@ evict_kernel(EvictArgs a)
         for (long long i = end + at; i < a.num_entries; i += step) a.indices_out[i] = a.page_indices[i];
     }
     if (int(blockIdx.x) >= a.num_samples) return;   // no samples: all there is to do was above
-    const EvictSample e = a.plan[blockIdx.x];
+    int height;
+    EvictSample e;
+    if (kPlanned) {
+        e = a.plan[blockIdx.x];
+        height = *a.height;
+    } else {
+        e = plan<false, kThreads>(a, int(blockIdx.x), &height);
+    }
     const int32_t *list = a.page_indices + e.list0;
     int32_t *out = a.indices_out + e.list0;
     const int go = e.pages - e.budget;
@@ -142,12 +172,13 @@ evict_kernel(EvictArgs a)
     }
     const int candidates = e.pages - e.recent, stay = e.budget - e.recent;   // of the candidates
     uint32_t *keys = candidates <= kSharedKeys ? shared_keys : a.keys + e.list0;
+    const int newest = int(threadIdx.x) < e.recent ? list[candidates + threadIdx.x] : 0;
 
     // ---- weights: `abreast` lanes a page
     const int vectors = a.cells / 4;
     const int abreast = vectors >= 32 ? 32 : vectors >= 16 ? 16 : vectors >= 8 ? 8 : 4;
     const int sub = lane / abreast, mine = lane % abreast, at_once = 32 / abreast;
-    constexpr int kAhead = 4;
+    constexpr int kAhead = 8;
     for (int c0 = warp * at_once * kAhead; c0 < candidates; c0 += kWarps * at_once * kAhead) {
         float top[kAhead];
         int page[kAhead];
@@ -181,7 +212,26 @@ evict_kernel(EvictArgs a)
 
     // ---- the key of the lightest candidate that stays, from its highest byte down
     uint32_t prefix = 0, wanted = uint32_t(stay);
-    if (stay > 0) {
+    __syncthreads();
+    if (stay > 0 && candidates <= kThreads) {
+        // a key a thread: bit by bit, counting those at least that large, until as many as may stay are
+        const uint32_t mine = int(threadIdx.x) < candidates ? keys[threadIdx.x] : 0;
+        const bool is = int(threadIdx.x) < candidates;
+        int above = 0;          // larger than every key that has `prefix`'s bits so far
+        for (int bit = 31; bit >= 0; --bit) {
+            const uint32_t test = prefix | 1u << bit;
+            const int n = __syncthreads_count(is && mine >= test);
+            if (n >= stay) prefix = test;
+            else above = n;
+            if (n == stay) break;
+        }
+        // a count that hit: everything at or above `prefix` stays
+        wanted = uint32_t(stay - above);
+        if (__syncthreads_count(is && mine >= prefix) == stay) {
+            prefix -= 1;        // not 0: some bit was set
+            wanted = 0;
+        }
+    } else if (stay > 0) {
         for (int shift = 24; shift >= 0; shift -= 8) {
             for (int i = threadIdx.x; i < 256; i += kThreads) bins[i] = 0;
             __syncthreads();
@@ -216,13 +266,11 @@ evict_kernel(EvictArgs a)
             prefix = found[0];
             wanted = found[1];
         }
-    } else {
-        __syncthreads();
     }
     // heavier than `prefix` stays, and the first `wanted` of those that weigh just that
 
     // ---- the list closes up
-    int32_t *stack = a.free_pages + *a.height + e.to;
+    int32_t *stack = a.free_pages + height + e.to;
     int stayed = 0, tied = 0;   // among the candidates before this round
     for (int c0 = 0; c0 < candidates; c0 += kThreads) {
         const int c = c0 + int(threadIdx.x);
@@ -255,7 +303,7 @@ evict_kernel(EvictArgs a)
     // the newest pages follow; then nothing, up to what was held
     for (int c0 = 0; c0 < e.recent; c0 += kThreads) {
         const int c = c0 + int(threadIdx.x);
-        const int page = c < e.recent ? list[candidates + c] : 0;
+        const int page = c0 == 0 ? newest : c < e.recent ? list[candidates + c] : 0;
         __syncthreads();
         if (c < e.recent) out[stay + c] = page;
     }
@@ -314,9 +362,16 @@ extern "C" psa_status_t psa_evict_pages(const float *weights, int64_t num_pool_p
     a.num_samples = num_samples; a.recent = recent; a.num_pool_pages = int32_t(num_pool_pages); a.cells = num_kv_heads * kPageSize;
     layout(a, scratch);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    evict_plan_kernel<<<1, kPlanThreads, 0, st>>>(a);
-    cudaError_t e = cudaGetLastError();
-    if (e == cudaSuccess) e = launch_dependent(evict_kernel, dim3(std::max(1, num_samples)), kThreads, 0, st, a);
+    cudaError_t e;
+    // one launch where no block writes what another one reads, and reading all samples' entries in every block is little
+    if (num_samples > 0 && num_samples <= kAlone && lens_out != kv_lens && free_count_out != free_count) {
+        evict_kernel<false><<<num_samples, kThreads, 0, st>>>(a);
+        e = cudaGetLastError();
+    } else {
+        evict_plan_kernel<<<1, kPlanThreads, 0, st>>>(a);
+        e = cudaGetLastError();
+        if (e == cudaSuccess) e = launch_dependent(evict_kernel<true>, dim3(std::max(1, num_samples)), kThreads, 0, st, a);
+    }
     if (e != cudaSuccess) return set_last_error(PSA_ERR_CUDA, std::string("eviction launch: ") + cudaGetErrorString(e));
     return PSA_OK;
 }

@@ -6,10 +6,13 @@
 // maximum moves, and they are joined at the end.  A row is a block, or a cluster of 2 to 8 blocks where there are few rows; the blocks'
 // results meet in the first one's shared memory.
 //
-// The likeliest tokens come out of the same pass.  A (logit, token) pair is ordered by a 64-bit key, equal logits by the lower token, so
-// nothing depends on who comes first.  From the threads' maxima over the first tile every warp takes its r-th largest, r = ceil(k / warps):
-// at least k logits are as large as the smallest of these, which is the first border.  What lies above the border is appended to a list;
-// a list that is full is cut to its k largest, whose least one is the new border, and the tile is gone through again.
+// The likeliest tokens cost the pass next to nothing.  Every warp gives the four largest of its threads' maxima, and the k-th largest of those
+// is the border: k logits reach it, so the k largest lie with the few threads whose maximum does.  Those find in
+// shared memory which of their tiles do (16 bits of each tile's maximum, rounded down); these are read once more, a vector a thread, and what
+// reaches the border is listed.
+// A (logit, token) pair is ordered by a 64-bit key, equal logits by the lower token, so nothing depends on who comes first.  A list that
+// is too short (many equal logits) gives a higher border, its own k-th largest, and is made again.  256 rows x 131072 bf16, k = 20:
+// listing inside the pass, with a border kept by the block 64 us, by each warp 164 us; all tiles read again 31 us; this way @@ us.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -28,13 +31,17 @@ constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kPer = 16;                          // logits of a thread in a tile
 constexpr int kTile = kThreads * kPer;
 constexpr int kList = 2048;
+constexpr int kCells = 512;
+constexpr int kMarks = 24;                        // tile maxima kept of a thread: longer rows keep those of runs of tiles
+constexpr int kGiven = 4;                         // maxima that a warp gives
 constexpr int kMostTop = 64, kMostCluster = 8;
+static_assert(kGiven * kWarps == 64 && kMostTop <= kGiven * kWarps, "the border is the kMostTop-th of them at most; two a lane");
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct LogprobArgs {
     const void *logits;
     int64_t stride, top_stride;
-    int32_t vocab, top, segment;                  // segment: logits of a block, a multiple of 8
+    int32_t vocab, top, segment, run_tiles;       // segment: logits of a block, a multiple of 8; run_tiles: tiles that share a mark
     const int32_t *tokens;
     const float *temperature;
     float *logprobs, *entropy, *top_logprobs;
@@ -49,25 +56,44 @@ __device__ __forceinline__ uint32_t ordered(float x)
 __device__ __forceinline__ float from_ordered(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 __device__ __forceinline__ unsigned long long key_of(float x, int token) { return (unsigned long long)ordered(x + 0.f) << 32 | uint32_t(~token); }
 
-// running (m, l, s = sum 2^d d), d in log2 units against m; m is -inf until something was seen
+// Running sums: l = sum 2^d, s = sum 2^d d, exponents d in log2 units against m, a logit at most 2^8 below the largest (-inf: nothing yet).
 struct Sums { float m, l, s; };
-__device__ __forceinline__ Sums joined(const Sums &a, const Sums &b, float c)
+// ... against another reference, above m or equal
+__device__ __forceinline__ Sums moved(const Sums &a, float m, float c)
 {
-    const float m = fmaxf(a.m, b.m);
-    if (m == -INFINITY) return {m, a.l + b.l, a.s + b.s};
-    Sums r{m, 0.f, 0.f};
-    const Sums both[2] = {a, b};
+    if (a.m == -INFINITY) return {m, a.l, a.s};    // nothing, or NaN alone
+    const float d = fmaxf((a.m - m) * c, -200.f);
+    float w;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(w) : "f"(d));
+    return {m, a.l * w, w * fmaf(a.l, d, a.s)};
+}
+// of the lanes below `lanes` of a whole warp, to every lane
+template <int kLanes>
+__device__ __forceinline__ Sums joined(Sums a, float c)
+{
+    const uint32_t top = __reduce_max_sync(0xffffffffu, ordered(a.m));
+    a = moved(a, from_ordered(top), c);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        if (both[i].m == -INFINITY) {             // nothing, or NaN alone
-            r.l += both[i].l;
-            r.s += both[i].s;
-            continue;
-        }
-        const float d = (both[i].m - m) * c, w = exp2f(d);
-        r.l += both[i].l * w;
-        r.s += w * (both[i].s + both[i].l * (d < -200.f ? 0.f : d));
+    for (int d = kLanes / 2; d; d >>= 1) {
+        a.l += __shfl_xor_sync(0xffffffffu, a.l, d);
+        a.s += __shfl_xor_sync(0xffffffffu, a.s, d);
     }
+    return a;
+}
+
+// two fp32 operations in one instruction
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 r;
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\tfma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    float2 r;
+    asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return r;
 }
 
@@ -75,7 +101,29 @@ template <class T>
 struct Vec;
 template <>
 struct Vec<__nv_bfloat16> {
+    static __device__ __forceinline__ void one(const uint4 &w, float (&x)[8])
+    {
+        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            x[2 * k] = __uint_as_float(u[k] << 16);
+            x[2 * k + 1] = __uint_as_float(u[k] & 0xffff0000u);
+        }
+    }
     static constexpr int kLoads = 2;              // of 16 bytes, for kPer logits
+    static constexpr int kAhead = 2;              // tiles on their way
+    // the largest of a thread's logits, in packed bf16 (NaN does not count)
+    static __device__ __forceinline__ float most(const uint4 (&w)[2], const float (&)[kPer])
+    {
+        const uint32_t u[8] = {w[0].x, w[0].y, w[0].z, w[0].w, w[1].x, w[1].y, w[1].z, w[1].w};
+        uint32_t m[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm("max.bf16x2 %0, %1, %2;" : "=r"(m[i]) : "r"(u[i]), "r"(u[i + 4]));
+        asm("max.bf16x2 %0, %0, %1;" : "+r"(m[0]) : "r"(m[1]));
+        asm("max.bf16x2 %0, %0, %1;" : "+r"(m[2]) : "r"(m[3]));
+        asm("max.bf16x2 %0, %0, %1;" : "+r"(m[0]) : "r"(m[2]));
+        return fmaxf(__uint_as_float(m[0] << 16), __uint_as_float(m[0] & 0xffff0000u));
+    }
     static __device__ __forceinline__ void get(const uint4 (&w)[2], float (&x)[kPer])
     {
 #pragma unroll
@@ -91,7 +139,18 @@ struct Vec<__nv_bfloat16> {
 };
 template <>
 struct Vec<float> {
-    static constexpr int kLoads = 4;
+    static __device__ __forceinline__ void one(const uint4 &w, float (&x)[4])
+    {
+        x[0] = __uint_as_float(w.x); x[1] = __uint_as_float(w.y); x[2] = __uint_as_float(w.z); x[3] = __uint_as_float(w.w);
+    }
+    static constexpr int kLoads = 4, kAhead = 1;
+    static __device__ __forceinline__ float most(const uint4 (&)[4], const float (&x)[kPer])
+    {
+        float top[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+        for (int i = 4; i < kPer; ++i) top[i & 3] = fmaxf(top[i & 3], x[i]);
+        return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+    }
     static __device__ __forceinline__ void get(const uint4 (&w)[4], float (&x)[kPer])
     {
 #pragma unroll
@@ -105,23 +164,26 @@ struct Vec<float> {
 struct Shared {
     unsigned long long list[kList], best[kMostTop], gathered[kMostCluster * kMostTop];
     Sums warp_sums[kWarps], block, all[kMostCluster];
-    uint32_t border[kWarps];
-    int count, listed;
+    uint32_t given[kGiven * kWarps], reached;
+    int count, cells_found, listed[kMostCluster];
+    uint16_t cells[kCells];
+    uint16_t marks[kMarks][kThreads];
 };
 
-// The k-th largest of list[0 .. n), n > k > 0: bit by bit, counting what is at least that large.
-__device__ unsigned long long kth(const unsigned long long *list, int n, int k)
+// The k-th largest of list[0 .. n), n >= k > 0, to every thread: bit by bit, counting what is at least that large.
+__device__ unsigned long long kth(const Shared &sh, int n, int k)
 {
+    unsigned long long mine[kList / kThreads];
+#pragma unroll
+    for (int i = 0; i < kList / kThreads; ++i) mine[i] = i * kThreads + int(threadIdx.x) < n ? sh.list[i * kThreads + threadIdx.x] : 0;
     unsigned long long at = 0;
     for (int bit = 63; bit >= 0; --bit) {
         const unsigned long long test = at | 1ull << bit;
-        int mine = 0;
-        for (int i = threadIdx.x; i < n; i += kThreads) mine += list[i] >= test;
-        // a thread has at most kList / kThreads of them: sum by counting each
         int total = 0;
 #pragma unroll
-        for (int i = 1; i <= kList / kThreads; ++i) total += __syncthreads_count(mine >= i);
+        for (int i = 0; i < kList / kThreads; ++i) total += __syncthreads_count(mine[i] >= test);
         if (total >= k) at = test;
+        if (total == k) break;
     }
     return at;
 }
@@ -132,6 +194,7 @@ __device__ int sorted_best(const unsigned long long *list, int n, int k, unsigne
     for (int i = threadIdx.x; i < n; i += kThreads) {
         const unsigned long long mine = list[i];
         int rank = 0;
+#pragma unroll 4
         for (int j = 0; j < n; ++j) rank += list[j] > mine;
         if (rank < k) to[rank] = mine;
     }
@@ -153,10 +216,21 @@ logprobs_kernel(const LogprobArgs a)
     float t = a.temperature ? a.temperature[row] : 1.f;
     if (!(t > 0.f && t < INFINITY)) t = 1.f;
     const float inv_t = 1.f / t, c = inv_t * kLog2e;
+    float asked = -INFINITY;                       // the given token's logit; its way is long, so it starts here
+    if (part == 0 && threadIdx.x == 0 && a.logprobs) {
+        const int token = a.tokens[row];
+        if (token >= 0 && token < a.vocab) asked = float(x_row[token]);
+    }
 
     constexpr int kLoads = Vec<T>::kLoads, kVec = 16 / int(sizeof(T));
+    if (blocks > 1) cluster.barrier_arrive();      // nobody writes to a block that has not begun
     // load i of a thread in the tile at v: kVec logits from v + (i * kThreads + thread) * kVec on
     auto load = [&](int v, uint4 (&w)[kLoads]) {
+        if (v + kTile <= v1) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) w[i] = __ldcs(reinterpret_cast<const uint4 *>(x_row + v + (i * kThreads + int(threadIdx.x)) * kVec));
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int at = v + (i * kThreads + int(threadIdx.x)) * kVec;
@@ -170,163 +244,211 @@ logprobs_kernel(const LogprobArgs a)
             }
         }
     };
-    if (threadIdx.x == 0) sh.count = 0;
-
     Sums sum{-INFINITY, 0.f, 0.f};
-    unsigned long long border = 0;                 // keys above it are listed
-    uint4 next[kLoads];
-    if (v0 < v1) load(v0, next);
-    for (int v = v0; v < v1; v += kTile) {
-        float x[kPer];
-        Vec<T>::get(next, x);
-        if (v + kTile < v1) load(v + kTile, next);
-        float top[4] = {x[0], x[1], x[2], x[3]};
+    float most = -INFINITY, limit = -INFINITY;     // the thread's largest logit; what the reference holds for
+    float run_top = -INFINITY;
+    int run = 0, marks = 0;
+    constexpr int kAhead = Vec<T>::kAhead;
+    uint4 w[kAhead][kLoads];
 #pragma unroll
-        for (int i = 4; i < kPer; ++i) top[i & 3] = fmaxf(top[i & 3], x[i]);
-        const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-        if (most > sum.m) {
-            if (sum.m != -INFINITY) {
-                const float d = (sum.m - most) * c, w = exp2f(d);
-                sum.s = w * (sum.s + sum.l * fmaxf(d, -200.f));
-                sum.l *= w;
+    for (int i = 0; i < kAhead; ++i)
+        if (v0 + i * kTile < v1) load(v0 + i * kTile, w[i]);
+    auto tile = [&](int v, uint4 (&now)[kLoads]) {
+        float x[kPer];
+        Vec<T>::get(now, x);
+        const float top_here = Vec<T>::most(now, x);
+        if (v + kAhead * kTile < v1) load(v + kAhead * kTile, now);
+        most = fmaxf(most, top_here);
+        if (a.top > 0) {
+            run_top = fmaxf(run_top, top_here);
+            if (++run == a.run_tiles) {
+                sh.marks[marks++][threadIdx.x] = uint16_t(ordered(run_top + 0.f) >> 16);
+                run = 0;
+                run_top = -INFINITY;
             }
-            sum.m = most;
+        }
+        // the reference moves when an exponent would pass 2^8; the sums do not mind being taken against a smaller one
+        if (top_here > limit) {
+            if (sum.m != -INFINITY) {
+                const float d = (sum.m - top_here) * c, r = exp2f(d);
+                sum.s = r * (sum.s + sum.l * fmaxf(d, -200.f));
+                sum.l *= r;
+            }
+            sum.m = top_here;
+            limit = top_here + 8.f / c;
         }
         const float off = sum.m == -INFINITY ? 0.f : -sum.m;
-        float l[2] = {0.f, 0.f}, s[2] = {0.f, 0.f};
+        float2 l = {0.f, 0.f}, s = {0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const float d = (x[i] + off) * c;
-            float e;
-            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(d));
-            l[i & 1] += e;
-            s[i & 1] = fmaf(e, fmaxf(d, -200.f), s[i & 1]);     // 0 x -inf; e is 0 there
+        for (int i = 0; i < kPer; i += 2) {
+            float2 d = add2(make_float2(x[i], x[i + 1]), make_float2(off, off)), e;      // exact where it matters: near the maximum
+            d = fma2(d, make_float2(c, c), make_float2(0.f, 0.f));
+            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.x) : "f"(d.x));
+            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.y) : "f"(d.y));
+            l = add2(l, e);
+            s = fma2(e, make_float2(fmaxf(d.x, -200.f), fmaxf(d.y, -200.f)), s);         // not 0 x -inf: e is 0 there
         }
-        sum.l += l[0] + l[1];
-        sum.s += s[0] + s[1];
-
-        if (a.top == 0) continue;
-        auto token = [&](int i) { return v + (i / kVec * kThreads + int(threadIdx.x)) * kVec + i % kVec; };
-        if (v == v0) {
-            // the first border, from the threads' maxima: below the smallest of the warps' r-th largest
-            const int full = min(kWarps, (min(v1 - v0, kThreads * kVec)) / (32 * kVec));    // warps all of whose threads have logits
-            uint32_t rth = 0;
-            if (full > 0) {
-                uint32_t mine = most == most ? ordered(most + 0.f) : 0u;
-                const int r = (a.top + full - 1) / full;
-                for (int i = 0; i < r && i < 32; ++i) {
-                    rth = __reduce_max_sync(0xffffffffu, mine);
-                    const unsigned has = __ballot_sync(0xffffffffu, mine == rth);
-                    if (lane == __ffs(has) - 1) mine = 0;
-                }
-                if (r > 32) rth = 0;
-            }
-            if (lane == 0) sh.border[warp] = rth;
-            __syncthreads();
-            uint32_t least = full > 0 ? 0xffffffffu : 0u;
-            for (int w = 0; w < full; ++w) least = min(least, sh.border[w]);
-            border = least == 0 ? 0 : ((unsigned long long)least << 32) - 1;    // keys of that value and above are listed
-        }
-        // what lies above the border; -inf only where its place alone can bring it among the first
-        int before = v == v0 ? 0 : sh.count;       // listed by earlier tiles
-        __syncthreads();
-        const unsigned long long first_border = border;
-        for (;;) {
-            // -inf is ordered as 0x007fffff: a border down there keeps nothing out
-            if (border < 0x00800000ull << 32 || most >= from_ordered(uint32_t(border >> 32))) {
-#pragma unroll
-                for (int i = 0; i < kPer; ++i) {
-                    const int id = token(i);
-                    const unsigned long long k = key_of(x[i], id);
-                    if (k > border && id < v1 && (x[i] > -INFINITY || (x[i] == -INFINITY && id < v0 + a.top))) {
-                        const int place = atomicAdd(&sh.count, 1);
-                        if (place < kList) sh.list[place] = k;
-                    }
-                }
-            }
-            __syncthreads();
-            if (sh.count <= kList) break;
-            // full: its k-th largest is the border of what can still count, for this tile again and for those to come
-            const unsigned long long least = kth(sh.list, kList, a.top);
-            unsigned long long mine[kList / kThreads];
-#pragma unroll
-            for (int i = 0; i < kList / kThreads; ++i) mine[i] = sh.list[i * kThreads + threadIdx.x];
-            __syncthreads();
-            if (threadIdx.x == 0) sh.count = 0;
-            __syncthreads();
-            // of what earlier tiles listed, the part that still counts; the tile's own is listed again
-#pragma unroll
-            for (int i = 0; i < kList / kThreads; ++i)
-                if (i * kThreads + int(threadIdx.x) < before && mine[i] >= least) sh.list[atomicAdd(&sh.count, 1)] = mine[i];
-            border = least - 1;
-            __syncthreads();
-            before = sh.count;
-            __syncthreads();
-        }
-        // as many as are wanted lie at or above the first border, at lower tokens than all to come: from here on only larger values count
-        if (v == v0 && border == first_border && border != 0) border += 1ull << 32;
+        sum.l += l.x + l.y;
+        sum.s += s.x + s.y;
+    };
+    for (int v = v0; v < v1; v += kAhead * kTile) {
+        tile(v, w[0]);
+        if constexpr (kAhead > 1)
+            if (v + kTile < v1) tile(v + kTile, w[kAhead - 1]);
     }
 
     // ---- the block's sums and best
-#pragma unroll
-    for (int d = 16; d; d >>= 1) {
-        const Sums o{__shfl_xor_sync(0xffffffffu, sum.m, d), __shfl_xor_sync(0xffffffffu, sum.l, d), __shfl_xor_sync(0xffffffffu, sum.s, d)};
-        sum = lane & d ? joined(o, sum, c) : joined(sum, o, c);
-    }
+    sum = joined<32>(sum, c);
     if (lane == 0) sh.warp_sums[warp] = sum;
-    __syncthreads();
-    int n = sh.count;
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < kWarps; ++w) sum = joined(sum, sh.warp_sums[w], c);
-        sh.block = sum;
-    }
+    if (threadIdx.x == 0) sh.count = sh.cells_found = 0;
+    const uint32_t top_key = ordered(most + 0.f);  // never NaN
     if (a.top > 0) {
-        if (n > kThreads) {
-            const unsigned long long least = kth(sh.list, n, a.top);
-            unsigned long long mine[kList / kThreads];
+        if (run > 0) sh.marks[marks++][threadIdx.x] = uint16_t(ordered(run_top + 0.f) >> 16);
+        uint32_t left = top_key;
 #pragma unroll
-            for (int i = 0; i < kList / kThreads; ++i) mine[i] = i * kThreads + int(threadIdx.x) < n ? sh.list[i * kThreads + threadIdx.x] : 0;
+        for (int r = 0; r < kGiven; ++r) {
+            const uint32_t one = __reduce_max_sync(0xffffffffu, left);
+            if (lane == __ffs(__ballot_sync(0xffffffffu, left == one)) - 1) left = 0;
+            if (lane == 0) sh.given[r * kWarps + warp] = one;
+        }
+    }
+    __syncthreads();
+    if (warp == kWarps - 1) {
+        sum = joined<kWarps>(lane < kWarps ? sh.warp_sums[lane] : Sums{-INFINITY, 0.f, 0.f}, c);
+        if (lane == 0) sh.block = sum;
+    }
+    int n = 0;
+    if (a.top > 0) {
+        // the a.top-th largest of what the warps gave
+        if (threadIdx.x < kGiven * kWarps) {
+            const uint32_t mine = sh.given[threadIdx.x];
+            int larger = 0;
+#pragma unroll
+            for (int i = 0; i < kGiven * kWarps; ++i) {
+                const uint32_t o = sh.given[i];
+                larger += o > mine || (o == mine && i < int(threadIdx.x));
+            }
+            if (larger == a.top - 1) sh.reached = mine;
+        }
+        __syncthreads();
+        const uint32_t reached = sh.reached;
+        // which tiles reach it: (mark, thread)
+        const bool again = top_key >= reached;
+        if (again) {
+            const uint16_t least = uint16_t(reached >> 16);
+#pragma unroll 4
+            for (int m = 0; m < marks; ++m)
+                if (sh.marks[m][threadIdx.x] >= least) {
+                    const int place = atomicAdd(&sh.cells_found, 1);
+                    if (place < kCells) sh.cells[place] = uint16_t(m * kThreads + threadIdx.x);
+                }
+        }
+        __syncthreads();
+        const int cells = sh.cells_found;
+        unsigned long long border = (unsigned long long)reached << 32;      // keys from it on are listed
+        for (;;) {
+            const float least = from_ordered(max(uint32_t(border >> 32), 0x007fffffu));     // at least -inf
+            // `per` consecutive logits from x on, the first of which is token `id`
+            auto list = [&](const float *x, int per, int id) {
+#pragma unroll
+                for (int i = 0; i < per; ++i)
+                    if (x[i] >= least) {
+                        const unsigned long long k = key_of(x[i], id + i);
+                        // of masked tokens only the first can be among the likeliest
+                        if (k >= border && id + i < v1 && (x[i] > -INFINITY || id + i < v0 + a.top)) {
+                            const int place = atomicAdd(&sh.count, 1);
+                            if (place < kList) sh.list[place] = k;
+                        }
+                    }
+            };
+            if (cells <= kCells) {
+                // a vector a thread
+                const int each = a.run_tiles * kLoads;
+                for (int i = threadIdx.x; i < cells * each; i += kThreads) {
+                    const int cell = sh.cells[i / each], which = i % each;
+                    const int id = v0 + (cell / kThreads * a.run_tiles + which / kLoads) * kTile + (which % kLoads * kThreads + cell % kThreads) * kVec;
+                    float x[kVec];
+                    if (id + kVec <= v1) {
+                        const uint4 u = __ldg(reinterpret_cast<const uint4 *>(x_row + id));
+                        Vec<T>::one(u, x);
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < kVec; ++k) x[k] = id + k < v1 ? float(x_row[id + k]) : -INFINITY;
+                    }
+                    list(x, kVec, id);
+                }
+            } else if (again) {
+                // too many for a list: everyone goes through their own
+                for (int v = v0; v < v1; v += kTile) {
+                    uint4 now[kLoads];
+                    float x[kPer];
+                    load(v, now);
+                    Vec<T>::get(now, x);
+                    if (!(Vec<T>::most(now, x) >= least)) continue;
+#pragma unroll
+                    for (int i = 0; i < kLoads; ++i) list(x + i * kVec, kVec, v + (i * kThreads + int(threadIdx.x)) * kVec);
+                }
+            }
+            __syncthreads();
+            n = sh.count;
+            if (n <= kList) break;
+            border = kth(sh, kList, a.top);        // k of what was listed reach it
+            __syncthreads();
+            if (threadIdx.x == 0) sh.count = 0;
+            __syncthreads();
+        }
+        if (n > kThreads) {
+            // few enough to be ranked against one another
+            const unsigned long long least = kth(sh, n, a.top);
+            unsigned long long kept[kList / kThreads];
+#pragma unroll
+            for (int i = 0; i < kList / kThreads; ++i) kept[i] = i * kThreads + int(threadIdx.x) < n ? sh.list[i * kThreads + threadIdx.x] : 0;
             __syncthreads();
             if (threadIdx.x == 0) sh.count = 0;
             __syncthreads();
 #pragma unroll
             for (int i = 0; i < kList / kThreads; ++i)
-                if (mine[i] >= least && i * kThreads + int(threadIdx.x) < n) sh.list[atomicAdd(&sh.count, 1)] = mine[i];
+                if (kept[i] >= least && kept[i]) sh.list[atomicAdd(&sh.count, 1)] = kept[i];
             __syncthreads();
             n = sh.count;
         }
         n = sorted_best(sh.list, n, a.top, sh.best);
     }
-    if (threadIdx.x == 0) sh.listed = n;
     if (blocks > 1) {
-        cluster.sync();
-        if (part == 0) {
-            int total = 0;
-            for (int b = 0; b < blocks; ++b) {
-                const Shared *o = cluster.map_shared_rank(&sh, b);
-                const int have = o->listed;
-                for (int i = threadIdx.x; i < have; i += kThreads) sh.gathered[total + i] = o->best[i];
-                total += have;
-                if (threadIdx.x == 0) sh.all[b] = o->block;
-            }
-            __syncthreads();
-            if (threadIdx.x == 0) {
-                Sums all = sh.all[0];
-                for (int b = 1; b < blocks; ++b) all = joined(all, sh.all[b], c);
-                sh.block = all;
-            }
-            if (a.top > 0) n = sorted_best(sh.gathered, total, a.top, sh.best);
+        // every block sends its part to the first one
+        Shared *const first = cluster.map_shared_rank(&sh, 0);
+        __syncthreads();                           // sh.block
+        cluster.barrier_wait();
+        for (int i = threadIdx.x; i < n; i += kThreads) first->gathered[part * kMostTop + i] = sh.best[i];
+        if (threadIdx.x == 0) {
+            first->all[part] = sh.block;
+            first->listed[part] = n;
         }
-        cluster.sync();                            // nobody leaves while its shared memory is read
+        cluster.sync();
         if (part != 0) return;
+        if (a.top > 0) {
+            // closed up (the list's memory is free), then ranked
+            if (warp < blocks) {
+                int to = 0;
+                for (int b = 0; b < warp; ++b) to += sh.listed[b];
+                for (int i = lane; i < sh.listed[warp]; i += 32) sh.list[to + i] = sh.gathered[warp * kMostTop + i];
+            }
+            int total = 0;
+            for (int b = 0; b < blocks; ++b) total += sh.listed[b];
+            __syncthreads();
+            n = sorted_best(sh.list, total, a.top, sh.best);
+        }
+        if (warp == kWarps - 1) {
+            sum = joined<kMostCluster>(lane < blocks ? sh.all[lane] : Sums{-INFINITY, 0.f, 0.f}, c);
+            if (lane == 0) sh.block = sum;
+        }
     }
     __syncthreads();
     const Sums all = sh.block;
     const float ln_l = logf(all.l);
     auto logprob = [&](float x) { return x == -INFINITY && !(all.l != all.l) ? -INFINITY : (x - all.m) * inv_t - ln_l; };
     if (threadIdx.x == 0) {
-        const int token = a.tokens ? a.tokens[row] : -1;
-        if (a.logprobs) a.logprobs[row] = token >= 0 && token < a.vocab ? logprob(float(x_row[token])) : -INFINITY;
+        if (a.logprobs) a.logprobs[row] = logprob(asked);
         if (a.entropy) a.entropy[row] = all.l == 0.f ? 0.f : fmaxf(ln_l - kLn2 * all.s / all.l, 0.f) + (all.l != all.l ? all.l : 0.f);
     }
     for (int i = threadIdx.x; i < a.top; i += kThreads) {
@@ -378,8 +500,9 @@ extern "C" psa_status_t psa_token_logprobs(const void *logits, int32_t logits_dt
     a.top = top_ids || top_logprobs ? top : 0;
     // blocks of a row: as many as keep the SMs (two blocks each) busy, with a tile of work for every one
     int blocks = 1;
-    while (blocks < kMostCluster && int64_t(num_rows) * blocks * 2 <= 2 * 148 && int64_t(vocab) > int64_t(kTile) * blocks) blocks *= 2;
+    while (blocks < kMostCluster && int64_t(num_rows) * blocks * 2 <= 148 && int64_t(vocab) > int64_t(kTile) * blocks) blocks *= 2;
     a.segment = int32_t(((int64_t(vocab) + blocks - 1) / blocks + 7) / 8 * 8);
+    a.run_tiles = ((a.segment + kTile - 1) / kTile + kMarks - 1) / kMarks;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     const cudaError_t e = logits_dtype == PSA_OUT_BF16 ? launch<__nv_bfloat16>(a, num_rows, blocks, st) : launch<float>(a, num_rows, blocks, st);
     if (e != cudaSuccess) return set_last_error(PSA_ERR_CUDA, std::string("log probabilities launch: ") + cudaGetErrorString(e));
