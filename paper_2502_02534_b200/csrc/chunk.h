@@ -10,7 +10,7 @@
 
 namespace psa {
 
-constexpr int kScheduleThreads = 1024;
+constexpr int kScheduleThreads = 256;
 constexpr int kGroupRows = 256;                              // rows of a group: two row tiles of 128
 constexpr int kMostBlocks = 160;                             // persistent blocks, at most one per SM
 constexpr int kMostTokens = 1 << 30;                         // of one sample
@@ -19,6 +19,7 @@ constexpr int64_t kMostChunkPages = int64_t(1) << 27, kMostChunkEntries = (int64
 struct ChunkHeader {
     long long per_head;    // cost of one KV head's groups
     int32_t groups, blocks;
+    int32_t whole, pad;    // a block for every group, uncut
 };
 // Up to kGroupRows rows of one sample: consecutive new tokens and the group's query heads, head fastest.
 struct ChunkGroup {
@@ -110,6 +111,7 @@ __device__ __forceinline__ ChunkGroup chunk_group(const ChunkSample &c, int i, i
 // bytes.  kPieceCost: loading Q, the first tiles' way, the epilogue.
 constexpr int kPieceCost = 4;
 constexpr int kLeastCost = 12;    // a share is not made smaller than this
+constexpr int kWholeTiles = 6;    // key tiles of samples that are not worth cutting
 __device__ __forceinline__ int chunk_tiles(int keys) { return (keys + 127) >> 7; }
 __device__ __forceinline__ int chunk_weight(const ChunkGroup &g, int group) { return g.n_tok * group > 128 ? 4 : 3; }
 __device__ __forceinline__ long long chunk_cost(const ChunkGroup &g, int group)
@@ -158,6 +160,11 @@ struct ChunkWalk {
     {
         head = a.num_kv_heads;
         if (block >= h.blocks || h.groups == 0) return;
+        if (h.whole) {
+            head = block / h.groups;
+            gi = block % h.groups;
+            return;
+        }
         const long long total = h.per_head * a.num_kv_heads;
         x0 = share_begin(total, block, h.blocks);
         x1 = share_begin(total, block + 1, h.blocks);
@@ -165,6 +172,17 @@ struct ChunkWalk {
     }
     __device__ __forceinline__ bool next(ChunkPiece &p)
     {
+        if (h.whole) {
+            if (head >= a.num_kv_heads) return false;
+            p.g = a.groups[gi];
+            p.head = head;
+            p.t0 = 0;
+            p.t1 = chunk_tiles(p.g.keys);
+            p.split = false;
+            p.slot = 0;
+            head = a.num_kv_heads;
+            return true;
+        }
         for (;;) {
             if (gi >= h.groups) {
                 gi = 0;
@@ -205,18 +223,18 @@ __device__ __forceinline__ Joined join(float a2, float b2)
     const float wa = exp2f(a2 - top), wb = exp2f(b2 - top), sum = wa + wb;
     return {wa / sum, wb / sum, top + log2f(sum)};
 }
-// 32 columns of the earlier result
-__device__ __forceinline__ void add_prior(const ChunkArgs &a, size_t at, float w, float (&v)[32])
+// 16 columns of the earlier result
+__device__ __forceinline__ void add_prior(const ChunkArgs &a, size_t at, float w, float (&v)[16])
 {
     if (a.prior_f32) {
 #pragma unroll
-        for (int i = 0; i < 32; i += 4) {
+        for (int i = 0; i < 16; i += 4) {
             const float4 p = *reinterpret_cast<const float4 *>(static_cast<const float *>(a.prior_out) + at + i);
             v[i] = fmaf(w, p.x, v[i]); v[i + 1] = fmaf(w, p.y, v[i + 1]); v[i + 2] = fmaf(w, p.z, v[i + 2]); v[i + 3] = fmaf(w, p.w, v[i + 3]);
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 32; i += 8) {
+        for (int i = 0; i < 16; i += 8) {
             const uint4 p = *reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(a.prior_out) + at + i);
             const uint32_t u[4] = {p.x, p.y, p.z, p.w};
 #pragma unroll

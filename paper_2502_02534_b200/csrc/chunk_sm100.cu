@@ -32,36 +32,70 @@ namespace {
 
 constexpr int kTileKeys = 128;
 constexpr int kRowTile = 128;
+constexpr int kChunkThreads = 11 * 32;
 constexpr int kPagesPerTile = kTileKeys / kPageSize;
 constexpr float kThreshold = 8.f;                      // log2 units
 constexpr float kHalfSumLimit = 64.f * 256.f * 1.01f;  // 64 exponentials of at most 2^8
 // P is truncated to bf16; exponents carry log2 of 1 / (1 - 2^-8 / (2 ln 2)), what truncation loses on average, and the sums are freed of it
 constexpr float kBias = 0.0040709119f, kUnbias = 0.99718224f;
+constexpr uint32_t kPolyOf16 = 0x1111;                 // pairs of 32 scores whose exponentials are polynomials
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 
 
 // ------------------------------------------------------------------------------------------------------------- schedule
-// Running sums over the samples by one block; every thread takes samples of its own (a sample's groups one after another).
+// Running sums over the samples by one block, a thread a sample; a sample of many groups is its warp's.
 __global__ void __launch_bounds__(kScheduleThreads)
 chunk_schedule_kernel(ChunkArgs a)
 {
-    __shared__ long long sum_cost[kScheduleThreads / 32];
-    __shared__ int sum_groups[kScheduleThreads / 32];
+    constexpr int kWarps = kScheduleThreads / 32, kAlone = 4;   // groups that a thread goes through by itself
+    __shared__ long long sum_cost[kWarps];
+    __shared__ int sum_groups[kWarps], longest;
     grid_release();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int per_group = kGroupRows / a.group;   // tokens
     long long carry_cost = 0;
-    int carry_groups = 0;
+    int carry_groups = 0, my_longest = 0;
+    if (threadIdx.x == 0) longest = 0;
     for (int s0 = 0; s0 < a.num_samples; s0 += kScheduleThreads) {
         const int s = s0 + int(threadIdx.x);
         ChunkSample c{};
-        int groups = 0;
-        long long cost = 0;
-        if (s < a.num_samples) {
-            c = chunk_sample(a, s);
-            groups = (c.n + per_group - 1) / per_group;
-            for (int i = 0; i < groups; ++i) cost += chunk_cost(chunk_group(c, i, per_group), a.group);
-        }
+        if (s < a.num_samples) c = chunk_sample(a, s);
+        const int groups = (c.n + per_group - 1) / per_group;
+        if (c.n > 0) my_longest = max(my_longest, chunk_tiles(c.len));
+        // put(place, group) for every group of the lane's sample, places from `to` on, costs from `at` on; returns the cost of all
+        auto each = [&](long long at, int to, auto put) {
+            const long long begin = at;
+            if (groups <= kAlone)
+                for (int i = 0; i < groups; ++i) {
+                    ChunkGroup g = chunk_group(c, i, per_group);
+                    g.cum = at;
+                    put(to + i, g);
+                    at += chunk_cost(g, a.group);
+                }
+            for (unsigned many = __ballot_sync(0xffffffffu, groups > kAlone); many; many &= many - 1) {
+                const int owner = __ffs(many) - 1;
+                const ChunkSample o{__shfl_sync(0xffffffffu, c.q0, owner), __shfl_sync(0xffffffffu, c.n, owner), __shfl_sync(0xffffffffu, c.len, owner),
+                                    __shfl_sync(0xffffffffu, c.list0, owner)};
+                const int its = __shfl_sync(0xffffffffu, groups, owner), first = __shfl_sync(0xffffffffu, to, owner);
+                long long before = __shfl_sync(0xffffffffu, at, owner);
+                for (int i0 = 0; i0 < its; i0 += 32) {
+                    ChunkGroup g = chunk_group(o, min(i0 + lane, its - 1), per_group);
+                    const long long cost = i0 + lane < its ? chunk_cost(g, a.group) : 0;
+                    long long x = cost;
+#pragma unroll
+                    for (int d = 1; d < 32; d <<= 1) {
+                        const long long u = __shfl_up_sync(0xffffffffu, x, d);
+                        if (lane >= d) x += u;
+                    }
+                    g.cum = before + x - cost;
+                    if (i0 + lane < its) put(first + i0 + lane, g);
+                    before += __shfl_sync(0xffffffffu, x, 31);
+                }
+                if (lane == owner) at = before;
+            }
+            return at - begin;
+        };
+        const long long cost = each(0, 0, [](int, const ChunkGroup &) {});
         // exclusive scans over the block
         long long x = cost;
         int y = groups;
@@ -73,23 +107,21 @@ chunk_schedule_kernel(ChunkArgs a)
         }
         if (lane == 31) { sum_cost[warp] = x; sum_groups[warp] = y; }
         __syncthreads();
-        long long before_cost = carry_cost;
-        int before_groups = carry_groups;
-        for (int w = 0; w < kScheduleThreads / 32; ++w) {
-            if (w < warp) { before_cost += sum_cost[w]; before_groups += sum_groups[w]; }
+        long long at = carry_cost + x - cost;
+        int to = carry_groups + y - groups;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            if (w < warp) { at += sum_cost[w]; to += sum_groups[w]; }
             carry_cost += sum_cost[w];
             carry_groups += sum_groups[w];
         }
         __syncthreads();
-        long long at = before_cost + x - cost;
-        int to = before_groups + y - groups;
-        for (int i = 0; i < groups; ++i, ++to) {
-            ChunkGroup g = chunk_group(c, i, per_group);
-            g.cum = at;
-            at += chunk_cost(g, a.group);
-            if (to < a.max_groups) a.groups[to] = g;
-        }
+        each(at, to, [&](int place, const ChunkGroup &g) {
+            if (place < a.max_groups) a.groups[place] = g;
+        });
     }
+    if (my_longest) atomicMax(&longest, my_longest);
+    __syncthreads();
     if (threadIdx.x == 0) {
         if (carry_groups > a.max_groups) {   // q_indptr that runs backwards: more rows than there are
             raise(a.status, PSA_ERR_BOUNDS);
@@ -101,6 +133,11 @@ chunk_schedule_kernel(ChunkArgs a)
         h.per_head = carry_cost;
         h.groups = carry_groups;
         h.blocks = int(max(1ll, min((long long)a.blocks, total / kLeastCost)));
+        // a block for every group, uncut, where there are enough of them and none is long: no results to join
+        if ((long long)carry_groups * a.num_kv_heads <= a.blocks && longest <= kWholeTiles) {
+            h.whole = 1;
+            h.blocks = max(1, carry_groups * a.num_kv_heads);
+        }
         *a.header = h;
     }
 }
@@ -135,33 +172,31 @@ __device__ __forceinline__ Travel travel(int m, int n, bool two)
 // place of V tile i in that order
 __device__ __forceinline__ int v_place(int i, int n, bool two) { return two ? 2 * i + 1 : i < n - 1 ? 2 * i + 2 : 2 * n - 1; }
 
-// 32 columns of one row to global memory
-__device__ __forceinline__ void store_f32(float *to, const float (&v)[32])
+// 16 columns of one row to global memory
+__device__ __forceinline__ void store_f32(float *to, const float (&v)[16])
 {
 #pragma unroll
-    for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4 *>(to + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+    for (int i = 0; i < 16; i += 4) *reinterpret_cast<float4 *>(to + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
 }
-__device__ __forceinline__ void store_bf16(__nv_bfloat16 *to, const float (&v)[32])
+__device__ __forceinline__ void store_bf16(__nv_bfloat16 *to, const float (&v)[16])
 {
+    uint32_t w[8];
 #pragma unroll
-    for (int i = 0; i < 32; i += 8) {
-        uint32_t w[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const __nv_bfloat162 p = __floats2bfloat162_rn(v[i + 2 * k], v[i + 2 * k + 1]);
-            w[k] = reinterpret_cast<const uint32_t &>(p);
-        }
-        *reinterpret_cast<uint4 *>(to + i) = make_uint4(w[0], w[1], w[2], w[3]);
+    for (int k = 0; k < 8; ++k) {
+        const __nv_bfloat162 p = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
+        w[k] = reinterpret_cast<const uint32_t &>(p);
     }
+    reinterpret_cast<uint4 *>(to)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    reinterpret_cast<uint4 *>(to)[1] = make_uint4(w[4], w[5], w[6], w[7]);
 }
 
 template <int D>
-__global__ void __launch_bounds__(320, 1)
+__global__ void __launch_bounds__(kChunkThreads, 1)
 chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
              const ChunkArgs a)
 {
     using L = ChunkSmem<D>;
-    constexpr int kProducerWarp = 8, kMmaWarp = 9;
+    constexpr int kMmaWarp = 8, kProducerWarp = 9, kProducers = 2;
     constexpr int kKSteps = D / 16;
     constexpr uint32_t kIdescQK = make_idesc(kTileKeys, false), kIdescPV = make_idesc(D, true);
     constexpr uint32_t kColO = 256;                    // S[t] at 128 t, O[t] at 256 + t D
@@ -183,7 +218,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
 
     if (threadIdx.x == 0) {
         *abort_flag = 0;
-        for (int i = 0; i < L::kNumBars; ++i) mbar_init(bar(i), i >= L::kBarP && i < L::kBarHalf ? 128 : i == L::kBarMet ? 256 : 1);
+        for (int i = 0; i < L::kNumBars; ++i) mbar_init(bar(i), i >= L::kBarFull && i < L::kBarEmpty ? kProducers : i >= L::kBarP && i < L::kBarHalf ? 128 : i == L::kBarMet ? 256 : 1);
         fence_barrier_init();
     }
     if (warp == kMmaWarp) {
@@ -201,8 +236,9 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
     ChunkWalk walk(a, blockIdx.x, lane);
     ChunkPiece pc;
 
-    if (warp == kProducerWarp) {
-        // ------------------------------------------------------------ TMA producer, one box per lane
+    if (warp >= kProducerWarp) {
+        // ------------------------------------------------------------ TMA producers: each takes every other page of a tile
+        const int part = warp - kProducerWarp;
         uint32_t e = 0, q_uses[2] = {0, 0}, q_sel = 0;
         bool ok = true;
         while (ok && walk.next(pc)) {
@@ -210,9 +246,12 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
             if (n == 0) continue;
             const bool two = pc.g.n_tok * a.group > kRowTile;
             auto page_of = [&](int m) {   // this lane's page of element m
-                const int page = (pc.t0 + travel(m, n, two).tile) * kPagesPerTile + lane / L::kHalves;
-                if (lane >= kPagesPerTile * L::kHalves || page * kPageSize >= pc.g.keys) return 0;
-                return a.page_indices[pc.g.list0 + page];   // inside the list: the schedule saw to that
+                const int page = (pc.t0 + travel(m, n, two).tile) * kPagesPerTile + lane;
+                if (lane >= kPagesPerTile || page * kPageSize >= pc.g.keys) return 0;
+                const int id = a.page_indices[pc.g.list0 + page];   // inside the list: the schedule saw to that
+                if (id >= 0 && id < a.num_pool_pages) return id;
+                raise(a.status, PSA_ERR_BOUNDS);
+                return a.num_pool_pages;                              // outside the map: zeros
             };
             int id = page_of(0);
             for (int m = 0; ok && m < 2 * n; ++m, ++e) {
@@ -223,29 +262,34 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
                 const int left = pc.g.keys - (pc.t0 + tr.tile) * kTileKeys;
                 const int pages = min(kPagesPerTile, (left + kPageSize - 1) / kPageSize);
                 const uint32_t full = bar(L::kBarFull + slot), dst = sbase + L::kRingOff + slot * L::kTileBytes;
-                if (lane == 0) mbar_expect_tx(full, pages * kPageSize * D * 2);
-                __syncwarp();
-                if (lane < pages * L::kHalves) {
-                    const int p = lane / L::kHalves, h = lane % L::kHalves;
-                    if (id < 0 || id >= a.num_pool_pages) {
-                        raise(a.status, PSA_ERR_BOUNDS);
-                        id = a.num_pool_pages;   // outside the map: zeros
-                    }
-                    tma_load_4d(dst + h * L::kHalfBytes + p * kPageSize * 128, tr.is_v ? &map_v : &map_k, full, h * 64, 0, pc.head, id);
+                int ids[kPagesPerTile];
+#pragma unroll
+                for (int p = 0; p < kPagesPerTile; ++p) ids[p] = __shfl_sync(0xffffffffu, id, p);
+                if (elect_one()) {
+                    mbar_expect_tx(full, (pages + kProducers - 1 - part) / kProducers * kPageSize * D * 2);
+                    const CUtensorMap *map = tr.is_v ? &map_v : &map_k;
+#pragma unroll
+                    for (int p = 0; p < kPagesPerTile; ++p)
+                        if (p < pages && p % kProducers == part)
+#pragma unroll
+                            for (int h = 0; h < L::kHalves; ++h)
+                                tma_load_4d(dst + h * L::kHalfBytes + p * kPageSize * 128, map, full, h * 64, 0, pc.head, ids[p]);
                 }
+                __syncwarp();
                 id = next;
-                if (m == 0) {   // Q behind the first K tile
+                if (m == 0 && part == 0) {   // Q behind the first K tile
                     const int tiles = two ? 2 : 1;
                     for (int t = 0; ok && t < tiles; ++t) {
                         const int b = two ? t : int(q_sel);
                         if (q_uses[b] > 0 && !(ok = warp_wait(bar(L::kBarQEmpty + b), (q_uses[b] - 1) & 1))) break;
                         ++q_uses[b];
-                        if (lane == 0) {
+                        if (elect_one()) {
                             mbar_expect_tx(bar(L::kBarQFull + b), L::kTileBytes);
                             for (int h = 0; h < L::kHalves; ++h)
                                 tma_load_4d(sbase + L::kQOff + b * L::kTileBytes + h * L::kHalfBytes, &map_q, bar(L::kBarQFull + b), h * 64, 0, pc.head,
                                             pc.g.q0 + t * (kRowTile / a.group));
                         }
+                        __syncwarp();
                     }
                     if (!two) q_sel ^= 1;
                 }
@@ -371,48 +415,53 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
                     continue;
                 }
                 const int valid = sees - tile * kTileKeys;
-                uint32_t s0[2][32], s1[2][32];
-                auto load = [&](int h, uint32_t (&r)[2][32]) {
-                    tmem_ld32(s_addr + h * 64, r[0]);
-                    tmem_ld32(s_addr + h * 64 + 32, r[1]);
-                };
-                auto mask = [&](int v, uint32_t (&r)[2][32]) {
-                    if (__any_sync(0xffffffffu, v < 64)) {
+                // A half is 64 scores, 32 at a time; S of the half stays in tensor memory until all of it is known to be in range, P in p.
+                uint32_t p[32];
+                auto mask = [&](int v, uint32_t (&r)[32]) {
+                    if (__any_sync(0xffffffffu, v < 32)) {
 #pragma unroll
-                        for (int i = 0; i < 64; ++i)
-                            if (i >= v) r[i / 32][i % 32] = 0xff800000u;
+                        for (int i = 0; i < 32; ++i)
+                            if (i >= v) r[i] = 0xff800000u;
                     }
                 };
-                // 64 scores -> 32 words of bf16 P in r[0]; returns their sum
-                auto exponentials = [&](uint32_t (&r)[2][32]) -> float {
+                // 32 scores -> 16 words of bf16 P; adds them to `sum`
+                auto exponentials = [&](const uint32_t (&r)[32], uint32_t *to, float2 (&sum)[2]) {
                     const float off = kBias - (m_ref == -INFINITY ? 0.f : m_ref);
-                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int i = 0; i < 64; i += 2) {
-                        const bool poly = ((i >> 1) % 3) == 2;   // a third by polynomial, where the special-function unit is the bound
-                        const float x0 = fmaf(__uint_as_float(r[i / 32][i % 32]), a.scale_log2, off);
-                        const float x1 = fmaf(__uint_as_float(r[i / 32][i % 32 + 1]), a.scale_log2, off);
-                        const float p0 = poly ? poly_exp2_fine<4>(x0) : fast_exp2(x0), p1 = poly ? poly_exp2_fine<4>(x1) : fast_exp2(x1);
-                        sum[(i >> 1) & 3] += p0 + p1;
-                        r[0][i / 2] = __byte_perm(__float_as_uint(p0), __float_as_uint(p1), 0x7632);
+                    for (int i = 0; i < 32; i += 2) {
+                        const float2 x = fma2(make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), make_float2(a.scale_log2, a.scale_log2), make_float2(off, off));
+                        // part of them by polynomial: it relieves the special-function unit, which has an exponential a score
+                        const bool poly = kPolyOf16 >> (i / 2) & 1;
+                        const float2 e = poly ? poly_exp2_pair(x) : make_float2(fast_exp2(x.x), fast_exp2(x.y));
+                        sum[i / 2 & 1] = add2(sum[i / 2 & 1], e);
+                        to[i / 2] = __byte_perm(__float_as_uint(e.x), __float_as_uint(e.y), 0x7632);
                     }
-                    return (sum[0] + sum[1]) + (sum[2] + sum[3]);
                 };
-                auto half = [&](int h, uint32_t (&r)[2][32]) -> bool {
+                auto half = [&](int h) -> bool {
                     const int v = valid - 64 * h;
-                    mask(v, r);
-                    float sum = 0.f;
+                    uint32_t r[2][32];
+                    float total;
+                    tmem_ld32(s_addr + h * 64, r[0]);
+                    tmem_wait_ld();
+                    tmem_ld32(s_addr + h * 64 + 32, r[1]);
                     bool redo = __any_sync(0xffffffffu, m_ref == -INFINITY && v > 0);   // nothing to exponentiate against yet
                     if (!redo) {
-                        sum = exponentials(r);
-                        redo = __any_sync(0xffffffffu, !(sum <= kHalfSumLimit));
-                        if (redo) {
-                            load(h, r);
-                            tmem_wait_ld();
-                            mask(v, r);
-                        }
+                        float2 sum[2] = {{0.f, 0.f}, {0.f, 0.f}};
+                        mask(v, r[0]);
+                        exponentials(r[0], p, sum);
+                        tmem_wait_ld();
+                        mask(v - 32, r[1]);
+                        exponentials(r[1], p + 16, sum);
+                        total = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+                        redo = __any_sync(0xffffffffu, !(total <= kHalfSumLimit));
                     }
                     if (redo) {
+                        tmem_wait_ld();
+                        tmem_ld32(s_addr + h * 64, r[0]);
+                        tmem_ld32(s_addr + h * 64 + 32, r[1]);
+                        tmem_wait_ld();
+                        mask(v, r[0]);
+                        mask(v - 32, r[1]);
                         float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
                         for (int i = 0; i < 64; ++i) mx[i & 3] = fmaxf(mx[i & 3], __uint_as_float(r[i / 32][i % 32]));
@@ -427,41 +476,43 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
                                     if (!warp_wait(bar(L::kBarHalf + t), uses & 1)) return false;
                                     tc_fence_after();
                                 }
-                                uint32_t o[32];
 #pragma unroll 1
                                 for (int c = 0; c < D / 32; ++c) {
-                                    tmem_ld32(o_base + t * D + c * 32, o);
+                                    tmem_ld32(o_base + t * D + c * 32, p);
                                     tmem_wait_ld();
 #pragma unroll
-                                    for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
-                                    tmem_st32(o_base + t * D + c * 32, o);
+                                    for (int i = 0; i < 32; ++i) p[i] = __float_as_uint(__uint_as_float(p[i]) * alpha);
+                                    tmem_st32(o_base + t * D + c * 32, p);
                                 }
                                 tmem_wait_st();
                             }
                             l_sum *= alpha;
                             if (need) m_ref = top;
                         }
-                        sum = exponentials(r);
+                        float2 sum[2] = {{0.f, 0.f}, {0.f, 0.f}};
+                        exponentials(r[0], p, sum);
+                        exponentials(r[1], p + 16, sum);
+                        total = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
                     }
-                    tmem_st32(s_addr + h * 32, r[0]);
-                    l_sum += sum;
+                    tmem_st32(s_addr + h * 32, p);
+                    l_sum += total;
                     tmem_wait_st();
                     tc_fence_before();
                     mbar_arrive(bar_p(t, h));
                     return true;
                 };
-                load(0, s0);
-                tmem_wait_ld();
-                load(1, s1);
-                if (!(ok = half(0, s0))) break;
-                tmem_wait_ld();
-                if (!(ok = half(1, s1))) break;
+                if (!(ok = half(0))) break;
+                if (!(ok = half(1))) break;
             }
             if (!ok) break;
             e += 2 * n;
 
             // ---- epilogue
             l_sum *= kUnbias;
+            const size_t out_row = size_t(pc.g.q0 + token) * a.num_q_heads + pc.head * a.group + in_group % a.group;
+            const size_t part_row = size_t(pc.slot) * a.slot_rows + in_group;
+            const bool joins = mine && !pc.split && a.prior_lse;
+            const float prior2 = joins ? a.prior_lse[out_row] * kLog2e : -INFINITY;
             const int streams = n == 0 ? 0 : two || n > 1 ? 2 : 1;
             if (two || n == 0) {
                 if (n > 0) {
@@ -492,40 +543,37 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
                 lse2 = total == 0.f ? -INFINITY : top + log2f(total);
             }
             // this warpgroup's columns: all of its own row tile, or half of the shared one
-            const int c0 = two ? 0 : t * (D / 64), c1 = two ? D / 32 : (t + 1) * (D / 64);
-            const size_t out_row = size_t(pc.g.q0 + token) * a.num_q_heads + pc.head * a.group + in_group % a.group;
-            const size_t part_row = size_t(pc.slot) * a.slot_rows + in_group;
+            const int c0 = two ? 0 : t * (D / 2), c1 = two ? D : (t + 1) * (D / 2);
             float from_prior = 0.f;
-            if (mine && !pc.split && a.prior_lse) {
-                const Joined jn = join(lse2, a.prior_lse[out_row] * kLog2e);
+            if (joins) {
+                const Joined jn = join(lse2, prior2);
                 share[0] *= jn.first;
                 share[1] *= jn.first;
                 from_prior = jn.second;
                 lse2 = jn.lse2;
             }
-            for (int c = c0; active && c < c1; ++c) {
+            for (int c = c0; active && c < c1; c += 16) {
                 __syncwarp();
-                float v[32];
+                float v[16];
 #pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = 0.f;
+                for (int i = 0; i < 16; ++i) v[i] = 0.f;
                 for (int i = 0; i < 2; ++i) {
-                    if (two ? i != t : i >= streams) continue;
-                    if (n == 0) continue;
-                    uint32_t o[32];
-                    tmem_ld32(o_base + i * D + c * 32, o);
+                    if (n == 0 || (two ? i != t : i >= streams)) continue;
+                    uint32_t o[16];
+                    tmem_ld16(o_base + i * D + c, o);
                     tmem_wait_ld();
                     if (share[i] != 0.f)
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) v[k] = fmaf(__uint_as_float(o[k]), share[i], v[k]);
+                        for (int k = 0; k < 16; ++k) v[k] = fmaf(__uint_as_float(o[k]), share[i], v[k]);
                 }
                 if (!mine) continue;
                 if (pc.split) {
-                    store_f32(a.partial_o + part_row * D + c * 32, v);
+                    store_f32(a.partial_o + part_row * D + c, v);
                     continue;
                 }
-                if (from_prior != 0.f) add_prior(a, out_row * D + c * 32, from_prior, v);
-                if (a.out_f32) store_f32(static_cast<float *>(a.out) + out_row * D + c * 32, v);
-                else store_bf16(static_cast<__nv_bfloat16 *>(a.out) + out_row * D + c * 32, v);
+                if (from_prior != 0.f) add_prior(a, out_row * D + c, from_prior, v);
+                if (a.out_f32) store_f32(static_cast<float *>(a.out) + out_row * D + c, v);
+                else store_bf16(static_cast<__nv_bfloat16 *>(a.out) + out_row * D + c, v);
             }
             tc_fence_before();
             if (!two) {
@@ -548,7 +596,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
     if (*abort_flag) {
         if (threadIdx.x == 0) raise(a.status, PSA_ERR_TIMEOUT);
         // let copies that were already issued land before the block's shared memory is released
-        if (warp == kProducerWarp && lane == 0) {
+        if (warp >= kProducerWarp && lane == 0) {
             const unsigned long long t0 = global_timer_ns();
             while (global_timer_ns() - t0 < 2000000ull) { }
         }
@@ -568,15 +616,17 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
 
 // ------------------------------------------------------------------------------------------------------------- merge
 // Block (cut, slice): the group that the end of share `cut` falls into, if that is the first cut inside it; a warp per row.
+constexpr int kMergeWarps = 8;
 template <int D>
-__global__ void __launch_bounds__(128)
+__global__ void __launch_bounds__(kMergeWarps * 32)
 chunk_merge_kernel(const ChunkArgs a)
 {
+    __shared__ int slots[2 * kMostBlocks];
     grid_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const ChunkHeader h = *a.header;
     const int cut = blockIdx.x;                 // between blocks cut and cut + 1
-    if (cut + 1 >= h.blocks || h.groups == 0) return;
+    if (cut + 1 >= h.blocks || h.groups == 0 || h.whole) return;
     const long long total = h.per_head * a.num_kv_heads;
     const long long x = share_begin(total, cut + 1, h.blocks);
     int head, gi;
@@ -588,19 +638,45 @@ chunk_merge_kernel(const ChunkArgs a)
     if (t_cut <= 0 || t_cut >= tiles) return;                                              // nothing is cut here
     if (cut > 0 && tile_at(g, a.group, base, share_begin(total, cut, h.blocks)) > 0) return;   // an earlier cut's group
     // pieces: blocks cut, cut + 1, ... until the group ends
+    __shared__ int last;
+    if (threadIdx.x == 0) last = h.blocks - 1;
+    __syncthreads();
+    for (int b = cut + threadIdx.x; b < h.blocks; b += blockDim.x) {
+        const int t0 = tile_at(g, a.group, base, share_begin(total, b, h.blocks)), t1 = tile_at(g, a.group, base, share_begin(total, b + 1, h.blocks));
+        slots[b - cut] = t1 > t0 ? 2 * b + (t0 > 0 ? 0 : 1) : -1;
+        if (t1 >= tiles) atomicMin(&last, b);
+    }
+    __syncthreads();
+    const int pieces = last - cut + 1;
     const int rows = g.n_tok * a.group;
     constexpr int kPer = D / 32;
-    for (int r = blockIdx.y * (blockDim.x >> 5) + warp; r < rows; r += gridDim.y * (blockDim.x >> 5)) {
+    for (int r = blockIdx.y * kMergeWarps + warp; r < rows; r += gridDim.y * kMergeWarps) {
+        const size_t row = size_t(g.q0 + r / a.group) * a.num_q_heads + head * a.group + r % a.group;
+        const float prior2 = a.prior_lse ? a.prior_lse[row] * kLog2e : -INFINITY;
         float top = -INFINITY, sum = 0.f, acc[kPer];
 #pragma unroll
         for (int i = 0; i < kPer; ++i) acc[i] = 0.f;
-        for (int b = cut; b < h.blocks; ++b) {
-            const int t0 = tile_at(g, a.group, base, share_begin(total, b, h.blocks)), t1 = tile_at(g, a.group, base, share_begin(total, b + 1, h.blocks));
-            if (t1 > t0) {
-                const size_t at = size_t(2 * b + (t0 > 0 ? 0 : 1)) * a.slot_rows + r;
-                const float lse2 = a.partial_lse[at];
+        for (int b0 = 0; b0 < pieces; b0 += 32) {
+            // a lane's piece
+            const int slot = b0 + lane < pieces ? slots[b0 + lane] : -1;
+            const float lse2 = slot >= 0 ? a.partial_lse[size_t(slot) * a.slot_rows + r] : -INFINITY;
+            float most = lse2;
+#pragma unroll
+            for (int d = 16; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+            const float next = fmaxf(top, most);
+            const float keep = top == -INFINITY ? 0.f : exp2f(top - next), w = lse2 == -INFINITY ? 0.f : exp2f(lse2 - next);
+            top = next;
+            sum *= keep;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) acc[i] *= keep;
+            const int here = min(32, pieces - b0);
+#pragma unroll 4
+            for (int i = 0; i < here; ++i) {
+                const int from_slot = __shfl_sync(0xffffffffu, slot, i);
+                const float from_w = __shfl_sync(0xffffffffu, w, i);
+                if (from_slot < 0 || from_w == 0.f) continue;
+                const float *from = a.partial_o + (size_t(from_slot) * a.slot_rows + r) * D + lane * kPer;
                 float o[kPer];
-                const float *from = a.partial_o + at * D + lane * kPer;
                 if constexpr (kPer == 4) {
                     const float4 q = *reinterpret_cast<const float4 *>(from);
                     o[0] = q.x; o[1] = q.y; o[2] = q.z; o[3] = q.w;
@@ -608,34 +684,31 @@ chunk_merge_kernel(const ChunkArgs a)
                     const float2 q = *reinterpret_cast<const float2 *>(from);
                     o[0] = q.x; o[1] = q.y;
                 }
-                if (lse2 != -INFINITY) {
-                    const float next = fmaxf(top, lse2);
-                    const float keep = top == -INFINITY ? 0.f : exp2f(top - next), w = exp2f(lse2 - next);
-                    sum = sum * keep + w;
+                sum += from_w;
 #pragma unroll
-                    for (int i = 0; i < kPer; ++i) acc[i] = acc[i] * keep + w * o[i];
-                    top = next;
-                }
+                for (int k = 0; k < kPer; ++k) acc[k] = fmaf(from_w, o[k], acc[k]);
             }
-            if (t1 >= tiles) break;
         }
         float lse2 = sum == 0.f ? -INFINITY : top + log2f(sum);
         float share = sum == 0.f ? 0.f : 1.f / sum, from_prior = 0.f;
-        const size_t row = size_t(g.q0 + r / a.group) * a.num_q_heads + head * a.group + r % a.group;
         if (a.prior_lse) {
-            const Joined jn = join(lse2, a.prior_lse[row] * kLog2e);
+            const Joined jn = join(lse2, prior2);
             share *= jn.first;
             from_prior = jn.second;
             lse2 = jn.lse2;
         }
+        const size_t at = row * D + lane * kPer;
+        float v[kPer];
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            const size_t at = row * D + lane * kPer + i;
-            float v = acc[i] * share;
+            v[i] = acc[i] * share;
             if (from_prior != 0.f)
-                v = fmaf(from_prior, a.prior_f32 ? static_cast<const float *>(a.prior_out)[at] : __bfloat162float(static_cast<const __nv_bfloat16 *>(a.prior_out)[at]), v);
-            if (a.out_f32) static_cast<float *>(a.out)[at] = v;
-            else static_cast<__nv_bfloat16 *>(a.out)[at] = __float2bfloat16_rn(v);
+                v[i] = fmaf(from_prior, a.prior_f32 ? static_cast<const float *>(a.prior_out)[at + i] : __bfloat162float(static_cast<const __nv_bfloat16 *>(a.prior_out)[at + i]), v[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < kPer; i += 2) {
+            if (a.out_f32) *reinterpret_cast<float2 *>(static_cast<float *>(a.out) + at + i) = make_float2(v[i], v[i + 1]);
+            else *reinterpret_cast<__nv_bfloat162 *>(static_cast<__nv_bfloat16 *>(a.out) + at + i) = __floats2bfloat162_rn(v[i], v[i + 1]);
         }
         __syncwarp();   // lse may be prior_lse: every lane has read it
         if (lane == 0) a.lse[row] = lse2 * kLn2;
@@ -650,8 +723,8 @@ cudaError_t launch(const ChunkArgs &a, const CUtensorMap &mq, const CUtensorMap 
         return cudaError_t(rc);
     chunk_schedule_kernel<<<1, kScheduleThreads, 0, st>>>(a);
     cudaError_t e = cudaGetLastError();
-    if (e == cudaSuccess) e = launch_dependent(chunk_kernel<D>, dim3(a.blocks), 320, ChunkSmem<D>::kTotal, st, mq, mk, mv, a);
-    if (e == cudaSuccess && a.blocks > 1) e = launch_dependent(chunk_merge_kernel<D>, dim3(a.blocks - 1, (a.slot_rows + 31) / 32), 128, 0, st, a);
+    if (e == cudaSuccess) e = launch_dependent(chunk_kernel<D>, dim3(a.blocks), kChunkThreads, ChunkSmem<D>::kTotal, st, mq, mk, mv, a);
+    if (e == cudaSuccess && a.blocks > 1) e = launch_dependent(chunk_merge_kernel<D>, dim3(a.blocks - 1, (a.slot_rows + 15) / 16), kMergeWarps * 32, 0, st, a);
     return e;
 }
 
