@@ -432,7 +432,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
                         const float2 x = fma2(make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), make_float2(a.scale_log2, a.scale_log2), make_float2(off, off));
                         // part of them by polynomial: it relieves the special-function unit, which has an exponential a score
                         const bool poly = kPolyOf16 >> (i / 2) & 1;
-                        const float2 e = poly ? poly_exp2_pair(x) : make_float2(fast_exp2(x.x), fast_exp2(x.y));
+                        const float2 e = poly ? poly_exp2_pair<4>(x) : make_float2(fast_exp2(x.x), fast_exp2(x.y));
                         sum[i / 2 & 1] = add2(sum[i / 2 & 1], e);
                         to[i / 2] = __byte_perm(__float_as_uint(e.x), __float_as_uint(e.y), 0x7632);
                     }

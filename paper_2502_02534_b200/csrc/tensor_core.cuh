@@ -180,31 +180,6 @@ __device__ __forceinline__ float poly_exp2(float x)
     asm("mul.ftz.f32 %0, %1, 0f3F800000;" : "=f"(r) : "f"(__uint_as_float(__float_as_uint(p) + (__float_as_uint(t) << 23))));
     return r;
 }
-// The same with a polynomial of degree 4 (relative error below 2.7e-6, mean 4e-8) or 5 (1.6e-7, mean 5e-8), for sums that are compared in
-// fp32.  Minimax fits of 2^f over [-0.5, 0.5] in the relative error, rounded to fp32.
-template <int kDegree>
-__device__ __forceinline__ float poly_exp2_fine(float x)
-{
-    x = fmaxf(x, -126.f);
-    const float t = x + 12582912.f;
-    const float f = x - (t - 12582912.f);
-    float p;
-    if constexpr (kDegree == 4) {
-        p = fmaf(f, 0.009570102207362652f, 0.05591785907745361f);
-        p = fmaf(p, f, 0.240247443318367f);
-        p = fmaf(p, f, 0.6931217908859253f);
-        p = fmaf(p, f, 0.9999992847442627f);
-    } else {
-        p = fmaf(f, 0.0013276472454890609f, 0.009675540961325169f);
-        p = fmaf(p, f, 0.05550713092088699f);
-        p = fmaf(p, f, 0.24022120237350464f);
-        p = fmaf(p, f, 0.6931469440460205f);
-        p = fmaf(p, f, 1.0000001192092896f);
-    }
-    float r;
-    asm("mul.ftz.f32 %0, %1, 0f3F800000;" : "=f"(r) : "f"(__uint_as_float(__float_as_uint(p) + (__float_as_uint(t) << 23))));
-    return r;
-}
 __device__ __forceinline__ float fast_exp2(float x)
 {
     float y;
@@ -234,20 +209,31 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b)
         : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return r;
 }
-// poly_exp2_fine<4> of a pair
+// Of a pair, in fewer instructions, with a polynomial of degree 4 (relative error below 2.7e-6, mean 4e-8) or 5 (1.6e-7, mean 5e-8), for sums
+// that are compared in fp32.  Minimax fits of 2^f over [-0.5, 0.5] in the relative error, rounded to fp32.
+template <int kDegree>
 __device__ __forceinline__ float2 poly_exp2_pair(float2 x)
 {
+    auto both = [](float v) { return make_float2(v, v); };
     x.x = fmaxf(x.x, -126.f);
     x.y = fmaxf(x.y, -126.f);
-    const float2 magic = {12582912.f, 12582912.f}, back = {-12582912.f, -12582912.f};
-    const float2 t = add2(x, magic), n = add2(t, back), f = add2(x, make_float2(-n.x, -n.y));
-    float2 p = fma2(f, make_float2(0.009570102207362652f, 0.009570102207362652f), make_float2(0.05591785907745361f, 0.05591785907745361f));
-    p = fma2(p, f, make_float2(0.240247443318367f, 0.240247443318367f));
-    p = fma2(p, f, make_float2(0.6931217908859253f, 0.6931217908859253f));
-    p = fma2(p, f, make_float2(0.9999992847442627f, 0.9999992847442627f));
+    const float2 t = add2(x, both(12582912.f)), n = add2(t, both(-12582912.f)), f = add2(x, make_float2(-n.x, -n.y));
+    float2 p;
+    if constexpr (kDegree == 4) {
+        p = fma2(f, both(0.009570102207362652f), both(0.05591785907745361f));
+        p = fma2(p, f, both(0.240247443318367f));
+        p = fma2(p, f, both(0.6931217908859253f));
+        p = fma2(p, f, both(0.9999992847442627f));
+    } else {
+        p = fma2(f, both(0.0013276472454890609f), both(0.009675540961325169f));
+        p = fma2(p, f, both(0.05550713092088699f));
+        p = fma2(p, f, both(0.24022120237350464f));
+        p = fma2(p, f, both(0.6931469440460205f));
+        p = fma2(p, f, both(1.0000001192092896f));
+    }
     p.x = __uint_as_float(__float_as_uint(p.x) + (__float_as_uint(t.x) << 23));
     p.y = __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(t.y) << 23));
-    return mul2(p, make_float2(1.f, 1.f));   // what the clamp left as a denormal becomes 0
+    return mul2(p, both(1.f));   // what the clamp left as a denormal becomes 0
 }
 
 // ---------------------------------------------------------------- descriptors

@@ -10,8 +10,8 @@
 // Work units are (KV head, sample, key pair, row tile); a share is a run of them, as in chunk.h.  A pair's rows may be cut between shares:
 // each then leaves 256 partial sums, which weights_merge_kernel adds in order.
 //
-// 10 warps: 0-3 and 4-7 take the first and second key tile of a pair (thread = key), 8 producer (TMA; also the rows' log-sum-exps), 9 MMA
-// issuer and owner of the tensor memory.  Two score buffers of 128 columns for each key tile.  Every wait is bounded.
+// 11 warps: 0-3 and 4-7 take the first and second key tile of a pair (thread = key), 8 is the MMA issuer and owner of the tensor memory, 9 and
+// 10 bring in K and the rows with their log-sum-exps.  Two score buffers of 128 columns for each key tile.  Every wait is bounded.
 #include <algorithm>
 
 #include "chunk.h"
@@ -21,6 +21,7 @@
 namespace psa {
 namespace {
 
+constexpr int kWeightsThreads = 11 * 32, kPagesPerTile = 128 / kPageSize;
 constexpr int kPairKeys = 256, kTileKeys = 128, kRowTile = 128, kFewRows = 16;
 constexpr int kPairCost = 4, kRowCost = 2, kLeastShare = 8;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -219,12 +220,12 @@ struct WeightsSmem {
 };
 
 template <int D>
-__global__ void __launch_bounds__(320, 1)
+__global__ void __launch_bounds__(kWeightsThreads, 1)
 weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_few, const __grid_constant__ CUtensorMap map_k,
                const WeightsArgs w)
 {
     using L = WeightsSmem<D>;
-    constexpr int kProducerWarp = 8, kMmaWarp = 9, kKSteps = D / 16;
+    constexpr int kMmaWarp = 8, kKeyWarp = 9, kRowWarp = 10, kKSteps = D / 16;
     const ChunkArgs &a = w.c;
     extern __shared__ __align__(1024) unsigned char smem[];
     const uint32_t sbase = smem_u32(smem);
@@ -265,8 +266,45 @@ weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
 
     // The order of things, which every role follows: for each pair of a piece its K tiles, then its row tiles one by one.  A sample with
     // one row tile has it loaded once for all pairs of a piece.
-    if (warp == kProducerWarp) {
-        uint32_t ke = 0, qe = 0, le = 0;
+    if (warp == kKeyWarp) {
+        uint32_t ke = 0;
+        while (ok && walk.next(pc)) {
+            const WeightsGroup &g = pc.g;
+            each_pair(pc, row_tiles(g.n, a.group) - g.first_tile, [&](int pair, int, int) {
+                auto page_of = [&](int t) {   // this lane's page of a key tile
+                    const int page = (g.first_pair + pair) * (kPairKeys / kPageSize) + t * kPagesPerTile + lane;
+                    if (lane >= kPagesPerTile || page * kPageSize >= g.len) return 0;
+                    const int id = a.page_indices[g.list0 + page];   // inside the list: the schedule saw to that
+                    if (id >= 0 && id < a.num_pool_pages) return id;
+                    raise(a.status, PSA_ERR_BOUNDS);
+                    return a.num_pool_pages;                          // outside the map: zeros
+                };
+                const int id[2] = {page_of(0), page_of(1)};
+                for (int t = 0; t < 2; ++t, ++ke) {
+                    const int left = g.len - ((g.first_pair + pair) * kPairKeys + t * kTileKeys);
+                    const int pages = min(kPagesPerTile, max(0, (left + kPageSize - 1) / kPageSize));
+                    const int slot = ke % L::kKRing, use = ke / L::kKRing;
+                    if (use > 0 && !(ok = warp_wait(bar(L::kBarKEmpty + slot), (use - 1) & 1))) return false;
+                    const uint32_t full = bar(L::kBarKFull + slot), dst = sbase + L::kKOff + slot * L::kTileBytes;
+                    int ids[kPagesPerTile];
+#pragma unroll
+                    for (int p = 0; p < kPagesPerTile; ++p) ids[p] = __shfl_sync(0xffffffffu, t ? id[1] : id[0], p);
+                    if (elect_one()) {
+                        mbar_expect_tx(full, pages * kPageSize * D * 2);   // no page: the barrier completes at once
+#pragma unroll
+                        for (int p = 0; p < kPagesPerTile; ++p)
+                            if (p < pages)
+#pragma unroll
+                                for (int h = 0; h < L::kHalves; ++h)
+                                    tma_load_4d(dst + h * L::kHalfBytes + p * kPageSize * 128, &map_k, full, h * 64, 0, pc.head, ids[p]);
+                    }
+                    __syncwarp();
+                }
+                return true;
+            });
+        }
+    } else if (warp == kRowWarp) {
+        uint32_t qe = 0, le = 0;
         const int shift = __ffs(a.group) - 1;
         while (ok && walk.next(pc)) {
             const WeightsGroup &g = pc.g;
@@ -277,12 +315,13 @@ weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                 const int slot = qe % L::kQRing, use = qe / L::kQRing;
                 if (use > 0 && !(ok = warp_wait(bar(L::kBarQEmpty + slot), (use - 1) & 1))) return;
                 ++qe;
-                if (lane == 0) {
+                if (elect_one()) {
                     const uint32_t full = bar(L::kBarQFull + slot), dst = sbase + L::kQOff + slot * L::kTileBytes;
                     mbar_expect_tx(full, (few ? kFewRows : kRowTile) * D * 2);
                     for (int h = 0; h < L::kHalves; ++h)
                         tma_load_4d(dst + h * L::kHalfBytes, few ? &map_few : &map_q, full, h * 64, 0, pc.head, g.q0 + tile * (kRowTile / a.group));
                 }
+                __syncwarp();
                 // minus the rows' log-sum-exps, in log2; what does not exist or saw nothing gives no weight
                 const int ls = le % L::kLseRing, lu = le / L::kLseRing;
                 if (lu > 0 && !(ok = warp_wait(bar(L::kBarLEmpty + ls), (lu - 1) & 1))) return;
@@ -302,26 +341,7 @@ weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                 *reinterpret_cast<float4 *>(smem + L::kLseOff + ls * 512 + lane * 16) = v;
                 mbar_arrive(bar(L::kBarLFull + ls));
             };
-            each_pair(pc, count, [&](int pair, int r0, int r1) {
-                for (int t = 0; t < 2; ++t, ++ke) {
-                    const int key0 = (g.first_pair + pair) * kPairKeys + t * kTileKeys;
-                    const int pages = min(8, max(0, (g.len - key0 + kPageSize - 1) / kPageSize));
-                    int id = 0;
-                    if (lane < pages * L::kHalves) id = a.page_indices[g.list0 + key0 / kPageSize + lane / L::kHalves];
-                    const int slot = ke % L::kKRing, use = ke / L::kKRing;
-                    if (use > 0 && !(ok = warp_wait(bar(L::kBarKEmpty + slot), (use - 1) & 1))) return false;
-                    const uint32_t full = bar(L::kBarKFull + slot), dst = sbase + L::kKOff + slot * L::kTileBytes;
-                    if (lane == 0) mbar_expect_tx(full, pages * kPageSize * D * 2);   // no page: the barrier completes at once
-                    __syncwarp();
-                    if (lane < pages * L::kHalves) {
-                        const int p = lane / L::kHalves, h = lane % L::kHalves;
-                        if (id < 0 || id >= a.num_pool_pages) {
-                            raise(a.status, PSA_ERR_BOUNDS);
-                            id = a.num_pool_pages;   // outside the map: zeros
-                        }
-                        tma_load_4d(dst + h * L::kHalfBytes + p * kPageSize * 128, &map_k, full, h * 64, 0, pc.head, id);
-                    }
-                }
+            each_pair(pc, count, [&](int, int r0, int r1) {
                 if (tiles == 1) {
                     if (!have_q) load_q(0);
                     have_q = true;
@@ -406,17 +426,22 @@ weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                     const int row0 = (g.first_tile + r) * kRowTile;
                     const int lo = first_row - row0, hi = rows - row0;   // rows [lo, hi) give weight
                     const bool whole = __all_sync(0xffffffffu, lo <= 0 && hi >= 128);
-                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
-                    auto add = [&](const uint32_t *s, int c, int n, bool masked, bool exact) {
+                    float2 sum[2] = {{0.f, 0.f}, {0.f, 0.f}};
+                    auto add = [&](const uint32_t *s, int c, int n, bool masked) {
 #pragma unroll
                         for (int i = 0; i < n; i += 4) {
                             const float4 o = off[(c + i) / 4];
-                            const float ov[4] = {o.x, o.y, o.z, o.w};
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                float x = fmaf(__uint_as_float(s[i + k]), a.scale_log2, ov[k]);
-                                if (masked && (c + i + k < lo || c + i + k >= hi)) x = -INFINITY;
-                                sum[k] += !exact && k == 3 ? poly_exp2_fine<5>(x) : fast_exp2(x);
+                            for (int k = 0; k < 4; k += 2) {
+                                float2 x = fma2(make_float2(__uint_as_float(s[i + k]), __uint_as_float(s[i + k + 1])), make_float2(a.scale_log2, a.scale_log2),
+                                                k == 0 ? make_float2(o.x, o.y) : make_float2(o.z, o.w));
+                                if (masked) {
+                                    if (c + i + k < lo || c + i + k >= hi) x.x = -INFINITY;
+                                    if (c + i + k + 1 < lo || c + i + k + 1 >= hi) x.y = -INFINITY;
+                                }
+                                // a quarter by polynomial: the special-function unit, an exponential a score, is the bound
+                                const float2 e = !masked && (i / 2 + k / 2) % 4 == 3 ? poly_exp2_pair<5>(x) : make_float2(fast_exp2(x.x), fast_exp2(x.y));
+                                sum[k / 2] = add2(sum[k / 2], e);
                             }
                         }
                     };
@@ -424,7 +449,7 @@ weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                         uint32_t s[16];
                         tmem_ld16(s_addr, s);
                         tmem_wait_ld();
-                        add(s, 0, 16, true, true);
+                        add(s, 0, 16, true);
                     } else {
                         uint32_t s[2][32];
                         tmem_ld32(s_addr, s[0]);
@@ -432,8 +457,8 @@ weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
 #pragma unroll
                         for (int c = 0; c < 4; ++c) {
                             if (c < 3) tmem_ld32(s_addr + (c + 1) * 32, s[(c + 1) & 1]);
-                            if (whole) add(s[c & 1], c * 32, 32, false, false);
-                            else add(s[c & 1], c * 32, 32, true, true);
+                            if (whole) add(s[c & 1], c * 32, 32, false);
+                            else add(s[c & 1], c * 32, 32, true);
                             tmem_wait_ld();
                         }
                     }
@@ -443,7 +468,7 @@ weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                         mbar_arrive(bar(L::kBarSFree + b));
                         if (tiles > 1) mbar_arrive(bar(L::kBarLEmpty + ls));
                     }
-                    total += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                    total += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
                 }
                 const bool cut = r0 > 0 || r1 < count;
                 if (cut) w.partial[size_t(2 * blockIdx.x + (r0 > 0 ? 0 : 1)) * kPairKeys + t * kTileKeys + key] = total;
@@ -461,7 +486,7 @@ weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     if (*abort_flag) {
         if (threadIdx.x == 0) raise(a.status, PSA_ERR_TIMEOUT);
         // let copies that were already issued land before the block's shared memory is released
-        if (warp == kProducerWarp && lane == 0) {
+        if (warp >= kKeyWarp && lane == 0) {
             const unsigned long long t0 = global_timer_ns();
             while (global_timer_ns() - t0 < 2000000ull) { }
         }
@@ -519,7 +544,7 @@ cudaError_t launch(const WeightsArgs &w, const CUtensorMap *maps, cudaStream_t s
         return cudaError_t(rc);
     weights_schedule_kernel<<<1, kScheduleThreads, 0, st>>>(w);
     cudaError_t e = cudaGetLastError();
-    if (e == cudaSuccess) e = launch_dependent(weights_kernel<D>, dim3(w.c.blocks), 320, WeightsSmem<D>::kTotal, st, maps[0], maps[1], maps[2], w);
+    if (e == cudaSuccess) e = launch_dependent(weights_kernel<D>, dim3(w.c.blocks), kWeightsThreads, WeightsSmem<D>::kTotal, st, maps[0], maps[1], maps[2], w);
     if (e == cudaSuccess && w.c.blocks > 1) e = launch_dependent(weights_merge_kernel, dim3(w.c.blocks - 1), kPairKeys, 0, st, w);
     return e;
 }
