@@ -137,7 +137,7 @@ __device__ __forceinline__ uint32_t ordered(float x)
 }
 
 template <bool kPlanned>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 2)
 evict_kernel(EvictArgs a)
 {
     __shared__ uint32_t shared_keys[kSharedKeys];
@@ -174,40 +174,42 @@ evict_kernel(EvictArgs a)
     uint32_t *keys = candidates <= kSharedKeys ? shared_keys : a.keys + e.list0;
     const int newest = int(threadIdx.x) < e.recent ? list[candidates + threadIdx.x] : 0;
 
-    // ---- weights: `abreast` lanes a page
+    // ---- weights: a warp takes runs of kRun pages, a lane knows one's id and in the end its key; all lanes read a page
+    constexpr int kRun = 16, kAhead = 4;
     const int vectors = a.cells / 4;
-    const int abreast = vectors >= 32 ? 32 : vectors >= 16 ? 16 : vectors >= 8 ? 8 : 4;
-    const int sub = lane / abreast, mine = lane % abreast, at_once = 32 / abreast;
-    constexpr int kAhead = 8;
-    for (int c0 = warp * at_once * kAhead; c0 < candidates; c0 += kWarps * at_once * kAhead) {
-        float top[kAhead];
-        int page[kAhead];
+    for (int c0 = warp * kRun; c0 < candidates; c0 += kWarps * kRun) {
+        const int c = c0 + lane;
+        int page = lane < kRun && c < candidates ? list[c] : -1;
+        if (lane < kRun && c < candidates && (page < 0 || page >= a.num_pool_pages)) {
+            raise(a.status, PSA_ERR_BOUNDS);
+            page = -1;                            // weighs less than any other
+        }
+        uint32_t key = 0;
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const int c = c0 + i * at_once + sub;
-            top[i] = -INFINITY;
-            page[i] = c < candidates ? list[c] : 0;
-            if (page[i] < 0 || page[i] >= a.num_pool_pages) {
-                raise(a.status, PSA_ERR_BOUNDS);
-                page[i] = -1;                     // weighs less than any other
+        for (int r = 0; r < kRun; r += kAhead) {
+            float top[kAhead];
+            int at[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                top[i] = -INFINITY;
+                at[i] = __shfl_sync(0xffffffffu, page, r + i);
             }
-            if (c >= candidates) page[i] = -1;
-        }
-        for (int v = mine; v < vectors; v += abreast) {
-            float4 x[kAhead];
+            for (int v = lane; v < vectors; v += 32) {
+                float4 x[kAhead];
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i)
-                if (page[i] >= 0) x[i] = __ldcs(reinterpret_cast<const float4 *>(a.weights + size_t(page[i]) * a.cells) + v);
+                for (int i = 0; i < kAhead; ++i)
+                    if (at[i] >= 0) x[i] = __ldcs(reinterpret_cast<const float4 *>(a.weights + size_t(at[i]) * a.cells) + v);
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i)
-                if (page[i] >= 0) top[i] = fmaxf(top[i], fmaxf(fmaxf(x[i].x, x[i].y), fmaxf(x[i].z, x[i].w)));
-        }
+                for (int i = 0; i < kAhead; ++i)
+                    if (at[i] >= 0) top[i] = fmaxf(top[i], fmaxf(fmaxf(x[i].x, x[i].y), fmaxf(x[i].z, x[i].w)));
+            }
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            for (int d = abreast / 2; d; d >>= 1) top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], d));
-            const int c = c0 + i * at_once + sub;
-            if (mine == 0 && c < candidates) keys[c] = page[i] < 0 ? 0u : ordered(top[i] + 0.f);   // + 0: -0 weighs as much as 0
+            for (int i = 0; i < kAhead; ++i) {
+                const uint32_t k = __reduce_max_sync(0xffffffffu, ordered(top[i] + 0.f));   // + 0: -0 weighs as much as 0
+                if (lane == r + i && page >= 0) key = k;
+            }
         }
+        if (lane < kRun && c < candidates) keys[c] = key;
     }
 
     // ---- the key of the lightest candidate that stays, from its highest byte down
