@@ -107,10 +107,10 @@ __device__ __forceinline__ ChunkGroup chunk_group(const ChunkSample &c, int i, i
     return g;
 }
 
-// Cost of a piece in quarters of a key tile of two row tiles.  A single row tile's key tile costs three: half the arithmetic, but as many
-// bytes.  kPieceCost: loading Q, the first tiles' way, the epilogue.
-constexpr int kPieceCost = 4;
-constexpr int kLeastCost = 12;    // a share is not made smaller than this
+// Cost of a piece in quarters of a key tile of two row tiles (2.1 us).  A single row tile's key tile costs three: half the arithmetic, but as
+// many bytes.  kPieceCost: loading Q, the first tiles' way and the epilogue, measured at 4 to 5 us a piece.
+constexpr int kPieceCost = 8;
+constexpr int kLeastCost = 14;    // a share is not made smaller than this
 constexpr int kWholeTiles = 6;    // key tiles of samples that are not worth cutting
 __device__ __forceinline__ int chunk_tiles(int keys) { return (keys + 127) >> 7; }
 __device__ __forceinline__ int chunk_weight(const ChunkGroup &g, int group) { return g.n_tok * group > 128 ? 4 : 3; }
