@@ -10,8 +10,8 @@
 // Work units are (KV head, sample, key pair, row tile); a share is a run of them, as in chunk.h.  A pair's rows may be cut between shares:
 // each then leaves 256 partial sums, which weights_merge_kernel adds in order.
 //
-// 11 warps: 0-3 and 4-7 take the first and second key tile of a pair (thread = key), 8 is the MMA issuer and owner of the tensor memory, 9 and
-// 10 bring in K and the rows with their log-sum-exps.  Two score buffers of 128 columns for each key tile.  Every wait is bounded.
+// 19 warps: 0-15 sum (thread = key), a warpgroup for each of a pair's two key tiles and score buffers; 16 is the MMA issuer and owner of the
+// tensor memory, 17 and 18 bring in K and the rows with their log-sum-exps.  Two score buffers of 128 columns for each key tile.  Every wait is bounded.
 #include <algorithm>
 
 #include "chunk.h"
@@ -21,7 +21,7 @@
 namespace psa {
 namespace {
 
-constexpr int kWeightsThreads = 11 * 32, kPagesPerTile = 128 / kPageSize;
+constexpr int kWeightsThreads = 19 * 32, kPagesPerTile = 128 / kPageSize;
 constexpr int kPairKeys = 256, kTileKeys = 128, kRowTile = 128, kFewRows = 16;
 constexpr int kPairCost = 4, kRowCost = 2, kLeastShare = 8;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -207,16 +207,17 @@ struct WeightsSmem {
     static constexpr int kHalfBytes = 128 * 128;
     static constexpr int kTileBytes = kHalves * kHalfBytes;
     static constexpr int kKRing = D == 128 ? 4 : 8, kQRing = D == 128 ? 3 : 6;   // tiles; K comes in pairs
-    static constexpr int kLseRing = 4;
+    static constexpr int kLseRing = 3;
     static constexpr int kBarKFull = 0, kBarKEmpty = kBarKFull + kKRing, kBarQFull = kBarKEmpty + kKRing, kBarQEmpty = kBarQFull + kQRing,
                          kBarLFull = kBarQEmpty + kQRing, kBarLEmpty = kBarLFull + kLseRing, kBarS = kBarLEmpty + kLseRing, kBarSFree = kBarS + 4,
-                         kBarDrain = kBarSFree + 4, kNumBars = kBarDrain + 1;
+                         kBarPassed = kBarSFree + 4, kBarTaken = kBarPassed + 2, kBarDrain = kBarTaken + 2, kNumBars = kBarDrain + 1;
     static constexpr int kTmemPtrOff = 8 * kNumBars, kAbortOff = kTmemPtrOff + 4;
-    static constexpr int kLseOff = 1024;
-    static constexpr int kQOff = kLseOff + kLseRing * 512;
+    static constexpr int kPassOff = 512;                         // a sum for every key of a pair
+    static constexpr int kLseOff = kPassOff + 1024;
+    static constexpr int kQOff = 3072;
     static constexpr int kKOff = kQOff + kQRing * kTileBytes;
     static constexpr int kTotal = kKOff + kKRing * kTileBytes;
-    static_assert(kAbortOff + 4 <= kLseOff && kQOff % 1024 == 0 && kTotal <= 227 * 1024, "shared memory plan");
+    static_assert(kAbortOff + 4 <= kPassOff && kLseOff + kLseRing * 512 <= kQOff && kTotal <= 227 * 1024, "shared memory plan");
 };
 
 template <int D>
@@ -225,7 +226,7 @@ weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                const WeightsArgs w)
 {
     using L = WeightsSmem<D>;
-    constexpr int kMmaWarp = 8, kKeyWarp = 9, kRowWarp = 10, kKSteps = D / 16;
+    constexpr int kMmaWarp = 16, kKeyWarp = 17, kRowWarp = 18, kKSteps = D / 16;
     const ChunkArgs &a = w.c;
     extern __shared__ __align__(1024) unsigned char smem[];
     const uint32_t sbase = smem_u32(smem);
@@ -243,8 +244,8 @@ weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     if (threadIdx.x == 0) {
         *abort_flag = 0;
         for (int i = 0; i < L::kNumBars; ++i) {
-            // a log-sum-exp slot is filled by 32 lanes and read by 8 warps, a score buffer is read by 4
-            const int count = i >= L::kBarLFull && i < L::kBarLEmpty ? 32 : i >= L::kBarLEmpty && i < L::kBarS ? 8 : i >= L::kBarSFree && i < L::kBarDrain ? 4 : 1;
+            // a log-sum-exp slot is filled by 32 lanes and let go by 16 warps; a score buffer, a passed sum are four warps'
+            const int count = i >= L::kBarLFull && i < L::kBarLEmpty ? 32 : i >= L::kBarLEmpty && i < L::kBarS ? 16 : i >= L::kBarSFree && i < L::kBarDrain ? 4 : 1;
             mbar_init(bar(i), count);
         }
         fence_barrier_init();
@@ -311,7 +312,15 @@ weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             const int tiles = row_tiles(g.n, a.group), count = tiles - g.first_tile;
             const bool few = g.n * a.group <= kFewRows;
             bool have_q = false;
-            auto load_q = [&](int tile) {
+            // four rows' log-sum-exps a lane; the next tile's are asked for before they are needed, or their way would be the pace of it all
+            auto ask = [&](int tile, float (&x)[4]) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = tile * kRowTile + lane * 4 + i;
+                    x[i] = r < g.n * a.group ? w.lse[size_t(g.q0 + (r >> shift)) * a.num_q_heads + pc.head * a.group + (r & (a.group - 1))] : -INFINITY;
+                }
+            };
+            auto load_q = [&](int tile, const float (&x)[4]) {
                 const int slot = qe % L::kQRing, use = qe / L::kQRing;
                 if (use > 0 && !(ok = warp_wait(bar(L::kBarQEmpty + slot), (use - 1) & 1))) return;
                 ++qe;
@@ -322,31 +331,30 @@ weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                         tma_load_4d(dst + h * L::kHalfBytes, few ? &map_few : &map_q, full, h * 64, 0, pc.head, g.q0 + tile * (kRowTile / a.group));
                 }
                 __syncwarp();
-                // minus the rows' log-sum-exps, in log2; what does not exist or saw nothing gives no weight
                 const int ls = le % L::kLseRing, lu = le / L::kLseRing;
                 if (lu > 0 && !(ok = warp_wait(bar(L::kBarLEmpty + ls), (lu - 1) & 1))) return;
                 ++le;
-                float4 v;
-                float *pv = reinterpret_cast<float *>(&v);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int r = tile * kRowTile + lane * 4 + i;
-                    float off = -INFINITY;
-                    if (r < g.n * a.group) {
-                        const float x = w.lse[size_t(g.q0 + (r >> shift)) * a.num_q_heads + pc.head * a.group + (r & (a.group - 1))];
-                        off = x == -INFINITY ? -INFINITY : -x * kLog2e;
-                    }
-                    pv[i] = off;
-                }
-                *reinterpret_cast<float4 *>(smem + L::kLseOff + ls * 512 + lane * 16) = v;
+                // minus the log-sum-exps, in log2; what does not exist or saw nothing gives no weight
+                auto off = [](float v) { return v == -INFINITY ? -INFINITY : -v * kLog2e; };
+                *reinterpret_cast<float4 *>(smem + L::kLseOff + ls * 512 + lane * 16) = make_float4(off(x[0]), off(x[1]), off(x[2]), off(x[3]));
                 mbar_arrive(bar(L::kBarLFull + ls));
             };
             each_pair(pc, count, [&](int, int r0, int r1) {
+                float x[2][4];
                 if (tiles == 1) {
-                    if (!have_q) load_q(0);
+                    if (!have_q) {
+                        ask(0, x[0]);
+                        load_q(0, x[0]);
+                    }
                     have_q = true;
-                } else {
-                    for (int r = r0; ok && r < r1; ++r) load_q(g.first_tile + r);
+                    return ok;
+                }
+                ask(g.first_tile + r0, x[0]);
+                for (int r = r0; ok && r < r1; r += 2) {
+                    if (r + 1 < r1) ask(g.first_tile + r + 1, x[1]);
+                    load_q(g.first_tile + r, x[0]);
+                    if (r + 2 < r1) ask(g.first_tile + r + 2, x[0]);
+                    if (ok && r + 1 < r1) load_q(g.first_tile + r + 1, x[1]);
                 }
                 return ok;
             });
@@ -398,9 +406,15 @@ weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             }
         }
     } else {
-        const int t = warp >> 2, key = (warp & 3) * 32 + lane;       // key tile of the pair, key inside it
-        const uint32_t lane_addr = uint32_t((warp & 3) * 32) << 16;
-        uint32_t se = 0, le = 0;
+        // Four warpgroups: key tile t of the pair, score buffer b.  Row tiles go to the buffers in turns, and with them to the warpgroups.
+        const int t = (warp >> 2) & 1, b = warp >> 3, key = (warp & 3) * 32 + lane;
+        const uint32_t s_addr = tmem_base + (uint32_t((warp & 3) * 32) << 16) + uint32_t(2 * t + b) * 128;
+        float *const passed = reinterpret_cast<float *>(smem + L::kPassOff) + t * 128 + key;   // buffer 1's sum for buffer 0's warpgroup
+        auto warp_arrive = [&](uint32_t x) {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(x);
+        };
+        uint32_t se = 0, le = 0, passes = 0;
         while (ok && walk.next(pc)) {
             const WeightsGroup &g = pc.g;
             const int tiles = row_tiles(g.n, a.group), count = tiles - g.first_tile;
@@ -410,6 +424,7 @@ weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             each_pair(pc, count, [&](int pair, int r0, int r1) {
                 const int pos = (g.first_pair + pair) * kPairKeys + t * kTileKeys + key;
                 const int first_row = max(0, min(pos - g.pos0, g.n)) * a.group, rows = g.n * a.group;   // below 2^28
+                const bool alone = r1 - r0 == 1, first_mine = int(se & 1) == b;   // one row tile is one warpgroup's
                 float total = 0.f;
                 for (int r = r0; r < r1; ++r, ++se) {
                     if (tiles > 1 || !have_q) {
@@ -418,64 +433,71 @@ weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                         ++le;
                         have_q = true;
                     }
-                    const int b = 2 * t + int(se & 1);
-                    if (!(ok = warp_wait(bar(L::kBarS + b), (se >> 1) & 1))) return false;
-                    tc_fence_after();
-                    const uint32_t s_addr = tmem_base + lane_addr + uint32_t(b) * 128;
-                    const float4 *off = reinterpret_cast<const float4 *>(smem + L::kLseOff + ls * 512);
-                    const int row0 = (g.first_tile + r) * kRowTile;
-                    const int lo = first_row - row0, hi = rows - row0;   // rows [lo, hi) give weight
-                    const bool whole = __all_sync(0xffffffffu, lo <= 0 && hi >= 128);
-                    float2 sum[2] = {{0.f, 0.f}, {0.f, 0.f}};
-                    auto add = [&](const uint32_t *s, int c, int n, bool masked) {
+                    if (int(se & 1) == b) {
+                        if (!(ok = warp_wait(bar(L::kBarS + 2 * t + b), (se >> 1) & 1))) return false;
+                        tc_fence_after();
+                        const float4 *off = reinterpret_cast<const float4 *>(smem + L::kLseOff + ls * 512);
+                        const int row0 = (g.first_tile + r) * kRowTile;
+                        const int lo = first_row - row0, hi = rows - row0;   // rows [lo, hi) give weight
+                        const bool whole = __all_sync(0xffffffffu, lo <= 0 && hi >= 128);
+                        float2 sum[2] = {{0.f, 0.f}, {0.f, 0.f}};
+                        auto add = [&](const uint32_t (&s)[16], int c, bool masked) {
 #pragma unroll
-                        for (int i = 0; i < n; i += 4) {
-                            const float4 o = off[(c + i) / 4];
+                            for (int i = 0; i < 16; i += 4) {
+                                const float4 o = off[(c + i) / 4];
 #pragma unroll
-                            for (int k = 0; k < 4; k += 2) {
-                                float2 x = fma2(make_float2(__uint_as_float(s[i + k]), __uint_as_float(s[i + k + 1])), make_float2(a.scale_log2, a.scale_log2),
-                                                k == 0 ? make_float2(o.x, o.y) : make_float2(o.z, o.w));
-                                if (masked) {
-                                    if (c + i + k < lo || c + i + k >= hi) x.x = -INFINITY;
-                                    if (c + i + k + 1 < lo || c + i + k + 1 >= hi) x.y = -INFINITY;
+                                for (int k = 0; k < 4; k += 2) {
+                                    float2 x = fma2(make_float2(__uint_as_float(s[i + k]), __uint_as_float(s[i + k + 1])), make_float2(a.scale_log2, a.scale_log2),
+                                                    k == 0 ? make_float2(o.x, o.y) : make_float2(o.z, o.w));
+                                    if (masked) {
+                                        if (c + i + k < lo || c + i + k >= hi) x.x = -INFINITY;
+                                        if (c + i + k + 1 < lo || c + i + k + 1 >= hi) x.y = -INFINITY;
+                                    }
+                                    // a quarter by polynomial: the special-function unit, an exponential a score, is the bound
+                                    const float2 e = !masked && (i / 2 + k / 2) % 4 == 3 ? poly_exp2_pair<5>(x) : make_float2(fast_exp2(x.x), fast_exp2(x.y));
+                                    sum[k / 2] = add2(sum[k / 2], e);
                                 }
-                                // a quarter by polynomial: the special-function unit, an exponential a score, is the bound
-                                const float2 e = !masked && (i / 2 + k / 2) % 4 == 3 ? poly_exp2_pair<5>(x) : make_float2(fast_exp2(x.x), fast_exp2(x.y));
-                                sum[k / 2] = add2(sum[k / 2], e);
+                            }
+                        };
+                        uint32_t s[2][16];
+                        tmem_ld16(s_addr, s[0]);
+                        tmem_wait_ld();
+                        if (few) {
+                            add(s[0], 0, true);
+                        } else {
+#pragma unroll
+                            for (int c = 0; c < 8; ++c) {
+                                if (c < 7) tmem_ld16(s_addr + (c + 1) * 16, s[(c + 1) & 1]);
+                                if (whole) add(s[c & 1], c * 16, false);
+                                else add(s[c & 1], c * 16, true);
+                                tmem_wait_ld();
                             }
                         }
-                    };
-                    if (few) {
-                        uint32_t s[16];
-                        tmem_ld16(s_addr, s);
-                        tmem_wait_ld();
-                        add(s, 0, 16, true);
-                    } else {
-                        uint32_t s[2][32];
-                        tmem_ld32(s_addr, s[0]);
-                        tmem_wait_ld();
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            if (c < 3) tmem_ld32(s_addr + (c + 1) * 32, s[(c + 1) & 1]);
-                            if (whole) add(s[c & 1], c * 32, 32, false);
-                            else add(s[c & 1], c * 32, 32, true);
-                            tmem_wait_ld();
-                        }
+                        tc_fence_before();
+                        warp_arrive(bar(L::kBarSFree + 2 * t + b));
+                        total += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
                     }
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) {
-                        mbar_arrive(bar(L::kBarSFree + b));
-                        if (tiles > 1) mbar_arrive(bar(L::kBarLEmpty + ls));
-                    }
-                    total += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+                    if (tiles > 1) warp_arrive(bar(L::kBarLEmpty + ls));
+                }
+                if (alone ? !first_mine : b == 1) {
+                    if (alone) return true;
+                    if (passes > 0 && !(ok = warp_wait(bar(L::kBarTaken + t), (passes - 1) & 1))) return false;
+                    ++passes;
+                    *passed = total;
+                    warp_arrive(bar(L::kBarPassed + t));
+                    return true;
+                }
+                if (!alone) {
+                    if (!(ok = warp_wait(bar(L::kBarPassed + t), passes++ & 1))) return false;
+                    total += *passed;
+                    warp_arrive(bar(L::kBarTaken + t));
                 }
                 const bool cut = r0 > 0 || r1 < count;
                 if (cut) w.partial[size_t(2 * blockIdx.x + (r0 > 0 ? 0 : 1)) * kPairKeys + t * kTileKeys + key] = total;
                 else finish(w, g, pc.head, pos, total);
                 return true;
             });
-            if (ok && tiles == 1 && have_q && lane == 0) mbar_arrive(bar(L::kBarLEmpty + ls));
+            if (ok && tiles == 1 && have_q) warp_arrive(bar(L::kBarLEmpty + ls));
         }
         if (!ok) *abort_flag = 1;
     }
