@@ -10,8 +10,8 @@
 // Work units are (KV head, sample, key pair, row tile); a share is a run of them, as in chunk.h.  A pair's rows may be cut between shares:
 // each then leaves 256 partial sums, which weights_merge_kernel adds in order.
 //
-// 19 warps: 0-15 sum (thread = key), a warpgroup for each of a pair's two key tiles and score buffers; 16 is the MMA issuer and owner of the
-// tensor memory, 17 and 18 bring in K and the rows with their log-sum-exps.  Two score buffers of 128 columns for each key tile.  Every wait is bounded.
+// 20 warps: 0-15 sum (thread = key), a warpgroup for each of a pair's two key tiles and score buffers; 16 is the MMA issuer and owner of the
+// tensor memory, 17 brings in the rows with their log-sum-exps, 18 and 19 the key tiles.  Two score buffers of 128 columns for each key tile.  Every wait is bounded.
 #include <algorithm>
 
 #include "chunk.h"
@@ -21,7 +21,7 @@
 namespace psa {
 namespace {
 
-constexpr int kWeightsThreads = 19 * 32, kPagesPerTile = 128 / kPageSize;
+constexpr int kWeightsThreads = 20 * 32, kPagesPerTile = 128 / kPageSize;
 constexpr int kPairKeys = 256, kTileKeys = 128, kRowTile = 128, kFewRows = 16;
 constexpr int kPairCost = 4, kRowCost = 2, kLeastShare = 8;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -226,7 +226,7 @@ weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                const WeightsArgs w)
 {
     using L = WeightsSmem<D>;
-    constexpr int kMmaWarp = 16, kKeyWarp = 17, kRowWarp = 18, kKSteps = D / 16;
+    constexpr int kMmaWarp = 16, kRowWarp = 17, kKeyWarp = 18, kKSteps = D / 16;
     const ChunkArgs &a = w.c;
     extern __shared__ __align__(1024) unsigned char smem[];
     const uint32_t sbase = smem_u32(smem);
@@ -267,40 +267,39 @@ weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
 
     // The order of things, which every role follows: for each pair of a piece its K tiles, then its row tiles one by one.  A sample with
     // one row tile has it loaded once for all pairs of a piece.
-    if (warp == kKeyWarp) {
-        uint32_t ke = 0;
+    if (warp >= kKeyWarp) {
+        const int t = warp - kKeyWarp;      // key tile of the pairs
+        uint32_t ke = t;
         while (ok && walk.next(pc)) {
             const WeightsGroup &g = pc.g;
             each_pair(pc, row_tiles(g.n, a.group) - g.first_tile, [&](int pair, int, int) {
-                auto page_of = [&](int t) {   // this lane's page of a key tile
-                    const int page = (g.first_pair + pair) * (kPairKeys / kPageSize) + t * kPagesPerTile + lane;
-                    if (lane >= kPagesPerTile || page * kPageSize >= g.len) return 0;
-                    const int id = a.page_indices[g.list0 + page];   // inside the list: the schedule saw to that
-                    if (id >= 0 && id < a.num_pool_pages) return id;
-                    raise(a.status, PSA_ERR_BOUNDS);
-                    return a.num_pool_pages;                          // outside the map: zeros
-                };
-                const int id[2] = {page_of(0), page_of(1)};
-                for (int t = 0; t < 2; ++t, ++ke) {
-                    const int left = g.len - ((g.first_pair + pair) * kPairKeys + t * kTileKeys);
-                    const int pages = min(kPagesPerTile, max(0, (left + kPageSize - 1) / kPageSize));
-                    const int slot = ke % L::kKRing, use = ke / L::kKRing;
-                    if (use > 0 && !(ok = warp_wait(bar(L::kBarKEmpty + slot), (use - 1) & 1))) return false;
-                    const uint32_t full = bar(L::kBarKFull + slot), dst = sbase + L::kKOff + slot * L::kTileBytes;
-                    int ids[kPagesPerTile];
-#pragma unroll
-                    for (int p = 0; p < kPagesPerTile; ++p) ids[p] = __shfl_sync(0xffffffffu, t ? id[1] : id[0], p);
-                    if (elect_one()) {
-                        mbar_expect_tx(full, pages * kPageSize * D * 2);   // no page: the barrier completes at once
-#pragma unroll
-                        for (int p = 0; p < kPagesPerTile; ++p)
-                            if (p < pages)
-#pragma unroll
-                                for (int h = 0; h < L::kHalves; ++h)
-                                    tma_load_4d(dst + h * L::kHalfBytes + p * kPageSize * 128, &map_k, full, h * 64, 0, pc.head, ids[p]);
+                const int key0 = (g.first_pair + pair) * kPairKeys + t * kTileKeys;
+                const int pages = min(kPagesPerTile, max(0, (g.len - key0 + kPageSize - 1) / kPageSize));
+                int id = 0;
+                if (lane < pages) {
+                    id = a.page_indices[g.list0 + key0 / kPageSize + lane];   // inside the list: the schedule saw to that
+                    if (id < 0 || id >= a.num_pool_pages) {
+                        raise(a.status, PSA_ERR_BOUNDS);
+                        id = a.num_pool_pages;                                // outside the map: zeros
                     }
-                    __syncwarp();
                 }
+                const int slot = ke % L::kKRing, use = ke / L::kKRing;
+                ke += 2;
+                if (use > 0 && !(ok = warp_wait(bar(L::kBarKEmpty + slot), (use - 1) & 1))) return false;
+                const uint32_t full = bar(L::kBarKFull + slot), dst = sbase + L::kKOff + slot * L::kTileBytes;
+                int ids[kPagesPerTile];
+#pragma unroll
+                for (int p = 0; p < kPagesPerTile; ++p) ids[p] = __shfl_sync(0xffffffffu, id, p);
+                if (elect_one()) {
+                    mbar_expect_tx(full, pages * kPageSize * D * 2);   // no page: the barrier completes at once
+#pragma unroll
+                    for (int p = 0; p < kPagesPerTile; ++p)
+                        if (p < pages)
+#pragma unroll
+                            for (int h = 0; h < L::kHalves; ++h)
+                                tma_load_4d(dst + h * L::kHalfBytes + p * kPageSize * 128, &map_k, full, h * 64, 0, pc.head, ids[p]);
+                }
+                __syncwarp();
                 return true;
             });
         }
@@ -508,7 +507,7 @@ weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     if (*abort_flag) {
         if (threadIdx.x == 0) raise(a.status, PSA_ERR_TIMEOUT);
         // let copies that were already issued land before the block's shared memory is released
-        if (warp >= kKeyWarp && lane == 0) {
+        if (warp >= kRowWarp && lane == 0) {
             const unsigned long long t0 = global_timer_ns();
             while (global_timer_ns() - t0 < 2000000ull) { }
         }
