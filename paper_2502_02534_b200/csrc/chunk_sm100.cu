@@ -32,7 +32,7 @@ namespace {
 
 constexpr int kTileKeys = 128;
 constexpr int kRowTile = 128;
-constexpr int kChunkThreads = 11 * 32;
+constexpr int kChunkThreads = 12 * 32;
 constexpr int kPagesPerTile = kTileKeys / kPageSize;
 constexpr float kThreshold = 8.f;                      // log2 units
 constexpr float kHalfSumLimit = 64.f * 256.f * 1.01f;  // 64 exponentials of at most 2^8
@@ -196,7 +196,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
              const ChunkArgs a)
 {
     using L = ChunkSmem<D>;
-    constexpr int kMmaWarp = 8, kProducerWarp = 9, kProducers = 2;
+    constexpr int kMmaWarp = 8, kProducerWarp = 9, kProducers = 3;
     constexpr int kKSteps = D / 16;
     constexpr uint32_t kIdescQK = make_idesc(kTileKeys, false), kIdescPV = make_idesc(D, true);
     constexpr uint32_t kColO = 256;                    // S[t] at 128 t, O[t] at 256 + t D
@@ -218,7 +218,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
 
     if (threadIdx.x == 0) {
         *abort_flag = 0;
-        for (int i = 0; i < L::kNumBars; ++i) mbar_init(bar(i), i >= L::kBarFull && i < L::kBarEmpty ? kProducers : i >= L::kBarP && i < L::kBarHalf ? 128 : i == L::kBarMet ? 256 : 1);
+        for (int i = 0; i < L::kNumBars; ++i) mbar_init(bar(i), i >= L::kBarP && i < L::kBarHalf ? 128 : i == L::kBarMet ? 256 : 1);
         fence_barrier_init();
     }
     if (warp == kMmaWarp) {
@@ -237,7 +237,10 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
     ChunkPiece pc;
 
     if (warp >= kProducerWarp) {
-        // ------------------------------------------------------------ TMA producers: each takes every other page of a tile
+        // ------------------------------------------------------------ TMA producers, which take the elements of the ring in turns: a box is one
+        // page's 2 KB, and a single warp issues them too slowly for HBM.  Elements are freed in the order in which they are filled, so a
+        // slot's earlier uses are over when a warp's last element was let in: parities cannot be those of an older phase, although a warp
+        // sees only its own elements.
         const int part = warp - kProducerWarp;
         uint32_t e = 0, q_uses[2] = {0, 0}, q_sel = 0;
         bool ok = true;
@@ -247,17 +250,18 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
             const bool two = pc.g.n_tok * a.group > kRowTile;
             auto page_of = [&](int m) {   // this lane's page of element m
                 const int page = (pc.t0 + travel(m, n, two).tile) * kPagesPerTile + lane;
-                if (lane >= kPagesPerTile || page * kPageSize >= pc.g.keys) return 0;
+                if (m >= 2 * n || lane >= kPagesPerTile || page * kPageSize >= pc.g.keys) return 0;
                 const int id = a.page_indices[pc.g.list0 + page];   // inside the list: the schedule saw to that
                 if (id >= 0 && id < a.num_pool_pages) return id;
                 raise(a.status, PSA_ERR_BOUNDS);
                 return a.num_pool_pages;                              // outside the map: zeros
             };
-            int id = page_of(0);
-            for (int m = 0; ok && m < 2 * n; ++m, ++e) {
+            int m = (part + kProducers - int(e % kProducers)) % kProducers;
+            int id = page_of(m);
+            for (; ok && m < 2 * n; m += kProducers) {
                 const Travel tr = travel(m, n, two);
-                const int next = m + 1 < 2 * n ? page_of(m + 1) : 0;
-                const int slot = e % L::kRing, use = e / L::kRing;
+                const int next = page_of(m + kProducers);
+                const int slot = (e + m) % L::kRing, use = (e + m) / L::kRing;
                 if (use > 0 && !(ok = warp_wait(bar(L::kBarEmpty + slot), (use - 1) & 1))) break;
                 const int left = pc.g.keys - (pc.t0 + tr.tile) * kTileKeys;
                 const int pages = min(kPagesPerTile, (left + kPageSize - 1) / kPageSize);
@@ -266,33 +270,36 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
 #pragma unroll
                 for (int p = 0; p < kPagesPerTile; ++p) ids[p] = __shfl_sync(0xffffffffu, id, p);
                 if (elect_one()) {
-                    mbar_expect_tx(full, (pages + kProducers - 1 - part) / kProducers * kPageSize * D * 2);
+                    mbar_expect_tx(full, pages * kPageSize * D * 2);
                     const CUtensorMap *map = tr.is_v ? &map_v : &map_k;
 #pragma unroll
                     for (int p = 0; p < kPagesPerTile; ++p)
-                        if (p < pages && p % kProducers == part)
+                        if (p < pages)
 #pragma unroll
                             for (int h = 0; h < L::kHalves; ++h)
                                 tma_load_4d(dst + h * L::kHalfBytes + p * kPageSize * 128, map, full, h * 64, 0, pc.head, ids[p]);
                 }
                 __syncwarp();
                 id = next;
-                if (m == 0 && part == 0) {   // Q behind the first K tile
-                    const int tiles = two ? 2 : 1;
-                    for (int t = 0; ok && t < tiles; ++t) {
-                        const int b = two ? t : int(q_sel);
-                        if (q_uses[b] > 0 && !(ok = warp_wait(bar(L::kBarQEmpty + b), (q_uses[b] - 1) & 1))) break;
-                        ++q_uses[b];
-                        if (elect_one()) {
-                            mbar_expect_tx(bar(L::kBarQFull + b), L::kTileBytes);
-                            for (int h = 0; h < L::kHalves; ++h)
-                                tma_load_4d(sbase + L::kQOff + b * L::kTileBytes + h * L::kHalfBytes, &map_q, bar(L::kBarQFull + b), h * 64, 0, pc.head,
-                                            pc.g.q0 + t * (kRowTile / a.group));
-                        }
-                        __syncwarp();
+                for (int t = 0; ok && m == 0 && t < (two ? 2 : 1); ++t) {   // Q behind the first K tile
+                    const int b = two ? t : int(q_sel);
+                    if (q_uses[b] > 0 && !(ok = warp_wait(bar(L::kBarQEmpty + b), (q_uses[b] - 1) & 1))) break;
+                    if (elect_one()) {
+                        mbar_expect_tx(bar(L::kBarQFull + b), L::kTileBytes);
+                        for (int h = 0; h < L::kHalves; ++h)
+                            tma_load_4d(sbase + L::kQOff + b * L::kTileBytes + h * L::kHalfBytes, &map_q, bar(L::kBarQFull + b), h * 64, 0, pc.head,
+                                        pc.g.q0 + t * (kRowTile / a.group));
                     }
-                    if (!two) q_sel ^= 1;
+                    __syncwarp();
                 }
+            }
+            e += 2 * n;
+            if (two) {
+                ++q_uses[0];
+                ++q_uses[1];
+            } else {
+                ++q_uses[q_sel];
+                q_sel ^= 1;
             }
         }
     } else if (warp == kMmaWarp) {
