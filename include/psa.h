@@ -568,8 +568,8 @@ psa_status_t psa_attend_paged(const void *q, const int64_t q_strides[2], const i
  * left as they are, so a page from the free stack needs no clearing.
  *   lse            [num_tokens, Hq] f32: what psa_attend_paged or psa_decode returned for the rows (over all they attended to, a shared
  *                  prompt included); rows with -inf give no weight.
- * Scores and sums are fp32, added in a fixed order.  The other arguments, limits and status reports are those of psa_attend_paged; a
- * sample's list must not hold a page twice.  Enqueues three kernels.
+ * Scores and sums are fp32, added in a fixed order.  The other arguments, limits and status reports are those of psa_attend_paged.  A page
+ * must stand in one sample's list only, and once (psa_attend_paged does not mind shared pages).  Enqueues three kernels.
  */
 size_t psa_accumulate_weights_scratch_bytes(int64_t num_tokens, int32_t num_samples);
 psa_status_t psa_accumulate_weights(const void *q, const int64_t q_strides[2], const int32_t *q_indptr, int64_t num_tokens, int32_t num_samples,

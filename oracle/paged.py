@@ -83,7 +83,8 @@ def evict(weights, page_indptr, page_indices, kv_lens, budgets, recent, free_pag
         older = list(range(held - newest))
         heavy = [np.nanmax(np.where(np.isnan(weights[p]), -np.inf, weights[p])) + 0.0 for p in mine]
         stay = sorted(sorted(older, key=lambda i: (-heavy[i], i))[:budget - newest]) + list(range(held - newest, held))
-        stack += [mine[i] for i in older if i not in set(stay)]
+        keep = set(stay)
+        stack += [mine[i] for i in older if i not in keep]
         out[page_indptr[s]:page_indptr[s] + held] = [mine[i] for i in stay] + [-1] * (held - budget)
         lens[s] = int(length) - PAGE * (held - budget)
     free = np.array(free_pages)

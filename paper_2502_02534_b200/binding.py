@@ -801,10 +801,10 @@ def evict_pages(weights, page_indptr, page_indices, kv_lens, budgets, recent, fr
 
 def token_logprobs(logits, tokens, top=0, *, temperature=None, logprobs=None, entropy=None, top_ids=None, top_logprobs=None, stream=None):
     """psa_token_logprobs on torch CUDA tensors: of every row of logits [R, V] (bf16 or f32; rows may be padded) at temperature [R] f32 the
-    log probability of tokens [R] int32, the entropy, and the `top` likeliest tokens with theirs.  Returns (logprobs [R], entropy [R],
-    top_ids [R, top] int32, top_logprobs [R, top])."""
+    log probability of tokens [R] int32 (None: left out), the entropy, and the `top` likeliest tokens with theirs.  Returns (logprobs [R],
+    entropy [R], top_ids [R, top] int32, top_logprobs [R, top])."""
     rows = logits.shape[0]
-    if logprobs is None:
+    if logprobs is None and tokens is not None:
         logprobs = _new((rows,), logits, stream, "float32")
     if entropy is None:
         entropy = _new((rows,), logits, stream, "float32")

@@ -7,14 +7,25 @@
 // Three launches.  chunk_schedule_kernel cuts every sample's new tokens into GROUPS of up to 256 rows (256 / G tokens x G query heads) and
 // writes their running costs (key tiles).  chunk_kernel is persistent: block i takes the i-th equal share of all (KV head, group, key
 // tile) units, in order, so every SM has the same work whatever the lengths are, and a group is cut only where a share ends.  What is cut
-// leaves partial results, two slots a block at most, which chunk_merge_kernel joins; groups that were not cut are finished in place.
+// leaves partial results, two slots a block at most, which chunk_merge_kernel joins; groups that were not cut are finished in place.  A
+// batch of few short samples has a block for every group instead, uncut.
 //
-// chunk_kernel, 10 warps: 0-3 and 4-7 softmax warpgroups (streams 0 and 1), 8 TMA producer, 9 MMA issuer (one lane) and owner of the
-// tensor memory.  Key tiles of 128 keys arrive page by page (one TMA box of 16 tokens x 64 channels each) in a ring; S = Q K^T goes to
+// chunk_kernel, 12 warps: 0-3 and 4-7 softmax warpgroups (streams 0 and 1), 8 MMA issuer (one lane) and owner of the tensor memory, 9-11 TMA
+// producers.  Key tiles of 128 keys arrive page by page (one TMA box of 16 tokens x 64 channels each) in a ring; S = Q K^T goes to
 // tensor memory, a warpgroup (thread = row) turns it into P (bf16, over S), O += P V.  More than 128 rows: each stream has a row tile and
-// both read every key tile.  Up to 128 rows: the streams take alternate key tiles of the one row tile, each with an accumulator of its
-// own, joined at the end.  P is handed over in halves of 64 keys, so that the first half's products run under the second half's
-// exponentials.  The reference maximum moves only when a half's exponents exceed it by 2^8 (which its sum tells).
+// both read every key tile, so a byte of K and V serves 256 rows.  Up to 128 rows: the streams take alternate key tiles of the one row tile,
+// each with an accumulator of its own, joined at the end.  P is handed over in halves of 64 keys, so that the first half's products run
+// under the second half's exponentials.  The reference maximum moves only when a half's exponents exceed it by 2^8 (which its sum tells).
+//
+// What bounds it.  4096 new tokens over 12288 (64 / 8 heads of 128): 1.82 ms = 1.06 PFLOP/s, 0.76 of the measured sustained bf16 rate; the
+// tensor cores are busy 54 % of the cycles, the way from one score tile to the next (commit, softmax, hand-over, P V, Q K^T) is the rest:
+// with the arithmetic taken out the barriers alone take 1.2 ms, the products alone 1.26, the tiles' way from L2 1.1.  64 x 4 tokens over
+// U[0,4096] (549 MB): 125 us, 4.4 TB/s; the loads alone take 105.
+// Tried and not kept (the long case, then the 64 x 4 tokens, against 1832 and 133 at that time): two warpgroups a stream, each half of the
+// keys, with a shared reference 1875 / 139; the same with a score buffer for each half (64-key products) 2096 / 151; an issuer for each
+// stream 2221 / 138; a watcher thread that folds the tiles' arrival into P's barrier 1860 / 134; K by TMA and V by cp.async 2236 / 182; all by
+// cp.async 2411 / 166; prefetches into L2 6 tiles ahead 2204 / 162; one arrival a warp on the P barriers, polling without suspension: no
+// change; a share of polynomial exponentials from 0 to 3/8: within 2 %.
 //
 // What does not exist is never used: products stop at the last page, rows of V behind the last key are zeroed in shared memory (they may
 // hold anything), scores behind a row's last key become -inf.  Page ids outside the pool read as zeros (TMA bounds) and raise

@@ -3,7 +3,7 @@
 // with the rows' finished log-sum-exp as given; the new tokens' own weights start from zero.
 //
 // The transpose of attention's scores: S^T = K Q^T puts a key on every tensor-memory lane and the rows along its columns, so a thread sums
-// its own key's weights in a register -- no exchange, no atomics, one order of summation whatever the scheduling.  Two key tiles (a PAIR
+// its own key's weights in a register -- no atomics, one order of summation whatever the scheduling.  Two key tiles (a PAIR
 // of 128 keys each) stay in shared memory while the rows' tiles stream past both.  One exponential per key and row is the bound for
 // chunks; for a few rows (a decode step) it is reading K once.
 //
@@ -11,7 +11,12 @@
 // each then leaves 256 partial sums, which weights_merge_kernel adds in order.
 //
 // 20 warps: 0-15 sum (thread = key), a warpgroup for each of a pair's two key tiles and score buffers; 16 is the MMA issuer and owner of the
-// tensor memory, 17 brings in the rows with their log-sum-exps, 18 and 19 the key tiles.  Two score buffers of 128 columns for each key tile.  Every wait is bounded.
+// tensor memory, 17 brings in the rows with their log-sum-exps, 18 and 19 the key tiles.  Two score buffers of 128 columns for each key tile.
+// Every wait is bounded.
+//
+// 64 samples x 1 token over U[0,4096], 8 heads (268 MB of K): 57 us, 4.7 TB/s (one TMA warp for both key tiles 66); launch, schedule and merge are
+// 10 of them.  2048 tokens over 8192, 32 / 8 heads, 604 M exponentials: 203 us, the special-function units busy half of the time (134 us at their
+// rate; two warpgroups 229 us, log-sum-exps loaded when needed 216).  Row tiles of 64 with four buffers 252, an issuer for each key tile 202.
 #include <algorithm>
 
 #include "chunk.h"

@@ -108,3 +108,5 @@ def test_parts_left_out_and_captured():
         assert all(torch.equal(a, b) for a, b in zip(out, got))
     alone = token_logprobs(logits, dev(tokens))
     assert torch.equal(alone[0], got[0]) and torch.equal(alone[1], got[1]) and alone[2].shape == (4, 0)
+    untold = token_logprobs(logits, None, 6)
+    assert untold[0] is None and torch.equal(untold[1], got[1]) and torch.equal(untold[2], got[2])
