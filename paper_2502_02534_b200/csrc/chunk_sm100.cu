@@ -208,6 +208,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
 {
     using L = ChunkSmem<D>;
     constexpr int kMmaWarp = 8, kProducerWarp = 9, kProducers = 3;
+    static_assert(kProducers <= L::kRing, "a slot's use before the last is over when a warp waits for it");
     constexpr int kKSteps = D / 16;
     constexpr uint32_t kIdescQK = make_idesc(kTileKeys, false), kIdescPV = make_idesc(D, true);
     constexpr uint32_t kColO = 256;                    // S[t] at 128 t, O[t] at 256 + t D
@@ -249,9 +250,9 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
 
     if (warp >= kProducerWarp) {
         // ------------------------------------------------------------ TMA producers, which take the elements of the ring in turns: a box is one
-        // page's 2 KB, and a single warp issues them too slowly for HBM.  Elements are freed in the order in which they are filled, so a
-        // slot's earlier uses are over when a warp's last element was let in: parities cannot be those of an older phase, although a warp
-        // sees only its own elements.
+        // page's 2 KB, and a single warp issues them too slowly for HBM.  Elements are freed in the order in which they are filled, so the use
+        // of a slot before its last one was over when the warp's previous element, kProducers earlier, was let in: a parity cannot be that of
+        // an older phase, although a warp sees only its own elements.
         const int part = warp - kProducerWarp;
         uint32_t e = 0, q_uses[2] = {0, 0}, q_sel = 0;
         bool ok = true;
@@ -267,6 +268,24 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
                 raise(a.status, PSA_ERR_BOUNDS);
                 return a.num_pool_pages;                              // outside the map: zeros
             };
+            // Q is the first warp's, always: the others may be ahead of it by more pieces than there are buffers.  It goes before the warp's first
+            // element where two buffers take turns, and behind it where the buffers are waited for until the last piece's scores are made.
+            bool q_due = part == 0;
+            auto load_q = [&]() {
+                for (int t = 0; ok && q_due && t < (two ? 2 : 1); ++t) {
+                    const int b = two ? t : int(q_sel);
+                    if (q_uses[b] > 0 && !(ok = warp_wait(bar(L::kBarQEmpty + b), (q_uses[b] - 1) & 1))) break;
+                    if (elect_one()) {
+                        mbar_expect_tx(bar(L::kBarQFull + b), L::kTileBytes);
+                        for (int h = 0; h < L::kHalves; ++h)
+                            tma_load_4d(sbase + L::kQOff + b * L::kTileBytes + h * L::kHalfBytes, &map_q, bar(L::kBarQFull + b), h * 64, 0, pc.head,
+                                        pc.g.q0 + t * (kRowTile / a.group));
+                    }
+                    __syncwarp();
+                }
+                q_due = false;
+            };
+            if (!two) load_q();
             int m = (part + kProducers - int(e % kProducers)) % kProducers;
             int id = page_of(m);
             for (; ok && m < 2 * n; m += kProducers) {
@@ -292,18 +311,9 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
                 }
                 __syncwarp();
                 id = next;
-                for (int t = 0; ok && m == 0 && t < (two ? 2 : 1); ++t) {   // Q behind the first K tile
-                    const int b = two ? t : int(q_sel);
-                    if (q_uses[b] > 0 && !(ok = warp_wait(bar(L::kBarQEmpty + b), (q_uses[b] - 1) & 1))) break;
-                    if (elect_one()) {
-                        mbar_expect_tx(bar(L::kBarQFull + b), L::kTileBytes);
-                        for (int h = 0; h < L::kHalves; ++h)
-                            tma_load_4d(sbase + L::kQOff + b * L::kTileBytes + h * L::kHalfBytes, &map_q, bar(L::kBarQFull + b), h * 64, 0, pc.head,
-                                        pc.g.q0 + t * (kRowTile / a.group));
-                    }
-                    __syncwarp();
-                }
+                load_q();
             }
+            load_q();   // a piece may have no element of this warp's
             e += 2 * n;
             if (two) {
                 ++q_uses[0];

@@ -61,6 +61,22 @@ def test_single_lengths(samples):
         check(*run(c), reference(c), True)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("most_new", [4, 60])
+def test_many_pieces_of_one_tile(D, most_new):
+    """A share of a dozen pieces of one key tile each, with up to 128 rows or more: copies run several pieces ahead of the products."""
+    import torch
+    rng = np.random.default_rng(most_new)
+    samples = [(int(rng.integers(0, 60)), int(rng.integers(1, most_new + 1))) for _ in range(600)]
+    c = case(D, 24, 3, samples, seed=21)
+    d = on_device(c)
+    out, lse = run(c, d, out=torch.empty(c["q"].shape, device="cuda"))
+    check(out, lse, reference(c), False)
+    for _ in range(10):
+        again, again_lse = run(c, d, out=torch.empty_like(out))
+        assert torch.equal(again, out) and torch.equal(again_lse, lse)
+
+
 def test_tokens_that_see_nothing():
     """Lengths below the number of new tokens: the first rows stand before the cache begins."""
     c = case(64, 4, 2, [(40, 9), (3, 6)], seed=3)
