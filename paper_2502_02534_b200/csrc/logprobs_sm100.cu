@@ -201,7 +201,7 @@ logprobs_kernel(const LogprobArgs a)
     const int v0 = min(a.vocab, part * a.segment), v1 = min(a.vocab, v0 + a.segment);
     float t = a.temperature ? a.temperature[row] : 1.f;
     if (!(t > 0.f && t < INFINITY)) t = 1.f;
-    const float inv_t = 1.f / t, c = inv_t * kLog2e;
+    const float inv_t = fminf(1.f / t, 1e38f), c = inv_t * kLog2e;   // finite: 0 / T is 0 for the smallest T too
     float asked = -INFINITY;                       // the given token's logit; its way is long, so it starts here
     if (part == 0 && threadIdx.x == 0 && a.logprobs) {
         const int token = a.tokens[row];

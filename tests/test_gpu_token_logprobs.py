@@ -110,3 +110,21 @@ def test_parts_left_out_and_captured():
     assert torch.equal(alone[0], got[0]) and torch.equal(alone[1], got[1]) and alone[2].shape == (4, 0)
     untold = token_logprobs(logits, None, 6)
     assert untold[0] is None and torch.equal(untold[1], got[1]) and torch.equal(untold[2], got[2])
+
+
+def test_extreme_temperatures():
+    """The largest logits share everything at the smallest positive temperature, and all tokens are equally likely at the largest."""
+    import torch
+    from paper_2502_02534_b200 import token_logprobs
+    x = torch.linspace(-9.0, 9.0, 1003, device="cuda").repeat(4, 1)
+    x[:, 17] = x[:, -1]
+    logits = torch.zeros(4, 1008, device="cuda")[:, :1003]
+    logits.copy_(x)
+    temperature = torch.tensor([1e-45, 1e-39, 1e-30, 3e38], device="cuda")
+    tokens = torch.tensor([17, 1002, 1002, 500], dtype=torch.int32, device="cuda")
+    lp, entropy, ids, top = token_logprobs(logits, tokens, 3, temperature=temperature)
+    want = np.log([0.5, 0.5, 0.5, 1 / 1003])
+    assert np.all(np.abs(lp.cpu().numpy() - want) <= 1e-6 * np.abs(want))
+    assert np.all(np.abs(entropy.cpu().numpy() + want) <= 1e-6 * np.abs(want))
+    assert ids[:, :2].tolist() == [[17, 1002]] * 4
+    assert np.all(top[:3, 2].cpu().numpy() < -1e20) and not torch.isnan(top).any()
