@@ -783,6 +783,7 @@ psa_status_t chunk_check(const ChunkArgs &a, const void *q, const int64_t q_stri
     if (head_dim != 64 && head_dim != 128) return set_last_error(PSA_ERR_UNSUPPORTED, "head_dim must be 64 or 128");
     if (a.num_q_heads % a.num_kv_heads || (a.group != 1 && a.group != 2 && a.group != 4 && a.group != 8))
         return set_last_error(PSA_ERR_UNSUPPORTED, "num_q_heads / num_kv_heads must be 1, 2, 4 or 8");
+    if (a.num_q_heads > 65536) return set_last_error(PSA_ERR_UNSUPPORTED, "at most 2^16 query heads");
     if (a.num_samples > (1 << 20)) return set_last_error(PSA_ERR_UNSUPPORTED, "at most 2^20 samples per call");
     if (a.num_tokens > (1 << 24)) return set_last_error(PSA_ERR_UNSUPPORTED, "at most 2^24 new tokens per call");
     if (a.num_pool_pages > kMostChunkPages || a.num_entries > kMostChunkEntries)
