@@ -45,7 +45,7 @@ struct ChunkArgs {
     int32_t blocks, max_groups, slot_rows;
     ChunkHeader *header;
     ChunkGroup *groups;
-    float *partial_lse, *partial_o;    // [2 * blocks, slot_rows] log2, [2 * blocks, slot_rows, D] normalised
+    float *partial_lse, *partial_o;    // [2 * blocks, slot_rows] log2, [2 * blocks, D / 4, slot_rows, 4] normalised
 };
 
 #ifdef __CUDACC__
@@ -222,28 +222,6 @@ __device__ __forceinline__ Joined join(float a2, float b2)
     if (top == -INFINITY) return {0.f, 0.f, -INFINITY};
     const float wa = exp2f(a2 - top), wb = exp2f(b2 - top), sum = wa + wb;
     return {wa / sum, wb / sum, top + log2f(sum)};
-}
-// 16 columns of the earlier result
-__device__ __forceinline__ void add_prior(const ChunkArgs &a, size_t at, float w, float (&v)[16])
-{
-    if (a.prior_f32) {
-#pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-            const float4 p = *reinterpret_cast<const float4 *>(static_cast<const float *>(a.prior_out) + at + i);
-            v[i] = fmaf(w, p.x, v[i]); v[i + 1] = fmaf(w, p.y, v[i + 1]); v[i + 2] = fmaf(w, p.z, v[i + 2]); v[i + 3] = fmaf(w, p.w, v[i + 3]);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 16; i += 8) {
-            const uint4 p = *reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(a.prior_out) + at + i);
-            const uint32_t u[4] = {p.x, p.y, p.z, p.w};
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                v[i + 2 * k] = fmaf(w, __uint_as_float(u[k] << 16), v[i + 2 * k]);
-                v[i + 2 * k + 1] = fmaf(w, __uint_as_float(u[k] & 0xffff0000u), v[i + 2 * k + 1]);
-            }
-        }
-    }
 }
 #endif
 

@@ -183,22 +183,63 @@ __device__ __forceinline__ Travel travel(int m, int n, bool two)
 // place of V tile i in that order
 __device__ __forceinline__ int v_place(int i, int n, bool two) { return two ? 2 * i + 1 : i < n - 1 ? 2 * i + 2 : 2 * n - 1; }
 
-// 16 columns of one row to global memory
-__device__ __forceinline__ void store_f32(float *to, const float (&v)[16])
+// 8 columns of one row to global memory
+__device__ __forceinline__ void store_row(const ChunkArgs &a, size_t at, const float (&v)[8])
 {
+    if (a.out_f32) {
+        float *to = static_cast<float *>(a.out) + at;
+        *reinterpret_cast<float4 *>(to) = make_float4(v[0], v[1], v[2], v[3]);
+        *reinterpret_cast<float4 *>(to + 4) = make_float4(v[4], v[5], v[6], v[7]);
+        return;
+    }
+    uint32_t w[4];
 #pragma unroll
-    for (int i = 0; i < 16; i += 4) *reinterpret_cast<float4 *>(to + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-}
-__device__ __forceinline__ void store_bf16(__nv_bfloat16 *to, const float (&v)[16])
-{
-    uint32_t w[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < 4; ++k) {
         const __nv_bfloat162 p = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
         w[k] = reinterpret_cast<const uint32_t &>(p);
     }
-    reinterpret_cast<uint4 *>(to)[0] = make_uint4(w[0], w[1], w[2], w[3]);
-    reinterpret_cast<uint4 *>(to)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(a.out) + at) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+// Lane i of four has row i, v[j] its columns 8 j ..: afterwards v[j] is row j's columns 8 i ...
+__device__ __forceinline__ void quad_transpose(float (&v)[4][8], int quad)
+{
+#pragma unroll
+    for (int bit = 1; bit < 4; bit <<= 1)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (!(j & bit))
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const bool upper = quad & bit;
+                    const float got = __shfl_xor_sync(0xffffffffu, upper ? v[j][k] : v[j | bit][k], bit);
+                    v[j][k] = upper ? got : v[j][k];
+                    v[j | bit][k] = upper ? v[j | bit][k] : got;
+                }
+}
+// 8 columns of the earlier result, on their way and added
+struct Earlier { uint4 w[2]; };
+__device__ __forceinline__ Earlier earlier_columns(const ChunkArgs &a, size_t at)
+{
+    if (a.prior_f32) {
+        const uint4 *from = reinterpret_cast<const uint4 *>(static_cast<const float *>(a.prior_out) + at);
+        return {from[0], from[1]};
+    }
+    return {*reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(a.prior_out) + at), {}};
+}
+__device__ __forceinline__ void add_earlier(const ChunkArgs &a, const Earlier &e, float w, float (&v)[8])
+{
+    if (w == 0.f) return;                          // not 0 x NaN
+    const uint32_t u[8] = {e.w[0].x, e.w[0].y, e.w[0].z, e.w[0].w, e.w[1].x, e.w[1].y, e.w[1].z, e.w[1].w};
+    if (a.prior_f32) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = fmaf(w, __uint_as_float(u[k]), v[k]);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            v[2 * k] = fmaf(w, __uint_as_float(u[k] << 16), v[2 * k]);
+            v[2 * k + 1] = fmaf(w, __uint_as_float(u[k] & 0xffff0000u), v[2 * k + 1]);
+        }
+    }
 }
 
 template <int D>
@@ -405,6 +446,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
         const uint32_t s_addr = tmem_base + lane_addr + uint32_t(t) * 128;
         const uint32_t o_base = tmem_base + lane_addr + kColO;
         float *exchange = reinterpret_cast<float *>(smem + L::kExchangeOff);   // [stream][m, l][row]
+        const int shift = __ffs(a.group) - 1;
         uint32_t e = 0, uses = 0, met = 0, done[2] = {0, 0};
         bool ok = true;
         while (ok && walk.next(pc)) {
@@ -414,8 +456,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
             const int in_group = (two ? t * kRowTile : 0) + row;
             const bool mine = in_group < rows;
             const bool active = __any_sync(0xffffffffu, mine);
-            const int token = in_group / a.group;
-            const int sees = mine ? max(0, min(pc.g.keys, pc.g.pos0 + token + 1)) : 0;   // keys the row sees
+            const int token = in_group >> shift;
+            const int sees = mine ? max(0, min(pc.g.keys, pc.g.pos0 + token + 1)) : pc.g.keys;   // keys the row sees
             const int my_uses = two ? n : (n - t + 1) / 2;
             const int tiles = (pc.g.keys + kTileKeys - 1) / kTileKeys;
             float m_ref = -INFINITY, l_sum = 0.f;
@@ -465,82 +507,102 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
                         to[i / 2] = __byte_perm(__float_as_uint(e.x), __float_as_uint(e.y), 0x7632);
                     }
                 };
-                auto half = [&](int h) -> bool {
-                    const int v = valid - 64 * h;
-                    uint32_t r[2][32];
-                    float total;
-                    tmem_ld32(s_addr + h * 64, r[0]);
-                    tmem_wait_ld();
-                    tmem_ld32(s_addr + h * 64 + 32, r[1]);
-                    bool redo = __any_sync(0xffffffffu, m_ref == -INFINITY && v > 0);   // nothing to exponentiate against yet
-                    if (!redo) {
-                        float2 sum[2] = {{0.f, 0.f}, {0.f, 0.f}};
-                        mask(v, r[0]);
-                        exponentials(r[0], p, sum);
-                        tmem_wait_ld();
-                        mask(v - 32, r[1]);
-                        exponentials(r[1], p + 16, sum);
-                        total = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
-                        redo = __any_sync(0xffffffffu, !(total <= kHalfSumLimit));
-                    }
-                    if (redo) {
-                        tmem_wait_ld();
-                        tmem_ld32(s_addr + h * 64, r[0]);
-                        tmem_ld32(s_addr + h * 64 + 32, r[1]);
-                        tmem_wait_ld();
-                        mask(v, r[0]);
-                        mask(v - 32, r[1]);
-                        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                        for (int i = 0; i < 64; ++i) mx[i & 3] = fmaxf(mx[i & 3], __uint_as_float(r[i / 32][i % 32]));
-                        const float top = a.scale_log2 * fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-                        const bool need = top > m_ref + kThreshold;
-                        if (__any_sync(0xffffffffu, need)) {
-                            const float alpha = need ? fast_exp2(m_ref - top) : 1.f;
-                            if (j > 0 || h == 1) {
-                                // O[t] is at rest: S of this unit was made behind the products before it; the first half's products of
-                                // this very unit are waited for
-                                if (h == 1) {
-                                    if (!warp_wait(bar(L::kBarHalf + t), uses & 1)) return false;
-                                    tc_fence_after();
-                                }
-#pragma unroll 1
-                                for (int c = 0; c < D / 32; ++c) {
-                                    tmem_ld32(o_base + t * D + c * 32, p);
-                                    tmem_wait_ld();
-#pragma unroll
-                                    for (int i = 0; i < 32; ++i) p[i] = __float_as_uint(__uint_as_float(p[i]) * alpha);
-                                    tmem_st32(o_base + t * D + c * 32, p);
-                                }
-                                tmem_wait_st();
-                            }
-                            l_sum *= alpha;
-                            if (need) m_ref = top;
-                        }
-                        float2 sum[2] = {{0.f, 0.f}, {0.f, 0.f}};
-                        exponentials(r[0], p, sum);
-                        exponentials(r[1], p + 16, sum);
-                        total = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
-                    }
+                auto hand_over = [&](int h, float total) {
                     tmem_st32(s_addr + h * 32, p);
                     l_sum += total;
                     tmem_wait_st();
                     tc_fence_before();
                     mbar_arrive(bar_p(t, h));
+                };
+                // The usual way: every score is seen and in range.  Else false, and nothing has happened.
+                auto plain = [&](int h) -> bool {
+                    uint32_t r[2][32];
+                    float2 sum[2] = {{0.f, 0.f}, {0.f, 0.f}};
+                    tmem_ld32(s_addr + h * 64, r[0]);
+                    tmem_wait_ld();
+                    tmem_ld32(s_addr + h * 64 + 32, r[1]);
+                    exponentials(r[0], p, sum);
+                    tmem_wait_ld();
+                    exponentials(r[1], p + 16, sum);
+                    const float total = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+                    if (__any_sync(0xffffffffu, !(total <= kHalfSumLimit))) return false;
+                    hand_over(h, total);
                     return true;
                 };
-                if (!(ok = half(0))) break;
-                if (!(ok = half(1))) break;
+                // Scores to be masked, or a reference to be moved.  There is one copy of this code, and it goes on to the second half: what
+                // the loop's code takes of the instruction cache is its speed (masks and both ways in both halves: the long case 1790 us, not 1665).
+                auto careful = [&](int h) -> bool {
+                    const int v = valid - 64 * h;
+                    uint32_t r[2][32];
+                    tmem_ld32(s_addr + h * 64, r[0]);
+                    tmem_ld32(s_addr + h * 64 + 32, r[1]);
+                    tmem_wait_ld();
+                    mask(v, r[0]);
+                    mask(v - 32, r[1]);
+                    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int i = 0; i < 64; ++i) mx[i & 3] = fmaxf(mx[i & 3], __uint_as_float(r[i / 32][i % 32]));
+                    const float top = a.scale_log2 * fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+                    const bool need = top > m_ref + kThreshold;
+                    if (__any_sync(0xffffffffu, need)) {
+                        const float alpha = need ? fast_exp2(m_ref - top) : 1.f;
+                        if (j > 0 || h == 1) {
+                            // O[t] is at rest: S of this unit was made behind the products before it; the first half's products of
+                            // this very unit are waited for
+                            if (h == 1) {
+                                if (!warp_wait(bar(L::kBarHalf + t), uses & 1)) return false;
+                                tc_fence_after();
+                            }
+#pragma unroll 1
+                            for (int c = 0; c < D / 32; ++c) {
+                                tmem_ld32(o_base + t * D + c * 32, p);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) p[i] = __float_as_uint(__uint_as_float(p[i]) * alpha);
+                                tmem_st32(o_base + t * D + c * 32, p);
+                            }
+                            tmem_wait_st();
+                        }
+                        l_sum *= alpha;
+                        if (need) m_ref = top;
+                    }
+                    float2 sum[2] = {{0.f, 0.f}, {0.f, 0.f}};
+                    exponentials(r[0], p, sum);
+                    exponentials(r[1], p + 16, sum);
+                    hand_over(h, (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y));
+                    return true;
+                };
+                int h = 0;
+                if (__all_sync(0xffffffffu, m_ref > -INFINITY && valid >= kTileKeys) && plain(0)) h = plain(1) ? 2 : 1;
+#pragma unroll 1
+                for (; ok && h < 2; ++h) ok = careful(h);
+                if (!ok) break;
             }
             if (!ok) break;
             e += 2 * n;
 
             // ---- epilogue
             l_sum *= kUnbias;
-            const size_t out_row = size_t(pc.g.q0 + token) * a.num_q_heads + pc.head * a.group + in_group % a.group;
+            auto out_row = [&](int r) { return size_t(pc.g.q0 + (r >> shift)) * a.num_q_heads + pc.head * a.group + (r & (a.group - 1)); };
             const size_t part_row = size_t(pc.slot) * a.slot_rows + in_group;
-            const bool joins = mine && !pc.split && a.prior_lse;
-            const float prior2 = joins ? a.prior_lse[out_row] * kLog2e : -INFINITY;
+            // this warpgroup's columns: all of its own row tile, or half of the shared one
+            const int c0 = two ? 0 : t * (D / 2), c1 = two ? D : (t + 1) * (D / 2);
+            // To memory four lanes go side by side: each has 8 of 32 columns of their four rows.  The earlier result comes that way, while the
+            // last products are waited for.
+            const int quad = lane & 3, quad_row = in_group - quad;
+            const bool joins = !pc.split && a.prior_lse;
+            const float prior2 = joins && mine ? a.prior_lse[out_row(in_group)] * kLog2e : -INFINITY;
+            size_t at[4];
+            Earlier earlier[4];
+            auto ask = [&](int c) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) earlier[k] = earlier_columns(a, at[k] + c);
+            };
+            if (active && !pc.split) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) at[k] = out_row(min(quad_row + k, rows - 1)) * D + quad * 8;
+                if (joins) ask(c0);
+            }
             const int streams = n == 0 ? 0 : two || n > 1 ? 2 : 1;
             if (two || n == 0) {
                 if (n > 0) {
@@ -570,8 +632,6 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
                 share[1] = total == 0.f ? 0.f : w1 / total;
                 lse2 = total == 0.f ? -INFINITY : top + log2f(total);
             }
-            // this warpgroup's columns: all of its own row tile, or half of the shared one
-            const int c0 = two ? 0 : t * (D / 2), c1 = two ? D : (t + 1) * (D / 2);
             float from_prior = 0.f;
             if (joins) {
                 const Joined jn = join(lse2, prior2);
@@ -580,28 +640,44 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
                 from_prior = jn.second;
                 lse2 = jn.lse2;
             }
-            for (int c = c0; active && c < c1; c += 16) {
-                __syncwarp();
-                float v[16];
+            float from[4];                         // the quad's rows'
 #pragma unroll
-                for (int i = 0; i < 16; ++i) v[i] = 0.f;
+            for (int k = 0; k < 4; ++k) from[k] = __shfl_sync(0xffffffffu, from_prior, (lane & ~3) + k);
+#pragma unroll 1
+            for (int c = c0; active && c < c1; c += 32) {
+                __syncwarp();
+                float v[4][8];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i / 8][i % 8] = 0.f;
+#pragma unroll 1
                 for (int i = 0; i < 2; ++i) {
                     if (n == 0 || (two ? i != t : i >= streams)) continue;
-                    uint32_t o[16];
-                    tmem_ld16(o_base + i * D + c, o);
+                    uint32_t o[32];
+                    tmem_ld32(o_base + i * D + c, o);
                     tmem_wait_ld();
-                    if (share[i] != 0.f)
+                    const float w = i ? share[1] : share[0];
+                    if (w != 0.f)
 #pragma unroll
-                        for (int k = 0; k < 16; ++k) v[k] = fmaf(__uint_as_float(o[k]), share[i], v[k]);
+                        for (int k = 0; k < 32; ++k) v[k / 8][k % 8] = fmaf(__uint_as_float(o[k]), w, v[k / 8][k % 8]);
                 }
-                if (!mine) continue;
                 if (pc.split) {
-                    store_f32(a.partial_o + part_row * D + c, v);
+                    // four columns of all rows stand together: whole lines, although a thread has a row
+                    if (mine)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            reinterpret_cast<float4 *>(a.partial_o)[(size_t(pc.slot) * (D / 4) + c / 4 + i) * a.slot_rows + in_group] =
+                                make_float4(v[i / 2][i % 2 * 4], v[i / 2][i % 2 * 4 + 1], v[i / 2][i % 2 * 4 + 2], v[i / 2][i % 2 * 4 + 3]);
                     continue;
                 }
-                if (from_prior != 0.f) add_prior(a, out_row * D + c, from_prior, v);
-                if (a.out_f32) store_f32(static_cast<float *>(a.out) + out_row * D + c, v);
-                else store_bf16(static_cast<__nv_bfloat16 *>(a.out) + out_row * D + c, v);
+                quad_transpose(v, quad);
+                if (joins) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) add_earlier(a, earlier[k], from[k], v[k]);
+                    if (c + 32 < c1) ask(c + 32);
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (quad_row + k < rows) store_row(a, at[k] + c, v[k]);
             }
             tc_fence_before();
             if (!two) {
@@ -612,7 +688,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
             }
             if (mine && (two || t == 0)) {
                 if (pc.split) a.partial_lse[part_row] = lse2;
-                else a.lse[out_row] = lse2 * kLn2;
+                else a.lse[out_row(in_group)] = lse2 * kLn2;
             }
         }
         if (!ok) *abort_flag = 1;
@@ -643,8 +719,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
 }
 
 // ------------------------------------------------------------------------------------------------------------- merge
-// Block (cut, slice): the group that the end of share `cut` falls into, if that is the first cut inside it; a warp per row.
-constexpr int kMergeWarps = 8;
+// Block (cut, slice): the group that the end of share `cut` falls into, if that is the first cut inside it; a warp for 8 rows.
+constexpr int kMergeWarps = 4;
 template <int D>
 __global__ void __launch_bounds__(kMergeWarps * 32)
 chunk_merge_kernel(const ChunkArgs a)
@@ -676,45 +752,64 @@ chunk_merge_kernel(const ChunkArgs a)
     }
     __syncthreads();
     const int pieces = last - cut + 1;
-    const int rows = g.n_tok * a.group;
-    constexpr int kPer = D / 32;
-    for (int r = blockIdx.y * kMergeWarps + warp; r < rows; r += gridDim.y * kMergeWarps) {
-        const size_t row = size_t(g.q0 + r / a.group) * a.num_q_heads + head * a.group + r % a.group;
+    const int rows = g.n_tok * a.group, shift = __ffs(a.group) - 1;
+    // a lane's part: a row, and four columns of every 16
+    constexpr int kSteps = D / 16;
+    const int quarter = lane >> 3;
+    for (int r0 = (blockIdx.y * kMergeWarps + warp) * 8; r0 < rows; r0 += gridDim.y * kMergeWarps * 8) {
+        const bool mine = r0 + (lane & 7) < rows;
+        const int r = min(r0 + (lane & 7), rows - 1);
+        const size_t row = size_t(g.q0 + (r >> shift)) * a.num_q_heads + head * a.group + (r & (a.group - 1));
         const float prior2 = a.prior_lse ? a.prior_lse[row] * kLog2e : -INFINITY;
-        float top = -INFINITY, sum = 0.f, acc[kPer];
+        // the earlier result's columns are asked for at once, like the pieces' log-sum-exps and columns: there is little else to wait for
+        uint4 earlier[kSteps];
+        if (a.prior_lse)
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) acc[i] = 0.f;
-        for (int b0 = 0; b0 < pieces; b0 += 32) {
-            // a lane's piece
-            const int slot = b0 + lane < pieces ? slots[b0 + lane] : -1;
-            const float lse2 = slot >= 0 ? a.partial_lse[size_t(slot) * a.slot_rows + r] : -INFINITY;
-            float most = lse2;
+            for (int j = 0; j < kSteps; ++j) {
+                const size_t at = row * D + (j * 4 + quarter) * 4;
+                if (a.prior_f32) {
+                    earlier[j] = *reinterpret_cast<const uint4 *>(static_cast<const float *>(a.prior_out) + at);
+                } else {
+                    const uint2 u = *reinterpret_cast<const uint2 *>(static_cast<const __nv_bfloat16 *>(a.prior_out) + at);
+                    earlier[j] = make_uint4(u.x << 16, u.x & 0xffff0000u, u.y << 16, u.y & 0xffff0000u);
+                }
+            }
+        float top = -INFINITY, sum = 0.f;
+        float acc[kSteps][4];
 #pragma unroll
-            for (int d = 16; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
-            const float next = fmaxf(top, most);
-            const float keep = top == -INFINITY ? 0.f : exp2f(top - next), w = lse2 == -INFINITY ? 0.f : exp2f(lse2 - next);
+        for (int j = 0; j < kSteps; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
+        constexpr int kAbreast = 4;
+        for (int i0 = 0; i0 < pieces; i0 += kAbreast) {
+            float lse2[kAbreast];
+            int slot[kAbreast];
+            float next = top;
+#pragma unroll
+            for (int i = 0; i < kAbreast; ++i) {
+                slot[i] = i0 + i < pieces ? slots[i0 + i] : -1;
+                lse2[i] = slot[i] >= 0 ? a.partial_lse[size_t(slot[i]) * a.slot_rows + r] : -INFINITY;
+            }
+#pragma unroll
+            for (int i = 0; i < kAbreast; ++i) next = fmaxf(next, lse2[i]);
+            const float keep = top == -INFINITY ? 0.f : exp2f(top - next);
             top = next;
             sum *= keep;
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) acc[i] *= keep;
-            const int here = min(32, pieces - b0);
-#pragma unroll 4
-            for (int i = 0; i < here; ++i) {
-                const int from_slot = __shfl_sync(0xffffffffu, slot, i);
-                const float from_w = __shfl_sync(0xffffffffu, w, i);
-                if (from_slot < 0 || from_w == 0.f) continue;
-                const float *from = a.partial_o + (size_t(from_slot) * a.slot_rows + r) * D + lane * kPer;
-                float o[kPer];
-                if constexpr (kPer == 4) {
-                    const float4 q = *reinterpret_cast<const float4 *>(from);
-                    o[0] = q.x; o[1] = q.y; o[2] = q.z; o[3] = q.w;
-                } else {
-                    const float2 q = *reinterpret_cast<const float2 *>(from);
-                    o[0] = q.x; o[1] = q.y;
-                }
-                sum += from_w;
+            for (int j = 0; j < kSteps; ++j) { acc[j][0] *= keep; acc[j][1] *= keep; acc[j][2] *= keep; acc[j][3] *= keep; }
 #pragma unroll
-                for (int k = 0; k < kPer; ++k) acc[k] = fmaf(from_w, o[k], acc[k]);
+            for (int i = 0; i < kAbreast; ++i) {
+                if (slot[i] < 0) continue;           // the same for all rows
+                const float4 *from = reinterpret_cast<const float4 *>(a.partial_o) + (size_t(slot[i]) * (D / 4) + quarter) * a.slot_rows + r;
+                float4 o[kSteps];
+#pragma unroll
+                for (int j = 0; j < kSteps; ++j) o[j] = from[size_t(4 * j) * a.slot_rows];
+                const float w = lse2[i] == -INFINITY ? 0.f : exp2f(lse2[i] - top);
+                if (w == 0.f) continue;
+                sum += w;
+#pragma unroll
+                for (int j = 0; j < kSteps; ++j) {
+                    acc[j][0] = fmaf(w, o[j].x, acc[j][0]); acc[j][1] = fmaf(w, o[j].y, acc[j][1]);
+                    acc[j][2] = fmaf(w, o[j].z, acc[j][2]); acc[j][3] = fmaf(w, o[j].w, acc[j][3]);
+                }
             }
         }
         float lse2 = sum == 0.f ? -INFINITY : top + log2f(sum);
@@ -725,21 +820,23 @@ chunk_merge_kernel(const ChunkArgs a)
             from_prior = jn.second;
             lse2 = jn.lse2;
         }
-        const size_t at = row * D + lane * kPer;
-        float v[kPer];
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            v[i] = acc[i] * share;
+        for (int j = 0; j < kSteps; ++j) {
+            const size_t at = row * D + (j * 4 + quarter) * 4;
+            float4 v = make_float4(acc[j][0] * share, acc[j][1] * share, acc[j][2] * share, acc[j][3] * share);
             if (from_prior != 0.f)
-                v[i] = fmaf(from_prior, a.prior_f32 ? static_cast<const float *>(a.prior_out)[at + i] : __bfloat162float(static_cast<const __nv_bfloat16 *>(a.prior_out)[at + i]), v[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < kPer; i += 2) {
-            if (a.out_f32) *reinterpret_cast<float2 *>(static_cast<float *>(a.out) + at + i) = make_float2(v[i], v[i + 1]);
-            else *reinterpret_cast<__nv_bfloat162 *>(static_cast<__nv_bfloat16 *>(a.out) + at + i) = __floats2bfloat162_rn(v[i], v[i + 1]);
+                v = make_float4(fmaf(from_prior, __uint_as_float(earlier[j].x), v.x), fmaf(from_prior, __uint_as_float(earlier[j].y), v.y),
+                                fmaf(from_prior, __uint_as_float(earlier[j].z), v.z), fmaf(from_prior, __uint_as_float(earlier[j].w), v.w));
+            if (!mine) continue;
+            if (a.out_f32) {
+                *reinterpret_cast<float4 *>(static_cast<float *>(a.out) + at) = v;
+            } else {
+                const __nv_bfloat162 x = __floats2bfloat162_rn(v.x, v.y), y = __floats2bfloat162_rn(v.z, v.w);
+                *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(a.out) + at) = make_uint2(reinterpret_cast<const uint32_t &>(x), reinterpret_cast<const uint32_t &>(y));
+            }
         }
         __syncwarp();   // lse may be prior_lse: every lane has read it
-        if (lane == 0) a.lse[row] = lse2 * kLn2;
+        if (quarter == 0 && mine) a.lse[row] = lse2 * kLn2;
     }
 }
 
@@ -752,7 +849,7 @@ cudaError_t launch(const ChunkArgs &a, const CUtensorMap &mq, const CUtensorMap 
     chunk_schedule_kernel<<<1, kScheduleThreads, 0, st>>>(a);
     cudaError_t e = cudaGetLastError();
     if (e == cudaSuccess) e = launch_dependent(chunk_kernel<D>, dim3(a.blocks), kChunkThreads, ChunkSmem<D>::kTotal, st, mq, mk, mv, a);
-    if (e == cudaSuccess && a.blocks > 1) e = launch_dependent(chunk_merge_kernel<D>, dim3(a.blocks - 1, (a.slot_rows + 15) / 16), kMergeWarps * 32, 0, st, a);
+    if (e == cudaSuccess && a.blocks > 1) e = launch_dependent(chunk_merge_kernel<D>, dim3(a.blocks - 1, (a.slot_rows + 8 * kMergeWarps - 1) / (8 * kMergeWarps)), kMergeWarps * 32, 0, st, a);
     return e;
 }
 
