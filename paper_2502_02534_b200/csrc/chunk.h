@@ -12,6 +12,7 @@ namespace psa {
 
 constexpr int kScheduleThreads = 256;
 constexpr int kGroupRows = 256;                              // rows of a group: two row tiles of 128
+constexpr int kKeptCums = 1024;                              // groups whose costs the schedule keeps in shared memory
 constexpr int kMostBlocks = 160;                             // persistent blocks, at most one per SM
 constexpr int kMostTokens = 1 << 30;                         // of one sample
 constexpr int64_t kMostChunkPages = int64_t(1) << 27, kMostChunkEntries = (int64_t(1) << 31) - 256;
@@ -29,6 +30,11 @@ struct ChunkGroup {
     int32_t list0, pad;    // where the sample's pages start in page_indices
 };
 static_assert(sizeof(ChunkGroup) == 32, "");
+// A block's share [x0, x1) of the cost of all heads, and the head and group that it starts in.
+struct ChunkStart {
+    long long x0, x1;
+    int32_t head, group;
+};
 
 struct ChunkArgs {
     int64_t num_tokens, num_entries;
@@ -44,6 +50,7 @@ struct ChunkArgs {
     // scratch
     int32_t blocks, max_groups, slot_rows;
     ChunkHeader *header;
+    ChunkStart *starts;    // [blocks]
     ChunkGroup *groups;
     float *partial_lse, *partial_o;    // [2 * blocks, slot_rows] log2, [2 * blocks, D / 4, slot_rows, 4] normalised
 };
@@ -79,16 +86,12 @@ struct ChunkSample { int q0, n, len, list0; };
 __device__ __forceinline__ ChunkSample chunk_sample(const ChunkArgs &a, int s)
 {
     const int tokens = int(a.num_tokens);
-    int b0 = s, b1 = s + 1;
-    if (a.q_indptr) {
-        const int r0 = a.q_indptr[s], r1 = a.q_indptr[s + 1];
-        b0 = min(max(r0, 0), tokens);
-        b1 = min(max(r1, b0), tokens);
-        if (b0 != r0 || b1 != r1) raise(a.status, PSA_ERR_BOUNDS);
-    }
-    if (b1 == b0) return {b0, 0, 0, 0};
+    const int r0 = a.q_indptr ? a.q_indptr[s] : s, r1 = a.q_indptr ? a.q_indptr[s + 1] : s + 1;
     const int l0 = a.page_indptr[s], l1 = a.page_indptr[s + 1];
     int len = a.kv_lens[s];
+    const int b0 = min(max(r0, 0), tokens), b1 = min(max(r1, b0), tokens);
+    if (b0 != r0 || b1 != r1) raise(a.status, PSA_ERR_BOUNDS);
+    if (b1 == b0) return {b0, 0, 0, 0};
     if (l0 < 0 || l1 < l0 || l1 > a.num_entries || len < 0 || len > kMostTokens || len > (long long)(l1 - l0) * kPageSize) {
         raise(a.status, PSA_ERR_BOUNDS);
         len = 0;
@@ -128,20 +131,25 @@ __device__ __forceinline__ int tile_at(const ChunkGroup &g, int group, long long
     const int tiles = chunk_tiles(g.keys), w = chunk_weight(g, group);
     return y >= (long long)tiles * w ? tiles : int(uint32_t(y) / uint32_t(w));
 }
-// the head and group that x lies in, searched by a whole warp
-template <class Group>
-__device__ __forceinline__ void locate(const Group *groups, const ChunkHeader &h, long long x, int lane, int *head, int *group)
+// Every block's share, by the block that made the groups; `cum(i)` is the cost before group i.
+template <class Cum>
+__device__ __forceinline__ void write_starts(const ChunkHeader &h, int heads, ChunkStart *starts, Cum cum)
 {
-    *head = int(x / h.per_head);
-    const long long y = x - *head * h.per_head;
-    int lo = 0, hi = h.groups;
-    while (hi - lo > 1) {
-        const int step = (hi - lo + 31) >> 5, at = lo + lane * step;
-        const unsigned below = __ballot_sync(0xffffffffu, at < hi && groups[at].cum <= y);
-        lo += (__popc(below) - 1) * step;
-        hi = min(hi, lo + step);
+    const long long total = h.per_head * heads;
+    for (int b = threadIdx.x; b < h.blocks; b += blockDim.x) {
+        ChunkStart s;
+        s.x0 = share_begin(total, b, h.blocks);
+        s.x1 = share_begin(total, b + 1, h.blocks);
+        s.head = int(s.x0 / h.per_head);
+        const long long y = s.x0 - s.head * h.per_head;
+        int lo = 0, hi = h.groups;                 // cum(lo) <= y < cum(hi)
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            (cum(mid) <= y ? lo : hi) = mid;
+        }
+        s.group = lo;
+        starts[b] = s;
     }
-    *group = lo;
 }
 
 struct ChunkPiece {
@@ -156,8 +164,9 @@ struct ChunkWalk {
     ChunkHeader h;
     long long x0 = 0, x1 = 0;
     int block, head, gi = 0;
-    __device__ __forceinline__ ChunkWalk(const ChunkArgs &args, int b, int lane) : a(args), h(*args.header), block(b)
+    __device__ __forceinline__ ChunkWalk(const ChunkArgs &args, int b) : a(args), h(*args.header), block(b)
     {
+        const ChunkStart s = args.starts[b];       // asked for together with the header
         head = a.num_kv_heads;
         if (block >= h.blocks || h.groups == 0) return;
         if (h.whole) {
@@ -165,10 +174,10 @@ struct ChunkWalk {
             gi = block % h.groups;
             return;
         }
-        const long long total = h.per_head * a.num_kv_heads;
-        x0 = share_begin(total, block, h.blocks);
-        x1 = share_begin(total, block + 1, h.blocks);
-        locate(a.groups, h, x0, lane, &head, &gi);
+        x0 = s.x0;
+        x1 = s.x1;
+        head = s.head;
+        gi = s.group;
     }
     __device__ __forceinline__ bool next(ChunkPiece &p)
     {

@@ -61,6 +61,8 @@ chunk_schedule_kernel(ChunkArgs a)
     constexpr int kWarps = kScheduleThreads / 32, kAlone = 4;   // groups that a thread goes through by itself
     __shared__ long long sum_cost[kWarps];
     __shared__ int sum_groups[kWarps], longest;
+    __shared__ long long cums[kKeptCums];
+    __shared__ ChunkHeader made;
     grid_release();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int per_group = kGroupRows / a.group;   // tokens
@@ -129,6 +131,7 @@ chunk_schedule_kernel(ChunkArgs a)
         __syncthreads();
         each(at, to, [&](int place, const ChunkGroup &g) {
             if (place < a.max_groups) a.groups[place] = g;
+            if (place < kKeptCums) cums[place] = g.cum;
         });
     }
     if (my_longest) atomicMax(&longest, my_longest);
@@ -149,8 +152,11 @@ chunk_schedule_kernel(ChunkArgs a)
             h.whole = 1;
             h.blocks = max(1, carry_groups * a.num_kv_heads);
         }
-        *a.header = h;
+        *a.header = made = h;
     }
+    __syncthreads();
+    if (made.groups > 0 && !made.whole)
+        write_starts(made, a.num_kv_heads, a.starts, [&](int i) { return made.groups <= kKeptCums ? cums[i] : a.groups[i].cum; });
 }
 
 // ------------------------------------------------------------------------------------------------------------- attention
@@ -286,7 +292,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
     grid_wait();
     grid_release();
 
-    ChunkWalk walk(a, blockIdx.x, lane);
+    ChunkWalk walk(a, blockIdx.x);
     ChunkPiece pc;
 
     if (warp >= kProducerWarp) {
@@ -731,22 +737,21 @@ chunk_merge_kernel(const ChunkArgs a)
     const ChunkHeader h = *a.header;
     const int cut = blockIdx.x;                 // between blocks cut and cut + 1
     if (cut + 1 >= h.blocks || h.groups == 0 || h.whole) return;
-    const long long total = h.per_head * a.num_kv_heads;
-    const long long x = share_begin(total, cut + 1, h.blocks);
-    int head, gi;
-    locate(a.groups, h, x, lane, &head, &gi);
+    const ChunkStart before = a.starts[cut], after = a.starts[cut + 1];
+    const int head = after.head;
+    const long long x = after.x0;
     if (head >= a.num_kv_heads) return;
-    const ChunkGroup g = a.groups[gi];
+    const ChunkGroup g = a.groups[after.group];
     const long long base = head * h.per_head + g.cum;
     const int tiles = chunk_tiles(g.keys), t_cut = tile_at(g, a.group, base, x);
     if (t_cut <= 0 || t_cut >= tiles) return;                                              // nothing is cut here
-    if (cut > 0 && tile_at(g, a.group, base, share_begin(total, cut, h.blocks)) > 0) return;   // an earlier cut's group
+    if (cut > 0 && tile_at(g, a.group, base, before.x0) > 0) return;   // an earlier cut's group
     // pieces: blocks cut, cut + 1, ... until the group ends
     __shared__ int last;
     if (threadIdx.x == 0) last = h.blocks - 1;
     __syncthreads();
     for (int b = cut + threadIdx.x; b < h.blocks; b += blockDim.x) {
-        const int t0 = tile_at(g, a.group, base, share_begin(total, b, h.blocks)), t1 = tile_at(g, a.group, base, share_begin(total, b + 1, h.blocks));
+        const int t0 = tile_at(g, a.group, base, a.starts[b].x0), t1 = tile_at(g, a.group, base, a.starts[b].x1);
         slots[b - cut] = t1 > t0 ? 2 * b + (t0 > 0 ? 0 : 1) : -1;
         if (t1 >= tiles) atomicMin(&last, b);
     }
@@ -865,6 +870,7 @@ size_t chunk_layout(ChunkArgs &a, void *scratch, int head_dim)
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t at = off; off = (off + bytes + 255) / 256 * 256; return static_cast<unsigned char *>(scratch) + at; };
     a.header = reinterpret_cast<ChunkHeader *>(take(sizeof(ChunkHeader)));
+    a.starts = reinterpret_cast<ChunkStart *>(take(sizeof(ChunkStart) * size_t(a.blocks)));
     a.groups = reinterpret_cast<ChunkGroup *>(take(sizeof(ChunkGroup) * size_t(a.max_groups)));
     if (head_dim > 0) {
         a.partial_lse = reinterpret_cast<float *>(take(4 * size_t(2 * a.blocks) * a.slot_rows));

@@ -77,6 +77,8 @@ weights_schedule_kernel(WeightsArgs w)
 {
     __shared__ long long sum_cost[kScheduleThreads / 32];
     __shared__ int sum_groups[kScheduleThreads / 32];
+    __shared__ long long cums[kKeptCums];
+    __shared__ ChunkHeader made;
     grid_release();
     const ChunkArgs &a = w.c;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -114,6 +116,7 @@ weights_schedule_kernel(WeightsArgs w)
         auto put = [&](int first, int pairs, int first_tile) {
             g.cum = at; g.first_pair = first; g.pairs = pairs; g.first_tile = first_tile;
             if (to < a.max_groups) w.groups[to] = g;
+            if (to < kKeptCums) cums[to] = at;
             ++to;
             at += (long long)pairs * pair_cost(g, a.group);
         };
@@ -130,8 +133,11 @@ weights_schedule_kernel(WeightsArgs w)
         h.per_head = carry_cost;
         h.groups = carry_groups;
         h.blocks = int(max(1ll, min((long long)a.blocks, carry_cost * a.num_kv_heads / kLeastShare)));
-        *a.header = h;
+        *a.header = made = h;
     }
+    __syncthreads();
+    if (made.groups > 0)
+        write_starts(made, a.num_kv_heads, a.starts, [&](int i) { return made.groups <= kKeptCums ? cums[i] : w.groups[i].cum; });
 }
 
 // A place inside a group: the pair, and how many of its row tiles lie before it.
@@ -155,14 +161,15 @@ struct WeightsWalk {
     ChunkHeader h;
     long long x0 = 0, x1 = 0;
     int head, gi = 0;
-    __device__ __forceinline__ WeightsWalk(const WeightsArgs &args, int block, int lane) : w(args), h(*args.c.header)
+    __device__ __forceinline__ WeightsWalk(const WeightsArgs &args, int block) : w(args), h(*args.c.header)
     {
+        const ChunkStart s = args.c.starts[block];   // asked for together with the header
         head = w.c.num_kv_heads;
         if (block >= h.blocks || h.groups == 0) return;
-        const long long total = h.per_head * w.c.num_kv_heads;
-        x0 = share_begin(total, block, h.blocks);
-        x1 = share_begin(total, block + 1, h.blocks);
-        locate(w.groups, h, x0, lane, &head, &gi);
+        x0 = s.x0;
+        x1 = s.x1;
+        head = s.head;
+        gi = s.group;
     }
     __device__ __forceinline__ bool next(WeightsPiece &p)
     {
@@ -266,7 +273,7 @@ weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     grid_wait();
     grid_release();
 
-    WeightsWalk walk(w, blockIdx.x, lane);
+    WeightsWalk walk(w, blockIdx.x);
     WeightsPiece pc;
     bool ok = true;
 
@@ -464,17 +471,21 @@ weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                             }
                         };
                         uint32_t s[2][16];
-                        tmem_ld16(s_addr, s[0]);
-                        tmem_wait_ld();
-                        if (few) {
-                            add(s[0], 0, true);
-                        } else {
+                        if (whole) {
+                            tmem_ld16(s_addr, s[0]);
+                            tmem_wait_ld();
 #pragma unroll
                             for (int c = 0; c < 8; ++c) {
                                 if (c < 7) tmem_ld16(s_addr + (c + 1) * 16, s[(c + 1) & 1]);
-                                if (whole) add(s[c & 1], c * 16, false);
-                                else add(s[c & 1], c * 16, true);
+                                add(s[c & 1], c * 16, false);
                                 tmem_wait_ld();
+                            }
+                        } else {
+#pragma unroll 1
+                            for (int c = 0; c < (few ? 16 : 128); c += 16) {
+                                tmem_ld16(s_addr + c, s[0]);
+                                tmem_wait_ld();
+                                add(s[0], c, true);
                             }
                         }
                         tc_fence_before();
@@ -538,23 +549,22 @@ weights_merge_kernel(const WeightsArgs w)
     const ChunkHeader h = *w.c.header;
     const int cut = blockIdx.x;
     if (cut + 1 >= h.blocks || h.groups == 0) return;
-    const long long total = h.per_head * w.c.num_kv_heads;
-    const long long x = share_begin(total, cut + 1, h.blocks);
-    int head, gi;
-    locate(w.groups, h, x, threadIdx.x & 31, &head, &gi);
+    const ChunkStart *starts = w.c.starts, before = starts[cut], after = starts[cut + 1];
+    const int head = after.head;
+    const long long x = after.x0;
     if (head >= w.c.num_kv_heads) return;
-    const WeightsGroup g = w.groups[gi];
+    const WeightsGroup g = w.groups[after.group];
     const long long base = head * h.per_head + g.cum;
     const int count = row_tiles(g.n, w.c.group) - g.first_tile;
     const Place at = place_of(g, w.c.group, x - base);
     if (at.pair >= g.pairs || at.rows <= 0 || at.rows >= count) return;                 // nothing is cut here
     if (cut > 0) {
-        const Place before = place_of(g, w.c.group, share_begin(total, cut, h.blocks) - base);
-        if (before.pair == at.pair && before.rows > 0) return;                          // an earlier cut's pair
+        const Place earlier = place_of(g, w.c.group, before.x0 - base);
+        if (earlier.pair == at.pair && earlier.rows > 0) return;                          // an earlier cut's pair
     }
     float sum = 0.f;
     for (int b = cut; b < h.blocks; ++b) {
-        const Place from = place_of(g, w.c.group, share_begin(total, b, h.blocks) - base), to = place_of(g, w.c.group, share_begin(total, b + 1, h.blocks) - base);
+        const Place from = place_of(g, w.c.group, starts[b].x0 - base), to = place_of(g, w.c.group, starts[b].x1 - base);
         const int r0 = from.pair == at.pair ? from.rows : 0, r1 = to.pair == at.pair ? to.rows : count;
         if (r0 < r1) sum += w.partial[size_t(2 * b + (r0 > 0 ? 0 : 1)) * kPairKeys + threadIdx.x];
         if (r1 >= count) break;
@@ -584,6 +594,7 @@ size_t layout(WeightsArgs &w, void *scratch)
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t at = off; off = (off + bytes + 255) / 256 * 256; return static_cast<unsigned char *>(scratch) + at; };
     a.header = reinterpret_cast<ChunkHeader *>(take(sizeof(ChunkHeader)));
+    a.starts = reinterpret_cast<ChunkStart *>(take(sizeof(ChunkStart) * size_t(a.blocks)));
     w.groups = reinterpret_cast<WeightsGroup *>(take(sizeof(WeightsGroup) * size_t(a.max_groups)));
     w.partial = reinterpret_cast<float *>(take(4 * size_t(2 * a.blocks) * kPairKeys));
     return off;
