@@ -110,13 +110,15 @@ __device__ __forceinline__ ChunkGroup chunk_group(const ChunkSample &c, int i, i
     return g;
 }
 
-// Cost of a piece in quarters of a key tile of two row tiles (2.1 us).  A single row tile's key tile costs three: half the arithmetic, but as
-// many bytes.  kPieceCost: loading Q, the first tiles' way and the epilogue, measured at 4 to 5 us a piece.
-constexpr int kPieceCost = 8;
-constexpr int kLeastCost = 14;    // a share is not made smaller than this
+// Cost of a piece in quarters of a key tile of two row tiles (1.9 us).  A single row tile's key tile, 1.05 to 1.15 us, costs two, and a piece
+// 14: the first tiles' way and the epilogue, 4.4 us with two row tiles, 6.5 with one, where other pieces' loads fill the gap less.  (14, 2)
+// against (8, 3), (10, 2), (12, 3), (18, 2) and (18, 3): 116 us for 64 x 4 tokens over U[0,4096] against 122, 118, 119, 117 and 118; 4096 tokens over
+// 12288 do not mind.
+constexpr int kPieceCost = 14;
+constexpr int kLeastCost = 8;     // a share is not made smaller than this: 4 x 4 tokens over 2000 21 us, with 14 23, with 20 26
 constexpr int kWholeTiles = 6;    // key tiles of samples that are not worth cutting
 __device__ __forceinline__ int chunk_tiles(int keys) { return (keys + 127) >> 7; }
-__device__ __forceinline__ int chunk_weight(const ChunkGroup &g, int group) { return g.n_tok * group > 128 ? 4 : 3; }
+__device__ __forceinline__ int chunk_weight(const ChunkGroup &g, int group) { return g.n_tok * group > 128 ? 4 : 2; }
 __device__ __forceinline__ long long chunk_cost(const ChunkGroup &g, int group)
 {
     return kPieceCost + (long long)chunk_tiles(g.keys) * chunk_weight(g, group);

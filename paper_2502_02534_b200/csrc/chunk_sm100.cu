@@ -17,15 +17,19 @@
 // each with an accumulator of its own, joined at the end.  P is handed over in halves of 64 keys, so that the first half's products run
 // under the second half's exponentials.  The reference maximum moves only when a half's exponents exceed it by 2^8 (which its sum tells).
 //
-// What bounds it.  4096 new tokens over 12288 (64 / 8 heads of 128): 1.82 ms = 1.06 PFLOP/s, 0.76 of the measured sustained bf16 rate; the
-// tensor cores are busy 54 % of the cycles, the way from one score tile to the next (commit, softmax, hand-over, P V, Q K^T) is the rest:
-// with the arithmetic taken out the barriers alone take 1.2 ms, the products alone 1.26, the tiles' way from L2 1.1.  64 x 4 tokens over
-// U[0,4096] (549 MB): 125 us, 4.4 TB/s; the loads alone take 105.
+// What bounds it.  4096 new tokens over 12288 (64 / 8 heads of 128): 1.66 to 1.69 ms = 1.16 PFLOP/s, 0.83 of the measured sustained bf16
+// rate; a key tile of two row tiles takes 1.9 us at the full clock, its products 1.5; the way from one score tile to the next (commit, softmax,
+// hand-over, P V, Q K^T) is the rest.  64 x 4 tokens over U[0,4096] (549 MB): 117 us, 4.7 TB/s: the tiles come at 6.1 TB/s while they come, but a
+// piece ends with 6.5 us of one warp's work (32 rows) that the ring's 160 KB cover half of, the first tile is 8 us on its way, the last shares
+// end 10 us behind the median.  Eight short samples: 10.9 us, a chain of schedule, lists, tiles, one unit and the epilogue.
+// The instruction cache was the limit for long: masks and the careful way inlined in both halves cost the long case 7 %, the epilogue two
+// thirds of its time.
 // Tried and not kept (the long case, then the 64 x 4 tokens, against 1832 and 133 at that time): two warpgroups a stream, each half of the
 // keys, with a shared reference 1875 / 139; the same with a score buffer for each half (64-key products) 2096 / 151; an issuer for each
 // stream 2221 / 138; a watcher thread that folds the tiles' arrival into P's barrier 1860 / 134; K by TMA and V by cp.async 2236 / 182; all by
 // cp.async 2411 / 166; prefetches into L2 6 tiles ahead 2204 / 162; one arrival a warp on the P barriers, polling without suspension: no
-// change; a share of polynomial exponentials from 0 to 3/8: within 2 %.
+// change.  Against 1660 and 122: no polynomials 1720 / 121, an eighth 1682 / 121, three eighths 1728 / 131, the careful way as a function that is
+// called (it spills) 1874 / 153, both halves in a rolled loop 1767 / 118.
 //
 // What does not exist is never used: products stop at the last page, rows of V behind the last key are zeroed in shared memory (they may
 // hold anything), scores behind a row's last key become -inf.  Page ids outside the pool read as zeros (TMA bounds) and raise
@@ -536,7 +540,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
                     return true;
                 };
                 // Scores to be masked, or a reference to be moved.  There is one copy of this code, and it goes on to the second half: what
-                // the loop's code takes of the instruction cache is its speed (masks and both ways in both halves: the long case 1790 us, not 1665).
+                // the loop's code takes of the instruction cache is its speed.
                 auto careful = [&](int h) -> bool {
                     const int v = valid - 64 * h;
                     uint32_t r[2][32];

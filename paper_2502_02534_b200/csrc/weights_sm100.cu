@@ -14,9 +14,11 @@
 // tensor memory, 17 brings in the rows with their log-sum-exps, 18 and 19 the key tiles.  Two score buffers of 128 columns for each key tile.
 // Every wait is bounded.
 //
-// 64 samples x 1 token over U[0,4096], 8 heads (268 MB of K): 57 us, 4.7 TB/s (one TMA warp for both key tiles 66); launch, schedule and merge are
-// 10 of them.  2048 tokens over 8192, 32 / 8 heads, 604 M exponentials: 203 us, the special-function units busy half of the time (134 us at their
-// rate; two warpgroups 229 us, log-sum-exps loaded when needed 216).  Row tiles of 64 with four buffers 252, an issuer for each key tile 202.
+// 64 samples x 1 token over U[0,4096], 8 heads (268 MB of K): 55.5 us, 4.8 TB/s (one TMA warp for both key tiles 66); launch, schedule and
+// merge are 10 of them.  2048 tokens over 8192, 32 / 8 heads, 604 M exponentials, a quarter by polynomial: 180 us; the special-function units'
+// share is 100 us, the products 111 (two warpgroups 229 us; log-sum-exps loaded when needed 216; masked rows unrolled beside the whole ones,
+// which is too much code, 205).  No polynomials 196, three eighths 181, half 208; row tiles of 64 with four buffers 252, an issuer for each key
+// tile 202, both against 203 at that time.
 #include <algorithm>
 
 #include "chunk.h"
