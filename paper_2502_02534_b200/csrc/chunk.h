@@ -49,6 +49,7 @@ struct ChunkArgs {
     bool prior_f32, out_f32;
     // scratch
     int32_t blocks, max_groups, slot_rows;
+    int32_t direct;        // not 0: no schedule, a block for each of so many groups a head
     ChunkHeader *header;
     ChunkStart *starts;    // [blocks]
     ChunkGroup *groups;
@@ -117,6 +118,9 @@ __device__ __forceinline__ ChunkGroup chunk_group(const ChunkSample &c, int i, i
 constexpr int kPieceCost = 14;
 constexpr int kLeastCost = 8;     // a share is not made smaller than this: 4 x 4 tokens over 2000 21 us, with 14 23, with 20 26
 constexpr int kWholeTiles = 6;    // key tiles of samples that are not worth cutting
+// ... nor a schedule and a merge, where all lists together are known to be no longer: one sample of 2 / 6 / 10 / 12 tiles 10.2 / 14.0 / 17.5 /
+// 19.3 us, cut and joined 12.1 / 15.9 / 18.0 / 18.5
+constexpr int kDirectTiles = 10;
 __device__ __forceinline__ int chunk_tiles(int keys) { return (keys + 127) >> 7; }
 __device__ __forceinline__ int chunk_weight(const ChunkGroup &g, int group) { return g.n_tok * group > 128 ? 4 : 2; }
 __device__ __forceinline__ long long chunk_cost(const ChunkGroup &g, int group)
@@ -154,38 +158,84 @@ __device__ __forceinline__ void write_starts(const ChunkHeader &h, int heads, Ch
     }
 }
 
+// Group number `want` of all, found by a whole warp, a lane a sample.  No tokens: there are fewer.
+__device__ __forceinline__ ChunkGroup find_group(const ChunkArgs &a, int want, int lane)
+{
+    const int per_group = kGroupRows / a.group;
+    for (int s0 = 0; s0 < a.num_samples; s0 += 32) {
+        ChunkSample c{};
+        if (s0 + lane < a.num_samples) c = chunk_sample(a, s0 + lane);
+        const int groups = (c.n + per_group - 1) / per_group;
+        int upto = groups;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int u = __shfl_up_sync(0xffffffffu, upto, d);
+            if (lane >= d) upto += u;
+        }
+        const unsigned has = __ballot_sync(0xffffffffu, want < upto);
+        if (has) {
+            const int owner = __ffs(has) - 1;
+            const ChunkSample o{__shfl_sync(0xffffffffu, c.q0, owner), __shfl_sync(0xffffffffu, c.n, owner), __shfl_sync(0xffffffffu, c.len, owner),
+                                __shfl_sync(0xffffffffu, c.list0, owner)};
+            return chunk_group(o, want - __shfl_sync(0xffffffffu, upto - groups, owner), per_group);
+        }
+        want -= __shfl_sync(0xffffffffu, upto, 31);
+    }
+    return {};
+}
+
 struct ChunkPiece {
     ChunkGroup g;
     int head, t0, t1;      // key tiles
     bool split;            // not the whole group: the result is partial and goes to `slot`
     int slot;
 };
+// What a block's warps have to know of its share, in shared memory: registers are scarce.
+struct ChunkShare {
+    long long per_head, x0, x1;
+    int32_t groups, whole;     // whole: `own` is all there is
+    int32_t head, group;       // where it starts; head num_kv_heads: nothing to do
+    ChunkGroup own;
+};
+// by a whole warp
+__device__ __forceinline__ ChunkShare chunk_share(const ChunkArgs &a, int block, int lane)
+{
+    ChunkShare s{};
+    s.head = a.num_kv_heads;
+    if (a.direct) {
+        s.whole = 1;
+        s.own = find_group(a, block % a.direct, lane);
+        if (s.own.n_tok > 0) s.head = block / a.direct;
+        return s;
+    }
+    const ChunkHeader h = *a.header;
+    const ChunkStart start = a.starts[block];      // asked for together with the header
+    if (block >= h.blocks || h.groups == 0) return s;
+    s.whole = h.whole;
+    s.groups = h.groups;
+    if (h.whole) {
+        s.head = block / h.groups;
+        s.own = a.groups[block % h.groups];
+        return s;
+    }
+    s.per_head = h.per_head;
+    s.x0 = start.x0;
+    s.x1 = start.x1;
+    s.head = start.head;
+    s.group = start.group;
+    return s;
+}
 // The pieces of one block's share, in order.
 struct ChunkWalk {
     const ChunkArgs &a;
-    ChunkHeader h;
-    long long x0 = 0, x1 = 0;
-    int block, head, gi = 0;
-    __device__ __forceinline__ ChunkWalk(const ChunkArgs &args, int b) : a(args), h(*args.header), block(b)
-    {
-        const ChunkStart s = args.starts[b];       // asked for together with the header
-        head = a.num_kv_heads;
-        if (block >= h.blocks || h.groups == 0) return;
-        if (h.whole) {
-            head = block / h.groups;
-            gi = block % h.groups;
-            return;
-        }
-        x0 = s.x0;
-        x1 = s.x1;
-        head = s.head;
-        gi = s.group;
-    }
+    const ChunkShare &share;
+    int head, gi;
+    __device__ __forceinline__ ChunkWalk(const ChunkArgs &args, const ChunkShare &s) : a(args), share(s), head(s.head), gi(s.group) {}
     __device__ __forceinline__ bool next(ChunkPiece &p)
     {
-        if (h.whole) {
+        if (share.whole) {
             if (head >= a.num_kv_heads) return false;
-            p.g = a.groups[gi];
+            p.g = share.own;
             p.head = head;
             p.t0 = 0;
             p.t1 = chunk_tiles(p.g.keys);
@@ -195,31 +245,31 @@ struct ChunkWalk {
             return true;
         }
         for (;;) {
-            if (gi >= h.groups) {
+            if (gi >= share.groups) {
                 gi = 0;
                 ++head;
             }
             if (head >= a.num_kv_heads) return false;
             p.g = a.groups[gi];
-            const long long base = head * h.per_head + p.g.cum;
-            if (base >= x1) {
+            const long long base = head * share.per_head + p.g.cum;
+            if (base >= share.x1) {
                 head = a.num_kv_heads;
                 return false;
             }
             ++gi;
             p.head = head;
             const int tiles = chunk_tiles(p.g.keys);
-            p.t0 = tile_at(p.g, a.group, base, x0);
-            p.t1 = tile_at(p.g, a.group, base, x1);
+            p.t0 = tile_at(p.g, a.group, base, share.x0);
+            p.t1 = tile_at(p.g, a.group, base, share.x1);
             p.split = false;
             p.slot = 0;
             if (tiles == 0) {
-                if (base < x0) continue;     // the share where it starts has it
+                if (base < share.x0) continue;     // the share where it starts has it
                 return true;
             }
             if (p.t1 <= p.t0) continue;
             p.split = p.t0 > 0 || p.t1 < tiles;
-            p.slot = 2 * block + (p.t0 > 0 ? 0 : 1);
+            p.slot = 2 * int(blockIdx.x) + (p.t0 > 0 ? 0 : 1);
             return true;
         }
     }

@@ -8,7 +8,8 @@
 // writes their running costs (key tiles).  chunk_kernel is persistent: block i takes the i-th equal share of all (KV head, group, key
 // tile) units, in order, so every SM has the same work whatever the lengths are, and a group is cut only where a share ends.  What is cut
 // leaves partial results, two slots a block at most, which chunk_merge_kernel joins; groups that were not cut are finished in place.  A
-// batch of few short samples has a block for every group instead, uncut.
+// batch of few short samples has a block for every group instead, uncut; where the lists' length alone says so, it is one launch, and
+// every block finds its group by itself.
 //
 // chunk_kernel, 12 warps: 0-3 and 4-7 softmax warpgroups (streams 0 and 1), 8 MMA issuer (one lane) and owner of the tensor memory, 9-11 TMA
 // producers.  Key tiles of 128 keys arrive page by page (one TMA box of 16 tokens x 64 channels each) in a ring; S = Q K^T goes to
@@ -21,7 +22,8 @@
 // rate; a key tile of two row tiles takes 1.9 us at the full clock, its products 1.5; the way from one score tile to the next (commit, softmax,
 // hand-over, P V, Q K^T) is the rest.  64 x 4 tokens over U[0,4096] (549 MB): 117 us, 4.7 TB/s: the tiles come at 6.1 TB/s while they come, but a
 // piece ends with 6.5 us of one warp's work (32 rows) that the ring's 160 KB cover half of, the first tile is 8 us on its way, the last shares
-// end 10 us behind the median.  Eight short samples: 10.9 us, a chain of schedule, lists, tiles, one unit and the epilogue.
+// end 10 us behind the median.  Eight short samples: 8.8 us (with a
+// schedule and a merge 10.9), a chain of launch, lists, page ids, tiles, one unit and the epilogue.
 // The instruction cache was the limit for long: masks and the careful way inlined in both halves cost the long case 7 %, the epilogue two
 // thirds of its time.
 // Tried and not kept (the long case, then the 64 x 4 tokens, against 1832 and 133 at that time): two warpgroups a stream, each half of the
@@ -173,11 +175,12 @@ struct ChunkSmem {
     static constexpr int kBarQFull = 0, kBarQEmpty = 2, kBarFull = 4, kBarEmpty = kBarFull + kRing, kBarS = kBarEmpty + kRing, kBarP = kBarS + 2,
                          kBarHalf = kBarP + 4, kBarDone = kBarHalf + 2, kBarMet = kBarDone + 2, kBarDrain = kBarMet + 1, kNumBars = kBarDrain + 1;
     static constexpr int kTmemPtrOff = 8 * kNumBars, kAbortOff = kTmemPtrOff + 4;
+    static constexpr int kShareOff = 512;
     static constexpr int kExchangeOff = 1024;                    // (m, l) of both streams' rows
     static constexpr int kQOff = 3072;
     static constexpr int kRingOff = kQOff + 2 * kTileBytes;
     static constexpr int kTotal = kRingOff + kRing * kTileBytes;
-    static_assert(kAbortOff + 4 <= kExchangeOff && kTotal <= 227 * 1024, "shared memory plan");
+    static_assert(kAbortOff + 4 <= kShareOff && kTotal <= 227 * 1024, "shared memory plan");
 };
 
 // Element m of the order in which K and V tiles travel: alternating with two row tiles, K two tiles ahead with one.
@@ -226,24 +229,17 @@ __device__ __forceinline__ void quad_transpose(float (&v)[4][8], int quad)
                     v[j | bit][k] = upper ? v[j | bit][k] : got;
                 }
 }
-// 8 columns of the earlier result, on their way and added
-struct Earlier { uint4 w[2]; };
-__device__ __forceinline__ Earlier earlier_columns(const ChunkArgs &a, size_t at)
-{
-    if (a.prior_f32) {
-        const uint4 *from = reinterpret_cast<const uint4 *>(static_cast<const float *>(a.prior_out) + at);
-        return {from[0], from[1]};
-    }
-    return {*reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(a.prior_out) + at), {}};
-}
-__device__ __forceinline__ void add_earlier(const ChunkArgs &a, const Earlier &e, float w, float (&v)[8])
+// 8 columns of the earlier result added: in bf16, the usual type, they have been asked for before
+__device__ __forceinline__ void add_earlier(const ChunkArgs &a, const uint4 &asked, size_t at, float w, float (&v)[8])
 {
     if (w == 0.f) return;                          // not 0 x NaN
-    const uint32_t u[8] = {e.w[0].x, e.w[0].y, e.w[0].z, e.w[0].w, e.w[1].x, e.w[1].y, e.w[1].z, e.w[1].w};
     if (a.prior_f32) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = fmaf(w, __uint_as_float(u[k]), v[k]);
+        const float4 *from = reinterpret_cast<const float4 *>(static_cast<const float *>(a.prior_out) + at);
+        const float4 x = from[0], y = from[1];
+        v[0] = fmaf(w, x.x, v[0]); v[1] = fmaf(w, x.y, v[1]); v[2] = fmaf(w, x.z, v[2]); v[3] = fmaf(w, x.w, v[3]);
+        v[4] = fmaf(w, y.x, v[4]); v[5] = fmaf(w, y.y, v[5]); v[6] = fmaf(w, y.z, v[6]); v[7] = fmaf(w, y.w, v[7]);
     } else {
+        const uint32_t u[4] = {asked.x, asked.y, asked.z, asked.w};
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             v[2 * k] = fmaf(w, __uint_as_float(u[k] << 16), v[2 * k]);
@@ -296,7 +292,13 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
     grid_wait();
     grid_release();
 
-    ChunkWalk walk(a, blockIdx.x);
+    ChunkShare *share = reinterpret_cast<ChunkShare *>(smem + L::kShareOff);
+    if (warp == 0) {
+        const ChunkShare s = chunk_share(a, blockIdx.x, lane);
+        if (lane == 0) *share = s;
+    }
+    __syncthreads();
+    ChunkWalk walk(a, *share);
     ChunkPiece pc;
 
     if (warp >= kProducerWarp) {
@@ -603,10 +605,11 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
             const bool joins = !pc.split && a.prior_lse;
             const float prior2 = joins && mine ? a.prior_lse[out_row(in_group)] * kLog2e : -INFINITY;
             size_t at[4];
-            Earlier earlier[4];
+            uint4 earlier[4];
             auto ask = [&](int c) {
+                if (!a.prior_f32)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) earlier[k] = earlier_columns(a, at[k] + c);
+                    for (int k = 0; k < 4; ++k) earlier[k] = *reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(a.prior_out) + at[k] + c);
             };
             if (active && !pc.split) {
 #pragma unroll
@@ -682,7 +685,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
                 quad_transpose(v, quad);
                 if (joins) {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) add_earlier(a, earlier[k], from[k], v[k]);
+                    for (int k = 0; k < 4; ++k) add_earlier(a, earlier[k], at[k] + c, from[k], v[k]);
                     if (c + 32 < c1) ask(c + 32);
                 }
 #pragma unroll
@@ -855,6 +858,10 @@ cudaError_t launch(const ChunkArgs &a, const CUtensorMap &mq, const CUtensorMap 
     static PerDeviceOnce once;
     if (const int rc = once.ensure([] { return int(cudaFuncSetAttribute(chunk_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, ChunkSmem<D>::kTotal)); }))
         return cudaError_t(rc);
+    if (a.direct) {
+        chunk_kernel<D><<<a.direct * a.num_kv_heads, kChunkThreads, ChunkSmem<D>::kTotal, st>>>(mq, mk, mv, a);
+        return cudaGetLastError();
+    }
     chunk_schedule_kernel<<<1, kScheduleThreads, 0, st>>>(a);
     cudaError_t e = cudaGetLastError();
     if (e == cudaSuccess) e = launch_dependent(chunk_kernel<D>, dim3(a.blocks), kChunkThreads, ChunkSmem<D>::kTotal, st, mq, mk, mv, a);
@@ -995,6 +1002,8 @@ extern "C" psa_status_t psa_attend_paged(const void *q, const int64_t q_strides[
     a.blocks = std::min(multiprocessors(), kMostBlocks);
     if (a.blocks <= 0) return set_last_error(PSA_ERR_CUDA, "no CUDA device");
     chunk_layout(a, scratch, head_dim);
+    // a few short lists: every group is a block's, which finds it by itself
+    if (num_entries * kPageSize <= kDirectTiles * kTileKeys && int64_t(a.max_groups) * num_kv_heads <= a.blocks) a.direct = a.max_groups;
     CUtensorMap maps[3];
     rc = chunk_q_map(a, q, q_strides, head_dim, kRowTile, &maps[0]);
     if (rc == PSA_OK) rc = chunk_pool_map(a, k_pool, pool_strides, head_dim, &maps[1]);

@@ -77,6 +77,23 @@ def test_many_pieces_of_one_tile(D, most_new):
         assert torch.equal(again, out) and torch.equal(again_lse, lse)
 
 
+@pytest.mark.parametrize("samples", [[(i % 16, 1) for i in range(90)], [(3, 0)] * 40 + [(5, 2), (0, 0), (40, 7)], [(1000, 1), (0, 300)], [(15, 1)] * 33 + [(0, 0)] * 30])
+def test_few_short_lists(samples):
+    """Up to 80 pages in all lists together, or a few more, and few groups: the blocks find their groups by themselves."""
+    import torch
+    for D, Hq, Hkv in ((128, 8, 1), (64, 1, 1)):
+        c = case(D, Hq, Hkv, samples, seed=len(samples))
+        c["indices"] = c["indices"][:max(1, int(c["indptr"][-1]))]
+        want = reference(c)
+        d = on_device(c)
+        check(*run(c, d), want, True)
+        rng = np.random.default_rng(3)
+        prior, prior_lse = rng.standard_normal(c["q"].shape).astype(np.float32), rng.standard_normal(c["q"].shape[:2]).astype(np.float32)
+        out = torch.empty(c["q"].shape, device="cuda")
+        got = run(c, d, out=out, prior_out=dev(prior), prior_lse=dev(prior_lse))
+        check(*got, reference(c, prior_out=prior.astype(np.float64), prior_lse=prior_lse.astype(np.float64)), False)
+
+
 def test_tokens_that_see_nothing():
     """Lengths below the number of new tokens: the first rows stand before the cache begins."""
     c = case(64, 4, 2, [(40, 9), (3, 6)], seed=3)
