@@ -94,6 +94,11 @@ def test_few_short_lists(samples):
         check(*got, reference(c, prior_out=prior.astype(np.float64), prior_lse=prior_lse.astype(np.float64)), False)
 
 
+def test_more_groups_than_the_schedule_keeps():
+    c = case(64, 2, 1, [(i % 40, 1 + i % 2) for i in range(1500)] + [(1900, 3)], seed=2)
+    check(*run(c), reference(c), True)
+
+
 def test_tokens_that_see_nothing():
     """Lengths below the number of new tokens: the first rows stand before the cache begins."""
     c = case(64, 4, 2, [(40, 9), (3, 6)], seed=3)

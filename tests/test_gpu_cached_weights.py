@@ -79,6 +79,18 @@ def test_against_the_definition(D, Hq, Hkv, samples):
         compare(out[torch.from_numpy(touched).cuda()], want[touched], c, before, lse)
 
 
+def test_more_groups_than_the_schedule_keeps():
+    c = case(64, 2, 1, [(i % 40, 1 + i % 2) for i in range(1500)], seed=2)
+    lse = lse_of(c)
+    before = clean(c, start(c))
+    want = want_of(c, before, lse)
+    w = dev(before)
+    run(c, dev(lse), w)
+    keep = ~np.isnan(want)
+    import torch
+    compare(w[torch.from_numpy(keep).cuda()], want[keep], c, before, lse)
+
+
 def test_rows_that_see_nothing_give_nothing_and_prompts_count():
     c = case(64, 4, 2, [(40, 9), (3, 6)], seed=3)
     lse = lse_of(c) + 2.0                           # most of the weight lies in a shared prompt
