@@ -177,7 +177,7 @@ struct ChunkSmem {
     static constexpr int kTmemPtrOff = 8 * kNumBars, kAbortOff = kTmemPtrOff + 4;
     static constexpr int kShareOff = 512;
     static constexpr int kExchangeOff = 1024;                    // (m, l) of both streams' rows
-    static constexpr int kQOff = 3072;
+    static constexpr int kQOff = 3 * 1024;
     static constexpr int kRingOff = kQOff + 2 * kTileBytes;
     static constexpr int kTotal = kRingOff + kRing * kTileBytes;
     static_assert(kAbortOff + 4 <= kShareOff && kTotal <= 227 * 1024, "shared memory plan");

@@ -229,7 +229,7 @@ struct WeightsSmem {
     static constexpr int kTmemPtrOff = 8 * kNumBars, kAbortOff = kTmemPtrOff + 4;
     static constexpr int kPassOff = 512;                         // a sum for every key of a pair
     static constexpr int kLseOff = kPassOff + 1024;
-    static constexpr int kQOff = 3072;
+    static constexpr int kQOff = 3 * 1024;
     static constexpr int kKOff = kQOff + kQRing * kTileBytes;
     static constexpr int kTotal = kKOff + kKRing * kTileBytes;
     static_assert(kAbortOff + 4 <= kPassOff && kLseOff + kLseRing * 512 <= kQOff && kTotal <= 227 * 1024, "shared memory plan");
