@@ -53,8 +53,6 @@ constexpr int kChunkThreads = 12 * 32;
 constexpr int kPagesPerTile = kTileKeys / kPageSize;
 constexpr float kThreshold = 8.f;                      // log2 units
 constexpr float kHalfSumLimit = 64.f * 256.f * 1.01f;  // 64 exponentials of at most 2^8
-// P is truncated to bf16; exponents carry log2 of 1 / (1 - 2^-8 / (2 ln 2)), what truncation loses on average, and the sums are freed of it
-constexpr float kBias = 0.0040709119f, kUnbias = 0.99718224f;
 constexpr uint32_t kPolyOf16 = 0x1111;                 // pairs of 32 scores whose exponentials are polynomials
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 
@@ -508,7 +506,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
                 };
                 // 32 scores -> 16 words of bf16 P; adds them to `sum`
                 auto exponentials = [&](const uint32_t (&r)[32], uint32_t *to, float2 (&sum)[2]) {
-                    const float off = kBias - (m_ref == -INFINITY ? 0.f : m_ref);
+                    const float off = m_ref == -INFINITY ? 0.f : -m_ref;
 #pragma unroll
                     for (int i = 0; i < 32; i += 2) {
                         const float2 x = fma2(make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), make_float2(a.scale_log2, a.scale_log2), make_float2(off, off));
@@ -516,7 +514,9 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
                         const bool poly = kPolyOf16 >> (i / 2) & 1;
                         const float2 e = poly ? poly_exp2_pair<4>(x) : make_float2(fast_exp2(x.x), fast_exp2(x.y));
                         sum[i / 2 & 1] = add2(sum[i / 2 & 1], e);
-                        to[i / 2] = __byte_perm(__float_as_uint(e.x), __float_as_uint(e.y), 0x7632);
+                        // P is rounded to nearest: its products need 16 bits; truncating it takes as long
+                        const __nv_bfloat162 both = __floats2bfloat162_rn(e.x, e.y);
+                        to[i / 2] = reinterpret_cast<const uint32_t &>(both);
                     }
                 };
                 auto hand_over = [&](int h, float total) {
@@ -594,7 +594,6 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
             e += 2 * n;
 
             // ---- epilogue
-            l_sum *= kUnbias;
             auto out_row = [&](int r) { return size_t(pc.g.q0 + (r >> shift)) * a.num_q_heads + pc.head * a.group + (r & (a.group - 1)); };
             const size_t part_row = size_t(pc.slot) * a.slot_rows + in_group;
             // this warpgroup's columns: all of its own row tile, or half of the shared one
