@@ -549,7 +549,7 @@ psa_status_t psa_store_kv(const void *new_k, const void *new_v, const int64_t kv
  * What stands in the pages behind a sample's last token does not matter, NaN included.  Within the new tokens V has to be finite
  * where earlier rows are to be: a tile's products are taken with weight 0 for what a row does not see.
  * D in {64, 128}, Hq / Hkv in {1, 2, 4, 8}, Hq at most 2^16; pointers 16-byte aligned, strides multiples of 8 elements; at most 2^20
- * samples and 2^24 new tokens.  Outputs do not overlap inputs but as said above.  Weights are rounded to bf16 as in psa_decode.  Enqueues one or three kernels.
+ * samples and 2^24 new tokens.  Outputs do not overlap inputs but as said above.  Weights are rounded to bf16.  Enqueues one or three kernels.
  */
 size_t psa_attend_paged_scratch_bytes(int64_t num_tokens, int32_t num_samples, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim);
 psa_status_t psa_attend_paged(const void *q, const int64_t q_strides[2], const int32_t *q_indptr, int64_t num_tokens, int32_t num_samples,

@@ -20,7 +20,7 @@
 //
 // What bounds it.  4096 new tokens over 12288 (64 / 8 heads of 128): 1.66 to 1.69 ms = 1.16 PFLOP/s, 0.83 of the measured sustained bf16
 // rate; a key tile of two row tiles takes 1.9 us at the full clock, its products 1.5; the way from one score tile to the next (commit, softmax,
-// hand-over, P V, Q K^T) is the rest.  64 x 4 tokens over U[0,4096] (549 MB): 117 us, 4.7 TB/s: the tiles come at 6.1 TB/s while they come, but a
+// hand-over, P V, Q K^T) is the rest.  64 x 4 tokens over U[0,4096] (549 MB): 113 us, 4.9 TB/s: the tiles come at 6.1 TB/s while they come, but a
 // piece ends with 6.5 us of one warp's work (32 rows) that the ring's 160 KB cover half of, the first tile is 8 us on its way, the last shares
 // end 10 us behind the median.  Eight short samples: 8.8 us (with a
 // schedule and a merge 10.9), a chain of launch, lists, page ids, tiles, one unit and the epilogue.
