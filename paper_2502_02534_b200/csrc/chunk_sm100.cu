@@ -16,7 +16,9 @@
 // tensor memory, a warpgroup (thread = row) turns it into P (bf16, over S), O += P V.  More than 128 rows: each stream has a row tile and
 // both read every key tile, so a byte of K and V serves 256 rows.  Up to 128 rows: the streams take alternate key tiles of the one row tile,
 // each with an accumulator of its own, joined at the end.  P is handed over in halves of 64 keys, so that the first half's products run
-// under the second half's exponentials.  The reference maximum moves only when a half's exponents exceed it by 2^8 (which its sum tells).
+// under the second half's exponentials.  The reference maximum moves only when a half's exponents exceed it by 2^8 (which its
+// sum tells, with the largest exponent that went to a polynomial: beyond 2^127 those are wrong; a three-way maximum a pair, +0.2 %, clamping each
+// +1.3 % on the long case).
 //
 // What bounds it.  4096 new tokens over 12288 (64 / 8 heads of 128): 1.66 to 1.69 ms = 1.16 PFLOP/s, 0.83 of the measured sustained bf16
 // rate; a key tile of two row tiles takes 1.9 us at the full clock, its products 1.5; the way from one score tile to the next (commit, softmax,
@@ -53,6 +55,7 @@ constexpr int kChunkThreads = 12 * 32;
 constexpr int kPagesPerTile = kTileKeys / kPageSize;
 constexpr float kThreshold = 8.f;                      // log2 units
 constexpr float kHalfSumLimit = 64.f * 256.f * 1.01f;  // 64 exponentials of at most 2^8
+constexpr float kMostPoly = 127.f;                     // exponents that the polynomials are good for
 constexpr uint32_t kPolyOf16 = 0x1111;                 // pairs of 32 scores whose exponentials are polynomials
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 
@@ -504,14 +507,16 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
                             if (i >= v) r[i] = 0xff800000u;
                     }
                 };
-                // 32 scores -> 16 words of bf16 P; adds them to `sum`
-                auto exponentials = [&](const uint32_t (&r)[32], uint32_t *to, float2 (&sum)[2]) {
+                // 32 scores -> 16 words of bf16 P; adds them to `sum`.  A sum tells of exponents out of range, but for those of polynomials, which
+                // go to `most`.
+                auto exponentials = [&](const uint32_t (&r)[32], uint32_t *to, float2 (&sum)[2], float &most) {
                     const float off = m_ref == -INFINITY ? 0.f : -m_ref;
 #pragma unroll
                     for (int i = 0; i < 32; i += 2) {
                         const float2 x = fma2(make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), make_float2(a.scale_log2, a.scale_log2), make_float2(off, off));
                         // part of them by polynomial: it relieves the special-function unit, which has an exponential a score
                         const bool poly = kPolyOf16 >> (i / 2) & 1;
+                        if (poly) most = max3(most, x.x, x.y);
                         const float2 e = poly ? poly_exp2_pair<4>(x) : make_float2(fast_exp2(x.x), fast_exp2(x.y));
                         sum[i / 2 & 1] = add2(sum[i / 2 & 1], e);
                         // P is rounded to nearest: its products need 16 bits; truncating it takes as long
@@ -530,14 +535,15 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
                 auto plain = [&](int h) -> bool {
                     uint32_t r[2][32];
                     float2 sum[2] = {{0.f, 0.f}, {0.f, 0.f}};
+                    float most = 0.f;
                     tmem_ld32(s_addr + h * 64, r[0]);
                     tmem_wait_ld();
                     tmem_ld32(s_addr + h * 64 + 32, r[1]);
-                    exponentials(r[0], p, sum);
+                    exponentials(r[0], p, sum, most);
                     tmem_wait_ld();
-                    exponentials(r[1], p + 16, sum);
+                    exponentials(r[1], p + 16, sum, most);
                     const float total = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
-                    if (__any_sync(0xffffffffu, !(total <= kHalfSumLimit))) return false;
+                    if (__any_sync(0xffffffffu, !(total <= kHalfSumLimit) || most > kMostPoly)) return false;
                     hand_over(h, total);
                     return true;
                 };
@@ -579,8 +585,9 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
                         if (need) m_ref = top;
                     }
                     float2 sum[2] = {{0.f, 0.f}, {0.f, 0.f}};
-                    exponentials(r[0], p, sum);
-                    exponentials(r[1], p + 16, sum);
+                    float most = 0.f;                  // of exponents that are in range
+                    exponentials(r[0], p, sum, most);
+                    exponentials(r[1], p + 16, sum, most);
                     hand_over(h, (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y));
                     return true;
                 };

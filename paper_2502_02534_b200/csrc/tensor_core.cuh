@@ -209,8 +209,16 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b)
         : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return r;
 }
+// the largest of three (NaN does not count)
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
 // Of a pair, in fewer instructions, with a polynomial of degree 4 (relative error below 2.7e-6, mean 4e-8) or 5 (1.6e-7, mean 5e-8), for sums
 // that are compared in fp32.  Minimax fits of 2^f over [-0.5, 0.5] in the relative error, rounded to fp32.
+// x must not be above 127: n would run over the exponent's bits, and a large power would read as a small or negative one.
 template <int kDegree>
 __device__ __forceinline__ float2 poly_exp2_pair(float2 x)
 {
