@@ -55,7 +55,6 @@ constexpr int kChunkThreads = 12 * 32;
 constexpr int kPagesPerTile = kTileKeys / kPageSize;
 constexpr float kThreshold = 8.f;                      // log2 units
 constexpr float kHalfSumLimit = 64.f * 256.f * 1.01f;  // 64 exponentials of at most 2^8
-constexpr float kMostPoly = 127.f;                     // exponents that the polynomials are good for
 constexpr uint32_t kPolyOf16 = 0x1111;                 // pairs of 32 scores whose exponentials are polynomials
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 
@@ -543,7 +542,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
                     tmem_wait_ld();
                     exponentials(r[1], p + 16, sum, most);
                     const float total = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
-                    if (__any_sync(0xffffffffu, !(total <= kHalfSumLimit) || most > kMostPoly)) return false;
+                    if (__any_sync(0xffffffffu, !(total <= kHalfSumLimit) || most > kMostPolyExp2)) return false;
                     hand_over(h, total);
                     return true;
                 };

@@ -861,7 +861,10 @@ prefix_body2(const CUtensorMap *pmap_q, const CUtensorMap *pmap_k, const CUtenso
             // and the bias of truncation (half a unit in the last place on average) is cancelled by exponentiating
             // x + trunc_bias, log2 of a factor: every p -- and with it the row sum, which is corrected once in the
             // epilogue by trunc_unbias -- carries that factor.  No running maximum either: if every exponent is below the threshold the
-            // tile sum is at most 64 * 2^8, so a sum above that bound is what sends the tile to the slow path.
+            // tile sum is at most 64 * 2^8, so a sum above that bound is what sends the tile to the slow path -- or a score (`most`) whose
+            // power a polynomial may give as a small one.  That maximum, three-way, of a third of the scores costs 8192 causal tokens 609 -> 617 us
+            // (taken of the exponents instead 619, polynomials clamped from above 656), the polynomials packed to make room for it.
+            float most = -INFINITY;
             auto exp_in_place = [&]() -> float {
                 const float off = trunc_bias - (m_ref == -INFINITY ? 0.f : m_ref);   // a row that has seen no key yet: exponentiate against 0
                 float ps[4] = {0.f, 0.f, 0.f, 0.f};
@@ -872,10 +875,12 @@ prefix_body2(const CUtensorMap *pmap_q, const CUtensorMap *pmap_k, const CUtenso
                         // every third pair takes the polynomial: with two warps per scheduler the pass is bound by the
                         // special-function unit, and a third of the work is what the other pipes absorb for free
                         const bool poly = ((e >> 1) % 3) == 2;
-                        const float x0 = fmaf(__uint_as_float(sreg[c][e]), scale_log2, off), x1 = fmaf(__uint_as_float(sreg[c][e + 1]), scale_log2, off);
-                        const float p0 = poly ? poly_exp2(x0) : fast_exp2(x0), p1 = poly ? poly_exp2(x1) : fast_exp2(x1);
-                        ps[(e >> 1) & 3] += p0 + p1;
-                        sreg[0][c * 16 + e / 2] = __byte_perm(__float_as_uint(p0), __float_as_uint(p1), 0x7632);
+                        const float s0 = __uint_as_float(sreg[c][e]), s1 = __uint_as_float(sreg[c][e + 1]);
+                        const float2 x = make_float2(fmaf(s0, scale_log2, off), fmaf(s1, scale_log2, off));
+                        if (poly) most = max3(most, s0, s1);
+                        const float2 p = poly ? poly_exp2_pair<3>(x) : make_float2(fast_exp2(x.x), fast_exp2(x.y));
+                        ps[(e >> 1) & 3] += p.x + p.y;
+                        sreg[0][c * 16 + e / 2] = __byte_perm(__float_as_uint(p.x), __float_as_uint(p.y), 0x7632);
                     }
                 return (ps[0] + ps[1]) + (ps[2] + ps[3]);
             };
@@ -907,7 +912,7 @@ prefix_body2(const CUtensorMap *pmap_q, const CUtensorMap *pmap_k, const CUtenso
                 // common case: ONE pass against the current reference maximum; S is still intact (P not stored yet),
                 // so a tile with an exponent above the threshold -- or a row's first visible key -- is simply done again
                 tile_sum = exp_in_place();
-                redo = __any_sync(0xffffffffu, !(tile_sum <= kTileSumLimit) || (m_ref == -INFINITY && valid > 0));
+                redo = __any_sync(0xffffffffu, !(tile_sum <= kTileSumLimit) || fmaf(most, scale_log2, -m_ref) > kMostPolyExp2 - 1.f /* room for the bias */ || (m_ref == -INFINITY && valid > 0));
                 if (redo) load_s();
             }
             if (redo) {

@@ -162,22 +162,11 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// 2^x without the special-function unit: x = n + f with n the nearest integer (magic-number rounding) and f in
-// [-0.5, 0.5], a minimax cubic for 2^f (relative error below 7.5e-5, mean error 5e-6), and n added to the exponent bits.
-// Three adds, three FMAs, a maximum and two integer operations: more instructions than one ex2, but on pipes that are
-// idle while the special-function unit, one exponential per score, is the scarce resource of the softmax pass.
-__device__ __forceinline__ float poly_exp2(float x)
+// the largest of three (NaN does not count)
+__device__ __forceinline__ float max3(float a, float b, float c)
 {
-    x = fmaxf(x, -126.f);                        // below that the result is zero for every purpose here
-    const float t = x + 12582912.f;              // 1.5 * 2^23: n lands in the low mantissa bits
-    const float f = x - (t - 12582912.f);
-    float p = fmaf(f, 0.0551716648f, 0.2426111251f);
-    p = fmaf(p, f, 0.6932609677f);
-    p = fmaf(p, f, 0.9999280572f);
-    // at the clamp (masked keys arrive as -inf) the value is a denormal just below 2^-126: a flushing multiply by one
-    // turns it into the exact zero that ex2 returns there
     float r;
-    asm("mul.ftz.f32 %0, %1, 0f3F800000;" : "=f"(r) : "f"(__uint_as_float(__float_as_uint(p) + (__float_as_uint(t) << 23))));
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
 __device__ __forceinline__ float fast_exp2(float x)
@@ -209,25 +198,27 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b)
         : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return r;
 }
-// the largest of three (NaN does not count)
-__device__ __forceinline__ float max3(float a, float b, float c)
-{
-    float r;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-    return r;
-}
-// Of a pair, in fewer instructions, with a polynomial of degree 4 (relative error below 2.7e-6, mean 4e-8) or 5 (1.6e-7, mean 5e-8), for sums
-// that are compared in fp32.  Minimax fits of 2^f over [-0.5, 0.5] in the relative error, rounded to fp32.
-// x must not be above 127: n would run over the exponent's bits, and a large power would read as a small or negative one.
+// 2^x of a pair without the special-function unit: x = n + f with n the nearest integer (magic-number rounding) and f in [-0.5, 0.5], a
+// minimax polynomial for 2^f, and n added to the exponent bits.  More instructions than two ex2, but on pipes that are idle while the
+// special-function unit, one exponential per score, is the scarce resource of a softmax pass.  Degree 3 (relative error below 7.5e-5, mean
+// 5e-6) for weights of 8 bits; degree 4 (2.7e-6, mean 4e-8) or 5 (1.6e-7, mean 5e-8) for sums that are compared in fp32.  Minimax fits over
+// [-0.5, 0.5] in the relative error, rounded to fp32.
+// x must not be above kMostPolyExp2: n would run over the exponent's bits, and a large power would read as a small or negative one.
+constexpr float kMostPolyExp2 = 127.f;
 template <int kDegree>
 __device__ __forceinline__ float2 poly_exp2_pair(float2 x)
 {
     auto both = [](float v) { return make_float2(v, v); };
-    x.x = fmaxf(x.x, -126.f);
+    x.x = fmaxf(x.x, -126.f);                    // below that the result is zero for every purpose here
     x.y = fmaxf(x.y, -126.f);
-    const float2 t = add2(x, both(12582912.f)), n = add2(t, both(-12582912.f)), f = add2(x, make_float2(-n.x, -n.y));
+    const float2 t = add2(x, both(12582912.f));  // 1.5 * 2^23: n lands in the low mantissa bits
+    const float2 n = add2(t, both(-12582912.f)), f = add2(x, make_float2(-n.x, -n.y));
     float2 p;
-    if constexpr (kDegree == 4) {
+    if constexpr (kDegree == 3) {
+        p = fma2(f, both(0.0551716648f), both(0.2426111251f));
+        p = fma2(p, f, both(0.6932609677f));
+        p = fma2(p, f, both(0.9999280572f));
+    } else if constexpr (kDegree == 4) {
         p = fma2(f, both(0.009570102207362652f), both(0.05591785907745361f));
         p = fma2(p, f, both(0.240247443318367f));
         p = fma2(p, f, both(0.6931217908859253f));
@@ -241,7 +232,9 @@ __device__ __forceinline__ float2 poly_exp2_pair(float2 x)
     }
     p.x = __uint_as_float(__float_as_uint(p.x) + (__float_as_uint(t.x) << 23));
     p.y = __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(t.y) << 23));
-    return mul2(p, both(1.f));   // what the clamp left as a denormal becomes 0
+    // at the clamp (masked keys arrive as -inf) the value is a denormal just below 2^-126: a flushing multiply by one turns it into the exact
+    // zero that ex2 returns there
+    return mul2(p, both(1.f));
 }
 
 // ---------------------------------------------------------------- descriptors
