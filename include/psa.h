@@ -547,7 +547,8 @@ psa_status_t psa_store_kv(const void *new_k, const void *new_v, const int64_t kv
  *   scratch        device, 256-byte aligned, psa_attend_paged_scratch_bytes(...) bytes, overwritten by every call (calls that share it
  *                  must be ordered on one stream).
  * What stands in the pages behind a sample's last token does not matter, NaN included.  Within the new tokens V has to be finite
- * where earlier rows are to be: a tile's products are taken with weight 0 for what a row does not see.
+ * where earlier rows are to be: a tile's products are taken with weight 0 for what a row does not see.  A row with a score of NaN or +inf
+ * among the keys it sees is NaN in out and lse, and no other row minds; a score of -inf weighs nothing, a row of nothing else sees nothing.
  * D in {64, 128}, Hq / Hkv in {1, 2, 4, 8}, Hq at most 2^16; pointers 16-byte aligned, strides multiples of 8 elements; at most 2^20
  * samples and 2^24 new tokens.  Outputs do not overlap inputs but as said above.  Weights are rounded to bf16.  Enqueues one or three kernels.
  */
@@ -567,7 +568,7 @@ psa_status_t psa_attend_paged(const void *q, const int64_t q_strides[2], const i
  * [num_pool_pages, Hkv, 16] f32, contiguous, in the order of the pool.  weights_out may be weights.  Cells of other tokens and samples are
  * left as they are, so a page from the free stack needs no clearing.
  *   lse            [num_tokens, Hq] f32: what psa_attend_paged or psa_decode returned for the rows (over all they attended to, a shared
- *                  prompt included); rows with -inf give no weight.
+ *                  prompt included); rows with -inf give no weight.  A NaN row makes NaN of the cells it sees, a NaN key of its own.
  * Scores and sums are fp32, added in a fixed order.  The other arguments, limits and status reports are those of psa_attend_paged.  A page
  * must stand in one sample's list only, and once (psa_attend_paged does not mind shared pages).  Enqueues three kernels.
  */

@@ -863,7 +863,8 @@ prefix_body2(const CUtensorMap *pmap_q, const CUtensorMap *pmap_k, const CUtenso
             // epilogue by trunc_unbias -- carries that factor.  No running maximum either: if every exponent is below the threshold the
             // tile sum is at most 64 * 2^8, so a sum above that bound is what sends the tile to the slow path -- or a score (`most`) whose
             // power a polynomial may give as a small one.  That maximum, three-way, of a third of the scores costs 8192 causal tokens 609 -> 617 us
-            // (taken of the exponents instead 619, polynomials clamped from above 656), the polynomials packed to make room for it.
+            // (taken of the exponents instead 619, polynomials clamped from above 656), the polynomials packed to make room for it; that they keep
+            // NaN 8 more.
             float most = -INFINITY;
             auto exp_in_place = [&]() -> float {
                 const float off = trunc_bias - (m_ref == -INFINITY ? 0.f : m_ref);   // a row that has seen no key yet: exponentiate against 0

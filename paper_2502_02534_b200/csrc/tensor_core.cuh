@@ -162,6 +162,13 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// the larger of two; NaN if one is
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
 // the largest of three (NaN does not count)
 __device__ __forceinline__ float max3(float a, float b, float c)
 {
@@ -191,11 +198,11 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b)
         : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return r;
 }
-__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+__device__ __forceinline__ float2 fma2_ftz(float2 a, float2 b, float2 c)   // denormals count as zeros
 {
     float2 r;
-    asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmul.rn.ftz.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
-        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\tfma.rn.ftz.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
     return r;
 }
 // 2^x of a pair without the special-function unit: x = n + f with n the nearest integer (magic-number rounding) and f in [-0.5, 0.5], a
@@ -203,14 +210,14 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b)
 // special-function unit, one exponential per score, is the scarce resource of a softmax pass.  Degree 3 (relative error below 7.5e-5, mean
 // 5e-6) for weights of 8 bits; degree 4 (2.7e-6, mean 4e-8) or 5 (1.6e-7, mean 5e-8) for sums that are compared in fp32.  Minimax fits over
 // [-0.5, 0.5] in the relative error, rounded to fp32.
-// x must not be above kMostPolyExp2: n would run over the exponent's bits, and a large power would read as a small or negative one.
+// NaN and infinities come out as NaN.  Else x must not be above kMostPolyExp2: n would run over the exponent's bits, and a large power would read as a small or negative one.
 constexpr float kMostPolyExp2 = 127.f;
 template <int kDegree>
 __device__ __forceinline__ float2 poly_exp2_pair(float2 x)
 {
     auto both = [](float v) { return make_float2(v, v); };
-    x.x = fmaxf(x.x, -126.f);                    // below that the result is zero for every purpose here
-    x.y = fmaxf(x.y, -126.f);
+    x.x = max_nan(x.x, -126.f);                  // below that the result is zero for every purpose here
+    x.y = max_nan(x.y, -126.f);
     const float2 t = add2(x, both(12582912.f));  // 1.5 * 2^23: n lands in the low mantissa bits
     const float2 n = add2(t, both(-12582912.f)), f = add2(x, make_float2(-n.x, -n.y));
     float2 p;
@@ -232,9 +239,9 @@ __device__ __forceinline__ float2 poly_exp2_pair(float2 x)
     }
     p.x = __uint_as_float(__float_as_uint(p.x) + (__float_as_uint(t.x) << 23));
     p.y = __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(t.y) << 23));
-    // at the clamp (masked keys arrive as -inf) the value is a denormal just below 2^-126: a flushing multiply by one turns it into the exact
-    // zero that ex2 returns there
-    return mul2(p, both(1.f));
+    // At the clamp (masked keys arrive as -inf) the value is a denormal just below 2^-126: a flushing multiply by one would turn it into the
+    // exact zero that ex2 returns there, and so does a flushing f * 0 + p, which also makes NaN of what the integer add made of a NaN.
+    return fma2_ftz(f, both(0.f), p);
 }
 
 // ---------------------------------------------------------------- descriptors

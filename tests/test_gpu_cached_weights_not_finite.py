@@ -1,0 +1,48 @@
+"""Weights of cached tokens where rows or keys are not finite, and rows that give no weight at all."""
+import numpy as np
+import pytest
+
+from paged_testlib import bf16, case, dev
+from test_gpu_cached_weights import clean, lse_of, run, start, want_of
+
+pytestmark = pytest.mark.gpu
+
+
+def touched(c):
+    t = np.zeros(c["k"].shape[:3], bool)
+    for s, n in enumerate(c["lens"]):
+        if c["q_indptr"][s] < c["q_indptr"][s + 1]:
+            for j in range(int(n)):
+                t[c["indices"][c["indptr"][s] + j // 16], :, j % 16] = True
+    return t
+
+
+@pytest.mark.parametrize("Hq,new", [(8, 1), (8, 3), (8, 40), (1, 300)])
+@pytest.mark.parametrize("what", ["query", "lse", "key", "infinite key"])
+def test_nan(Hq, new, what):
+    """A row of NaN, at every place of 16, spoils the cells that it sees; a key of NaN its own cell."""
+    for at in range(min(new, 16)):
+        c = case(64, Hq, 1, [(700, new), (90, new)], seed=at)
+        lse = lse_of(c)
+        w = clean(c, start(c))
+        w = np.where(np.isnan(w), 0.5, w).astype(np.float32)
+        if what == "query":
+            q = c["q"].copy()
+            q[at, at % Hq, 9] = np.nan
+            c["q_bits"], c["q"] = bf16(q)
+        elif what == "lse":
+            lse[at, at % Hq] = np.nan
+        else:
+            k = c["k"].copy()
+            k[c["indices"][(13 * at) // 16], 0, (13 * at) % 16] = np.nan if what == "key" else np.inf
+            c["k_bits"], c["k"] = bf16(k)
+        with np.errstate(all="ignore"):
+            want = want_of(c, w, lse)
+        got = dev(w)
+        run(c, dev(lse), got)
+        got = got.cpu().numpy()
+        t = touched(c)
+        assert np.array_equal(np.isnan(got[t]), np.isnan(want[t])), (at, np.isnan(got[t]).sum(), np.isnan(want[t]).sum())
+        assert np.array_equal(got[~t], w[~t])
+        ok = t & np.isfinite(want)
+        assert np.allclose(got[ok], want[ok], rtol=2e-5, atol=0)
