@@ -548,7 +548,7 @@ psa_status_t psa_store_kv(const void *new_k, const void *new_v, const int64_t kv
  *                  must be ordered on one stream).
  * What stands in the pages behind a sample's last token does not matter, NaN included.  Within the new tokens V has to be finite
  * where earlier rows are to be: a tile's products are taken with weight 0 for what a row does not see.  A row with a score of NaN or +inf
- * among the keys it sees is NaN in out and lse, and no other row minds; a score of -inf weighs nothing, a row of nothing else sees nothing.
+ * among the keys it sees is NaN in out and lse, whatever it is joined with; no other row minds.  A score of -inf weighs nothing, a row of nothing else sees nothing.
  * D in {64, 128}, Hq / Hkv in {1, 2, 4, 8}, Hq at most 2^16; pointers 16-byte aligned, strides multiples of 8 elements; at most 2^20
  * samples and 2^24 new tokens.  Outputs do not overlap inputs but as said above.  Weights are rounded to bf16.  Enqueues one or three kernels.
  */

@@ -280,7 +280,7 @@ struct Joined { float first, second, lse2; };
 __device__ __forceinline__ Joined join(float a2, float b2)
 {
     const float top = fmaxf(a2, b2);
-    if (top == -INFINITY) return {0.f, 0.f, -INFINITY};
+    if (a2 == -INFINITY && b2 == -INFINITY) return {0.f, 0.f, -INFINITY};   // not where one is NaN, which `top` does not show
     const float wa = exp2f(a2 - top), wb = exp2f(b2 - top), sum = wa + wb;
     return {wa / sum, wb / sum, top + log2f(sum)};
 }

@@ -92,3 +92,20 @@ def test_scores_of_minus_infinity_alone():
     prior, prior_lse = np.ones(c["q"].shape, np.float32), np.zeros(c["q"].shape[:2], np.float32)
     out, lse = attend(c, prior_out=dev(prior), prior_lse=dev(prior_lse))
     assert np.all(out == 1) and np.all(lse == 0)
+
+
+def test_joined_with_a_prior():
+    """A row that is NaN stays so, whether its prior result weighs something or nothing."""
+    c = case(64, 4, 2, [(400, 3), (90, 2), (3000, 2)], seed=6)
+    set_key(c, 0, 290, NAN)
+    set_key(c, 1, 4, INF, 7)
+    set_key(c, 2, 1000, NAN)
+    rng = np.random.default_rng(2)
+    prior, prior_lse = rng.standard_normal(c["q"].shape).astype(np.float32), rng.standard_normal(c["q"].shape[:2]).astype(np.float32) + 5
+    prior_lse[[0, 3, 5]] = -np.inf
+    with np.errstate(all="ignore"):
+        want = reference(c, prior_out=prior, prior_lse=prior_lse)
+    w_out, w_lse, size = want
+    alone = np.isnan(reference(c)[1])
+    w_out[alone] = w_lse[alone] = NAN                # logaddexp(NaN, x) is NaN
+    check(attend(c, prior_out=dev(prior), prior_lse=dev(prior_lse)), (w_out, w_lse, size + np.abs(prior)))
