@@ -216,8 +216,8 @@ template <int kDegree>
 __device__ __forceinline__ float2 poly_exp2_pair(float2 x)
 {
     auto both = [](float v) { return make_float2(v, v); };
-    x.x = max_nan(x.x, -126.f);                  // below that the result is zero for every purpose here
-    x.y = max_nan(x.y, -126.f);
+    x.x = max_nan(x.x, -126.4f);                 // below that the result is zero for every purpose here
+    x.y = max_nan(x.y, -126.4f);
     const float2 t = add2(x, both(12582912.f));  // 1.5 * 2^23: n lands in the low mantissa bits
     const float2 n = add2(t, both(-12582912.f)), f = add2(x, make_float2(-n.x, -n.y));
     float2 p;
@@ -239,8 +239,9 @@ __device__ __forceinline__ float2 poly_exp2_pair(float2 x)
     }
     p.x = __uint_as_float(__float_as_uint(p.x) + (__float_as_uint(t.x) << 23));
     p.y = __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(t.y) << 23));
-    // At the clamp (masked keys arrive as -inf) the value is a denormal just below 2^-126: a flushing multiply by one would turn it into the
-    // exact zero that ex2 returns there, and so does a flushing f * 0 + p, which also makes NaN of what the integer add made of a NaN.
+    // At the clamp (masked keys arrive as -inf) the value is a denormal, 2^-126.4 whichever polynomial it is (at 2^-126 one of them is above
+    // 1 and the value would stay): a flushing multiply by one would turn it into the exact zero that ex2 returns there, and so does a flushing
+    // f * 0 + p, which also makes NaN of what the integer add made of a NaN.
     return fma2_ftz(f, both(0.f), p);
 }
 

@@ -46,3 +46,18 @@ def test_nan(Hq, new, what):
         assert np.array_equal(got[~t], w[~t])
         ok = t & np.isfinite(want)
         assert np.allclose(got[ok], want[ok], rtol=2e-5, atol=0)
+
+
+@pytest.mark.parametrize("new", [1, 16, 40, 200])
+def test_rows_of_no_weight_leave_zeros(new):
+    """lse of -inf for all rows: cells keep their bits, zeros and the smallest numbers among them, and new tokens' become zero."""
+    c = case(128, 8, 1, [(600, new), (30, new)], seed=1)
+    w = np.zeros(c["k"].shape[:3], np.float32)
+    w[:, :, ::3] = 1.5e-38
+    got = dev(w)
+    run(c, dev(np.full(c["q"].shape[:2], -np.inf, np.float32)), got)
+    got = got.cpu().numpy()
+    for s, n in enumerate(c["lens"]):
+        for j in range(int(n)):
+            p = c["indices"][c["indptr"][s] + j // 16]
+            assert got[p, 0, j % 16] == (w[p, 0, j % 16] if j < n - new else 0.0), (s, j)
