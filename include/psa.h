@@ -568,7 +568,8 @@ psa_status_t psa_attend_paged(const void *q, const int64_t q_strides[2], const i
  * [num_pool_pages, Hkv, 16] f32, contiguous, in the order of the pool.  weights_out may be weights.  Cells of other tokens and samples are
  * left as they are, so a page from the free stack needs no clearing.
  *   lse            [num_tokens, Hq] f32: what psa_attend_paged or psa_decode returned for the rows (over all they attended to, a shared
- *                  prompt included); rows with -inf give no weight.  A NaN row makes NaN of the cells it sees, a NaN key of its own.
+ *                  prompt included); rows with -inf give no weight.  A NaN row makes NaN of the cells it sees, a NaN key of its own; weights above
+ *                  2^127, of an lse far below its row's scores, may come out as that much.
  * Scores and sums are fp32, added in a fixed order.  The other arguments, limits and status reports are those of psa_attend_paged.  A page
  * must stand in one sample's list only, and once (psa_attend_paged does not mind shared pages).  Enqueues three kernels.
  */

@@ -468,7 +468,9 @@ weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                                         if (c + i + k + 1 < lo || c + i + k + 1 >= hi) x.y = -INFINITY;
                                     }
                                     // a quarter by polynomial: the special-function unit, an exponential a score, is the bound
-                                    const float2 e = !masked && (i / 2 + k / 2) % 4 == 3 ? poly_exp2_pair<5>(x) : make_float2(fast_exp2(x.x), fast_exp2(x.y));
+                                    const bool poly = !masked && (i / 2 + k / 2) % 4 == 3;
+                                    if (poly) x = make_float2(min_nan(x.x, kMostPolyExp2), min_nan(x.y, kMostPolyExp2));   // an lse may be smaller than it should
+                                    const float2 e = poly ? poly_exp2_pair<5>(x) : make_float2(fast_exp2(x.x), fast_exp2(x.y));
                                     sum[k / 2] = add2(sum[k / 2], e);
                                 }
                             }

@@ -61,3 +61,20 @@ def test_rows_of_no_weight_leave_zeros(new):
         for j in range(int(n)):
             p = c["indices"][c["indptr"][s] + j // 16]
             assert got[p, 0, j % 16] == (w[p, 0, j % 16] if j < n - new else 0.0), (s, j)
+
+
+@pytest.mark.parametrize("nats", [20, 80, 95, 130, 170, 250, 300, 400, 700])
+def test_log_sum_exps_that_are_too_small(nats):
+    """One row's lse so far below its scores, at every place of 16: the cells it sees are large or infinite, never small."""
+    for at in range(16):
+        c = case(64, 8, 1, [(400, 40)], seed=at)
+        lse = lse_of(c)
+        lse[at // 8, at % 8] -= nats
+        w = np.ones(c["k"].shape[:3], np.float32)
+        want = want_of(c, w, lse)
+        got = dev(w)
+        run(c, dev(lse), got)
+        got, t = got.cpu().numpy(), touched(c)
+        sure = t & (want < 2.0 ** 126)
+        assert np.allclose(got[sure], want[sure], rtol=2e-5, atol=0)
+        assert np.all(got[t & (want >= 2.0 ** 126)] >= 2.0 ** 125)
