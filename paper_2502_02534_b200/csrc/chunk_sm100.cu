@@ -139,11 +139,13 @@ chunk_schedule_kernel(ChunkArgs a)
             if (place < a.max_groups) a.groups[place] = g;
             if (place < kKeptCums) cums[place] = g.cum;
         });
+        // q_indptr that runs backwards: more rows than there are.  Counting on would pass 32 bits; a round adds 2^27 at most.
+        if (carry_groups > a.max_groups) break;
     }
     if (my_longest) atomicMax(&longest, my_longest);
     __syncthreads();
     if (threadIdx.x == 0) {
-        if (carry_groups > a.max_groups) {   // q_indptr that runs backwards: more rows than there are
+        if (carry_groups > a.max_groups) {
             raise(a.status, PSA_ERR_BOUNDS);
             carry_groups = 0;
             carry_cost = 0;
