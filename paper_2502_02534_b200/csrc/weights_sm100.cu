@@ -125,9 +125,11 @@ weights_schedule_kernel(WeightsArgs w)
         };
         if (c.diagonal > 0) put(0, c.diagonal, 0);
         for (int p = c.diagonal; p < c.pairs; ++p) put(p, 1, first_tile_of(cs, p, a.group));
+        // q_indptr that runs backwards: more rows than there are.  Counting on would pass 32 bits; a round adds 2^25 at most.
+        if (carry_groups > a.max_groups) break;
     }
     if (threadIdx.x == 0) {
-        if (carry_groups > a.max_groups) {   // q_indptr that runs backwards: more rows than there are
+        if (carry_groups > a.max_groups) {
             raise(a.status, PSA_ERR_BOUNDS);
             carry_groups = 0;
             carry_cost = 0;

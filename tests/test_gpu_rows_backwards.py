@@ -43,3 +43,21 @@ def test_attention():
     attend_paged(q, pool, pool, dev(np.zeros(B + 1, np.int32)), dev(np.zeros(1, np.int32)), dev(np.zeros(B, np.int32)), dev(back_and_forth(B, T)), scratch=scratch,
                  status=status)
     check(whole, nbytes, status)
+
+
+def test_weights():
+    """2.7 billion groups of pairs, all lists of the one page there is."""
+    import torch
+    from paper_2502_02534_b200 import accumulate_weights, library
+    B, T, D = 1 << 20, 5 << 18, 64
+    assert B // 2 * (T // 256) > 1 << 31
+    q = torch.zeros(T, 1, D, dtype=torch.bfloat16, device="cuda")
+    pool = torch.zeros(1, 1, 16, D, dtype=torch.bfloat16, device="cuda")
+    weights = torch.ones(1, 1, 16, device="cuda")
+    nbytes = library().psa_accumulate_weights_scratch_bytes(T, B)
+    whole, scratch = padded_scratch(nbytes)
+    status = dev(np.zeros(1, np.int32))
+    accumulate_weights(q, torch.zeros(T, 1, device="cuda"), pool, dev(back_and_forth(B, T // 16)), dev(np.zeros(T // 16, np.int32)), dev(np.full(B, T, np.int32)),
+                       dev(back_and_forth(B, T)), weights, scratch=scratch, status=status)
+    check(whole, nbytes, status)
+    assert (weights == 1).all()
