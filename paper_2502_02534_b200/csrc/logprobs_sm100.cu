@@ -58,6 +58,8 @@ __device__ __forceinline__ uint32_t ordered(float x)
 __device__ __forceinline__ float from_ordered(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 __device__ __forceinline__ unsigned long long key_of(float x, int token) { return (unsigned long long)ordered(x + 0.f) << 32 | uint32_t(~token); }
 
+constexpr uint32_t kKeyOfNothing = 0x007fffffu;   // ordered(-inf)
+
 // Running sums: l = sum 2^d, s = sum 2^d d, exponents d in log2 units against m, a logit at most 2^8 below the largest (-inf: nothing yet).
 struct Sums { float m, l, s; };
 // ... against another reference, above m or equal
@@ -331,17 +333,27 @@ logprobs_kernel(const LogprobArgs a)
         }
         __syncthreads();
         const int cells = sh.cells_found;
+        // Of masked tokens only those can be among the likeliest that have fewer than a.top others before them.  NaN ones do not count, so
+        // where there are any, and masked tokens are needed, the others are counted.
+        int masked_end = v0 + a.top;
+        if (reached == kKeyOfNothing && sh.block.l != sh.block.l) {
+            masked_end = v0;
+            for (int others = 0; others < a.top && masked_end < v1; masked_end += kThreads) {
+                const int at = masked_end + int(threadIdx.x);
+                const float x = at < v1 ? float(x_row[at]) : -INFINITY;
+                others += __syncthreads_count(at < v1 && x == x);
+            }
+        }
         unsigned long long border = (unsigned long long)reached << 32;      // keys from it on are listed
         for (;;) {
-            const float least = from_ordered(max(uint32_t(border >> 32), 0x007fffffu));     // at least -inf
+            const float least = from_ordered(max(uint32_t(border >> 32), kKeyOfNothing));     // at least -inf
             // `per` consecutive logits from x on, the first of which is token `id`
             auto list = [&](const float *x, int per, int id) {
 #pragma unroll
                 for (int i = 0; i < per; ++i)
                     if (x[i] >= least) {
                         const unsigned long long k = key_of(x[i], id + i);
-                        // of masked tokens only the first can be among the likeliest
-                        if (k >= border && id + i < v1 && (x[i] > -INFINITY || id + i < v0 + a.top)) {
+                        if (k >= border && id + i < v1 && (x[i] > -INFINITY || id + i < masked_end)) {
                             const int place = atomicAdd(&sh.count, 1);
                             if (place < kList) sh.list[place] = k;
                         }
