@@ -19,6 +19,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <string>
 
 #include "psa_internal.h"
@@ -263,7 +264,7 @@ logprobs_kernel(const LogprobArgs a)
                 sum.l *= r;
             }
             sum.m = top_here;
-            limit = top_here + 8.f / c;
+            limit = fminf(top_here + 8.f / c, FLT_MAX);    // which a logit of +inf passes whatever the temperature
         }
         const float off = sum.m == -INFINITY ? 0.f : -sum.m;
         float2 l = {0.f, 0.f}, s = {0.f, 0.f};
