@@ -596,7 +596,8 @@ psa_status_t psa_accumulate_weights(const void *q, const int64_t q_strides[2], c
  *                     a page id outside the pool weighs less than any other and is pushed as -1; if the stack has no room for all that
  *                     would leave (or its height is out of range), nothing leaves.
  *   scratch           device, 16-byte aligned, psa_evict_pages_scratch_bytes(B, num_entries) bytes, as above.
- * Pages must belong to one list only.  The cache may be of either kind (ids are shared).  Enqueues two kernels.
+ * Outputs overlap no inputs and one another (refused) but as said.  Pages must belong to one list only.  The cache may be of either kind
+ * (ids are shared).  Enqueues two kernels, or one where nothing but the lists is updated in place and there are few samples.
  */
 size_t psa_evict_pages_scratch_bytes(int32_t num_samples, int64_t num_entries);
 psa_status_t psa_evict_pages(const float *weights, int64_t num_pool_pages, int32_t num_kv_heads, const int32_t *page_indptr,

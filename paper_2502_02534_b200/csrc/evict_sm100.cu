@@ -330,6 +330,27 @@ size_t layout(EvictArgs &a, void *scratch)
     return off;
 }
 
+// Whether an output lies over an input or another output, but for the three that may be updated in place.
+bool overlapping(const EvictArgs &a)
+{
+    struct Range { const void *p; int64_t bytes; };
+    const int64_t lens = 4 * int64_t(a.num_samples), list = 4 * a.num_entries;
+    const Range in[] = {{a.page_indices, list}, {a.kv_lens, lens}, {a.free_count, 4}, {a.budgets, lens}, {a.page_indptr, lens + 4},
+                        {a.weights, 4 * int64_t(a.num_pool_pages) * a.cells}};
+    const Range out[] = {{a.indices_out, list}, {a.lens_out, lens}, {a.free_count_out, 4}, {a.free_pages, 4 * a.free_capacity}};
+    auto meet = [](const Range &x, const Range &y) {
+        const uintptr_t u = reinterpret_cast<uintptr_t>(x.p), v = reinterpret_cast<uintptr_t>(y.p);
+        return x.p && y.p && x.bytes > 0 && y.bytes > 0 && u < v + uintptr_t(y.bytes) && v < u + uintptr_t(x.bytes);
+    };
+    for (int o = 0; o < 4; ++o) {
+        for (int i = 0; i < 6; ++i)
+            if (meet(out[o], in[i]) && !(o == i && o < 3 && out[o].p == in[i].p)) return true;
+        for (int p = 0; p < o; ++p)
+            if (meet(out[o], out[p])) return true;
+    }
+    return false;
+}
+
 }  // namespace
 }  // namespace psa
 
@@ -365,6 +386,7 @@ extern "C" psa_status_t psa_evict_pages(const float *weights, int64_t num_pool_p
     a.free_count = free_count; a.indices_out = page_indices_out; a.lens_out = lens_out; a.free_pages = free_pages;
     a.free_count_out = free_count_out; a.status = status; a.num_entries = num_entries; a.free_capacity = free_capacity;
     a.num_samples = num_samples; a.recent = recent; a.num_pool_pages = int32_t(num_pool_pages); a.cells = num_kv_heads * kPageSize;
+    if (overlapping(a)) return set_last_error(PSA_ERR_INVALID_ARG, "outputs must not overlap inputs or one another, but for the three updated in place");
     layout(a, scratch);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     cudaError_t e;
