@@ -137,7 +137,8 @@ merge_kernel(const SampleInfo *__restrict__ sample_info, const int32_t *__restri
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) gmax = fmaxf(gmax, __shfl_xor_sync(0xffffffffu, gmax, o));
                 const float new_top = fmaxf(top, gmax);
-                if (new_top != -INFINITY) {
+                // `top` does not show NaN pieces; where all are (or empty), what follows makes NaN of everything
+                if (new_top != -INFINITY || __any_sync(0xffffffffu, my_lse != my_lse)) {
                     const float scale = __expf(top - new_top);   // 0 when nothing was accumulated yet
 #pragma unroll
                     for (int v = 0; v < V; ++v) acc[v] *= scale;
@@ -159,7 +160,7 @@ merge_kernel(const SampleInfo *__restrict__ sample_info, const int32_t *__restri
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
-    if (top != -INFINITY) {
+    if (z != 0.f) {
         const float inv = 1.f / z;
 #pragma unroll
         for (int v = 0; v < V; ++v) acc[v] *= inv;
@@ -182,7 +183,7 @@ merge_kernel(const SampleInfo *__restrict__ sample_info, const int32_t *__restri
             *reinterpret_cast<__nv_bfloat162 *>(dst) = lo;
         }
     }
-    if (lane == 0) lse_out[row] = (top == -INFINITY) ? -INFINITY : top + logf(z);
+    if (lane == 0) lse_out[row] = (z == 0.f) ? -INFINITY : top + logf(z);
 }
 
 }  // namespace

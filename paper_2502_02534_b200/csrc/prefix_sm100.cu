@@ -512,7 +512,7 @@ prefix_body(const CUtensorMap *pmap_q, const CUtensorMap *pmap_k, const CUtensor
         float *stage = reinterpret_cast<float *>(smem + L::kRingOff + t * L::kStageBytes);
         if (ok) {
             tc_fence_after();
-            const float inv = l_sum > 0.f ? 1.f / l_sum : 0.f;   // a row that saw no key in this item: O = 0, lse = -inf
+            const float inv = l_sum != 0.f ? 1.f / l_sum : 0.f;   // a row that saw no key in this item: O = 0, lse = -inf; NaN stays
             float *mine = stage + row * L::kStageRowFloats;
 #pragma unroll 1
             for (int c = 0; c < D / 32; ++c) {
@@ -526,7 +526,7 @@ prefix_body(const CUtensorMap *pmap_q, const CUtensorMap *pmap_k, const CUtensor
                                     __uint_as_float(oreg[i + 2]) * inv, __uint_as_float(oreg[i + 3]) * inv);
             }
             const int r = t * kPrefixTileRows + row;
-            if (r < n_rows) partial_lse[prow0 + r] = l_sum > 0.f ? (m_ref + log2f(l_sum)) * 0.6931471805599453f : -INFINITY;
+            if (r < n_rows) partial_lse[prow0 + r] = l_sum != 0.f ? (m_ref + log2f(l_sum)) * 0.6931471805599453f : -INFINITY;
         }
         // the four warps of this row tile meet (named barrier 1 + t), then write rows round-robin
         asm volatile("bar.sync %0, 128;" ::"r"(1 + t) : "memory");
@@ -946,7 +946,7 @@ prefix_body2(const CUtensorMap *pmap_q, const CUtensorMap *pmap_k, const CUtenso
             float *mine = stage + row * L::kStageRowFloats;
             if constexpr (!kPing) {
                 if (ok) {
-                    const float inv = l_sum > 0.f ? 1.f / l_sum : 0.f;   // a row that saw no key in this item: O = 0, lse = -inf
+                    const float inv = l_sum != 0.f ? 1.f / l_sum : 0.f;   // a row that saw no key in this item: O = 0, lse = -inf; NaN stays
 #pragma unroll 1
                     for (int c = 0; c < D / 32; ++c) {
                         uint32_t oreg[32];
@@ -959,7 +959,7 @@ prefix_body2(const CUtensorMap *pmap_q, const CUtensorMap *pmap_k, const CUtenso
                                             __uint_as_float(oreg[e + 2]) * inv, __uint_as_float(oreg[e + 3]) * inv);
                     }
                     const int r = t * kPrefixTileRows + row;
-                    if (r < n_rows) partial_lse[prow0 + r] = l_sum > 0.f ? (m_ref + log2f(l_sum)) * 0.6931471805599453f : -INFINITY;
+                    if (r < n_rows) partial_lse[prow0 + r] = l_sum != 0.f ? (m_ref + log2f(l_sum)) * 0.6931471805599453f : -INFINITY;
                 }
                 asm volatile("bar.sync %0, 128;" ::"r"(1 + t) : "memory");   // the four warps of this row tile
             } else {
@@ -976,7 +976,7 @@ prefix_body2(const CUtensorMap *pmap_q, const CUtensorMap *pmap_k, const CUtenso
                 const float top = fmaxf(m0, m1);
                 const float a0 = m0 == -INFINITY ? 0.f : fast_exp2(m0 - top), a1 = m1 == -INFINITY ? 0.f : fast_exp2(m1 - top);
                 const float l = a0 * l0 + a1 * l1;
-                const float inv = l > 0.f ? 1.f / l : 0.f;
+                const float inv = l != 0.f ? 1.f / l : 0.f;
                 const bool have1 = n_streams > 1;    // otherwise O_1 was never written
                 if (ok) {
                     const uint32_t o0 = tmem_base + lane_addr + kColO, o1 = o0 + D;
@@ -998,7 +998,7 @@ prefix_body2(const CUtensorMap *pmap_q, const CUtensorMap *pmap_k, const CUtenso
                             *reinterpret_cast<float4 *>(mine + c * 32 + e) = make_float4(v[0], v[1], v[2], v[3]);
                         }
                     }
-                    if (t == 0 && row < n_rows) partial_lse[prow0 + row] = l > 0.f ? (top + log2f(l)) * 0.6931471805599453f : -INFINITY;
+                    if (t == 0 && row < n_rows) partial_lse[prow0 + row] = l != 0.f ? (top + log2f(l)) * 0.6931471805599453f : -INFINITY;
                 }
                 asm volatile("bar.sync 1, 256;" ::: "memory");
             }
