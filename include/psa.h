@@ -548,7 +548,8 @@ psa_status_t psa_store_kv(const void *new_k, const void *new_v, const int64_t kv
  *                  must be ordered on one stream).
  * What stands in the pages behind a sample's last token does not matter, NaN included.  Within the new tokens V has to be finite
  * where earlier rows are to be: a tile's products are taken with weight 0 for what a row does not see.  A row with a score of NaN or +inf
- * among the keys it sees is NaN in out and lse, whatever it is joined with; no other row minds.  A score of -inf weighs nothing, a row of nothing else sees nothing.
+ * among the keys it sees is NaN in out and lse, whatever it is joined with; no other row minds.  A score of -inf weighs nothing, and a row
+ * of nothing else is as one that sees nothing.
  * D in {64, 128}, Hq / Hkv in {1, 2, 4, 8}, Hq at most 2^16; pointers 16-byte aligned, strides multiples of 8 elements; at most 2^20
  * samples and 2^24 new tokens.  Outputs do not overlap inputs but as said above.  Weights are rounded to bf16.  Enqueues one or three kernels.
  */
@@ -571,7 +572,9 @@ psa_status_t psa_attend_paged(const void *q, const int64_t q_strides[2], const i
  *                  prompt included); rows with -inf give no weight.  A NaN row makes NaN of the cells it sees, a NaN key of its own; weights above
  *                  2^127, of an lse far below its row's scores, may come out as that much.
  * Scores and sums are fp32, added in a fixed order.  The other arguments, limits and status reports are those of psa_attend_paged.  A page
- * must stand in one sample's list only, and once (psa_attend_paged does not mind shared pages).  Enqueues three kernels.
+ * must stand in one sample's list only, and once (psa_attend_paged does not mind shared pages).  A cell is cleared by the call in which its
+ * token is new, so every token has to be new in one.  K is read in bf16 only: a 4-bit cache's weights have to come from elsewhere.
+ * Enqueues three kernels.
  */
 size_t psa_accumulate_weights_scratch_bytes(int64_t num_tokens, int32_t num_samples);
 psa_status_t psa_accumulate_weights(const void *q, const int64_t q_strides[2], const int32_t *q_indptr, int64_t num_tokens, int32_t num_samples,
@@ -582,7 +585,7 @@ psa_status_t psa_accumulate_weights(const void *q, const int64_t q_strides[2], c
 
 /*
  * Pages that leave a cache which has grown beyond its budget, chosen by the weights above.  A page weighs as much as its heaviest cell
- * (max over KV heads and its 16 slots; NaN cells do not count, a page of nothing else weighs less than any).  Sample s holds
+ * (max over KV heads and its 16 slots; NaN cells do not count, a page of nothing else weighs -inf).  Sample s holds
  * P = ceil(kv_lens[s] / 16) pages; if P > budgets[s], its min(recent, budgets[s]) newest pages stay and of the others the heaviest, so that
  * budgets[s] >= 1 are left (of equal weights the older page stays).  The list closes up in order -- K and V do not move --, entries
  * budgets[s] .. P - 1 become -1, the length drops by 16 a page (the newest page, the only one that may be part full, stays: recent >= 1), and
@@ -590,7 +593,8 @@ psa_status_t psa_accumulate_weights(const void *q, const int64_t q_strides[2], c
  * free_pages[*free_count .. *free_count_out).
  *   weights           [num_pool_pages, Hkv, 16] f32 device, 16-byte aligned;  budgets [B] int32 device, pages.
  *   free_pages        int32 device, in/out, room for free_capacity ids.
- *   page_indices_out  [num_entries] int32 device: all of page_indices with the lists changed; may be page_indices.
+ *   page_indices_out  [num_entries] int32 device: all of page_indices with the lists changed; may be page_indices.  (Elsewhere, a list whose
+ *                     ends in page_indptr descend or lie outside is not copied; PSA_ERR_BOUNDS.)
  *   lens_out          [B] int32 device or NULL; may be kv_lens.   free_count_out  may be free_count.
  *   status            receives PSA_ERR_BOUNDS: a sample with a negative length or one beyond its list, or a budget below 1, is left as it is;
  *                     a page id outside the pool weighs less than any other and is pushed as -1; if the stack has no room for all that

@@ -8,9 +8,10 @@
 // block runs it for itself, from all samples' lengths and budgets; otherwise, and for many samples, evict_plan_kernel (one block) does so
 // before.  evict_kernel has a block per sample: weights are read once (all of the bytes that matter) by whole warps, one redux a page, and
 // kept as ordered 32-bit keys in shared memory.  The border between what stays and goes: up to 512 pages bit by bit with a block-wide count
-// (20 barriers or so), else by four histograms of 8 bits.  One scan closes up the list.  8 samples x 512 tokens 5.8 us (two launches and
-// histograms alone 10.3); 256 samples of up to 8192 tokens, 33.5 MB, 15.8 us (8 lanes-a-page loops 26, floor 5.1): the chain of dependent
-// steps of the longest samples' blocks, behind a launch.
+// (20 barriers or so), else by four histograms of 8 bits.  One scan closes up the list.  8 samples x 512 tokens 6.3 us (two launches and
+// histograms alone 10.3); 256 samples of up to 8192 tokens, 33.5 MB, 14.9 us (8 lanes-a-page loops 26, floor 5.1): latency and uneven
+// blocks.  A warp waits for memory in five of the cycles between two of its instructions, 22 % of the issue slots are taken, and an SM is
+// busy 22 k cycles on average, 30 k at most.
 #include <cuda_runtime.h>
 
 #include <algorithm>

@@ -12,8 +12,11 @@
 // reaches the border is listed.
 // A (logit, token) pair is ordered by a 64-bit key, equal logits by the lower token, so nothing depends on who comes first.  A list that
 // is too short (many equal logits) gives a higher border, its own k-th largest, and is made again.  256 rows x 131072 bf16, k = 20:
-// listing inside the pass, with a border kept by the block 64 us, by each warp 164 us; all tiles read again 31 us; this way 21.7 us, of which
-// 5 are the tail, and 16.9 us without likeliest tokens (floor 10.3).
+// listing inside the pass, with a border kept by the block 64 us, by each warp 164 us; all tiles read again 31 us; this way 22 us, of which
+// 5 are the tail, and 16.9 us without likeliest tokens (floor 10.3).  256 rows x 131072 f32 24.8 us (floor 20.5).
+// What bounds it: 24 instructions a pair of logits and warp, selection included, are 11 us of all issue slots (58 % of them taken with four
+// rows an SM, special-function units 43 %); the rest is the begin and the end, when SMs have nothing to do (23 % of the time with 256 rows), and
+// 256 rows on 148 SMs (the busiest SM 1.11 of the mean).
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -497,7 +500,8 @@ extern "C" psa_status_t psa_token_logprobs(const void *logits, int32_t logits_dt
     a.logits = logits; a.stride = row_stride; a.vocab = vocab; a.tokens = tokens; a.temperature = temperature;
     a.logprobs = logprobs; a.entropy = entropy; a.top_ids = top_ids; a.top_logprobs = top_logprobs; a.top_stride = top_stride;
     a.top = top_ids || top_logprobs ? top : 0;
-    // blocks of a row: as many as keep the SMs (two blocks each) busy, with a tile of work for every one
+    // Blocks of a row: doubled while all of them still have an SM of the 148 each, and a tile of work.  x 131072 bf16, 20 likeliest: 8, 19, 38,
+    // 74, 76, 148, 256 rows 9.5, 9.7, 11.7, 12.5, 14.8, 15.7, 21.5 us; with two blocks an SM 9.4, 10.9, 11.4, 17.7, 14.7, 16.2, 21.6.
     int blocks = 1;
     while (blocks < kMostCluster && int64_t(num_rows) * blocks * 2 <= 148 && int64_t(vocab) > int64_t(kTile) * blocks) blocks *= 2;
     a.segment = int32_t(((int64_t(vocab) + blocks - 1) / blocks + 7) / 8 * 8);

@@ -15,7 +15,9 @@
 // Every wait is bounded.
 //
 // 64 samples x 1 token over U[0,4096], 8 heads (268 MB of K): 55.5 us, 4.8 TB/s (one TMA warp for both key tiles 66); launch, schedule and
-// merge are 10 of them.  2048 tokens over 8192, 32 / 8 heads, 604 M exponentials, a quarter by polynomial: 180 us; the special-function units'
+// merge are 10 of them.  17 to 127 rows take the products and sums of 128: 64 x 4 tokens, 64 / 8 heads, 78 us (64 x 16, 128 rows, 65).
+// 2048 tokens over 8192, 32 / 8 heads, 604 M exponentials, a quarter by polynomial: 185 us (before NaN and large exponents were kept 180, to
+// which the following compare); the special-function units'
 // share is 100 us, the products 111 (two warpgroups 229 us; log-sum-exps loaded when needed 216; masked rows unrolled beside the whole ones,
 // which is too much code, 205).  No polynomials 196, three eighths 181, half 208, a score buffer let go
 // before its last 16 columns are summed 185; row tiles of 64 with four buffers 252, an issuer for each key
