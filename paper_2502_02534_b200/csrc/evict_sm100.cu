@@ -10,8 +10,8 @@
 // kept as ordered 32-bit keys in shared memory.  The border between what stays and goes: up to 512 pages bit by bit with a block-wide count
 // (20 barriers or so), else by four histograms of 8 bits.  One scan closes up the list.  8 samples x 512 tokens 6.3 us (two launches and
 // histograms alone 10.3); 256 samples of up to 8192 tokens, 33.5 MB, 14.9 us (8 lanes-a-page loops 26, floor 5.1): latency and uneven
-// blocks.  A warp waits for memory in five of the cycles between two of its instructions, 22 % of the issue slots are taken, and an SM is
-// busy 22 k cycles on average, 30 k at most.
+// blocks.  Five warps wait for memory for every instruction that is issued, 22 % of the issue slots are taken, and an SM is busy 22 k
+// cycles on average, 30 k at most.
 #include <cuda_runtime.h>
 
 #include <algorithm>

@@ -913,7 +913,8 @@ prefix_body2(const CUtensorMap *pmap_q, const CUtensorMap *pmap_k, const CUtenso
                 // common case: ONE pass against the current reference maximum; S is still intact (P not stored yet),
                 // so a tile with an exponent above the threshold -- or a row's first visible key -- is simply done again
                 tile_sum = exp_in_place();
-                redo = __any_sync(0xffffffffu, !(tile_sum <= kTileSumLimit) || fmaf(most, scale_log2, -m_ref) > kMostPolyExp2 - 1.f /* room for the bias */ || (m_ref == -INFINITY && valid > 0));
+                const bool beyond = fmaf(most, scale_log2, -m_ref) > kMostPolyExp2 - 1.f;   // less 1: room for the bias
+                redo = __any_sync(0xffffffffu, !(tile_sum <= kTileSumLimit) || beyond || (m_ref == -INFINITY && valid > 0));
                 if (redo) load_s();
             }
             if (redo) {

@@ -216,7 +216,8 @@ __device__ __forceinline__ float2 fma2_ftz(float2 a, float2 b, float2 c)   // de
 // special-function unit, one exponential per score, is the scarce resource of a softmax pass.  Degree 3 (relative error below 7.5e-5, mean
 // 5e-6) for weights of 8 bits; degree 4 (2.7e-6, mean 4e-8) or 5 (1.6e-7, mean 5e-8) for sums that are compared in fp32.  Minimax fits over
 // [-0.5, 0.5] in the relative error, rounded to fp32.
-// NaN and infinities come out as NaN.  Else x must not be above kMostPolyExp2: n would run over the exponent's bits, and a large power would read as a small or negative one.
+// NaN and +inf come out as NaN.  A finite x must not be above kMostPolyExp2: n would run over the exponent's bits, and a large power would
+// read as a small or negative one.
 constexpr float kMostPolyExp2 = 127.f;
 template <int kDegree>
 __device__ __forceinline__ float2 poly_exp2_pair(float2 x)
